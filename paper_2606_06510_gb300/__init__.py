@@ -15,6 +15,10 @@ import os
 
 import torch
 
+from . import layers
+from .layers import (AdamWPlan, oz2_adamw, oz2_adamw_plan, oz2_adamw_states, oz2_linear,  # noqa: F401
+                     oz2_linear_grad)
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liboz2.so")
 
@@ -82,6 +86,7 @@ _SIGS = {
     "oz2_reconstruct": (_I, [_I64, _I64, _I, _P, _I64, _P, _P, _P, _I64, _P]),
     "oz2_fallback": (_I, [_I64, _I64, _I64, _P, _I64, _P, _I64, _P, _P, _P, _I64, _P]),
     "oz2_native_dgemm": (_I, [_I64, _I64, _I64, _P, _I64, _P, _I64, _P, _I64, _P]),
+    **layers.SIGS,
 }
 _LIB = None
 

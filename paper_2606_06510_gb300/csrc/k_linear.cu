@@ -1,0 +1,520 @@
+// The products of a linear layer and of its gradient: D = epilogue(P·Qᵀ) on
+// tcgen05 (16-bit types by kind::f16, E4M3 by kind::f8f6f4), FP32 sums.
+//
+//   forward   Y = act(X·Wᵀ·scales + b) + R   P = X, Q = W, both K-major
+//   gradient  dX = dZ·W                      P = dZ K-major, Q = W MN-major
+//             dW = dZᵀ·X                     both MN-major
+//
+// An operand tile is 128 rows × 128 bytes of depth in K-major storage (rows of
+// 128 bytes), or 64 depth rows × two 64-element row blocks in MN-major storage;
+// both land in shared memory with the 128-byte swizzle, and the descriptor and
+// the instruction's transpose bits tell them apart.
+#include <algorithm>
+
+#include "lin_common.cuh"
+
+namespace oz2 {
+namespace {
+
+constexpr int kLinThreads = 320;      // TMA warp, MMA warp, 8 epilogue warps
+constexpr int kLinStages = 5;
+constexpr int kLinEpiWarps = 8;
+constexpr int kLinTile = 256;         // rows and columns of a CTA pair's tile
+constexpr int kLinStage = 2 * kTileBytes;
+constexpr int kStageBytes = 32 * 128; // an epilogue warp's 32 rows × 128 bytes
+constexpr int kLinCols = 128;         // columns of an epilogue warp
+constexpr int kLinSmem = 1024 + kLinStages * kLinStage + kLinEpiWarps * (kStageBytes + 2 * 4 * kLinCols) + 256;
+
+struct LinUnits {                     // one product of a launch
+  int64_t rows, cols;
+  int64_t ntm, ntn, units;
+  int64_t steps;                      // of 128 bytes of depth
+  uint32_t idesc;
+  uint32_t p_mn, q_mn;
+  LinEpilogue ep;
+};
+struct LinLaunch {
+  int count;
+  int64_t units;
+  LinUnits u[kMaxProducts];
+};
+struct LinMaps {
+  CUtensorMap p[kMaxProducts], q[kMaxProducts];
+};
+
+// Instruction descriptor of kind::f16 with FP32 sums: D = F32 (bits 4-5 = 1), A
+// and B BF16 (1) or F16 (0) in bits 7-9 and 10-12, MN-major A and B in bits 15
+// and 16, N >> 3 in 17-22, M >> 4 in 24-28.
+constexpr uint32_t idesc_16(int M, int N, bool bf16, bool a_mn, bool b_mn) {
+  return (1u << 4) | (bf16 ? 1u << 7 | 1u << 10 : 0u) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) |
+         (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
+}
+
+// The descriptor of a tile in MN-major storage: 64-element (128-byte) row
+// blocks kTileBytes/2 apart (leading byte offset), groups of 8 depth rows 1024
+// bytes apart (stride byte offset), 128-byte swizzle.
+__device__ __forceinline__ uint64_t smem_desc_mn(uint32_t saddr) {
+  return (smem_desc_sw128(saddr) & ~(0x3FFFull << 16)) | (static_cast<uint64_t>(kTileBytes / 2 >> 4) << 16);
+}
+
+template <bool F8>
+__device__ __forceinline__ void mma_pair(uint32_t me, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                         uint32_t accumulate) {
+  if (F8) {
+    mma_f8_pair(me, d_tmem, a_desc, b_desc, idesc, accumulate);
+  } else {
+    asm volatile(
+        "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
+        " @q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(me)
+        : "memory");
+  }
+}
+
+// Tile (tm, tn) of unit u: bands of 8 tile rows, so that the tiles in flight
+// share operand rows in L2.
+__device__ __forceinline__ void unit_tile(const LinUnits& x, int64_t u, int64_t* tm, int64_t* tn) {
+  const int64_t per = 8 * x.ntn, band = u / per, in = u - band * per;
+  const int64_t h = min(static_cast<int64_t>(8), x.ntm - band * 8);
+  *tn = in / h;
+  *tm = band * 8 + (in - *tn * h);
+}
+
+// --- an epilogue warp's 32 rows × 128 bytes in shared memory --------------------
+// 16-byte piece c of row r at r·128 + (c ^ (r & 7))·16: a thread's own row and
+// eight threads' one row are both free of bank conflicts.
+__device__ __forceinline__ uint32_t piece_at(int row, int c) { return row * 128 + ((c ^ (row & 7)) << 4); }
+
+__device__ __forceinline__ uint4 lds128(const uint8_t* p) { return *reinterpret_cast<const uint4*>(p); }
+__device__ __forceinline__ void sts128(uint8_t* p, uint4 v) { *reinterpret_cast<uint4*>(p) = v; }
+
+// Rows row0.. and columns col0.. (64 of 16 bits) between global and shared memory, a
+// whole warp; what lies past the matrix is not touched.
+__device__ __forceinline__ bool vec_ok(const void* p, int64_t ld, int bytes) {
+  return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(ld * bytes)) & 15) == 0;
+}
+__device__ __forceinline__ void fetch16(const LinUnits& x, const void* src, int64_t ld, int64_t row0, int64_t col0,
+                                        int lane, uint8_t* buf) {
+  const uint16_t* s = static_cast<const uint16_t*>(src);
+  if (vec_ok(src, ld, 2) && col0 + 64 <= x.cols) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = 4 * i + (lane >> 3), c = lane & 7;
+      if (row0 + r < x.rows)
+        sts128(buf + piece_at(r, c), __ldg(reinterpret_cast<const uint4*>(s + (row0 + r) * ld + col0 + 8 * c)));
+    }
+  } else {
+    for (int r = 0; r < 32 && row0 + r < x.rows; ++r)
+#pragma unroll
+      for (int e = lane; e < 64; e += 32)
+        if (col0 + e < x.cols)
+          *reinterpret_cast<uint16_t*>(buf + piece_at(r, e >> 3) + 2 * (e & 7)) = __ldg(s + (row0 + r) * ld + col0 + e);
+  }
+}
+__device__ __forceinline__ void store16(const LinUnits& x, void* dst, int64_t ld, int64_t row0, int64_t col0, int lane,
+                                        const uint8_t* buf) {
+  uint16_t* d = static_cast<uint16_t*>(dst);
+  if (vec_ok(dst, ld, 2) && col0 + 64 <= x.cols) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = 4 * i + (lane >> 3), c = lane & 7;
+      if (row0 + r < x.rows)
+        *reinterpret_cast<uint4*>(d + (row0 + r) * ld + col0 + 8 * c) = lds128(buf + piece_at(r, c));
+    }
+  } else {
+    for (int r = 0; r < 32 && row0 + r < x.rows; ++r)
+#pragma unroll
+      for (int e = lane; e < 64; e += 32)
+        if (col0 + e < x.cols)
+          d[(row0 + r) * ld + col0 + e] = *reinterpret_cast<const uint16_t*>(buf + piece_at(r, e >> 3) + 2 * (e & 7));
+  }
+}
+// 32 columns of FP32, stored or added to.
+__device__ __forceinline__ void store32(const LinUnits& x, void* dst, int64_t ld, int64_t row0, int64_t col0, int lane,
+                                        const uint8_t* buf, bool add) {
+  float* d = static_cast<float*>(dst);
+  for (int r = 0; r < 32 && row0 + r < x.rows; ++r) {
+    if (col0 + lane < x.cols) {
+      float* at = d + (row0 + r) * ld + col0 + lane;
+      const float v = *reinterpret_cast<const float*>(buf + piece_at(r, lane >> 2) + 4 * (lane & 3));
+      *at = add ? *at + v : v;
+    }
+  }
+}
+
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
+        "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]),
+        "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+      : "r"(taddr));
+}
+
+// 32 sums of one row (columns c.. of the warp's) with their scales and biases.
+__device__ __forceinline__ void scaled(const float* scale_s, const float* bias_s, float row_scale, const uint32_t (&v)[32],
+                                       int c, bool scales, float (&z)[32]) {
+#pragma unroll
+  for (int j = 0; j < 32; j += 4) {
+    const float4 b = *reinterpret_cast<const float4*>(bias_s + c + j);
+    z[j] = __uint_as_float(v[j]);
+    z[j + 1] = __uint_as_float(v[j + 1]);
+    z[j + 2] = __uint_as_float(v[j + 2]);
+    z[j + 3] = __uint_as_float(v[j + 3]);
+    if (scales) {
+      const float4 s = *reinterpret_cast<const float4*>(scale_s + c + j);
+      z[j] *= row_scale * s.x;
+      z[j + 1] *= row_scale * s.y;
+      z[j + 2] *= row_scale * s.z;
+      z[j + 3] *= row_scale * s.w;
+    }
+    z[j] += b.x;
+    z[j + 1] += b.y;
+    z[j + 2] += b.z;
+    z[j + 3] += b.w;
+  }
+}
+
+// act(z) + r for 32 columns, into the warp's buffer (which holds r there).
+template <int ACT>
+__device__ __forceinline__ void finish32(const float (&z)[32], bool add, bool bf16, uint8_t* buf, int lane, int c) {
+#pragma unroll
+  for (int j = 0; j < 32; j += 8) {
+    uint8_t* at = buf + piece_at(lane, (c + j) >> 3);
+    float y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = activate<ACT>(z[j + e]);
+    if (add) {
+      const uint4 r = lds128(at);
+      const uint32_t rw[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 f = unpack16(rw[e], bf16);
+        y[2 * e] += f.x;
+        y[2 * e + 1] += f.y;
+      }
+    }
+    sts128(at, make_uint4(pack16(y[0], y[1], bf16), pack16(y[2], y[3], bf16), pack16(y[4], y[5], bf16),
+                          pack16(y[6], y[7], bf16)));
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Tiles of 256 × 256 on CTA pairs (cta_group::2: each CTA stages 128 rows of P
+// and 128 of Q), persistent, two accumulators in tensor memory so that a
+// tile's epilogue runs beside the next tile's products.
+// ---------------------------------------------------------------------------
+template <bool F8>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
+    linear_pair_kernel(const __grid_constant__ LinMaps maps, const __grid_constant__ LinLaunch L, Oz2Device* dev) {
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* epi = smem + kLinStages * kLinStage;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(epi + kLinEpiWarps * (kStageBytes + 2 * 4 * kLinCols));
+  // bars: full[S], empty[S], acc_full[2], acc_empty[2], drain
+  __shared__ uint32_t tmem_base_s;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const bool leader = rank == 0;
+  const int64_t pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
+  const uint32_t full0 = smem_u32(bars), empty0 = smem_u32(bars + kLinStages);
+  const uint32_t acc_full = smem_u32(bars + 2 * kLinStages), acc_empty = smem_u32(bars + 2 * kLinStages + 2);
+  const uint32_t drain_bar = smem_u32(bars + 2 * kLinStages + 4);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kLinStages; ++s) {
+      mbar_init(full0 + 8 * s, 1);
+      mbar_init(empty0 + 8 * s, 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(acc_full + 8 * a, 1);
+      mbar_init(acc_empty + 8 * a, 2 * kLinEpiWarps);
+    }
+    mbar_init(drain_bar, 1);
+    fence_barrier_init();
+  }
+  if (warp == 1) {
+    tmem_alloc_pair(smem_u32(&tmem_base_s), 512);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem = tmem_base_s;
+  bool ok = true;
+  pdl_wait();  // the operands are written; the set-up above overlaps that kernel's tail
+
+  // Product and tile of the pair's unit u.
+  auto locate = [&](int64_t u, int64_t* tm, int64_t* tn) {
+    int i = 0;
+    if (L.count > 1 && u >= L.u[0].units) {
+      u -= L.u[0].units;
+      i = 1;
+    }
+    unit_tile(L.u[i], u, tm, tn);
+    return i;
+  };
+
+  if (warp == 0) {
+    // ---------------- TMA producer (both CTAs) ----------------
+    if (lane == 0) {
+      const uint32_t full_leader0 = mapa_shared(full0, 0);
+      uint32_t it = 0, s = 0, ph = 1;
+      for (int64_t u = pair; u < L.units && ok; u += npairs) {
+        int64_t tm, tn;
+        const int i = locate(u, &tm, &tn);
+        const LinUnits& x = L.u[i];
+        const int prow = static_cast<int>(tm * kLinTile + rank * kRows);
+        const int qrow = static_cast<int>(tn * kLinTile + rank * kRows);
+        for (int64_t t = 0; t < x.steps; ++t) {
+          if (!mbar_wait_bounded(empty0 + 8 * s, ph, kWaitLimit)) {
+            ok = false;
+            break;
+          }
+          if (leader) mbar_arrive_expect_tx(full0 + 8 * s, 2u * kLinStage);
+          const uint32_t sa = smem_u32(smem + s * kLinStage), sb = sa + kTileBytes, bar = full_leader0 + 8 * s;
+          const int d = static_cast<int>(t) * (F8 ? 128 : 64);
+          if (!x.p_mn) {
+            tma_load_2d_pair(sa, &maps.p[i], bar, d, prow);
+          } else {
+            tma_load_2d_pair(sa, &maps.p[i], bar, prow, d);
+            tma_load_2d_pair(sa + kTileBytes / 2, &maps.p[i], bar, prow + 64, d);
+          }
+          if (!x.q_mn) {
+            tma_load_2d_pair(sb, &maps.q[i], bar, d, qrow);
+          } else {
+            tma_load_2d_pair(sb, &maps.q[i], bar, qrow, d);
+            tma_load_2d_pair(sb + kTileBytes / 2, &maps.q[i], bar, qrow + 64, d);
+          }
+          ++it;
+          if (++s == kLinStages) {
+            s = 0;
+            ph ^= 1;
+          }
+        }
+      }
+      if (!ok) {
+        dev->status = kStatusTimeout;
+        dev->timeout_site = 21;
+      }
+      if (leader)  // the leader's stage barriers also count the peer's bytes
+        for (uint32_t j = (it > kLinStages ? it - kLinStages : 0); j < it; ++j)
+          mbar_wait_bounded(full0 + 8 * (j % kLinStages), (j / kLinStages) & 1, kWaitLimit);
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    // ---------------- MMA issuer (leader CTA) ----------------
+    if (leader) {  // the whole warp; lane 0 issues
+      const uint32_t me = lane == 0;
+      const uint32_t base = smem_u32(smem);
+      uint32_t s = 0, ph = 0, acc = 0, accph = 1;
+      for (int64_t u = pair; u < L.units && ok; u += npairs) {
+        int64_t tm, tn;
+        const LinUnits& x = L.u[locate(u, &tm, &tn)];
+        if (x.steps == 0) continue;
+        // 32 bytes of depth an instruction: 32 bytes along a K-major row, 16
+        // depth rows of 128 bytes in MN-major storage.
+        const uint64_t pd = x.p_mn ? smem_desc_mn(base) : smem_desc_sw128(base);
+        const uint64_t qd = x.q_mn ? smem_desc_mn(base + kTileBytes) : smem_desc_sw128(base + kTileBytes);
+        const uint32_t pk = x.p_mn ? 128 : 2, qk = x.q_mn ? 128 : 2;
+        ok = mbar_wait_warp(acc_empty + 8 * acc, accph, kWaitLimit);
+        tc_fence_after();
+        for (int64_t t = 0; t < x.steps && ok; ++t) {
+          if (!(ok = mbar_wait_warp(full0 + 8 * s, ph, kWaitLimit))) break;
+          tc_fence_after();
+          const uint64_t a = pd + s * (kLinStage >> 4), b = qd + s * (kLinStage >> 4);
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk)
+            mma_pair<F8>(me, tmem + acc * kLinTile, a + kk * pk, b + kk * qk, x.idesc, (t | kk) ? 1u : 0u);
+          mma_commit_pair_mc(me, empty0 + 8 * s, 0x3);
+          if (++s == kLinStages) {
+            s = 0;
+            ph ^= 1;
+          }
+        }
+        if (!ok) break;
+        mma_commit_pair_mc(me, acc_full + 8 * acc, 0x3);
+        acc ^= 1;
+        if (acc == 0) accph ^= 1;
+      }
+      if (!ok && me) {
+        dev->status = kStatusTimeout;
+        dev->timeout_site = 22;
+      }
+      mma_commit_pair(me, drain_bar);
+      mbar_wait_bounded(drain_bar, 0, kWaitLimit);
+    }
+    __syncwarp();
+  } else {
+    // ---------------- epilogue (warps 2..9, both CTAs) ----------------
+    const int q = warp & 3, h = (warp - 2) >> 2;  // TMEM lane quarter, column half
+    uint8_t* buf = epi + (warp - 2) * kStageBytes;
+    float* bias_s = reinterpret_cast<float*>(epi + kLinEpiWarps * kStageBytes) + (warp - 2) * 2 * kLinCols;
+    float* scale_s = bias_s + kLinCols;
+    const uint32_t acc_empty_leader = mapa_shared(acc_empty, 0);
+    uint32_t acc = 0, accph = 0;
+    for (int64_t u = pair; u < L.units; u += npairs) {
+      int64_t tm, tn;
+      const LinUnits& x = L.u[locate(u, &tm, &tn)];
+      const LinEpilogue& ep = x.ep;
+      const int64_t row0 = tm * kLinTile + rank * kRows + 32 * q, col0 = tn * kLinTile + kLinCols * h;
+      const bool bf16 = ep.out_type == OZ2_TYPE_BF16, scales = ep.row_scale != nullptr;
+      __syncwarp();
+      for (int c = lane; c < kLinCols; c += 32) {
+        const int64_t j = col0 + c;
+        float b = 0.f;
+        if (ep.bias && j < x.cols)
+          b = ep.bias_type == OZ2_TYPE_F32 ? __ldg(static_cast<const float*>(ep.bias) + j)
+                                           : load16(static_cast<const uint16_t*>(ep.bias) + j, ep.bias_type == OZ2_TYPE_BF16);
+        bias_s[c] = b;
+        if (scales) scale_s[c] = j < x.cols ? __ldg(ep.col_scale + j) : 0.f;
+      }
+      const float row_scale = scales && row0 + lane < x.rows ? __ldg(ep.row_scale + row0 + lane) : 0.f;
+      __syncwarp();
+      if (x.steps) {
+        if (!mbar_wait_bounded(acc_full + 8 * acc, accph, kWaitLimit)) ok = false;
+        if (!__all_sync(0xffffffffu, ok)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+      }
+      const uint32_t at = tmem + (static_cast<uint32_t>(32 * q) << 16) + acc * kLinTile + kLinCols * h;
+      auto sums = [&](int c, float (&z)[32]) {
+        uint32_t v[32];
+        if (x.steps) {
+          tmem_ld32(at + c, v);
+          tmem_ld_wait();
+        } else {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = 0u;
+        }
+        scaled(scale_s, bias_s, row_scale, v, c, scales, z);
+      };
+      auto release = [&] {
+        if (x.steps) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_remote_relaxed(acc_empty_leader + 8 * acc);
+        }
+      };
+      if (ep.out_type == OZ2_TYPE_F32) {
+        for (int c = 0; c < kLinCols; c += 32) {
+          float z[32];
+          sums(c, z);
+          if (c == kLinCols - 32) release();
+#pragma unroll
+          for (int j = 0; j < 32; j += 4)
+            sts128(buf + piece_at(lane, j >> 2), make_uint4(__float_as_uint(z[j]), __float_as_uint(z[j + 1]),
+                                                            __float_as_uint(z[j + 2]), __float_as_uint(z[j + 3])));
+          __syncwarp();
+          store32(x, ep.out, ep.ld_out, row0, col0 + c, lane, buf, ep.accumulate != 0);
+          __syncwarp();
+        }
+      } else {
+        for (int c0 = 0; c0 < kLinCols; c0 += 64) {
+          if (ep.pre) {
+            for (int c = c0; c < c0 + 64; c += 32) {
+              float z[32];
+              sums(c, z);
+              finish32<OZ2_ACT_NONE>(z, false, bf16, buf, lane, c - c0);
+            }
+            __syncwarp();
+            store16(x, ep.pre, ep.ld_pre, row0, col0 + c0, lane, buf);
+            __syncwarp();
+          }
+          if (ep.add) {
+            fetch16(x, ep.add, ep.ld_add, row0, col0 + c0, lane, buf);
+            __syncwarp();
+          }
+          for (int c = c0; c < c0 + 64; c += 32) {
+            float z[32];
+            sums(c, z);
+            if (c == kLinCols - 32) release();
+            const bool add = ep.add != nullptr;
+            switch (ep.act) {
+              case OZ2_ACT_RELU: finish32<OZ2_ACT_RELU>(z, add, bf16, buf, lane, c - c0); break;
+              case OZ2_ACT_GELU: finish32<OZ2_ACT_GELU>(z, add, bf16, buf, lane, c - c0); break;
+              case OZ2_ACT_GELU_TANH: finish32<OZ2_ACT_GELU_TANH>(z, add, bf16, buf, lane, c - c0); break;
+              case OZ2_ACT_SILU: finish32<OZ2_ACT_SILU>(z, add, bf16, buf, lane, c - c0); break;
+              default: finish32<OZ2_ACT_NONE>(z, add, bf16, buf, lane, c - c0);
+            }
+          }
+          __syncwarp();
+          store16(x, ep.out, ep.ld_out, row0, col0 + c0, lane, buf);
+          __syncwarp();
+        }
+      }
+      if (x.steps) {
+        acc ^= 1;
+        if (acc == 0) accph ^= 1;
+      }
+    }
+    if (!ok) {
+      dev->status = kStatusTimeout;
+      dev->timeout_site = 23;
+    }
+  }
+  tc_fence_before();
+  cluster_sync_all();  // neither CTA leaves while the pair's MMAs or loads may touch it
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc_pair(tmem, 512);
+}
+
+// One operand as a 2-D tensor.  K-major: rows of `depth`, boxes of 128 bytes of
+// depth × 128 rows.  MN-major: depth rows of `rows`, boxes of 64 × 64.
+bool make_operand_map(CUtensorMap* map, const void* base, int64_t rows, int64_t depth, int64_t ld, int type, bool mn) {
+  EncodeTiledFn enc = get_encode_fn();
+  if (!enc) return false;
+  const int es = type_bytes(type);
+  cuuint64_t dims[2] = {static_cast<cuuint64_t>(mn ? rows : depth), static_cast<cuuint64_t>(mn ? depth : rows)};
+  cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld) * es};
+  cuuint32_t box[2] = {static_cast<cuuint32_t>(128 / es), mn ? 64u : 128u};
+  cuuint32_t estr[2] = {1, 1};
+  return enc(map, es == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void*>(base),
+             dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace
+
+cudaError_t launch_linear(const LinProduct* products, int count, int type, Oz2Device* dev, cudaStream_t st) {
+  LinMaps maps{};
+  LinLaunch L{};
+  const bool f8 = type == OZ2_TYPE_E4M3;
+  const int64_t step = 128 / type_bytes(type);
+  for (int i = 0; i < count; ++i) {
+    const LinProduct& p = products[i];
+    LinUnits& x = L.u[i];
+    x.rows = p.rows;
+    x.cols = p.cols;
+    x.ntm = (p.rows + kLinTile - 1) / kLinTile;
+    x.ntn = (p.cols + kLinTile - 1) / kLinTile;
+    x.units = x.ntm * x.ntn;
+    x.steps = (p.depth + step - 1) / step;
+    x.p_mn = p.p_mn;
+    x.q_mn = p.q_mn;
+    x.idesc = f8 ? idesc_f8_f32(kLinTile, kLinTile)
+                 : idesc_16(kLinTile, kLinTile, type == OZ2_TYPE_BF16, p.p_mn, p.q_mn);
+    x.ep = p.ep;
+    L.units += x.units;
+    if (x.steps && (!make_operand_map(&maps.p[i], p.p, p.rows, p.depth, p.ldp, type, p.p_mn) ||
+                    !make_operand_map(&maps.q[i], p.q, p.cols, p.depth, p.ldq, type, p.q_mn)))
+      return cudaErrorInvalidValue;
+  }
+  L.count = count;
+  if (L.units == 0) return cudaSuccess;
+  auto kern = f8 ? linear_pair_kernel<true> : linear_pair_kernel<false>;
+  cudaError_t err = allow_smem(reinterpret_cast<const void*>(kern), kLinSmem);
+  if (err != cudaSuccess) return err;
+  const int64_t pairs =
+      std::min(L.units, resident_pairs(reinterpret_cast<const void*>(kern), kLinThreads, kLinSmem));
+  count_launch();
+  return launch_dependent(kern, dim3(static_cast<unsigned>(2 * pairs)), dim3(kLinThreads), kLinSmem, st, maps, L, dev);
+}
+
+}  // namespace oz2

@@ -1,0 +1,178 @@
+// The memory-bound steps around the products of a linear layer: rows copied to
+// 16-byte boundaries for operands that TMA cannot read where they are, and the
+// gradient's dz = dy·act'(z) with its column sums db.
+#include <algorithm>
+
+#include "lin_common.cuh"
+
+namespace oz2 {
+namespace {
+
+// ---------------------------------------------------------------------------
+// Pack: a thread writes 16 bytes of a destination row from as many loads as the
+// source's alignment allows (its elements, one by one).
+// ---------------------------------------------------------------------------
+template <typename T>
+__global__ void __launch_bounds__(256) pack_rows_kernel(const T* __restrict__ src, int64_t ld_src, int64_t rows,
+                                                        int64_t cols, T* __restrict__ dst, int64_t ld_dst) {
+  pdl_trigger();
+  pdl_wait();
+  constexpr int kVec = 16 / sizeof(T);
+  const int64_t per = (cols + kVec - 1) / kVec;
+  for (int64_t i = blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x; i < rows * per;
+       i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
+    const int64_t r = i / per, c = (i - r * per) * kVec;
+    const T* s = src + r * ld_src + c;
+    union {
+      uint4 v;
+      T e[kVec];
+    } w;
+    w.v = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int j = 0; j < kVec; ++j)
+      if (c + j < cols) w.e[j] = __ldg(s + j);
+    *reinterpret_cast<uint4*>(dst + r * ld_dst + c) = w.v;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// dz and db.  A block takes 256 columns (a lane 8 of them) and a chunk of rows,
+// which its 8 warps walk in turn; the warps' sums are joined in shared memory in
+// a fixed order and the block's written to `partial` (chunk, column).  A second
+// kernel adds the chunks in order: the sums never depend on who came first.
+// ---------------------------------------------------------------------------
+constexpr int kGradCols = 256, kGradWarps = 8;
+
+template <int ACT>
+__global__ void __launch_bounds__(32 * kGradWarps)
+    act_grad_kernel(int64_t m, int64_t n, int64_t chunk_rows, bool bf16, bool vec, const uint16_t* __restrict__ dy,
+                    int64_t ld_dy, const uint16_t* __restrict__ z, int64_t ld_z, uint16_t* __restrict__ dz,
+                    int64_t ld_dz, float* __restrict__ partial) {
+  __shared__ float sums[kGradWarps][kGradCols];
+  pdl_trigger();
+  pdl_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t col = static_cast<int64_t>(blockIdx.x) * kGradCols + 8 * lane;
+  const int64_t r0 = static_cast<int64_t>(blockIdx.y) * chunk_rows, r1 = min(m, r0 + chunk_rows);
+  const bool whole = vec && col + 8 <= n;
+  float s[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s[e] = 0.f;
+  if (col < n) {
+#pragma unroll 4
+    for (int64_t r = r0 + warp; r < r1; r += kGradWarps) {
+      const uint16_t* a = dy + r * ld_dy + col;
+      const uint16_t* b = ACT == OZ2_ACT_NONE ? nullptr : z + r * ld_z + col;
+      uint32_t aw[4] = {0, 0, 0, 0}, bw[4] = {0, 0, 0, 0};
+      if (whole) {
+        const uint4 v = __ldg(reinterpret_cast<const uint4*>(a));
+        aw[0] = v.x, aw[1] = v.y, aw[2] = v.z, aw[3] = v.w;
+        if (ACT != OZ2_ACT_NONE) {
+          const uint4 w = __ldg(reinterpret_cast<const uint4*>(b));
+          bw[0] = w.x, bw[1] = w.y, bw[2] = w.z, bw[3] = w.w;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (col + e < n) {
+            aw[e >> 1] |= static_cast<uint32_t>(__ldg(a + e)) << (16 * (e & 1));
+            if (ACT != OZ2_ACT_NONE) bw[e >> 1] |= static_cast<uint32_t>(__ldg(b + e)) << (16 * (e & 1));
+          }
+      }
+      float g[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 f = unpack16(aw[e], bf16);
+        g[2 * e] = f.x;
+        g[2 * e + 1] = f.y;
+        if (ACT != OZ2_ACT_NONE) {
+          const float2 t = unpack16(bw[e], bf16);
+          g[2 * e] *= act_slope<ACT>(t.x);
+          g[2 * e + 1] *= act_slope<ACT>(t.y);
+        }
+        s[2 * e] += g[2 * e];
+        s[2 * e + 1] += g[2 * e + 1];
+      }
+      if (dz)  // rows of 16-byte pieces: what lies past n in the last one is padding
+        *reinterpret_cast<uint4*>(dz + r * ld_dz + col) = make_uint4(pack16(g[0], g[1], bf16), pack16(g[2], g[3], bf16),
+                                                                     pack16(g[4], g[5], bf16), pack16(g[6], g[7], bf16));
+    }
+  }
+  if (partial) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[warp][8 * lane + e] = s[e];
+    __syncthreads();
+    const int64_t j = static_cast<int64_t>(blockIdx.x) * kGradCols + threadIdx.x;
+    if (j < n) {
+      float t = 0.f;
+#pragma unroll
+      for (int w = 0; w < kGradWarps; ++w) t += sums[w][threadIdx.x];
+      partial[blockIdx.y * n + j] = t;
+    }
+  }
+}
+
+__global__ void __launch_bounds__(128) sum_chunks_kernel(int64_t n, int64_t chunks, const float* __restrict__ partial,
+                                                         float* __restrict__ db, bool accumulate) {
+  pdl_trigger();
+  pdl_wait();
+  const int64_t j = blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x;
+  if (j >= n) return;
+  float t = 0.f;
+#pragma unroll 4
+  for (int64_t c = 0; c < chunks; ++c) t += partial[c * n + j];
+  db[j] = accumulate ? db[j] + t : t;
+}
+
+int64_t chunk_rows_for(int64_t m, int64_t n) {
+  // About four blocks an SM, of at least 32 rows.
+  const int64_t across = (n + kGradCols - 1) / kGradCols;
+  const int64_t chunks = std::max<int64_t>(1, 4 * static_cast<int64_t>(num_sms()) / across);
+  int64_t rows = std::max<int64_t>(32, (m + chunks - 1) / chunks);
+  return std::max(rows, (m + 65534) / 65535);  // the grid's second axis
+}
+
+}  // namespace
+
+int64_t lin_db_chunks(int64_t m, int64_t n) {
+  const int64_t r = chunk_rows_for(m, n);
+  return std::max<int64_t>(1, (m + r - 1) / r);
+}
+
+cudaError_t launch_pack_rows(const void* src, int64_t ld_src, int64_t rows, int64_t cols, int bytes, void* dst,
+                             int64_t ld_dst, cudaStream_t st) {
+  const int64_t pieces = rows * ((cols * bytes + 15) / 16);
+  if (pieces == 0) return cudaSuccess;
+  const unsigned blocks = static_cast<unsigned>(std::min<int64_t>((pieces + 255) / 256, 16LL * num_sms()));
+  count_launch();
+  if (bytes == 1)
+    return launch_dependent(pack_rows_kernel<uint8_t>, dim3(blocks), dim3(256), 0, st,
+                            static_cast<const uint8_t*>(src), ld_src, rows, cols, static_cast<uint8_t*>(dst), ld_dst);
+  return launch_dependent(pack_rows_kernel<uint16_t>, dim3(blocks), dim3(256), 0, st,
+                          static_cast<const uint16_t*>(src), ld_src, rows, cols, static_cast<uint16_t*>(dst), ld_dst);
+}
+
+cudaError_t launch_act_grad(int64_t m, int64_t n, int type, int act, const void* dy, int64_t ld_dy, const void* z,
+                            int64_t ld_z, void* dz, int64_t ld_dz, float* db, float* partial, bool accumulate,
+                            cudaStream_t st) {
+  if (n == 0) return cudaSuccess;
+  const int64_t rows = chunk_rows_for(m, n), chunks = lin_db_chunks(m, n);
+  auto aligned = [](const void* p, int64_t ld) { return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(2 * ld)) & 15) == 0; };
+  const bool vec = aligned(dy, ld_dy) && (act == OZ2_ACT_NONE || aligned(z, ld_z));
+  auto kern = act == OZ2_ACT_RELU        ? act_grad_kernel<OZ2_ACT_RELU>
+              : act == OZ2_ACT_GELU      ? act_grad_kernel<OZ2_ACT_GELU>
+              : act == OZ2_ACT_GELU_TANH ? act_grad_kernel<OZ2_ACT_GELU_TANH>
+              : act == OZ2_ACT_SILU      ? act_grad_kernel<OZ2_ACT_SILU>
+                                         : act_grad_kernel<OZ2_ACT_NONE>;
+  count_launch();
+  cudaError_t err = launch_dependent(
+      kern, dim3(static_cast<unsigned>((n + kGradCols - 1) / kGradCols), static_cast<unsigned>(chunks)),
+      dim3(32 * kGradWarps), 0, st, m, n, rows, type == OZ2_TYPE_BF16, vec, static_cast<const uint16_t*>(dy), ld_dy,
+      static_cast<const uint16_t*>(z), ld_z, static_cast<uint16_t*>(dz), ld_dz, db ? partial : nullptr);
+  if (err != cudaSuccess || !db) return err;
+  count_launch();
+  return launch_dependent(sum_chunks_kernel, dim3(static_cast<unsigned>((n + 127) / 128)), dim3(128), 0, st, n, chunks,
+                          partial, db, accumulate);
+}
+
+}  // namespace oz2

@@ -1,0 +1,125 @@
+// Definitions shared by the layer operators' translation units (linear layer,
+// its gradient, AdamW): element types, activations, and the launchers.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "../../include/oz2_layers.h"
+#include "oz2_gemm.cuh"
+
+namespace oz2 {
+
+constexpr int type_bytes(int t) { return t == OZ2_TYPE_F32 ? 4 : t == OZ2_TYPE_E4M3 ? 1 : 2; }
+constexpr bool is_16bit(int t) { return t == OZ2_TYPE_BF16 || t == OZ2_TYPE_F16; }
+
+// Two 16-bit values of either format in a word (the lower address in the low
+// half), to and from FP32; the rounding is to nearest even.
+__device__ __forceinline__ uint32_t pack16(float lo, float hi, bool bf16) {
+  uint32_t w;
+  if (bf16) {
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
+  } else {
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
+  }
+  return w;
+}
+__device__ __forceinline__ float2 unpack16(uint32_t w, bool bf16) {
+  if (bf16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+  return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+__device__ __forceinline__ float load16(const uint16_t* p, bool bf16) { return unpack16(*p, bf16).x; }
+
+// --- activations ---------------------------------------------------------------
+// In the epilogue of a product, whose result is rounded to 16 bits, exp is the
+// fast one (about 2^-21 of the value); the gradient's FP32 sums take expf.
+constexpr float kSqrtHalf = 0.70710678118654752f, kSqrt2OverPi = 0.79788456080286536f, kInvSqrt2Pi = 0.39894228040143268f;
+constexpr float kGeluCubic = 0.044715f;
+
+template <int ACT>
+__device__ __forceinline__ float activate(float z) {
+  if (ACT == OZ2_ACT_RELU) return z < 0.f ? 0.f : z;  // NaN stays NaN
+  if (ACT == OZ2_ACT_GELU) return 0.5f * z * (1.f + erff(z * kSqrtHalf));
+  if (ACT == OZ2_ACT_GELU_TANH) {
+    // z(1 + tanh u)/2 = z/(1 + exp(-2u))
+    const float u = kSqrt2OverPi * fmaf(kGeluCubic * z * z, z, z);
+    return __fdividef(z, 1.f + __expf(-2.f * u));
+  }
+  if (ACT == OZ2_ACT_SILU) return __fdividef(z, 1.f + __expf(-z));
+  return z;
+}
+
+// d act(z)/dz.
+template <int ACT>
+__device__ __forceinline__ float act_slope(float z) {
+  if (ACT == OZ2_ACT_RELU) return z > 0.f ? 1.f : z == z ? 0.f : z;
+  if (ACT == OZ2_ACT_GELU)
+    return fmaf(z * kInvSqrt2Pi, expf(-0.5f * z * z), 0.5f * (1.f + erff(z * kSqrtHalf)));
+  if (ACT == OZ2_ACT_GELU_TANH) {
+    // with g = (1 + tanh u)/2 = 1/(1 + exp(-2u)):  g + z·2g(1 - g)·u'
+    const float zz = z * z;
+    const float u = kSqrt2OverPi * fmaf(kGeluCubic * zz, z, z);
+    const float g = 1.f / (1.f + expf(-2.f * u));
+    const float du = kSqrt2OverPi * fmaf(3.f * kGeluCubic, zz, 1.f);
+    return fmaf(2.f * z * g * (1.f - g), du, g);
+  }
+  if (ACT == OZ2_ACT_SILU) {
+    const float g = 1.f / (1.f + expf(-z));
+    return g * fmaf(z, 1.f - g, 1.f);
+  }
+  return 1.f;
+}
+
+// --- one product D = P·Qᵀ of the layer kernels ------------------------------------
+// P has `rows` rows and Q `cols` rows of `depth` bytes' worth of elements each;
+// an operand is stored with its depth contiguous ("K-major") or, 16-bit types
+// only, with its rows contiguous ("MN-major").  D is row-major.
+struct LinEpilogue {
+  const float* row_scale;  // of D's rows, or null
+  const float* col_scale;  // of D's columns, or null
+  const void* bias;        // of D's columns, or null
+  const void* add;         // R, like D, or null
+  void* pre;               // Z, like D, or null
+  void* out;               // D
+  int64_t ld_add, ld_pre, ld_out;
+  int bias_type;           // oz2_type
+  int out_type;            // oz2_type: 16-bit, or F32 (then nothing but `accumulate` applies)
+  int act;                 // oz2_act
+  int accumulate;          // F32 out: D += P·Qᵀ
+};
+struct LinProduct {
+  int64_t rows, cols;
+  int64_t depth;           // elements summed over
+  const void *p, *q;
+  int64_t ldp, ldq;
+  bool p_mn, q_mn;         // MN-major
+  LinEpilogue ep;
+};
+constexpr int kMaxProducts = 2;
+
+// Up to two independent products in one launch; operands' base addresses and
+// leading dimensions are multiples of 16 bytes.  `type` is the operands'.
+cudaError_t launch_linear(const LinProduct* products, int count, int type, Oz2Device* dev, cudaStream_t st);
+
+// Rows of elements of `bytes` bytes copied to rows that start on 16-byte
+// boundaries (ld_dst·bytes a multiple of 16).
+cudaError_t launch_pack_rows(const void* src, int64_t ld_src, int64_t rows, int64_t cols, int bytes, void* dst,
+                             int64_t ld_dst, cudaStream_t st);
+
+// dz = dy·act'(z) in the operands' type into rows of ld_dz elements (16-byte
+// rows; null: not wanted), and db = its column sums before that rounding
+// (null: not wanted; `partial` holds lin_db_chunks(m, n)·n floats for them).
+int64_t lin_db_chunks(int64_t m, int64_t n);
+cudaError_t launch_act_grad(int64_t m, int64_t n, int type, int act, const void* dy, int64_t ld_dy, const void* z,
+                            int64_t ld_z, void* dz, int64_t ld_dz, float* db, float* partial, bool accumulate,
+                            cudaStream_t st);
+
+cudaError_t launch_adamw(const oz2_adamw_tensor* tensors, int count, int param_type, int grad_type, int state_bits,
+                         const oz2_adamw_step& a, cudaStream_t st);
+
+// From the entry points' translation unit: the library's stream-ordered pool
+// and the current device's status block.
+cudaError_t workspace_alloc(void** p, size_t bytes, cudaStream_t st);
+Oz2Device* device_status();
+
+}  // namespace oz2

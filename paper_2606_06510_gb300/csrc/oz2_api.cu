@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "k_scan.cuh"
+#include "lin_common.cuh"
 
 namespace oz2 {
 
@@ -367,6 +368,13 @@ static cudaError_t pool_alloc(void** p, size_t bytes, cudaStream_t s) {
     }
   }
   return ds->pool ? cudaMallocFromPoolAsync(p, bytes, ds->pool, s) : cudaMallocAsync(p, bytes, s);
+}
+
+// For the layer operators' entry points.
+cudaError_t workspace_alloc(void** p, size_t bytes, cudaStream_t s) { return pool_alloc(p, bytes, s); }
+Oz2Device* device_status() {
+  DeviceState* ds = nullptr;
+  return device_state(&ds) == OZ2_OK ? ds->status : nullptr;
 }
 
 // Column-major rows × cols matrix copy; one linear copy when both sides are

@@ -1,0 +1,200 @@
+"""oz2_linear against its formula in 64 bits."""
+import pytest
+
+import layers_ref as ref
+from helpers import ensure_built
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def env():
+    ensure_built()
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    import paper_2606_06510_gb300 as oz
+    yield oz, torch
+    torch.cuda.synchronize()
+    assert oz.oz2_check_device_status() == 0
+
+
+def make(torch, m, n, k, dtype, seed=0, pad=(0, 0)):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1000 * seed + m + 3 * n + 7 * k)
+
+    def normal(*shape):
+        return torch.randn(shape, generator=g, device="cuda")
+
+    x, w = normal(m, k + pad[0]), normal(n, k + pad[1]) * max(k, 1) ** -0.5
+    xs = ws = None
+    if dtype == torch.float8_e4m3fn:
+        x, xs = ref.e4m3_rows(x) if x.numel() else (x.to(dtype), normal(m))
+        w, ws = ref.e4m3_rows(w) if w.numel() else (w.to(dtype), normal(n))
+    else:
+        x, w = x.to(dtype), w.to(dtype)
+    return x[:, :k], w[:, :k], xs, ws, normal
+
+
+SHAPES = [(1, 1, 1), (1, 128, 64), (2, 129, 63), (3, 4096, 4096), (8, 1000, 520), (16, 640, 16384), (17, 257, 130),
+          (33, 96, 1032), (64, 2048, 512), (100, 300, 257), (128, 128, 128), (129, 255, 129), (256, 256, 256),
+          (257, 513, 1027), (500, 64, 8192), (1000, 777, 1333), (1024, 2304, 640)]
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("kind", ["bf16", "f16", "e4m3"])
+def test_shapes(env, shape, kind):
+    oz, torch = env
+    dt = {"bf16": torch.bfloat16, "f16": torch.float16, "e4m3": torch.float8_e4m3fn}[kind]
+    m, n, k = shape
+    x, w, xs, ws, normal = make(torch, m, n, k, dt)
+    out = torch.bfloat16 if kind == "e4m3" else dt
+    name = ref.ACTS[(m + n + k) % 5]
+    bias, r = normal(n).to(out), normal(m, n).to(out)
+    y, z = oz.oz2_linear(x, w, bias=bias, act=name, residual=r, x_scale=xs, w_scale=ws, save_pre=True)
+    wy, wz, by, bz = ref.linear(x, w, bias, name, r, xs, ws)
+    ref.close(y, wy, by, "y")
+    ref.close(z, wz, bz, "z")
+    # Without its options, and again: the same bits.
+    y0 = oz.oz2_linear(x, w, x_scale=xs, w_scale=ws)
+    wy, _, by, _ = ref.linear(x, w, x_scale=xs, w_scale=ws)
+    ref.close(y0, wy, by, "plain")
+    assert torch.equal(y0, oz.oz2_linear(x, w, x_scale=xs, w_scale=ws))
+
+
+@pytest.mark.parametrize("name", ref.ACTS)
+@pytest.mark.parametrize("m", [1, 24, 300])
+def test_activations_at_all_magnitudes(env, name, m):
+    """z from bias alone (k = 0) and from products, tiny to huge."""
+    oz, torch = env
+    n = 777
+    bias = torch.linspace(-12, 12, n, device="cuda")
+    bias[:8] = torch.tensor([0.0, -0.0, 1e-30, -1e-30, 300.0, -300.0, 60000.0, -60000.0])
+    for dt in (torch.bfloat16, torch.float16):
+        x, w = torch.zeros(m, 0, dtype=dt, device="cuda"), torch.zeros(n, 0, dtype=dt, device="cuda")
+        y = oz.oz2_linear(x, w, bias=bias, act=name)
+        wy, _, by, _ = ref.linear(x, w, bias, name, out=dt)
+        ref.close(y, wy, by, "k = 0")
+        x, w = torch.ones(m, 40, dtype=dt, device="cuda"), torch.zeros(n, 40, dtype=dt, device="cuda")
+        w[:, 7] = bias.clamp(-200, 200).to(dt)
+        y = oz.oz2_linear(x, w, act=name)
+        wy, _, by, _ = ref.linear(x, w, None, name)
+        ref.close(y, wy, by, "products")
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 300, 200), (20, 300, 200), (300, 300, 200), (300, 333, 201)])
+def test_strided_operands_and_outputs(env, m, n, k):
+    """Rows inside larger arrays, bases off the 16-byte grid, residual and out
+    the same array; what lies beside the rows keeps its values."""
+    oz, torch = env
+    for pad in ((8, 16), (1, 3), (2, 5)):
+        x, w, _, _, normal = make(torch, m, n, k, torch.bfloat16, seed=2, pad=pad)
+        x, w = x[:, 1:], w[:, 1:]
+        hold = normal(m, n + 2 * pad[0]).to(torch.bfloat16)
+        keep = hold.clone()
+        y = hold[:, pad[0]:pad[0] + n]
+        r = keep[:, pad[0]:pad[0] + n]
+        got = oz.oz2_linear(x, w, act="silu", residual=y, out=y)
+        wy, _, by, _ = ref.linear(x, w, None, "silu", r)
+        assert got.data_ptr() == y.data_ptr()
+        ref.close(y, wy, by, "y")
+        assert torch.equal(hold[:, :pad[0]], keep[:, :pad[0]]) and torch.equal(hold[:, pad[0] + n:], keep[:, pad[0] + n:])
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 256, 512), (20, 256, 512), (300, 256, 512)])
+def test_nothing_outside_the_operands_matters(env, m, n, k):
+    """NaN beside and behind the operands' rows and around the outputs."""
+    oz, torch = env
+    nan = float("nan")
+    for dt in (torch.bfloat16, torch.float8_e4m3fn):
+        x, w, xs, ws, _ = make(torch, m, n, k, dt, seed=3)
+        k2 = k - 5
+        X = torch.full((m + 1, k + 16), nan, device="cuda").to(dt)
+        W = torch.full((n + 1, k + 16), nan, device="cuda").to(dt)
+        X[:m, :k2], W[:n, :k2] = x[:, :k2], w[:, :k2]
+        y = oz.oz2_linear(X[:m, :k2], W[:n, :k2], x_scale=xs, w_scale=ws)
+        wy, _, by, _ = ref.linear(x[:, :k2], w[:, :k2], x_scale=xs, w_scale=ws)
+        ref.close(y, wy, by)
+
+
+@pytest.mark.parametrize("m", [1, 5, 200])
+def test_non_finite_values_stay_in_their_rows(env, m):
+    oz, torch = env
+    n, k = 260, 192
+    x, w, _, _, _ = make(torch, m, n, k, torch.float16, seed=4)
+    w[7, 3] = float("nan")
+    w[9, 5] = float("inf")
+    x[:, 5] = 1.0
+    y = oz.oz2_linear(x, w)
+    assert torch.isnan(y[:, 7]).all()
+    assert torch.isposinf(y[:, 9]).all()
+    y[:, 7] = y[:, 9] = 0
+    assert torch.isfinite(y).all()
+    assert torch.isnan(oz.oz2_linear(x, w, act="relu")[:, 7]).all()
+
+
+def test_empty_problems(env):
+    oz, torch = env
+    bf = torch.bfloat16
+    e = lambda *s: torch.empty(s, dtype=bf, device="cuda")  # noqa: E731
+    assert oz.oz2_linear(e(0, 64), e(32, 64)).shape == (0, 32)
+    assert oz.oz2_linear(e(5, 64), e(0, 64)).shape == (5, 0)
+    assert torch.equal(oz.oz2_linear(e(5, 0), e(9, 0)), torch.zeros(5, 9, dtype=bf, device="cuda"))
+
+
+def test_e4m3_without_scales_and_with_f16_results(env):
+    oz, torch = env
+    x, w, _, _, normal = make(torch, 70, 90, 300, torch.float8_e4m3fn, seed=5)
+    x, w = (x.float() / 64).to(x.dtype), (w.float() / 64).to(w.dtype)
+    y = oz.oz2_linear(x, w, out_dtype=torch.float16)
+    wy, _, by, _ = ref.linear(x, w, out=torch.float16)
+    ref.close(y, wy, by)
+
+
+def test_zero_tokens_and_zero_scales(env):
+    """Padding tokens: rows of zeros, with a scale of zero."""
+    oz, torch = env
+    x, w, xs, ws, normal = make(torch, 40, 90, 300, torch.float8_e4m3fn, seed=6)
+    x[10:20] = 0
+    xs[10:20] = 0
+    b = normal(90)
+    y = oz.oz2_linear(x, w, bias=b, x_scale=xs, w_scale=ws)
+    assert torch.equal(y[10:20], b.to(torch.bfloat16).expand(10, 90))
+
+
+def test_on_another_stream_and_in_a_graph(env):
+    oz, torch = env
+    x, w, _, _, normal = make(torch, 37, 515, 333, torch.bfloat16, seed=7)
+    want = oz.oz2_linear(x, w, act="gelu")
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        got = oz.oz2_linear(x, w, act="gelu")
+    s.synchronize()
+    assert torch.equal(got, want)
+    out = torch.empty_like(want)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        oz.oz2_linear(x, w, act="gelu", out=out)
+    x2 = normal(37, 333).to(torch.bfloat16)
+    x.copy_(x2)
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, oz.oz2_linear(x2, w, act="gelu"))
+
+
+def test_offsets_beyond_32_bits(env):
+    """A token array and a result of more than 2^31 elements' extent."""
+    oz, torch = env
+    m, n, k = 3, 136, 128
+    ld = (1 << 30) + 64
+    big = torch.empty(2 * ld + k + n, dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(8)
+    xs = torch.randn(m, k, generator=g, device="cuda").to(torch.bfloat16)
+    w = torch.randn(n, k, generator=g, device="cuda").to(torch.bfloat16)
+    x = big.as_strided((m, k), (ld, 1), 0)
+    y = big.as_strided((m, n), (ld, 1), k)
+    x.copy_(xs)
+    oz.oz2_linear(x, w, out=y)
+    wy, _, by, _ = ref.linear(xs, w)
+    ref.close(y, wy, by)
