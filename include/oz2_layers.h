@@ -85,7 +85,8 @@ int oz2_linear_grad(int64_t m, int64_t n, int64_t k, int type,
                     void* d_dX, int64_t lddx, void* d_dW, int64_t lddw, int dw_type,
                     float* d_db, unsigned flags, void* stream);
 
-/* One AdamW step over `count` tensors, in one launch for up to 320 of them:
+/* One AdamW step over `count` tensors, in one launch for up to 256 of them (twice
+ * that where some have a master and some have none):
  *   g' = c·g    m ← β1·m + (1-β1)·g'    v ← β2·v + (1-β2)·g'²
  *   w ← w - lr·λ·w - lr·(m/(1-β1^t))/(√(v/(1-β2^t)) + ε)
  * with t = step, λ = weight_decay, c = *d_grad_scale (1 if null; read on the
@@ -108,7 +109,8 @@ int oz2_linear_grad(int64_t m, int64_t n, int64_t k, int type,
  * state.  A value that is not finite is kept as E4M3's NaN; the others of its
  * block are not touched by it.
  *
- * param_type F32, BF16 or F16; grad_type F32 or param_type.  Errors:
+ * param_type F32, BF16 or F16 (a master wants a 16-bit one); grad_type F32 or
+ * param_type.  Errors:
  * OZ2_ERR_INVALID_ARG for null pointers, negative sizes, step < 1, betas
  * outside [0, 1), or a combination of types not named here. */
 typedef struct {

@@ -13,6 +13,15 @@
 // A warp takes 256 values at a time, a lane 4 of each half, so a block's largest
 // magnitude is one warp reduction and every access is 16 (FP32), 8 or 4 bytes a
 // lane, consecutive over the warp.
+//
+// With FP32 states memory bounds it: 201 M bf16 parameters with masters and bf16
+// gradients, 28 bytes each, take 814 µs (6.9 TB/s, a plain copy's rate).  With
+// 8-bit states there are 16 bytes and some 105 instructions a parameter (the hash
+// and the two roundings are a third of them): issue bounds it, 714 µs at 4.5 TB/s.
+// Loading the next block ahead took it from 1209 to 826 µs, a kernel for each
+// combination of types to 741, and a fifth block of 128 threads an SM, at 24 to 44
+// bytes of spills, to 714 (six: 792).  A square root without the compiler's branch
+// cost as many instructions as it saved.
 #include <algorithm>
 
 #include "lin_common.cuh"
@@ -21,12 +30,13 @@ namespace oz2 {
 namespace {
 
 constexpr int kAdamBlock = 256;      // values under one scale, and of a warp's turn
-constexpr int kAdamWarps = 8;
-constexpr int kAdamTurns = 4;        // a warp's consecutive blocks
+constexpr int kAdamWarps = 4;
+constexpr int kAdamTurns = 8;        // a warp's consecutive blocks, at most
 
 struct AdamEntry {
   int64_t numel;
   int64_t first;                     // number of its first block in this launch
+  int64_t number;                    // and in the whole list
   void* param;
   const void* grad;
   float* master;
@@ -38,9 +48,8 @@ struct AdamEntry {
 template <int CAP>
 struct AdamTable {
   int count;
-  int param_type, grad_type;
+  int turns;                         // a warp's consecutive blocks
   int64_t blocks;                    // of this launch
-  int64_t base;                      // blocks of the launches before it
   float b1, c1, b2, c2;              // β1, 1-β1, β2, 1-β2
   float step, decay, root, eps;      // lr/(1-β1^t), lr·λ, 1/√(1-β2^t), ε
   uint32_t key;
@@ -57,89 +66,93 @@ __host__ __device__ __forceinline__ uint32_t scatter32(uint32_t x) {
   return x ^ (x >> 16);
 }
 
-struct Four {
-  float v[4];
-};
-__device__ __forceinline__ Four load4(const void* p, int64_t at, int type, int n, bool vec) {
-  Four f;
-  if (type == OZ2_TYPE_F32) {
-    const float* s = static_cast<const float*>(p) + at;
-    if (vec && n == 4) {
-      const float4 w = *reinterpret_cast<const float4*>(s);
-      f.v[0] = w.x, f.v[1] = w.y, f.v[2] = w.z, f.v[3] = w.w;
+// Four consecutive values as they lie in memory: 16-bit types fill two words,
+// E4M3 one.  A whole vector, or the first n of them one by one (the others 0).
+template <typename T, int kWords = sizeof(T)>
+__device__ __forceinline__ void load_words(const void* p, int64_t at, bool whole, int n, uint32_t* w) {
+  constexpr int kPer = 4 / sizeof(T);
+  const T* s = static_cast<const T*>(p) + at;
+  if (__builtin_expect(whole, 1)) {
+    if (kWords == 4) {
+      const uint4 v = *reinterpret_cast<const uint4*>(s);
+      w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    } else if (kWords == 2) {
+      const uint2 v = *reinterpret_cast<const uint2*>(s);
+      w[0] = v.x, w[1] = v.y;
     } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) f.v[e] = e < n ? s[e] : 0.f;
+      w[0] = *reinterpret_cast<const uint32_t*>(s);
     }
   } else {
-    const uint16_t* s = static_cast<const uint16_t*>(p) + at;
-    const bool bf16 = type == OZ2_TYPE_BF16;
-    uint32_t w[2] = {0, 0};
-    if (vec && n == 4) {
-      const uint2 u = *reinterpret_cast<const uint2*>(s);
-      w[0] = u.x, w[1] = u.y;
-    } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (e < n) w[e >> 1] |= static_cast<uint32_t>(s[e]) << (16 * (e & 1));
-    }
-    const float2 a = unpack16(w[0], bf16), b = unpack16(w[1], bf16);
-    f.v[0] = a.x, f.v[1] = a.y, f.v[2] = b.x, f.v[3] = b.y;
+    for (int i = 0; i < kWords; ++i) w[i] = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < n) w[e / kPer] |= static_cast<uint32_t>(s[e]) << (8 * sizeof(T) * (e % kPer));
   }
-  return f;
 }
-__device__ __forceinline__ void store4(void* p, int64_t at, int type, const Four& f, int n, bool vec) {
-  if (type == OZ2_TYPE_F32) {
-    float* d = static_cast<float*>(p) + at;
-    if (vec && n == 4) {
-      *reinterpret_cast<float4*>(d) = make_float4(f.v[0], f.v[1], f.v[2], f.v[3]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (e < n) d[e] = f.v[e];
-    }
-  } else {
-    uint16_t* d = static_cast<uint16_t*>(p) + at;
-    const bool bf16 = type == OZ2_TYPE_BF16;
-    const uint32_t w[2] = {pack16(f.v[0], f.v[1], bf16), pack16(f.v[2], f.v[3], bf16)};
-    if (vec && n == 4) {
+template <typename T, int kWords = sizeof(T)>
+__device__ __forceinline__ void store_words(void* p, int64_t at, bool whole, int n, const uint32_t* w) {
+  constexpr int kPer = 4 / sizeof(T);
+  T* d = static_cast<T*>(p) + at;
+  if (__builtin_expect(whole, 1)) {
+    if (kWords == 4) {
+      *reinterpret_cast<uint4*>(d) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else if (kWords == 2) {
       *reinterpret_cast<uint2*>(d) = make_uint2(w[0], w[1]);
     } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (e < n) d[e] = static_cast<uint16_t>(w[e >> 1] >> (16 * (e & 1)));
+      *reinterpret_cast<uint32_t*>(d) = w[0];
     }
-  }
-}
-
-// Four E4M3 codes in a word, and their values.
-__device__ __forceinline__ uint32_t load_codes(const void* p, int64_t at, int n, bool vec) {
-  const uint8_t* s = static_cast<const uint8_t*>(p) + at;
-  if (vec && n == 4) return *reinterpret_cast<const uint32_t*>(s);
-  uint32_t w = 0;
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (e < n) w |= static_cast<uint32_t>(s[e]) << (8 * e);
-  return w;
-}
-__device__ __forceinline__ void store_codes(void* p, int64_t at, uint32_t w, int n, bool vec) {
-  uint8_t* d = static_cast<uint8_t*>(p) + at;
-  if (vec && n == 4) {
-    *reinterpret_cast<uint32_t*>(d) = w;
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (e < n) d[e] = static_cast<uint8_t>(w >> (8 * e));
+      if (e < n) d[e] = static_cast<T>(w[e / kPer] >> (8 * sizeof(T) * (e % kPer)));
   }
 }
-__device__ __forceinline__ Four decode4(uint32_t w) {
+template <int TYPE>
+__device__ __forceinline__ void load4(const void* p, int64_t at, bool whole, int n, uint32_t* w) {
+  if (TYPE == OZ2_TYPE_F32) {
+    load_words<uint32_t>(p, at, whole, n, w);
+  } else {
+    load_words<uint16_t>(p, at, whole, n, w);
+  }
+}
+template <int TYPE>
+__device__ __forceinline__ void values4(const uint32_t* w, float* f) {
+  if (TYPE == OZ2_TYPE_F32) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = __uint_as_float(w[e]);
+  } else {
+    const float2 a = unpack16(w[0], TYPE == OZ2_TYPE_BF16), b = unpack16(w[1], TYPE == OZ2_TYPE_BF16);
+    f[0] = a.x, f[1] = a.y, f[2] = b.x, f[3] = b.y;
+  }
+}
+template <int TYPE>
+__device__ __forceinline__ void store4(void* p, int64_t at, bool whole, int n, const float* f) {
+  uint32_t w[4];
+  if (TYPE == OZ2_TYPE_F32) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(f[e]);
+    store_words<uint32_t>(p, at, whole, n, w);
+  } else {
+    w[0] = pack16(f[0], f[1], TYPE == OZ2_TYPE_BF16);
+    w[1] = pack16(f[2], f[3], TYPE == OZ2_TYPE_BF16);
+    store_words<uint16_t>(p, at, whole, n, w);
+  }
+}
+// The values of four E4M3 codes.
+__device__ __forceinline__ void decode4(uint32_t w, float* f) {
   uint32_t lo, hi;
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(lo) : "h"(static_cast<uint16_t>(w)));
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(hi) : "h"(static_cast<uint16_t>(w >> 16)));
   const float2 a = unpack16(lo, false), b = unpack16(hi, false);
-  Four f;
-  f.v[0] = a.x, f.v[1] = a.y, f.v[2] = b.x, f.v[3] = b.y;
-  return f;
+  f[0] = a.x, f[1] = a.y, f[2] = b.x, f[3] = b.y;
+}
+// The codes of four values that E4M3 holds exactly (or of NaN).
+__device__ __forceinline__ uint32_t encode4(const float* f) {
+  uint16_t lo, hi;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(f[1]), "f"(f[0]));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(f[3]), "f"(f[2]));
+  return static_cast<uint32_t>(lo) | static_cast<uint32_t>(hi) << 16;
 }
 
 // The exponent field of a block's scale: the power of two that brings its largest
@@ -149,31 +162,69 @@ __device__ __forceinline__ int scale_exponent(uint32_t top) {
   return max(1, static_cast<int>(top >> 23) - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0));
 }
 
-// E4M3 of y (|y| ≤ 448), away from zero with the probability of what is cut
-// off, by the 16 bits of u.  Below 2^-6 the spacing is constant: 2^-6 is added,
-// which leaves the value's last three bits where a normal one's are.
-__device__ __forceinline__ uint32_t encode_stochastic(float y, uint32_t u) {
-  const uint32_t bits = __float_as_uint(y);
-  const float a = fabsf(y);
-  const bool small = a < 0.015625f;
-  const uint32_t b = __float_as_uint(small ? __fadd_rn(a, 0.015625f) : a);
-  const uint32_t code = ((b + (u << 4)) >> 20) - (small ? 968u : 960u);
-  const uint32_t sign = (bits >> 24) & 0x80u;
-  return (bits & 0x7F800000u) == 0x7F800000u ? sign | 0x7Fu : sign | code;
+// y (|y| ≤ 448) cut to one of its two E4M3 neighbours, the one away from zero
+// with the probability of what is cut off: `u` (16 bits, shifted left by 4) is
+// added below the three bits that E4M3 keeps, and the rest dropped.  Below 2^-6
+// the spacing is constant: 2^-6 is added first, which leaves the value's last
+// three bits where a normal one's are, and taken off again (both exact but for
+// what lies under 2^-29).
+template <bool SIGNED>
+__device__ __forceinline__ float cut_stochastic(float y, uint32_t u) {
+  const float c = fabsf(y) < 0.015625f ? SIGNED ? copysignf(0.015625f, y) : 0.015625f : 0.f;
+  const float t = __fadd_rn(y, c);
+  const float r = __uint_as_float((__float_as_uint(t) + u) & 0xFFF00000u) - c;
+  return SIGNED ? copysignf(r, y) : r;
 }
 
-__device__ __forceinline__ uint32_t finite_bits(float x) {
-  const uint32_t b = __float_as_uint(x) & 0x7FFFFFFFu;
-  return b < 0x7F800000u ? b : 0u;
+// 1/x to about 2^-23 (x below 2^-126 counts as 0).
+__device__ __forceinline__ float reciprocal(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
 }
 
-template <int BITS, int CAP>
-__global__ void __launch_bounds__(32 * kAdamWarps) adamw_kernel(const __grid_constant__ AdamTable<CAP> T) {
+// A warp's 256 values as they were loaded.
+struct AdamRaw {
+  uint32_t g[2][4], w[2][4], m[2][4], v[2][4];
+  float m_scale, v_scale;
+};
+
+// Elements of the four at `at` that the tensor has.
+__device__ __forceinline__ int part_of(const AdamEntry& x, int64_t at) {
+  return static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(4), x.numel - at)));
+}
+
+template <int BITS, int W, int G, bool MASTER>
+__device__ __forceinline__ void load_raw(const AdamEntry& x, int64_t in, bool whole, int lane, AdamRaw& r) {
+  const void* weight = MASTER ? x.master : x.param;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int64_t at = in * kAdamBlock + 128 * h + 4 * lane;
+    const int n = whole ? 4 : part_of(x, at);
+    load4<G>(x.grad, at, whole, n, r.g[h]);
+    load4<MASTER ? OZ2_TYPE_F32 : W>(weight, at, whole, n, r.w[h]);
+    if (BITS == 32) {
+      load_words<uint32_t>(x.m, at, whole, n, r.m[h]);
+      load_words<uint32_t>(x.v, at, whole, n, r.v[h]);
+    } else {
+      load_words<uint8_t>(x.m, at, whole, n, r.m[h]);
+      load_words<uint8_t>(x.v, at, whole, n, r.v[h]);
+    }
+  }
+  if (BITS == 8) {
+    r.m_scale = x.m_scale[in];
+    r.v_scale = x.v_scale[in];
+  }
+}
+
+// W: the parameters' type; G: the gradients'; MASTER: FP32 weights beside them.
+template <int BITS, int W, int G, bool MASTER, int CAP>
+__global__ void __launch_bounds__(32 * kAdamWarps, BITS == 8 ? 5 : 1) adamw_kernel(const __grid_constant__ AdamTable<CAP> T) {
   pdl_trigger();
   pdl_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  int64_t b = (static_cast<int64_t>(blockIdx.x) * kAdamWarps + warp) * kAdamTurns;
-  const int64_t end = min(b + kAdamTurns, T.blocks);
+  int64_t b = (static_cast<int64_t>(blockIdx.x) * kAdamWarps + warp) * T.turns;
+  const int64_t end = min(b + T.turns, T.blocks);
   if (b >= end) return;
   const float gscale = T.grad_scale ? __ldg(T.grad_scale) : 1.f;
   int lo = 0, hi = T.count;  // the tensor that holds block b
@@ -181,63 +232,81 @@ __global__ void __launch_bounds__(32 * kAdamWarps) adamw_kernel(const __grid_con
     const int mid = (lo + hi) >> 1;
     if (T.e[mid].first <= b) lo = mid; else hi = mid;
   }
+  auto is_whole = [&](const AdamEntry& x, int64_t in) { return x.vec && (in + 1) * kAdamBlock <= x.numel; };
+  // The next block is on its way while one is computed: an 8-bit block is some 80
+  // instructions an element and few bytes, and a load would otherwise be waited
+  // for between them.
+  AdamRaw next;
+  bool next_whole = is_whole(T.e[lo], b - T.e[lo].first);
+  load_raw<BITS, W, G, MASTER>(T.e[lo], b - T.e[lo].first, next_whole, lane, next);
   for (; b < end; ++b) {
-    while (lo + 1 < T.count && T.e[lo + 1].first <= b) ++lo;
     const AdamEntry& x = T.e[lo];
+    const AdamRaw r = next;
+    const bool whole = next_whole;
     const int64_t in = b - x.first, at0 = in * kAdamBlock + 4 * lane;
-    const bool vec = x.vec != 0;
-    const int wtype = x.master ? OZ2_TYPE_F32 : T.param_type;
-    void* const weight = x.master ? static_cast<void*>(x.master) : x.param;
-    const float step = T.step * x.lr_scale, decay = T.decay * x.lr_scale * x.decay_scale;
-    Four w[2], g[2], m[2], v[2];
-    int n[2];
-    float ms = 1.f, vs = 1.f;
-    if (BITS == 8) {
-      ms = x.m_scale[in];
-      vs = x.v_scale[in];
+    if (b + 1 < end) {
+      if (lo + 1 < T.count && T.e[lo + 1].first <= b + 1) ++lo;
+      next_whole = is_whole(T.e[lo], b + 1 - T.e[lo].first);
+      load_raw<BITS, W, G, MASTER>(T.e[lo], b + 1 - T.e[lo].first, next_whole, lane, next);
     }
+    const float step = T.step * x.lr_scale, decay = T.decay * x.lr_scale * x.decay_scale;
+    float w[2][4], m[2][4], v[2][4];
+    float mtop = 0.f, vtop = 0.f;
+    bool odd = false;  // something is not a number
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int64_t at = at0 + 128 * h;
-      n[h] = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(4), x.numel - at)));
-      g[h] = load4(x.grad, at, T.grad_type, n[h], vec);
-      w[h] = load4(weight, at, wtype, n[h], vec);
+      float g[4];
+      values4<G>(r.g[h], g);
+      values4<MASTER ? OZ2_TYPE_F32 : W>(r.w[h], w[h]);
       if (BITS == 32) {
-        m[h] = load4(x.m, at, OZ2_TYPE_F32, n[h], vec);
-        v[h] = load4(x.v, at, OZ2_TYPE_F32, n[h], vec);
+        values4<OZ2_TYPE_F32>(r.m[h], m[h]);
+        values4<OZ2_TYPE_F32>(r.v[h], v[h]);
       } else {
-        m[h] = decode4(load_codes(x.m, at, n[h], vec));
-        v[h] = decode4(load_codes(x.v, at, n[h], vec));
+        decode4(r.m[h][0], m[h]);
+        decode4(r.v[h][0], v[h]);
       }
-    }
-    uint32_t mtop = 0, vtop = 0;
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float gg = g[h].v[e] * gscale;
-        float mm = m[h].v[e], vv = v[h].v[e];
+        const float gg = g[e] * gscale;
+        float mm = m[h][e], vv = v[h][e];
         if (BITS == 8) {
-          mm *= ms;
-          vv *= vs;
+          mm *= r.m_scale;
+          vv *= r.v_scale;
           vv *= vv;
         }
         // Rounded one by one, so that the 8-bit states can be checked bit for bit.
         mm = __fadd_rn(__fmul_rn(mm, T.b1), __fmul_rn(gg, T.c1));
         vv = __fadd_rn(__fmul_rn(vv, T.b2), __fmul_rn(__fmul_rn(gg, gg), T.c2));
         const float root = __fsqrt_rn(vv);
-        const float p = w[h].v[e];
-        w[h].v[e] = fmaf(-decay, p, p) - step * __fdividef(mm, fmaf(root, T.root, T.eps));
-        m[h].v[e] = mm;
-        v[h].v[e] = BITS == 32 ? vv : root;
-        if (BITS == 8 && e < n[h]) {
-          mtop = max(mtop, finite_bits(mm));
-          vtop = max(vtop, finite_bits(root));
+        const float p = w[h][e];
+        const float u = mm * reciprocal(fmaf(root, T.root, T.eps));
+        w[h][e] = fmaf(-step, u, fmaf(-decay, p, p));
+        m[h][e] = mm;
+        v[h][e] = BITS == 32 ? vv : root;
+        if (BITS == 8) {
+          mtop = fmaxf(mtop, fabsf(mm));  // drops a NaN
+          vtop = fmaxf(vtop, root);
+          odd |= !(fabsf(u) < 1e38f);
         }
       }
+    }
     if (BITS == 8) {
-      const int me = scale_exponent(__reduce_max_sync(0xffffffffu, mtop));
-      const int ve = scale_exponent(__reduce_max_sync(0xffffffffu, vtop));
+      // Padding of a last block is zeros, which change no maximum.
+      uint32_t mbits = __float_as_uint(mtop), vbits = __float_as_uint(vtop);
+      odd |= !(mtop < INFINITY) || !(vtop < INFINITY);
+      const bool rare = __any_sync(0xffffffffu, odd);
+      if (rare) {  // the largest finite magnitudes
+        mbits = vbits = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (isfinite(m[h][e])) mbits = max(mbits, __float_as_uint(fabsf(m[h][e])));
+            if (isfinite(v[h][e])) vbits = max(vbits, __float_as_uint(v[h][e]));
+          }
+      }
+      const int me = scale_exponent(__reduce_max_sync(0xffffffffu, mbits));
+      const int ve = scale_exponent(__reduce_max_sync(0xffffffffu, vbits));
       const float minv = __uint_as_float(static_cast<uint32_t>(254 - me) << 23);
       const float vinv = __uint_as_float(static_cast<uint32_t>(254 - ve) << 23);
       if (lane == 0) {
@@ -245,66 +314,112 @@ __global__ void __launch_bounds__(32 * kAdamWarps) adamw_kernel(const __grid_con
         x.v_scale[in] = __uint_as_float(static_cast<uint32_t>(ve) << 23);
       }
       // Values are numbered through the whole list, every tensor starting a block.
-      const uint64_t number = static_cast<uint64_t>(T.base + b) * kAdamBlock + 4 * lane;
-      const uint32_t high = static_cast<uint32_t>(number >> 32) * 0x3C6EF372u + T.key;
+      const uint64_t number = static_cast<uint64_t>(x.number + in) * kAdamBlock + 4 * lane;
+      const uint32_t from = static_cast<uint32_t>(number) * 0x9E3779B1u +
+                            static_cast<uint32_t>(number >> 32) * 0x3C6EF372u + T.key;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        uint32_t mw = 0, vw = 0;
+        float mc[4], vc[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const uint32_t r = scatter32(static_cast<uint32_t>(number + 128 * h + e) * 0x9E3779B1u + high);
-          mw |= encode_stochastic(m[h].v[e] * minv, r & 0xFFFFu) << (8 * e);
-          vw |= encode_stochastic(v[h].v[e] * vinv, r >> 16) << (8 * e);
+          const uint32_t bits = scatter32(from + static_cast<uint32_t>(128 * h + e) * 0x9E3779B1u);
+          mc[e] = cut_stochastic<true>(m[h][e] * minv, bits << 4 & 0xFFFF0u);
+          vc[e] = cut_stochastic<false>(v[h][e] * vinv, bits >> 12 & 0xFFFF0u);
         }
-        store_codes(x.m, at0 + 128 * h, mw, n[h], vec);
-        store_codes(x.v, at0 + 128 * h, vw, n[h], vec);
+        uint32_t mw = encode4(mc), vw = encode4(vc);
+        if (rare) {  // infinities and NaN are kept as the NaN of their sign
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (!isfinite(m[h][e]))
+              mw = (mw & ~(0xFFu << 8 * e)) | ((__float_as_uint(m[h][e]) >> 24 & 0x80u) | 0x7Fu) << 8 * e;
+            if (!isfinite(v[h][e]))
+              vw = (vw & ~(0xFFu << 8 * e)) | ((__float_as_uint(v[h][e]) >> 24 & 0x80u) | 0x7Fu) << 8 * e;
+          }
+        }
+        const int n = whole ? 4 : part_of(x, at0 + 128 * h);
+        store_words<uint8_t>(x.m, at0 + 128 * h, whole, n, &mw);
+        store_words<uint8_t>(x.v, at0 + 128 * h, whole, n, &vw);
       }
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int64_t at = at0 + 128 * h;
+      const int n = whole ? 4 : part_of(x, at);
       if (BITS == 32) {
-        store4(x.m, at, OZ2_TYPE_F32, m[h], n[h], vec);
-        store4(x.v, at, OZ2_TYPE_F32, v[h], n[h], vec);
+        store4<OZ2_TYPE_F32>(x.m, at, whole, n, m[h]);
+        store4<OZ2_TYPE_F32>(x.v, at, whole, n, v[h]);
       }
-      store4(weight, at, wtype, w[h], n[h], vec);
-      if (x.master && x.param) store4(x.param, at, T.param_type, w[h], n[h], vec);
+      if (MASTER) {
+        store4<OZ2_TYPE_F32>(x.master, at, whole, n, w[h]);
+        if (x.param) store4<W>(x.param, at, whole, n, w[h]);
+      } else {
+        store4<W>(x.param, at, whole, n, w[h]);
+      }
     }
   }
 }
 
-template <int BITS, int CAP>
-cudaError_t launch_table(AdamTable<CAP>& T, const oz2_adamw_tensor* t, int count, cudaStream_t st) {
-  T.count = 0;
-  T.blocks = 0;
-  for (int i = 0; i < count; ++i) {
-    if (t[i].numel == 0) continue;
-    AdamEntry& e = T.e[T.count++];
-    e = AdamEntry{t[i].numel, T.blocks, t[i].param, t[i].grad, t[i].master, t[i].m,
-                  t[i].v, t[i].m_scale, t[i].v_scale, t[i].lr_scale, t[i].decay_scale, 0};
-    auto on = [](const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % (4 * bytes) == 0; };
-    const int state = BITS == 32 ? 4 : 1;
-    e.vec = on(e.param, type_bytes(T.param_type)) && on(e.grad, type_bytes(T.grad_type)) && on(e.master, 4) &&
-            on(e.m, state) && on(e.v, state);
-    T.blocks += (e.numel + kAdamBlock - 1) / kAdamBlock;
-  }
-  if (T.blocks == 0) return cudaSuccess;
-  const int64_t per = kAdamWarps * kAdamTurns, grid = (T.blocks + per - 1) / per;
-  if (grid > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
-  count_launch();
-  const cudaError_t err = launch_dependent(adamw_kernel<BITS, CAP>, dim3(static_cast<unsigned>(grid)),
-                                           dim3(32 * kAdamWarps), 0, st, T);
-  T.base += T.blocks;
-  return err;
+template <int CAP>
+using AdamKernel = void (*)(const AdamTable<CAP>);
+
+template <int BITS, bool MASTER, int CAP>
+AdamKernel<CAP> kernel_for(int w, int g) {
+  if (w == OZ2_TYPE_F32) return adamw_kernel<BITS, OZ2_TYPE_F32, OZ2_TYPE_F32, false, CAP>;
+  if (w == OZ2_TYPE_BF16)
+    return g == OZ2_TYPE_F32 ? adamw_kernel<BITS, OZ2_TYPE_BF16, OZ2_TYPE_F32, MASTER, CAP>
+                             : adamw_kernel<BITS, OZ2_TYPE_BF16, OZ2_TYPE_BF16, MASTER, CAP>;
+  return g == OZ2_TYPE_F32 ? adamw_kernel<BITS, OZ2_TYPE_F16, OZ2_TYPE_F32, MASTER, CAP>
+                           : adamw_kernel<BITS, OZ2_TYPE_F16, OZ2_TYPE_F16, MASTER, CAP>;
 }
 
-template <int BITS, int CAP>
-cudaError_t launch_list(const oz2_adamw_tensor* t, int count, int param_type, int grad_type, const oz2_adamw_step& a,
+// The tensors of the list that have a master (or those that have none), in
+// launches of up to CAP of them.
+template <int CAP>
+cudaError_t launch_some(AdamTable<CAP>& T, const oz2_adamw_tensor* t, int count, bool master, int w, int g, int bits,
+                        cudaStream_t st) {
+  T.count = 0;
+  T.blocks = 0;
+  int64_t number = 0;
+  auto flush = [&]() -> cudaError_t {
+    if (T.count == 0) return cudaSuccess;
+    // A warp's turns: as many as leave every SM 24 warps.
+    T.turns = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kAdamTurns, T.blocks / (24LL * num_sms()))));
+    const int64_t per = static_cast<int64_t>(kAdamWarps) * T.turns, grid = (T.blocks + per - 1) / per;
+    if (grid > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
+    auto kern = bits == 8 ? (master ? kernel_for<8, true, CAP>(w, g) : kernel_for<8, false, CAP>(w, g))
+                          : (master ? kernel_for<32, true, CAP>(w, g) : kernel_for<32, false, CAP>(w, g));
+    count_launch();
+    const cudaError_t err =
+        launch_dependent(kern, dim3(static_cast<unsigned>(grid)), dim3(32 * kAdamWarps), 0, st, T);
+    T.count = 0;
+    T.blocks = 0;
+    return err;
+  };
+  for (int i = 0; i < count; ++i) {
+    const int64_t blocks = (t[i].numel + kAdamBlock - 1) / kAdamBlock;
+    if (blocks && (t[i].master != nullptr) == master) {
+      AdamEntry& e = T.e[T.count++];
+      e = AdamEntry{t[i].numel, T.blocks, number, t[i].param, t[i].grad, t[i].master, t[i].m,
+                    t[i].v, t[i].m_scale, t[i].v_scale, t[i].lr_scale, t[i].decay_scale, 0};
+      auto on = [](const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % (4 * bytes) == 0; };
+      const int state = bits == 32 ? 4 : 1;
+      e.vec = on(e.param, type_bytes(w)) && on(e.grad, type_bytes(g)) && on(e.master, 4) && on(e.m, state) &&
+              on(e.v, state);
+      T.blocks += blocks;
+    }
+    number += blocks;
+    if (T.count == CAP || i + 1 == count) {
+      const cudaError_t err = flush();
+      if (err != cudaSuccess) return err;
+    }
+  }
+  return cudaSuccess;
+}
+
+template <int CAP>
+cudaError_t launch_list(const oz2_adamw_tensor* t, int count, int w, int g, int bits, const oz2_adamw_step& a,
                         cudaStream_t st) {
   static thread_local AdamTable<CAP> T;  // up to 30 KB: not on the stack
-  T.param_type = param_type;
-  T.grad_type = grad_type;
-  T.base = 0;
   T.b1 = static_cast<float>(a.beta1);
   T.c1 = static_cast<float>(1.0 - a.beta1);
   T.b2 = static_cast<float>(a.beta2);
@@ -316,11 +431,13 @@ cudaError_t launch_list(const oz2_adamw_tensor* t, int count, int param_type, in
   T.eps = static_cast<float>(a.eps);
   T.key = scatter32(scatter32(a.seed) + static_cast<uint32_t>(a.step));
   T.grad_scale = a.d_grad_scale;
-  for (int i = 0; i < count; i += CAP) {
-    const cudaError_t err = launch_table<BITS, CAP>(T, t + i, std::min(CAP, count - i), st);
-    if (err != cudaSuccess) return err;
-  }
-  return cudaSuccess;
+  bool some[2] = {false, false};
+  for (int i = 0; i < count; ++i)
+    if (t[i].numel) some[t[i].master != nullptr] = true;
+  cudaError_t err = cudaSuccess;
+  for (int master = 0; master < 2 && err == cudaSuccess; ++master)
+    if (some[master]) err = launch_some<CAP>(T, t, count, master != 0, w, g, bits, st);
+  return err;
 }
 
 }  // namespace
@@ -329,12 +446,9 @@ cudaError_t launch_list(const oz2_adamw_tensor* t, int count, int param_type, in
 // small lists should not pay for copying a large one.
 cudaError_t launch_adamw(const oz2_adamw_tensor* t, int count, int param_type, int grad_type, int state_bits,
                          const oz2_adamw_step& a, cudaStream_t st) {
-  constexpr int kSmall = 32, kLarge = 320;
-  if (state_bits == 8)
-    return count <= kSmall ? launch_list<8, kSmall>(t, count, param_type, grad_type, a, st)
-                           : launch_list<8, kLarge>(t, count, param_type, grad_type, a, st);
-  return count <= kSmall ? launch_list<32, kSmall>(t, count, param_type, grad_type, a, st)
-                         : launch_list<32, kLarge>(t, count, param_type, grad_type, a, st);
+  constexpr int kSmall = 32, kLarge = 256;
+  return count <= kSmall ? launch_list<kSmall>(t, count, param_type, grad_type, state_bits, a, st)
+                         : launch_list<kLarge>(t, count, param_type, grad_type, state_bits, a, st);
 }
 
 }  // namespace oz2

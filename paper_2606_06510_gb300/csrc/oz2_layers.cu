@@ -218,7 +218,7 @@ int oz2_adamw(const oz2_adamw_tensor* tensors, int count, int param_type, int gr
     const oz2_adamw_tensor& t = tensors[i];
     if (t.numel < 0) return OZ2_ERR_INVALID_ARG;
     if (t.numel == 0) continue;
-    if ((!t.param && !t.master) || !t.grad || !t.m || !t.v || (state_bits == 8 && (!t.m_scale || !t.v_scale)))
+    if ((!t.param && !t.master) || (t.master && param_type == OZ2_TYPE_F32) || !t.grad || !t.m || !t.v || (state_bits == 8 && (!t.m_scale || !t.v_scale)))
       return OZ2_ERR_INVALID_ARG;
     if (!on(t.param, type_bytes(param_type)) || !on(t.grad, type_bytes(grad_type)) || !on(t.master, 4) ||
         !on(t.m, sb) || !on(t.v, sb) || !on(t.m_scale, 4) || !on(t.v_scale, 4))

@@ -284,3 +284,25 @@ def test_repeats_bit_for_bit_and_on_another_stream(env):
         torch.cuda.synchronize()
         outs.append([a.clone() for a in p] + [a.view(torch.uint8).clone() for a in st["m"] + st["v"]])
     assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+def test_masters_for_some_of_the_tensors(env):
+    """A list in which every other tensor has a master: two launches, one numbering."""
+    oz, torch = env
+    sizes = [700, 256, 513, 9]
+    outs = []
+    for mixed in (False, True):
+        p, g, _, _ = tensors(torch, sizes, torch.bfloat16, torch.bfloat16, 11)
+        st = oz.oz2_adamw_states(p, bits=8)
+        plan = oz.oz2_adamw_plan(p, g, **st)
+        masters = [a.float() for a in p]
+        if mixed:
+            for i in (1, 3):
+                plan.tensors[i].master = masters[i].data_ptr()
+        for t in (1, 2):
+            oz.oz2_adamw(plan, step=t, seed=3, **HYPER)
+        outs.append((p, masters, [a.view(torch.uint8) for a in st["m"] + st["v"]]))
+    assert all(torch.equal(a, b) for a, b in zip(outs[0][2], outs[1][2]))
+    assert torch.equal(outs[0][0][0], outs[1][0][0]) and torch.equal(outs[0][0][2], outs[1][0][2])
+    for i in (1, 3):
+        assert torch.equal(outs[1][0][i], outs[1][1][i].to(torch.bfloat16))

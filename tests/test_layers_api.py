@@ -91,7 +91,7 @@ def adamw(oz, change=None, count=1, param=BF16, grad=BF16, bits=32, args=None, s
     dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0), dict(beta2=float("nan")), dict(gs=66),
     dict(change=dict(numel=-1)), dict(change=dict(grad=N)), dict(change=dict(m=N)), dict(change=dict(v=N)),
     dict(change=dict(param=N, master=N)), dict(bits=8, change=dict(m_scale=N)), dict(change=dict(m=66)),
-    dict(change=dict(param=65)), dict(bits=8, change=dict(v_scale=66))])
+    dict(change=dict(param=65)), dict(param=F32, grad=F32), dict(bits=8, change=dict(v_scale=66))])
 def test_adamw_refuses(oz, bad):
     assert adamw(oz, **bad) == -1
 
