@@ -465,19 +465,392 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
   if (warp == 1) tmem_dealloc_pair(tmem, 512);
 }
 
+// ---------------------------------------------------------------------------
+// Tiles of NT rows × 128 columns of D on single CTAs, the depth split over the
+// CTAs of a cluster: for a D of few tiles.  The tile is formed transposed: Q's
+// 128 rows are the MMA's M (D's columns on tensor-memory lanes), P's NT rows its
+// N, so that a few tokens fill a small N, and a warp's lanes are consecutive
+// columns of D.  Each CTA leaves its sums in its shared memory (where the operands
+// were), and after a cluster barrier takes an equal share of the tile's rows, adds
+// up the parts in the order of the CTAs and finishes them: no workspace, and the
+// same bits every time.
+// ---------------------------------------------------------------------------
+constexpr int kSplitThreads = 256;    // TMA warp, MMA warp, 4 that drain, all 8 finish
+constexpr int kMaxSplit = 8;
+constexpr int kSplitMaxStages = 12;
+constexpr int split_stage_bytes(int nt) { return (kRows + nt) * 128; }
+constexpr int split_smem(int nt, int stages) {
+  const int ring = stages * split_stage_bytes(nt), sums = nt * kRows * 4;
+  return 1024 + (ring > sums ? ring : sums) + 8 * (2 * kSplitMaxStages + 2);
+}
+
+template <bool F8>
+__device__ __forceinline__ void mma_one(uint32_t me, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                        uint32_t accumulate) {
+  if (F8) {
+    asm volatile(
+        "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
+        " @q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(me)
+        : "memory");
+  } else {
+    mma_f16_by(me, d_tmem, a_desc, b_desc, idesc, accumulate);
+  }
+}
+
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+  return v;
+}
+
+__device__ __forceinline__ float activate_any(float z, int act) {
+  switch (act) {
+    case OZ2_ACT_RELU: return activate<OZ2_ACT_RELU>(z);
+    case OZ2_ACT_GELU: return activate<OZ2_ACT_GELU>(z);
+    case OZ2_ACT_GELU_TANH: return activate<OZ2_ACT_GELU_TANH>(z);
+    case OZ2_ACT_SILU: return activate<OZ2_ACT_SILU>(z);
+    default: return z;
+  }
+}
+
+// Eight columns of one row of D from their sums.
+__device__ __forceinline__ void finish8(const LinUnits& x, int64_t row, int64_t col, float (&z)[8]) {
+  const LinEpilogue& ep = x.ep;
+  const int n = static_cast<int>(min(static_cast<int64_t>(8), x.cols - col));
+  if (ep.out_type == OZ2_TYPE_F32) {
+    float* d = static_cast<float*>(ep.out) + row * ep.ld_out + col;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) d[e] = ep.accumulate ? d[e] + z[e] : z[e];
+    return;
+  }
+  const bool bf16 = ep.out_type == OZ2_TYPE_BF16;
+  if (ep.row_scale) {
+    const float rs = __ldg(ep.row_scale + row);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) z[e] *= rs * __ldg(ep.col_scale + col + e);
+  }
+  if (ep.bias) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n)
+        z[e] += ep.bias_type == OZ2_TYPE_F32 ? __ldg(static_cast<const float*>(ep.bias) + col + e)
+                                             : load16(static_cast<const uint16_t*>(ep.bias) + col + e, bf16);
+  }
+  auto put = [&](void* dst, int64_t ld) {
+    uint16_t* d = static_cast<uint16_t*>(dst) + row * ld + col;
+    const uint32_t w[4] = {pack16(z[0], z[1], bf16), pack16(z[2], z[3], bf16), pack16(z[4], z[5], bf16),
+                           pack16(z[6], z[7], bf16)};
+    if (n == 8 && vec_ok(dst, ld, 2)) {
+      *reinterpret_cast<uint4*>(d) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < n) d[e] = static_cast<uint16_t>(w[e >> 1] >> (16 * (e & 1)));
+    }
+  };
+  if (ep.pre) put(ep.pre, ep.ld_pre);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) z[e] = activate_any(z[e], ep.act);
+  if (ep.add) {
+    const uint16_t* s = static_cast<const uint16_t*>(ep.add) + row * ep.ld_add + col;
+    if (n == 8 && vec_ok(ep.add, ep.ld_add, 2)) {
+      const uint4 r = *reinterpret_cast<const uint4*>(s);
+      const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 f = unpack16(w[e], bf16);
+        z[2 * e] += f.x;
+        z[2 * e + 1] += f.y;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < n) z[e] += unpack16(s[e], bf16).x;
+    }
+  }
+  put(ep.out, ep.ld_out);
+}
+
+template <bool F8, int NT>
+__global__ void __launch_bounds__(kSplitThreads)
+    linear_split_kernel(const __grid_constant__ LinMaps maps, const __grid_constant__ LinLaunch L, int stages, int split,
+                        Oz2Device* dev) {
+  constexpr int kStage = split_stage_bytes(NT);
+  constexpr int kCols = NT < 32 ? 32 : NT;   // tensor memory is allocated in powers of two from 32 columns
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  __shared__ uint64_t bars[2 * kSplitMaxStages + 1];
+  __shared__ uint32_t tmem_base_s;
+  __shared__ int failed_s;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = split > 1 ? cluster_ctarank() : 0;
+  const uint32_t full0 = smem_u32(bars), empty0 = smem_u32(bars + kSplitMaxStages);
+  const uint32_t done = smem_u32(bars + 2 * kSplitMaxStages);
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < stages; ++s) {
+      mbar_init(full0 + 8 * s, 1);
+      mbar_init(empty0 + 8 * s, 1);
+    }
+    mbar_init(done, 1);
+    fence_barrier_init();
+    failed_s = 0;
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(&tmem_base_s), kCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_base_s;
+  pdl_wait();
+
+  int64_t u = blockIdx.x / split;
+  const int i = L.count > 1 && u >= L.u[0].units ? 1 : 0;
+  const LinUnits& x = L.u[i];
+  if (i) u -= L.u[0].units;
+  const int64_t tn = u / x.ntm, tm = u - tn * x.ntm;   // tiles that share Q's rows run together
+  const int64_t per = (x.steps + split - 1) / split;
+  const int64_t t0 = min(x.steps, static_cast<int64_t>(rank) * per), t1 = min(x.steps, t0 + per);
+
+  if (warp == 0) {
+    if (lane == 0) {
+      const int prow = static_cast<int>(tm * NT), qrow = static_cast<int>(tn * kRows);
+      uint32_t s = 0, ph = 1;
+      bool ok = true;
+      for (int64_t t = t0; t < t1; ++t) {
+        if (!mbar_wait_bounded(empty0 + 8 * s, ph, kWaitLimit)) {
+          ok = false;
+          break;
+        }
+        mbar_arrive_expect_tx(full0 + 8 * s, kStage);
+        const uint32_t sa = smem_u32(smem + s * kStage), sb = sa + kTileBytes, bar = full0 + 8 * s;
+        const int d = static_cast<int>(t) * (F8 ? 128 : 64);
+        if (!x.q_mn) {
+          tma_load_2d(sa, &maps.q[i], bar, d, qrow);
+        } else {
+          tma_load_2d(sa, &maps.q[i], bar, qrow, d);
+          tma_load_2d(sa + kTileBytes / 2, &maps.q[i], bar, qrow + 64, d);
+        }
+        if (!x.p_mn) {
+          tma_load_2d(sb, &maps.p[i], bar, d, prow);
+        } else {
+#pragma unroll
+          for (int r = 0; r < NT; r += 64) tma_load_2d(sb + r * 128, &maps.p[i], bar, prow + r, d);
+        }
+        if (++s == static_cast<uint32_t>(stages)) {
+          s = 0;
+          ph ^= 1;
+        }
+      }
+      if (!ok) {
+        failed_s = 1;
+        dev->status = kStatusTimeout;
+        dev->timeout_site = 24;
+        // Copies in flight land before the block goes.
+        for (int j = 0; j < stages; ++j)
+          if (t0 + j < t1) mbar_wait_bounded(full0 + 8 * j, j < static_cast<int>(s) ? ph ^ 1 : ph, kWaitLimit);
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    const uint32_t me = lane == 0, base = smem_u32(smem);
+    const uint64_t ad = x.q_mn ? smem_desc_mn(base) : smem_desc_sw128(base);
+    const uint64_t bd = x.p_mn ? smem_desc_mn(base + kTileBytes) : smem_desc_sw128(base + kTileBytes);
+    const uint32_t ak = x.q_mn ? 128 : 2, bk = x.p_mn ? 128 : 2;
+    uint32_t s = 0, ph = 0;
+    for (int64_t t = t0; t < t1; ++t) {
+      if (!mbar_wait_warp(full0 + 8 * s, ph, kWaitLimit)) {
+        if (me) {
+          failed_s = 1;
+          dev->status = kStatusTimeout;
+          dev->timeout_site = 25;
+        }
+        break;
+      }
+      tc_fence_after();
+      const uint64_t a = ad + s * (kStage >> 4), b = bd + s * (kStage >> 4);
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) mma_one<F8>(me, tmem, a + kk * ak, b + kk * bk, x.idesc, t > t0 || kk ? 1u : 0u);
+      mma_commit_by(me, empty0 + 8 * s);
+      if (++s == static_cast<uint32_t>(stages)) {
+        s = 0;
+        ph ^= 1;
+      }
+    }
+    mma_commit_by(me, done);
+    __syncwarp();
+  }
+  // The sums, NT columns of 128 lanes, to shared memory: the operands there have
+  // been multiplied.
+  float* sums = reinterpret_cast<float*>(smem);
+  if (warp >= 2 && warp < 6) {
+    const int q = warp & 3;
+    const bool ok = mbar_wait_warp(done, 0, kWaitLimit);
+    if (!ok && lane == 0) {
+      failed_s = 1;
+      dev->status = kStatusTimeout;
+      dev->timeout_site = 26;
+    }
+    tc_fence_after();
+    if (ok && !*static_cast<volatile int*>(&failed_s)) {
+#pragma unroll
+      for (int c = 0; c < NT; c += 16) {
+        uint32_t v[16];
+        if (t1 > t0) {
+          tmem_ld16(tmem + (static_cast<uint32_t>(32 * q) << 16) + c, v);
+          tmem_ld_wait();
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) v[j] = 0u;
+        }
+#pragma unroll
+        for (int j = 0; j < 16; ++j) sums[(c + j) * kRows + 32 * q + lane] = __uint_as_float(v[j]);
+      }
+    }
+  }
+  tc_fence_before();
+  if (split > 1) {
+    cluster_sync_all();
+  } else {
+    __syncthreads();
+  }
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc(tmem, kCols);
+  // This CTA's rows of the tile, eight columns a thread.
+  {
+    const int share = NT / split, r0 = static_cast<int>(rank) * share;
+    const uint32_t mine = smem_u32(sums);
+    for (int w = threadIdx.x; w < share * 16; w += kSplitThreads) {
+      const int r = r0 + (w >> 4), c = (w & 15) * 8;
+      const int64_t row = tm * NT + r, col = tn * kRows + c;
+      if (row >= x.rows || col >= x.cols) continue;
+      const uint32_t at = mine + (r * kRows + c) * 4;
+      float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      for (int p = 0; p < split; ++p) {
+        const uint32_t from = split > 1 ? mapa_shared(at, p) : at;
+        const float4 a = ld_cluster_f4(from), b = ld_cluster_f4(from + 16);
+        z[0] += a.x, z[1] += a.y, z[2] += a.z, z[3] += a.w;
+        z[4] += b.x, z[5] += b.y, z[6] += b.z, z[7] += b.w;
+      }
+      finish8(x, row, col, z);
+    }
+  }
+  if (split > 1) cluster_sync_all();  // no CTA leaves while another reads its sums
+}
+
 // One operand as a 2-D tensor.  K-major: rows of `depth`, boxes of 128 bytes of
-// depth × 128 rows.  MN-major: depth rows of `rows`, boxes of 64 × 64.
-bool make_operand_map(CUtensorMap* map, const void* base, int64_t rows, int64_t depth, int64_t ld, int type, bool mn) {
+// depth × box_rows rows.  MN-major: depth rows of `rows`, boxes of 64 × 64.
+bool make_operand_map(CUtensorMap* map, const void* base, int64_t rows, int64_t depth, int64_t ld, int type, bool mn,
+                      int box_rows = kRows) {
   EncodeTiledFn enc = get_encode_fn();
   if (!enc) return false;
   const int es = type_bytes(type);
   cuuint64_t dims[2] = {static_cast<cuuint64_t>(mn ? rows : depth), static_cast<cuuint64_t>(mn ? depth : rows)};
   cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld) * es};
-  cuuint32_t box[2] = {static_cast<cuuint32_t>(128 / es), mn ? 64u : 128u};
+  cuuint32_t box[2] = {static_cast<cuuint32_t>(128 / es), mn ? 64u : static_cast<cuuint32_t>(box_rows)};
   cuuint32_t estr[2] = {1, 1};
   return enc(map, es == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void*>(base),
              dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace
+
+namespace {
+
+// How a launch runs: on CTA pairs (nt = 0), or in tiles of nt rows with the depth
+// split over `split` CTAs and `stages` of operands in flight.
+struct LinPlan {
+  int nt = 0, split = 1, stages = 0;
+};
+
+// The plan of least estimated time.  The estimates (µs) follow a model of one
+// launch: the operands' bytes through an SM's share of L2, the tensor cores' cycles,
+// waves of CTAs, and fixed costs, each fitted to measurements on one GB300.
+LinPlan choose_plan(const LinProduct* products, int count, int type) {
+  const int64_t step = 128 / type_bytes(type), sms = num_sms();
+  constexpr double kGHz = 1.85;
+  bool p_mn = false;
+  double pair_work = 0;
+  int64_t pair_units = 0, max_steps = 0;
+  for (int i = 0; i < count; ++i) {
+    const LinProduct& p = products[i];
+    const int64_t units = ((p.rows + kLinTile - 1) / kLinTile) * ((p.cols + kLinTile - 1) / kLinTile);
+    const int64_t steps = (p.depth + step - 1) / step;
+    pair_units += units;
+    max_steps = std::max(max_steps, steps);
+    pair_work += static_cast<double>(units) * (steps * 540.0 + 300.0);
+    p_mn = p_mn || p.p_mn;
+  }
+  const int64_t pairs = sms / 2;
+  LinPlan best;
+  double best_us = 4.0 + (max_steps * 540.0 + 4000.0) / (1000 * kGHz);
+  if (pair_units > pairs)
+    best_us = 4.0 + std::max(pair_work / pairs, ((pair_units + pairs - 1) / pairs) * (pair_work / pair_units)) /
+                        (1000 * kGHz) + 2.0;
+  for (int nt : {16, 32, 64, 128}) {
+    if (p_mn && nt < 64) continue;
+    for (int split = 1; split <= kMaxSplit; split *= 2) {
+      if (nt / split < 1) continue;
+      const double step_cycles = std::max(2.0 * nt, (kRows + nt) * 128 / 60.0);
+      double work = 0, longest = 0;
+      int64_t ctas = 0;
+      for (int i = 0; i < count; ++i) {
+        const LinProduct& p = products[i];
+        const int64_t units = ((p.rows + nt - 1) / nt) * ((p.cols + kRows - 1) / kRows);
+        const int64_t steps = ((p.depth + step - 1) / step + split - 1) / split;
+        ctas += units * split;
+        const double t = steps * step_cycles + 1500.0 + (split > 1 ? 800.0 : 0.0) + nt * 10.0;
+        work += units * split * t;
+        longest = std::max(longest, t);
+      }
+      const double cycles = std::max(longest, ((ctas + sms - 1) / sms) * (work / ctas));
+      const double us = 3.5 + cycles / (1000 * kGHz);
+      if (us < best_us) {
+        best_us = us;
+        best.nt = nt;
+        best.split = split;
+        const int per_sm = ctas > sms ? 2 : 1;
+        best.stages = std::min(kSplitMaxStages, (per_sm == 2 ? 110 * 1024 : 220 * 1024) / split_stage_bytes(nt));
+      }
+    }
+  }
+  return best;
+}
+
+using SplitKernel = void (*)(const LinMaps, const LinLaunch, int, int, Oz2Device*);
+template <bool F8>
+SplitKernel split_kernel(int nt) {
+  return nt == 16   ? linear_split_kernel<F8, 16>
+         : nt == 32 ? linear_split_kernel<F8, 32>
+         : nt == 64 ? linear_split_kernel<F8, 64>
+                    : linear_split_kernel<F8, 128>;
+}
+
+// As launch_dependent, in clusters.
+template <typename... KArgs, typename... Args>
+cudaError_t launch_clusters(void (*kernel)(KArgs...), unsigned grid, unsigned block, size_t smem, unsigned cluster,
+                            cudaStream_t st, Args... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
 
 }  // namespace
@@ -487,27 +860,41 @@ cudaError_t launch_linear(const LinProduct* products, int count, int type, Oz2De
   LinLaunch L{};
   const bool f8 = type == OZ2_TYPE_E4M3;
   const int64_t step = 128 / type_bytes(type);
+  const LinPlan plan = choose_plan(products, count, type);
+  const int tile_rows = plan.nt ? plan.nt : kLinTile, tile_cols = plan.nt ? kRows : kLinTile;
   for (int i = 0; i < count; ++i) {
     const LinProduct& p = products[i];
     LinUnits& x = L.u[i];
     x.rows = p.rows;
     x.cols = p.cols;
-    x.ntm = (p.rows + kLinTile - 1) / kLinTile;
-    x.ntn = (p.cols + kLinTile - 1) / kLinTile;
+    x.ntm = (p.rows + tile_rows - 1) / tile_rows;
+    x.ntn = (p.cols + tile_cols - 1) / tile_cols;
     x.units = x.ntm * x.ntn;
     x.steps = (p.depth + step - 1) / step;
     x.p_mn = p.p_mn;
     x.q_mn = p.q_mn;
-    x.idesc = f8 ? idesc_f8_f32(kLinTile, kLinTile)
-                 : idesc_16(kLinTile, kLinTile, type == OZ2_TYPE_BF16, p.p_mn, p.q_mn);
+    // The pairs' A is P; the split kernel's is Q.
+    const int M = plan.nt ? kRows : kLinTile, N = plan.nt ? plan.nt : kLinTile;
+    x.idesc = f8 ? idesc_f8_f32(M, N)
+                 : idesc_16(M, N, type == OZ2_TYPE_BF16, plan.nt ? p.q_mn : p.p_mn, plan.nt ? p.p_mn : p.q_mn);
     x.ep = p.ep;
     L.units += x.units;
-    if (x.steps && (!make_operand_map(&maps.p[i], p.p, p.rows, p.depth, p.ldp, type, p.p_mn) ||
+    if (x.steps && (!make_operand_map(&maps.p[i], p.p, p.rows, p.depth, p.ldp, type, p.p_mn, plan.nt ? plan.nt : kRows) ||
                     !make_operand_map(&maps.q[i], p.q, p.cols, p.depth, p.ldq, type, p.q_mn)))
       return cudaErrorInvalidValue;
   }
   L.count = count;
   if (L.units == 0) return cudaSuccess;
+  if (plan.nt) {
+    if (L.units * plan.split > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
+    SplitKernel kern = f8 ? split_kernel<true>(plan.nt) : split_kernel<false>(plan.nt);
+    const size_t smem = split_smem(plan.nt, plan.stages);
+    cudaError_t err = allow_smem(reinterpret_cast<const void*>(kern), smem);
+    if (err != cudaSuccess) return err;
+    count_launch();
+    return launch_clusters(kern, static_cast<unsigned>(L.units * plan.split), kSplitThreads, smem, plan.split, st, maps, L,
+                           plan.stages, plan.split, dev);
+  }
   auto kern = f8 ? linear_pair_kernel<true> : linear_pair_kernel<false>;
   cudaError_t err = allow_smem(reinterpret_cast<const void*>(kern), kLinSmem);
   if (err != cudaSuccess) return err;
