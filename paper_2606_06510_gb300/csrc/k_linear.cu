@@ -29,7 +29,6 @@ struct LinUnits {                     // one product of a launch
   int64_t rows, cols;
   int64_t ntm, ntn, units;
   int64_t steps;                      // of 128 bytes of depth
-  uint32_t idesc;
   uint32_t p_mn, q_mn;
   LinEpilogue ep;
 };
@@ -50,11 +49,37 @@ constexpr uint32_t idesc_16(int M, int N, bool bf16, bool a_mn, bool b_mn) {
          (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
 }
 
+// The instruction descriptor and the operands' descriptors of the MMAs of one
+// operand type and storage, constants but for the tile's address.
+template <int TYPE, bool A_MN, bool B_MN, int M, int N>
+struct MmaShape {
+  static constexpr uint32_t idesc =
+      TYPE == OZ2_TYPE_E4M3 ? idesc_f8_f32(M, N) : idesc_16(M, N, TYPE == OZ2_TYPE_BF16, A_MN, B_MN);
+  // 32 bytes of depth an instruction: 32 bytes along a K-major row, 16 depth rows
+  // of 128 bytes in MN-major storage (in the descriptors' units of 16 bytes).
+  static constexpr uint32_t a_next = A_MN ? 128 : 2, b_next = B_MN ? 128 : 2;
+};
+
 // The descriptor of a tile in MN-major storage: 64-element (128-byte) row
 // blocks kTileBytes/2 apart (leading byte offset), groups of 8 depth rows 1024
 // bytes apart (stride byte offset), 128-byte swizzle.
 __device__ __forceinline__ uint64_t smem_desc_mn(uint32_t saddr) {
   return (smem_desc_sw128(saddr) & ~(0x3FFFull << 16)) | (static_cast<uint64_t>(kTileBytes / 2 >> 4) << 16);
+}
+
+// One lane of a whole warp, known to the compiler as one: its TMA and tensor-core
+// instructions take their operands from uniform registers as they are.  Under
+// `lane == 0` each is issued in a loop over the lanes that might be there (a
+// producer's step of two loads took 660 cycles in place of 300).
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n .reg .pred P;\n elect.sync _|P, 0xffffffff;\n selp.u32 %0, 1, 0, P;\n}\n" : "=r"(p));
+  return p != 0;
+}
+
+template <bool MN>
+__device__ __forceinline__ uint64_t operand_desc(uint32_t saddr) {
+  return MN ? smem_desc_mn(saddr) : smem_desc_sw128(saddr);
 }
 
 template <bool F8>
@@ -207,9 +232,10 @@ __device__ __forceinline__ void finish32(const float (&z)[32], bool add, bool bf
 // and 128 of Q), persistent, two accumulators in tensor memory so that a
 // tile's epilogue runs beside the next tile's products.
 // ---------------------------------------------------------------------------
-template <bool F8>
+template <int TYPE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
     linear_pair_kernel(const __grid_constant__ LinMaps maps, const __grid_constant__ LinLaunch L, Oz2Device* dev) {
+  constexpr bool F8 = TYPE == OZ2_TYPE_E4M3;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* epi = smem + kLinStages * kLinStage;
@@ -217,7 +243,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
   // bars: full[S], empty[S], acc_full[2], acc_empty[2], drain
   __shared__ uint32_t tmem_base_s;
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const bool leader = rank == 0;
   const int64_t pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
@@ -244,7 +270,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
   tc_fence_before();
   cluster_sync_all();
   tc_fence_after();
-  const uint32_t tmem = tmem_base_s;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base_s, 0);
   bool ok = true;
   pdl_wait();  // the operands are written; the set-up above overlaps that kernel's tail
 
@@ -261,34 +287,38 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
 
   if (warp == 0) {
     // ---------------- TMA producer (both CTAs) ----------------
-    if (lane == 0) {
-      const uint32_t full_leader0 = mapa_shared(full0, 0);
+    if (elect_one()) {
+      const uint32_t full_leader0 = mapa_shared(full0, 0), ring0 = smem_u32(smem);
       uint32_t it = 0, s = 0, ph = 1;
       for (int64_t u = pair; u < L.units && ok; u += npairs) {
         int64_t tm, tn;
         const int i = locate(u, &tm, &tn);
         const LinUnits& x = L.u[i];
+        // In registers: what is read from the launch's parameters is read again at
+        // every step (and each TMA instruction's operands wait for it).
         const int prow = static_cast<int>(tm * kLinTile + rank * kRows);
         const int qrow = static_cast<int>(tn * kLinTile + rank * kRows);
-        for (int64_t t = 0; t < x.steps; ++t) {
+        const int steps = static_cast<int>(x.steps);
+        const bool p_mn = x.p_mn != 0, q_mn = x.q_mn != 0;
+        const CUtensorMap *mp = &maps.p[i], *mq = &maps.q[i];
+        for (int t = 0, d = 0; t < steps; ++t, d += F8 ? 128 : 64) {
           if (!mbar_wait_bounded(empty0 + 8 * s, ph, kWaitLimit)) {
             ok = false;
             break;
           }
+          const uint32_t sa = ring0 + s * kLinStage, sb = sa + kTileBytes, bar = full_leader0 + 8 * s;
           if (leader) mbar_arrive_expect_tx(full0 + 8 * s, 2u * kLinStage);
-          const uint32_t sa = smem_u32(smem + s * kLinStage), sb = sa + kTileBytes, bar = full_leader0 + 8 * s;
-          const int d = static_cast<int>(t) * (F8 ? 128 : 64);
-          if (!x.p_mn) {
-            tma_load_2d_pair(sa, &maps.p[i], bar, d, prow);
+          if (!p_mn) {
+            tma_load_2d_pair(sa, mp, bar, d, prow);
           } else {
-            tma_load_2d_pair(sa, &maps.p[i], bar, prow, d);
-            tma_load_2d_pair(sa + kTileBytes / 2, &maps.p[i], bar, prow + 64, d);
+            tma_load_2d_pair(sa, mp, bar, prow, d);
+            tma_load_2d_pair(sa + kTileBytes / 2, mp, bar, prow + 64, d);
           }
-          if (!x.q_mn) {
-            tma_load_2d_pair(sb, &maps.q[i], bar, d, qrow);
+          if (!q_mn) {
+            tma_load_2d_pair(sb, mq, bar, d, qrow);
           } else {
-            tma_load_2d_pair(sb, &maps.q[i], bar, qrow, d);
-            tma_load_2d_pair(sb + kTileBytes / 2, &maps.q[i], bar, qrow + 64, d);
+            tma_load_2d_pair(sb, mq, bar, qrow, d);
+            tma_load_2d_pair(sb + kTileBytes / 2, mq, bar, qrow + 64, d);
           }
           ++it;
           if (++s == kLinStages) {
@@ -312,29 +342,37 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
       const uint32_t me = lane == 0;
       const uint32_t base = smem_u32(smem);
       uint32_t s = 0, ph = 0, acc = 0, accph = 1;
-      for (int64_t u = pair; u < L.units && ok; u += npairs) {
-        int64_t tm, tn;
-        const LinUnits& x = L.u[locate(u, &tm, &tn)];
-        if (x.steps == 0) continue;
-        // 32 bytes of depth an instruction: 32 bytes along a K-major row, 16
-        // depth rows of 128 bytes in MN-major storage.
-        const uint64_t pd = x.p_mn ? smem_desc_mn(base) : smem_desc_sw128(base);
-        const uint64_t qd = x.q_mn ? smem_desc_mn(base + kTileBytes) : smem_desc_sw128(base + kTileBytes);
-        const uint32_t pk = x.p_mn ? 128 : 2, qk = x.q_mn ? 128 : 2;
-        ok = mbar_wait_warp(acc_empty + 8 * acc, accph, kWaitLimit);
-        tc_fence_after();
-        for (int64_t t = 0; t < x.steps && ok; ++t) {
+      auto multiply = [&](auto shape, uint64_t pd, uint64_t qd, int steps, uint32_t d) {
+        for (int t = 0; t < steps && ok; ++t) {
           if (!(ok = mbar_wait_warp(full0 + 8 * s, ph, kWaitLimit))) break;
           tc_fence_after();
           const uint64_t a = pd + s * (kLinStage >> 4), b = qd + s * (kLinStage >> 4);
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk)
-            mma_pair<F8>(me, tmem + acc * kLinTile, a + kk * pk, b + kk * qk, x.idesc, (t | kk) ? 1u : 0u);
+            mma_pair<F8>(me, d, a + kk * shape.a_next, b + kk * shape.b_next, shape.idesc, (t | kk) ? 1u : 0u);
           mma_commit_pair_mc(me, empty0 + 8 * s, 0x3);
           if (++s == kLinStages) {
             s = 0;
             ph ^= 1;
           }
+        }
+      };
+      for (int64_t u = pair; u < L.units && ok; u += npairs) {
+        int64_t tm, tn;
+        const LinUnits& x = L.u[locate(u, &tm, &tn)];
+        if (x.steps == 0) continue;
+        ok = mbar_wait_warp(acc_empty + 8 * acc, accph, kWaitLimit);
+        tc_fence_after();
+        const int steps = static_cast<int>(x.steps);
+        if (F8 || !x.q_mn) {
+          multiply(MmaShape<TYPE, false, false, kLinTile, kLinTile>{}, operand_desc<false>(base),
+                   operand_desc<false>(base + kTileBytes), steps, tmem + acc * kLinTile);
+        } else if (!x.p_mn) {
+          multiply(MmaShape<TYPE, false, true, kLinTile, kLinTile>{}, operand_desc<false>(base),
+                   operand_desc<true>(base + kTileBytes), steps, tmem + acc * kLinTile);
+        } else {
+          multiply(MmaShape<TYPE, true, true, kLinTile, kLinTile>{}, operand_desc<true>(base),
+                   operand_desc<true>(base + kTileBytes), steps, tmem + acc * kLinTile);
         }
         if (!ok) break;
         mma_commit_pair_mc(me, acc_full + 8 * acc, 0x3);
@@ -574,10 +612,11 @@ __device__ __forceinline__ void finish8(const LinUnits& x, int64_t row, int64_t 
   put(ep.out, ep.ld_out);
 }
 
-template <bool F8, int NT>
+template <int TYPE, int NT>
 __global__ void __launch_bounds__(kSplitThreads)
     linear_split_kernel(const __grid_constant__ LinMaps maps, const __grid_constant__ LinLaunch L, int stages, int split,
                         Oz2Device* dev) {
+  constexpr bool F8 = TYPE == OZ2_TYPE_E4M3;
   constexpr int kStage = split_stage_bytes(NT);
   constexpr int kCols = NT < 32 ? 32 : NT;   // tensor memory is allocated in powers of two from 32 columns
   extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -586,7 +625,7 @@ __global__ void __launch_bounds__(kSplitThreads)
   __shared__ uint32_t tmem_base_s;
   __shared__ int failed_s;
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t rank = split > 1 ? cluster_ctarank() : 0;
   const uint32_t full0 = smem_u32(bars), empty0 = smem_u32(bars + kSplitMaxStages);
   const uint32_t done = smem_u32(bars + 2 * kSplitMaxStages);
@@ -606,7 +645,7 @@ __global__ void __launch_bounds__(kSplitThreads)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = tmem_base_s;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base_s, 0);
   pdl_wait();
 
   int64_t u = blockIdx.x / split;
@@ -618,29 +657,33 @@ __global__ void __launch_bounds__(kSplitThreads)
   const int64_t t0 = min(x.steps, static_cast<int64_t>(rank) * per), t1 = min(x.steps, t0 + per);
 
   if (warp == 0) {
-    if (lane == 0) {
+    if (elect_one()) {
       const int prow = static_cast<int>(tm * NT), qrow = static_cast<int>(tn * kRows);
       uint32_t s = 0, ph = 1;
       bool ok = true;
-      for (int64_t t = t0; t < t1; ++t) {
+      const bool p_mn = x.p_mn != 0, q_mn = x.q_mn != 0;
+      const CUtensorMap *mp = &maps.p[i], *mq = &maps.q[i];
+      const uint32_t ring0 = smem_u32(smem);
+      const int steps = static_cast<int>(t1 - t0);
+      int d = static_cast<int>(t0) * (F8 ? 128 : 64);
+      for (int t = 0; t < steps; ++t, d += F8 ? 128 : 64) {
         if (!mbar_wait_bounded(empty0 + 8 * s, ph, kWaitLimit)) {
           ok = false;
           break;
         }
-        mbar_arrive_expect_tx(full0 + 8 * s, kStage);
-        const uint32_t sa = smem_u32(smem + s * kStage), sb = sa + kTileBytes, bar = full0 + 8 * s;
-        const int d = static_cast<int>(t) * (F8 ? 128 : 64);
-        if (!x.q_mn) {
-          tma_load_2d(sa, &maps.q[i], bar, d, qrow);
+        const uint32_t sa = ring0 + s * kStage, sb = sa + kTileBytes, bar = full0 + 8 * s;
+        mbar_arrive_expect_tx(bar, kStage);
+        if (!q_mn) {
+          tma_load_2d(sa, mq, bar, d, qrow);
         } else {
-          tma_load_2d(sa, &maps.q[i], bar, qrow, d);
-          tma_load_2d(sa + kTileBytes / 2, &maps.q[i], bar, qrow + 64, d);
+          tma_load_2d(sa, mq, bar, qrow, d);
+          tma_load_2d(sa + kTileBytes / 2, mq, bar, qrow + 64, d);
         }
-        if (!x.p_mn) {
-          tma_load_2d(sb, &maps.p[i], bar, d, prow);
+        if (!p_mn) {
+          tma_load_2d(sb, mp, bar, d, prow);
         } else {
 #pragma unroll
-          for (int r = 0; r < NT; r += 64) tma_load_2d(sb + r * 128, &maps.p[i], bar, prow + r, d);
+          for (int r = 0; r < NT; r += 64) tma_load_2d(sb + r * 128, mp, bar, prow + r, d);
         }
         if (++s == static_cast<uint32_t>(stages)) {
           s = 0;
@@ -653,34 +696,42 @@ __global__ void __launch_bounds__(kSplitThreads)
         dev->timeout_site = 24;
         // Copies in flight land before the block goes.
         for (int j = 0; j < stages; ++j)
-          if (t0 + j < t1) mbar_wait_bounded(full0 + 8 * j, j < static_cast<int>(s) ? ph ^ 1 : ph, kWaitLimit);
+          if (j < steps) mbar_wait_bounded(full0 + 8 * j, j < static_cast<int>(s) ? ph ^ 1 : ph, kWaitLimit);
       }
     }
     __syncwarp();
   } else if (warp == 1) {
     const uint32_t me = lane == 0, base = smem_u32(smem);
-    const uint64_t ad = x.q_mn ? smem_desc_mn(base) : smem_desc_sw128(base);
-    const uint64_t bd = x.p_mn ? smem_desc_mn(base + kTileBytes) : smem_desc_sw128(base + kTileBytes);
-    const uint32_t ak = x.q_mn ? 128 : 2, bk = x.p_mn ? 128 : 2;
+    const int steps = static_cast<int>(t1 - t0);
     uint32_t s = 0, ph = 0;
-    for (int64_t t = t0; t < t1; ++t) {
-      if (!mbar_wait_warp(full0 + 8 * s, ph, kWaitLimit)) {
-        if (me) {
-          failed_s = 1;
-          dev->status = kStatusTimeout;
-          dev->timeout_site = 25;
+    auto multiply = [&](auto shape, uint64_t ad, uint64_t bd) {
+      for (int t = 0; t < steps; ++t) {
+        if (!mbar_wait_warp(full0 + 8 * s, ph, kWaitLimit)) {
+          if (me) {
+            failed_s = 1;
+            dev->status = kStatusTimeout;
+            dev->timeout_site = 25;
+          }
+          break;
         }
-        break;
-      }
-      tc_fence_after();
-      const uint64_t a = ad + s * (kStage >> 4), b = bd + s * (kStage >> 4);
+        tc_fence_after();
+        const uint64_t a = ad + s * (kStage >> 4), b = bd + s * (kStage >> 4);
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) mma_one<F8>(me, tmem, a + kk * ak, b + kk * bk, x.idesc, t > t0 || kk ? 1u : 0u);
-      mma_commit_by(me, empty0 + 8 * s);
-      if (++s == static_cast<uint32_t>(stages)) {
-        s = 0;
-        ph ^= 1;
+        for (int kk = 0; kk < 4; ++kk)
+          mma_one<F8>(me, tmem, a + kk * shape.a_next, b + kk * shape.b_next, shape.idesc, (t | kk) ? 1u : 0u);
+        mma_commit_by(me, empty0 + 8 * s);
+        if (++s == static_cast<uint32_t>(stages)) {
+          s = 0;
+          ph ^= 1;
+        }
       }
+    };
+    if (F8 || !x.q_mn) {
+      multiply(MmaShape<TYPE, false, false, kRows, NT>{}, operand_desc<false>(base), operand_desc<false>(base + kTileBytes));
+    } else if (!x.p_mn) {
+      multiply(MmaShape<TYPE, true, false, kRows, NT>{}, operand_desc<true>(base), operand_desc<false>(base + kTileBytes));
+    } else {
+      multiply(MmaShape<TYPE, true, true, kRows, NT>{}, operand_desc<true>(base), operand_desc<true>(base + kTileBytes));
     }
     mma_commit_by(me, done);
     __syncwarp();
@@ -824,12 +875,12 @@ LinPlan choose_plan(const LinProduct* products, int count, int type) {
 }
 
 using SplitKernel = void (*)(const LinMaps, const LinLaunch, int, int, Oz2Device*);
-template <bool F8>
+template <int TYPE>
 SplitKernel split_kernel(int nt) {
-  return nt == 16   ? linear_split_kernel<F8, 16>
-         : nt == 32 ? linear_split_kernel<F8, 32>
-         : nt == 64 ? linear_split_kernel<F8, 64>
-                    : linear_split_kernel<F8, 128>;
+  return nt == 16   ? linear_split_kernel<TYPE, 16>
+         : nt == 32 ? linear_split_kernel<TYPE, 32>
+         : nt == 64 ? linear_split_kernel<TYPE, 64>
+                    : linear_split_kernel<TYPE, 128>;
 }
 
 // As launch_dependent, in clusters.
@@ -858,7 +909,6 @@ cudaError_t launch_clusters(void (*kernel)(KArgs...), unsigned grid, unsigned bl
 cudaError_t launch_linear(const LinProduct* products, int count, int type, Oz2Device* dev, cudaStream_t st) {
   LinMaps maps{};
   LinLaunch L{};
-  const bool f8 = type == OZ2_TYPE_E4M3;
   const int64_t step = 128 / type_bytes(type);
   const LinPlan plan = choose_plan(products, count, type);
   const int tile_rows = plan.nt ? plan.nt : kLinTile, tile_cols = plan.nt ? kRows : kLinTile;
@@ -873,10 +923,6 @@ cudaError_t launch_linear(const LinProduct* products, int count, int type, Oz2De
     x.steps = (p.depth + step - 1) / step;
     x.p_mn = p.p_mn;
     x.q_mn = p.q_mn;
-    // The pairs' A is P; the split kernel's is Q.
-    const int M = plan.nt ? kRows : kLinTile, N = plan.nt ? plan.nt : kLinTile;
-    x.idesc = f8 ? idesc_f8_f32(M, N)
-                 : idesc_16(M, N, type == OZ2_TYPE_BF16, plan.nt ? p.q_mn : p.p_mn, plan.nt ? p.p_mn : p.q_mn);
     x.ep = p.ep;
     L.units += x.units;
     if (x.steps && (!make_operand_map(&maps.p[i], p.p, p.rows, p.depth, p.ldp, type, p.p_mn, plan.nt ? plan.nt : kRows) ||
@@ -887,7 +933,9 @@ cudaError_t launch_linear(const LinProduct* products, int count, int type, Oz2De
   if (L.units == 0) return cudaSuccess;
   if (plan.nt) {
     if (L.units * plan.split > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
-    SplitKernel kern = f8 ? split_kernel<true>(plan.nt) : split_kernel<false>(plan.nt);
+    SplitKernel kern = type == OZ2_TYPE_BF16  ? split_kernel<OZ2_TYPE_BF16>(plan.nt)
+                       : type == OZ2_TYPE_F16 ? split_kernel<OZ2_TYPE_F16>(plan.nt)
+                                              : split_kernel<OZ2_TYPE_E4M3>(plan.nt);
     const size_t smem = split_smem(plan.nt, plan.stages);
     cudaError_t err = allow_smem(reinterpret_cast<const void*>(kern), smem);
     if (err != cudaSuccess) return err;
@@ -895,7 +943,9 @@ cudaError_t launch_linear(const LinProduct* products, int count, int type, Oz2De
     return launch_clusters(kern, static_cast<unsigned>(L.units * plan.split), kSplitThreads, smem, plan.split, st, maps, L,
                            plan.stages, plan.split, dev);
   }
-  auto kern = f8 ? linear_pair_kernel<true> : linear_pair_kernel<false>;
+  auto kern = type == OZ2_TYPE_BF16  ? linear_pair_kernel<OZ2_TYPE_BF16>
+              : type == OZ2_TYPE_F16 ? linear_pair_kernel<OZ2_TYPE_F16>
+                                     : linear_pair_kernel<OZ2_TYPE_E4M3>;
   cudaError_t err = allow_smem(reinterpret_cast<const void*>(kern), kLinSmem);
   if (err != cudaSuccess) return err;
   const int64_t pairs =
