@@ -16,25 +16,35 @@
 namespace oz2 {
 namespace {
 
-constexpr int kLinThreads = 320;      // TMA warp, MMA warp, 8 epilogue warps
+constexpr int kLinEpiWarps = 16;
+constexpr int kLinThreads = 64 + 32 * kLinEpiWarps;  // TMA warp, MMA warp, epilogue warps
 constexpr int kLinStages = 5;
-constexpr int kLinEpiWarps = 8;
 constexpr int kLinTile = 256;         // rows and columns of a CTA pair's tile
 constexpr int kLinStage = 2 * kTileBytes;
-constexpr int kStageBytes = 32 * 128; // an epilogue warp's 32 rows × 128 bytes
-constexpr int kLinCols = 128;         // columns of an epilogue warp
+constexpr int kLinCols = kLinTile / (kLinEpiWarps / 4);  // columns of an epilogue warp
+constexpr int kChunk = 32;            // of which it takes this many at a time
+constexpr int kStageBytes = 32 * 2 * kChunk;             // an epilogue warp's 32 rows × 32 columns of 16 bits
 constexpr int kLinSmem = 1024 + kLinStages * kLinStage + kLinEpiWarps * (kStageBytes + 2 * 4 * kLinCols) + 256;
+constexpr int kMaxPairSplit = 16;     // parts of a tile's depth on pairs
+constexpr int kPartFloats = kLinTile * kLinTile;         // a part of a tile's sums in the workspace
 
 struct LinUnits {                     // one product of a launch
   int64_t rows, cols;
-  int64_t ntm, ntn, units;
-  int64_t steps;                      // of 128 bytes of depth
+  int ntm, ntn, units;
+  int steps;                          // of 128 bytes of depth
+  int split;                          // on pairs: parts that the depth of each tile is cut into
   uint32_t p_mn, q_mn;
   LinEpilogue ep;
 };
 struct LinLaunch {
   int count;
-  int64_t units;
+  int units;                          // whole tiles (of the products with split = 1)
+  // On pairs: the parts of the tiles of products with split > 1, one to a pair from
+  // the first on; the pairs without one take whole tiles in `ahead` rounds of their
+  // own meanwhile.
+  int parts, ahead;
+  float* sums;                        // the parts' sums: kPartFloats each
+  int* arrived;                       // parts done, for each of their tiles, CTA and epilogue warp
   LinUnits u[kMaxProducts];
 };
 struct LinMaps {
@@ -98,72 +108,84 @@ __device__ __forceinline__ void mma_pair(uint32_t me, uint32_t d_tmem, uint64_t 
 
 // Tile (tm, tn) of unit u: bands of 8 tile rows, so that the tiles in flight
 // share operand rows in L2.
-__device__ __forceinline__ void unit_tile(const LinUnits& x, int64_t u, int64_t* tm, int64_t* tn) {
-  const int64_t per = 8 * x.ntn, band = u / per, in = u - band * per;
-  const int64_t h = min(static_cast<int64_t>(8), x.ntm - band * 8);
+__device__ __forceinline__ void unit_tile(const LinUnits& x, int u, int* tm, int* tn) {
+  const int per = 8 * x.ntn, band = u / per, in = u - band * per;
+  const int h = min(8, x.ntm - band * 8);
   *tn = in / h;
   *tm = band * 8 + (in - *tn * h);
 }
 
-// --- an epilogue warp's 32 rows × 128 bytes in shared memory --------------------
-// 16-byte piece c of row r at r·128 + (c ^ (r & 7))·16: a thread's own row and
-// eight threads' one row are both free of bank conflicts.
-__device__ __forceinline__ uint32_t piece_at(int row, int c) { return row * 128 + ((c ^ (row & 7)) << 4); }
+// --- an epilogue warp's 32 rows × 64 bytes in shared memory ---------------------
+// 16-byte piece c of row r at r·64 + (c ^ (r/2 & 3))·16: eight threads' own rows and
+// two rows' eight pieces are both free of bank conflicts.
+__device__ __forceinline__ uint32_t piece_at(int row, int c) { return row * 64 + ((c ^ (row >> 1 & 3)) << 4); }
 
 __device__ __forceinline__ uint4 lds128(const uint8_t* p) { return *reinterpret_cast<const uint4*>(p); }
 __device__ __forceinline__ void sts128(uint8_t* p, uint4 v) { *reinterpret_cast<uint4*>(p) = v; }
 
-// Rows row0.. and columns col0.. (64 of 16 bits) between global and shared memory, a
-// whole warp; what lies past the matrix is not touched.
 __device__ __forceinline__ bool vec_ok(const void* p, int64_t ld, int bytes) {
   return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(ld * bytes)) & 15) == 0;
 }
-__device__ __forceinline__ void fetch16(const LinUnits& x, const void* src, int64_t ld, int64_t row0, int64_t col0,
-                                        int lane, uint8_t* buf) {
+
+// A warp's 32 rows × 32 columns of 16 bits between global and shared memory; what
+// lies past the matrix is not touched.  The fetch is in two halves, so that its
+// loads can be on their way early.
+struct Fetched {
+  uint4 v[4];
+};
+__device__ __forceinline__ void fetch_begin(const LinUnits& x, const void* src, int64_t ld, int64_t row0, int64_t col0,
+                                            int lane, Fetched& f) {
   const uint16_t* s = static_cast<const uint16_t*>(src);
-  if (vec_ok(src, ld, 2) && col0 + 64 <= x.cols) {
+  if (vec_ok(src, ld, 2) && col0 + kChunk <= x.cols) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int r = 4 * i + (lane >> 3), c = lane & 7;
-      if (row0 + r < x.rows)
-        sts128(buf + piece_at(r, c), __ldg(reinterpret_cast<const uint4*>(s + (row0 + r) * ld + col0 + 8 * c)));
+    for (int i = 0; i < 4; ++i) {
+      const int r = 8 * i + (lane >> 2), c = lane & 3;
+      f.v[i] = make_uint4(0, 0, 0, 0);
+      if (row0 + r < x.rows) f.v[i] = __ldg(reinterpret_cast<const uint4*>(s + (row0 + r) * ld + col0 + 8 * c));
     }
-  } else {
-    for (int r = 0; r < 32 && row0 + r < x.rows; ++r)
+  }
+}
+__device__ __forceinline__ void fetch_end(const LinUnits& x, const void* src, int64_t ld, int64_t row0, int64_t col0,
+                                          int lane, uint8_t* buf, const Fetched& f) {
+  const uint16_t* s = static_cast<const uint16_t*>(src);
+  if (vec_ok(src, ld, 2) && col0 + kChunk <= x.cols) {
 #pragma unroll
-      for (int e = lane; e < 64; e += 32)
-        if (col0 + e < x.cols)
-          *reinterpret_cast<uint16_t*>(buf + piece_at(r, e >> 3) + 2 * (e & 7)) = __ldg(s + (row0 + r) * ld + col0 + e);
+    for (int i = 0; i < 4; ++i) sts128(buf + piece_at(8 * i + (lane >> 2), lane & 3), f.v[i]);
+  } else if (col0 + lane < x.cols) {
+#pragma unroll 8
+    for (int r = 0; r < 32; ++r)
+      if (row0 + r < x.rows)
+        *reinterpret_cast<uint16_t*>(buf + piece_at(r, lane >> 3) + 2 * (lane & 7)) =
+            __ldg(s + (row0 + r) * ld + col0 + lane);
   }
 }
 __device__ __forceinline__ void store16(const LinUnits& x, void* dst, int64_t ld, int64_t row0, int64_t col0, int lane,
                                         const uint8_t* buf) {
   uint16_t* d = static_cast<uint16_t*>(dst);
-  if (vec_ok(dst, ld, 2) && col0 + 64 <= x.cols) {
+  if (vec_ok(dst, ld, 2) && col0 + kChunk <= x.cols) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int r = 4 * i + (lane >> 3), c = lane & 7;
+    for (int i = 0; i < 4; ++i) {
+      const int r = 8 * i + (lane >> 2), c = lane & 3;
       if (row0 + r < x.rows)
         *reinterpret_cast<uint4*>(d + (row0 + r) * ld + col0 + 8 * c) = lds128(buf + piece_at(r, c));
     }
-  } else {
-    for (int r = 0; r < 32 && row0 + r < x.rows; ++r)
-#pragma unroll
-      for (int e = lane; e < 64; e += 32)
-        if (col0 + e < x.cols)
-          d[(row0 + r) * ld + col0 + e] = *reinterpret_cast<const uint16_t*>(buf + piece_at(r, e >> 3) + 2 * (e & 7));
+  } else if (col0 + lane < x.cols) {
+#pragma unroll 8
+    for (int r = 0; r < 32; ++r)
+      if (row0 + r < x.rows)
+        d[(row0 + r) * ld + col0 + lane] = *reinterpret_cast<const uint16_t*>(buf + piece_at(r, lane >> 3) + 2 * (lane & 7));
   }
 }
-// 32 columns of FP32, stored or added to.
+// 16 columns of FP32, stored or added to.
 __device__ __forceinline__ void store32(const LinUnits& x, void* dst, int64_t ld, int64_t row0, int64_t col0, int lane,
                                         const uint8_t* buf, bool add) {
   float* d = static_cast<float*>(dst);
-  for (int r = 0; r < 32 && row0 + r < x.rows; ++r) {
-    if (col0 + lane < x.cols) {
-      float* at = d + (row0 + r) * ld + col0 + lane;
-      const float v = *reinterpret_cast<const float*>(buf + piece_at(r, lane >> 2) + 4 * (lane & 3));
-      *at = add ? *at + v : v;
-    }
+  const int c = lane & 15;
+  if (col0 + c >= x.cols) return;
+  for (int r = lane >> 4; r < 32 && row0 + r < x.rows; r += 2) {
+    float* at = d + (row0 + r) * ld + col0 + c;
+    const float v = *reinterpret_cast<const float*>(buf + piece_at(r, c >> 2) + 4 * (c & 3));
+    *at = add ? *at + v : v;
   }
 }
 
@@ -205,10 +227,10 @@ __device__ __forceinline__ void scaled(const float* scale_s, const float* bias_s
 
 // act(z) + r for 32 columns, into the warp's buffer (which holds r there).
 template <int ACT>
-__device__ __forceinline__ void finish32(const float (&z)[32], bool add, bool bf16, uint8_t* buf, int lane, int c) {
+__device__ __forceinline__ void finish32(const float (&z)[32], bool add, bool bf16, uint8_t* buf, int lane) {
 #pragma unroll
   for (int j = 0; j < 32; j += 8) {
-    uint8_t* at = buf + piece_at(lane, (c + j) >> 3);
+    uint8_t* at = buf + piece_at(lane, j >> 3);
     float y[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] = activate<ACT>(z[j + e]);
@@ -227,10 +249,65 @@ __device__ __forceinline__ void finish32(const float (&z)[32], bool add, bool bf
   }
 }
 
+// --- the work of a CTA pair --------------------------------------------------------
+// First a part of a tile whose depth is split, then whole tiles.  The parts come
+// first so that the last of a tile's parts, which joins them, is not at the launch's
+// end, and all at once so that tiles that share rows of an operand read the same
+// depth at the same time.
+struct Piece {
+  int i;               // product
+  int tm, tn;          // tile
+  int t0, t1;          // steps of its depth
+  int parts;           // of the tile (1: whole)
+  int slot, first_slot, stride;  // of its sums: this part's, the first part's, from part to part
+  int tile;            // number among the tiles whose depth is split
+};
+struct PairWork {
+  const LinLaunch& L;
+  int pair, npairs, round;
+  __device__ PairWork(const LinLaunch& launch, int p, int np) : L(launch), pair(p), npairs(np), round(p < launch.parts ? -1 : 0) {}
+  __device__ bool next(Piece& p) {
+    if (round < 0) {
+      round = L.ahead;
+      const int first = L.u[0].split > 1 ? L.u[0].units * L.u[0].split : 0;
+      p.i = pair >= first ? 1 : 0;
+      const LinUnits& x = L.u[p.i];
+      const int v = p.i ? pair - first : pair, part = v / x.units, tile = v - part * x.units;
+      const int per = (x.steps + x.split - 1) / x.split;
+      unit_tile(x, tile, &p.tm, &p.tn);
+      p.t0 = min(x.steps, part * per);
+      p.t1 = min(x.steps, p.t0 + per);
+      p.parts = x.split;
+      p.slot = pair;
+      p.first_slot = pair - part * x.units;
+      p.stride = x.units;
+      p.tile = tile + (p.i && first ? L.u[0].units : 0);
+      return true;
+    }
+    const int others = npairs - L.parts;
+    int u = round < L.ahead ? round * others + pair - L.parts : L.ahead * others + (round - L.ahead) * npairs + pair;
+    ++round;
+    if (u >= L.units) return false;
+    const int first = L.u[0].split > 1 ? 0 : L.u[0].units;
+    p.i = u >= first ? 1 : 0;
+    const LinUnits& x = L.u[p.i];
+    unit_tile(x, p.i ? u - first : u, &p.tm, &p.tn);
+    p.t0 = 0;
+    p.t1 = x.steps;
+    p.parts = 1;
+    return true;
+  }
+};
+
 // ---------------------------------------------------------------------------
 // Tiles of 256 × 256 on CTA pairs (cta_group::2: each CTA stages 128 rows of P
 // and 128 of Q), persistent, two accumulators in tensor memory so that a
 // tile's epilogue runs beside the next tile's products.
+//
+// A product of few tiles and a long depth (a weight's gradient over many tokens)
+// has its tiles' depth split over pairs.  A part's sums go to the workspace in FP32;
+// each epilogue warp counts its own 32 × 64 corner in, and the warp that comes last
+// adds up the tile's parts, in their order whoever is last, and finishes them.
 // ---------------------------------------------------------------------------
 template <int TYPE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
@@ -246,7 +323,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const bool leader = rank == 0;
-  const int64_t pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
+  const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
   const uint32_t full0 = smem_u32(bars), empty0 = smem_u32(bars + kLinStages);
   const uint32_t acc_full = smem_u32(bars + 2 * kLinStages), acc_empty = smem_u32(bars + 2 * kLinStages + 2);
   const uint32_t drain_bar = smem_u32(bars + 2 * kLinStages + 4);
@@ -274,34 +351,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
   bool ok = true;
   pdl_wait();  // the operands are written; the set-up above overlaps that kernel's tail
 
-  // Product and tile of the pair's unit u.
-  auto locate = [&](int64_t u, int64_t* tm, int64_t* tn) {
-    int i = 0;
-    if (L.count > 1 && u >= L.u[0].units) {
-      u -= L.u[0].units;
-      i = 1;
-    }
-    unit_tile(L.u[i], u, tm, tn);
-    return i;
-  };
+  PairWork work(L, pair, npairs);
+  Piece pc;
 
   if (warp == 0) {
     // ---------------- TMA producer (both CTAs) ----------------
     if (elect_one()) {
       const uint32_t full_leader0 = mapa_shared(full0, 0), ring0 = smem_u32(smem);
       uint32_t it = 0, s = 0, ph = 1;
-      for (int64_t u = pair; u < L.units && ok; u += npairs) {
-        int64_t tm, tn;
-        const int i = locate(u, &tm, &tn);
-        const LinUnits& x = L.u[i];
+      while (ok && work.next(pc)) {
+        const LinUnits& x = L.u[pc.i];
         // In registers: what is read from the launch's parameters is read again at
         // every step (and each TMA instruction's operands wait for it).
-        const int prow = static_cast<int>(tm * kLinTile + rank * kRows);
-        const int qrow = static_cast<int>(tn * kLinTile + rank * kRows);
-        const int steps = static_cast<int>(x.steps);
+        const int prow = pc.tm * kLinTile + rank * kRows;
+        const int qrow = pc.tn * kLinTile + rank * kRows;
+        const int t1 = pc.t1;
         const bool p_mn = x.p_mn != 0, q_mn = x.q_mn != 0;
-        const CUtensorMap *mp = &maps.p[i], *mq = &maps.q[i];
-        for (int t = 0, d = 0; t < steps; ++t, d += F8 ? 128 : 64) {
+        const CUtensorMap *mp = &maps.p[pc.i], *mq = &maps.q[pc.i];
+        for (int t = pc.t0, d = t * (F8 ? 128 : 64); t < t1; ++t, d += F8 ? 128 : 64) {
           if (!mbar_wait_bounded(empty0 + 8 * s, ph, kWaitLimit)) {
             ok = false;
             break;
@@ -357,13 +424,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
           }
         }
       };
-      for (int64_t u = pair; u < L.units && ok; u += npairs) {
-        int64_t tm, tn;
-        const LinUnits& x = L.u[locate(u, &tm, &tn)];
-        if (x.steps == 0) continue;
+      while (ok && work.next(pc)) {
+        const LinUnits& x = L.u[pc.i];
+        if (pc.t0 == pc.t1) continue;
         ok = mbar_wait_warp(acc_empty + 8 * acc, accph, kWaitLimit);
         tc_fence_after();
-        const int steps = static_cast<int>(x.steps);
+        const int steps = pc.t1 - pc.t0;
         if (F8 || !x.q_mn) {
           multiply(MmaShape<TYPE, false, false, kLinTile, kLinTile>{}, operand_desc<false>(base),
                    operand_desc<false>(base + kTileBytes), steps, tmem + acc * kLinTile);
@@ -388,20 +454,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
     }
     __syncwarp();
   } else {
-    // ---------------- epilogue (warps 2..9, both CTAs) ----------------
-    const int q = warp & 3, h = (warp - 2) >> 2;  // TMEM lane quarter, column half
-    uint8_t* buf = epi + (warp - 2) * kStageBytes;
-    float* bias_s = reinterpret_cast<float*>(epi + kLinEpiWarps * kStageBytes) + (warp - 2) * 2 * kLinCols;
+    // ---------------- epilogue (warps 2..17, both CTAs) ----------------
+    const int ew = warp - 2;
+    const int q = warp & 3, h = ew >> 2;  // TMEM lane quarter, column quarter
+    uint8_t* buf = epi + ew * kStageBytes;
+    float* bias_s = reinterpret_cast<float*>(epi + kLinEpiWarps * kStageBytes) + ew * 2 * kLinCols;
     float* scale_s = bias_s + kLinCols;
     const uint32_t acc_empty_leader = mapa_shared(acc_empty, 0);
     uint32_t acc = 0, accph = 0;
-    for (int64_t u = pair; u < L.units; u += npairs) {
-      int64_t tm, tn;
-      const LinUnits& x = L.u[locate(u, &tm, &tn)];
+    while (work.next(pc)) {
+      const LinUnits& x = L.u[pc.i];
       const LinEpilogue& ep = x.ep;
-      const int64_t row0 = tm * kLinTile + rank * kRows + 32 * q, col0 = tn * kLinTile + kLinCols * h;
-      const bool bf16 = ep.out_type == OZ2_TYPE_BF16, scales = ep.row_scale != nullptr;
+      const int64_t row0 = pc.tm * kLinTile + rank * kRows + 32 * q, col0 = pc.tn * kLinTile + kLinCols * h;
+      const bool bf16 = ep.out_type == OZ2_TYPE_BF16, scales = ep.row_scale != nullptr, add = ep.add != nullptr;
+      const bool sums = pc.t1 > pc.t0;
       __syncwarp();
+#pragma unroll
       for (int c = lane; c < kLinCols; c += 32) {
         const int64_t j = col0 + c;
         float b = 0.f;
@@ -412,8 +480,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
         if (scales) scale_s[c] = j < x.cols ? __ldg(ep.col_scale + j) : 0.f;
       }
       const float row_scale = scales && row0 + lane < x.rows ? __ldg(ep.row_scale + row0 + lane) : 0.f;
+      Fetched r;
+      if (add) fetch_begin(x, ep.add, ep.ld_add, row0, col0, lane, r);
       __syncwarp();
-      if (x.steps) {
+      if (sums) {
         if (!mbar_wait_bounded(acc_full + 8 * acc, accph, kWaitLimit)) ok = false;
         if (!__all_sync(0xffffffffu, ok)) {
           ok = false;
@@ -422,74 +492,110 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
         tc_fence_after();
       }
       const uint32_t at = tmem + (static_cast<uint32_t>(32 * q) << 16) + acc * kLinTile + kLinCols * h;
-      auto sums = [&](int c, float (&z)[32]) {
+      auto release = [&] {
+        if (sums) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_remote_relaxed(acc_empty_leader + 8 * acc);
+          acc ^= 1;
+          if (acc == 0) accph ^= 1;
+        }
+      };
+      // This warp's corner of a slot: chunks of 32 columns, four at a time, 32 rows.
+      const int corner = ((rank * kLinEpiWarps + ew) * (kLinCols / 4)) * 128 + 4 * lane;
+      if (pc.parts > 1) {
+        float* to = L.sums + static_cast<int64_t>(pc.slot) * kPartFloats + corner;
+#pragma unroll 1
+        for (int c = 0; c < kLinCols; c += kChunk) {
+          uint32_t v[32];
+          if (sums) {
+            tmem_ld32(at + c, v);
+            tmem_ld_wait();
+          } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = 0u;
+          }
+#pragma unroll
+          for (int j = 0; j < 32; j += 4)
+            __stcg(reinterpret_cast<uint4*>(to + (c + j) * 32), make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]));
+        }
+        release();
+        __threadfence();
+        __syncwarp();
+        int before = 0;
+        if (lane == 0)
+          before = atomicAdd(L.arrived + (pc.tile * 2 + rank) * kLinEpiWarps + ew, 1);
+        if (__shfl_sync(0xffffffffu, before, 0) != pc.parts - 1) continue;
+        __threadfence();
+      }
+      auto load = [&](int c, float (&z)[32]) {
         uint32_t v[32];
-        if (x.steps) {
+        if (pc.parts > 1) {
+#pragma unroll
+          for (int j = 0; j < 32; j += 4) {
+            const float4 a = __ldcg(reinterpret_cast<const float4*>(L.sums + static_cast<int64_t>(pc.first_slot) * kPartFloats +
+                                                                    corner + (c + j) * 32));
+            z[j] = a.x, z[j + 1] = a.y, z[j + 2] = a.z, z[j + 3] = a.w;
+          }
+#pragma unroll 2
+          for (int p = 1; p < pc.parts; ++p) {
+            const float* from = L.sums + static_cast<int64_t>(pc.first_slot + p * pc.stride) * kPartFloats + corner;
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+              const float4 a = __ldcg(reinterpret_cast<const float4*>(from + (c + j) * 32));
+              z[j] += a.x, z[j + 1] += a.y, z[j + 2] += a.z, z[j + 3] += a.w;
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(z[j]);
+        } else if (sums) {
           tmem_ld32(at + c, v);
           tmem_ld_wait();
+          if (c == kLinCols - kChunk) release();
         } else {
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = 0u;
         }
         scaled(scale_s, bias_s, row_scale, v, c, scales, z);
       };
-      auto release = [&] {
-        if (x.steps) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_remote_relaxed(acc_empty_leader + 8 * acc);
-        }
-      };
-      if (ep.out_type == OZ2_TYPE_F32) {
-        for (int c = 0; c < kLinCols; c += 32) {
-          float z[32];
-          sums(c, z);
-          if (c == kLinCols - 32) release();
+#pragma unroll 1
+      for (int c = 0; c < kLinCols; c += kChunk) {
+        float z[32];
+        load(c, z);
+        if (ep.out_type == OZ2_TYPE_F32) {
 #pragma unroll
-          for (int j = 0; j < 32; j += 4)
-            sts128(buf + piece_at(lane, j >> 2), make_uint4(__float_as_uint(z[j]), __float_as_uint(z[j + 1]),
-                                                            __float_as_uint(z[j + 2]), __float_as_uint(z[j + 3])));
+          for (int g = 0; g < 32; g += 16) {
+#pragma unroll
+            for (int j = 0; j < 16; j += 4)
+              sts128(buf + piece_at(lane, j >> 2), make_uint4(__float_as_uint(z[g + j]), __float_as_uint(z[g + j + 1]),
+                                                              __float_as_uint(z[g + j + 2]), __float_as_uint(z[g + j + 3])));
+            __syncwarp();
+            store32(x, ep.out, ep.ld_out, row0, col0 + c + g, lane, buf, ep.accumulate != 0);
+            __syncwarp();
+          }
+          continue;
+        }
+        if (ep.pre) {
+          finish32<OZ2_ACT_NONE>(z, false, bf16, buf, lane);
           __syncwarp();
-          store32(x, ep.out, ep.ld_out, row0, col0 + c, lane, buf, ep.accumulate != 0);
+          store16(x, ep.pre, ep.ld_pre, row0, col0 + c, lane, buf);
           __syncwarp();
         }
-      } else {
-        for (int c0 = 0; c0 < kLinCols; c0 += 64) {
-          if (ep.pre) {
-            for (int c = c0; c < c0 + 64; c += 32) {
-              float z[32];
-              sums(c, z);
-              finish32<OZ2_ACT_NONE>(z, false, bf16, buf, lane, c - c0);
-            }
-            __syncwarp();
-            store16(x, ep.pre, ep.ld_pre, row0, col0 + c0, lane, buf);
-            __syncwarp();
-          }
-          if (ep.add) {
-            fetch16(x, ep.add, ep.ld_add, row0, col0 + c0, lane, buf);
-            __syncwarp();
-          }
-          for (int c = c0; c < c0 + 64; c += 32) {
-            float z[32];
-            sums(c, z);
-            if (c == kLinCols - 32) release();
-            const bool add = ep.add != nullptr;
-            switch (ep.act) {
-              case OZ2_ACT_RELU: finish32<OZ2_ACT_RELU>(z, add, bf16, buf, lane, c - c0); break;
-              case OZ2_ACT_GELU: finish32<OZ2_ACT_GELU>(z, add, bf16, buf, lane, c - c0); break;
-              case OZ2_ACT_GELU_TANH: finish32<OZ2_ACT_GELU_TANH>(z, add, bf16, buf, lane, c - c0); break;
-              case OZ2_ACT_SILU: finish32<OZ2_ACT_SILU>(z, add, bf16, buf, lane, c - c0); break;
-              default: finish32<OZ2_ACT_NONE>(z, add, bf16, buf, lane, c - c0);
-            }
-          }
-          __syncwarp();
-          store16(x, ep.out, ep.ld_out, row0, col0 + c0, lane, buf);
+        if (add) {
+          fetch_end(x, ep.add, ep.ld_add, row0, col0 + c, lane, buf, r);
+          if (c + kChunk < kLinCols) fetch_begin(x, ep.add, ep.ld_add, row0, col0 + c + kChunk, lane, r);
           __syncwarp();
         }
-      }
-      if (x.steps) {
-        acc ^= 1;
-        if (acc == 0) accph ^= 1;
+        switch (ep.act) {
+          case OZ2_ACT_RELU: finish32<OZ2_ACT_RELU>(z, add, bf16, buf, lane); break;
+          case OZ2_ACT_GELU: finish32<OZ2_ACT_GELU>(z, add, bf16, buf, lane); break;
+          case OZ2_ACT_GELU_TANH: finish32<OZ2_ACT_GELU_TANH>(z, add, bf16, buf, lane); break;
+          case OZ2_ACT_SILU: finish32<OZ2_ACT_SILU>(z, add, bf16, buf, lane); break;
+          default: finish32<OZ2_ACT_NONE>(z, add, bf16, buf, lane);
+        }
+        __syncwarp();
+        store16(x, ep.out, ep.ld_out, row0, col0 + c, lane, buf);
+        __syncwarp();
       }
     }
     if (!ok) {
@@ -648,24 +754,24 @@ __global__ void __launch_bounds__(kSplitThreads)
   const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base_s, 0);
   pdl_wait();
 
-  int64_t u = blockIdx.x / split;
+  int u = blockIdx.x / split;
   const int i = L.count > 1 && u >= L.u[0].units ? 1 : 0;
   const LinUnits& x = L.u[i];
   if (i) u -= L.u[0].units;
-  const int64_t tn = u / x.ntm, tm = u - tn * x.ntm;   // tiles that share Q's rows run together
-  const int64_t per = (x.steps + split - 1) / split;
-  const int64_t t0 = min(x.steps, static_cast<int64_t>(rank) * per), t1 = min(x.steps, t0 + per);
+  const int tn = u / x.ntm, tm = u - tn * x.ntm;   // tiles that share Q's rows run together
+  const int per = (x.steps + split - 1) / split;
+  const int t0 = min(x.steps, static_cast<int>(rank) * per), t1 = min(x.steps, t0 + per);
 
   if (warp == 0) {
     if (elect_one()) {
-      const int prow = static_cast<int>(tm * NT), qrow = static_cast<int>(tn * kRows);
+      const int prow = tm * NT, qrow = tn * kRows;
       uint32_t s = 0, ph = 1;
       bool ok = true;
       const bool p_mn = x.p_mn != 0, q_mn = x.q_mn != 0;
       const CUtensorMap *mp = &maps.p[i], *mq = &maps.q[i];
       const uint32_t ring0 = smem_u32(smem);
-      const int steps = static_cast<int>(t1 - t0);
-      int d = static_cast<int>(t0) * (F8 ? 128 : 64);
+      const int steps = t1 - t0;
+      int d = t0 * (F8 ? 128 : 64);
       for (int t = 0; t < steps; ++t, d += F8 ? 128 : 64) {
         if (!mbar_wait_bounded(empty0 + 8 * s, ph, kWaitLimit)) {
           ok = false;
@@ -702,7 +808,7 @@ __global__ void __launch_bounds__(kSplitThreads)
     __syncwarp();
   } else if (warp == 1) {
     const uint32_t me = lane == 0, base = smem_u32(smem);
-    const int steps = static_cast<int>(t1 - t0);
+    const int steps = t1 - t0;
     uint32_t s = 0, ph = 0;
     auto multiply = [&](auto shape, uint64_t ad, uint64_t bd) {
       for (int t = 0; t < steps; ++t) {
@@ -814,65 +920,114 @@ bool make_operand_map(CUtensorMap* map, const void* base, int64_t rows, int64_t 
 
 namespace {
 
-// How a launch runs: on CTA pairs (nt = 0), or in tiles of nt rows with the depth
-// split over `split` CTAs and `stages` of operands in flight.
-struct LinPlan {
-  int nt = 0, split = 1, stages = 0;
-};
+int64_t steps_of(const LinProduct& p, int type) {
+  const int64_t step = 128 / type_bytes(type);
+  return (p.depth + step - 1) / step;
+}
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// The plan of least estimated time.  The estimates (µs) follow a model of one
-// launch: the operands' bytes through an SM's share of L2, the tensor cores' cycles,
-// waves of CTAs, and fixed costs, each fitted to measurements on one GB300.
-LinPlan choose_plan(const LinProduct* products, int count, int type) {
-  const int64_t step = 128 / type_bytes(type), sms = num_sms();
-  constexpr double kGHz = 1.85;
+// The estimates (cycles of an SM) behind a plan, fitted to measurements on one
+// GB300: a step of a pair's tile 535, a tile's epilogue and start 1500, the launch's
+// own start and last epilogue 10000; the exchange of a split tile's parts 12000.
+constexpr double kPairStep = 535, kPairTile = 1500, kPairLaunch = 10000, kExchange = 12000;
+
+}  // namespace
+
+LinPlan plan_linear(const LinProduct* products, int count, int type) {
+  const int64_t sms = num_sms(), pairs = sms / 2;
+  int64_t tiles[kMaxProducts], steps[kMaxProducts];
   bool p_mn = false;
-  double pair_work = 0;
-  int64_t pair_units = 0, max_steps = 0;
+  int64_t units = 0;
+  double work = 0, longest = 0;
   for (int i = 0; i < count; ++i) {
     const LinProduct& p = products[i];
-    const int64_t units = ((p.rows + kLinTile - 1) / kLinTile) * ((p.cols + kLinTile - 1) / kLinTile);
-    const int64_t steps = (p.depth + step - 1) / step;
-    pair_units += units;
-    max_steps = std::max(max_steps, steps);
-    pair_work += static_cast<double>(units) * (steps * 540.0 + 300.0);
+    tiles[i] = ceil_div(p.rows, kLinTile) * ceil_div(p.cols, kLinTile);
+    steps[i] = steps_of(p, type);
     p_mn = p_mn || p.p_mn;
+    const double tile = steps[i] * kPairStep + kPairTile;
+    units += tiles[i];
+    work += tiles[i] * tile;
+    if (tiles[i]) longest = std::max(longest, tile);
   }
-  const int64_t pairs = sms / 2;
   LinPlan best;
-  double best_us = 4.0 + (max_steps * 540.0 + 4000.0) / (1000 * kGHz);
-  if (pair_units > pairs)
-    best_us = 4.0 + std::max(pair_work / pairs, ((pair_units + pairs - 1) / pairs) * (pair_work / pair_units)) /
-                        (1000 * kGHz) + 2.0;
+  if (units == 0) return best;
+  // On pairs, tiles whole: rounds of tiles, of the tiles' mean where they differ.
+  double best_cycles = kPairLaunch + std::max(longest, ceil_div(units, pairs) * (work / units));
+  // Or with split depths: the parts of the products of few tiles, while they fit,
+  // each next one to the tile that takes longest.
+  {
+    int split[kMaxProducts] = {1, 1};
+    bool few[kMaxProducts] = {false, false};
+    for (int i = 0; i < count; ++i) few[i] = tiles[i] > 0 && 2 * tiles[i] <= pairs;
+    int64_t taken = 0;
+    for (int i = 0; i < count; ++i)
+      if (few[i]) taken += tiles[i];
+    for (bool more = taken > 0; more;) {
+      int at = -1;
+      for (int i = 0; i < count; ++i)
+        if (few[i] && split[i] < kMaxPairSplit && taken + tiles[i] <= pairs &&
+            steps[i] / (split[i] + 1) >= 8 && (at < 0 || steps[i] / split[i] > steps[at] / split[at]))
+          at = i;
+      if ((more = at >= 0)) {
+        ++split[at];
+        taken += tiles[at];
+      }
+    }
+    double part = 0, all = 0, tile = 0;
+    int64_t parts = 0, whole = 0;
+    for (int i = 0; i < count; ++i) {
+      const double t = ceil_div(steps[i], split[i]) * kPairStep + kPairTile;
+      all += tiles[i] * split[i] * t;
+      if (split[i] > 1) {
+        parts += tiles[i] * split[i];
+        part = std::max(part, t);
+      } else if (tiles[i]) {
+        whole += tiles[i];
+        tile = std::max(tile, t);
+      }
+    }
+    if (parts) {
+      const double cycles = kPairLaunch + kExchange + std::max(part, whole ? all / pairs + tile / 2 : part);
+      if (cycles < best_cycles) {
+        best_cycles = cycles;
+        for (int i = 0; i < count; ++i) best.pair_split[i] = split[i];
+        best.parts = static_cast<int>(parts);
+        // Rounds of whole tiles that the other pairs have time for beside a part.
+        best.ahead = whole && parts < pairs ? static_cast<int>(std::min<int64_t>(part / tile, whole / (pairs - parts))) : 0;
+      }
+    }
+  }
   for (int nt : {16, 32, 64, 128}) {
     if (p_mn && nt < 64) continue;
     for (int split = 1; split <= kMaxSplit; split *= 2) {
       if (nt / split < 1) continue;
       const double step_cycles = std::max(2.0 * nt, (kRows + nt) * 128 / 60.0);
-      double work = 0, longest = 0;
+      double work = 0, longest_cta = 0;
       int64_t ctas = 0;
       for (int i = 0; i < count; ++i) {
         const LinProduct& p = products[i];
-        const int64_t units = ((p.rows + nt - 1) / nt) * ((p.cols + kRows - 1) / kRows);
-        const int64_t steps = ((p.depth + step - 1) / step + split - 1) / split;
-        ctas += units * split;
-        const double t = steps * step_cycles + 1500.0 + (split > 1 ? 800.0 : 0.0) + nt * 10.0;
-        work += units * split * t;
-        longest = std::max(longest, t);
+        const int64_t n = ceil_div(p.rows, nt) * ceil_div(p.cols, kRows);
+        const double t = ceil_div(steps[i], split) * step_cycles + 1500.0 + (split > 1 ? 800.0 : 0.0) + nt * 10.0;
+        ctas += n * split;
+        work += static_cast<double>(n * split) * t;
+        longest_cta = std::max(longest_cta, t);
       }
-      const double cycles = std::max(longest, ((ctas + sms - 1) / sms) * (work / ctas));
-      const double us = 3.5 + cycles / (1000 * kGHz);
-      if (us < best_us) {
-        best_us = us;
+      if (ctas == 0) continue;
+      const double cycles = 3000 + std::max(longest_cta, ceil_div(ctas, sms) * (work / ctas));
+      if (cycles < best_cycles) {
+        best_cycles = cycles;
+        best = LinPlan{};
         best.nt = nt;
         best.split = split;
-        const int per_sm = ctas > sms ? 2 : 1;
-        best.stages = std::min(kSplitMaxStages, (per_sm == 2 ? 110 * 1024 : 220 * 1024) / split_stage_bytes(nt));
+        best.stages = std::min(kSplitMaxStages, (ctas > sms ? 110 * 1024 : 220 * 1024) / split_stage_bytes(nt));
       }
     }
   }
+  if (best.parts) best.scratch = (sizeof(float) * kPartFloats + sizeof(int) * 2 * kLinEpiWarps) * best.parts;
   return best;
 }
+
+namespace {
 
 using SplitKernel = void (*)(const LinMaps, const LinLaunch, int, int, Oz2Device*);
 template <int TYPE>
@@ -906,33 +1061,40 @@ cudaError_t launch_clusters(void (*kernel)(KArgs...), unsigned grid, unsigned bl
 
 }  // namespace
 
-cudaError_t launch_linear(const LinProduct* products, int count, int type, Oz2Device* dev, cudaStream_t st) {
+cudaError_t launch_linear(const LinProduct* products, int count, int type, const LinPlan& plan, void* scratch,
+                          Oz2Device* dev, cudaStream_t st) {
   LinMaps maps{};
   LinLaunch L{};
-  const int64_t step = 128 / type_bytes(type);
-  const LinPlan plan = choose_plan(products, count, type);
   const int tile_rows = plan.nt ? plan.nt : kLinTile, tile_cols = plan.nt ? kRows : kLinTile;
+  int split_tiles = 0;
   for (int i = 0; i < count; ++i) {
     const LinProduct& p = products[i];
     LinUnits& x = L.u[i];
     x.rows = p.rows;
     x.cols = p.cols;
-    x.ntm = (p.rows + tile_rows - 1) / tile_rows;
-    x.ntn = (p.cols + tile_cols - 1) / tile_cols;
+    // (A result of more tiles than an int counts is larger than the memory.)
+    const int64_t ntm = ceil_div(p.rows, tile_rows), ntn = ceil_div(p.cols, tile_cols);
+    if (ntm * ntn * plan.split * 8 > 0x3FFFFFFFLL) return cudaErrorInvalidValue;
+    x.ntm = static_cast<int>(ntm);
+    x.ntn = static_cast<int>(ntn);
     x.units = x.ntm * x.ntn;
-    x.steps = (p.depth + step - 1) / step;
+    x.split = plan.pair_split[i];
+    x.steps = static_cast<int>(steps_of(p, type));
     x.p_mn = p.p_mn;
     x.q_mn = p.q_mn;
     x.ep = p.ep;
-    L.units += x.units;
+    if (x.split > 1) {
+      split_tiles += x.units;
+    } else {
+      L.units += x.units;
+    }
     if (x.steps && (!make_operand_map(&maps.p[i], p.p, p.rows, p.depth, p.ldp, type, p.p_mn, plan.nt ? plan.nt : kRows) ||
                     !make_operand_map(&maps.q[i], p.q, p.cols, p.depth, p.ldq, type, p.q_mn)))
       return cudaErrorInvalidValue;
   }
   L.count = count;
-  if (L.units == 0) return cudaSuccess;
+  if (L.units + split_tiles == 0) return cudaSuccess;
   if (plan.nt) {
-    if (L.units * plan.split > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
     SplitKernel kern = type == OZ2_TYPE_BF16  ? split_kernel<OZ2_TYPE_BF16>(plan.nt)
                        : type == OZ2_TYPE_F16 ? split_kernel<OZ2_TYPE_F16>(plan.nt)
                                               : split_kernel<OZ2_TYPE_E4M3>(plan.nt);
@@ -948,8 +1110,18 @@ cudaError_t launch_linear(const LinProduct* products, int count, int type, Oz2De
                                      : linear_pair_kernel<OZ2_TYPE_E4M3>;
   cudaError_t err = allow_smem(reinterpret_cast<const void*>(kern), kLinSmem);
   if (err != cudaSuccess) return err;
-  const int64_t pairs =
-      std::min(L.units, resident_pairs(reinterpret_cast<const void*>(kern), kLinThreads, kLinSmem));
+  const int64_t resident = resident_pairs(reinterpret_cast<const void*>(kern), kLinThreads, kLinSmem);
+  int64_t pairs = std::min<int64_t>(L.units, resident);
+  if (plan.parts) {
+    // Each part has a pair of its own, resident or not: no pair waits for another.
+    pairs = num_sms() / 2;
+    L.parts = plan.parts;
+    L.ahead = plan.ahead;
+    L.sums = static_cast<float*>(scratch);
+    L.arrived = reinterpret_cast<int*>(L.sums + static_cast<int64_t>(plan.parts) * kPartFloats);
+    err = cudaMemsetAsync(L.arrived, 0, sizeof(int) * split_tiles * 2 * kLinEpiWarps, st);
+    if (err != cudaSuccess) return err;
+  }
   count_launch();
   return launch_dependent(kern, dim3(static_cast<unsigned>(2 * pairs)), dim3(kLinThreads), kLinSmem, st, maps, L, dev);
 }

@@ -43,9 +43,34 @@ __global__ void __launch_bounds__(256) pack_rows_kernel(const T* __restrict__ sr
 // ---------------------------------------------------------------------------
 constexpr int kGradCols = 256, kGradWarps = 8;
 
+// Eight columns of a row: g ← dy·act'(z), the sums, and dz.
 template <int ACT>
+__device__ __forceinline__ void grad8(const uint32_t (&aw)[4], const uint32_t (&bw)[4], bool bf16, float (&s)[8],
+                                      uint16_t* dz) {
+  float g[8];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float2 f = unpack16(aw[e], bf16);
+    g[2 * e] = f.x;
+    g[2 * e + 1] = f.y;
+    if (ACT != OZ2_ACT_NONE) {
+      const float2 t = unpack16(bw[e], bf16);
+      g[2 * e] *= act_slope<ACT>(t.x);
+      g[2 * e + 1] *= act_slope<ACT>(t.y);
+    }
+    s[2 * e] += g[2 * e];
+    s[2 * e + 1] += g[2 * e + 1];
+  }
+  if (dz)  // rows of 16-byte pieces: what lies past n in the last one is padding
+    *reinterpret_cast<uint4*>(dz) = make_uint4(pack16(g[0], g[1], bf16), pack16(g[2], g[3], bf16),
+                                               pack16(g[4], g[5], bf16), pack16(g[6], g[7], bf16));
+}
+
+constexpr int kGradAhead = 4;        // rows that a warp loads before it works on them
+
+template <int ACT, bool BF16>
 __global__ void __launch_bounds__(32 * kGradWarps)
-    act_grad_kernel(int64_t m, int64_t n, int64_t chunk_rows, bool bf16, bool vec, const uint16_t* __restrict__ dy,
+    act_grad_kernel(int64_t m, int64_t n, int64_t chunk_rows, bool vec, const uint16_t* __restrict__ dy,
                     int64_t ld_dy, const uint16_t* __restrict__ z, int64_t ld_z, uint16_t* __restrict__ dz,
                     int64_t ld_dz, float* __restrict__ partial) {
   __shared__ float sums[kGradWarps][kGradCols];
@@ -54,48 +79,45 @@ __global__ void __launch_bounds__(32 * kGradWarps)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t col = static_cast<int64_t>(blockIdx.x) * kGradCols + 8 * lane;
   const int64_t r0 = static_cast<int64_t>(blockIdx.y) * chunk_rows, r1 = min(m, r0 + chunk_rows);
-  const bool whole = vec && col + 8 <= n;
   float s[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) s[e] = 0.f;
-  if (col < n) {
-#pragma unroll 4
+  if (vec && col + 8 <= n) {
+    int64_t r = r0 + warp;
+    for (; r + (kGradAhead - 1) * kGradWarps < r1; r += kGradAhead * kGradWarps) {
+      uint4 a[kGradAhead], b[kGradAhead];
+#pragma unroll
+      for (int i = 0; i < kGradAhead; ++i) {
+        a[i] = __ldg(reinterpret_cast<const uint4*>(dy + (r + i * kGradWarps) * ld_dy + col));
+        b[i] = make_uint4(0, 0, 0, 0);
+        if (ACT != OZ2_ACT_NONE) b[i] = __ldg(reinterpret_cast<const uint4*>(z + (r + i * kGradWarps) * ld_z + col));
+      }
+#pragma unroll
+      for (int i = 0; i < kGradAhead; ++i) {
+        const uint32_t aw[4] = {a[i].x, a[i].y, a[i].z, a[i].w}, bw[4] = {b[i].x, b[i].y, b[i].z, b[i].w};
+        grad8<ACT>(aw, bw, BF16, s, dz ? dz + (r + i * kGradWarps) * ld_dz + col : nullptr);
+      }
+    }
+    for (; r < r1; r += kGradWarps) {
+      const uint4 a = __ldg(reinterpret_cast<const uint4*>(dy + r * ld_dy + col));
+      uint4 b = make_uint4(0, 0, 0, 0);
+      if (ACT != OZ2_ACT_NONE) b = __ldg(reinterpret_cast<const uint4*>(z + r * ld_z + col));
+      const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+      grad8<ACT>(aw, bw, BF16, s, dz ? dz + r * ld_dz + col : nullptr);
+    }
+  } else if (col < n) {
+#pragma unroll 2
     for (int64_t r = r0 + warp; r < r1; r += kGradWarps) {
       const uint16_t* a = dy + r * ld_dy + col;
       const uint16_t* b = ACT == OZ2_ACT_NONE ? nullptr : z + r * ld_z + col;
       uint32_t aw[4] = {0, 0, 0, 0}, bw[4] = {0, 0, 0, 0};
-      if (whole) {
-        const uint4 v = __ldg(reinterpret_cast<const uint4*>(a));
-        aw[0] = v.x, aw[1] = v.y, aw[2] = v.z, aw[3] = v.w;
-        if (ACT != OZ2_ACT_NONE) {
-          const uint4 w = __ldg(reinterpret_cast<const uint4*>(b));
-          bw[0] = w.x, bw[1] = w.y, bw[2] = w.z, bw[3] = w.w;
-        }
-      } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (col + e < n) {
-            aw[e >> 1] |= static_cast<uint32_t>(__ldg(a + e)) << (16 * (e & 1));
-            if (ACT != OZ2_ACT_NONE) bw[e >> 1] |= static_cast<uint32_t>(__ldg(b + e)) << (16 * (e & 1));
-          }
-      }
-      float g[8];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float2 f = unpack16(aw[e], bf16);
-        g[2 * e] = f.x;
-        g[2 * e + 1] = f.y;
-        if (ACT != OZ2_ACT_NONE) {
-          const float2 t = unpack16(bw[e], bf16);
-          g[2 * e] *= act_slope<ACT>(t.x);
-          g[2 * e + 1] *= act_slope<ACT>(t.y);
+      for (int e = 0; e < 8; ++e)
+        if (col + e < n) {
+          aw[e >> 1] |= static_cast<uint32_t>(__ldg(a + e)) << (16 * (e & 1));
+          if (ACT != OZ2_ACT_NONE) bw[e >> 1] |= static_cast<uint32_t>(__ldg(b + e)) << (16 * (e & 1));
         }
-        s[2 * e] += g[2 * e];
-        s[2 * e + 1] += g[2 * e + 1];
-      }
-      if (dz)  // rows of 16-byte pieces: what lies past n in the last one is padding
-        *reinterpret_cast<uint4*>(dz + r * ld_dz + col) = make_uint4(pack16(g[0], g[1], bf16), pack16(g[2], g[3], bf16),
-                                                                     pack16(g[4], g[5], bf16), pack16(g[6], g[7], bf16));
+      grad8<ACT>(aw, bw, BF16, s, dz ? dz + r * ld_dz + col : nullptr);
     }
   }
   if (partial) {
@@ -132,6 +154,15 @@ int64_t chunk_rows_for(int64_t m, int64_t n) {
   return std::max(rows, (m + 65534) / 65535);  // the grid's second axis
 }
 
+template <bool BF16>
+auto grad_kernel(int act) {
+  return act == OZ2_ACT_RELU        ? act_grad_kernel<OZ2_ACT_RELU, BF16>
+         : act == OZ2_ACT_GELU      ? act_grad_kernel<OZ2_ACT_GELU, BF16>
+         : act == OZ2_ACT_GELU_TANH ? act_grad_kernel<OZ2_ACT_GELU_TANH, BF16>
+         : act == OZ2_ACT_SILU      ? act_grad_kernel<OZ2_ACT_SILU, BF16>
+                                    : act_grad_kernel<OZ2_ACT_NONE, BF16>;
+}
+
 }  // namespace
 
 int64_t lin_db_chunks(int64_t m, int64_t n) {
@@ -159,15 +190,11 @@ cudaError_t launch_act_grad(int64_t m, int64_t n, int type, int act, const void*
   const int64_t rows = chunk_rows_for(m, n), chunks = lin_db_chunks(m, n);
   auto aligned = [](const void* p, int64_t ld) { return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(2 * ld)) & 15) == 0; };
   const bool vec = aligned(dy, ld_dy) && (act == OZ2_ACT_NONE || aligned(z, ld_z));
-  auto kern = act == OZ2_ACT_RELU        ? act_grad_kernel<OZ2_ACT_RELU>
-              : act == OZ2_ACT_GELU      ? act_grad_kernel<OZ2_ACT_GELU>
-              : act == OZ2_ACT_GELU_TANH ? act_grad_kernel<OZ2_ACT_GELU_TANH>
-              : act == OZ2_ACT_SILU      ? act_grad_kernel<OZ2_ACT_SILU>
-                                         : act_grad_kernel<OZ2_ACT_NONE>;
+  auto kern = type == OZ2_TYPE_BF16 ? grad_kernel<true>(act) : grad_kernel<false>(act);
   count_launch();
   cudaError_t err = launch_dependent(
       kern, dim3(static_cast<unsigned>((n + kGradCols - 1) / kGradCols), static_cast<unsigned>(chunks)),
-      dim3(32 * kGradWarps), 0, st, m, n, rows, type == OZ2_TYPE_BF16, vec, static_cast<const uint16_t*>(dy), ld_dy,
+      dim3(32 * kGradWarps), 0, st, m, n, rows, vec, static_cast<const uint16_t*>(dy), ld_dy,
       static_cast<const uint16_t*>(z), ld_z, static_cast<uint16_t*>(dz), ld_dz, db ? partial : nullptr);
   if (err != cudaSuccess || !db) return err;
   count_launch();

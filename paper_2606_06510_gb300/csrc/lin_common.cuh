@@ -31,15 +31,28 @@ __device__ __forceinline__ float2 unpack16(uint32_t w, bool bf16) {
 __device__ __forceinline__ float load16(const uint16_t* p, bool bf16) { return unpack16(*p, bf16).x; }
 
 // --- activations ---------------------------------------------------------------
-// In the epilogue of a product, whose result is rounded to 16 bits, exp is the
-// fast one (about 2^-21 of the value); the gradient's FP32 sums take expf.
+// exp and division are the fast ones (off by some 2^-21 of the value): results are
+// rounded to 16 bits, and in db's FP32 sums such errors average out.
 constexpr float kSqrtHalf = 0.70710678118654752f, kSqrt2OverPi = 0.79788456080286536f, kInvSqrt2Pi = 0.39894228040143268f;
 constexpr float kGeluCubic = 0.044715f;
+
+// Φ(-|z|) = exp(-x²)·(a1 t + ... + a5 t⁵)/2 with x = |z|/√2 and t = 1/(1 + p·x), off
+// by at most 7.5e-8 (Hastings; Abramowitz and Stegun 7.1.26), given ex = exp(-x²).  A
+// third of erff's time, without its branch.
+__device__ __forceinline__ float gauss_tail(float x, float ex) {
+  const float t = __fdividef(1.f, fmaf(0.3275911f, x, 1.f));
+  return 0.5f * t * ex *
+         fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+}
 
 template <int ACT>
 __device__ __forceinline__ float activate(float z) {
   if (ACT == OZ2_ACT_RELU) return z < 0.f ? 0.f : z;  // NaN stays NaN
-  if (ACT == OZ2_ACT_GELU) return 0.5f * z * (1.f + erff(z * kSqrtHalf));
+  if (ACT == OZ2_ACT_GELU) {
+    const float x = fabsf(z) * kSqrtHalf;
+    const float h = gauss_tail(x, __expf(-x * x));
+    return z > 0.f ? fmaf(-z, h, z) : z * h;
+  }
   if (ACT == OZ2_ACT_GELU_TANH) {
     // z(1 + tanh u)/2 = z/(1 + exp(-2u))
     const float u = kSqrt2OverPi * fmaf(kGeluCubic * z * z, z, z);
@@ -49,22 +62,29 @@ __device__ __forceinline__ float activate(float z) {
   return z;
 }
 
-// d act(z)/dz.
+// d act(z)/dz.  Far out, where the slope is 0 or 1 to FP32, z is held (its powers
+// and products with 0 would not be numbers).
 template <int ACT>
 __device__ __forceinline__ float act_slope(float z) {
   if (ACT == OZ2_ACT_RELU) return z > 0.f ? 1.f : z == z ? 0.f : z;
-  if (ACT == OZ2_ACT_GELU)
-    return fmaf(z * kInvSqrt2Pi, expf(-0.5f * z * z), 0.5f * (1.f + erff(z * kSqrtHalf)));
+  if (ACT == OZ2_ACT_GELU) {
+    z = fabsf(z) > 16.f ? copysignf(16.f, z) : z;
+    const float x = fabsf(z) * kSqrtHalf, ex = __expf(-x * x);
+    const float h = gauss_tail(x, ex);
+    return fmaf(z * kInvSqrt2Pi, ex, z > 0.f ? 1.f - h : h);
+  }
   if (ACT == OZ2_ACT_GELU_TANH) {
     // with g = (1 + tanh u)/2 = 1/(1 + exp(-2u)):  g + z·2g(1 - g)·u'
+    z = fabsf(z) > 16.f ? copysignf(16.f, z) : z;
     const float zz = z * z;
     const float u = kSqrt2OverPi * fmaf(kGeluCubic * zz, z, z);
-    const float g = 1.f / (1.f + expf(-2.f * u));
+    const float g = __fdividef(1.f, 1.f + __expf(-2.f * u));
     const float du = kSqrt2OverPi * fmaf(3.f * kGeluCubic, zz, 1.f);
     return fmaf(2.f * z * g * (1.f - g), du, g);
   }
   if (ACT == OZ2_ACT_SILU) {
-    const float g = 1.f / (1.f + expf(-z));
+    z = fabsf(z) > 80.f ? copysignf(80.f, z) : z;
+    const float g = __fdividef(1.f, 1.f + __expf(-z));
     return g * fmaf(z, 1.f - g, 1.f);
   }
   return 1.f;
@@ -97,9 +117,21 @@ struct LinProduct {
 };
 constexpr int kMaxProducts = 2;
 
-// Up to two independent products in one launch; operands' base addresses and
-// leading dimensions are multiples of 16 bytes.  `type` is the operands'.
-cudaError_t launch_linear(const LinProduct* products, int count, int type, Oz2Device* dev, cudaStream_t st);
+// How a launch runs: on CTA pairs (nt = 0), the depth of product i's tiles cut into
+// pair_split[i] parts (`parts` of them in all, `ahead`: see LinLaunch), or in tiles
+// of nt rows with the depth split over `split` CTAs and `stages` of operands in
+// flight.  `scratch` bytes of workspace.
+struct LinPlan {
+  int nt = 0, split = 1, stages = 0;
+  int pair_split[kMaxProducts] = {1, 1}, parts = 0, ahead = 0;
+  size_t scratch = 0;
+};
+// The plan for up to two independent products in one launch (by their sizes and
+// storage alone).  `type` is the operands'.
+LinPlan plan_linear(const LinProduct* products, int count, int type);
+// Operands' base addresses and leading dimensions are multiples of 16 bytes.
+cudaError_t launch_linear(const LinProduct* products, int count, int type, const LinPlan& plan, void* scratch,
+                          Oz2Device* dev, cudaStream_t st);
 
 // Rows of elements of `bytes` bytes copied to rows that start on 16-byte
 // boundaries (ld_dst·bytes a multiple of 16).

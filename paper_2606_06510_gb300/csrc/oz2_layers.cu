@@ -104,22 +104,24 @@ int oz2_linear(int64_t m, int64_t n, int64_t k, int type, const void* d_X, int64
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   Oz2Device* dev = device_status();
   if (!dev) return OZ2_ERR_CUDA;
-  Workspace ws(st);
-  Operand X(d_X, ldx, k ? m : 0, k, es, ws), W(d_W, ldw, k ? n : 0, k, es, ws);
-  if (!ws.take()) return OZ2_ERR_ALLOC;
-  cudaError_t err = X.place(ws, st);
-  if (err == cudaSuccess) err = W.place(ws, st);
-  if (err != cudaSuccess) return status_of(err);
   LinProduct p{};
   p.rows = m;
   p.cols = n;
   p.depth = k;
+  p.ep = LinEpilogue{d_x_scale, d_w_scale, d_bias, d_R, d_Z, d_Y, ldr, ldz, ldy, bias_type, out_type, act, 0};
+  const LinPlan plan = plan_linear(&p, 1, type);
+  Workspace ws(st);
+  Operand X(d_X, ldx, k ? m : 0, k, es, ws), W(d_W, ldw, k ? n : 0, k, es, ws);
+  const size_t scratch = ws.ask(plan.scratch);
+  if (!ws.take()) return OZ2_ERR_ALLOC;
+  cudaError_t err = X.place(ws, st);
+  if (err == cudaSuccess) err = W.place(ws, st);
+  if (err != cudaSuccess) return status_of(err);
   p.p = X.p;
   p.ldp = X.ld;
   p.q = W.p;
   p.ldq = W.ld;
-  p.ep = LinEpilogue{d_x_scale, d_w_scale, d_bias, d_R, d_Z, d_Y, ldr, ldz, ldy, bias_type, out_type, act, 0};
-  return status_of(launch_linear(&p, 1, type, dev, st));
+  return status_of(launch_linear(&p, 1, type, plan, ws.at<void>(scratch), dev, st));
 }
 
 int oz2_linear_grad(int64_t m, int64_t n, int64_t k, int type, const void* d_dY, int64_t lddy, const void* d_Z,
@@ -146,14 +148,40 @@ int oz2_linear_grad(int64_t m, int64_t n, int64_t k, int type, const void* d_dY,
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   Oz2Device* dev = device_status();
   if (!dev) return OZ2_ERR_CUDA;
+  LinProduct p[kMaxProducts] = {};
+  int count = 0;
+  LinProduct* pdx = nullptr;
+  LinProduct* pdw = nullptr;
+  if (want_dx) {
+    LinProduct& a = *(pdx = &p[count++]);
+    a.rows = m;
+    a.cols = k;
+    a.depth = n;
+    a.q_mn = true;
+    a.ep.out = d_dX;
+    a.ep.ld_out = lddx;
+    a.ep.out_type = type;
+  }
+  if (want_dw) {
+    LinProduct& a = *(pdw = &p[count++]);
+    a.rows = n;
+    a.cols = k;
+    a.depth = m;
+    a.p_mn = a.q_mn = true;
+    a.ep.out = d_dW;
+    a.ep.ld_out = lddw;
+    a.ep.out_type = dw_type;
+    a.ep.accumulate = accumulate;
+  }
+  const LinPlan plan = count ? plan_linear(p, count, type) : LinPlan{};
   Workspace ws(st);
   // dZ is dY itself where there is no activation and TMA can read it.
-  const bool products = want_dx || want_dw;
-  const bool own_dz = products && any && (act != OZ2_ACT_NONE || !on16(d_dY, lddy, 2));
+  const bool own_dz = count && any && (act != OZ2_ACT_NONE || !on16(d_dY, lddy, 2));
   const int64_t ld_dz = padded_ld(n, 2);
   const size_t dz_off = own_dz ? ws.ask(static_cast<size_t>(m) * ld_dz * 2) : 0;
   const size_t part_off = want_db && m > 0 ? ws.ask(sizeof(float) * static_cast<size_t>(lin_db_chunks(m, n)) * n) : 0;
   Operand X(d_X, ldx, want_dw ? m : 0, k, 2, ws), W(d_W, ldw, want_dx ? n : 0, k, 2, ws);
+  const size_t scratch = ws.ask(plan.scratch);
   if (!ws.take()) return OZ2_ERR_ALLOC;
   cudaError_t err = cudaSuccess;
   if (want_db && m == 0) err = cudaMemsetAsync(d_db, 0, sizeof(float) * n, st);
@@ -169,39 +197,20 @@ int oz2_linear_grad(int64_t m, int64_t n, int64_t k, int type, const void* d_dY,
   }
   if (err == cudaSuccess) err = X.place(ws, st);
   if (err == cudaSuccess) err = W.place(ws, st);
-  if (err != cudaSuccess) return status_of(err);
-  LinProduct p[kMaxProducts] = {};
-  int count = 0;
-  if (want_dx) {
-    LinProduct& a = p[count++];
-    a.rows = m;
-    a.cols = k;
-    a.depth = n;
-    a.p = dz;
-    a.ldp = ldz_used;
-    a.q = W.p;
-    a.ldq = W.ld;
-    a.q_mn = true;
-    a.ep.out = d_dX;
-    a.ep.ld_out = lddx;
-    a.ep.out_type = type;
+  if (err != cudaSuccess || !count) return status_of(err);
+  if (pdx) {
+    pdx->p = dz;
+    pdx->ldp = ldz_used;
+    pdx->q = W.p;
+    pdx->ldq = W.ld;
   }
-  if (want_dw) {
-    LinProduct& a = p[count++];
-    a.rows = n;
-    a.cols = k;
-    a.depth = m;
-    a.p = dz;
-    a.ldp = ldz_used;
-    a.q = X.p;
-    a.ldq = X.ld;
-    a.p_mn = a.q_mn = true;
-    a.ep.out = d_dW;
-    a.ep.ld_out = lddw;
-    a.ep.out_type = dw_type;
-    a.ep.accumulate = accumulate;
+  if (pdw) {
+    pdw->p = dz;
+    pdw->ldp = ldz_used;
+    pdw->q = X.p;
+    pdw->ldq = X.ld;
   }
-  return count ? status_of(launch_linear(p, count, type, dev, st)) : OZ2_OK;
+  return status_of(launch_linear(p, count, type, plan, ws.at<void>(scratch), dev, st));
 }
 
 int oz2_adamw(const oz2_adamw_tensor* tensors, int count, int param_type, int grad_type, int state_bits,
