@@ -648,20 +648,67 @@ __device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
   return v;
 }
 
-__device__ __forceinline__ float activate_any(float z, int act) {
-  switch (act) {
-    case OZ2_ACT_RELU: return activate<OZ2_ACT_RELU>(z);
-    case OZ2_ACT_GELU: return activate<OZ2_ACT_GELU>(z);
-    case OZ2_ACT_GELU_TANH: return activate<OZ2_ACT_GELU_TANH>(z);
-    case OZ2_ACT_SILU: return activate<OZ2_ACT_SILU>(z);
-    default: return z;
+template <int ACT>
+__device__ __forceinline__ void activate8(float (&z)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) z[e] = activate<ACT>(z[e]);
+}
+
+// Eight 16-bit values of a row of D, from its column col on (n of them there).
+__device__ __forceinline__ uint4 load8(const void* src, int64_t ld, int64_t row, int64_t col, int n) {
+  const uint16_t* s = static_cast<const uint16_t*>(src) + row * ld + col;
+  if (n == 8 && vec_ok(src, ld, 2)) return __ldg(reinterpret_cast<const uint4*>(s));
+  uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e < n) w[e >> 1] |= static_cast<uint32_t>(__ldg(s + e)) << (16 * (e & 1));
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void store8(void* dst, int64_t ld, int64_t row, int64_t col, int n, const float (&z)[8],
+                                       bool bf16) {
+  uint16_t* d = static_cast<uint16_t*>(dst) + row * ld + col;
+  const uint32_t w[4] = {pack16(z[0], z[1], bf16), pack16(z[2], z[3], bf16), pack16(z[4], z[5], bf16),
+                         pack16(z[6], z[7], bf16)};
+  if (n == 8 && vec_ok(dst, ld, 2)) {
+    *reinterpret_cast<uint4*>(d) = make_uint4(w[0], w[1], w[2], w[3]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) d[e] = static_cast<uint16_t>(w[e >> 1] >> (16 * (e & 1)));
   }
 }
 
-// Eight columns of one row of D from their sums.
-__device__ __forceinline__ void finish8(const LinUnits& x, int64_t row, int64_t col, float (&z)[8]) {
-  const LinEpilogue& ep = x.ep;
-  const int n = static_cast<int>(min(static_cast<int64_t>(8), x.cols - col));
+// What a thread needs of its eight columns of D, whichever the row.
+struct ColumnTerms {
+  float bias[8], scale[8];
+};
+__device__ __forceinline__ void load_terms(const LinEpilogue& ep, int64_t col, int n, ColumnTerms& t) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) t.bias[e] = 0.f, t.scale[e] = 1.f;
+  if (ep.bias && ep.bias_type == OZ2_TYPE_F32) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) t.bias[e] = __ldg(static_cast<const float*>(ep.bias) + col + e);
+  } else if (ep.bias) {
+    const uint4 v = load8(ep.bias, 0, 0, col, n);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 f = unpack16(w[e], ep.bias_type == OZ2_TYPE_BF16);
+      t.bias[2 * e] = f.x;
+      t.bias[2 * e + 1] = f.y;
+    }
+  }
+  if (ep.col_scale) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) t.scale[e] = __ldg(ep.col_scale + col + e);
+  }
+}
+
+// Eight columns of one row of D from their sums; r holds R's, where there is one.
+__device__ __forceinline__ void finish8(const LinEpilogue& ep, int64_t row, int64_t col, int n, const ColumnTerms& t,
+                                        uint4 r, float (&z)[8]) {
   if (ep.out_type == OZ2_TYPE_F32) {
     float* d = static_cast<float*>(ep.out) + row * ep.ld_out + col;
 #pragma unroll
@@ -670,52 +717,55 @@ __device__ __forceinline__ void finish8(const LinUnits& x, int64_t row, int64_t 
     return;
   }
   const bool bf16 = ep.out_type == OZ2_TYPE_BF16;
-  if (ep.row_scale) {
-    const float rs = __ldg(ep.row_scale + row);
+  const float rs = ep.row_scale ? __ldg(ep.row_scale + row) : 1.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e < n) z[e] *= rs * __ldg(ep.col_scale + col + e);
+  for (int e = 0; e < 8; ++e) z[e] = fmaf(z[e], rs * t.scale[e], t.bias[e]);
+  if (ep.pre) store8(ep.pre, ep.ld_pre, row, col, n, z, bf16);
+  switch (ep.act) {
+    case OZ2_ACT_RELU: activate8<OZ2_ACT_RELU>(z); break;
+    case OZ2_ACT_GELU: activate8<OZ2_ACT_GELU>(z); break;
+    case OZ2_ACT_GELU_TANH: activate8<OZ2_ACT_GELU_TANH>(z); break;
+    case OZ2_ACT_SILU: activate8<OZ2_ACT_SILU>(z); break;
+    default: break;
   }
-  if (ep.bias) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e < n)
-        z[e] += ep.bias_type == OZ2_TYPE_F32 ? __ldg(static_cast<const float*>(ep.bias) + col + e)
-                                             : load16(static_cast<const uint16_t*>(ep.bias) + col + e, bf16);
-  }
-  auto put = [&](void* dst, int64_t ld) {
-    uint16_t* d = static_cast<uint16_t*>(dst) + row * ld + col;
-    const uint32_t w[4] = {pack16(z[0], z[1], bf16), pack16(z[2], z[3], bf16), pack16(z[4], z[5], bf16),
-                           pack16(z[6], z[7], bf16)};
-    if (n == 8 && vec_ok(dst, ld, 2)) {
-      *reinterpret_cast<uint4*>(d) = make_uint4(w[0], w[1], w[2], w[3]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e < n) d[e] = static_cast<uint16_t>(w[e >> 1] >> (16 * (e & 1)));
-    }
-  };
-  if (ep.pre) put(ep.pre, ep.ld_pre);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) z[e] = activate_any(z[e], ep.act);
   if (ep.add) {
-    const uint16_t* s = static_cast<const uint16_t*>(ep.add) + row * ep.ld_add + col;
-    if (n == 8 && vec_ok(ep.add, ep.ld_add, 2)) {
-      const uint4 r = *reinterpret_cast<const uint4*>(s);
-      const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float2 f = unpack16(w[e], bf16);
-        z[2 * e] += f.x;
-        z[2 * e + 1] += f.y;
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e < n) z[e] += unpack16(s[e], bf16).x;
+    for (int e = 0; e < 4; ++e) {
+      const float2 f = unpack16(w[e], bf16);
+      z[2 * e] += f.x;
+      z[2 * e + 1] += f.y;
     }
   }
-  put(ep.out, ep.ld_out);
+  store8(ep.out, ep.ld_out, row, col, n, z, bf16);
+}
+
+// The rows of the tile that a CTA finishes: from row r on, every 16th, of SPLIT
+// CTAs' sums (`at`: this thread's columns of row 0 in this CTA's).  All of a row's
+// loads are under way before the first is added.
+template <int SPLIT>
+__device__ __forceinline__ void finish_rows(const LinUnits& x, int64_t row0, int64_t col, int n, int r, int end,
+                                            uint32_t at, const ColumnTerms& t, uint4 first) {
+  bool have = true;
+#pragma unroll 1
+  for (; r < end && row0 + r < x.rows; r += 16) {
+    float4 a[SPLIT], b[SPLIT];
+#pragma unroll
+    for (int p = 0; p < SPLIT; ++p) {
+      const uint32_t from = (SPLIT > 1 ? mapa_shared(at, p) : at) + r * kRows * 4;
+      a[p] = ld_cluster_f4(from);
+      b[p] = ld_cluster_f4(from + 16);
+    }
+    const uint4 add = have ? first : x.ep.add ? load8(x.ep.add, x.ep.ld_add, row0 + r, col, n) : first;
+    have = false;
+    float z[8] = {a[0].x, a[0].y, a[0].z, a[0].w, b[0].x, b[0].y, b[0].z, b[0].w};
+#pragma unroll
+    for (int p = 1; p < SPLIT; ++p) {
+      z[0] += a[p].x, z[1] += a[p].y, z[2] += a[p].z, z[3] += a[p].w;
+      z[4] += b[p].x, z[5] += b[p].y, z[6] += b[p].z, z[7] += b[p].w;
+    }
+    finish8(x.ep, row0 + r, col, n, t, add, z);
+  }
 }
 
 template <int TYPE, int NT>
@@ -752,6 +802,7 @@ __global__ void __launch_bounds__(kSplitThreads)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base_s, 0);
+  pdl_trigger();
   pdl_wait();
 
   int u = blockIdx.x / split;
@@ -842,6 +893,18 @@ __global__ void __launch_bounds__(kSplitThreads)
     mma_commit_by(me, done);
     __syncwarp();
   }
+  // This thread's part of the epilogue: eight columns of every 16th row of the CTA's
+  // share of the tile.  What does not depend on the sums is loaded before them.
+  const int share = NT / split, r_first = static_cast<int>(rank) * share + (threadIdx.x >> 4);
+  const int64_t row0 = static_cast<int64_t>(tm) * NT, col = static_cast<int64_t>(tn) * kRows + (threadIdx.x & 15) * 8;
+  const int n = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(8), x.cols - col)));
+  const int r_end = n > 0 ? (static_cast<int>(rank) + 1) * share : 0;
+  ColumnTerms terms;
+  uint4 first = make_uint4(0, 0, 0, 0);
+  if (r_first < r_end && row0 + r_first < x.rows) {
+    load_terms(x.ep, col, n, terms);
+    if (x.ep.add) first = load8(x.ep.add, x.ep.ld_add, row0 + r_first, col, n);
+  }
   // The sums, NT columns of 128 lanes, to shared memory: the operands there have
   // been multiplied.
   float* sums = reinterpret_cast<float*>(smem);
@@ -878,24 +941,12 @@ __global__ void __launch_bounds__(kSplitThreads)
   }
   tc_fence_after();
   if (warp == 1) tmem_dealloc(tmem, kCols);
-  // This CTA's rows of the tile, eight columns a thread.
-  {
-    const int share = NT / split, r0 = static_cast<int>(rank) * share;
-    const uint32_t mine = smem_u32(sums);
-    for (int w = threadIdx.x; w < share * 16; w += kSplitThreads) {
-      const int r = r0 + (w >> 4), c = (w & 15) * 8;
-      const int64_t row = tm * NT + r, col = tn * kRows + c;
-      if (row >= x.rows || col >= x.cols) continue;
-      const uint32_t at = mine + (r * kRows + c) * 4;
-      float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      for (int p = 0; p < split; ++p) {
-        const uint32_t from = split > 1 ? mapa_shared(at, p) : at;
-        const float4 a = ld_cluster_f4(from), b = ld_cluster_f4(from + 16);
-        z[0] += a.x, z[1] += a.y, z[2] += a.z, z[3] += a.w;
-        z[4] += b.x, z[5] += b.y, z[6] += b.z, z[7] += b.w;
-      }
-      finish8(x, row, col, z);
-    }
+  const uint32_t at = smem_u32(sums) + (threadIdx.x & 15) * 32;
+  switch (split) {
+    case 1: finish_rows<1>(x, row0, col, n, r_first, r_end, at, terms, first); break;
+    case 2: finish_rows<2>(x, row0, col, n, r_first, r_end, at, terms, first); break;
+    case 4: finish_rows<4>(x, row0, col, n, r_first, r_end, at, terms, first); break;
+    default: finish_rows<8>(x, row0, col, n, r_first, r_end, at, terms, first);
   }
   if (split > 1) cluster_sync_all();  // no CTA leaves while another reads its sums
 }

@@ -9,20 +9,23 @@ namespace oz2 {
 namespace {
 
 // ---------------------------------------------------------------------------
-// Pack: a thread writes 16 bytes of a destination row from as many loads as the
-// source's alignment allows (its elements, one by one).
+// Pack: a thread writes 16 bytes of a destination row from its elements, one by one
+// (consecutive threads' are consecutive).  Up to two operands in one launch: the
+// blocks of the second grid row take the second.
 // ---------------------------------------------------------------------------
 template <typename T>
-__global__ void __launch_bounds__(256) pack_rows_kernel(const T* __restrict__ src, int64_t ld_src, int64_t rows,
-                                                        int64_t cols, T* __restrict__ dst, int64_t ld_dst) {
+__global__ void __launch_bounds__(256) pack_rows_kernel(PackJob a, PackJob b) {
   pdl_trigger();
   pdl_wait();
   constexpr int kVec = 16 / sizeof(T);
-  const int64_t per = (cols + kVec - 1) / kVec;
-  for (int64_t i = blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x; i < rows * per;
+  const PackJob& x = blockIdx.y ? b : a;
+  const T* src = static_cast<const T*>(x.src);
+  T* dst = static_cast<T*>(x.dst);
+  const int64_t per = (x.cols + kVec - 1) / kVec;
+  for (int64_t i = blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x; i < x.rows * per;
        i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
     const int64_t r = i / per, c = (i - r * per) * kVec;
-    const T* s = src + r * ld_src + c;
+    const T* s = src + r * x.ld_src + c;
     union {
       uint4 v;
       T e[kVec];
@@ -30,8 +33,8 @@ __global__ void __launch_bounds__(256) pack_rows_kernel(const T* __restrict__ sr
     w.v = make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int j = 0; j < kVec; ++j)
-      if (c + j < cols) w.e[j] = __ldg(s + j);
-    *reinterpret_cast<uint4*>(dst + r * ld_dst + c) = w.v;
+      if (c + j < x.cols) w.e[j] = __ldg(s + j);
+    *reinterpret_cast<uint4*>(dst + r * x.ld_dst + c) = w.v;
   }
 }
 
@@ -134,16 +137,28 @@ __global__ void __launch_bounds__(32 * kGradWarps)
   }
 }
 
-__global__ void __launch_bounds__(128) sum_chunks_kernel(int64_t n, int64_t chunks, const float* __restrict__ partial,
+// db from the chunks' sums: a warp's lanes are 32 columns, its 8 warps each add every
+// eighth chunk, and their sums are joined in order.
+__global__ void __launch_bounds__(256) sum_chunks_kernel(int64_t n, int64_t chunks, const float* __restrict__ partial,
                                                          float* __restrict__ db, bool accumulate) {
+  __shared__ float sums[8][32];
   pdl_trigger();
   pdl_wait();
-  const int64_t j = blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x;
-  if (j >= n) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t j = blockIdx.x * 32LL + lane;
   float t = 0.f;
-#pragma unroll 4
-  for (int64_t c = 0; c < chunks; ++c) t += partial[c * n + j];
-  db[j] = accumulate ? db[j] + t : t;
+  if (j < n) {
+#pragma unroll 8
+    for (int64_t c = warp; c < chunks; c += 8) t += partial[c * n + j];
+  }
+  sums[warp][lane] = t;
+  __syncthreads();
+  if (warp == 0 && j < n) {
+    t = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) t += sums[w][lane];
+    db[j] = accumulate ? db[j] + t : t;
+  }
 }
 
 int64_t chunk_rows_for(int64_t m, int64_t n) {
@@ -170,17 +185,14 @@ int64_t lin_db_chunks(int64_t m, int64_t n) {
   return std::max<int64_t>(1, (m + r - 1) / r);
 }
 
-cudaError_t launch_pack_rows(const void* src, int64_t ld_src, int64_t rows, int64_t cols, int bytes, void* dst,
-                             int64_t ld_dst, cudaStream_t st) {
-  const int64_t pieces = rows * ((cols * bytes + 15) / 16);
+cudaError_t launch_pack_rows(const PackJob* jobs, int count, int bytes, cudaStream_t st) {
+  int64_t pieces = 0;
+  for (int i = 0; i < count; ++i) pieces = std::max(pieces, jobs[i].rows * ((jobs[i].cols * bytes + 15) / 16));
   if (pieces == 0) return cudaSuccess;
   const unsigned blocks = static_cast<unsigned>(std::min<int64_t>((pieces + 255) / 256, 16LL * num_sms()));
   count_launch();
-  if (bytes == 1)
-    return launch_dependent(pack_rows_kernel<uint8_t>, dim3(blocks), dim3(256), 0, st,
-                            static_cast<const uint8_t*>(src), ld_src, rows, cols, static_cast<uint8_t*>(dst), ld_dst);
-  return launch_dependent(pack_rows_kernel<uint16_t>, dim3(blocks), dim3(256), 0, st,
-                          static_cast<const uint16_t*>(src), ld_src, rows, cols, static_cast<uint16_t*>(dst), ld_dst);
+  return launch_dependent(bytes == 1 ? pack_rows_kernel<uint8_t> : pack_rows_kernel<uint16_t>,
+                          dim3(blocks, static_cast<unsigned>(count)), dim3(256), 0, st, jobs[0], jobs[count - 1]);
 }
 
 cudaError_t launch_act_grad(int64_t m, int64_t n, int type, int act, const void* dy, int64_t ld_dy, const void* z,
@@ -198,7 +210,7 @@ cudaError_t launch_act_grad(int64_t m, int64_t n, int type, int act, const void*
       static_cast<const uint16_t*>(z), ld_z, static_cast<uint16_t*>(dz), ld_dz, db ? partial : nullptr);
   if (err != cudaSuccess || !db) return err;
   count_launch();
-  return launch_dependent(sum_chunks_kernel, dim3(static_cast<unsigned>((n + 127) / 128)), dim3(128), 0, st, n, chunks,
+  return launch_dependent(sum_chunks_kernel, dim3(static_cast<unsigned>((n + 31) / 32)), dim3(256), 0, st, n, chunks,
                           partial, db, accumulate);
 }
 

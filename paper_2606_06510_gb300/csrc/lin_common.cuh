@@ -134,9 +134,14 @@ cudaError_t launch_linear(const LinProduct* products, int count, int type, const
                           Oz2Device* dev, cudaStream_t st);
 
 // Rows of elements of `bytes` bytes copied to rows that start on 16-byte
-// boundaries (ld_dst·bytes a multiple of 16).
-cudaError_t launch_pack_rows(const void* src, int64_t ld_src, int64_t rows, int64_t cols, int bytes, void* dst,
-                             int64_t ld_dst, cudaStream_t st);
+// boundaries (ld_dst·bytes a multiple of 16), for one or two operands at once.
+struct PackJob {
+  const void* src;
+  int64_t ld_src, rows, cols;
+  void* dst;
+  int64_t ld_dst;
+};
+cudaError_t launch_pack_rows(const PackJob* jobs, int count, int bytes, cudaStream_t st);
 
 // dz = dy·act'(z) in the operands' type into rows of ld_dz elements (16-byte
 // rows; null: not wanted), and db = its column sums before that rounding

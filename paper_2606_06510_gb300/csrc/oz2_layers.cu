@@ -62,16 +62,21 @@ struct Operand {
       : p(src), ld(r > 1 ? ld_src : padded_ld(c, b)), rows(r), cols(c), bytes(b), copy(!on16(src, ld, b)), off(0) {
     if (copy) off = ws.ask(static_cast<size_t>(rows) * padded_ld(cols, bytes) * bytes);
   }
-  cudaError_t place(const Workspace& ws, cudaStream_t st) {
-    if (!copy) return cudaSuccess;
-    void* dst = ws.at<void>(off);
-    const int64_t ld_dst = padded_ld(cols, bytes);
-    const cudaError_t err = launch_pack_rows(p, ld, rows, cols, bytes, dst, ld_dst, st);
-    p = dst;
-    ld = ld_dst;
-    return err;
-  }
 };
+
+// The copies that the operands want, in one launch.
+cudaError_t place(Operand& a, Operand& b, const Workspace& ws, cudaStream_t st) {
+  PackJob jobs[2];
+  int count = 0;
+  for (Operand* o : {&a, &b}) {
+    if (!o->copy || o->rows == 0 || o->cols == 0) continue;
+    PackJob& j = jobs[count++];
+    j = PackJob{o->p, o->ld, o->rows, o->cols, ws.at<void>(o->off), padded_ld(o->cols, o->bytes)};
+    o->p = j.dst;
+    o->ld = j.ld_dst;
+  }
+  return count ? launch_pack_rows(jobs, count, a.bytes, st) : cudaSuccess;
+}
 
 bool valid_act(int act) { return act >= OZ2_ACT_NONE && act <= OZ2_ACT_SILU; }
 
@@ -114,8 +119,7 @@ int oz2_linear(int64_t m, int64_t n, int64_t k, int type, const void* d_X, int64
   Operand X(d_X, ldx, k ? m : 0, k, es, ws), W(d_W, ldw, k ? n : 0, k, es, ws);
   const size_t scratch = ws.ask(plan.scratch);
   if (!ws.take()) return OZ2_ERR_ALLOC;
-  cudaError_t err = X.place(ws, st);
-  if (err == cudaSuccess) err = W.place(ws, st);
+  const cudaError_t err = place(X, W, ws, st);
   if (err != cudaSuccess) return status_of(err);
   p.p = X.p;
   p.ldp = X.ld;
@@ -195,8 +199,7 @@ int oz2_linear_grad(int64_t m, int64_t n, int64_t k, int type, const void* d_dY,
       ldz_used = ld_dz;
     }
   }
-  if (err == cudaSuccess) err = X.place(ws, st);
-  if (err == cudaSuccess) err = W.place(ws, st);
+  if (err == cudaSuccess) err = place(X, W, ws, st);
   if (err != cudaSuccess || !count) return status_of(err);
   if (pdx) {
     pdx->p = dz;

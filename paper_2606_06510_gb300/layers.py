@@ -42,16 +42,44 @@ SIGS = {
 }
 
 
-def _rows(t: torch.Tensor, rows: int, cols: int, what: str) -> int:
-    """The row stride of a (rows, cols) CUDA matrix."""
+# The C entry points by name, looked up on first use (an import inside each call is
+# some 2 µs of it).
+_ENTRIES = {}
+
+
+def _entry(name):
+    from . import lib
+    f = _ENTRIES[name] = getattr(lib(), name)
+    return f
+
+
+def _done(code, what):
+    if code:
+        from . import Oz2Error
+        raise Oz2Error(code, what)
+
+
+def _stream(stream):
+    if stream is not None:
+        return stream.cuda_stream
+    if not torch.cuda.is_initialized():
+        torch.cuda.init()
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
+def _ld(t, rows, cols, what):
+    """The row stride of a CUDA matrix of this shape."""
     assert t.is_cuda, f"{what}: oz2 operates on CUDA tensors"
-    assert t.shape == (rows, cols), f"{what}: expected shape ({rows}, {cols}), got {tuple(t.shape)}"
     s0, s1 = t.stride()
-    if rows > 1:
-        assert (s1 == 1 or cols <= 1) and s0 >= cols, f"{what}: rows must be contiguous (stride(1) == 1)"
-        return max(s0, 1)
-    assert s1 == 1 or cols <= 1, f"{what}: rows must be contiguous (stride(1) == 1)"
-    return max(cols, 1)
+    assert (s1 == 1 or cols <= 1) and (s0 >= cols or rows <= 1), f"{what}: rows must be contiguous (stride(1) == 1)"
+    return s0 if rows > 1 and s0 > 0 else cols or 1
+
+
+def _rows(t, rows, cols, dtype, what):
+    """(address, row stride) of a CUDA matrix of this shape and dtype."""
+    assert t.shape == (rows, cols) and t.dtype == dtype, \
+        f"{what}: expected shape ({rows}, {cols}) and {dtype}, got {tuple(t.shape)} and {t.dtype}"
+    return t.data_ptr(), _ld(t, rows, cols, what)
 
 
 def _vector(t, count, dtype, what):
@@ -72,30 +100,34 @@ def oz2_linear(x, w, bias=None, act="none", residual=None, x_scale=None, w_scale
     activation's argument, which oz2_linear_grad wants.  `out` may be the
     residual itself.
     """
-    from . import _check, _stream, lib
     m, k = x.shape
     n, k2 = w.shape
-    assert k == k2 and x.dtype == w.dtype, "x and w: expected (m, k) and (n, k) of one dtype"
-    dt = x.dtype if x.dtype != torch.float8_e4m3fn else out_dtype or torch.bfloat16
+    xt = dt = x.dtype
+    assert k == k2 and w.dtype == xt, "x and w: expected (m, k) and (n, k) of one dtype"
+    if xt == torch.float8_e4m3fn:
+        dt = out_dtype or torch.bfloat16
     assert out_dtype is None or out_dtype == dt, "out_dtype: a 16-bit product has its operands' dtype"
-    ldx, ldw = _rows(x, m, k, "x"), _rows(w, n, k, "w")
-    y = torch.empty((m, n), dtype=dt, device=x.device) if out is None else out
-    assert y.dtype == dt, f"out: expected {dt}"
-    ldy = _rows(y, m, n, "out") if out is not None else max(n, 1)
-    z, zp, ldr, rp, bp, bt = None, None, 0, None, None, 0
+    ldx, ldw = _ld(x, m, k, "x"), _ld(w, n, k, "w")
+    if out is None:
+        y, ldy = x.new_empty((m, n), dtype=dt), n or 1
+        yp = y.data_ptr()
+    else:
+        y = out
+        yp, ldy = _rows(y, m, n, dt, "out")
+    z = zp = rp = bp = None
+    ldr = bt = 0
     if save_pre:
-        z = torch.empty((m, n), dtype=dt, device=x.device)
+        z = x.new_empty((m, n), dtype=dt)
         zp = z.data_ptr()
     if residual is not None:
-        assert residual.dtype == dt, f"residual: expected {dt}"
-        ldr, rp = _rows(residual, m, n, "residual"), residual.data_ptr()
+        rp, ldr = _rows(residual, m, n, dt, "residual")
     if bias is not None:
         bp, bt = _vector(bias, n, (dt, torch.float32), "bias"), TYPE[bias.dtype]
     xs = _vector(x_scale, m, (torch.float32,), "x_scale") if x_scale is not None else None
     ws = _vector(w_scale, n, (torch.float32,), "w_scale") if w_scale is not None else None
-    _check(lib().oz2_linear(m, n, k, TYPE.get(x.dtype, -1), x.data_ptr(), ldx, w.data_ptr(), ldw, xs, ws, bp, bt,
-                            ACT[act], rp, ldr, zp, max(n, 1), y.data_ptr(), ldy, TYPE.get(dt, -1), _stream(stream)),
-           "oz2_linear")
+    _done((_ENTRIES.get("oz2_linear") or _entry("oz2_linear"))(
+        m, n, k, TYPE.get(xt, -1), x.data_ptr(), ldx, w.data_ptr(), ldw, xs, ws, bp, bt, ACT[act], rp, ldr, zp, n or 1,
+        yp, ldy, TYPE.get(dt, -1), _stream(stream)), "oz2_linear")
     return (y, z) if save_pre else y
 
 
@@ -108,47 +140,45 @@ def oz2_linear_grad(dy, x, w, pre=None, act="none", need=("dx", "dw", "db"), dx=
     tensor to write.  With accumulate, dw (float32) and db are added to, and
     must be given.  The residual's gradient is dy itself.
     """
-    from . import _check, _stream, lib
     m, n = dy.shape
     k = x.shape[1]
     dt = dy.dtype
-    assert x.dtype == w.dtype == dt, "dy, x and w: expected one dtype"
-    ldy, ldx, ldw = _rows(dy, m, n, "dy"), _rows(x, m, k, "x"), _rows(w, n, k, "w")
+    assert x.dtype == w.dtype == dt and x.shape[0] == m and w.shape == (n, k), \
+        "dy, x and w: expected (m, n), (m, k) and (n, k) of one dtype"
+    ldy, ldx, ldw = _ld(dy, m, n, "dy"), _ld(x, m, k, "x"), _ld(w, n, k, "w")
     ldz, zp = 1, None
     if act != "none":
-        assert pre is not None and pre.dtype == dt, "pre: the activation's gradient wants the z that was kept"
-        ldz, zp = _rows(pre, m, n, "pre"), pre.data_ptr()
-    assert not accumulate or all(t is not None for t, name in ((dw, "dw"), (db, "db")) if name in need), \
+        assert pre is not None, "pre: the activation's gradient wants the z that was kept"
+        zp, ldz = _rows(pre, m, n, dt, "pre")
+    assert not accumulate or (("dw" not in need or dw is not None) and ("db" not in need or db is not None)), \
         "accumulate: dw and db have to be given"
     xp = wp = bp = None
-    lddx = lddw = max(k, 1)
+    lddx = lddw = k or 1
     wt = 0
-    if "dx" in need:
-        if dx is None:
-            dx = torch.empty((m, k), dtype=dt, device=dy.device)
-        else:
-            assert dx.dtype == dt, f"dx: expected {dt}"
-            lddx = _rows(dx, m, k, "dx")
+    if "dx" not in need:
+        dx = None
+    elif dx is None:
+        dx = dy.new_empty((m, k))
         xp = dx.data_ptr()
     else:
-        dx = None
-    if "dw" in need:
-        if dw is None:
-            dw = torch.empty((n, k), dtype=dw_dtype or dt, device=dy.device)
-        else:
-            lddw = _rows(dw, n, k, "dw")
+        xp, lddx = _rows(dx, m, k, dt, "dx")
+    if "dw" not in need:
+        dw = None
+    elif dw is None:
+        dw = dy.new_empty((n, k), dtype=dw_dtype or dt)
         wp, wt = dw.data_ptr(), TYPE.get(dw.dtype, -1)
     else:
-        dw = None
-    if "db" in need:
-        if db is None:
-            db = torch.empty(n, dtype=torch.float32, device=dy.device)
-        bp = _vector(db, n, (torch.float32,), "db")
-    else:
+        wp, lddw = _rows(dw, n, k, dw.dtype, "dw")
+        wt = TYPE.get(dw.dtype, -1)
+    if "db" not in need:
         db = None
-    _check(lib().oz2_linear_grad(m, n, k, TYPE.get(dt, -1), dy.data_ptr(), ldy, zp, ldz, ACT[act], x.data_ptr(), ldx,
-                                 w.data_ptr(), ldw, xp, lddx, wp, lddw, wt, bp, GRAD_ACCUMULATE if accumulate else 0,
-                                 _stream(stream)), "oz2_linear_grad")
+    else:
+        if db is None:
+            db = dy.new_empty(n, dtype=torch.float32)
+        bp = _vector(db, n, (torch.float32,), "db")
+    _done((_ENTRIES.get("oz2_linear_grad") or _entry("oz2_linear_grad"))(
+        m, n, k, TYPE.get(dt, -1), dy.data_ptr(), ldy, zp, ldz, ACT[act], x.data_ptr(), ldx, w.data_ptr(), ldw, xp, lddx,
+        wp, lddw, wt, bp, GRAD_ACCUMULATE if accumulate else 0, _stream(stream)), "oz2_linear_grad")
     return dx, dw, db
 
 
@@ -227,7 +257,6 @@ def oz2_adamw(plan: AdamWPlan, step: int, lr: float, beta1=0.9, beta2=0.999, eps
               grad_scale=None, seed=0, stream=None):
     """One AdamW step, in place.  step counts from 1; grad_scale: a float32 CUDA
     scalar that multiplies the gradients; seed: of the 8-bit states' rounding."""
-    from . import _check, _stream, lib
     a = plan.args
     a.step, a.lr, a.beta1, a.beta2, a.eps, a.weight_decay, a.seed = step, lr, beta1, beta2, eps, weight_decay, seed
     if grad_scale is not None:
@@ -235,5 +264,6 @@ def oz2_adamw(plan: AdamWPlan, step: int, lr: float, beta1=0.9, beta2=0.999, eps
         a.d_grad_scale = grad_scale.data_ptr()
     else:
         a.d_grad_scale = None
-    _check(lib().oz2_adamw(plan.tensors, len(plan.tensors), TYPE.get(plan.param_type, -1),
-                           TYPE.get(plan.grad_type, -1), plan.bits, ctypes.byref(a), _stream(stream)), "oz2_adamw")
+    _done((_ENTRIES.get("oz2_adamw") or _entry("oz2_adamw"))(
+        plan.tensors, len(plan.tensors), TYPE.get(plan.param_type, -1), TYPE.get(plan.grad_type, -1), plan.bits,
+        ctypes.byref(a), _stream(stream)), "oz2_adamw")
