@@ -176,13 +176,6 @@ __device__ __forceinline__ float cut_stochastic(float y, uint32_t u) {
   return SIGNED ? copysignf(r, y) : r;
 }
 
-// 1/x to about 2^-23 (x below 2^-126 counts as 0).
-__device__ __forceinline__ float reciprocal(float x) {
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-
 // A warp's 256 values as they were loaded.
 struct AdamRaw {
   uint32_t g[2][4], w[2][4], m[2][4], v[2][4];

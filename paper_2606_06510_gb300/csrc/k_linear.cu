@@ -127,57 +127,48 @@ __device__ __forceinline__ bool vec_ok(const void* p, int64_t ld, int bytes) {
   return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(ld * bytes)) & 15) == 0;
 }
 
-// A warp's 32 rows × 32 columns of 16 bits between global and shared memory; what
-// lies past the matrix is not touched.  The fetch is in two halves, so that its
-// loads can be on their way early.
+// A warp's 32 rows × 32 columns of 16 bits between global and shared memory: by 16
+// bytes a lane, eight rows at a time, where the whole of them lies inside the matrix
+// and on 16-byte boundaries (`from`, `to`: this lane's place in the first eight rows),
+// else by single values, and what lies past the matrix is not touched.  The fetch is
+// in two halves, so that its loads can be on their way early.
 struct Fetched {
   uint4 v[4];
 };
-__device__ __forceinline__ void fetch_begin(const LinUnits& x, const void* src, int64_t ld, int64_t row0, int64_t col0,
-                                            int lane, Fetched& f) {
-  const uint16_t* s = static_cast<const uint16_t*>(src);
-  if (vec_ok(src, ld, 2) && col0 + kChunk <= x.cols) {
+__device__ __forceinline__ void fetch_begin(const uint16_t* from, int64_t ld, Fetched& f) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = 8 * i + (lane >> 2), c = lane & 3;
-      f.v[i] = make_uint4(0, 0, 0, 0);
-      if (row0 + r < x.rows) f.v[i] = __ldg(reinterpret_cast<const uint4*>(s + (row0 + r) * ld + col0 + 8 * c));
-    }
-  }
+  for (int i = 0; i < 4; ++i) f.v[i] = __ldg(reinterpret_cast<const uint4*>(from + 8 * i * ld));
 }
-__device__ __forceinline__ void fetch_end(const LinUnits& x, const void* src, int64_t ld, int64_t row0, int64_t col0,
-                                          int lane, uint8_t* buf, const Fetched& f) {
-  const uint16_t* s = static_cast<const uint16_t*>(src);
-  if (vec_ok(src, ld, 2) && col0 + kChunk <= x.cols) {
+__device__ __forceinline__ void fetch_end(const Fetched& f, int lane, uint8_t* buf) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sts128(buf + piece_at(8 * i + (lane >> 2), lane & 3), f.v[i]);
-  } else if (col0 + lane < x.cols) {
-#pragma unroll 8
-    for (int r = 0; r < 32; ++r)
-      if (row0 + r < x.rows)
-        *reinterpret_cast<uint16_t*>(buf + piece_at(r, lane >> 3) + 2 * (lane & 7)) =
-            __ldg(s + (row0 + r) * ld + col0 + lane);
-  }
+  for (int i = 0; i < 4; ++i) sts128(buf + piece_at(8 * i + (lane >> 2), lane & 3), f.v[i]);
 }
-__device__ __forceinline__ void store16(const LinUnits& x, void* dst, int64_t ld, int64_t row0, int64_t col0, int lane,
-                                        const uint8_t* buf) {
-  uint16_t* d = static_cast<uint16_t*>(dst);
-  if (vec_ok(dst, ld, 2) && col0 + kChunk <= x.cols) {
+__device__ __forceinline__ void store_fast(uint16_t* to, int64_t ld, int lane, const uint8_t* buf) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = 8 * i + (lane >> 2), c = lane & 3;
-      if (row0 + r < x.rows)
-        *reinterpret_cast<uint4*>(d + (row0 + r) * ld + col0 + 8 * c) = lds128(buf + piece_at(r, c));
-    }
-  } else if (col0 + lane < x.cols) {
+  for (int i = 0; i < 4; ++i)
+    *reinterpret_cast<uint4*>(to + 8 * i * ld) = lds128(buf + piece_at(8 * i + (lane >> 2), lane & 3));
+}
+__device__ __forceinline__ uint8_t* value_at(uint8_t* buf, int row, int col) {
+  return buf + piece_at(row, col >> 3) + 2 * (col & 7);
+}
+__device__ __noinline__ void fetch_slow(const void* src, int64_t ld, int64_t rows, int64_t cols, int64_t row0,
+                                        int64_t col0, int lane, uint8_t* buf) {
+  const uint16_t* s = static_cast<const uint16_t*>(src) + row0 * ld + col0 + lane;
+  if (col0 + lane >= cols) return;
 #pragma unroll 8
-    for (int r = 0; r < 32; ++r)
-      if (row0 + r < x.rows)
-        d[(row0 + r) * ld + col0 + lane] = *reinterpret_cast<const uint16_t*>(buf + piece_at(r, lane >> 3) + 2 * (lane & 7));
-  }
+  for (int r = 0; r < 32; ++r)
+    if (row0 + r < rows) *reinterpret_cast<uint16_t*>(value_at(buf, r, lane)) = __ldg(s + r * ld);
+}
+__device__ __noinline__ void store_slow(void* dst, int64_t ld, int64_t rows, int64_t cols, int64_t row0, int64_t col0,
+                                        int lane, uint8_t* buf) {
+  uint16_t* d = static_cast<uint16_t*>(dst) + row0 * ld + col0 + lane;
+  if (col0 + lane >= cols) return;
+#pragma unroll 8
+  for (int r = 0; r < 32; ++r)
+    if (row0 + r < rows) d[r * ld] = *reinterpret_cast<const uint16_t*>(value_at(buf, r, lane));
 }
 // 16 columns of FP32, stored or added to.
-__device__ __forceinline__ void store32(const LinUnits& x, void* dst, int64_t ld, int64_t row0, int64_t col0, int lane,
+__device__ __noinline__ void store32(const LinUnits& x, void* dst, int64_t ld, int64_t row0, int64_t col0, int lane,
                                         const uint8_t* buf, bool add) {
   float* d = static_cast<float*>(dst);
   const int c = lane & 15;
@@ -202,22 +193,20 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&v)[32]) {
 }
 
 // 32 sums of one row (columns c.. of the warp's) with their scales and biases.
-__device__ __forceinline__ void scaled(const float* scale_s, const float* bias_s, float row_scale, const uint32_t (&v)[32],
-                                       int c, bool scales, float (&z)[32]) {
+__device__ __forceinline__ void scale32(const float* scale_s, float row_scale, int c, float (&z)[32]) {
+#pragma unroll
+  for (int j = 0; j < 32; j += 4) {
+    const float4 s = *reinterpret_cast<const float4*>(scale_s + c + j);
+    z[j] *= row_scale * s.x;
+    z[j + 1] *= row_scale * s.y;
+    z[j + 2] *= row_scale * s.z;
+    z[j + 3] *= row_scale * s.w;
+  }
+}
+__device__ __forceinline__ void bias32(const float* bias_s, int c, float (&z)[32]) {
 #pragma unroll
   for (int j = 0; j < 32; j += 4) {
     const float4 b = *reinterpret_cast<const float4*>(bias_s + c + j);
-    z[j] = __uint_as_float(v[j]);
-    z[j + 1] = __uint_as_float(v[j + 1]);
-    z[j + 2] = __uint_as_float(v[j + 2]);
-    z[j + 3] = __uint_as_float(v[j + 3]);
-    if (scales) {
-      const float4 s = *reinterpret_cast<const float4*>(scale_s + c + j);
-      z[j] *= row_scale * s.x;
-      z[j + 1] *= row_scale * s.y;
-      z[j + 2] *= row_scale * s.z;
-      z[j + 3] *= row_scale * s.w;
-    }
     z[j] += b.x;
     z[j + 1] += b.y;
     z[j + 2] += b.z;
@@ -247,6 +236,12 @@ __device__ __forceinline__ void finish32(const float (&z)[32], bool add, bool bf
     sts128(at, make_uint4(pack16(y[0], y[1], bf16), pack16(y[2], y[3], bf16), pack16(y[4], y[5], bf16),
                           pack16(y[6], y[7], bf16)));
   }
+}
+
+__device__ __forceinline__ int count_part(int* at) {
+  int before;
+  asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(before) : "l"(at) : "memory");
+  return before;
 }
 
 // --- the work of a CTA pair --------------------------------------------------------
@@ -466,22 +461,35 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
       const LinUnits& x = L.u[pc.i];
       const LinEpilogue& ep = x.ep;
       const int64_t row0 = pc.tm * kLinTile + rank * kRows + 32 * q, col0 = pc.tn * kLinTile + kLinCols * h;
-      const bool bf16 = ep.out_type == OZ2_TYPE_BF16, scales = ep.row_scale != nullptr, add = ep.add != nullptr;
+      const bool bf16 = TYPE == OZ2_TYPE_BF16 || (F8 && ep.out_type == OZ2_TYPE_BF16);
+      const bool scales = F8 && ep.row_scale != nullptr, add = ep.add != nullptr;
       const bool sums = pc.t1 > pc.t0;
+      // Where this warp's corner is inside the matrix and on 16-byte boundaries.
+      const bool inside = row0 + 32 <= x.rows && col0 + kLinCols <= x.cols;
+      const bool fast_add = inside && vec_ok(ep.add, ep.ld_add, 2), fast_pre = inside && vec_ok(ep.pre, ep.ld_pre, 2),
+                 fast_out = inside && vec_ok(ep.out, ep.ld_out, 2);
+      const int64_t lane_row = row0 + (lane >> 2), lane_col = col0 + 8 * (lane & 3);
       __syncwarp();
+      if (ep.bias) {
 #pragma unroll
-      for (int c = lane; c < kLinCols; c += 32) {
-        const int64_t j = col0 + c;
-        float b = 0.f;
-        if (ep.bias && j < x.cols)
-          b = ep.bias_type == OZ2_TYPE_F32 ? __ldg(static_cast<const float*>(ep.bias) + j)
-                                           : load16(static_cast<const uint16_t*>(ep.bias) + j, ep.bias_type == OZ2_TYPE_BF16);
-        bias_s[c] = b;
-        if (scales) scale_s[c] = j < x.cols ? __ldg(ep.col_scale + j) : 0.f;
+        for (int c = lane; c < kLinCols; c += 32) {
+          const int64_t j = col0 + c;
+          float b = 0.f;
+          if (j < x.cols)
+            b = ep.bias_type == OZ2_TYPE_F32 ? __ldg(static_cast<const float*>(ep.bias) + j)
+                                             : load16(static_cast<const uint16_t*>(ep.bias) + j, bf16);
+          bias_s[c] = b;
+        }
       }
-      const float row_scale = scales && row0 + lane < x.rows ? __ldg(ep.row_scale + row0 + lane) : 0.f;
+      float row_scale = 0.f;
+      if (scales) {
+#pragma unroll
+        for (int c = lane; c < kLinCols; c += 32) scale_s[c] = col0 + c < x.cols ? __ldg(ep.col_scale + col0 + c) : 0.f;
+        if (row0 + lane < x.rows) row_scale = __ldg(ep.row_scale + row0 + lane);
+      }
       Fetched r;
-      if (add) fetch_begin(x, ep.add, ep.ld_add, row0, col0, lane, r);
+      const uint16_t* from = static_cast<const uint16_t*>(ep.add) + lane_row * ep.ld_add + lane_col;
+      if (fast_add && add) fetch_begin(from, ep.ld_add, r);
       __syncwarp();
       if (sums) {
         if (!mbar_wait_bounded(acc_full + 8 * acc, accph, kWaitLimit)) ok = false;
@@ -520,16 +528,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
             __stcg(reinterpret_cast<uint4*>(to + (c + j) * 32), make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]));
         }
         release();
-        __threadfence();
+        // The warp's stores come before its lane's count (which releases them, and
+        // takes over those that it counts after), the last warp's loads after it.
         __syncwarp();
         int before = 0;
-        if (lane == 0)
-          before = atomicAdd(L.arrived + (pc.tile * 2 + rank) * kLinEpiWarps + ew, 1);
+        if (lane == 0) before = count_part(L.arrived + (pc.tile * 2 + rank) * kLinEpiWarps + ew);
         if (__shfl_sync(0xffffffffu, before, 0) != pc.parts - 1) continue;
-        __threadfence();
+        __syncwarp();
       }
-      auto load = [&](int c, float (&z)[32]) {
-        uint32_t v[32];
+#pragma unroll 1
+      for (int c = 0; c < kLinCols; c += kChunk) {
+        float z[32];
         if (pc.parts > 1) {
 #pragma unroll
           for (int j = 0; j < 32; j += 4) {
@@ -539,29 +548,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
           }
 #pragma unroll 2
           for (int p = 1; p < pc.parts; ++p) {
-            const float* from = L.sums + static_cast<int64_t>(pc.first_slot + p * pc.stride) * kPartFloats + corner;
+            const float* part = L.sums + static_cast<int64_t>(pc.first_slot + p * pc.stride) * kPartFloats + corner;
 #pragma unroll
             for (int j = 0; j < 32; j += 4) {
-              const float4 a = __ldcg(reinterpret_cast<const float4*>(from + (c + j) * 32));
+              const float4 a = __ldcg(reinterpret_cast<const float4*>(part + (c + j) * 32));
               z[j] += a.x, z[j + 1] += a.y, z[j + 2] += a.z, z[j + 3] += a.w;
             }
           }
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(z[j]);
         } else if (sums) {
+          uint32_t v[32];
           tmem_ld32(at + c, v);
           tmem_ld_wait();
           if (c == kLinCols - kChunk) release();
+#pragma unroll
+          for (int j = 0; j < 32; ++j) z[j] = __uint_as_float(v[j]);
         } else {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = 0u;
+          for (int j = 0; j < 32; ++j) z[j] = 0.f;
         }
-        scaled(scale_s, bias_s, row_scale, v, c, scales, z);
-      };
-#pragma unroll 1
-      for (int c = 0; c < kLinCols; c += kChunk) {
-        float z[32];
-        load(c, z);
         if (ep.out_type == OZ2_TYPE_F32) {
 #pragma unroll
           for (int g = 0; g < 32; g += 16) {
@@ -575,15 +579,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
           }
           continue;
         }
+        if (scales) scale32(scale_s, row_scale, c, z);
+        if (ep.bias) bias32(bias_s, c, z);
         if (ep.pre) {
           finish32<OZ2_ACT_NONE>(z, false, bf16, buf, lane);
           __syncwarp();
-          store16(x, ep.pre, ep.ld_pre, row0, col0 + c, lane, buf);
+          if (fast_pre) {
+            store_fast(static_cast<uint16_t*>(ep.pre) + lane_row * ep.ld_pre + lane_col + c, ep.ld_pre, lane, buf);
+          } else {
+            store_slow(ep.pre, ep.ld_pre, x.rows, x.cols, row0, col0 + c, lane, buf);
+          }
           __syncwarp();
         }
         if (add) {
-          fetch_end(x, ep.add, ep.ld_add, row0, col0 + c, lane, buf, r);
-          if (c + kChunk < kLinCols) fetch_begin(x, ep.add, ep.ld_add, row0, col0 + c + kChunk, lane, r);
+          if (fast_add) {
+            fetch_end(r, lane, buf);
+            if (c + kChunk < kLinCols) fetch_begin(from + c + kChunk, ep.ld_add, r);
+          } else {
+            fetch_slow(ep.add, ep.ld_add, x.rows, x.cols, row0, col0 + c, lane, buf);
+          }
           __syncwarp();
         }
         switch (ep.act) {
@@ -594,7 +608,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
           default: finish32<OZ2_ACT_NONE>(z, add, bf16, buf, lane);
         }
         __syncwarp();
-        store16(x, ep.out, ep.ld_out, row0, col0 + c, lane, buf);
+        if (fast_out) {
+          store_fast(static_cast<uint16_t*>(ep.out) + lane_row * ep.ld_out + lane_col + c, ep.ld_out, lane, buf);
+        } else {
+          store_slow(ep.out, ep.ld_out, x.rows, x.cols, row0, col0 + c, lane, buf);
+        }
         __syncwarp();
       }
     }

@@ -32,33 +32,46 @@ __device__ __forceinline__ float load16(const uint16_t* p, bool bf16) { return u
 
 // --- activations ---------------------------------------------------------------
 // exp and division are the fast ones (off by some 2^-21 of the value): results are
-// rounded to 16 bits, and in db's FP32 sums such errors average out.
+// rounded to 16 bits, and in db's FP32 sums such errors average out.  Results below
+// 2^-126 count as 0.
 constexpr float kSqrtHalf = 0.70710678118654752f, kSqrt2OverPi = 0.79788456080286536f, kInvSqrt2Pi = 0.39894228040143268f;
-constexpr float kGeluCubic = 0.044715f;
+constexpr float kGeluCubic = 0.044715f, kLog2E = 1.4426950408889634f;
 
-// Φ(-|z|) = exp(-x²)·(a1 t + ... + a5 t⁵)/2 with x = |z|/√2 and t = 1/(1 + p·x), off
-// by at most 7.5e-8 (Hastings; Abramowitz and Stegun 7.1.26), given ex = exp(-x²).  A
+__device__ __forceinline__ float reciprocal(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// Φ(-|z|) = exp(-z²/2)·(a1 t + ... + a5 t⁵)/2 with t = 1/(1 + p·|z|/√2), off by at
+// most 7.5e-8 (Hastings; Abramowitz and Stegun 7.1.26), given ex = exp(-z²/2).  A
 // third of erff's time, without its branch.
-__device__ __forceinline__ float gauss_tail(float x, float ex) {
-  const float t = __fdividef(1.f, fmaf(0.3275911f, x, 1.f));
-  return 0.5f * t * ex *
-         fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+__device__ __forceinline__ float gauss_tail(float z, float ex) {
+  const float t = reciprocal(fmaf(0.3275911f * kSqrtHalf, fabsf(z), 1.f));
+  return t * ex *
+         fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f), 0.5f * 1.421413741f),
+                      0.5f * -0.284496736f),
+              0.5f * 0.254829592f);
 }
 
 template <int ACT>
 __device__ __forceinline__ float activate(float z) {
   if (ACT == OZ2_ACT_RELU) return z < 0.f ? 0.f : z;  // NaN stays NaN
   if (ACT == OZ2_ACT_GELU) {
-    const float x = fabsf(z) * kSqrtHalf;
-    const float h = gauss_tail(x, __expf(-x * x));
-    return z > 0.f ? fmaf(-z, h, z) : z * h;
+    const float h = gauss_tail(z, exp2_fast(z * z * (-0.5f * kLog2E)));
+    return z * (z > 0.f ? 1.f - h : h);
   }
   if (ACT == OZ2_ACT_GELU_TANH) {
-    // z(1 + tanh u)/2 = z/(1 + exp(-2u))
-    const float u = kSqrt2OverPi * fmaf(kGeluCubic * z * z, z, z);
-    return __fdividef(z, 1.f + __expf(-2.f * u));
+    // z(1 + tanh u)/2 = z/(1 + exp(-2u)), u = √(2/π)(z + 0.044715 z³)
+    const float v = z * fmaf(-2.f * kLog2E * kSqrt2OverPi * kGeluCubic, z * z, -2.f * kLog2E * kSqrt2OverPi);
+    return z * reciprocal(1.f + exp2_fast(v));
   }
-  if (ACT == OZ2_ACT_SILU) return __fdividef(z, 1.f + __expf(-z));
+  if (ACT == OZ2_ACT_SILU) return z * reciprocal(1.f + exp2_fast(-kLog2E * z));
   return z;
 }
 
@@ -69,22 +82,21 @@ __device__ __forceinline__ float act_slope(float z) {
   if (ACT == OZ2_ACT_RELU) return z > 0.f ? 1.f : z == z ? 0.f : z;
   if (ACT == OZ2_ACT_GELU) {
     z = fabsf(z) > 16.f ? copysignf(16.f, z) : z;
-    const float x = fabsf(z) * kSqrtHalf, ex = __expf(-x * x);
-    const float h = gauss_tail(x, ex);
+    const float ex = exp2_fast(z * z * (-0.5f * kLog2E)), h = gauss_tail(z, ex);
     return fmaf(z * kInvSqrt2Pi, ex, z > 0.f ? 1.f - h : h);
   }
   if (ACT == OZ2_ACT_GELU_TANH) {
     // with g = (1 + tanh u)/2 = 1/(1 + exp(-2u)):  g + z·2g(1 - g)·u'
     z = fabsf(z) > 16.f ? copysignf(16.f, z) : z;
     const float zz = z * z;
-    const float u = kSqrt2OverPi * fmaf(kGeluCubic * zz, z, z);
-    const float g = __fdividef(1.f, 1.f + __expf(-2.f * u));
-    const float du = kSqrt2OverPi * fmaf(3.f * kGeluCubic, zz, 1.f);
-    return fmaf(2.f * z * g * (1.f - g), du, g);
+    const float v = z * fmaf(-2.f * kLog2E * kSqrt2OverPi * kGeluCubic, zz, -2.f * kLog2E * kSqrt2OverPi);
+    const float g = reciprocal(1.f + exp2_fast(v));
+    const float du2 = fmaf(6.f * kGeluCubic * kSqrt2OverPi, zz, 2.f * kSqrt2OverPi);
+    return fmaf(z * g * (1.f - g), du2, g);
   }
   if (ACT == OZ2_ACT_SILU) {
     z = fabsf(z) > 80.f ? copysignf(80.f, z) : z;
-    const float g = __fdividef(1.f, 1.f + __expf(-z));
+    const float g = reciprocal(1.f + exp2_fast(-kLog2E * z));
     return g * fmaf(z, 1.f - g, 1.f);
   }
   return 1.f;
