@@ -995,105 +995,147 @@ int64_t steps_of(const LinProduct& p, int type) {
 }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// The estimates (cycles of an SM) behind a plan, fitted to measurements on one
-// GB300: a step of a pair's tile 535, a tile's epilogue and start 1500, the launch's
-// own start and last epilogue 10000; the exchange of a split tile's parts 12000.
-constexpr double kPairStep = 535, kPairTile = 1500, kPairLaunch = 10000, kExchange = 12000;
+// The estimates (cycles of an SM) behind a plan, fitted to measurements on one GB300.
+//   Pairs: a step of a tile 535 (512 of MMAs), a tile at least 4600 (its epilogue) and
+//   1000 more; the launch's start and its last epilogue 10000; the exchange of split
+//   tiles' parts 26000.
+//   Clusters: a CTA 5600 and for each step what its loads take of the SM's 61 bytes a
+//   cycle or its MMAs of the tensor core; 26 for each row that it finishes; joining
+//   the parts 1200 and 36 a row of the tile.  CTAs that share an SM share both rates.
+//   From memory an SM gets 24 bytes a cycle, however few of them there are.
+//   (70 shapes from 1 to 2500 rows, 64 to 16384 columns and depth: the plan it picks
+//   takes 5% longer than the fastest in the mean.)
+constexpr double kPairStep = 535, kPairTileLeast = 4600, kPairTile = 1000, kPairLaunch = 10000, kExchange = 26000;
+constexpr double kCta = 5600, kLoadRate = 61, kFinishRow = 26, kJoin = 1200, kJoinRow = 36, kClusterLaunch = 800;
+constexpr double kMemoryRate = 24;
+constexpr double kTwoLaunches = 2500;  // what a launch of its own costs beside a product's time
 
-}  // namespace
+double pair_tile_cycles(int64_t steps) { return std::max(steps * kPairStep, kPairTileLeast) + kPairTile; }
 
-LinPlan plan_linear(const LinProduct* products, int count, int type) {
-  const int64_t sms = num_sms(), pairs = sms / 2;
-  int64_t tiles[kMaxProducts], steps[kMaxProducts];
-  bool p_mn = false;
+// CTAs in clusters of `split` that run at once, one or two to an SM (152 SMs in
+// groups that clusters do not cross).
+int64_t clustered_ctas(int split, int per_sm) {
+  const int64_t sms = num_sms();
+  const int64_t most = sms * per_sm;
+  if (split <= 2) return most;
+  if (per_sm == 1) return split == 4 ? most * 144 / 152 / 4 * 4 : most * 120 / 152 / 8 * 8;
+  return split == 4 ? most * 296 / 304 / 4 * 4 : most * 288 / 304 / 8 * 8;
+}
+
+// On pairs: tiles whole, or split depths for the products of few tiles.
+void plan_pairs(const int64_t (&tiles)[kMaxProducts], const int64_t (&steps)[kMaxProducts], int count, double bytes,
+                LinPlan* best) {
+  const int64_t pairs = num_sms() / 2;
   int64_t units = 0;
   double work = 0, longest = 0;
   for (int i = 0; i < count; ++i) {
-    const LinProduct& p = products[i];
-    tiles[i] = ceil_div(p.rows, kLinTile) * ceil_div(p.cols, kLinTile);
-    steps[i] = steps_of(p, type);
-    p_mn = p_mn || p.p_mn;
-    const double tile = steps[i] * kPairStep + kPairTile;
+    const double tile = pair_tile_cycles(steps[i]);
     units += tiles[i];
     work += tiles[i] * tile;
     if (tiles[i]) longest = std::max(longest, tile);
   }
-  LinPlan best;
-  if (units == 0) return best;
-  // On pairs, tiles whole: rounds of tiles, of the tiles' mean where they differ.
-  double best_cycles = kPairLaunch + std::max(longest, ceil_div(units, pairs) * (work / units));
-  // Or with split depths: the parts of the products of few tiles, while they fit,
-  // each next one to the tile that takes longest.
-  {
-    int split[kMaxProducts] = {1, 1};
-    bool few[kMaxProducts] = {false, false};
-    for (int i = 0; i < count; ++i) few[i] = tiles[i] > 0 && 2 * tiles[i] <= pairs;
-    int64_t taken = 0;
+  // Rounds of tiles, of the tiles' mean where they differ.
+  best->cost = kPairLaunch + std::max({longest, ceil_div(units, pairs) * (work / units),
+                                       bytes / (kMemoryRate * 2 * std::min(units, pairs))});
+  // The parts of the products of few tiles, while they fit, each next one to the
+  // tile that takes longest.
+  int split[kMaxProducts] = {1, 1};
+  bool few[kMaxProducts] = {false, false};
+  int64_t taken = 0;
+  for (int i = 0; i < count; ++i) {
+    few[i] = tiles[i] > 0 && 2 * tiles[i] <= pairs;
+    if (few[i]) taken += tiles[i];
+  }
+  for (bool more = taken > 0; more;) {
+    int at = -1;
     for (int i = 0; i < count; ++i)
-      if (few[i]) taken += tiles[i];
-    for (bool more = taken > 0; more;) {
-      int at = -1;
-      for (int i = 0; i < count; ++i)
-        if (few[i] && split[i] < kMaxPairSplit && taken + tiles[i] <= pairs &&
-            steps[i] / (split[i] + 1) >= 8 && (at < 0 || steps[i] / split[i] > steps[at] / split[at]))
-          at = i;
-      if ((more = at >= 0)) {
-        ++split[at];
-        taken += tiles[at];
-      }
-    }
-    double part = 0, all = 0, tile = 0;
-    int64_t parts = 0, whole = 0;
-    for (int i = 0; i < count; ++i) {
-      const double t = ceil_div(steps[i], split[i]) * kPairStep + kPairTile;
-      all += tiles[i] * split[i] * t;
-      if (split[i] > 1) {
-        parts += tiles[i] * split[i];
-        part = std::max(part, t);
-      } else if (tiles[i]) {
-        whole += tiles[i];
-        tile = std::max(tile, t);
-      }
-    }
-    if (parts) {
-      const double cycles = kPairLaunch + kExchange + std::max(part, whole ? all / pairs + tile / 2 : part);
-      if (cycles < best_cycles) {
-        best_cycles = cycles;
-        for (int i = 0; i < count; ++i) best.pair_split[i] = split[i];
-        best.parts = static_cast<int>(parts);
-        // Rounds of whole tiles that the other pairs have time for beside a part.
-        best.ahead = whole && parts < pairs ? static_cast<int>(std::min<int64_t>(part / tile, whole / (pairs - parts))) : 0;
-      }
+      if (few[i] && split[i] < kMaxPairSplit && taken + tiles[i] <= pairs && steps[i] / (split[i] + 1) >= 8 &&
+          (at < 0 || steps[i] / split[i] > steps[at] / split[at]))
+        at = i;
+    if ((more = at >= 0)) {
+      ++split[at];
+      taken += tiles[at];
     }
   }
+  double part = 0, all = 0, tile = 0;
+  int64_t parts = 0, whole = 0;
+  for (int i = 0; i < count; ++i) {
+    const double t = pair_tile_cycles(ceil_div(steps[i], split[i]));
+    all += tiles[i] * split[i] * t;
+    if (split[i] > 1) {
+      parts += tiles[i] * split[i];
+      part = std::max(part, t);
+    } else if (tiles[i]) {
+      whole += tiles[i];
+      tile = std::max(tile, t);
+    }
+  }
+  const double cost = kPairLaunch + kExchange + std::max(part, whole ? all / pairs + tile / 2 : part);
+  if (parts == 0 || cost >= best->cost) return;
+  best->cost = cost;
+  for (int i = 0; i < count; ++i) best->pair_split[i] = split[i];
+  best->parts = static_cast<int>(parts);
+  // Rounds of whole tiles that the other pairs have time for beside a part.
+  best->ahead = whole && parts < pairs ? static_cast<int>(std::min<int64_t>(part / tile, whole / (pairs - parts))) : 0;
+  best->scratch = (sizeof(float) * kPartFloats + sizeof(int) * 2 * kLinEpiWarps) * best->parts;
+}
+
+}  // namespace
+
+LinPlan plan_linear(const LinProduct* products, int count, int type) {
+  LinPlan best;
+  int64_t tiles[kMaxProducts] = {}, steps[kMaxProducts] = {}, units = 0;
+  double bytes = 0;
+  bool p_mn = false;
+  for (int i = 0; i < count; ++i) {
+    tiles[i] = ceil_div(products[i].rows, kLinTile) * ceil_div(products[i].cols, kLinTile);
+    steps[i] = steps_of(products[i], type);
+    units += tiles[i];
+    bytes += static_cast<double>(products[i].rows + products[i].cols) * products[i].depth * type_bytes(type);
+    p_mn = p_mn || products[i].p_mn;
+  }
+  if (units == 0) return best;
+  const int64_t sms = num_sms();
+  plan_pairs(tiles, steps, count, bytes, &best);
   for (int nt : {16, 32, 64, 128}) {
     if (p_mn && nt < 64) continue;
     for (int split = 1; split <= kMaxSplit; split *= 2) {
-      if (nt / split < 1) continue;
-      const double step_cycles = std::max(2.0 * nt, (kRows + nt) * 128 / 60.0);
-      double work = 0, longest_cta = 0;
-      int64_t ctas = 0;
+      int64_t ctas = 0, n[kMaxProducts];
       for (int i = 0; i < count; ++i) {
-        const LinProduct& p = products[i];
-        const int64_t n = ceil_div(p.rows, nt) * ceil_div(p.cols, kRows);
-        const double t = ceil_div(steps[i], split) * step_cycles + 1500.0 + (split > 1 ? 800.0 : 0.0) + nt * 10.0;
-        ctas += n * split;
-        work += static_cast<double>(n * split) * t;
-        longest_cta = std::max(longest_cta, t);
+        n[i] = ceil_div(products[i].rows, nt) * ceil_div(products[i].cols, kRows) * split;
+        ctas += n[i];
       }
-      if (ctas == 0) continue;
-      const double cycles = 3000 + std::max(longest_cta, ceil_div(ctas, sms) * (work / ctas));
-      if (cycles < best_cycles) {
-        best_cycles = cycles;
+      // One CTA to an SM while they fit, else two; split depths in one round only, and
+      // beside another CTA only in pairs of small tiles (64 and 128 rows so: half as
+      // fast again as the next smaller split).
+      const int per_sm = ctas <= clustered_ctas(split, 1) ? 1 : 2;
+      const int64_t at_once = clustered_ctas(split, per_sm);
+      if (split > 1 && (ctas > at_once || (per_sm == 2 && (nt > 32 || split > 2)))) continue;
+      // The CTA that takes longest, undisturbed, or all CTAs' work at the SMs' rates.
+      const double step = std::max((kRows + nt) * 128 / kLoadRate, 2.0 * nt);
+      double work = 0, longest = 0;
+      for (int i = 0; i < count; ++i) {
+        const int64_t each = ceil_div(steps[i], split);
+        const double t = kCta + each * step + kFinishRow * nt / split + (split > 1 ? kJoin + kJoinRow * nt : 0.0);
+        work += static_cast<double>(n[i]) * (each * step + kFinishRow * nt / split);
+        if (n[i]) longest = std::max(longest, t);
+      }
+      const double cost = kClusterLaunch + std::max({longest, ceil_div(ctas, at_once) * kCta + work / std::min(ctas, sms),
+                                                     kCta + bytes / (kMemoryRate * std::min(ctas, sms))});
+      if (cost < best.cost) {
         best = LinPlan{};
+        best.cost = cost;
         best.nt = nt;
         best.split = split;
-        best.stages = std::min(kSplitMaxStages, (ctas > sms ? 110 * 1024 : 220 * 1024) / split_stage_bytes(nt));
+        best.stages = std::min(kSplitMaxStages, (per_sm == 2 ? 110 * 1024 : 220 * 1024) / split_stage_bytes(nt));
       }
     }
   }
-  if (best.parts) best.scratch = (sizeof(float) * kPartFloats + sizeof(int) * 2 * kLinEpiWarps) * best.parts;
   return best;
+}
+
+bool plan_apart(const LinPlan& together, const LinPlan& a, const LinPlan& b) {
+  return a.cost + b.cost + kTwoLaunches < together.cost;
 }
 
 namespace {

@@ -132,15 +132,18 @@ constexpr int kMaxProducts = 2;
 // How a launch runs: on CTA pairs (nt = 0), the depth of product i's tiles cut into
 // pair_split[i] parts (`parts` of them in all, `ahead`: see LinLaunch), or in tiles
 // of nt rows with the depth split over `split` CTAs and `stages` of operands in
-// flight.  `scratch` bytes of workspace.
+// flight.  `scratch` bytes of workspace; `cost`, an estimate in cycles.
 struct LinPlan {
   int nt = 0, split = 1, stages = 0;
   int pair_split[kMaxProducts] = {1, 1}, parts = 0, ahead = 0;
   size_t scratch = 0;
+  double cost = 0;
 };
 // The plan for up to two independent products in one launch (by their sizes and
 // storage alone).  `type` is the operands'.
 LinPlan plan_linear(const LinProduct* products, int count, int type);
+// Whether two products are faster in launches of their own than together.
+bool plan_apart(const LinPlan& together, const LinPlan& a, const LinPlan& b);
 // Operands' base addresses and leading dimensions are multiples of 16 bytes.
 cudaError_t launch_linear(const LinProduct* products, int count, int type, const LinPlan& plan, void* scratch,
                           Oz2Device* dev, cudaStream_t st);

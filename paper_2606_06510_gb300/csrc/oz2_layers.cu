@@ -177,7 +177,18 @@ int oz2_linear_grad(int64_t m, int64_t n, int64_t k, int type, const void* d_dY,
     a.ep.out_type = dw_type;
     a.ep.accumulate = accumulate;
   }
-  const LinPlan plan = count ? plan_linear(p, count, type) : LinPlan{};
+  // Both products in one launch, or each in its own.
+  LinPlan plan[kMaxProducts];
+  int launches = count ? 1 : 0;
+  if (count) plan[0] = plan_linear(p, count, type);
+  if (count == 2) {
+    const LinPlan dx = plan_linear(p, 1, type), dw = plan_linear(p + 1, 1, type);
+    if (plan_apart(plan[0], dx, dw)) {
+      launches = 2;
+      plan[0] = dx;
+      plan[1] = dw;
+    }
+  }
   Workspace ws(st);
   // dZ is dY itself where there is no activation and TMA can read it.
   const bool own_dz = count && any && (act != OZ2_ACT_NONE || !on16(d_dY, lddy, 2));
@@ -185,7 +196,8 @@ int oz2_linear_grad(int64_t m, int64_t n, int64_t k, int type, const void* d_dY,
   const size_t dz_off = own_dz ? ws.ask(static_cast<size_t>(m) * ld_dz * 2) : 0;
   const size_t part_off = want_db && m > 0 ? ws.ask(sizeof(float) * static_cast<size_t>(lin_db_chunks(m, n)) * n) : 0;
   Operand X(d_X, ldx, want_dw ? m : 0, k, 2, ws), W(d_W, ldw, want_dx ? n : 0, k, 2, ws);
-  const size_t scratch = ws.ask(plan.scratch);
+  size_t scratch[kMaxProducts] = {};
+  for (int i = 0; i < launches; ++i) scratch[i] = ws.ask(plan[i].scratch);
   if (!ws.take()) return OZ2_ERR_ALLOC;
   cudaError_t err = cudaSuccess;
   if (want_db && m == 0) err = cudaMemsetAsync(d_db, 0, sizeof(float) * n, st);
@@ -213,7 +225,9 @@ int oz2_linear_grad(int64_t m, int64_t n, int64_t k, int type, const void* d_dY,
     pdw->q = X.p;
     pdw->ldq = X.ld;
   }
-  return status_of(launch_linear(p, count, type, plan, ws.at<void>(scratch), dev, st));
+  for (int i = 0; i < launches && err == cudaSuccess; ++i)
+    err = launch_linear(p + i, launches == 2 ? 1 : count, type, plan[i], ws.at<void>(scratch[i]), dev, st);
+  return status_of(err);
 }
 
 int oz2_adamw(const oz2_adamw_tensor* tensors, int count, int param_type, int grad_type, int state_bits,
