@@ -673,14 +673,9 @@ __device__ __forceinline__ void activate8(float (&z)[8]) {
 }
 
 // Eight 16-bit values of a row of D, from its column col on (n of them there).
-__device__ __forceinline__ uint4 load8(const void* src, int64_t ld, int64_t row, int64_t col, int n) {
-  const uint16_t* s = static_cast<const uint16_t*>(src) + row * ld + col;
-  if (n == 8 && vec_ok(src, ld, 2)) return __ldg(reinterpret_cast<const uint4*>(s));
-  uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-  for (int e = 0; e < 8; ++e)
-    if (e < n) w[e >> 1] |= static_cast<uint32_t>(__ldg(s + e)) << (16 * (e & 1));
-  return make_uint4(w[0], w[1], w[2], w[3]);
+__device__ __forceinline__ uint4 load8(const LinUnits& x, const void* src, int64_t ld, int64_t row, int64_t col, int n) {
+  const uint16_t* s = static_cast<const uint16_t*>(src);
+  return load16_any(s + row * ld + col, s, s + (x.rows - 1) * ld + x.cols, n);
 }
 __device__ __forceinline__ void store8(void* dst, int64_t ld, int64_t row, int64_t col, int n, const float (&z)[8],
                                        bool bf16) {
@@ -689,6 +684,14 @@ __device__ __forceinline__ void store8(void* dst, int64_t ld, int64_t row, int64
                          pack16(z[6], z[7], bf16)};
   if (n == 8 && vec_ok(dst, ld, 2)) {
     *reinterpret_cast<uint4*>(d) = make_uint4(w[0], w[1], w[2], w[3]);
+  } else if (n == 8 && (reinterpret_cast<uintptr_t>(d) & 2) == 0) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) reinterpret_cast<uint32_t*>(d)[e] = w[e];
+  } else if (n == 8) {
+    d[0] = static_cast<uint16_t>(w[0]);
+#pragma unroll
+    for (int e = 0; e < 3; ++e) reinterpret_cast<uint32_t*>(d + 1)[e] = __funnelshift_r(w[e], w[e + 1], 16);
+    d[7] = static_cast<uint16_t>(w[3] >> 16);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
@@ -700,7 +703,7 @@ __device__ __forceinline__ void store8(void* dst, int64_t ld, int64_t row, int64
 struct ColumnTerms {
   float bias[8], scale[8];
 };
-__device__ __forceinline__ void load_terms(const LinEpilogue& ep, int64_t col, int n, ColumnTerms& t) {
+__device__ __forceinline__ void load_terms(const LinEpilogue& ep, int64_t cols, int64_t col, int n, ColumnTerms& t) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) t.bias[e] = 0.f, t.scale[e] = 1.f;
   if (ep.bias && ep.bias_type == OZ2_TYPE_F32) {
@@ -708,7 +711,8 @@ __device__ __forceinline__ void load_terms(const LinEpilogue& ep, int64_t col, i
     for (int e = 0; e < 8; ++e)
       if (e < n) t.bias[e] = __ldg(static_cast<const float*>(ep.bias) + col + e);
   } else if (ep.bias) {
-    const uint4 v = load8(ep.bias, 0, 0, col, n);
+    const uint16_t* b = static_cast<const uint16_t*>(ep.bias);
+    const uint4 v = load16_any(b + col, b, b + cols, n);
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -763,8 +767,7 @@ __device__ __forceinline__ void finish8(const LinEpilogue& ep, int64_t row, int6
 // loads are under way before the first is added.
 template <int SPLIT>
 __device__ __forceinline__ void finish_rows(const LinUnits& x, int64_t row0, int64_t col, int n, int r, int end,
-                                            uint32_t at, const ColumnTerms& t, uint4 first) {
-  bool have = true;
+                                            uint32_t at, const ColumnTerms& t, uint4 add) {
 #pragma unroll 1
   for (; r < end && row0 + r < x.rows; r += 16) {
     float4 a[SPLIT], b[SPLIT];
@@ -774,15 +777,15 @@ __device__ __forceinline__ void finish_rows(const LinUnits& x, int64_t row0, int
       a[p] = ld_cluster_f4(from);
       b[p] = ld_cluster_f4(from + 16);
     }
-    const uint4 add = have ? first : x.ep.add ? load8(x.ep.add, x.ep.ld_add, row0 + r, col, n) : first;
-    have = false;
+    const uint4 now = add;  // R's values of the next row are on their way while this one is finished
+    if (x.ep.add && r + 16 < end && row0 + r + 16 < x.rows) add = load8(x, x.ep.add, x.ep.ld_add, row0 + r + 16, col, n);
     float z[8] = {a[0].x, a[0].y, a[0].z, a[0].w, b[0].x, b[0].y, b[0].z, b[0].w};
 #pragma unroll
     for (int p = 1; p < SPLIT; ++p) {
       z[0] += a[p].x, z[1] += a[p].y, z[2] += a[p].z, z[3] += a[p].w;
       z[4] += b[p].x, z[5] += b[p].y, z[6] += b[p].z, z[7] += b[p].w;
     }
-    finish8(x.ep, row0 + r, col, n, t, add, z);
+    finish8(x.ep, row0 + r, col, n, t, now, z);
   }
 }
 
@@ -920,8 +923,8 @@ __global__ void __launch_bounds__(kSplitThreads)
   ColumnTerms terms;
   uint4 first = make_uint4(0, 0, 0, 0);
   if (r_first < r_end && row0 + r_first < x.rows) {
-    load_terms(x.ep, col, n, terms);
-    if (x.ep.add) first = load8(x.ep.add, x.ep.ld_add, row0 + r_first, col, n);
+    load_terms(x.ep, x.cols, col, n, terms);
+    if (x.ep.add) first = load8(x, x.ep.add, x.ep.ld_add, row0 + r_first, col, n);
   }
   // The sums, NT columns of 128 lanes, to shared memory: the operands there have
   // been multiplied.
@@ -1014,8 +1017,7 @@ double pair_tile_cycles(int64_t steps) { return std::max(steps * kPairStep, kPai
 
 // CTAs in clusters of `split` that run at once, one or two to an SM (152 SMs in
 // groups that clusters do not cross).
-int64_t clustered_ctas(int split, int per_sm) {
-  const int64_t sms = num_sms();
+int64_t clustered_ctas(int64_t sms, int split, int per_sm) {
   const int64_t most = sms * per_sm;
   if (split <= 2) return most;
   if (per_sm == 1) return split == 4 ? most * 144 / 152 / 4 * 4 : most * 120 / 152 / 8 * 8;
@@ -1024,8 +1026,7 @@ int64_t clustered_ctas(int split, int per_sm) {
 
 // On pairs: tiles whole, or split depths for the products of few tiles.
 void plan_pairs(const int64_t (&tiles)[kMaxProducts], const int64_t (&steps)[kMaxProducts], int count, double bytes,
-                LinPlan* best) {
-  const int64_t pairs = num_sms() / 2;
+                int64_t pairs, LinPlan* best) {
   int64_t units = 0;
   double work = 0, longest = 0;
   for (int i = 0; i < count; ++i) {
@@ -1096,7 +1097,7 @@ LinPlan plan_linear(const LinProduct* products, int count, int type) {
   }
   if (units == 0) return best;
   const int64_t sms = num_sms();
-  plan_pairs(tiles, steps, count, bytes, &best);
+  plan_pairs(tiles, steps, count, bytes, sms / 2, &best);
   for (int nt : {16, 32, 64, 128}) {
     if (p_mn && nt < 64) continue;
     for (int split = 1; split <= kMaxSplit; split *= 2) {
@@ -1108,8 +1109,8 @@ LinPlan plan_linear(const LinProduct* products, int count, int type) {
       // One CTA to an SM while they fit, else two; split depths in one round only, and
       // beside another CTA only in pairs of small tiles (64 and 128 rows so: half as
       // fast again as the next smaller split).
-      const int per_sm = ctas <= clustered_ctas(split, 1) ? 1 : 2;
-      const int64_t at_once = clustered_ctas(split, per_sm);
+      const int per_sm = ctas <= clustered_ctas(sms, split, 1) ? 1 : 2;
+      const int64_t at_once = clustered_ctas(sms, split, per_sm);
       if (split > 1 && (ctas > at_once || (per_sm == 2 && (nt > 32 || split > 2)))) continue;
       // The CTA that takes longest, undisturbed, or all CTAs' work at the SMs' rates.
       const double step = std::max((kRows + nt) * 128 / kLoadRate, 2.0 * nt);

@@ -9,9 +9,9 @@ namespace oz2 {
 namespace {
 
 // ---------------------------------------------------------------------------
-// Pack: a thread writes 16 bytes of a destination row from its elements, one by one
-// (consecutive threads' are consecutive).  Up to two operands in one launch: the
-// blocks of the second grid row take the second.
+// Pack: a thread writes 16 bytes of a destination row (consecutive threads' are
+// consecutive).  Up to two operands in one launch: the blocks of the second grid row
+// take the second.
 // ---------------------------------------------------------------------------
 template <typename T>
 __global__ void __launch_bounds__(256) pack_rows_kernel(PackJob a, PackJob b) {
@@ -22,29 +22,23 @@ __global__ void __launch_bounds__(256) pack_rows_kernel(PackJob a, PackJob b) {
   const T* src = static_cast<const T*>(x.src);
   T* dst = static_cast<T*>(x.dst);
   const int64_t per = (x.cols + kVec - 1) / kVec;
+  const T* end = src + (x.rows - 1) * x.ld_src + x.cols;
   for (int64_t i = blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x; i < x.rows * per;
        i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
     const int64_t r = i / per, c = (i - r * per) * kVec;
-    const T* s = src + r * x.ld_src + c;
-    union {
-      uint4 v;
-      T e[kVec];
-    } w;
-    w.v = make_uint4(0, 0, 0, 0);
-#pragma unroll
-    for (int j = 0; j < kVec; ++j)
-      if (c + j < x.cols) w.e[j] = __ldg(s + j);
-    *reinterpret_cast<uint4*>(dst + r * x.ld_dst + c) = w.v;
+    *reinterpret_cast<uint4*>(dst + r * x.ld_dst + c) =
+        load16_any(src + r * x.ld_src + c, src, end, static_cast<int>(min(static_cast<int64_t>(kVec), x.cols - c)));
   }
 }
 
 // ---------------------------------------------------------------------------
 // dz and db.  A block takes 256 columns (a lane 8 of them) and a chunk of rows,
 // which its 8 warps walk in turn; the warps' sums are joined in shared memory in
-// a fixed order and the block's written to `partial` (chunk, column).  A second
-// kernel adds the chunks in order: the sums never depend on who came first.
+// a fixed order.  Up to 8 chunks (2048 rows) are a cluster, whose first block adds up
+// the others' sums; more of them write theirs to `partial` (chunk, column) and a second
+// kernel adds those.  Either way in order: the sums never depend on who came first.
 // ---------------------------------------------------------------------------
-constexpr int kGradCols = 256, kGradWarps = 8;
+constexpr int kGradCols = 256, kGradWarps = 8, kGradBlocks = 3;  // blocks an SM
 
 // Eight columns of a row: g ← dy·act'(z), the sums, and dz.
 template <int ACT>
@@ -58,8 +52,9 @@ __device__ __forceinline__ void grad8(const uint32_t (&aw)[4], const uint32_t (&
     g[2 * e + 1] = f.y;
     if (ACT != OZ2_ACT_NONE) {
       const float2 t = unpack16(bw[e], bf16);
-      g[2 * e] *= act_slope<ACT>(t.x);
-      g[2 * e + 1] *= act_slope<ACT>(t.y);
+      // (Not fused into the sums: db does not depend on whether dz is wanted.)
+      g[2 * e] = __fmul_rn(g[2 * e], act_slope<ACT>(t.x));
+      g[2 * e + 1] = __fmul_rn(g[2 * e + 1], act_slope<ACT>(t.y));
     }
     s[2 * e] += g[2 * e];
     s[2 * e + 1] += g[2 * e + 1];
@@ -69,72 +64,79 @@ __device__ __forceinline__ void grad8(const uint32_t (&aw)[4], const uint32_t (&
                                                pack16(g[4], g[5], bf16), pack16(g[6], g[7], bf16));
 }
 
-constexpr int kGradAhead = 4;        // rows that a warp loads before it works on them
+// Rows that a warp loads before it works on them (shifted loads take twice the
+// registers).
+template <bool ALIGNED>
+constexpr int kGradAhead = ALIGNED ? 4 : 2;
 
-template <int ACT, bool BF16>
-__global__ void __launch_bounds__(32 * kGradWarps)
-    act_grad_kernel(int64_t m, int64_t n, int64_t chunk_rows, bool vec, const uint16_t* __restrict__ dy,
-                    int64_t ld_dy, const uint16_t* __restrict__ z, int64_t ld_z, uint16_t* __restrict__ dz,
-                    int64_t ld_dz, float* __restrict__ partial) {
+// ALIGNED: rows start on 16-byte boundaries.
+template <int ACT, bool BF16, bool ALIGNED>
+__global__ void __launch_bounds__(32 * kGradWarps, kGradBlocks)
+    act_grad_kernel(int64_t m, int64_t n, int64_t chunk_rows, const uint16_t* __restrict__ dy, int64_t ld_dy,
+                    const uint16_t* __restrict__ z, int64_t ld_z, uint16_t* __restrict__ dz, int64_t ld_dz,
+                    float* __restrict__ partial, float* __restrict__ db, bool accumulate) {
   __shared__ float sums[kGradWarps][kGradCols];
   pdl_trigger();
   pdl_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t col = static_cast<int64_t>(blockIdx.x) * kGradCols + 8 * lane;
   const int64_t r0 = static_cast<int64_t>(blockIdx.y) * chunk_rows, r1 = min(m, r0 + chunk_rows);
+  const int left = static_cast<int>(min(static_cast<int64_t>(8), n - col));
   float s[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) s[e] = 0.f;
-  if (vec && col + 8 <= n) {
+  auto load = [&](const uint16_t* src, int64_t ld, int64_t r) {
+    const uint16_t* p = src + r * ld + col;
+    if (ALIGNED) return left == 8 ? __ldg(reinterpret_cast<const uint4*>(p)) : load16_singly(p, left);
+    return load16_any(p, src, src + (m - 1) * ld + n, left);
+  };
+  auto work = [&](uint4 a, uint4 b, int64_t r) {
+    const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+    grad8<ACT>(aw, bw, BF16, s, dz ? dz + r * ld_dz + col : nullptr);
+  };
+  if (left > 0) {
+    constexpr int kAhead = kGradAhead<ALIGNED>;
     int64_t r = r0 + warp;
-    for (; r + (kGradAhead - 1) * kGradWarps < r1; r += kGradAhead * kGradWarps) {
-      uint4 a[kGradAhead], b[kGradAhead];
+    for (; r + (kAhead - 1) * kGradWarps < r1; r += kAhead * kGradWarps) {
+      uint4 a[kAhead], b[kAhead];
 #pragma unroll
-      for (int i = 0; i < kGradAhead; ++i) {
-        a[i] = __ldg(reinterpret_cast<const uint4*>(dy + (r + i * kGradWarps) * ld_dy + col));
+      for (int i = 0; i < kAhead; ++i) {
+        a[i] = load(dy, ld_dy, r + i * kGradWarps);
         b[i] = make_uint4(0, 0, 0, 0);
-        if (ACT != OZ2_ACT_NONE) b[i] = __ldg(reinterpret_cast<const uint4*>(z + (r + i * kGradWarps) * ld_z + col));
+        if (ACT != OZ2_ACT_NONE) b[i] = load(z, ld_z, r + i * kGradWarps);
       }
 #pragma unroll
-      for (int i = 0; i < kGradAhead; ++i) {
-        const uint32_t aw[4] = {a[i].x, a[i].y, a[i].z, a[i].w}, bw[4] = {b[i].x, b[i].y, b[i].z, b[i].w};
-        grad8<ACT>(aw, bw, BF16, s, dz ? dz + (r + i * kGradWarps) * ld_dz + col : nullptr);
-      }
+      for (int i = 0; i < kAhead; ++i) work(a[i], b[i], r + i * kGradWarps);
     }
-    for (; r < r1; r += kGradWarps) {
-      const uint4 a = __ldg(reinterpret_cast<const uint4*>(dy + r * ld_dy + col));
-      uint4 b = make_uint4(0, 0, 0, 0);
-      if (ACT != OZ2_ACT_NONE) b = __ldg(reinterpret_cast<const uint4*>(z + r * ld_z + col));
-      const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
-      grad8<ACT>(aw, bw, BF16, s, dz ? dz + r * ld_dz + col : nullptr);
-    }
-  } else if (col < n) {
-#pragma unroll 2
-    for (int64_t r = r0 + warp; r < r1; r += kGradWarps) {
-      const uint16_t* a = dy + r * ld_dy + col;
-      const uint16_t* b = ACT == OZ2_ACT_NONE ? nullptr : z + r * ld_z + col;
-      uint32_t aw[4] = {0, 0, 0, 0}, bw[4] = {0, 0, 0, 0};
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (col + e < n) {
-          aw[e >> 1] |= static_cast<uint32_t>(__ldg(a + e)) << (16 * (e & 1));
-          if (ACT != OZ2_ACT_NONE) bw[e >> 1] |= static_cast<uint32_t>(__ldg(b + e)) << (16 * (e & 1));
-        }
-      grad8<ACT>(aw, bw, BF16, s, dz ? dz + r * ld_dz + col : nullptr);
-    }
+    for (; r < r1; r += kGradWarps)
+      work(load(dy, ld_dy, r), ACT == OZ2_ACT_NONE ? make_uint4(0, 0, 0, 0) : load(z, ld_z, r), r);
   }
+  if (!db) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sums[warp][8 * lane + e] = s[e];
+  __syncthreads();
+  const int64_t j = static_cast<int64_t>(blockIdx.x) * kGradCols + threadIdx.x;
+  float t = 0.f;
+#pragma unroll
+  for (int w = 0; w < kGradWarps; ++w) t += sums[w][threadIdx.x];
   if (partial) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sums[warp][8 * lane + e] = s[e];
-    __syncthreads();
-    const int64_t j = static_cast<int64_t>(blockIdx.x) * kGradCols + threadIdx.x;
-    if (j < n) {
-      float t = 0.f;
-#pragma unroll
-      for (int w = 0; w < kGradWarps; ++w) t += sums[w][threadIdx.x];
-      partial[blockIdx.y * n + j] = t;
-    }
+    if (j < n) partial[blockIdx.y * n + j] = t;
+    return;
   }
+  __syncthreads();
+  sums[0][threadIdx.x] = t;
+  cluster_sync_all();
+  if (blockIdx.y == 0 && j < n) {
+    const uint32_t at = smem_u32(&sums[0][threadIdx.x]);
+    t = 0.f;
+    for (uint32_t c = 0; c < gridDim.y; ++c) {
+      float v;
+      asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(mapa_shared(at, c)));
+      t += v;
+    }
+    db[j] = accumulate ? db[j] + t : t;
+  }
+  cluster_sync_all();  // no block leaves while the first reads its sums
 }
 
 // db from the chunks' sums: a warp's lanes are 32 columns, its 8 warps each add every
@@ -161,28 +163,36 @@ __global__ void __launch_bounds__(256) sum_chunks_kernel(int64_t n, int64_t chun
   }
 }
 
+constexpr int kGradCluster = 8;      // blocks of a cluster, of up to 256 rows each
+
 int64_t chunk_rows_for(int64_t m, int64_t n) {
-  // About four blocks an SM, of at least 32 rows.
+  if (m <= kGradCluster * 256) return std::max<int64_t>(32, (m + kGradCluster - 1) / kGradCluster);
+  // As many blocks as run at once, of whole rounds of the warps' rows.
   const int64_t across = (n + kGradCols - 1) / kGradCols;
-  const int64_t chunks = std::max<int64_t>(1, 4 * static_cast<int64_t>(num_sms()) / across);
-  int64_t rows = std::max<int64_t>(32, (m + chunks - 1) / chunks);
-  return std::max(rows, (m + 65534) / 65535);  // the grid's second axis
+  const int64_t chunks = std::max<int64_t>(1, kGradBlocks * static_cast<int64_t>(num_sms()) / across);
+  const int64_t rows = std::max((m + chunks - 1) / chunks, (m + 65534) / 65535);  // (the grid's second axis)
+  return (rows + 15) / 16 * 16;
 }
 
-template <bool BF16>
+template <bool BF16, bool ALIGNED>
 auto grad_kernel(int act) {
-  return act == OZ2_ACT_RELU        ? act_grad_kernel<OZ2_ACT_RELU, BF16>
-         : act == OZ2_ACT_GELU      ? act_grad_kernel<OZ2_ACT_GELU, BF16>
-         : act == OZ2_ACT_GELU_TANH ? act_grad_kernel<OZ2_ACT_GELU_TANH, BF16>
-         : act == OZ2_ACT_SILU      ? act_grad_kernel<OZ2_ACT_SILU, BF16>
-                                    : act_grad_kernel<OZ2_ACT_NONE, BF16>;
+  return act == OZ2_ACT_RELU        ? act_grad_kernel<OZ2_ACT_RELU, BF16, ALIGNED>
+         : act == OZ2_ACT_GELU      ? act_grad_kernel<OZ2_ACT_GELU, BF16, ALIGNED>
+         : act == OZ2_ACT_GELU_TANH ? act_grad_kernel<OZ2_ACT_GELU_TANH, BF16, ALIGNED>
+         : act == OZ2_ACT_SILU      ? act_grad_kernel<OZ2_ACT_SILU, BF16, ALIGNED>
+                                    : act_grad_kernel<OZ2_ACT_NONE, BF16, ALIGNED>;
 }
 
 }  // namespace
 
-int64_t lin_db_chunks(int64_t m, int64_t n) {
+static int64_t chunks_of(int64_t m, int64_t n) {
   const int64_t r = chunk_rows_for(m, n);
   return std::max<int64_t>(1, (m + r - 1) / r);
+}
+
+int64_t lin_db_chunks(int64_t m, int64_t n) {
+  const int64_t chunks = chunks_of(m, n);
+  return chunks <= kGradCluster ? 0 : chunks;
 }
 
 cudaError_t launch_pack_rows(const PackJob* jobs, int count, int bytes, cudaStream_t st) {
@@ -199,19 +209,33 @@ cudaError_t launch_act_grad(int64_t m, int64_t n, int type, int act, const void*
                             int64_t ld_z, void* dz, int64_t ld_dz, float* db, float* partial, bool accumulate,
                             cudaStream_t st) {
   if (n == 0) return cudaSuccess;
-  const int64_t rows = chunk_rows_for(m, n), chunks = lin_db_chunks(m, n);
+  const int64_t rows = chunk_rows_for(m, n), chunks = chunks_of(m, n);
   auto aligned = [](const void* p, int64_t ld) { return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(2 * ld)) & 15) == 0; };
   const bool vec = aligned(dy, ld_dy) && (act == OZ2_ACT_NONE || aligned(z, ld_z));
-  auto kern = type == OZ2_TYPE_BF16 ? grad_kernel<true>(act) : grad_kernel<false>(act);
+  auto kern = type == OZ2_TYPE_BF16 ? (vec ? grad_kernel<true, true>(act) : grad_kernel<true, false>(act))
+                                    : (vec ? grad_kernel<false, true>(act) : grad_kernel<false, false>(act));
+  const bool joined = chunks <= kGradCluster;
   count_launch();
-  cudaError_t err = launch_dependent(
-      kern, dim3(static_cast<unsigned>((n + kGradCols - 1) / kGradCols), static_cast<unsigned>(chunks)),
-      dim3(32 * kGradWarps), 0, st, m, n, rows, vec, static_cast<const uint16_t*>(dy), ld_dy,
-      static_cast<const uint16_t*>(z), ld_z, static_cast<uint16_t*>(dz), ld_dz, db ? partial : nullptr);
-  if (err != cudaSuccess || !db) return err;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>((n + kGradCols - 1) / kGradCols), static_cast<unsigned>(chunks));
+  cfg.blockDim = dim3(32 * kGradWarps);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 1;
+  attr[1].val.clusterDim.y = static_cast<unsigned>(joined ? chunks : 1);
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  cudaError_t err = cudaLaunchKernelEx(&cfg, kern, m, n, rows, static_cast<const uint16_t*>(dy), ld_dy,
+                                       static_cast<const uint16_t*>(z), ld_z, static_cast<uint16_t*>(dz), ld_dz,
+                                       joined ? static_cast<float*>(nullptr) : partial, db, accumulate);
+  if (err != cudaSuccess || !db || joined) return err;
   count_launch();
   return launch_dependent(sum_chunks_kernel, dim3(static_cast<unsigned>((n + 31) / 32)), dim3(256), 0, st, n, chunks,
-                          partial, db, accumulate);
+                          static_cast<const float*>(partial), db, accumulate);
 }
 
 }  // namespace oz2

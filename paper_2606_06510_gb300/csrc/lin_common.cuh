@@ -30,6 +30,37 @@ __device__ __forceinline__ float2 unpack16(uint32_t w, bool bf16) {
 }
 __device__ __forceinline__ float load16(const uint16_t* p, bool bf16) { return unpack16(*p, bf16).x; }
 
+// 16 bytes from an address that need not be a multiple of 16: the two 16-byte words
+// that hold them, shifted together.  `base` and `end` bound what may be read; where a
+// word reaches past them, the first n elements (of T) one by one.  Past those n the
+// result is of no meaning.
+template <typename T>
+__device__ __noinline__ uint4 load16_singly(const T* p, int n) {
+  union {
+    uint4 v;
+    T e[16 / sizeof(T)];
+  } u;
+  u.v = make_uint4(0, 0, 0, 0);
+#pragma unroll
+  for (int e = 0; e < static_cast<int>(16 / sizeof(T)); ++e)
+    if (e < n) u.e[e] = __ldg(p + e);
+  return u.v;
+}
+template <typename T>
+__device__ __forceinline__ uint4 load16_any(const T* p, const T* base, const T* end, int n) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p), word = at & ~static_cast<uintptr_t>(15);
+  const unsigned s = static_cast<unsigned>(at & 15);
+  if (word < reinterpret_cast<uintptr_t>(base) || word + (s ? 32 : 16) > reinterpret_cast<uintptr_t>(end))
+    return load16_singly(p, n);
+  const uint4 a = __ldg(reinterpret_cast<const uint4*>(word)), b = s ? __ldg(reinterpret_cast<const uint4*>(word + 16)) : a;
+  uint32_t w[6] = {a.x, a.y, a.z, a.w, b.x, b.y};
+  if (s & 8) w[0] = w[2], w[1] = w[3], w[2] = w[4], w[3] = w[5], w[4] = b.z, w[5] = b.w;
+  if (s & 4) w[0] = w[1], w[1] = w[2], w[2] = w[3], w[3] = w[4], w[4] = w[5];
+  const unsigned bits = 8 * (s & 3);
+  return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits),
+                    __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
+}
+
 // --- activations ---------------------------------------------------------------
 // exp and division are the fast ones (off by some 2^-21 of the value): results are
 // rounded to 16 bits, and in db's FP32 sums such errors average out.  Results below
@@ -160,7 +191,8 @@ cudaError_t launch_pack_rows(const PackJob* jobs, int count, int bytes, cudaStre
 
 // dz = dy·act'(z) in the operands' type into rows of ld_dz elements (16-byte
 // rows; null: not wanted), and db = its column sums before that rounding
-// (null: not wanted; `partial` holds lin_db_chunks(m, n)·n floats for them).
+// (null: not wanted; `partial` holds lin_db_chunks(m, n)·n floats for them, of which
+// there may be none).
 int64_t lin_db_chunks(int64_t m, int64_t n);
 cudaError_t launch_act_grad(int64_t m, int64_t n, int type, int act, const void* dy, int64_t ld_dy, const void* z,
                             int64_t ld_z, void* dz, int64_t ld_dz, float* db, float* partial, bool accumulate,
