@@ -162,6 +162,32 @@ __device__ __forceinline__ int scale_exponent(uint32_t top) {
   return max(1, static_cast<int>(top >> 23) - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0));
 }
 
+// Two FP32 values in one 64-bit register pair, and the packed instructions on them:
+// each is rounded as the single ones are, at half the issue slots.
+struct Two {
+  uint64_t v;
+  __device__ __forceinline__ Two() {}
+  __device__ __forceinline__ Two(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+  __device__ __forceinline__ explicit Two(float a) : Two(a, a) {}
+  __device__ __forceinline__ float x() const { return __uint_as_float(static_cast<uint32_t>(v)); }
+  __device__ __forceinline__ float y() const { return __uint_as_float(static_cast<uint32_t>(v >> 32)); }
+};
+__device__ __forceinline__ Two mul2(Two a, Two b) {
+  Two r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Two add2(Two a, Two b) {
+  Two r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+  Two r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+
 // y (|y| ≤ 448) cut to one of its two E4M3 neighbours, the one away from zero
 // with the probability of what is cut off: `u` (16 bits, shifted left by 4) is
 // added below the three bits that E4M3 keeps, and the rest dropped.  Below 2^-6
@@ -169,11 +195,16 @@ __device__ __forceinline__ int scale_exponent(uint32_t top) {
 // three bits where a normal one's are, and taken off again (both exact but for
 // what lies under 2^-29).
 template <bool SIGNED>
-__device__ __forceinline__ float cut_stochastic(float y, uint32_t u) {
-  const float c = fabsf(y) < 0.015625f ? SIGNED ? copysignf(0.015625f, y) : 0.015625f : 0.f;
-  const float t = __fadd_rn(y, c);
-  const float r = __uint_as_float((__float_as_uint(t) + u) & 0xFFF00000u) - c;
-  return SIGNED ? copysignf(r, y) : r;
+__device__ __forceinline__ void cut_stochastic(Two y, uint32_t u0, uint32_t u1, float* out) {
+  const float a = y.x(), b = y.y();
+  const float ca = fabsf(a) < 0.015625f ? SIGNED ? copysignf(0.015625f, a) : 0.015625f : 0.f;
+  const float cb = fabsf(b) < 0.015625f ? SIGNED ? copysignf(0.015625f, b) : 0.015625f : 0.f;
+  const Two t = add2(y, Two(ca, cb));
+  const Two r = add2(Two(__uint_as_float((__float_as_uint(t.x()) + u0) & 0xFFF00000u),
+                         __uint_as_float((__float_as_uint(t.y()) + u1) & 0xFFF00000u)),
+                     Two(-ca, -cb));
+  out[0] = SIGNED ? copysignf(r.x(), a) : r.x();
+  out[1] = SIGNED ? copysignf(r.y(), b) : r.y();
 }
 
 // A warp's 256 values as they were loaded.
@@ -212,7 +243,7 @@ __device__ __forceinline__ void load_raw(const AdamEntry& x, int64_t in, bool wh
 
 // W: the parameters' type; G: the gradients'; MASTER: FP32 weights beside them.
 template <int BITS, int W, int G, bool MASTER, int CAP>
-__global__ void __launch_bounds__(32 * kAdamWarps, BITS == 8 ? 5 : 1) adamw_kernel(const __grid_constant__ AdamTable<CAP> T) {
+__global__ void __launch_bounds__(32 * kAdamWarps, BITS == 8 ? 6 : 1) adamw_kernel(const __grid_constant__ AdamTable<CAP> T) {
   pdl_trigger();
   pdl_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -259,28 +290,44 @@ __global__ void __launch_bounds__(32 * kAdamWarps, BITS == 8 ? 5 : 1) adamw_kern
         decode4(r.v[h][0], v[h]);
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float gg = g[e] * gscale;
-        float mm = m[h][e], vv = v[h][e];
+      for (int e = 0; e < 4; e += 2) {
+        const Two gg = mul2(Two(g[e], g[e + 1]), Two(gscale));
+        Two mm(m[h][e], m[h][e + 1]), vv(v[h][e], v[h][e + 1]);
         if (BITS == 8) {
-          mm *= r.m_scale;
-          vv *= r.v_scale;
-          vv *= vv;
+          mm = mul2(mm, Two(r.m_scale));
+          vv = mul2(vv, Two(r.v_scale));
+          vv = mul2(vv, vv);
         }
         // Rounded one by one, so that the 8-bit states can be checked bit for bit.
-        mm = __fadd_rn(__fmul_rn(mm, T.b1), __fmul_rn(gg, T.c1));
-        vv = __fadd_rn(__fmul_rn(vv, T.b2), __fmul_rn(__fmul_rn(gg, gg), T.c2));
-        const float root = __fsqrt_rn(vv);
-        const float p = w[h][e];
-        const float u = mm * reciprocal(fmaf(root, T.root, T.eps));
-        w[h][e] = fmaf(-step, u, fmaf(-decay, p, p));
-        m[h][e] = mm;
-        v[h][e] = BITS == 32 ? vv : root;
+        const Two mb = mul2(mm, Two(T.b1)), mc = mul2(gg, Two(T.c1));
+        const Two vb = mul2(vv, Two(T.b2)), vc = mul2(mul2(gg, gg), Two(T.c2));
+        mm = Two(__fadd_rn(mb.x(), mc.x()), __fadd_rn(mb.y(), mc.y()));
+        vv = Two(__fadd_rn(vb.x(), vc.x()), __fadd_rn(vb.y(), vc.y()));
+        const Two root(__fsqrt_rn(vv.x()), __fsqrt_rn(vv.y()));
+        const Two den = fma2(root, Two(T.root), Two(T.eps)), p(w[h][e], w[h][e + 1]);
+        const Two u = mul2(mm, Two(reciprocal(den.x()), reciprocal(den.y())));
+        const Two now = fma2(Two(-step), u, fma2(Two(-decay), p, p));
+        w[h][e] = now.x(), w[h][e + 1] = now.y();
+        m[h][e] = mm.x(), m[h][e + 1] = mm.y();
+        const Two kept = BITS == 32 ? vv : root;
+        v[h][e] = kept.x(), v[h][e + 1] = kept.y();
         if (BITS == 8) {
-          mtop = fmaxf(mtop, fabsf(mm));  // drops a NaN
-          vtop = fmaxf(vtop, root);
-          odd |= !(fabsf(u) < 1e38f);
+          mtop = fmaxf(mtop, fmaxf(fabsf(mm.x()), fabsf(mm.y())));  // drops a NaN
+          vtop = fmaxf(vtop, fmaxf(root.x(), root.y()));
+          odd |= !(fabsf(u.x()) < 1e38f) | !(fabsf(u.y()) < 1e38f);
         }
+      }
+      const int64_t at = at0 + 128 * h;
+      const int n = whole ? 4 : part_of(x, at);
+      if (BITS == 32) {
+        store4<OZ2_TYPE_F32>(x.m, at, whole, n, m[h]);
+        store4<OZ2_TYPE_F32>(x.v, at, whole, n, v[h]);
+      }
+      if (MASTER) {
+        store4<OZ2_TYPE_F32>(x.master, at, whole, n, w[h]);
+        if (x.param) store4<W>(x.param, at, whole, n, w[h]);
+      } else {
+        store4<W>(x.param, at, whole, n, w[h]);
       }
     }
     if (BITS == 8) {
@@ -314,10 +361,11 @@ __global__ void __launch_bounds__(32 * kAdamWarps, BITS == 8 ? 5 : 1) adamw_kern
       for (int h = 0; h < 2; ++h) {
         float mc[4], vc[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t bits = scatter32(from + static_cast<uint32_t>(128 * h + e) * 0x9E3779B1u);
-          mc[e] = cut_stochastic<true>(m[h][e] * minv, bits << 4 & 0xFFFF0u);
-          vc[e] = cut_stochastic<false>(v[h][e] * vinv, bits >> 12 & 0xFFFF0u);
+        for (int e = 0; e < 4; e += 2) {
+          const uint32_t u = scatter32(from + static_cast<uint32_t>(128 * h + e) * 0x9E3779B1u);
+          const uint32_t w = scatter32(from + static_cast<uint32_t>(128 * h + e + 1) * 0x9E3779B1u);
+          cut_stochastic<true>(mul2(Two(m[h][e], m[h][e + 1]), Two(minv)), u << 4 & 0xFFFF0u, w << 4 & 0xFFFF0u, mc + e);
+          cut_stochastic<false>(mul2(Two(v[h][e], v[h][e + 1]), Two(vinv)), u >> 12 & 0xFFFF0u, w >> 12 & 0xFFFF0u, vc + e);
         }
         uint32_t mw = encode4(mc), vw = encode4(vc);
         if (rare) {  // infinities and NaN are kept as the NaN of their sign
@@ -332,21 +380,6 @@ __global__ void __launch_bounds__(32 * kAdamWarps, BITS == 8 ? 5 : 1) adamw_kern
         const int n = whole ? 4 : part_of(x, at0 + 128 * h);
         store_words<uint8_t>(x.m, at0 + 128 * h, whole, n, &mw);
         store_words<uint8_t>(x.v, at0 + 128 * h, whole, n, &vw);
-      }
-    }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int64_t at = at0 + 128 * h;
-      const int n = whole ? 4 : part_of(x, at);
-      if (BITS == 32) {
-        store4<OZ2_TYPE_F32>(x.m, at, whole, n, m[h]);
-        store4<OZ2_TYPE_F32>(x.v, at, whole, n, v[h]);
-      }
-      if (MASTER) {
-        store4<OZ2_TYPE_F32>(x.master, at, whole, n, w[h]);
-        if (x.param) store4<W>(x.param, at, whole, n, w[h]);
-      } else {
-        store4<W>(x.param, at, whole, n, w[h]);
       }
     }
   }
