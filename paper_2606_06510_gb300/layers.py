@@ -59,20 +59,17 @@ def _done(code, what):
         raise Oz2Error(code, what)
 
 
-def _stream(stream):
-    if stream is not None:
-        return stream.cuda_stream
-    if not torch.cuda.is_initialized():
-        torch.cuda.init()
+def _stream():
+    """The current stream (there is a CUDA tensor, so CUDA is up)."""
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _ld(t, rows, cols, what):
     """The row stride of a CUDA matrix of this shape."""
     assert t.is_cuda, f"{what}: oz2 operates on CUDA tensors"
-    s0, s1 = t.stride()
-    assert (s1 == 1 or cols <= 1) and (s0 >= cols or rows <= 1), f"{what}: rows must be contiguous (stride(1) == 1)"
-    return s0 if rows > 1 and s0 > 0 else cols or 1
+    ld, one = t.stride()
+    assert (one == 1 or cols <= 1) and (ld >= cols or rows <= 1), f"{what}: rows must be contiguous (stride(1) == 1)"
+    return ld if rows > 1 and ld > 0 else cols or 1
 
 
 def _rows(t, rows, cols, dtype, what):
@@ -82,9 +79,11 @@ def _rows(t, rows, cols, dtype, what):
     return t.data_ptr(), _ld(t, rows, cols, what)
 
 
-def _vector(t, count, dtype, what):
-    assert t.is_cuda and t.dim() == 1 and t.shape[0] == count and (t.stride(0) == 1 or count <= 1) and t.dtype in dtype, \
-        f"{what}: expected {count} contiguous values of {dtype} on the GPU"
+def _vector(t, count, dtype, other, what):
+    """The address of a contiguous CUDA vector of one of two dtypes."""
+    dt = t.dtype
+    assert (dt == dtype or dt == other) and t.is_cuda and t.shape == (count,) and t.is_contiguous(), \
+        f"{what}: expected {count} contiguous values of {dtype} or {other} on the GPU"
     return t.data_ptr()
 
 
@@ -109,7 +108,7 @@ def oz2_linear(x, w, bias=None, act="none", residual=None, x_scale=None, w_scale
     assert out_dtype is None or out_dtype == dt, "out_dtype: a 16-bit product has its operands' dtype"
     ldx, ldw = _ld(x, m, k, "x"), _ld(w, n, k, "w")
     if out is None:
-        y, ldy = x.new_empty((m, n), dtype=dt), n or 1
+        y, ldy = (x.new_empty((m, n)) if dt == xt else x.new_empty((m, n), dtype=dt)), n or 1
         yp = y.data_ptr()
     else:
         y = out
@@ -122,12 +121,12 @@ def oz2_linear(x, w, bias=None, act="none", residual=None, x_scale=None, w_scale
     if residual is not None:
         rp, ldr = _rows(residual, m, n, dt, "residual")
     if bias is not None:
-        bp, bt = _vector(bias, n, (dt, torch.float32), "bias"), TYPE[bias.dtype]
-    xs = _vector(x_scale, m, (torch.float32,), "x_scale") if x_scale is not None else None
-    ws = _vector(w_scale, n, (torch.float32,), "w_scale") if w_scale is not None else None
+        bp, bt = _vector(bias, n, dt, torch.float32, "bias"), TYPE[bias.dtype]
+    xs = _vector(x_scale, m, torch.float32, torch.float32, "x_scale") if x_scale is not None else None
+    ws = _vector(w_scale, n, torch.float32, torch.float32, "w_scale") if w_scale is not None else None
     _done((_ENTRIES.get("oz2_linear") or _entry("oz2_linear"))(
         m, n, k, TYPE.get(xt, -1), x.data_ptr(), ldx, w.data_ptr(), ldw, xs, ws, bp, bt, ACT[act], rp, ldr, zp, n or 1,
-        yp, ldy, TYPE.get(dt, -1), _stream(stream)), "oz2_linear")
+        yp, ldy, TYPE.get(dt, -1), _stream() if stream is None else stream.cuda_stream), "oz2_linear")
     return (y, z) if save_pre else y
 
 
@@ -175,10 +174,10 @@ def oz2_linear_grad(dy, x, w, pre=None, act="none", need=("dx", "dw", "db"), dx=
     else:
         if db is None:
             db = dy.new_empty(n, dtype=torch.float32)
-        bp = _vector(db, n, (torch.float32,), "db")
+        bp = _vector(db, n, torch.float32, torch.float32, "db")
     _done((_ENTRIES.get("oz2_linear_grad") or _entry("oz2_linear_grad"))(
         m, n, k, TYPE.get(dt, -1), dy.data_ptr(), ldy, zp, ldz, ACT[act], x.data_ptr(), ldx, w.data_ptr(), ldw, xp, lddx,
-        wp, lddw, wt, bp, GRAD_ACCUMULATE if accumulate else 0, _stream(stream)), "oz2_linear_grad")
+        wp, lddw, wt, bp, GRAD_ACCUMULATE if accumulate else 0, _stream() if stream is None else stream.cuda_stream), "oz2_linear_grad")
     return dx, dw, db
 
 
@@ -266,4 +265,4 @@ def oz2_adamw(plan: AdamWPlan, step: int, lr: float, beta1=0.9, beta2=0.999, eps
         a.d_grad_scale = None
     _done((_ENTRIES.get("oz2_adamw") or _entry("oz2_adamw"))(
         plan.tensors, len(plan.tensors), TYPE.get(plan.param_type, -1), TYPE.get(plan.grad_type, -1), plan.bits,
-        ctypes.byref(a), _stream(stream)), "oz2_adamw")
+        ctypes.byref(a), _stream() if stream is None else stream.cuda_stream), "oz2_adamw")

@@ -38,7 +38,8 @@ def make(torch, m, n, k, dtype, seed=0, pad=(0, 0)):
 
 SHAPES = [(1, 1, 1), (1, 128, 64), (2, 129, 63), (3, 4096, 4096), (8, 1000, 520), (16, 640, 16384), (17, 257, 130),
           (33, 96, 1032), (64, 2048, 512), (100, 300, 257), (128, 128, 128), (129, 255, 129), (256, 256, 256),
-          (257, 513, 1027), (500, 64, 8192), (1000, 777, 1333), (1024, 2304, 640)]
+          (257, 513, 1027), (500, 64, 8192), (1000, 777, 1333), (1024, 2304, 640),
+          (128, 4096, 4096), (300, 1024, 12288), (512, 4096, 16384), (2500, 3001, 500), (5000, 2600, 72)]
 
 
 @pytest.mark.parametrize("shape", SHAPES)
@@ -198,3 +199,25 @@ def test_offsets_beyond_32_bits(env):
     oz.oz2_linear(x, w, out=y)
     wy, _, by, _ = ref.linear(xs, w)
     ref.close(y, wy, by)
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 4096, 4096), (7, 640, 8192), (40, 4672, 6016), (16, 16384, 8192), (200, 2048, 2048),
+                                   (512, 4096, 16384), (3000, 2500, 512), (9, 8200, 64), (1000, 72, 4000)])
+def test_calls_repeat_bit_for_bit_beside_others(env, m, n, k):
+    """Each way that a product runs (few rows, many, split depths): the same bits
+    alone, and while other products run on another stream."""
+    oz, torch = env
+    x, w, _, _, normal = make(torch, m, n, k, torch.bfloat16, seed=9)
+    b = normal(n)
+    want = oz.oz2_linear(x, w, bias=b, act="silu")
+    x2, w2, _, _, _ = make(torch, 700, 900, 1100, torch.bfloat16, seed=10)
+    other = oz.oz2_linear(x2, w2, act="gelu")
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    got, beside = [], []
+    for _ in range(4):
+        with torch.cuda.stream(s):
+            beside.append(oz.oz2_linear(x2, w2, act="gelu"))
+        got.append(oz.oz2_linear(x, w, bias=b, act="silu"))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, want) for a in got) and all(torch.equal(a, other) for a in beside)

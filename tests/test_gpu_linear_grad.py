@@ -37,7 +37,8 @@ def check(got, dy, x, w, z, name, torch):
 
 @pytest.mark.parametrize("shape", [(1, 1, 1), (1, 300, 200), (8, 128, 64), (17, 257, 130), (100, 64, 1032), (128, 128, 128),
                                    (129, 255, 129), (256, 256, 256), (300, 1000, 72), (513, 257, 1027),
-                                   (5000, 96, 130), (8192, 256, 192), (1000, 1333, 777)])
+                                   (5000, 96, 130), (8192, 256, 192), (1000, 1333, 777), (16384, 512, 512),
+                                   (20000, 200, 1000), (40, 2000, 3000), (2304, 1536, 1280)])
 @pytest.mark.parametrize("kind", ["bf16", "f16"])
 def test_shapes(env, shape, kind):
     oz, torch = env
@@ -163,3 +164,27 @@ def test_on_another_stream_and_in_a_graph(env):
     g.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+def test_accumulation_with_split_depths(env):
+    """Many tokens into small weights: the parts of the depth and what was there."""
+    oz, torch = env
+    m, n, k = 16384, 512, 300
+    dy, x, w, _ = make(torch, m, n, k, torch.bfloat16, seed=7)
+    want, (_, _, bb), ew = ref.grad(dy, x, w, None, "none")
+    dw, db = torch.full((n, k), 5.0, device="cuda"), torch.full((n,), 1.0, device="cuda")
+    oz.oz2_linear_grad(dy, x, w, dw=dw, db=db, accumulate=True)
+    ref.close(dw, want[1] + 5, ew + 2.0 ** -23 * (want[1].abs() + 5), "dw")
+    ref.close(db, want[2] + 1, bb + 2.0 ** -23 * (want[2].abs() + 1), "db")
+
+
+def test_db_of_many_rows(env):
+    """One column block, rows beyond a cluster's: sums in a fixed order."""
+    oz, torch = env
+    for m, n in ((2048, 40), (2049, 40), (100000, 24), (3000, 1001)):
+        dy = torch.randn(m, n, generator=torch.Generator(device="cuda").manual_seed(m), device="cuda").to(torch.float16)
+        x, w = torch.zeros(m, 8, dtype=torch.float16, device="cuda"), torch.zeros(n, 8, dtype=torch.float16, device="cuda")
+        db = oz.oz2_linear_grad(dy, x, w, need=("db",))[2]
+        d = dy.double()
+        ref.close(db, d.sum(0), (m / 8 + 16) * 2.0 ** -23 * d.abs().sum(0), (m, n))
+        assert torch.equal(db, oz.oz2_linear_grad(dy, x, w, need=("db",))[2])
