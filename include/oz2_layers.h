@@ -15,7 +15,10 @@
  * the row-major (m, k) array that deep-learning frameworks hold.  W is k×n, an
  * output's k weights contiguous: the row-major (n, k) weight of a linear layer.
  *
- * Sums are held in FP32 and rounded once to the output's type.  Base addresses
+ * Sums are held in FP32 and rounded once to the output's type.  (The tensor
+ * cores' FP32 sums truncate: against 64 bits a sum is low by 1e-9 to 5e-9 of
+ * itself for each element summed over, some 2e-5 at 16384, below a 16-bit
+ * rounding; it shows in an F32 dW over very many tokens.)  Base addresses
  * are multiples of the element size; leading dimensions are in elements.  Where
  * an operand's base or leading dimension is no multiple of 16 bytes its rows are
  * first copied to ones that are (a pass over that operand, and workspace for it).

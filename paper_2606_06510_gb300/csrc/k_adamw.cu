@@ -15,13 +15,14 @@
 // lane, consecutive over the warp.
 //
 // With FP32 states memory bounds it: 201 M bf16 parameters with masters and bf16
-// gradients, 28 bytes each, take 814 µs (6.9 TB/s, a plain copy's rate).  With
-// 8-bit states there are 16 bytes and some 105 instructions a parameter (the hash
-// and the two roundings are a third of them): issue bounds it, 714 µs at 4.5 TB/s.
-// Loading the next block ahead took it from 1209 to 826 µs, a kernel for each
-// combination of types to 741, and a fifth block of 128 threads an SM, at 24 to 44
-// bytes of spills, to 714 (six: 792).  A square root without the compiler's branch
-// cost as many instructions as it saved.
+// gradients, 28 bytes each, take 814 µs (6.9 TB/s, a plain copy's rate).  With 8-bit
+// states there are 16 bytes and some 100 instructions a parameter (the hash and the two
+// roundings are a third of them): issue bounds it (77% of the slots, integer pipe 58%),
+// 648 µs at 5 TB/s.  Loading the next block ahead took it from 1209 to 826 µs, a kernel
+// for each combination of types to 741, packed FP32 instructions and the weights'
+// stores before the rounding, which leave room for six blocks of 128 threads an SM, to
+// 648 (four: 700).  A square root without the compiler's branch cost as many
+// instructions as it saved.
 #include <algorithm>
 
 #include "lin_common.cuh"
@@ -299,6 +300,7 @@ __global__ void __launch_bounds__(32 * kAdamWarps, BITS == 8 ? 6 : 1) adamw_kern
           vv = mul2(vv, vv);
         }
         // Rounded one by one, so that the 8-bit states can be checked bit for bit.
+        // (The compiler joins packed products and sums; single sums it leaves alone.)
         const Two mb = mul2(mm, Two(T.b1)), mc = mul2(gg, Two(T.c1));
         const Two vb = mul2(vv, Two(T.b2)), vc = mul2(mul2(gg, gg), Two(T.c2));
         mm = Two(__fadd_rn(mb.x(), mc.x()), __fadd_rn(mb.y(), mc.y()));

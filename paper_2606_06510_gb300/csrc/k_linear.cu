@@ -303,6 +303,23 @@ struct PairWork {
 // has its tiles' depth split over pairs.  A part's sums go to the workspace in FP32;
 // each epilogue warp counts its own 32 × 64 corner in, and the warp that comes last
 // adds up the tile's parts, in their order whoever is last, and finishes them.
+//
+// What bounds it: the tensor pipes and, as closely, what an SM takes in.  A step of
+// 64 elements of depth is 512 cycles of MMAs and 32 KB a CTA at 64 bytes a cycle, 247
+// ns at 2.07 GHz; one pair alone takes 262, all 76 together 282 (and the power cap the
+// rest).  So a narrower tile would only load more for its MMAs, and five stages are
+// wanted (four: 339 ns).  4864×4096×4096 bf16, four even rounds of tiles, takes 84 µs
+// (1.94 PFLOP/s); 4096³ 80, its fourth round a third full; 16384²×4096 1.11 ms; E4M3
+// 8192³ 268 µs (4.1 PFLOP/s).  Sharing out the last round's steps of depth evenly
+// (parts of every tile's) won 1% at 4096³ and lost where there were fewer tiles: a
+// part's sums are 256 KB to write and to read.  Split depths: 65536 tokens' dX and dW at
+// 1024×1024 take 160 µs, 344 with dW's 16 tiles whole.
+//
+// The epilogue is 16 warps, 32 rows × 64 columns each, in 32-column chunks through
+// two KB of shared memory that turn a thread's row into 64-byte pieces of eight rows.
+// At a depth of 64, where it is all there is, a round takes 3.3 µs (a relu adds 0.5,
+// silu 0.3, gelu_tanh 1.4, gelu 2.3, a residual 2.2, which is memory's): it hides
+// behind the next tile's products from a depth of about 1024 on.
 // ---------------------------------------------------------------------------
 template <int TYPE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
@@ -393,6 +410,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
         dev->status = kStatusTimeout;
         dev->timeout_site = 21;
       }
+      pdl_trigger();  // the next kernel's start overlaps the last tiles
       if (leader)  // the leader's stage barriers also count the peer's bytes
         for (uint32_t j = (it > kLinStages ? it - kLinStages : 0); j < it; ++j)
           mbar_wait_bounded(full0 + 8 * (j % kLinStages), (j / kLinStages) & 1, kWaitLimit);
@@ -636,6 +654,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
 // were), and after a cluster barrier takes an equal share of the tile's rows, adds
 // up the parts in the order of the CTAs and finishes them: no workspace, and the
 // same bits every time.
+//
+// What bounds it: memory, where the weights stream through (16 tokens × 16384² E4M3
+// 43 µs, 6.2 TB/s; bf16 81 µs, 6.6), else the chain of a launch, its first loads, the
+// MMAs, the parts' exchange and the stores: 1 × 512 × 512 takes 3.7 µs, one token × 4096²
+// bf16 9.1 (34 MB in 128 CTAs), 256³ 3.7, 1024×2048×2048 12.6.  A thread's columns of the
+// tile are the same for every row it finishes, so biases and scales are in registers
+// before the sums come, and a residual's row is loaded one ahead.
 // ---------------------------------------------------------------------------
 constexpr int kSplitThreads = 256;    // TMA warp, MMA warp, 4 that drain, all 8 finish
 constexpr int kMaxSplit = 8;

@@ -37,6 +37,11 @@ __global__ void __launch_bounds__(256) pack_rows_kernel(PackJob a, PackJob b) {
 // a fixed order.  Up to 8 chunks (2048 rows) are a cluster, whose first block adds up
 // the others' sums; more of them write theirs to `partial` (chunk, column) and a second
 // kernel adds those.  Either way in order: the sums never depend on who came first.
+//
+// Memory bounds it without an activation (65536×1024 bf16: 134 MB in 26 µs, 5.2 TB/s),
+// with one the load-work-store chain of three blocks an SM (4096² gelu_tanh: 101 MB in
+// 24 µs; exp and erf by their slow functions it was 62).  Rows off the 16-byte grid
+// are put together from two aligned loads each: 2500×3001 gelu 21 µs.
 // ---------------------------------------------------------------------------
 constexpr int kGradCols = 256, kGradWarps = 8, kGradBlocks = 3;  // blocks an SM
 

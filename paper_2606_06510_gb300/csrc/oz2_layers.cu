@@ -1,7 +1,6 @@
 // Entry points of the layer operators (declared in include/oz2_layers.h):
 // argument checks, workspace, and the order of their launches.
 #include <algorithm>
-#include <vector>
 
 #include "lin_common.cuh"
 
