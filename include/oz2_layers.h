@@ -108,8 +108,8 @@ int oz2_linear_grad(int64_t m, int64_t n, int64_t k, int type,
  * seed, step and the value's number: the list's values are numbered through,
  * every tensor starting a new block of 256 (so a step can be repeated bit for
  * bit, and a tensor's place in the list matters).  w is updated from the
- * unrounded m and v.  States of zero bytes with any scales are the initial
- * state.  A value that is not finite is kept as E4M3's NaN; the others of its
+ * unrounded m and v.  States of zero bytes with any finite scales are the
+ * initial state.  A value that is not finite is kept as E4M3's NaN; the others of its
  * block are not touched by it.
  *
  * param_type F32, BF16 or F16 (a master wants a 16-bit one); grad_type F32 or

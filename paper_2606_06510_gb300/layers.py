@@ -3,10 +3,10 @@ epilogue, that layer's gradient, and AdamW over many tensors.
 
 Arrays are those of a PyTorch program, row-major: x (tokens, k), w (n, k),
 y (tokens, n), with stride(1) == 1 and any row stride.  They are the C ABI's
-column-major matrices with tokens as columns.  Outputs of rows that are read
-back as operands do best with row strides that are multiples of 16 bytes (8
-elements of 16 bits), which the tensor cores' loads want: other rows are copied
-to such ones first.
+column-major matrices with tokens as columns.  Row strides (and starts) that are
+multiples of 16 bytes, 8 elements of 16 bits, are what the tensor cores' loads
+want: other operands are copied to such rows first.  A call runs on the current
+stream, or on `stream`, whose memory its new outputs then are.
 """
 from __future__ import annotations
 
@@ -64,6 +64,14 @@ def _stream():
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
+def _new(like, shape, dtype, stream):
+    """An output, of the memory of the stream that writes it."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
+
+
 def _ld(t, rows, cols, what):
     """The row stride of a CUDA matrix of this shape."""
     assert t.is_cuda, f"{what}: oz2 operates on CUDA tensors"
@@ -108,7 +116,7 @@ def oz2_linear(x, w, bias=None, act="none", residual=None, x_scale=None, w_scale
     assert out_dtype is None or out_dtype == dt, "out_dtype: a 16-bit product has its operands' dtype"
     ldx, ldw = _ld(x, m, k, "x"), _ld(w, n, k, "w")
     if out is None:
-        y, ldy = (x.new_empty((m, n)) if dt == xt else x.new_empty((m, n), dtype=dt)), n or 1
+        y, ldy = _new(x, (m, n), dt, stream), n or 1
         yp = y.data_ptr()
     else:
         y = out
@@ -116,7 +124,7 @@ def oz2_linear(x, w, bias=None, act="none", residual=None, x_scale=None, w_scale
     z = zp = rp = bp = None
     ldr = bt = 0
     if save_pre:
-        z = x.new_empty((m, n), dtype=dt)
+        z = _new(x, (m, n), dt, stream)
         zp = z.data_ptr()
     if residual is not None:
         rp, ldr = _rows(residual, m, n, dt, "residual")
@@ -157,14 +165,14 @@ def oz2_linear_grad(dy, x, w, pre=None, act="none", need=("dx", "dw", "db"), dx=
     if "dx" not in need:
         dx = None
     elif dx is None:
-        dx = dy.new_empty((m, k))
+        dx = _new(dy, (m, k), dt, stream)
         xp = dx.data_ptr()
     else:
         xp, lddx = _rows(dx, m, k, dt, "dx")
     if "dw" not in need:
         dw = None
     elif dw is None:
-        dw = dy.new_empty((n, k), dtype=dw_dtype or dt)
+        dw = _new(dy, (n, k), dw_dtype or dt, stream)
         wp, wt = dw.data_ptr(), TYPE.get(dw.dtype, -1)
     else:
         wp, lddw = _rows(dw, n, k, dw.dtype, "dw")
@@ -173,7 +181,7 @@ def oz2_linear_grad(dy, x, w, pre=None, act="none", need=("dx", "dw", "db"), dx=
         db = None
     else:
         if db is None:
-            db = dy.new_empty(n, dtype=torch.float32)
+            db = _new(dy, (n,), torch.float32, stream)
         bp = _vector(db, n, torch.float32, torch.float32, "db")
     _done((_ENTRIES.get("oz2_linear_grad") or _entry("oz2_linear_grad"))(
         m, n, k, TYPE.get(dt, -1), dy.data_ptr(), ldy, zp, ldz, ACT[act], x.data_ptr(), ldx, w.data_ptr(), ldw, xp, lddx,

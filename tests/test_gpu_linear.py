@@ -221,3 +221,22 @@ def test_calls_repeat_bit_for_bit_beside_others(env, m, n, k):
         got.append(oz.oz2_linear(x, w, bias=b, act="silu"))
     torch.cuda.synchronize()
     assert all(torch.equal(a, want) for a in got) and all(torch.equal(a, other) for a in beside)
+
+
+def test_a_given_stream_owns_the_outputs(env):
+    """Outputs of a call on another stream come from that stream's memory: freed at
+    once and allocated again there, they are not handed to the current stream."""
+    oz, torch = env
+    x, w, _, _, _ = make(torch, 300, 200, 100, torch.bfloat16, seed=11)
+    dy = torch.ones(300, 200, dtype=torch.bfloat16, device="cuda")
+    want = oz.oz2_linear(x, w, act="silu"), oz.oz2_linear_grad(dy, x, w)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = oz.oz2_linear(x, w, act="silu", stream=s), oz.oz2_linear_grad(dy, x, w, stream=s)
+    at = got[0].data_ptr()
+    s.synchronize()
+    assert torch.equal(got[0], want[0]) and all(torch.equal(a, b) for a, b in zip(got[1], want[1]))
+    del got
+    with torch.cuda.stream(s):
+        again = [torch.empty(300, 200, dtype=torch.bfloat16, device="cuda") for _ in range(4)]
+    assert at in [t.data_ptr() for t in again]
