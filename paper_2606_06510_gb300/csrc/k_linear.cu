@@ -10,6 +10,7 @@
 // both land in shared memory with the 128-byte swizzle, and the descriptor and
 // the instruction's transpose bits tell them apart.
 #include <algorithm>
+#include <type_traits>
 
 #include "lin_common.cuh"
 
@@ -33,12 +34,14 @@ struct LinUnits {                     // one product of a launch
   int ntm, ntn, units;
   int steps;                          // of 128 bytes of depth
   int split;                          // on pairs: parts that the depth of each tile is cut into
+  int halves;                         // on pairs: last tiles that are taken as two halves
   uint32_t p_mn, q_mn;
   LinEpilogue ep;
 };
 struct LinLaunch {
   int count;
   int units;                          // whole tiles (of the products with split = 1)
+  int half_units;                     // on pairs: halves of tiles, after those, all of the last product
   // On pairs: the parts of the tiles of products with split > 1, one to a pair from
   // the first on; the pairs without one take whole tiles in `ahead` rounds of their
   // own meanwhile.
@@ -49,6 +52,7 @@ struct LinLaunch {
 };
 struct LinMaps {
   CUtensorMap p[kMaxProducts], q[kMaxProducts];
+  CUtensorMap q_half;                 // the last product's Q in boxes of half the rows (K-major)
 };
 
 // Instruction descriptor of kind::f16 with FP32 sums: D = F32 (bits 4-5 = 1), A
@@ -252,6 +256,7 @@ __device__ __forceinline__ int count_part(int* at) {
 struct Piece {
   int i;               // product
   int tm, tn;          // tile
+  int col, width;      // its first column of the result and how many (256, or 128 of a half)
   int t0, t1;          // steps of its depth
   int parts;           // of the tile (1: whole)
   int slot, first_slot, stride;  // of its sums: this part's, the first part's, from part to part
@@ -262,6 +267,7 @@ struct PairWork {
   int pair, npairs, round;
   __device__ PairWork(const LinLaunch& launch, int p, int np) : L(launch), pair(p), npairs(np), round(p < launch.parts ? -1 : 0) {}
   __device__ bool next(Piece& p) {
+    p.width = kLinTile;
     if (round < 0) {
       round = L.ahead;
       const int first = L.u[0].split > 1 ? L.u[0].units * L.u[0].split : 0;
@@ -270,6 +276,7 @@ struct PairWork {
       const int v = p.i ? pair - first : pair, part = v / x.units, tile = v - part * x.units;
       const int per = (x.steps + x.split - 1) / x.split;
       unit_tile(x, tile, &p.tm, &p.tn);
+      p.col = p.tn * kLinTile;
       p.t0 = min(x.steps, part * per);
       p.t1 = min(x.steps, p.t0 + per);
       p.parts = x.split;
@@ -282,11 +289,16 @@ struct PairWork {
     const int others = npairs - L.parts;
     int u = round < L.ahead ? round * others + pair - L.parts : L.ahead * others + (round - L.ahead) * npairs + pair;
     ++round;
-    if (u >= L.units) return false;
-    const int first = L.u[0].split > 1 ? 0 : L.u[0].units;
-    p.i = u >= first ? 1 : 0;
+    if (u >= L.units + L.half_units) return false;
+    const int first = L.u[0].split > 1 ? 0 : L.u[0].units - L.u[0].halves, half = u - L.units;
+    p.i = half >= 0 ? L.count - 1 : u >= first ? 1 : 0;
     const LinUnits& x = L.u[p.i];
-    unit_tile(x, p.i ? u - first : u, &p.tm, &p.tn);
+    unit_tile(x, half >= 0 ? x.units - x.halves + half / 2 : p.i ? u - first : u, &p.tm, &p.tn);
+    p.col = p.tn * kLinTile;
+    if (half >= 0) {
+      p.width = kLinTile / 2;
+      p.col += (half & 1) * p.width;
+    }
     p.t0 = 0;
     p.t1 = x.steps;
     p.parts = 1;
@@ -309,9 +321,11 @@ struct PairWork {
 // ns at 2.07 GHz; one pair alone takes 262, all 76 together 282 (and the power cap the
 // rest).  So a narrower tile would only load more for its MMAs, and five stages are
 // wanted (four: 339 ns).  4864×4096×4096 bf16, four even rounds of tiles, takes 84 µs
-// (1.94 PFLOP/s); 4096³ 80, its fourth round a third full; 16384²×4096 1.11 ms; E4M3
-// 8192³ 268 µs (4.1 PFLOP/s).  Sharing out the last round's steps of depth evenly
-// (parts of every tile's) won 1% at 4096³ and lost where there were fewer tiles: a
+// (1.94 PFLOP/s); 4096³ 76; 16384²×4096 1.11 ms; E4M3
+// 8192³ 268 µs (4.1 PFLOP/s).  A last round that is at most half full takes its tiles
+// as halves on twice as many pairs (a half's step, its loads, 390 cycles of 535: 4096³
+// 80 to 76 µs, the gradient of 2504×3008×2048 44 to 39).  Sharing out that round's steps
+// of depth evenly instead (parts of every tile's) won 1% at 4096³ and lost elsewhere: a
 // part's sums are 256 KB to write and to read.  Split depths: 65536 tokens' dX and dW at
 // 1024×1024 take 160 µs, 344 with dW's 16 tiles whole.
 //
@@ -376,17 +390,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
         // In registers: what is read from the launch's parameters is read again at
         // every step (and each TMA instruction's operands wait for it).
         const int prow = pc.tm * kLinTile + rank * kRows;
-        const int qrow = pc.tn * kLinTile + rank * kRows;
+        const int qrow = pc.col + rank * (pc.width / 2);
         const int t1 = pc.t1;
-        const bool p_mn = x.p_mn != 0, q_mn = x.q_mn != 0;
-        const CUtensorMap *mp = &maps.p[pc.i], *mq = &maps.q[pc.i];
+        const bool p_mn = x.p_mn != 0, q_mn = x.q_mn != 0, half = pc.width != kLinTile;
+        const CUtensorMap *mp = &maps.p[pc.i], *mq = half ? &maps.q_half : &maps.q[pc.i];
+        const uint32_t bytes = 2u * (kTileBytes + (half ? kTileBytes / 2 : kTileBytes));
         for (int t = pc.t0, d = t * (F8 ? 128 : 64); t < t1; ++t, d += F8 ? 128 : 64) {
           if (!mbar_wait_bounded(empty0 + 8 * s, ph, kWaitLimit)) {
             ok = false;
             break;
           }
           const uint32_t sa = ring0 + s * kLinStage, sb = sa + kTileBytes, bar = full_leader0 + 8 * s;
-          if (leader) mbar_arrive_expect_tx(full0 + 8 * s, 2u * kLinStage);
+          if (leader) mbar_arrive_expect_tx(full0 + 8 * s, bytes);
           if (!p_mn) {
             tma_load_2d_pair(sa, mp, bar, d, prow);
           } else {
@@ -397,7 +412,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
             tma_load_2d_pair(sb, mq, bar, d, qrow);
           } else {
             tma_load_2d_pair(sb, mq, bar, qrow, d);
-            tma_load_2d_pair(sb + kTileBytes / 2, mq, bar, qrow + 64, d);
+            if (!half) tma_load_2d_pair(sb + kTileBytes / 2, mq, bar, qrow + 64, d);
           }
           ++it;
           if (++s == kLinStages) {
@@ -443,15 +458,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
         ok = mbar_wait_warp(acc_empty + 8 * acc, accph, kWaitLimit);
         tc_fence_after();
         const int steps = pc.t1 - pc.t0;
+        auto by_width = [&](auto p_mn, auto q_mn) {
+          constexpr bool PM = decltype(p_mn)::value, QM = decltype(q_mn)::value;
+          const uint64_t pd = operand_desc<PM>(base), qd = operand_desc<QM>(base + kTileBytes);
+          if (pc.width == kLinTile) {
+            multiply(MmaShape<TYPE, PM, QM, kLinTile, kLinTile>{}, pd, qd, steps, tmem + acc * kLinTile);
+          } else {
+            multiply(MmaShape<TYPE, PM, QM, kLinTile, kLinTile / 2>{}, pd, qd, steps, tmem + acc * kLinTile);
+          }
+        };
         if (F8 || !x.q_mn) {
-          multiply(MmaShape<TYPE, false, false, kLinTile, kLinTile>{}, operand_desc<false>(base),
-                   operand_desc<false>(base + kTileBytes), steps, tmem + acc * kLinTile);
+          by_width(std::false_type{}, std::false_type{});
         } else if (!x.p_mn) {
-          multiply(MmaShape<TYPE, false, true, kLinTile, kLinTile>{}, operand_desc<false>(base),
-                   operand_desc<true>(base + kTileBytes), steps, tmem + acc * kLinTile);
+          by_width(std::false_type{}, std::true_type{});
         } else {
-          multiply(MmaShape<TYPE, true, true, kLinTile, kLinTile>{}, operand_desc<true>(base),
-                   operand_desc<true>(base + kTileBytes), steps, tmem + acc * kLinTile);
+          by_width(std::true_type{}, std::true_type{});
         }
         if (!ok) break;
         mma_commit_pair_mc(me, acc_full + 8 * acc, 0x3);
@@ -478,19 +499,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
     while (work.next(pc)) {
       const LinUnits& x = L.u[pc.i];
       const LinEpilogue& ep = x.ep;
-      const int64_t row0 = pc.tm * kLinTile + rank * kRows + 32 * q, col0 = pc.tn * kLinTile + kLinCols * h;
+      const int cols = pc.width / 4;  // of this warp
+      const int64_t row0 = pc.tm * kLinTile + rank * kRows + 32 * q, col0 = pc.col + cols * h;
       const bool bf16 = TYPE == OZ2_TYPE_BF16 || (F8 && ep.out_type == OZ2_TYPE_BF16);
       const bool scales = F8 && ep.row_scale != nullptr, add = ep.add != nullptr;
       const bool sums = pc.t1 > pc.t0;
       // Where this warp's corner is inside the matrix and on 16-byte boundaries.
-      const bool inside = row0 + 32 <= x.rows && col0 + kLinCols <= x.cols;
+      const bool inside = row0 + 32 <= x.rows && col0 + cols <= x.cols;
       const bool fast_add = inside && vec_ok(ep.add, ep.ld_add, 2), fast_pre = inside && vec_ok(ep.pre, ep.ld_pre, 2),
                  fast_out = inside && vec_ok(ep.out, ep.ld_out, 2);
       const int64_t lane_row = row0 + (lane >> 2), lane_col = col0 + 8 * (lane & 3);
       __syncwarp();
       if (ep.bias) {
-#pragma unroll
-        for (int c = lane; c < kLinCols; c += 32) {
+        for (int c = lane; c < cols; c += 32) {
           const int64_t j = col0 + c;
           float b = 0.f;
           if (j < x.cols)
@@ -501,8 +522,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
       }
       float row_scale = 0.f;
       if (scales) {
-#pragma unroll
-        for (int c = lane; c < kLinCols; c += 32) scale_s[c] = col0 + c < x.cols ? __ldg(ep.col_scale + col0 + c) : 0.f;
+        for (int c = lane; c < cols; c += 32) scale_s[c] = col0 + c < x.cols ? __ldg(ep.col_scale + col0 + c) : 0.f;
         if (row0 + lane < x.rows) row_scale = __ldg(ep.row_scale + row0 + lane);
       }
       Fetched r;
@@ -517,7 +537,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
         }
         tc_fence_after();
       }
-      const uint32_t at = tmem + (static_cast<uint32_t>(32 * q) << 16) + acc * kLinTile + kLinCols * h;
+      const uint32_t at = tmem + (static_cast<uint32_t>(32 * q) << 16) + acc * kLinTile + cols * h;
       auto release = [&] {
         if (sums) {
           tc_fence_before();
@@ -555,7 +575,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
         __syncwarp();
       }
 #pragma unroll 1
-      for (int c = 0; c < kLinCols; c += kChunk) {
+      for (int c = 0; c < cols; c += kChunk) {
         float z[32];
         if (pc.parts > 1) {
 #pragma unroll
@@ -577,7 +597,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
           uint32_t v[32];
           tmem_ld32(at + c, v);
           tmem_ld_wait();
-          if (c == kLinCols - kChunk) release();
+          if (c == cols - kChunk) release();
 #pragma unroll
           for (int j = 0; j < 32; ++j) z[j] = __uint_as_float(v[j]);
         } else {
@@ -612,7 +632,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
         if (add) {
           if (fast_add) {
             fetch_end(r, lane, buf);
-            if (c + kChunk < kLinCols) fetch_begin(from + c + kChunk, ep.ld_add, r);
+            if (c + kChunk < cols) fetch_begin(from + c + kChunk, ep.ld_add, r);
           } else {
             fetch_slow(ep.add, ep.ld_add, x.rows, x.cols, row0, col0 + c, lane, buf);
           }
@@ -1024,8 +1044,8 @@ int64_t steps_of(const LinProduct& p, int type) {
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // The estimates (cycles of an SM) behind a plan, fitted to measurements on one GB300.
-//   Pairs: a step of a tile 535 (512 of MMAs), a tile at least 4600 (its epilogue) and
-//   1000 more; the launch's start and its last epilogue 10000; the exchange of split
+//   Pairs: a step of a tile 535 (512 of MMAs), of half a tile 390 (its loads), a tile
+//   at least 4600 (its epilogue) and 1000 more; the launch's start and its last epilogue 10000; the exchange of split
 //   tiles' parts 26000.
 //   Clusters: a CTA 5600 and for each step what its loads take of the SM's 61 bytes a
 //   cycle or its MMAs of the tensor core; 26 for each row that it finishes; joining
@@ -1038,7 +1058,9 @@ constexpr double kCta = 5600, kLoadRate = 61, kFinishRow = 26, kJoin = 1200, kJo
 constexpr double kMemoryRate = 24;
 constexpr double kTwoLaunches = 2500;  // what a launch of its own costs beside a product's time
 
+constexpr double kHalfStep = 390;
 double pair_tile_cycles(int64_t steps) { return std::max(steps * kPairStep, kPairTileLeast) + kPairTile; }
+double half_tile_cycles(int64_t steps) { return std::max(steps * kHalfStep, kPairTileLeast / 2) + kPairTile; }
 
 // CTAs in clusters of `split` that run at once, one or two to an SM (152 SMs in
 // groups that clusters do not cross).
@@ -1063,6 +1085,15 @@ void plan_pairs(const int64_t (&tiles)[kMaxProducts], const int64_t (&steps)[kMa
   // Rounds of tiles, of the tiles' mean where they differ.
   best->cost = kPairLaunch + std::max({longest, ceil_div(units, pairs) * (work / units),
                                        bytes / (kMemoryRate * 2 * std::min(units, pairs))});
+  // A last round of few tiles: they are taken as halves, by twice as many pairs.
+  const int64_t last = units % pairs;
+  if (units > pairs && last > 0 && 2 * last <= pairs && last <= tiles[count - 1]) {
+    const double cost = best->cost - pair_tile_cycles(steps[count - 1]) + half_tile_cycles(steps[count - 1]);
+    if (cost < best->cost) {
+      best->cost = cost;
+      best->halves = static_cast<int>(last);
+    }
+  }
   // The parts of the products of few tiles, while they fit, each next one to the
   // tile that takes longest.
   int split[kMaxProducts] = {1, 1};
@@ -1099,6 +1130,7 @@ void plan_pairs(const int64_t (&tiles)[kMaxProducts], const int64_t (&steps)[kMa
   const double cost = kPairLaunch + kExchange + std::max(part, whole ? all / pairs + tile / 2 : part);
   if (parts == 0 || cost >= best->cost) return;
   best->cost = cost;
+  best->halves = 0;
   for (int i = 0; i < count; ++i) best->pair_split[i] = split[i];
   best->parts = static_cast<int>(parts);
   // Rounds of whole tiles that the other pairs have time for beside a part.
@@ -1216,6 +1248,7 @@ cudaError_t launch_linear(const LinProduct* products, int count, int type, const
     x.ntn = static_cast<int>(ntn);
     x.units = x.ntm * x.ntn;
     x.split = plan.pair_split[i];
+    x.halves = i + 1 == count ? plan.halves : 0;
     x.steps = static_cast<int>(steps_of(p, type));
     x.p_mn = p.p_mn;
     x.q_mn = p.q_mn;
@@ -1223,10 +1256,13 @@ cudaError_t launch_linear(const LinProduct* products, int count, int type, const
     if (x.split > 1) {
       split_tiles += x.units;
     } else {
-      L.units += x.units;
+      L.units += x.units - x.halves;
+      L.half_units += 2 * x.halves;
     }
     if (x.steps && (!make_operand_map(&maps.p[i], p.p, p.rows, p.depth, p.ldp, type, p.p_mn, plan.nt ? plan.nt : kRows) ||
-                    !make_operand_map(&maps.q[i], p.q, p.cols, p.depth, p.ldq, type, p.q_mn)))
+                    !make_operand_map(&maps.q[i], p.q, p.cols, p.depth, p.ldq, type, p.q_mn) ||
+                    (x.halves &&
+                     !make_operand_map(&maps.q_half, p.q, p.cols, p.depth, p.ldq, type, p.q_mn, kRows / 2))))
       return cudaErrorInvalidValue;
   }
   L.count = count;

@@ -13,6 +13,8 @@ namespace {
 // consecutive).  Up to two operands in one launch: the blocks of the second grid row
 // take the second.
 // ---------------------------------------------------------------------------
+constexpr int kPackAhead = 2;  // pieces of a thread on their way at once
+
 template <typename T>
 __global__ void __launch_bounds__(256) pack_rows_kernel(PackJob a, PackJob b) {
   pdl_trigger();
@@ -23,11 +25,32 @@ __global__ void __launch_bounds__(256) pack_rows_kernel(PackJob a, PackJob b) {
   T* dst = static_cast<T*>(x.dst);
   const int64_t per = (x.cols + kVec - 1) / kVec;
   const T* end = src + (x.rows - 1) * x.ld_src + x.cols;
-  for (int64_t i = blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x; i < x.rows * per;
-       i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
-    const int64_t r = i / per, c = (i - r * per) * kVec;
-    *reinterpret_cast<uint4*>(dst + r * x.ld_dst + c) =
-        load16_any(src + r * x.ld_src + c, src, end, static_cast<int>(min(static_cast<int64_t>(kVec), x.cols - c)));
+  const int64_t pieces = x.rows * per, stride = static_cast<int64_t>(gridDim.x) * blockDim.x;
+  for (int64_t i = blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x; i < pieces; i += kPackAhead * stride) {
+    const T* from[kPackAhead];
+    T* to[kPackAhead];
+    int n[kPackAhead];
+    bool inside = true;
+#pragma unroll
+    for (int j = 0; j < kPackAhead; ++j) {
+      const int64_t at = min(i + j * stride, pieces - 1), r = at / per, c = (at - r * per) * kVec;
+      from[j] = src + r * x.ld_src + c;
+      to[j] = dst + r * x.ld_dst + c;
+      n[j] = static_cast<int>(min(static_cast<int64_t>(kVec), x.cols - c));
+      inside = inside && words_inside(from[j], src, end);
+    }
+    if (inside) {
+      Words w[kPackAhead];
+#pragma unroll
+      for (int j = 0; j < kPackAhead; ++j) w[j] = load_words16(from[j]);
+#pragma unroll
+      for (int j = 0; j < kPackAhead; ++j)
+        if (i + j * stride < pieces) *reinterpret_cast<uint4*>(to[j]) = shift_words16(from[j], w[j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kPackAhead; ++j)
+        if (i + j * stride < pieces) *reinterpret_cast<uint4*>(to[j]) = load16_any(from[j], src, end, n[j]);
+    }
   }
 }
 
@@ -38,10 +61,11 @@ __global__ void __launch_bounds__(256) pack_rows_kernel(PackJob a, PackJob b) {
 // the others' sums; more of them write theirs to `partial` (chunk, column) and a second
 // kernel adds those.  Either way in order: the sums never depend on who came first.
 //
-// Memory bounds it without an activation (65536×1024 bf16: 134 MB in 26 µs, 5.2 TB/s),
+// Memory bounds it without an activation (65536×1024 bf16: 134 MB in 23 µs, 5.9 TB/s),
 // with one the load-work-store chain of three blocks an SM (4096² gelu_tanh: 101 MB in
-// 24 µs; exp and erf by their slow functions it was 62).  Rows off the 16-byte grid
-// are put together from two aligned loads each: 2500×3001 gelu 21 µs.
+// 19 µs; exp and erf by their slow functions it was 62).  Rows off the 16-byte grid
+// are put together from two aligned loads each, all of a round's under way at once:
+// 2500×3001 gelu 16 µs (27 when each row's bounds were asked before its loads).
 // ---------------------------------------------------------------------------
 constexpr int kGradCols = 256, kGradWarps = 8, kGradBlocks = 3;  // blocks an SM
 
@@ -90,31 +114,55 @@ __global__ void __launch_bounds__(32 * kGradWarps, kGradBlocks)
   float s[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) s[e] = 0.f;
-  auto load = [&](const uint16_t* src, int64_t ld, int64_t r) {
-    const uint16_t* p = src + r * ld + col;
-    if (ALIGNED) return left == 8 ? __ldg(reinterpret_cast<const uint4*>(p)) : load16_singly(p, left);
-    return load16_any(p, src, src + (m - 1) * ld + n, left);
-  };
   auto work = [&](uint4 a, uint4 b, int64_t r) {
     const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
     grad8<ACT>(aw, bw, BF16, s, dz ? dz + r * ld_dz + col : nullptr);
   };
+  auto one = [&](const uint16_t* src, int64_t ld, int64_t r) {
+    const uint16_t* p = src + r * ld + col;
+    if (ALIGNED) return left == 8 ? __ldg(reinterpret_cast<const uint4*>(p)) : load16_singly(p, left);
+    return load16_any(p, src, src + (m - 1) * ld + n, left);
+  };
   if (left > 0) {
     constexpr int kAhead = kGradAhead<ALIGNED>;
+    constexpr bool kZ = ACT != OZ2_ACT_NONE;
     int64_t r = r0 + warp;
     for (; r + (kAhead - 1) * kGradWarps < r1; r += kAhead * kGradWarps) {
-      uint4 a[kAhead], b[kAhead];
+      // The first and the last of these rows: what lies between them is inside too.
+      const int64_t last = r + (kAhead - 1) * kGradWarps;
+      const uint16_t *dy_end = dy + (m - 1) * ld_dy + n, *z_end = z + (m - 1) * ld_z + n;
+      if (ALIGNED ? left == 8
+                  : words_inside(dy + r * ld_dy + col, dy, dy_end) && words_inside(dy + last * ld_dy + col, dy, dy_end) &&
+                        (!kZ || (words_inside(z + r * ld_z + col, z, z_end) && words_inside(z + last * ld_z + col, z, z_end)))) {
+        if (ALIGNED) {
+          uint4 a[kAhead], b[kAhead];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        a[i] = load(dy, ld_dy, r + i * kGradWarps);
-        b[i] = make_uint4(0, 0, 0, 0);
-        if (ACT != OZ2_ACT_NONE) b[i] = load(z, ld_z, r + i * kGradWarps);
+          for (int i = 0; i < kAhead; ++i) {
+            a[i] = __ldg(reinterpret_cast<const uint4*>(dy + (r + i * kGradWarps) * ld_dy + col));
+            b[i] = kZ ? __ldg(reinterpret_cast<const uint4*>(z + (r + i * kGradWarps) * ld_z + col)) : make_uint4(0, 0, 0, 0);
+          }
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i) work(a[i], b[i], r + i * kGradWarps);
+        } else {
+          Words a[kAhead], b[kAhead];
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i) {
+            a[i] = load_words16(dy + (r + i * kGradWarps) * ld_dy + col);
+            if (kZ) b[i] = load_words16(z + (r + i * kGradWarps) * ld_z + col);
+          }
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i)
+            work(shift_words16(dy + (r + i * kGradWarps) * ld_dy + col, a[i]),
+                 kZ ? shift_words16(z + (r + i * kGradWarps) * ld_z + col, b[i]) : make_uint4(0, 0, 0, 0), r + i * kGradWarps);
+        }
+      } else {
+        for (int i = 0; i < kAhead; ++i) {
+          const int64_t at = r + i * kGradWarps;
+          work(one(dy, ld_dy, at), kZ ? one(z, ld_z, at) : make_uint4(0, 0, 0, 0), at);
+        }
       }
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) work(a[i], b[i], r + i * kGradWarps);
     }
-    for (; r < r1; r += kGradWarps)
-      work(load(dy, ld_dy, r), ACT == OZ2_ACT_NONE ? make_uint4(0, 0, 0, 0) : load(z, ld_z, r), r);
+    for (; r < r1; r += kGradWarps) work(one(dy, ld_dy, r), kZ ? one(z, ld_z, r) : make_uint4(0, 0, 0, 0), r);
   }
   if (!db) return;
 #pragma unroll
@@ -204,7 +252,7 @@ cudaError_t launch_pack_rows(const PackJob* jobs, int count, int bytes, cudaStre
   int64_t pieces = 0;
   for (int i = 0; i < count; ++i) pieces = std::max(pieces, jobs[i].rows * ((jobs[i].cols * bytes + 15) / 16));
   if (pieces == 0) return cudaSuccess;
-  const unsigned blocks = static_cast<unsigned>(std::min<int64_t>((pieces + 255) / 256, 16LL * num_sms()));
+  const unsigned blocks = static_cast<unsigned>(std::min<int64_t>((pieces + 256 * kPackAhead - 1) / (256 * kPackAhead), 16LL * num_sms()));
   count_launch();
   return launch_dependent(bytes == 1 ? pack_rows_kernel<uint8_t> : pack_rows_kernel<uint16_t>,
                           dim3(blocks, static_cast<unsigned>(count)), dim3(256), 0, st, jobs[0], jobs[count - 1]);

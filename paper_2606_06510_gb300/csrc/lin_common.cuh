@@ -46,19 +46,32 @@ __device__ __noinline__ uint4 load16_singly(const T* p, int n) {
     if (e < n) u.e[e] = __ldg(p + e);
   return u.v;
 }
-template <typename T>
-__device__ __forceinline__ uint4 load16_any(const T* p, const T* base, const T* end, int n) {
+// The two words, and whether they lie within the bounds; the loads themselves ask for
+// nothing, so that several can be under way.
+struct Words {
+  uint4 a, b;
+};
+__device__ __forceinline__ bool words_inside(const void* p, const void* base, const void* end) {
   const uintptr_t at = reinterpret_cast<uintptr_t>(p), word = at & ~static_cast<uintptr_t>(15);
-  const unsigned s = static_cast<unsigned>(at & 15);
-  if (word < reinterpret_cast<uintptr_t>(base) || word + (s ? 32 : 16) > reinterpret_cast<uintptr_t>(end))
-    return load16_singly(p, n);
-  const uint4 a = __ldg(reinterpret_cast<const uint4*>(word)), b = s ? __ldg(reinterpret_cast<const uint4*>(word + 16)) : a;
-  uint32_t w[6] = {a.x, a.y, a.z, a.w, b.x, b.y};
-  if (s & 8) w[0] = w[2], w[1] = w[3], w[2] = w[4], w[3] = w[5], w[4] = b.z, w[5] = b.w;
+  return word >= reinterpret_cast<uintptr_t>(base) && word + (at & 15 ? 32 : 16) <= reinterpret_cast<uintptr_t>(end);
+}
+__device__ __forceinline__ Words load_words16(const void* p) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p), word = at & ~static_cast<uintptr_t>(15);
+  return Words{__ldg(reinterpret_cast<const uint4*>(word)),
+               __ldg(reinterpret_cast<const uint4*>(word + (at & 15 ? 16 : 0)))};
+}
+__device__ __forceinline__ uint4 shift_words16(const void* p, const Words& x) {
+  const unsigned s = static_cast<unsigned>(reinterpret_cast<uintptr_t>(p) & 15);
+  uint32_t w[6] = {x.a.x, x.a.y, x.a.z, x.a.w, x.b.x, x.b.y};
+  if (s & 8) w[0] = w[2], w[1] = w[3], w[2] = w[4], w[3] = w[5], w[4] = x.b.z, w[5] = x.b.w;
   if (s & 4) w[0] = w[1], w[1] = w[2], w[2] = w[3], w[3] = w[4], w[4] = w[5];
   const unsigned bits = 8 * (s & 3);
   return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits),
                     __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
+}
+template <typename T>
+__device__ __forceinline__ uint4 load16_any(const T* p, const T* base, const T* end, int n) {
+  return words_inside(p, base, end) ? shift_words16(p, load_words16(p)) : load16_singly(p, n);
 }
 
 // --- activations ---------------------------------------------------------------
@@ -161,12 +174,13 @@ struct LinProduct {
 constexpr int kMaxProducts = 2;
 
 // How a launch runs: on CTA pairs (nt = 0), the depth of product i's tiles cut into
-// pair_split[i] parts (`parts` of them in all, `ahead`: see LinLaunch), or in tiles
+// pair_split[i] parts (`parts` of them in all, `ahead`: see LinLaunch) and the last
+// product's last `halves` tiles taken as two halves each, or in tiles
 // of nt rows with the depth split over `split` CTAs and `stages` of operands in
 // flight.  `scratch` bytes of workspace; `cost`, an estimate in cycles.
 struct LinPlan {
   int nt = 0, split = 1, stages = 0;
-  int pair_split[kMaxProducts] = {1, 1}, parts = 0, ahead = 0;
+  int pair_split[kMaxProducts] = {1, 1}, parts = 0, ahead = 0, halves = 0;
   size_t scratch = 0;
   double cost = 0;
 };

@@ -39,7 +39,7 @@ def make(torch, m, n, k, dtype, seed=0, pad=(0, 0)):
 SHAPES = [(1, 1, 1), (1, 128, 64), (2, 129, 63), (3, 4096, 4096), (8, 1000, 520), (16, 640, 16384), (17, 257, 130),
           (33, 96, 1032), (64, 2048, 512), (100, 300, 257), (128, 128, 128), (129, 255, 129), (256, 256, 256),
           (257, 513, 1027), (500, 64, 8192), (1000, 777, 1333), (1024, 2304, 640),
-          (128, 4096, 4096), (300, 1024, 12288), (512, 4096, 16384), (2500, 3001, 500), (5000, 2600, 72)]
+          (128, 4096, 4096), (300, 1024, 12288), (512, 4096, 16384), (2500, 3001, 500), (5000, 2600, 72), (4096, 4096, 200), (5000, 4200, 72)]
 
 
 @pytest.mark.parametrize("shape", SHAPES)

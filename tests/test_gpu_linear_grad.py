@@ -38,7 +38,8 @@ def check(got, dy, x, w, z, name, torch):
 @pytest.mark.parametrize("shape", [(1, 1, 1), (1, 300, 200), (8, 128, 64), (17, 257, 130), (100, 64, 1032), (128, 128, 128),
                                    (129, 255, 129), (256, 256, 256), (300, 1000, 72), (513, 257, 1027),
                                    (5000, 96, 130), (8192, 256, 192), (1000, 1333, 777), (16384, 512, 512),
-                                   (20000, 200, 1000), (40, 2000, 3000), (2304, 1536, 1280)])
+                                   (20000, 200, 1000), (40, 2000, 3000), (2304, 1536, 1280), (2304, 2200, 2304),
+                                   (1000, 2500, 5000)])
 @pytest.mark.parametrize("kind", ["bf16", "f16"])
 def test_shapes(env, shape, kind):
     oz, torch = env
