@@ -135,17 +135,23 @@ __device__ __forceinline__ bool vec_ok(const void* p, int64_t ld, int bytes) {
 // bytes a lane, eight rows at a time, where the whole of them lies inside the matrix
 // and on 16-byte boundaries (`from`, `to`: this lane's place in the first eight rows),
 // else by single values, and what lies past the matrix is not touched.  The fetch is
-// in two halves, so that its loads can be on their way early.
+// in two halves, so that all its loads are on their way before the first is waited for
+// (value by value in turn, 4096×4095 with a residual at a depth of 1024 took 95 µs; so 39).
 struct Fetched {
-  uint4 v[4];
+  uint32_t v[16];
 };
 __device__ __forceinline__ void fetch_begin(const uint16_t* from, int64_t ld, Fetched& f) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) f.v[i] = __ldg(reinterpret_cast<const uint4*>(from + 8 * i * ld));
+  for (int i = 0; i < 4; ++i) {
+    const uint4 v = *reinterpret_cast<const uint4*>(from + 8 * i * ld);
+    f.v[4 * i] = v.x, f.v[4 * i + 1] = v.y, f.v[4 * i + 2] = v.z, f.v[4 * i + 3] = v.w;
+  }
 }
 __device__ __forceinline__ void fetch_end(const Fetched& f, int lane, uint8_t* buf) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) sts128(buf + piece_at(8 * i + (lane >> 2), lane & 3), f.v[i]);
+  for (int i = 0; i < 4; ++i)
+    sts128(buf + piece_at(8 * i + (lane >> 2), lane & 3),
+           make_uint4(f.v[4 * i], f.v[4 * i + 1], f.v[4 * i + 2], f.v[4 * i + 3]));
 }
 __device__ __forceinline__ void store_fast(uint16_t* to, int64_t ld, int lane, const uint8_t* buf) {
 #pragma unroll
@@ -155,13 +161,24 @@ __device__ __forceinline__ void store_fast(uint16_t* to, int64_t ld, int lane, c
 __device__ __forceinline__ uint8_t* value_at(uint8_t* buf, int row, int col) {
   return buf + piece_at(row, col >> 3) + 2 * (col & 7);
 }
-__device__ __noinline__ void fetch_slow(const void* src, int64_t ld, int64_t rows, int64_t cols, int64_t row0,
-                                        int64_t col0, int lane, uint8_t* buf) {
-  const uint16_t* s = static_cast<const uint16_t*>(src) + row0 * ld + col0 + lane;
-  if (col0 + lane >= cols) return;
-#pragma unroll 8
-  for (int r = 0; r < 32; ++r)
-    if (row0 + r < rows) *reinterpret_cast<uint16_t*>(value_at(buf, r, lane)) = __ldg(s + r * ld);
+// Two columns a lane, two rows at a time.
+__device__ __forceinline__ void fetch_begin_slow(const void* src, int64_t ld, int64_t rows, int64_t cols, int64_t row0,
+                                                 int64_t col0, int lane, Fetched& f) {
+  const int64_t row = row0 + (lane >> 4), col = col0 + 2 * (lane & 15);
+  const uint16_t* s = static_cast<const uint16_t*>(src) + row * ld + col;
+  const int n = static_cast<int>(min(int64_t(32), rows - row));  // of these rows, 2·i < n are there
+  const bool one = col < cols, two = col + 1 < cols;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const bool there = 2 * i < n;
+    const uint32_t a = there && one ? s[2 * i * ld] : 0, b = there && two ? s[2 * i * ld + 1] : 0;
+    f.v[i] = a | b << 16;
+  }
+}
+__device__ __forceinline__ void fetch_end_slow(const Fetched& f, int lane, uint8_t* buf) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    *reinterpret_cast<uint32_t*>(value_at(buf, 2 * i + (lane >> 4), 2 * (lane & 15))) = f.v[i];
 }
 __device__ __noinline__ void store_slow(void* dst, int64_t ld, int64_t rows, int64_t cols, int64_t row0, int64_t col0,
                                         int lane, uint8_t* buf) {
@@ -528,6 +545,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
       Fetched r;
       const uint16_t* from = static_cast<const uint16_t*>(ep.add) + lane_row * ep.ld_add + lane_col;
       if (fast_add && add) fetch_begin(from, ep.ld_add, r);
+      if (add && !fast_add) fetch_begin_slow(ep.add, ep.ld_add, x.rows, x.cols, row0, col0, lane, r);
       __syncwarp();
       if (sums) {
         if (!mbar_wait_bounded(acc_full + 8 * acc, accph, kWaitLimit)) ok = false;
@@ -634,7 +652,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
             fetch_end(r, lane, buf);
             if (c + kChunk < cols) fetch_begin(from + c + kChunk, ep.ld_add, r);
           } else {
-            fetch_slow(ep.add, ep.ld_add, x.rows, x.cols, row0, col0 + c, lane, buf);
+            fetch_end_slow(r, lane, buf);
           }
           __syncwarp();
         }
@@ -645,6 +663,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
           case OZ2_ACT_SILU: finish32<OZ2_ACT_SILU>(z, add, bf16, buf, lane); break;
           default: finish32<OZ2_ACT_NONE>(z, add, bf16, buf, lane);
         }
+        if (add && !fast_add && c + kChunk < cols)  // z's registers are free now for its loads
+          fetch_begin_slow(ep.add, ep.ld_add, x.rows, x.cols, row0, col0 + c + kChunk, lane, r);
         __syncwarp();
         if (fast_out) {
           store_fast(static_cast<uint16_t*>(ep.out) + lane_row * ep.ld_out + lane_col + c, ep.ld_out, lane, buf);
@@ -717,10 +737,10 @@ __device__ __forceinline__ void activate8(float (&z)[8]) {
   for (int e = 0; e < 8; ++e) z[e] = activate<ACT>(z[e]);
 }
 
-// Eight 16-bit values of a row of D, from its column col on (n of them there).
+// Eight 16-bit values of a row of R, from its column col on (n of them there).
 __device__ __forceinline__ uint4 load8(const LinUnits& x, const void* src, int64_t ld, int64_t row, int64_t col, int n) {
   const uint16_t* s = static_cast<const uint16_t*>(src);
-  return load16_any(s + row * ld + col, s, s + (x.rows - 1) * ld + x.cols, n);
+  return load16_any<false>(s + row * ld + col, s, s + (x.rows - 1) * ld + x.cols, n);
 }
 __device__ __forceinline__ void store8(void* dst, int64_t ld, int64_t row, int64_t col, int n, const float (&z)[8],
                                        bool bf16) {

@@ -33,8 +33,14 @@ __device__ __forceinline__ float load16(const uint16_t* p, bool bf16) { return u
 // 16 bytes from an address that need not be a multiple of 16: the two 16-byte words
 // that hold them, shifted together.  `base` and `end` bound what may be read; where a
 // word reaches past them, the first n elements (of T) one by one.  Past those n the
-// result is of no meaning.
-template <typename T>
+// result is of no meaning.  FIXED: nothing writes there during the kernel (a residual
+// may be the result's own memory, where each value is read by the thread that then
+// writes it).
+template <bool FIXED, typename T>
+__device__ __forceinline__ T load_global(const T* p) {
+  return FIXED ? __ldg(p) : *p;
+}
+template <bool FIXED = true, typename T>
 __device__ __noinline__ uint4 load16_singly(const T* p, int n) {
   union {
     uint4 v;
@@ -43,7 +49,7 @@ __device__ __noinline__ uint4 load16_singly(const T* p, int n) {
   u.v = make_uint4(0, 0, 0, 0);
 #pragma unroll
   for (int e = 0; e < static_cast<int>(16 / sizeof(T)); ++e)
-    if (e < n) u.e[e] = __ldg(p + e);
+    if (e < n) u.e[e] = load_global<FIXED>(p + e);
   return u.v;
 }
 // The two words, and whether they lie within the bounds; the loads themselves ask for
@@ -55,10 +61,11 @@ __device__ __forceinline__ bool words_inside(const void* p, const void* base, co
   const uintptr_t at = reinterpret_cast<uintptr_t>(p), word = at & ~static_cast<uintptr_t>(15);
   return word >= reinterpret_cast<uintptr_t>(base) && word + (at & 15 ? 32 : 16) <= reinterpret_cast<uintptr_t>(end);
 }
+template <bool FIXED = true>
 __device__ __forceinline__ Words load_words16(const void* p) {
   const uintptr_t at = reinterpret_cast<uintptr_t>(p), word = at & ~static_cast<uintptr_t>(15);
-  return Words{__ldg(reinterpret_cast<const uint4*>(word)),
-               __ldg(reinterpret_cast<const uint4*>(word + (at & 15 ? 16 : 0)))};
+  return Words{load_global<FIXED>(reinterpret_cast<const uint4*>(word)),
+               load_global<FIXED>(reinterpret_cast<const uint4*>(word + (at & 15 ? 16 : 0)))};
 }
 __device__ __forceinline__ uint4 shift_words16(const void* p, const Words& x) {
   const unsigned s = static_cast<unsigned>(reinterpret_cast<uintptr_t>(p) & 15);
@@ -69,9 +76,9 @@ __device__ __forceinline__ uint4 shift_words16(const void* p, const Words& x) {
   return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits),
                     __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
 }
-template <typename T>
+template <bool FIXED = true, typename T>
 __device__ __forceinline__ uint4 load16_any(const T* p, const T* base, const T* end, int n) {
-  return words_inside(p, base, end) ? shift_words16(p, load_words16(p)) : load16_singly(p, n);
+  return words_inside(p, base, end) ? shift_words16(p, load_words16<FIXED>(p)) : load16_singly<FIXED>(p, n);
 }
 
 // --- activations ---------------------------------------------------------------
