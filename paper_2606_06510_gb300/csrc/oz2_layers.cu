@@ -17,6 +17,17 @@ int64_t padded_ld(int64_t cols, int bytes) { return (cols * bytes + 127) / 128 *
 bool on16(const void* p, int64_t ld, int bytes) {
   return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(ld * bytes)) & 15) == 0;
 }
+// Rows on 16-byte boundaries that are not 32-byte ones.  Where both operands' are, TMA's
+// pieces touch a fifth sector each and bound the product (9728×8192² bf16: 965 µs against
+// 701, and 783 with one of them on 32 bytes), and a copy of one of them pays once its
+// bytes, there and back at 6.8 TB/s, and its launch take less than a fifth of the product.
+bool on16_only(const void* p, int64_t ld, int bytes) {
+  return on16(p, ld, bytes) && ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(ld * bytes)) & 16) != 0;
+}
+bool copy_pays(double copied_bytes, double multiplications, int bytes) {
+  const double product_us = multiplications / (bytes == 1 ? 1.9e9 : 0.95e9);
+  return 2 * copied_bytes / 6.8e6 + 3 < 0.2 * product_us;
+}
 bool on(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 int status_of(cudaError_t e) { return e == cudaSuccess ? OZ2_OK : OZ2_ERR_CUDA; }
 
@@ -60,8 +71,8 @@ struct Operand {
   int bytes;
   bool copy;
   size_t off;
-  Operand(const void* src, int64_t ld_src, int64_t r, int64_t c, int b, Workspace& ws)
-      : p(src), ld(r > 1 ? ld_src : padded_ld(c, b)), rows(r), cols(c), bytes(b), copy(!on16(src, ld, b)), off(0) {
+  Operand(const void* src, int64_t ld_src, int64_t r, int64_t c, int b, Workspace& ws, bool must = false)
+      : p(src), ld(r > 1 ? ld_src : padded_ld(c, b)), rows(r), cols(c), bytes(b), copy(must || !on16(src, ld, b)), off(0) {
     if (copy) off = ws.ask(static_cast<size_t>(rows) * padded_ld(cols, bytes) * bytes);
   }
 };
@@ -118,7 +129,10 @@ int oz2_linear(int64_t m, int64_t n, int64_t k, int type, const void* d_X, int64
   p.ep = LinEpilogue{d_x_scale, d_w_scale, d_bias, d_R, d_Z, d_Y, ldr, ldz, ldy, bias_type, out_type, act, 0};
   const LinPlan plan = plan_linear(&p, 1, type);
   Workspace ws(st);
-  Operand X(d_X, ldx, k ? m : 0, k, es, ws), W(d_W, ldw, k ? n : 0, k, es, ws);
+  const double product = static_cast<double>(m) * n * k;
+  const bool one = on16_only(d_X, ldx, es) && on16_only(d_W, ldw, es) &&
+                   copy_pays(static_cast<double>(std::min(m, n)) * k * es, product, es);
+  Operand X(d_X, ldx, k ? m : 0, k, es, ws, one && m <= n), W(d_W, ldw, k ? n : 0, k, es, ws, one && m > n);
   const size_t scratch = ws.ask(plan.scratch);
   if (!ws.take()) return OZ2_ERR_ALLOC;
   const cudaError_t err = place(X, W, ws, st);
@@ -192,8 +206,10 @@ int oz2_linear_grad(int64_t m, int64_t n, int64_t k, int type, const void* d_dY,
     }
   }
   Workspace ws(st);
-  // dZ is dY itself where there is no activation and TMA can read it.
-  const bool own_dz = count && any && (act != OZ2_ACT_NONE || !on16(d_dY, lddy, 2));
+  // dZ is dY itself where there is no activation and TMA can read it (well).
+  const bool slow = on16_only(d_dY, lddy, 2) && ((pdx && on16_only(d_W, ldw, 2)) || (pdw && on16_only(d_X, ldx, 2))) &&
+                    copy_pays(2.0 * m * n, static_cast<double>(count) * m * n * k, 2);
+  const bool own_dz = count && any && (act != OZ2_ACT_NONE || !on16(d_dY, lddy, 2) || slow);
   const int64_t ld_dz = padded_ld(n, 2);
   const size_t dz_off = own_dz ? ws.ask(static_cast<size_t>(m) * ld_dz * 2) : 0;
   const size_t part_off = want_db && m > 0 ? ws.ask(sizeof(float) * static_cast<size_t>(lin_db_chunks(m, n)) * n) : 0;

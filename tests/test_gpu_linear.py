@@ -240,3 +240,26 @@ def test_a_given_stream_owns_the_outputs(env):
     with torch.cuda.stream(s):
         again = [torch.empty(300, 200, dtype=torch.bfloat16, device="cuda") for _ in range(4)]
     assert at in [t.data_ptr() for t in again]
+
+
+@pytest.mark.parametrize("kind, shape", [("bf16", (2000, 5000, 4104)), ("f16", (5000, 2100, 4104)),
+                                         ("e4m3", (4200, 5000, 4112)), ("bf16", (40, 96, 1032))])
+def test_rows_on_16_bytes_only(env, kind, shape):
+    """Both operands' rows on odd multiples of 16 bytes: the larger products copy one
+    of them; either way the bits of the same values on whole lines."""
+    oz, torch = env
+    dt = {"bf16": torch.bfloat16, "f16": torch.float16, "e4m3": torch.float8_e4m3fn}[kind]
+    x, w, xs, ws, _ = make(torch, *shape, dt, seed=12)
+    es = x.element_size()
+
+    def lined(t):
+        """The same values on rows of whole 128-byte lines."""
+        rows = torch.zeros(t.shape[0], -(-t.shape[1] * es // 128) * 128, dtype=torch.uint8, device="cuda")
+        rows[:, :t.shape[1] * es] = t.contiguous().view(torch.uint8)
+        return rows.view(dt)[:, :t.shape[1]]
+
+    assert x.stride(0) * es % 32 == 16 and w.stride(0) * es % 32 == 16
+    want = oz.oz2_linear(lined(x), lined(w), x_scale=xs, w_scale=ws, act="relu")
+    assert torch.equal(oz.oz2_linear(x, w, x_scale=xs, w_scale=ws, act="relu"), want)
+    wy, _, by, _ = ref.linear(x, w, None, "relu", None, xs, ws)
+    ref.close(want, wy, by, shape)

@@ -189,3 +189,25 @@ def test_db_of_many_rows(env):
         d = dy.double()
         ref.close(db, d.sum(0), (m / 8 + 16) * 2.0 ** -23 * d.abs().sum(0), (m, n))
         assert torch.equal(db, oz.oz2_linear_grad(dy, x, w, need=("db",))[2])
+
+
+@pytest.mark.parametrize("shape", [(3400, 2504, 2504), (40, 72, 104)])
+def test_rows_on_16_bytes_only(env, shape):
+    """dY, X and W all on odd multiples of 16 bytes: the larger products take a copy of
+    dY; either way the bits of the same values on whole lines."""
+    oz, torch = env
+    dy, x, w, _ = make(torch, *shape, torch.bfloat16, seed=8)
+
+    def lined(t):
+        return torch.nn.functional.pad(t, (0, -t.shape[1] % 64))[:, :t.shape[1]]
+
+    assert all(t.stride(0) * 2 % 32 == 16 for t in (dy, x, w))
+    want = oz.oz2_linear_grad(lined(dy), lined(x), lined(w))
+    got = oz.oz2_linear_grad(dy, x, w)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    got = oz.oz2_linear_grad(dy, x, w, need=("dx", "dw"))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    (wx, ww, wb), (bx, bw, bb), _ = ref.grad(dy, x, w, None, "none")
+    ref.close(want[0], wx, bx, "dx")
+    ref.close(want[1], ww, bw, "dw")
+    ref.close(want[2], wb, bb, "db")
