@@ -1094,17 +1094,14 @@ int64_t clustered_ctas(int64_t sms, int split, int per_sm) {
 // On pairs: tiles whole, or split depths for the products of few tiles.
 void plan_pairs(const int64_t (&tiles)[kMaxProducts], const int64_t (&steps)[kMaxProducts], int count, double bytes,
                 int64_t pairs, LinPlan* best) {
-  int64_t units = 0;
-  double work = 0, longest = 0;
-  for (int i = 0; i < count; ++i) {
-    const double tile = pair_tile_cycles(steps[i]);
-    units += tiles[i];
-    work += tiles[i] * tile;
-    if (tiles[i]) longest = std::max(longest, tile);
-  }
-  // Rounds of tiles, of the tiles' mean where they differ.
-  best->cost = kPairLaunch + std::max({longest, ceil_div(units, pairs) * (work / units),
-                                       bytes / (kMemoryRate * 2 * std::min(units, pairs))});
+  // Tiles go to the pairs in turn, the first product's first: the pair that takes the most
+  // of those, and the first that takes one fewer.
+  const double t0 = pair_tile_cycles(steps[0]), t1 = pair_tile_cycles(steps[count - 1]);
+  const int64_t units = tiles[0] + (count > 1 ? tiles[1] : 0);
+  const int64_t even = tiles[0] / pairs, odd = tiles[0] % pairs;
+  const double most = (even + (odd > 0)) * t0 + (ceil_div(units, pairs) - even - (odd > 0)) * t1;
+  const double fewer = even * t0 + (ceil_div(units - odd, pairs) - even) * t1;
+  best->cost = kPairLaunch + std::max({most, fewer, bytes / (kMemoryRate * 2 * std::min(units, pairs))});
   // A last round of few tiles: they are taken as halves, by twice as many pairs.
   const int64_t last = units % pairs;
   if (units > pairs && last > 0 && 2 * last <= pairs && last <= tiles[count - 1]) {
