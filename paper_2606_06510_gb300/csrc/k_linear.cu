@@ -350,8 +350,7 @@ struct PairWork {
 // two KB of shared memory that turn a thread's row into 64-byte pieces of eight rows.
 // At a depth of 64, where it is all there is, a round takes 3.4 µs, 10 MB at a fill's
 // rate (relu, silu and gelu_tanh add up to 0.6, gelu 2.5, a residual 2.1, which is
-// memory's): it hides
-// behind the next tile's products from a depth of about 1024 on.
+// memory's): it hides behind the next tile's products from a depth of about 1024 on.
 // ---------------------------------------------------------------------------
 template <int TYPE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
