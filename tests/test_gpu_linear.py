@@ -263,3 +263,20 @@ def test_rows_on_16_bytes_only(env, kind, shape):
     assert torch.equal(oz.oz2_linear(x, w, x_scale=xs, w_scale=ws, act="relu"), want)
     wy, _, by, _ = ref.linear(x, w, None, "relu", None, xs, ws)
     ref.close(want, wy, by, shape)
+
+
+@pytest.mark.parametrize("m, n, k, pad", [(2500, 3001, 200, 0), (2500, 3002, 64, 0), (4099, 2048, 300, 3), (600, 9000, 1024, 1)])
+def test_large_results_in_place_of_unaligned_residuals(env, m, n, k, pad):
+    """Tiles whose residual is fetched value by value, ahead of the stores over it."""
+    oz, torch = env
+    x, w, _, _, normal = make(torch, m, n, k, torch.bfloat16, seed=13)
+    hold = normal(m, n + pad).to(torch.bfloat16)
+    r = hold[:, pad:].clone()
+    y = hold[:, pad:]
+    beside = hold[:, :pad].clone()
+    want, z = oz.oz2_linear(x, w, act="gelu_tanh", residual=r, save_pre=True)
+    oz.oz2_linear(x, w, act="gelu_tanh", residual=y, out=y)
+    assert torch.equal(y, want) and torch.equal(hold[:, :pad], beside)
+    wy, wz, by, bz = ref.linear(x, w, None, "gelu_tanh", r)
+    ref.close(y, wy, by, "y")
+    ref.close(z, wz, bz, "z")
