@@ -200,6 +200,10 @@ bool plan_apart(const LinPlan& together, const LinPlan& a, const LinPlan& b);
 cudaError_t launch_linear(const LinProduct* products, int count, int type, const LinPlan& plan, void* scratch,
                           Oz2Device* dev, cudaStream_t st);
 
+// A product of up to kFewRows rows, both operands K-major and anywhere.
+constexpr int kFewRows = 16;
+cudaError_t launch_linear_rows(const LinProduct& p, int type, cudaStream_t st);
+
 // Rows of elements of `bytes` bytes copied to rows that start on 16-byte
 // boundaries (ld_dst·bytes a multiple of 16), for one or two operands at once.
 struct PackJob {

@@ -127,6 +127,16 @@ int oz2_linear(int64_t m, int64_t n, int64_t k, int type, const void* d_X, int64
   p.cols = n;
   p.depth = k;
   p.ep = LinEpilogue{d_x_scale, d_w_scale, d_bias, d_R, d_Z, d_Y, ldr, ldz, ldy, bias_type, out_type, act, 0};
+  // Few tokens and weights that TMA cannot read: they are read where they lie (8 tokens ×
+  // 10240×7569 bf16 47 µs, 78 with a copy).  Short rows of many weights are left to the
+  // copy (16 tokens × 16384×101: 7 µs, so 14).
+  if (m <= kFewRows && k > 0 && !on16(d_W, ldw, es) && (k * es >= 512 || n <= 4096)) {
+    p.p = d_X;
+    p.ldp = ldx;
+    p.q = d_W;
+    p.ldq = ldw;
+    return status_of(launch_linear_rows(p, type, st));
+  }
   const LinPlan plan = plan_linear(&p, 1, type);
   Workspace ws(st);
   const double product = static_cast<double>(m) * n * k;

@@ -280,3 +280,34 @@ def test_large_results_in_place_of_unaligned_residuals(env, m, n, k, pad):
     wy, wz, by, bz = ref.linear(x, w, None, "gelu_tanh", r)
     ref.close(y, wy, by, "y")
     ref.close(z, wz, bz, "z")
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "e4m3"])
+@pytest.mark.parametrize("m, n, k", [(1, 1, 3), (1, 4096, 4097), (3, 15, 31), (7, 17, 33), (8, 333, 395), (9, 100, 2049),
+                                     (16, 64, 16383), (13, 2001, 1000 + 3), (2, 5000, 257), (16, 16384, 101), (5, 40, 8191)])
+def test_few_tokens_and_unaligned_weights(env, kind, m, n, k):
+    """Weights that are read where they lie: depths that end inside a piece, deep and
+    narrow ones, NaN around the rows, residuals in place."""
+    oz, torch = env
+    dt = {"bf16": torch.bfloat16, "f16": torch.float16, "e4m3": torch.float8_e4m3fn}[kind]
+    out = torch.bfloat16 if kind == "e4m3" else dt
+    x, w, xs, ws, normal = make(torch, m, n, k, dt, seed=14)
+    bias, r = normal(n), normal(m, n).to(out)
+    name = ref.ACTS[(m + n + k) % 5]
+    wy, wz, by, bz = ref.linear(x, w, bias, name, r, xs, ws)
+
+    def inside_nan(t, left):
+        held = torch.full((t.shape[0] + 2, t.shape[1] + left + 2), float("nan"), device="cuda").to(dt)
+        held[1:-1, left:left + t.shape[1]] = t
+        return held[1:-1, left:left + t.shape[1]]
+
+    for left in (0, 1, 5):
+        X, W = inside_nan(x, left), inside_nan(w, left + 1)
+        y, z = oz.oz2_linear(X, W, bias=bias, act=name, residual=r, x_scale=xs, w_scale=ws, save_pre=True)
+        ref.close(y, wy, by, ("y", left))
+        ref.close(z, wz, bz, ("z", left))
+        held = r.clone()
+        oz.oz2_linear(X, W, bias=bias, act=name, residual=held, out=held, x_scale=xs, w_scale=ws)
+        assert torch.equal(held, y)
+        again = oz.oz2_linear(X, W, bias=bias, act=name, residual=r, x_scale=xs, w_scale=ws)
+        assert torch.equal(again, y)
