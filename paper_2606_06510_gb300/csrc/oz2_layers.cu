@@ -107,13 +107,14 @@ int oz2_linear(int64_t m, int64_t n, int64_t k, int type, const void* d_X, int64
   if (m < 0 || n < 0 || k < 0 || !valid_act(act)) return OZ2_ERR_INVALID_ARG;
   if (type != OZ2_TYPE_E4M3 && !is_16bit(type)) return OZ2_ERR_INVALID_ARG;
   if (!is_16bit(out_type) || (is_16bit(type) && out_type != type)) return OZ2_ERR_INVALID_ARG;
-  if (!d_x_scale != !d_w_scale || (d_x_scale && type != OZ2_TYPE_E4M3)) return OZ2_ERR_INVALID_ARG;
+  if ((d_x_scale || d_w_scale) && type != OZ2_TYPE_E4M3) return OZ2_ERR_INVALID_ARG;
   if (d_bias && bias_type != OZ2_TYPE_F32 && bias_type != out_type) return OZ2_ERR_INVALID_ARG;
   if (ldx < std::max<int64_t>(1, k) || ldw < std::max<int64_t>(1, k) || ldy < std::max<int64_t>(1, n) ||
       (d_R && ldr < n) || (d_Z && ldz < n))
     return OZ2_ERR_INVALID_ARG;
   if (m >= kMaxSize || n >= kMaxSize || k >= kMaxSize) return OZ2_ERR_UNSUPPORTED;
-  if (m == 0 || n == 0) return OZ2_OK;
+  if (m == 0 || n == 0) return OZ2_OK;  // (before the pointers: an empty array's, scales' among them, may be null)
+  if (!d_x_scale != !d_w_scale) return OZ2_ERR_INVALID_ARG;
   if (!d_Y || (k > 0 && (!d_X || !d_W))) return OZ2_ERR_INVALID_ARG;
   const int es = type_bytes(type);
   if (!on(d_X, es) || !on(d_W, es) || !on(d_Y, 2) || !on(d_R, 2) || !on(d_Z, 2) ||
