@@ -214,8 +214,11 @@ class AdamWPlan:
         self.param_type = params[0].dtype
         self.args = oz2_adamw_step()
         self.tensors = (oz2_adamw_tensor * count)()
-        self.m, self.v, self.m_scales, self.v_scales = list(m), list(v), m_scales, v_scales
-        self.params, self.masters = list(params), masters
+        # Its own tuples: where a caller's list gets another entry, the tensor whose
+        # address is taken below stays.
+        self.params, self.m, self.v = tuple(params), tuple(m), tuple(v)
+        self.masters, self.m_scales, self.v_scales = (None if t is None else tuple(t)
+                                                      for t in (masters, m_scales, v_scales))
         for i, t in enumerate(self.tensors):
             e = params[i].numel()
             blocks = (e + ADAMW_BLOCK - 1) // ADAMW_BLOCK
