@@ -240,12 +240,15 @@ class AdamWPlan:
         return t.data_ptr() if numel else None
 
     def set_grads(self, grads):
-        """Take other gradients, one for each parameter."""
-        assert len(grads) == len(self.tensors)
-        self.grad_type = grads[0].dtype
-        for t, g in zip(self.tensors, grads):
-            t.grad = self._flat(g, t.numel, self.grad_type, "grads")
-        self.grads = list(grads)
+        """Take other gradients, one for each parameter.  Where one of them is refused,
+        the plan keeps the ones that it had."""
+        grads = tuple(grads)
+        assert len(grads) == len(self.tensors), "one gradient for every parameter"
+        kind = grads[0].dtype
+        at = [self._flat(g, t.numel, kind, "grads") for t, g in zip(self.tensors, grads)]
+        self.grads, self.grad_type = grads, kind
+        for t, a in zip(self.tensors, at):
+            t.grad = a
 
 
 def oz2_adamw_states(params, bits=32):

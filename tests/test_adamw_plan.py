@@ -44,3 +44,54 @@ def test_a_plan_holds_every_tensor_it_was_made_of(bits):
     for (name, i), (ref, address) in seen.items():
         assert ref() is not None, (name, i)
         assert getattr(plan.tensors[i], FIELD[name]) == address == ref().data_ptr(), (name, i)
+
+
+@pytest.mark.parametrize("what", ["type", "size", "count"])
+def test_refused_gradients_change_nothing(what):
+    """The first of the new ones is fit, of another type than the old; a later one is not."""
+    given = lists(32)
+    plan = Plan(**given)
+    before = [t.grad for t in plan.tensors]
+    seen = [weakref.ref(g) for g in given["grads"]]
+    new = [torch.zeros(e) for e in SIZES]
+    if what == "type":
+        new[1] = new[1].bfloat16()
+    elif what == "size":
+        new[1] = new[1][:-1]
+    else:
+        new.pop()
+    with pytest.raises(AssertionError):
+        plan.set_grads(new)
+    del given, new
+    gc.collect()
+    assert plan.grad_type == torch.bfloat16 and [t.grad for t in plan.tensors] == before
+    assert [r().data_ptr() for r in seen] == before
+
+
+def test_other_gradients_are_taken_and_held():
+    plan = Plan(**lists(32))
+    new = [torch.zeros(e) for e in SIZES]
+    seen = [(weakref.ref(g), g.data_ptr()) for g in new]
+    plan.set_grads(new)
+    new.clear()
+    gc.collect()
+    assert plan.grad_type == torch.float32
+    assert [(r().data_ptr(), t.grad) for (r, _), t in zip(seen, plan.tensors)] == [(a, a) for _, a in seen]
+
+
+@pytest.mark.gpu
+def test_a_step_after_refused_gradients():
+    """It runs on the gradients that the plan had."""
+    from helpers import ensure_built
+    ensure_built()
+    out = []
+    for refuse in (False, True):
+        p = [torch.ones(e, device="cuda").bfloat16() for e in SIZES]
+        g = [torch.full((e,), 0.5, device="cuda").bfloat16() for e in SIZES]
+        plan = oz.oz2_adamw_plan(p, g, **oz.oz2_adamw_states(p))
+        if refuse:
+            with pytest.raises(AssertionError):
+                plan.set_grads([torch.full((SIZES[0],), -0.5, device="cuda"), torch.zeros(SIZES[1])])
+        oz.oz2_adamw(plan, step=1, lr=1e-2)
+        out.append(p)
+    assert all(torch.equal(a, b) for a, b in zip(*out))
