@@ -108,9 +108,12 @@ int oz2_linear_grad(int64_t m, int64_t n, int64_t k, int type,
  * seed, step and the value's number: the list's values are numbered through,
  * every tensor starting a new block of 256 (so a step can be repeated bit for
  * bit, and a tensor's place in the list matters).  w is updated from the
- * unrounded m and v.  States of zero bytes with any finite scales are the
- * initial state.  A value that is not finite is kept as E4M3's NaN; the others of its
- * block are not touched by it.
+ * unrounded m and v.  An element whose √v is zero has no history: its m counts as
+ * zero too.  (So it is with elements whose gradients stay some 10^-5 of their
+ * block's largest: √v may be rounded to zero, and their steps are those of single
+ * gradients, up to (1-β1)/√(1-β2) of lr.  Tensors where those matter want 32 bits.)
+ * States of zero bytes with any finite scales are the initial state.  A value that
+ * is not finite is kept as E4M3's NaN; the others of its block are not touched by it.
  *
  * param_type F32, BF16 or F16 (a master wants a 16-bit one); grad_type F32 or
  * param_type.  Errors:

@@ -10,6 +10,12 @@
 // (1-β2) of itself a step would never leave a value whose neighbours are 1/16
 // to 1/8 away.  The update of w itself uses the unrounded m and v.
 //
+// m and √v are rounded each for itself, so an element whose gradients are some 10^-5 of
+// its block's largest may keep an m beside a √v of zero, and the next step, with only the
+// new gradient in √v, would be hundreds of times lr.  A √v of zero is an element without
+// history: its m counts as zero too (four instructions for four elements), and steps stay
+// within what AdamW's are for any gradients.
+//
 // A warp takes 256 values at a time, a lane 4 of each half, so a block's largest
 // magnitude is one warp reduction and every access is 16 (FP32), 8 or 4 bytes a
 // lane, consecutive over the warp.
@@ -147,6 +153,13 @@ __device__ __forceinline__ void decode4(uint32_t w, float* f) {
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(hi) : "h"(static_cast<uint16_t>(w >> 16)));
   const float2 a = unpack16(lo, false), b = unpack16(hi, false);
   f[0] = a.x, f[1] = a.y, f[2] = b.x, f[3] = b.y;
+}
+// Four codes of m, 0 where √v's code is (of either sign): 0x7F and 7 bits carry into
+// a byte's sign unless they are 0, and prmt spreads that sign over the byte.
+__device__ __forceinline__ uint32_t with_history(uint32_t m, uint32_t v) {
+  uint32_t mask;
+  asm("prmt.b32 %0, %1, 0, 0xBA98;" : "=r"(mask) : "r"((v & 0x7F7F7F7Fu) + 0x7F7F7F7Fu));
+  return m & mask;
 }
 // The codes of four values that E4M3 holds exactly (or of NaN).
 __device__ __forceinline__ uint32_t encode4(const float* f) {
@@ -287,7 +300,7 @@ __global__ void __launch_bounds__(32 * kAdamWarps, BITS == 8 ? 6 : 1) adamw_kern
         values4<OZ2_TYPE_F32>(r.m[h], m[h]);
         values4<OZ2_TYPE_F32>(r.v[h], v[h]);
       } else {
-        decode4(r.m[h][0], m[h]);
+        decode4(with_history(r.m[h][0], r.v[h][0]), m[h]);
         decode4(r.v[h][0], v[h]);
       }
 #pragma unroll
