@@ -225,7 +225,7 @@ class AdamWPlan:
             t.numel = e
             t.param = self._flat(params[i], e, self.param_type, "params")
             t.m, t.v = self._flat(m[i], e, state, "m"), self._flat(v[i], e, state, "v")
-            if masters is not None:
+            if masters is not None and masters[i] is not None:
                 t.master = self._flat(masters[i], e, torch.float32, "masters")
             if self.bits == 8:
                 t.m_scale = self._flat(m_scales[i], blocks, torch.float32, "m_scales")
@@ -269,8 +269,8 @@ def oz2_adamw_plan(params, grads, m, v, masters=None, m_scales=None, v_scales=No
     """The handle of a step over these tensors (lists, contiguous): params of one
     dtype (float32, bfloat16, float16), grads of that or float32, states m and v
     float32 or float8_e4m3fn with float32 scales (oz2_adamw_states); masters:
-    float32 weights beside 16-bit params; lr_scales and decay_scales: factors of
-    each tensor's own (0 for no weight decay)."""
+    float32 weights beside 16-bit params, None for a tensor that has none; lr_scales
+    and decay_scales: factors of each tensor's own (0 for no weight decay)."""
     return AdamWPlan(params, grads, m, v, masters, m_scales, v_scales, lr_scales, decay_scales)
 
 

@@ -95,3 +95,34 @@ def test_a_step_after_refused_gradients():
         oz.oz2_adamw(plan, step=1, lr=1e-2)
         out.append(p)
     assert all(torch.equal(a, b) for a, b in zip(*out))
+
+
+def test_masters_for_some_of_the_tensors():
+    given = lists(32)
+    given["masters"][0] = None
+    plan = Plan(**given)
+    assert plan.tensors[0].master is None
+    assert plan.tensors[1].master == given["masters"][1].data_ptr()
+
+
+@pytest.mark.gpu
+def test_steps_with_masters_for_some():
+    """A tensor's step does not depend on whether another has a master."""
+    from helpers import ensure_built
+    ensure_built()
+    out = []
+    for has in ((0, 0), (1, 1), (0, 1), (1, 0)):
+        g = torch.Generator(device="cuda").manual_seed(3)
+        p = [torch.randn(e, generator=g, device="cuda").bfloat16() for e in SIZES]
+        grad = [torch.randn(e, generator=g, device="cuda").bfloat16() for e in SIZES]
+        masters = [t.float() if h else None for t, h in zip(p, has)]
+        plan = oz.oz2_adamw_plan(p, grad, masters=masters, **oz.oz2_adamw_states(p, bits=8))
+        for step in (1, 2):
+            oz.oz2_adamw(plan, step=step, lr=1e-2, seed=4)
+        for t, m in zip(p, masters):
+            assert m is None or torch.equal(t, m.bfloat16())
+        out.append((p, masters))
+    (none, _), (both, masters), (second, m2), (first, m1) = out
+    assert torch.equal(second[0], none[0]) and torch.equal(first[1], none[1])
+    assert torch.equal(second[1], both[1]) and torch.equal(m2[1], masters[1])
+    assert torch.equal(first[0], both[0]) and torch.equal(m1[0], masters[0])
