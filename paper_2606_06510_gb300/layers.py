@@ -113,8 +113,14 @@ def oz2_linear(x, w, bias=None, act="none", residual=None, x_scale=None, w_scale
     the result's dtype or float32, residual the result's.  act: "none", "relu",
     "gelu", "gelu_tanh" or "silu".  With save_pre, returns (y, z) with z the
     activation's argument, which oz2_linear_grad wants.  `out` may be the
-    residual itself.
+    residual itself.  No graph of gradients is recorded: tensors that require them
+    are refused unless that is off (torch.no_grad()).
     """
+    if x.requires_grad or w.requires_grad or (bias is not None and bias.requires_grad) or \
+            (residual is not None and residual.requires_grad) or (x_scale is not None and x_scale.requires_grad) or \
+            (w_scale is not None and w_scale.requires_grad):
+        assert not torch.is_grad_enabled(), "a tensor requires its gradient, which would be lost: call oz2_linear " \
+            "under torch.no_grad(), and oz2_linear_grad for the gradients"
     m, k = x.shape
     n, k2 = w.shape
     xt = dt = x.dtype
