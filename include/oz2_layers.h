@@ -35,7 +35,9 @@ extern "C" {
 typedef enum { OZ2_TYPE_F32 = 0, OZ2_TYPE_BF16 = 1, OZ2_TYPE_F16 = 2, OZ2_TYPE_E4M3 = 3 } oz2_type;
 
 /* act(z): z; max(z, 0); z·Φ(z); z·(1 + tanh(√(2/π)(z + 0.044715 z³)))/2;
- * z/(1 + e^-z). */
+ * z/(1 + e^-z).  In FP32, off by some 2^-19 of the value and 2^-21 of it for each
+ * unit of exp's argument, far into the tails too; a factor of z below 2^-126 counts
+ * as 0. */
 typedef enum {
   OZ2_ACT_NONE = 0,
   OZ2_ACT_RELU = 1,
