@@ -152,7 +152,7 @@ __device__ __forceinline__ float act_slope(float z) {
     return fmaf(z * g * (1.f - g), du2, g);
   }
   if (ACT == OZ2_ACT_SILU) {
-    z = fabsf(z) > 80.f ? copysignf(80.f, z) : z;
+    z = fabsf(z) > 100.f ? copysignf(100.f, z) : z;
     const float g = reciprocal(1.f + exp2_fast(-kLog2E * z));
     return g * fmaf(z, 1.f - g, 1.f);
   }
