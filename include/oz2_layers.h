@@ -117,6 +117,11 @@ int oz2_linear_grad(int64_t m, int64_t n, int64_t k, int type,
  * States of zero bytes with any finite scales are the initial state.  A value that
  * is not finite is kept as E4M3's NaN; the others of its block are not touched by it.
  *
+ * The tensors' addresses and all of `args` but *d_grad_scale go by value: a captured
+ * call is this step again at every replay, with its bias corrections and its random
+ * bits (8-bit states then are not rounded at random from replay to replay).  Training
+ * calls it anew for each step, after the replay of what was captured.
+ *
  * param_type F32, BF16 or F16 (a master wants a 16-bit one); grad_type F32 or
  * param_type.  Errors:
  * OZ2_ERR_INVALID_ARG for null pointers, negative sizes, step < 1, betas

@@ -283,7 +283,10 @@ def oz2_adamw_plan(params, grads, m, v, masters=None, m_scales=None, v_scales=No
 def oz2_adamw(plan: AdamWPlan, step: int, lr: float, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01,
               grad_scale=None, seed=0, stream=None):
     """One AdamW step, in place.  step counts from 1; grad_scale: a float32 CUDA
-    scalar that multiplies the gradients; seed: of the 8-bit states' rounding."""
+    scalar that multiplies the gradients; seed: of the 8-bit states' rounding.
+
+    Captured into a CUDA graph, a replay is the same step again (step, lr and seed as
+    they were; grad_scale is read anew): a training program calls it for each step."""
     a = plan.args
     a.step, a.lr, a.beta1, a.beta2, a.eps, a.weight_decay, a.seed = step, lr, beta1, beta2, eps, weight_decay, seed
     if grad_scale is not None:
