@@ -19,9 +19,15 @@
  * cores' FP32 sums truncate: against 64 bits a sum is low by 1e-9 to 5e-9 of
  * itself for each element summed over, some 2e-5 at 16384, below a 16-bit
  * rounding; it shows in an F32 dW over very many tokens.)  Base addresses
- * are multiples of the element size; leading dimensions are in elements.  Where
- * an operand's base or leading dimension is no multiple of 16 bytes its rows are
- * first copied to ones that are (a pass over that operand, and workspace for it).
+ * are multiples of the element size; leading dimensions are in elements.
+ *
+ * An operand of a product is copied first (a pass over it, and workspace for it)
+ *   - where its base or leading dimension is no multiple of 16 bytes: its rows go to
+ *     ones that are multiples of 128.  But weights off the 16-byte grid are read where
+ *     they lie for up to 16 tokens, without workspace, unless there are over 4096 rows
+ *     of less than 512 bytes;
+ *   - where both operands' rows lie on odd multiples of 16 bytes and the product is so
+ *     long that it pays: the smaller one of oz2_linear's, dY of oz2_linear_grad.
  */
 #ifndef OZ2_LAYERS_H
 #define OZ2_LAYERS_H

@@ -23,7 +23,7 @@
 // With FP32 states memory bounds it: 201 M bf16 parameters with masters and bf16
 // gradients, 28 bytes each, take 814 µs (6.9 TB/s, a plain copy's rate).  With 8-bit
 // states there are 16 bytes and some 100 instructions a parameter (the hash and the two
-// roundings are a third of them): issue bounds it (77% of the slots, integer pipe 58%),
+// roundings are a third of them): issue bounds it (77% of the slots, integer pipe 59%),
 // 648 µs at 5 TB/s.  Loading the next block ahead took it from 1209 to 826 µs, a kernel
 // for each combination of types to 741, packed FP32 instructions and the weights'
 // stores before the rounding, which leave room for six blocks of 128 threads an SM, to
@@ -320,6 +320,7 @@ __global__ void __launch_bounds__(32 * kAdamWarps, BITS == 8 ? 6 : 1) adamw_kern
         vv = Two(__fadd_rn(vb.x(), vc.x()), __fadd_rn(vb.y(), vc.y()));
         const Two root(__fsqrt_rn(vv.x()), __fsqrt_rn(vv.y()));
         const Two den = fma2(root, Two(T.root), Two(T.eps)), p(w[h][e], w[h][e + 1]);
+        // The quotient by rcp.approx, 2^-23 of an update that the weight takes lr of.
         const Two u = mul2(mm, Two(reciprocal(den.x()), reciprocal(den.y())));
         const Two now = fma2(Two(-step), u, fma2(Two(-decay), p, p));
         w[h][e] = now.x(), w[h][e + 1] = now.y();

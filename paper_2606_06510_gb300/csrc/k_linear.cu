@@ -337,9 +337,9 @@ struct PairWork {
 // 64 elements of depth is 512 cycles of MMAs and 32 KB a CTA at 64 bytes a cycle, 247
 // ns at 2.07 GHz; one pair alone takes 262, all 76 together 282 (and the power cap the
 // rest).  So a narrower tile would only load more for its MMAs, and five stages are
-// wanted (four: 339 ns).  4864×4096×4096 bf16, four even rounds of tiles, takes 84 µs
-// (1.94 PFLOP/s); 4096³ 76; 16384²×4096 1.11 ms; E4M3
-// 8192³ 268 µs (4.1 PFLOP/s).  A last round that is at most half full takes its tiles
+// wanted (four: 339 ns).  4864×4096×4096 bf16, four even rounds of tiles, takes 86 µs
+// (1.89 PFLOP/s); 4096³ 78; 16384²×4096 1.12 ms; E4M3 of normal values
+// 8192³ 298 µs (3.7 PFLOP/s).  A last round that is at most half full takes its tiles
 // as halves on twice as many pairs (a half's step, its loads, 390 cycles of 535: 4096³
 // 80 to 76 µs, the gradient of 2504×3008×2048 44 to 39).  Sharing out that round's steps
 // of depth evenly instead (parts of every tile's) won 1% at 4096³ and lost elsewhere: a
@@ -348,8 +348,8 @@ struct PairWork {
 //
 // The epilogue is 16 warps, 32 rows × 64 columns each, in 32-column chunks through
 // two KB of shared memory that turn a thread's row into 64-byte pieces of eight rows.
-// At a depth of 64, where it is all there is, a round takes 3.4 µs, 10 MB at a fill's
-// rate (relu, silu and gelu_tanh add up to 0.6, gelu 2.5, a residual 2.1, which is
+// At a depth of 64, where it is all there is, a round takes 3.5 µs, 10 MB at a fill's
+// rate (relu adds 0.4, silu 1.1, gelu_tanh 1.3, gelu 2.1, a residual 2.1, which is
 // memory's): it hides behind the next tile's products from a depth of about 1024 on.
 // ---------------------------------------------------------------------------
 template <int TYPE>
@@ -696,7 +696,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
 // same bits every time.
 //
 // What bounds it: memory, where the weights stream through (16 tokens × 16384² E4M3
-// 43 µs, 6.2 TB/s; bf16 81 µs, 6.6), else the chain of a launch, its first loads, the
+// 45 µs, 6.0 TB/s; bf16 85 µs, 6.3), else the chain of a launch, its first loads, the
 // MMAs, the parts' exchange and the stores: 1 × 512 × 512 takes 3.7 µs, one token × 4096²
 // bf16 9.1 (34 MB in 128 CTAs), 256³ 3.7, 1024×2048×2048 12.6.  A thread's columns of the
 // tile are the same for every row it finishes, so biases and scales are in registers

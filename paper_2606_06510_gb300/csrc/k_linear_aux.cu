@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(256) pack_rows_kernel(PackJob a, PackJob b) {
 // with one the load-work-store chain of three blocks an SM (4096² gelu_tanh: 101 MB in
 // 19 µs; exp and erf by their slow functions it was 62).  Rows off the 16-byte grid
 // are put together from two aligned loads each, all of a round's under way at once:
-// 2500×3001 gelu 16 µs (27 when each row's bounds were asked before its loads).
+// 2500×3001 gelu 17 µs (27 when each row's bounds were asked before its loads).
 // ---------------------------------------------------------------------------
 constexpr int kGradCols = 256, kGradWarps = 8, kGradBlocks = 3;  // blocks an SM
 
