@@ -189,7 +189,7 @@ def prepare(case, seed):
         s["teacher"] = (12 + 2 * torch.randn((m, top), generator=gen, device="cuda")).sort(dim=1, descending=True)[0]
     if c["grad"]:  # what the forward pass kept, and the mean's gradient (scaled, as 16-bit floats want it)
         z = _logits(s)
-        s["lse"], s["picked"] = _lse(z), _picked(s, z)
+        s["lse"] = _lse(z)
         scale = 1024.0 if c["type"] == "f16" else 1.0
         s["dloss"] = scale / m * (0.5 + torch.rand(m, generator=gen, device="cuda"))
     return s
@@ -323,11 +323,11 @@ def _own(s):
     if c["op"] == "xent":
         if not c["grad"]:
             return list(oz.oz2_linear_xent(s["x"], s["w"], s["targets"], scale=c["scale"], z_loss=c["z_loss"]))
-        return list(oz.oz2_linear_xent_grad(s["dloss"], s["x"], s["w"], s["targets"], s["lse"], s["picked"],
-                                            scale=c["scale"], z_loss=c["z_loss"]))
+        return list(oz.oz2_linear_xent_grad(s["dloss"], s["x"], s["w"], s["targets"], s["lse"], scale=c["scale"],
+                                            z_loss=c["z_loss"]))
     if not c["grad"]:
         return list(oz.oz2_linear_distill(s["x"], s["w"], s["ids"], s["teacher"], temperature=c["temperature"]))
-    return list(oz.oz2_linear_distill_grad(s["dloss"], s["x"], s["w"], s["ids"], s["teacher"], s["lse"], s["picked"],
+    return list(oz.oz2_linear_distill_grad(s["dloss"], s["x"], s["w"], s["ids"], s["teacher"], s["lse"],
                                            temperature=c["temperature"]))
 
 
