@@ -172,9 +172,10 @@ struct LinEpilogue {
   void* out;               // D
   int64_t ld_add, ld_pre, ld_out;
   int bias_type;           // oz2_type
-  int out_type;            // oz2_type: 16-bit, or F32 (then nothing but `accumulate` applies)
+  int out_type;            // oz2_type: 16-bit, or F32 (then nothing but `accumulate` and `factor` applies)
   int act;                 // oz2_act
   int accumulate;          // F32 out: D += P·Qᵀ
+  const float* factor;     // of the sums, on the device, or null: 1
 };
 struct LinProduct {
   int64_t rows, cols;
