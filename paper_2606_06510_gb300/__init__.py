@@ -15,9 +15,11 @@ import os
 
 import torch
 
-from . import layers
+from . import layers, lm
 from .layers import (AdamWPlan, oz2_adamw, oz2_adamw_plan, oz2_adamw_states, oz2_linear,  # noqa: F401
                      oz2_linear_grad)
+from .lm import (oz2_embedding, oz2_embedding_grad, oz2_layer_norm, oz2_layer_norm_grad,  # noqa: F401
+                 oz2_linear_distill, oz2_linear_distill_grad, oz2_linear_xent, oz2_linear_xent_grad)
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liboz2.so")
@@ -87,6 +89,7 @@ _SIGS = {
     "oz2_fallback": (_I, [_I64, _I64, _I64, _P, _I64, _P, _I64, _P, _P, _P, _I64, _P]),
     "oz2_native_dgemm": (_I, [_I64, _I64, _I64, _P, _I64, _P, _I64, _P, _I64, _P]),
     **layers.SIGS,
+    **lm.SIGS,
 }
 _LIB = None
 

@@ -1,0 +1,531 @@
+// Embedding: rows of a table by tokens, and the table's gradient by sorted tokens.
+//
+//   forward    Y_t = s·E[id_t]           id < 0: zeros; id ≥ n: NaN
+//   gradient   dE_j = s·Σ_{t: id_t = j} dY_t, or added to dE; ids outside [0, n) have no
+//              row and count for nothing
+#include <algorithm>
+
+#include "lm_common.cuh"
+
+namespace oz2 {
+namespace {
+
+// ---------------------------------------------------------------------------
+// Forward: a thread takes 16-byte pieces of the result, one grid's stride apart; its
+// row and place in it are found by one division and carried on.  The id is read, then
+// the piece: kAhead of these chains are under way at once.
+// ---------------------------------------------------------------------------
+constexpr int kAhead = 4, kBlocks = 8;  // pieces of a thread at once, blocks an SM
+
+template <int TYPE, bool ALIGNED>
+__global__ void __launch_bounds__(256)
+    embedding_kernel(int64_t m, int64_t n, int64_t k, Ids ids, const void* E, int64_t lde, float scale, void* Y, int64_t ldy) {
+  using X = Elem<TYPE>;
+  using T = typename X::T;
+  pdl_trigger();
+  pdl_wait();
+  const T* src = static_cast<const T*>(E);
+  const T* end = src + (n - 1) * lde + k;
+  T* dst = static_cast<T*>(Y);
+  const uint32_t per = static_cast<uint32_t>((k + X::V - 1) / X::V);
+  const uint32_t first = blockIdx.x * blockDim.x + threadIdx.x, stride = gridDim.x * blockDim.x;
+  const uint32_t stride_rows = stride / per, stride_pieces = stride - stride_rows * per;
+  int64_t r = first / per;
+  uint32_t c = first - static_cast<uint32_t>(r) * per;
+  while (r < m) {
+    int64_t row[kAhead], id[kAhead];
+    int col[kAhead];
+    uint4 v[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      row[j] = r;
+      col[j] = static_cast<int>(c) * X::V;
+      id[j] = r < m ? ids[r] : -1;
+      r += stride_rows;
+      c += stride_pieces;
+      if (c >= per) c -= per, ++r;
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      v[j] = make_uint4(0, 0, 0, 0);
+      if (id[j] >= 0 && id[j] < n)
+        v[j] = load_piece<ALIGNED>(src + id[j] * lde + col[j], src, end, static_cast<int>(min(int64_t(X::V), k - col[j])));
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (row[j] >= m) continue;
+      float f[X::V];
+      X::unpack(v[j], f);
+#pragma unroll
+      for (int e = 0; e < X::V; ++e) f[e] = id[j] >= n ? __int_as_float(0x7FC00000) : f[e] * scale;
+      const int there = static_cast<int>(min(int64_t(X::V), k - col[j]));
+      store16_any(dst + row[j] * ldy + col[j], X::pack(f), there, ALIGNED && there == X::V);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The gradient's tokens in the order of their rows: (row, token) pairs, sorted by row
+// and within a row by token, rows that are not there (as n) last.  A radix sort of the
+// rows' bits, up to 9 at a time, by one cluster: each warp has a stretch of the tokens,
+// counts its digits in shared memory, and after the counts have been summed over warps
+// and blocks (by distributed shared memory) gives each pair its place, which depends on
+// the order of the pairs alone.  The other blocks of the launch write the zeros of a
+// gradient that is not added to meanwhile.
+// ---------------------------------------------------------------------------
+constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kDigitBits = 9, kDigits = 1 << kDigitBits;
+constexpr int kSortCluster = 8;
+constexpr int kSortSmem = (kSortWarps + 2) * kDigits * 4;
+
+struct SortJob {
+  Ids ids;
+  int64_t m;
+  uint32_t n;
+  int passes, bits;    // of `bits` bits each
+  uint2 *a, *b;        // the passes write a, b, a, ...
+  int* long_runs;      // a counter that is set to zero
+};
+struct FillJob {       // `rows` rows of `bytes` bytes, `ld` bytes apart (one row: all of it)
+  char* p;
+  int64_t rows, bytes, ld;
+  int unit;            // bytes of an element
+};
+
+// A row's zeros: 16 bytes a lane from its first boundary on, elements before and after.
+__device__ __forceinline__ void zero_row(char* p, int64_t bytes, int unit, int64_t first, int64_t stride) {
+  int64_t head = static_cast<int64_t>(-reinterpret_cast<uintptr_t>(p) & 15);
+  head = head < bytes ? head : bytes;
+  const int64_t words = (bytes - head) >> 4, tail = head + 16 * words;
+  for (int64_t i = first; i < words; i += stride) reinterpret_cast<uint4*>(p + head)[i] = make_uint4(0, 0, 0, 0);
+  for (int64_t i = first * unit; i < head; i += stride * unit)
+    for (int b = 0; b < unit; b += 2) *reinterpret_cast<uint16_t*>(p + i + b) = 0;
+  for (int64_t i = tail + first * unit; i < bytes; i += stride * unit)
+    for (int b = 0; b < unit; b += 2) *reinterpret_cast<uint16_t*>(p + i + b) = 0;
+}
+
+__global__ void __launch_bounds__(kSortThreads, 1) sort_tokens_kernel(SortJob s, FillJob f, int sorters) {
+  extern __shared__ uint32_t sort_smem[];
+  pdl_trigger();
+  pdl_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (static_cast<int>(blockIdx.x) >= sorters) {
+    const int64_t blocks = gridDim.x - sorters, block = blockIdx.x - sorters;
+    if (f.rows == 1) {
+      zero_row(f.p, f.bytes, f.unit, block * kSortThreads + threadIdx.x, blocks * kSortThreads);
+    } else {
+      for (int64_t r = block * kSortWarps + warp; r < f.rows; r += blocks * kSortWarps)
+        zero_row(f.p + r * f.ld, f.bytes, f.unit, lane, 32);
+    }
+    return;
+  }
+  uint32_t* mine = sort_smem + warp * kDigits;             // this warp's counts, then its next places
+  uint32_t* total = sort_smem + kSortWarps * kDigits;      // the block's
+  uint32_t* scan = total + kDigits;
+  const uint32_t rank = sorters > 1 ? cluster_ctarank() : 0, blocks = sorters;
+  if (rank == 0 && threadIdx.x == 0) *s.long_runs = 0;
+  const int64_t each = ((s.m + blocks * kSortWarps - 1) / (blocks * kSortWarps) + 31) / 32 * 32;
+  const int64_t i0 = min(s.m, (static_cast<int64_t>(rank) * kSortWarps + warp) * each), i1 = min(s.m, i0 + each);
+  const int digits = 1 << s.bits;
+  uint2 *from = s.b, *to = s.a;
+  for (int pass = 0; pass < s.passes; ++pass) {
+    const int shift = pass * s.bits;
+    auto pair = [&](int64_t i) {
+      if (pass) return __ldcg(from + i);
+      const int64_t id = s.ids[i];
+      return make_uint2(id < 0 || id >= s.n ? s.n : static_cast<uint32_t>(id), static_cast<uint32_t>(i));
+    };
+    for (int d = lane; d < digits; d += 32) mine[d] = 0;
+    __syncwarp();
+#pragma unroll 4
+    for (int64_t i = i0 + lane; i < i1; i += 32) atomicAdd(mine + (pair(i).x >> shift & (digits - 1)), 1u);
+    __syncthreads();
+    // Places: of the pairs of smaller digits, of the blocks before, of the warps before.
+    const int d = threadIdx.x;
+    uint32_t sum = 0;
+    if (d < digits) {
+#pragma unroll 8
+      for (int w = 0; w < kSortWarps; ++w) {
+        const uint32_t c = sort_smem[w * kDigits + d];
+        sort_smem[w * kDigits + d] = sum;
+        sum += c;
+      }
+      total[d] = sum;
+    }
+    uint32_t before = 0, all = sum;
+    if (blocks > 1) {
+      cluster_sync_all();
+      if (d < digits) {
+        all = 0;
+        for (uint32_t b = 0; b < blocks; ++b) {
+          uint32_t v;
+          asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(mapa_shared(smem_u32(total + d), b)));
+          if (b < rank) before += v;
+          all += v;
+        }
+      }
+    }
+    // Exclusive sums over the digits.
+    uint32_t inc = d < digits ? all : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t v = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += v;
+    }
+    if (lane == 31) scan[warp] = inc;
+    __syncthreads();
+    if (warp == 0) {
+      uint32_t v = scan[lane], t = v;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t u = __shfl_up_sync(0xffffffffu, t, o);
+        if (lane >= o) t += u;
+      }
+      scan[lane] = t - v;
+    }
+    __syncthreads();
+    if (d < digits) {
+      const uint32_t base = scan[warp] + inc - all + before;
+#pragma unroll 8
+      for (int w = 0; w < kSortWarps; ++w) sort_smem[w * kDigits + d] += base;
+    }
+    __syncthreads();
+    for (int64_t i = i0; i < i1; i += 32) {
+      const bool there = i + lane < i1;
+      const uint2 p = there ? pair(i + lane) : make_uint2(0, 0);
+      const uint32_t digit = there ? p.x >> shift & (digits - 1) : kDigits + lane;
+      const uint32_t same = __match_any_sync(0xffffffffu, digit);
+      const uint32_t at = there ? mine[digit] : 0;
+      __syncwarp();
+      if (there) {
+        const int ahead = __popc(same & ((1u << lane) - 1));
+        if (ahead == 0) mine[digit] = at + __popc(same);
+        __stcg(to + at + ahead, p);
+      }
+      __syncwarp();
+    }
+    uint2* t = from;
+    from = to;
+    to = t;
+    // (The pairs are read by other blocks, and the counts are set to zero.)
+    if (blocks > 1) {
+      __threadfence();
+      cluster_sync_all();
+    } else {
+      __syncthreads();
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The sums over runs of equal rows.  A warp takes the runs that start in a chunk of 16
+// sorted pairs, 512 bytes of the rows (a lane 16).  Runs of more than 32 pairs are cut
+// at the chunks' ends: what of one lies in a chunk is summed into the chunk's FP32
+// rows `parts` (its first one for a run that started before, its second for one that
+// starts here), and join_runs_kernel adds those up in order.  So the work of a warp is
+// bounded, however often a row is named, and every sum has one order.
+// ---------------------------------------------------------------------------
+constexpr int kChunkPairs = 16, kLongRun = 32, kSumWarps = 8;
+
+// The rows around a chunk: the 32 pairs before it and the 64 from its first on.
+struct Window {
+  uint32_t before, a, b;  // rows (n where there is no pair)
+  uint32_t ta, tb;        // tokens
+  __device__ __forceinline__ void load(const uint2* sorted, int64_t m, uint32_t n, int64_t p0, int lane) {
+    const int64_t p = p0 - 32 + lane;
+    before = p >= 0 ? __ldg(&sorted[p].x) : 0xFFFFFFFFu;
+    const uint2 none = make_uint2(n, 0), u = p0 + lane < m ? __ldg(sorted + p0 + lane) : none,
+                v = p0 + 32 + lane < m ? __ldg(sorted + p0 + 32 + lane) : none;
+    a = u.x, ta = u.y, b = v.x, tb = v.y;
+  }
+  __device__ __forceinline__ uint32_t row(int i) const { return __shfl_sync(0xffffffffu, a, i); }  // i < 32
+  // Pairs of row r from place i on (of which it holds).
+  __device__ __forceinline__ int count(uint32_t r, int i) const {
+    return __popc(__ballot_sync(0xffffffffu, a == r) >> i) + __popc(__ballot_sync(0xffffffffu, b == r));
+  }
+  // Pairs of row r directly before the chunk (32: or more).
+  __device__ __forceinline__ int behind(uint32_t r) const {
+    const uint32_t other = ~__ballot_sync(0xffffffffu, before == r);
+    return __clz(static_cast<int>(other));
+  }
+  __device__ __forceinline__ uint32_t token(int i) const {
+    const uint32_t x = __shfl_sync(0xffffffffu, ta, i & 31), y = __shfl_sync(0xffffffffu, tb, i & 31);
+    return i < 32 ? x : y;
+  }
+};
+
+template <int TYPE, int OUT>
+__device__ __forceinline__ void finish_row(void* dE, int64_t row, int64_t ldde, int64_t col, int n, float scale,
+                                           bool accumulate, bool vec, float (&s)[Elem<TYPE>::V]) {
+  constexpr int V = Elem<TYPE>::V;
+#pragma unroll
+  for (int e = 0; e < V; ++e) s[e] *= scale;
+  if constexpr (OUT == TYPE) {
+    using X = Elem<TYPE>;
+    typename X::T* p = static_cast<typename X::T*>(dE) + row * ldde + col;
+    if (accumulate) {
+      float o[V];
+      X::unpack(vec && n >= V ? *reinterpret_cast<const uint4*>(p) : load16_singly<false>(p, n), o);
+#pragma unroll
+      for (int e = 0; e < V; ++e) s[e] += o[e];
+    }
+    store16_any(p, X::pack(s), n, vec && n >= V);
+  } else {  // F32 from 16 bits
+    float* p = static_cast<float*>(dE) + row * ldde + col;
+    if (vec && n >= V) {
+#pragma unroll
+      for (int h = 0; h < V; h += 4) {
+        float4 o = accumulate ? *reinterpret_cast<const float4*>(p + h) : make_float4(0, 0, 0, 0);
+        o.x += s[h], o.y += s[h + 1], o.z += s[h + 2], o.w += s[h + 3];
+        *reinterpret_cast<float4*>(p + h) = o;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (e < n) p[e] = accumulate ? p[e] + s[e] : s[e];
+    }
+  }
+}
+
+struct SumJob {
+  int64_t m, k;
+  uint32_t n;
+  const void* dY;
+  int64_t lddy;
+  void* dE;
+  int64_t ldde;
+  float scale;
+  int accumulate, vec;     // vec: dE's rows are on 16-byte boundaries
+  const uint2* sorted;
+  float* parts;            // two rows a chunk, `slices` pieces of 32 lanes' values each
+  int2* runs;              // long runs: first chunk, and how many chunks
+  int* long_runs;
+  int slices;
+};
+
+template <int TYPE, int OUT, bool ALIGNED>
+__global__ void __launch_bounds__(32 * kSumWarps) sum_runs_kernel(SumJob j) {
+  using X = Elem<TYPE>;
+  using T = typename X::T;
+  constexpr int V = X::V;
+  pdl_trigger();
+  pdl_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t unit = static_cast<int64_t>(blockIdx.x) * kSumWarps + warp, chunk = unit / j.slices;
+  const int slice = static_cast<int>(unit - chunk * j.slices);
+  const int64_t p0 = chunk * kChunkPairs;
+  if (p0 >= j.m) return;
+  Window w;
+  w.load(j.sorted, j.m, j.n, p0, lane);
+  const int64_t col = (static_cast<int64_t>(slice) * 32 + lane) * V;
+  const int n = static_cast<int>(max(int64_t(0), min(int64_t(V), j.k - col)));
+  const T* src = static_cast<const T*>(j.dY);
+  const T* end = src + (j.m - 1) * j.lddy + j.k;
+  float s[V];
+  auto add = [&](int from, int to) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) s[e] = 0.f;
+    for (; from < to; from += 8) {
+      uint4 v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int64_t t = w.token(min(from + i, to - 1));
+        v[i] = make_uint4(0, 0, 0, 0);
+        if (from + i < to && n > 0) v[i] = load_piece<ALIGNED>(src + t * j.lddy + col, src, end, n);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float f[V];
+        X::unpack(v[i], f);
+        if (from + i < to) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) s[e] += f[e];
+        }
+      }
+    }
+  };
+  auto keep = [&](int which) {
+    float* p = j.parts + ((2 * chunk + which) * j.slices + slice) * (32 * V) + lane * V;
+#pragma unroll
+    for (int h = 0; h < V; h += 4) *reinterpret_cast<float4*>(p + h) = make_float4(s[h], s[h + 1], s[h + 2], s[h + 3]);
+  };
+  int i = 0;
+  uint32_t r = w.row(0);
+  if (r >= j.n) return;
+  const int behind = w.behind(r);
+  if (behind) {  // a run that started before: another warp's, or a part of a long one
+    const int here = w.count(r, 0);
+    if (behind + here > kLongRun) {
+      add(0, min(here, kChunkPairs));
+      keep(0);
+    }
+    i = here;
+  }
+  while (i < kChunkPairs) {
+    r = w.row(i);
+    if (r >= j.n) return;
+    const int here = w.count(r, i);
+    if (here > kLongRun) {
+      add(i, kChunkPairs);
+      keep(1);
+      if (slice == 0) {  // how many chunks it reaches: those whose first pair is its
+        int64_t c = chunk + 1;
+        for (;;) {
+          const int64_t p = (c + lane) * kChunkPairs;
+          const uint32_t in = __ballot_sync(0xffffffffu, p < j.m && __ldg(&j.sorted[p < j.m ? p : 0].x) == r);
+          c += __popc(in);
+          if (in != 0xFFFFFFFFu) break;
+        }
+        if (lane == 0) j.runs[atomicAdd(j.long_runs, 1)] = make_int2(static_cast<int>(chunk), static_cast<int>(c - chunk));
+      }
+      return;
+    }
+    add(i, i + here);
+    if (n > 0) finish_row<TYPE, OUT>(j.dE, r, j.ldde, col, n, j.scale, j.accumulate, j.vec, s);
+    i += here;
+  }
+}
+
+// The parts of a long run, 512 bytes' worth of its columns to a block: each warp adds up
+// a stretch of them, and the warps' sums are added in order.
+template <int TYPE, int OUT>
+__global__ void __launch_bounds__(32 * kSumWarps) join_runs_kernel(SumJob j) {
+  constexpr int V = Elem<TYPE>::V;
+  __shared__ float sums[kSumWarps][32 * V];
+  pdl_trigger();
+  pdl_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t units = static_cast<int64_t>(*j.long_runs) * j.slices;
+  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+    const int run = static_cast<int>(u / j.slices), slice = static_cast<int>(u - static_cast<int64_t>(run) * j.slices);
+    const int64_t chunk = j.runs[run].x;
+    const int chunks = j.runs[run].y, each = (chunks + kSumWarps - 1) / kSumWarps;
+    const int c0 = min(chunks, warp * each), c1 = min(chunks, c0 + each);
+    float s[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) s[e] = 0.f;
+#pragma unroll 4
+    for (int c = c0; c < c1; ++c) {
+      const float* p = j.parts + ((2 * (chunk + c) + (c == 0)) * j.slices + slice) * (32 * V) + lane * V;
+#pragma unroll
+      for (int h = 0; h < V; h += 4) {
+        const float4 v = *reinterpret_cast<const float4*>(p + h);
+        s[h] += v.x, s[h + 1] += v.y, s[h + 2] += v.z, s[h + 3] += v.w;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < V; ++e) sums[warp][lane * V + e] = s[e];
+    __syncthreads();
+    if (warp == 0) {
+      for (int o = 1; o < kSumWarps; ++o)
+#pragma unroll
+        for (int e = 0; e < V; ++e) s[e] += sums[o][lane * V + e];
+      const int64_t col = (static_cast<int64_t>(slice) * 32 + lane) * V;
+      const int n = static_cast<int>(max(int64_t(0), min(int64_t(V), j.k - col)));
+      const uint32_t r = j.sorted[(chunk + 1) * kChunkPairs - 1].x;  // the chunk's last pair is the run's
+      if (n > 0) finish_row<TYPE, OUT>(j.dE, r, j.ldde, col, n, j.scale, j.accumulate, j.vec, s);
+    }
+  }
+}
+
+int64_t slices_of(int64_t k, int type) { return (k * type_bytes(type) + 511) / 512; }
+int64_t chunks_of(int64_t m) { return (m + kChunkPairs - 1) / kChunkPairs; }
+size_t up(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
+
+template <int TYPE>
+cudaError_t launch_sums(const SumJob& j, int de_type, cudaStream_t st) {
+  const bool aligned = rows_on16(j.dY, j.lddy, type_bytes(TYPE));
+  const int64_t blocks = (chunks_of(j.m) * j.slices + kSumWarps - 1) / kSumWarps;
+  if (blocks > 0x7FFFFFFF) return cudaErrorInvalidValue;
+  constexpr int F32 = OZ2_TYPE_F32;
+  const bool same = de_type == TYPE;
+  auto sum = same ? (aligned ? sum_runs_kernel<TYPE, TYPE, true> : sum_runs_kernel<TYPE, TYPE, false>)
+                  : (aligned ? sum_runs_kernel<TYPE, F32, true> : sum_runs_kernel<TYPE, F32, false>);
+  count_launch();
+  cudaError_t err = launch_dependent(sum, dim3(static_cast<unsigned>(blocks)), dim3(32 * kSumWarps), 0, st, j);
+  if (err != cudaSuccess || j.m <= kLongRun) return err;
+  const int64_t most = j.m / (kLongRun + 1) * j.slices;
+  count_launch();
+  return launch_dependent(same ? join_runs_kernel<TYPE, TYPE> : join_runs_kernel<TYPE, F32>,
+                          dim3(static_cast<unsigned>(std::min<int64_t>(most, 4 * num_sms()))), dim3(32 * kSumWarps), 0, st, j);
+}
+
+}  // namespace
+
+cudaError_t launch_embedding(int64_t m, int64_t n, int64_t k, int type, Ids ids, const void* E, int64_t lde, float scale,
+                             void* Y, int64_t ldy, cudaStream_t st) {
+  const int es = type_bytes(type);
+  const bool aligned = rows_on16(E, lde, es) && rows_on16(Y, ldy, es);
+  const int64_t per = (k * es + 15) / 16;
+  // (A grid's stride in pieces is below 2^20, so pieces count in 32 bits within a row.)
+  const int64_t blocks = std::min<int64_t>((m * per + 255) / 256, kBlocks * static_cast<int64_t>(num_sms()));
+  auto kern = type == OZ2_TYPE_F32    ? (aligned ? embedding_kernel<OZ2_TYPE_F32, true> : embedding_kernel<OZ2_TYPE_F32, false>)
+              : type == OZ2_TYPE_BF16 ? (aligned ? embedding_kernel<OZ2_TYPE_BF16, true> : embedding_kernel<OZ2_TYPE_BF16, false>)
+                                      : (aligned ? embedding_kernel<OZ2_TYPE_F16, true> : embedding_kernel<OZ2_TYPE_F16, false>);
+  count_launch();
+  return launch_dependent(kern, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, st, m, n, k, ids, E, lde, scale, Y, ldy);
+}
+
+size_t embedding_grad_scratch(int64_t m, int64_t k, int type) {
+  const size_t chunks = static_cast<size_t>(chunks_of(m));
+  const size_t values = 512 / type_bytes(type);  // of a slice
+  return 2 * up(sizeof(uint2) * m) + up(sizeof(int2) * (m / (kLongRun + 1) + 1)) + 256 +
+         up(m > kLongRun ? sizeof(float) * 2 * chunks * slices_of(k, type) * values : 0);
+}
+
+cudaError_t launch_embedding_grad(int64_t m, int64_t n, int64_t k, int type, const void* dY, int64_t lddy, Ids ids,
+                                  float scale, void* dE, int64_t ldde, int de_type, bool accumulate, void* scratch,
+                                  cudaStream_t st) {
+  char* at = static_cast<char*>(scratch);
+  auto take = [&](size_t bytes) {
+    char* p = at;
+    at += up(bytes);
+    return p;
+  };
+  uint2* a = reinterpret_cast<uint2*>(take(sizeof(uint2) * m));
+  uint2* b = reinterpret_cast<uint2*>(take(sizeof(uint2) * m));
+  int2* runs = reinterpret_cast<int2*>(take(sizeof(int2) * (m / (kLongRun + 1) + 1)));
+  int* long_runs = reinterpret_cast<int*>(take(256));
+  float* parts = reinterpret_cast<float*>(at);
+  int bits = 1;
+  while (n >> bits) ++bits;  // of the rows 0 to n
+  const int passes = (bits + kDigitBits - 1) / kDigitBits;
+  SortJob s{ids, m, static_cast<uint32_t>(n), passes, (bits + passes - 1) / passes, a, b, long_runs};
+  const int es = type_bytes(de_type);
+  FillJob f{static_cast<char*>(dE), 0, 0, 0, es};
+  if (!accumulate) {
+    const bool whole = ldde == k || n == 1;
+    f.rows = whole ? 1 : n;
+    f.bytes = (whole ? n : 1) * k * es;
+    f.ld = ldde * es;
+  }
+  const int sorters = m > 2048 ? kSortCluster : 1;
+  const int64_t fillers = accumulate ? 0 : std::min<int64_t>(n * k * es / (64 * kSortThreads) + 1, num_sms());
+  const int64_t blocks = sorters + (fillers + sorters - 1) / sorters * sorters;
+  cudaError_t err = allow_smem(reinterpret_cast<const void*>(sort_tokens_kernel), kSortSmem);
+  if (err != cudaSuccess) return err;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+  cfg.blockDim = dim3(kSortThreads);
+  cfg.dynamicSmemBytes = kSortSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = static_cast<unsigned>(sorters);
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  count_launch();
+  err = cudaLaunchKernelEx(&cfg, sort_tokens_kernel, s, f, sorters);
+  if (err != cudaSuccess) return err;
+  SumJob j{m, k, static_cast<uint32_t>(n), dY, lddy, dE, ldde, scale, accumulate, rows_on16(dE, ldde, es),
+           passes & 1 ? a : b, parts, runs, long_runs, static_cast<int>(slices_of(k, type))};
+  return type == OZ2_TYPE_F32    ? launch_sums<OZ2_TYPE_F32>(j, de_type, st)
+         : type == OZ2_TYPE_BF16 ? launch_sums<OZ2_TYPE_BF16>(j, de_type, st)
+                                 : launch_sums<OZ2_TYPE_F16>(j, de_type, st);
+}
+
+}  // namespace oz2

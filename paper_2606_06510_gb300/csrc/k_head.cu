@@ -1,0 +1,666 @@
+// Losses over a vocabulary from the last layer's input x and the head's weights w,
+// without keeping the logits z = scale·x·wᵀ:
+//
+//   forward    per token the sum of exponentials and its targets' logits
+//   gradient   dz = a·((1 + e)·exp(z - lse) - weights of its targets), z formed again;
+//              dx = dz·w and dw = dzᵀ·x are k_linear.cu's products
+//
+// A hard target has the weight 1, a teacher's listed rows the softmax of its logits.
+#include <algorithm>
+
+#include "lin_mma.cuh"
+#include "lm_common.cuh"
+
+namespace oz2 {
+namespace {
+
+constexpr int kEpiWarps = 16;
+constexpr int kThreads = 64 + 32 * kEpiWarps;  // TMA warp, MMA warp, epilogue warps
+constexpr int kStages = 5;
+constexpr int kTile = 256;                     // tokens and vocabulary rows of a CTA pair's tile
+constexpr int kStage = 2 * kTileBytes;
+constexpr int kChunk = 32;                     // columns that an epilogue warp takes at a time
+constexpr int kBuffer = 32 * 2 * kChunk;       // its 32 rows of them in 16 bits
+constexpr int kSmem = 1024 + kStages * kStage + kEpiWarps * kBuffer + 256;
+constexpr float kLn2 = 0.69314718055994531f;
+constexpr float kLowest = -3.402823466e38f;    // no maximum is below it: z - max is a number then, but for infinities
+
+struct HeadMaps {
+  CUtensorMap x, w, w_half;                    // w in boxes of 128 and of 64 rows
+};
+struct HeadUnits {
+  int ntm, ntn, units, half_units;             // whole tiles, and after those halves of tiles
+  int steps;                                   // of 64 elements of depth
+};
+
+// The unit's tile: bands of 8 tile rows, so that the tiles in flight share rows in L2.
+struct HeadTile {
+  int tm, col, width;
+};
+__device__ __forceinline__ bool head_tile(const HeadUnits& u, int i, HeadTile& t) {
+  if (i >= u.units + u.half_units) return false;
+  const int half = i - u.units, at = half >= 0 ? u.units + half / 2 : i;
+  const int per = 8 * u.ntn, band = at / per, in = at - band * per;
+  const int h = min(8, u.ntm - band * 8), tn = in / h;
+  t.tm = band * 8 + (in - tn * h);
+  t.col = tn * kTile;
+  t.width = kTile;
+  if (half >= 0) {
+    t.width = kTile / 2;
+    t.col += (half & 1) * t.width;
+  }
+  return true;
+}
+
+// v[j] for a j that the compiler does not know.
+__device__ __forceinline__ float pick32(const float (&v)[32], int j) {
+  float t[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) t[i] = j & 1 ? v[2 * i + 1] : v[2 * i];
+#pragma unroll
+  for (int n = 8, b = 2; n; n >>= 1, b <<= 1)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) t[i] = j & b ? t[2 * i + 1] : t[2 * i];
+  return t[0];
+}
+__device__ __forceinline__ void add32(float (&v)[32], int j, float d) {
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    if (i == j) v[i] += d;
+}
+__device__ __forceinline__ void set32(float (&v)[32], int j, float d) {
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    if (i == j) v[i] = d;
+}
+
+// ---------------------------------------------------------------------------
+// Tiles of 256 tokens × 256 rows of w on CTA pairs as in linear_pair_kernel: 128 rows
+// of each operand a CTA, two accumulators in tensor memory, so that a tile's epilogue
+// runs beside the next one's products.  An epilogue warp has 32 tokens, one a lane, and
+// 64 columns.
+//
+// Forward, a lane brings its logits to powers of two, takes their maximum and sums
+// exp2 of the differences, 32 columns and then the next 32 joined to them.
+// ---------------------------------------------------------------------------
+template <int TYPE, bool GRAD, bool SOFT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadArgs A, const HeadUnits U,
+                Oz2Device* dev) {
+  constexpr bool BF16 = TYPE == OZ2_TYPE_BF16;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* epi = smem + kStages * kStage;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(epi + kEpiWarps * kBuffer);
+  // bars: full[S], empty[S], acc_full[2], acc_empty[2], drain
+  __shared__ uint32_t tmem_base_s;
+
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const bool leader = rank == 0;
+  const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
+  const uint32_t full0 = smem_u32(bars), empty0 = smem_u32(bars + kStages);
+  const uint32_t acc_full = smem_u32(bars + 2 * kStages), acc_empty = smem_u32(bars + 2 * kStages + 2);
+  const uint32_t drain_bar = smem_u32(bars + 2 * kStages + 4);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(full0 + 8 * s, 1);
+      mbar_init(empty0 + 8 * s, 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(acc_full + 8 * a, 1);
+      mbar_init(acc_empty + 8 * a, 2 * kEpiWarps);
+    }
+    mbar_init(drain_bar, 1);
+    fence_barrier_init();
+  }
+  if (warp == 1) {
+    tmem_alloc_pair(smem_u32(&tmem_base_s), 512);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base_s, 0);
+  bool ok = true;
+  pdl_wait();
+
+  HeadTile tile;
+  const int steps = U.steps;
+  if (warp == 0) {
+    // ---------------- TMA producer (both CTAs) ----------------
+    if (elect_one()) {
+      const uint32_t full_leader0 = mapa_shared(full0, 0), ring0 = smem_u32(smem);
+      uint32_t it = 0, s = 0, ph = 1;
+      for (int i = pair; ok && steps && head_tile(U, i, tile); i += npairs) {
+        const bool half = tile.width != kTile;
+        const int xrow = tile.tm * kTile + rank * kRows, wrow = tile.col + rank * (tile.width / 2);
+        const CUtensorMap* mw = half ? &maps.w_half : &maps.w;
+        const uint32_t bytes = 2u * (kTileBytes + (half ? kTileBytes / 2 : kTileBytes));
+        for (int t = 0, d = 0; t < steps; ++t, d += 64) {
+          if (!mbar_wait_bounded(empty0 + 8 * s, ph, kWaitLimit)) {
+            ok = false;
+            break;
+          }
+          const uint32_t sa = ring0 + s * kStage, bar = full_leader0 + 8 * s;
+          if (leader) mbar_arrive_expect_tx(full0 + 8 * s, bytes);
+          tma_load_2d_pair(sa, &maps.x, bar, d, xrow);
+          tma_load_2d_pair(sa + kTileBytes, mw, bar, d, wrow);
+          ++it;
+          if (++s == kStages) {
+            s = 0;
+            ph ^= 1;
+          }
+        }
+      }
+      if (!ok) {
+        dev->status = kStatusTimeout;
+        dev->timeout_site = 31;
+      }
+      pdl_trigger();
+      if (leader)  // the leader's stage barriers also count the peer's bytes
+        for (uint32_t j = (it > kStages ? it - kStages : 0); j < it; ++j)
+          mbar_wait_bounded(full0 + 8 * (j % kStages), (j / kStages) & 1, kWaitLimit);
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    // ---------------- MMA issuer (leader CTA) ----------------
+    if (leader) {  // the whole warp; lane 0 issues
+      const uint32_t me = lane == 0;
+      const uint32_t base = smem_u32(smem);
+      const uint64_t xd = operand_desc<false>(base), wd = operand_desc<false>(base + kTileBytes);
+      uint32_t s = 0, ph = 0, acc = 0, accph = 1;
+      auto multiply = [&](auto shape, uint32_t d) {
+        for (int t = 0; t < steps && ok; ++t) {
+          if (!(ok = mbar_wait_warp(full0 + 8 * s, ph, kWaitLimit))) break;
+          tc_fence_after();
+          const uint64_t a = xd + s * (kStage >> 4), b = wd + s * (kStage >> 4);
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk)
+            mma_pair<false>(me, d, a + kk * shape.a_next, b + kk * shape.b_next, shape.idesc, (t | kk) ? 1u : 0u);
+          mma_commit_pair_mc(me, empty0 + 8 * s, 0x3);
+          if (++s == kStages) {
+            s = 0;
+            ph ^= 1;
+          }
+        }
+      };
+      for (int i = pair; ok && steps && head_tile(U, i, tile); i += npairs) {
+        ok = mbar_wait_warp(acc_empty + 8 * acc, accph, kWaitLimit);
+        tc_fence_after();
+        if (tile.width == kTile) {
+          multiply(MmaShape<TYPE, false, false, kTile, kTile>{}, tmem + acc * kTile);
+        } else {
+          multiply(MmaShape<TYPE, false, false, kTile, kTile / 2>{}, tmem + acc * kTile);
+        }
+        if (!ok) break;
+        mma_commit_pair_mc(me, acc_full + 8 * acc, 0x3);
+        acc ^= 1;
+        if (acc == 0) accph ^= 1;
+      }
+      if (!ok && me) {
+        dev->status = kStatusTimeout;
+        dev->timeout_site = 32;
+      }
+      mma_commit_pair(me, drain_bar);
+      mbar_wait_bounded(drain_bar, 0, kWaitLimit);
+    }
+    __syncwarp();
+  } else {
+    // ---------------- epilogue (warps 2..17, both CTAs) ----------------
+    const int ew = warp - 2;
+    const int q = warp & 3, h = ew >> 2;  // TMEM lane quarter, column quarter
+    uint8_t* buf = epi + ew * kBuffer;
+    const uint32_t acc_empty_leader = mapa_shared(acc_empty, 0);
+    const float to2 = A.scale * kLog2E;   // logits in powers of two
+    float up = 1.f;                       // dz's scale
+    if (GRAD && A.largest) {
+      const int bits = __ldg(A.largest), e = (bits >> 23) - 127;
+      const int s = bits > 0 ? max(-100, min(100, 14 - e)) : 0;
+      up = __int_as_float((127 + s) << 23);
+      if (blockIdx.x == 0 && threadIdx.x == 64) *A.unscale = __int_as_float((127 - s) << 23);
+    }
+    uint32_t acc = 0, accph = 0;
+    for (int i = pair; head_tile(U, i, tile); i += npairs) {
+      // A half tile is two warps' columns: the others have none.
+      const int64_t row = static_cast<int64_t>(tile.tm) * kTile + rank * kRows + 32 * q + lane;
+      const int col0 = tile.col + kHeadGroup * h;             // in the piece
+      const int cols = kHeadGroup * h < tile.width && col0 < A.cols ? min(static_cast<int64_t>(kHeadGroup), A.cols - col0) : 0;
+      // This lane's next target in these columns: its row of w (in the piece), its value, and its place.
+      const int2* targets = A.targets + (row < A.m ? row : 0) * A.top;
+      int next = kNoTarget, value = 0, at = 0;
+      HeadRow terms = {0.f, 0.f, 0.f, 0};
+      if (row < A.m && cols > 0) {
+        if (GRAD) {
+          const float4 f = __ldg(reinterpret_cast<const float4*>(A.rows) + row);
+          terms = HeadRow{f.x * up, f.y, f.z, __float_as_int(f.w)};
+        }
+        const int first = static_cast<int>(A.c0) + col0;
+        if (SOFT) {
+          int end = A.top;
+          while (at < end) {  // the first one from these columns on
+            const int mid = (at + end) >> 1;
+            if (__ldg(&targets[mid].x) < first) {
+              at = mid + 1;
+            } else {
+              end = mid;
+            }
+          }
+        }
+        if (at < A.top) {
+          const int2 t = __ldg(targets + at);
+          if (t.x >= first && t.x != kNoTarget) next = t.x - static_cast<int>(A.c0), value = t.y;
+        }
+      }
+      auto advance = [&] {
+        next = kNoTarget;
+        if (SOFT && ++at < A.top) {
+          const int2 t = __ldg(targets + at);
+          if (t.x != kNoTarget) next = t.x - static_cast<int>(A.c0), value = t.y;
+        }
+      };
+      if (steps) {
+        if (!mbar_wait_bounded(acc_full + 8 * acc, accph, kWaitLimit)) ok = false;
+        if (!__all_sync(0xffffffffu, ok)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+      }
+      const uint32_t from = tmem + (static_cast<uint32_t>(32 * q) << 16) + acc * kTile + kHeadGroup * h;
+      auto release = [&] {  // the sums are in registers: the next but one tile's products may begin
+        if (steps) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_remote_relaxed(acc_empty_leader + 8 * acc);
+          acc ^= 1;
+          if (acc == 0) accph ^= 1;
+        }
+      };
+      if (cols == 0) release();
+      float most = kLowest, sum = 0.f;
+      const float main = terms.a * (1.f + terms.e);
+      const int64_t row0 = row - lane;
+#pragma unroll 1
+      for (int c = 0; c < cols; c += kChunk) {
+        float z[32];
+        if (steps) {
+          uint32_t v[32];
+          tmem_ld32(from + c, v);
+          tmem_ld_wait();
+          if (c + kChunk >= cols) release();
+#pragma unroll
+          for (int j = 0; j < 32; ++j) z[j] = __uint_as_float(v[j]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) z[j] = 0.f;
+        }
+        const int left = cols - c, end = col0 + c + kChunk;
+        if (!GRAD) {
+          while (__any_sync(0xffffffffu, next < end)) {
+            if (next < end) {
+              A.picked[row * A.top + value] = pick32(z, next - (col0 + c)) * A.scale;
+              advance();
+            }
+          }
+          __syncwarp();
+#pragma unroll
+          for (int j = 0; j < 32; ++j) z[j] *= to2;
+          if (left < kChunk) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (j >= left) z[j] = -INFINITY;
+          }
+          float top = most;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) top = fmaxf(top, z[j]);
+          sum *= exp2_fast(most - top);
+          most = top;
+          float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int j = 0; j < 32; ++j) s[j & 3] += exp2_fast(z[j] - top);
+          sum += (s[0] + s[1]) + (s[2] + s[3]);
+        } else {
+          float hard = 0.f;
+          if (!SOFT && next < end) hard = pick32(z, next - (col0 + c));
+#pragma unroll
+          for (int j = 0; j < 32; ++j) z[j] = main * exp2_fast(fmaf(z[j], to2, -terms.lse2));
+          while (__any_sync(0xffffffffu, next < end)) {
+            if (next < end) {
+              if (SOFT) {
+                add32(z, next - (col0 + c), -terms.a * __int_as_float(value));
+              } else {  // (1 + e)·p - 1 with p near 1: by p - 1
+                set32(z, next - (col0 + c),
+                      terms.a * fmaf(1.f + terms.e, expm1f(fmaf(hard, to2, -terms.lse2) * kLn2), terms.e));
+              }
+              advance();
+            }
+          }
+          __syncwarp();
+          if (!terms.live) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) z[j] = 0.f;
+          }
+#pragma unroll
+          for (int j = 0; j < 32; j += 8)
+            sts128(buf + piece_at(lane, j >> 3),
+                   make_uint4(pack16(z[j], z[j + 1], BF16), pack16(z[j + 2], z[j + 3], BF16),
+                              pack16(z[j + 4], z[j + 5], BF16), pack16(z[j + 6], z[j + 7], BF16)));
+          __syncwarp();
+          // (dz's rows are on 16-byte boundaries, and there are multiples of 64 of its columns.)
+          if (row0 + 32 <= A.m) {
+            store_fast(A.dz + (row0 + (lane >> 2)) * A.ld_dz + col0 + c + 8 * (lane & 3), A.ld_dz, lane, buf);
+          } else {
+            store_slow(A.dz, A.ld_dz, A.m, A.cols, row0, col0 + c, lane, buf);
+          }
+          __syncwarp();
+        }
+      }
+      if (!GRAD && cols > 0 && row < A.m)
+        A.stats[static_cast<int64_t>(col0 / kHeadGroup) * A.ld_stats + row] = make_float2(most, sum);
+    }
+    if (!ok) {
+      dev->status = kStatusTimeout;
+      dev->timeout_site = 33;
+    }
+  }
+  tc_fence_before();
+  cluster_sync_all();  // neither CTA leaves while the pair's MMAs or loads may touch it
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc_pair(tmem, 512);
+}
+
+// ---------------------------------------------------------------------------
+// A token's targets, sorted by their rows (by place among equal ones), and with `rows`
+// its terms of the gradient: one warp to a token.
+// ---------------------------------------------------------------------------
+constexpr int kTargetWarps = 4;
+
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+__device__ __forceinline__ float warp_add(float v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+__device__ __forceinline__ float teacher_at(const HeadTargets& t, int64_t row, int i) {
+  const int64_t at = row * t.ld_teacher + i;
+  const float v = t.teacher_type == OZ2_TYPE_F32 ? __ldg(static_cast<const float*>(t.teacher) + at)
+                                                 : load16(static_cast<const uint16_t*>(t.teacher) + at,
+                                                          t.teacher_type == OZ2_TYPE_BF16);
+  return v / t.temperature;
+}
+// The listed logits' maximum and the logarithm of their exponentials' sum over it.
+__device__ __forceinline__ void teacher_sums(const HeadTargets& t, int64_t row, int lane, float* top, float* sum) {
+  float m = kLowest, s = 0.f;
+  for (int i = lane; i < t.top; i += 32)
+    if (t.ids[row * t.ld + i] >= 0) m = fmaxf(m, teacher_at(t, row, i));
+  m = warp_max(m);
+  for (int i = lane; i < t.top; i += 32)
+    if (t.ids[row * t.ld + i] >= 0) s += expf(teacher_at(t, row, i) - m);
+  *top = m;
+  *sum = warp_add(s);
+}
+
+__global__ void __launch_bounds__(32 * kTargetWarps)
+    head_targets_kernel(int64_t m, int64_t n, HeadTargets t, int padded, int2* sorted, HeadRow* rows, const float* lse,
+                        const float* dloss, int dloss_each, float scale, float z_loss, int* largest) {
+  extern __shared__ unsigned long long keys_s[];
+  pdl_trigger();
+  pdl_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * kTargetWarps + warp;
+  if (row >= m) return;
+  bool live = false, bad = false;
+  float top = 0.f, sum = 1.f;
+  unsigned long long* keys = keys_s + warp * padded;
+  for (int i = lane; i < padded; i += 32) {
+    int64_t id = i < t.top ? t.ids[row * t.ld + i] : -1;
+    live = live || id >= 0;
+    bad = bad || id >= n;
+    if (id < 0 || id >= n) id = kNoTarget;
+    keys[i] = static_cast<unsigned long long>(id) << 32 | static_cast<uint32_t>(i);
+  }
+  live = __any_sync(0xffffffffu, live);
+  bad = __any_sync(0xffffffffu, bad);
+  if (t.soft && rows) teacher_sums(t, row, lane, &top, &sum);
+  __syncwarp();
+  for (int size = 2; size <= padded; size <<= 1)
+    for (int step = size >> 1; step; step >>= 1) {
+      for (int p = lane; p < padded / 2; p += 32) {
+        const int i = 2 * p - (p & (step - 1)), j = i + step;
+        const unsigned long long a = keys[i], b = keys[j];
+        if ((a > b) == ((i & size) == 0)) keys[i] = b, keys[j] = a;
+      }
+      __syncwarp();
+    }
+  for (int i = lane; i < t.top; i += 32) {
+    const int id = static_cast<int>(keys[i] >> 32), place = static_cast<int>(keys[i] & 0xFFFFFFFFu);
+    int value = place;
+    if (rows) value = __float_as_int(t.soft && id != kNoTarget ? expf(teacher_at(t, row, place) - top) / sum : 1.f);
+    sorted[row * t.top + i] = make_int2(id, value);
+  }
+  if (rows && lane == 0) {
+    const float l = lse[row];
+    HeadRow r;
+    r.a = live ? (bad ? __int_as_float(0x7FC00000) : dloss[dloss_each ? row : 0] * scale) : 0.f;
+    r.lse2 = l * kLog2E;
+    r.e = z_loss != 0.f ? 2.f * z_loss * l : 0.f;
+    r.live = live;
+    rows[row] = r;
+    if (largest) {
+      const float size = fabsf(r.a) * fmaxf(1.f, fabsf(1.f + r.e));
+      if (live && size < INFINITY) atomicMax(largest, __float_as_int(size));
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// lse and losses.  A block has 32 tokens, one a lane; its warps take the groups of
+// columns in turn, and their maxima and sums are joined in shared memory.
+// ---------------------------------------------------------------------------
+constexpr int kJoinWarps = 32;
+
+__global__ void __launch_bounds__(32 * kJoinWarps)
+    head_join_kernel(int64_t m, int64_t n, HeadTargets t, const float2* __restrict__ stats, int64_t ld_stats, int groups,
+                     float z_loss, float* __restrict__ loss, float* __restrict__ lse, float* picked) {
+  __shared__ float2 parts[kJoinWarps][32];
+  __shared__ float lse_s[32];
+  pdl_trigger();
+  pdl_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * 32, row = row0 + lane;
+  float most = kLowest, sum = 0.f;
+  auto join = [&](float2 p) {
+    const float top = fmaxf(most, p.x);
+    sum = sum * exp2_fast(most - top) + p.y * exp2_fast(p.x - top);
+    most = top;
+  };
+  if (row < m) {
+#pragma unroll 4
+    for (int g = warp; g < groups; g += kJoinWarps) join(stats[g * ld_stats + row]);
+  }
+  parts[warp][lane] = make_float2(most, sum);
+  __syncthreads();
+  if (warp == 0) {
+    for (int w = 1; w < kJoinWarps; ++w) join(parts[w][lane]);
+    const float l = most == INFINITY ? INFINITY : kLn2 * most + logf(sum);
+    lse_s[lane] = l;
+    if (row < m) {
+      lse[row] = l;
+      if (!t.soft) {
+        const int64_t id = t.ids[row * t.ld];
+        float p = id >= n ? __int_as_float(0x7FC00000) : 0.f;
+        if (id >= 0 && id < n) {
+          p = picked[row];
+        } else {
+          picked[row] = p;
+        }
+        loss[row] = id < 0 ? 0.f : l - p + (z_loss != 0.f ? z_loss * l * l : 0.f);
+      }
+    }
+  }
+  if (!t.soft) return;
+  __syncthreads();
+  const int64_t mine = row0 + warp;
+  if (mine >= m) return;
+  float top, all;
+  teacher_sums(t, mine, lane, &top, &all);
+  const float log_all = logf(all);
+  float s = 0.f;
+  bool live = false;
+  for (int i = lane; i < t.top; i += 32) {
+    const int64_t id = t.ids[mine * t.ld + i];
+    float* p = picked + mine * t.top + i;
+    float z = 0.f;
+    if (id >= 0 && id < n) {
+      z = *p;
+    } else {
+      *p = z = id >= n ? __int_as_float(0x7FC00000) : 0.f;
+    }
+    if (id >= 0) {
+      live = true;
+      const float log_q = teacher_at(t, mine, i) - top - log_all, weight = expf(log_q);
+      if (weight != 0.f) s = fmaf(weight, log_q - z, s);  // (a row that the teacher rules out weighs nothing)
+    }
+  }
+  s = warp_add(s);
+  live = __any_sync(0xffffffffu, live);
+  if (lane == 0) loss[mine] = live ? s + lse_s[warp] : 0.f;
+}
+
+// ---------------------------------------------------------------------------
+// Rows of x, zeros for the tokens that do not count: their gradient is zero times what
+// they hold, which need not be a number.
+// ---------------------------------------------------------------------------
+__global__ void __launch_bounds__(256) live_rows_kernel(int64_t m, int64_t k, const uint16_t* __restrict__ x, int64_t ldx,
+                                                        const HeadRow* __restrict__ rows, uint16_t* __restrict__ dst,
+                                                        int64_t ld_dst) {
+  pdl_trigger();
+  pdl_wait();
+  const int per = static_cast<int>((k + 7) / 8);
+  const uint16_t* end = x + (m - 1) * ldx + k;
+  for (int64_t r = blockIdx.x; r < m; r += gridDim.x) {
+    const bool live = rows[r].live != 0;
+    for (int c = threadIdx.x; c < per; c += 256) {
+      const uint16_t* p = x + r * ldx + 8 * c;
+      *reinterpret_cast<uint4*>(dst + r * ld_dst + 8 * c) =
+          live ? load16_any(p, x, end, static_cast<int>(min(int64_t(8), k - 8 * c))) : make_uint4(0, 0, 0, 0);
+    }
+  }
+}
+
+// FP32 sums to the rows' type.
+template <bool BF16>
+__global__ void __launch_bounds__(256) round_rows_kernel(int64_t m, int64_t k, const float* __restrict__ src, int64_t ld_src,
+                                                         const float* __restrict__ unscale, uint16_t* __restrict__ dst,
+                                                         int64_t ld_dst, bool vec) {
+  pdl_trigger();
+  pdl_wait();
+  const float f = unscale ? *unscale : 1.f;
+  const int per = static_cast<int>((k + 7) / 8);
+  for (int64_t r = blockIdx.x; r < m; r += gridDim.x)
+    for (int c = threadIdx.x; c < per; c += 256) {
+      const float4 *p = reinterpret_cast<const float4*>(src + r * ld_src + 8 * c), a = p[0], b = p[1];  // (rows of multiples of 8)
+      const int n = static_cast<int>(min(int64_t(8), k - 8 * c));
+      store16_any(dst + r * ld_dst + 8 * c,
+                  make_uint4(pack16(a.x * f, a.y * f, BF16), pack16(a.z * f, a.w * f, BF16), pack16(b.x * f, b.y * f, BF16),
+                             pack16(b.z * f, b.w * f, BF16)),
+                  n, vec && n == 8);
+    }
+}
+
+bool make_rows_map(CUtensorMap* map, const void* base, int64_t rows, int64_t depth, int64_t ld, int box_rows) {
+  EncodeTiledFn enc = get_encode_fn();
+  if (!enc) return false;
+  cuuint64_t dims[2] = {static_cast<cuuint64_t>(depth), static_cast<cuuint64_t>(rows)};
+  cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld) * 2};
+  cuuint32_t box[2] = {64, static_cast<cuuint32_t>(box_rows)}, estr[2] = {1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void*>(base), dims, strides, box, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int TYPE, bool GRAD, bool SOFT>
+cudaError_t launch(const HeadArgs& a, Oz2Device* dev, cudaStream_t st) {
+  auto kern = head_kernel<TYPE, GRAD, SOFT>;
+  cudaError_t err = allow_smem(reinterpret_cast<const void*>(kern), kSmem);
+  if (err != cudaSuccess) return err;
+  const int64_t ntm = (a.m + kTile - 1) / kTile, ntn = (a.cols + kTile - 1) / kTile;
+  if (ntm * ntn > 0x1FFFFFFF) return cudaErrorInvalidValue;
+  const int64_t resident = resident_pairs(reinterpret_cast<const void*>(kern), kThreads, kSmem);
+  HeadUnits u{static_cast<int>(ntm), static_cast<int>(ntn), static_cast<int>(ntm * ntn), 0,
+              static_cast<int>((a.k + 63) / 64)};
+  // A last round of few tiles: they are taken as halves, by twice as many pairs.
+  const int last = static_cast<int>(u.units % resident);
+  if (2 * last <= resident) {
+    u.units -= last;
+    u.half_units = 2 * last;
+  }
+  HeadMaps maps{};
+  if (u.steps && (!make_rows_map(&maps.x, a.x, a.m, a.k, a.ldx, kRows) || !make_rows_map(&maps.w, a.w, a.cols, a.k, a.ldw, kRows) ||
+                  !make_rows_map(&maps.w_half, a.w, a.cols, a.k, a.ldw, kRows / 2)))
+    return cudaErrorInvalidValue;
+  const int64_t pairs = std::min<int64_t>(u.units + u.half_units, resident);
+  count_launch();
+  return launch_dependent(kern, dim3(static_cast<unsigned>(2 * pairs)), dim3(kThreads), kSmem, st, maps, a, u, dev);
+}
+
+int padded_top(int top) {
+  int p = 1;
+  while (p < top) p *= 2;
+  return p;
+}
+
+}  // namespace
+
+cudaError_t launch_head_targets(int64_t m, int64_t n, const HeadTargets& t, int2* sorted, HeadRow* rows, const float* lse,
+                                const float* dloss, int dloss_each, float scale, float z_loss, int* largest,
+                                cudaStream_t st) {
+  const int padded = padded_top(t.top);
+  count_launch();
+  return launch_dependent(head_targets_kernel, dim3(static_cast<unsigned>((m + kTargetWarps - 1) / kTargetWarps)),
+                          dim3(32 * kTargetWarps), sizeof(unsigned long long) * padded * kTargetWarps, st, m, n, t, padded,
+                          sorted, rows, lse, dloss, dloss_each, scale, z_loss, largest);
+}
+
+cudaError_t launch_live_rows(int64_t m, int64_t k, const void* x, int64_t ldx, const HeadRow* rows, void* dst,
+                             int64_t ld_dst, cudaStream_t st) {
+  count_launch();
+  return launch_dependent(live_rows_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(m, 8 * num_sms()))), dim3(256), 0, st, m,
+                          k, static_cast<const uint16_t*>(x), ldx, rows, static_cast<uint16_t*>(dst), ld_dst);
+}
+
+cudaError_t launch_head_forward(const HeadArgs& a, int type, Oz2Device* dev, cudaStream_t st) {
+  const bool soft = a.soft != 0;
+  if (type == OZ2_TYPE_BF16) return soft ? launch<OZ2_TYPE_BF16, false, true>(a, dev, st) : launch<OZ2_TYPE_BF16, false, false>(a, dev, st);
+  return soft ? launch<OZ2_TYPE_F16, false, true>(a, dev, st) : launch<OZ2_TYPE_F16, false, false>(a, dev, st);
+}
+
+cudaError_t launch_head_grad(const HeadArgs& a, int type, Oz2Device* dev, cudaStream_t st) {
+  const bool soft = a.soft != 0;
+  if (type == OZ2_TYPE_BF16) return soft ? launch<OZ2_TYPE_BF16, true, true>(a, dev, st) : launch<OZ2_TYPE_BF16, true, false>(a, dev, st);
+  return soft ? launch<OZ2_TYPE_F16, true, true>(a, dev, st) : launch<OZ2_TYPE_F16, true, false>(a, dev, st);
+}
+
+cudaError_t launch_head_join(int64_t m, int64_t n, const HeadTargets& t, const float2* stats, int64_t ld_stats,
+                             float z_loss, float* loss, float* lse, float* picked, cudaStream_t st) {
+  count_launch();
+  return launch_dependent(head_join_kernel, dim3(static_cast<unsigned>((m + 31) / 32)), dim3(32 * kJoinWarps), 0, st, m, n, t,
+                          stats, ld_stats, static_cast<int>((n + kHeadGroup - 1) / kHeadGroup), z_loss, loss, lse, picked);
+}
+
+cudaError_t launch_round_rows(int64_t m, int64_t k, int type, const float* src, int64_t ld_src, const float* unscale,
+                              void* dst, int64_t ld_dst, cudaStream_t st) {
+  count_launch();
+  return launch_dependent(type == OZ2_TYPE_BF16 ? round_rows_kernel<true> : round_rows_kernel<false>,
+                          dim3(static_cast<unsigned>(std::min<int64_t>(m, 8 * num_sms()))), dim3(256), 0, st, m, k, src, ld_src,
+                          unscale, static_cast<uint16_t*>(dst), ld_dst, rows_on16(dst, ld_dst, 2));
+}
+
+}  // namespace oz2

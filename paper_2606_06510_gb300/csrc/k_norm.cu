@@ -1,0 +1,576 @@
+// Layer norm over a row's k features, forward and backward:
+//   μ = mean x (0 where not centred)   r = 1/√(mean (x-μ)² + ε)   x̂ = (x-μ)·r
+//   y  = x̂·w + b
+//   dx = r·(g - mean g - x̂·mean(g·x̂)) + R   with g = dy·w (no mean g where not centred)
+//   dw = Σ_t dy·x̂      db = Σ_t dy
+// A row is held in registers: its mean first, then the squares of what deviates from it
+// (two passes over registers, none over memory; the difference of E x² and μ² would lose
+// what a large mean takes).
+#include <algorithm>
+
+#include "lm_common.cuh"
+
+namespace oz2 {
+namespace {
+
+constexpr int kNormThreads = 512;  // of the blocks whose rows take that many threads
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+// The N sums over a row's TPR threads, the same bits in each of them.  Groups of more
+// than one warp exchange theirs in `at` (two sets, taken in turn: a set is written again
+// two barriers later) behind a barrier of their own.
+template <int TPR, int N>
+struct RowSum {
+  static constexpr int kWarps = TPR / 32;
+  float* at;
+  int group, turn;
+  __device__ __forceinline__ void sum(float (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
+    if (kWarps == 1) return;
+    float* s = at + turn * (kWarps * N);
+    turn ^= 1;
+    const int w = (threadIdx.x >> 5) % kWarps, lane = threadIdx.x & 31;
+    if (lane == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[w * N + i] = v[i];
+    }
+    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(TPR) : "memory");
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = warp_sum(lane < kWarps ? s[lane * N + i] : 0.f);
+  }
+};
+
+// V values of a vector of the rows' type or F32, from its element `col` on.
+template <int TYPE>
+__device__ __forceinline__ void load_vector(const void* p, int wtype, int64_t col, int n, int64_t k,
+                                            float (&f)[Elem<TYPE>::V]) {
+  using X = Elem<TYPE>;
+  if (TYPE != OZ2_TYPE_F32 && wtype == OZ2_TYPE_F32) {
+    const float* s = static_cast<const float*>(p) + col;
+    if (n >= X::V && (reinterpret_cast<uintptr_t>(s) & 15) == 0) {
+#pragma unroll
+      for (int h = 0; h < X::V; h += 4) {
+        const float4 v = __ldg(reinterpret_cast<const float4*>(s + h));
+        f[h] = v.x, f[h + 1] = v.y, f[h + 2] = v.z, f[h + 3] = v.w;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < X::V; ++e) f[e] = e < n ? __ldg(s + e) : 0.f;
+    }
+  } else {
+    const typename X::T* s = static_cast<const typename X::T*>(p);
+    X::unpack(load_piece<false>(s + col, s, s + k, n), f);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Forward.  TPR threads to a row, VPT 16-byte pieces of it to a thread.
+// ---------------------------------------------------------------------------
+template <int TYPE, int TPR, int VPT, bool ALIGNED>
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) norm_kernel(NormArgs a) {
+  using X = Elem<TYPE>;
+  using T = typename X::T;
+  constexpr int V = X::V, kBlock = TPR < 128 ? 128 : TPR, kGroups = kBlock / TPR;
+  __shared__ float exchange[kGroups][2 * TPR / 32];
+  pdl_trigger();
+  pdl_wait();
+  const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
+  const T* src = static_cast<const T*>(a.x);
+  const T* end = src + (a.m - 1) * a.ldx + a.k;
+  const float inv_k = 1.f / static_cast<float>(a.k);
+  RowSum<TPR, 1> rows{exchange[group], group, 0};
+  for (int64_t r = static_cast<int64_t>(blockIdx.x) * kGroups + group; r < a.m; r += static_cast<int64_t>(gridDim.x) * kGroups) {
+    uint4 raw[VPT];
+    float x[VPT][V];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const int64_t col = static_cast<int64_t>(t + i * TPR) * V;
+      raw[i] = make_uint4(0, 0, 0, 0);
+      if (col < a.k)
+        raw[i] = load_piece<ALIGNED>(src + r * a.ldx + col, src, end, static_cast<int>(min(int64_t(V), a.k - col)));
+    }
+    float s[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      X::unpack(raw[i], x[i]);  // (zeros past the row's end)
+#pragma unroll
+      for (int e = 0; e < V; ++e) s[0] += x[i][e];
+    }
+    float mean = 0.f;
+    if (a.center) {
+      rows.sum(s);
+      mean = s[0] * inv_k;
+    }
+    s[0] = 0.f;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const int64_t col = static_cast<int64_t>(t + i * TPR) * V;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        x[i][e] -= mean;
+        if (col + e < a.k) s[0] = fmaf(x[i][e], x[i][e], s[0]);
+      }
+    }
+    rows.sum(s);
+    const float rstd = 1.f / sqrtf(fmaf(s[0], inv_k, a.eps));
+    if (t == 0) {
+      if (a.mean) a.mean[r] = mean;
+      if (a.rstd) a.rstd[r] = rstd;
+    }
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const int64_t col = static_cast<int64_t>(t + i * TPR) * V;
+      if (col >= a.k) continue;
+      const int n = static_cast<int>(min(int64_t(V), a.k - col));
+#pragma unroll
+      for (int e = 0; e < V; ++e) x[i][e] *= rstd;
+      if (a.w) {
+        float w[V];
+        load_vector<TYPE>(a.w, a.wtype, col, n, a.k, w);
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[i][e] *= w[e];
+      }
+      if (a.b) {
+        float b[V];
+        load_vector<TYPE>(a.b, a.wtype, col, n, a.k, b);
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[i][e] += b[e];
+      }
+      store16_any(static_cast<T*>(a.y) + r * a.ldy + col, X::pack(x[i]), n, ALIGNED && n == V);
+    }
+  }
+}
+
+// Rows too long for registers: a block to a row, which it reads again for each of the
+// two sums and the result (from L2, mostly).
+template <int TYPE>
+__global__ void __launch_bounds__(kNormThreads) norm_long_kernel(NormArgs a) {
+  using X = Elem<TYPE>;
+  using T = typename X::T;
+  constexpr int V = X::V;
+  __shared__ float exchange[2 * kNormThreads / 32];
+  pdl_trigger();
+  pdl_wait();
+  const T* src = static_cast<const T*>(a.x);
+  const T* end = src + (a.m - 1) * a.ldx + a.k;
+  const float inv_k = 1.f / static_cast<float>(a.k);
+  RowSum<kNormThreads, 1> rows{exchange, 0, 0};
+  for (int64_t r = blockIdx.x; r < a.m; r += gridDim.x) {
+    auto each = [&](auto work) {
+      for (int64_t col = static_cast<int64_t>(threadIdx.x) * V; col < a.k; col += kNormThreads * V) {
+        const int n = static_cast<int>(min(int64_t(V), a.k - col));
+        float x[V];
+        X::unpack(load_piece<false>(src + r * a.ldx + col, src, end, n), x);
+        work(col, n, x);
+      }
+    };
+    float s[1] = {0.f}, mean = 0.f;
+    if (a.center) {
+      each([&](int64_t, int n, float (&x)[V]) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) s[0] += e < n ? x[e] : 0.f;
+      });
+      rows.sum(s);
+      mean = s[0] * inv_k;
+    }
+    s[0] = 0.f;
+    each([&](int64_t, int n, float (&x)[V]) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) s[0] += e < n ? (x[e] - mean) * (x[e] - mean) : 0.f;
+    });
+    rows.sum(s);
+    const float rstd = 1.f / sqrtf(fmaf(s[0], inv_k, a.eps));
+    if (threadIdx.x == 0) {
+      if (a.mean) a.mean[r] = mean;
+      if (a.rstd) a.rstd[r] = rstd;
+    }
+    each([&](int64_t col, int n, float (&x)[V]) {
+      float w[V], b[V];
+      if (a.w) load_vector<TYPE>(a.w, a.wtype, col, n, a.k, w);
+      if (a.b) load_vector<TYPE>(a.b, a.wtype, col, n, a.k, b);
+#pragma unroll
+      for (int e = 0; e < V; ++e) x[e] = (x[e] - mean) * rstd * (a.w ? w[e] : 1.f) + (a.b ? b[e] : 0.f);
+      store16_any(static_cast<T*>(a.y) + r * a.ldy + col, X::pack(x), n, false);
+    });
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Backward.  As forward, with groups that walk over rows: a thread's columns are the
+// same in every row, so it adds up dw and db of them in registers; a block's groups add
+// theirs in shared memory, in order, into the block's row of `parts`, and
+// join_parts_kernel adds up the blocks'.
+// ---------------------------------------------------------------------------
+template <int TYPE, int TPR, int VPT, bool ALIGNED>
+__global__ void __launch_bounds__(kNormThreads, 1) norm_grad_kernel(NormGradArgs a, float* __restrict__ parts) {
+  using X = Elem<TYPE>;
+  using T = typename X::T;
+  constexpr int V = X::V, kGroups = kNormThreads / TPR;
+  __shared__ float exchange[kGroups][4 * TPR / 32];
+  extern __shared__ float columns[];  // of dw, then of db: TPR·VPT·V each, where there are groups to join
+  pdl_trigger();
+  pdl_wait();
+  const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
+  const T *dy = static_cast<const T*>(a.dy), *x = static_cast<const T*>(a.x), *res = static_cast<const T*>(a.r);
+  const T *dy_end = dy + (a.m - 1) * a.lddy + a.k, *x_end = x + (a.m - 1) * a.ldx + a.k,
+          *r_end = res + (a.m - 1) * a.ldr + a.k;
+  const float inv_k = 1.f / static_cast<float>(a.k);
+  RowSum<TPR, 2> rows{exchange[group], group, 0};
+  float dw[VPT][V], db[VPT][V];
+#pragma unroll
+  for (int i = 0; i < VPT; ++i)
+#pragma unroll
+    for (int e = 0; e < V; ++e) dw[i][e] = db[i][e] = 0.f;
+  const int64_t stride = static_cast<int64_t>(gridDim.x) * kGroups;
+  for (int64_t r = static_cast<int64_t>(blockIdx.x) * kGroups + group; r < a.m; r += stride) {
+    uint4 rd[VPT], rx[VPT], rr[VPT];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const int64_t col = static_cast<int64_t>(t + i * TPR) * V;
+      const int n = static_cast<int>(min(int64_t(V), a.k - col));
+      rd[i] = rx[i] = rr[i] = make_uint4(0, 0, 0, 0);
+      if (n > 0) {
+        rd[i] = load_piece<ALIGNED>(dy + r * a.lddy + col, dy, dy_end, n);
+        rx[i] = load_piece<ALIGNED>(x + r * a.ldx + col, x, x_end, n);
+        if (res) rr[i] = load_piece<ALIGNED, false>(res + r * a.ldr + col, res, r_end, n);
+      }
+    }
+    const float mean = a.mean ? __ldg(a.mean + r) : 0.f, rstd = __ldg(a.rstd + r);
+    float s[2] = {0.f, 0.f};
+    float g[VPT][V], h[VPT][V];  // g = dy·w and x̂
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const int64_t col = static_cast<int64_t>(t + i * TPR) * V;
+      const int n = static_cast<int>(min(int64_t(V), a.k - col));
+      X::unpack(rd[i], g[i]);
+      X::unpack(rx[i], h[i]);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        h[i][e] = e < n ? (h[i][e] - mean) * rstd : 0.f;
+        dw[i][e] = fmaf(g[i][e], h[i][e], dw[i][e]);
+        db[i][e] += g[i][e];
+      }
+      if (a.w && n > 0) {
+        float w[V];
+        load_vector<TYPE>(a.w, a.wtype, col, n, a.k, w);
+#pragma unroll
+        for (int e = 0; e < V; ++e) g[i][e] *= w[e];
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        s[0] += g[i][e];
+        s[1] = fmaf(g[i][e], h[i][e], s[1]);
+      }
+    }
+    if (!a.dx) continue;
+    rows.sum(s);
+    const float level = a.mean ? s[0] * inv_k : 0.f, along = s[1] * inv_k;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const int64_t col = static_cast<int64_t>(t + i * TPR) * V;
+      const int n = static_cast<int>(min(int64_t(V), a.k - col));
+      if (n <= 0) continue;
+#pragma unroll
+      for (int e = 0; e < V; ++e) g[i][e] = rstd * (g[i][e] - level - h[i][e] * along);
+      if (res) {
+        float o[V];
+        X::unpack(rr[i], o);
+#pragma unroll
+        for (int e = 0; e < V; ++e) g[i][e] += o[e];
+      }
+      store16_any(static_cast<T*>(a.dx) + r * a.lddx + col, X::pack(g[i]), n, ALIGNED && n == V);
+    }
+  }
+  if (!parts) return;
+  float* to = parts + static_cast<int64_t>(blockIdx.x) * 2 * a.k;
+  constexpr int kCols = TPR * VPT * V;
+  auto keep = [&](const float (&v)[VPT][V], float* row, float* join) {
+    if (kGroups > 1) {
+      for (int q = 0; q < kGroups; ++q) {
+        __syncthreads();
+        if (group == q) {
+#pragma unroll
+          for (int i = 0; i < VPT; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+              const int c = (t + i * TPR) * V + e;
+              join[c] = q ? join[c] + v[i][e] : v[i][e];
+            }
+        }
+      }
+      __syncthreads();
+      for (int c = threadIdx.x; c < a.k; c += kNormThreads) row[c] = join[c];
+    } else {
+#pragma unroll
+      for (int i = 0; i < VPT; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const int64_t c = static_cast<int64_t>(t + i * TPR) * V + e;
+          if (c < a.k) row[c] = v[i][e];
+        }
+    }
+  };
+  if (a.dw) keep(dw, to, columns);
+  if (a.db) keep(db, to + a.k, columns + kCols);
+}
+
+// Long rows: dx by a block to a row, which reads it twice.
+template <int TYPE>
+__global__ void __launch_bounds__(kNormThreads) norm_grad_long_kernel(NormGradArgs a) {
+  using X = Elem<TYPE>;
+  using T = typename X::T;
+  constexpr int V = X::V;
+  __shared__ float exchange[4 * kNormThreads / 32];
+  pdl_trigger();
+  pdl_wait();
+  const T *dy = static_cast<const T*>(a.dy), *x = static_cast<const T*>(a.x), *res = static_cast<const T*>(a.r);
+  const T *dy_end = dy + (a.m - 1) * a.lddy + a.k, *x_end = x + (a.m - 1) * a.ldx + a.k,
+          *r_end = res + (a.m - 1) * a.ldr + a.k;
+  const float inv_k = 1.f / static_cast<float>(a.k);
+  RowSum<kNormThreads, 2> rows{exchange, 0, 0};
+  for (int64_t r = blockIdx.x; r < a.m; r += gridDim.x) {
+    const float mean = a.mean ? __ldg(a.mean + r) : 0.f, rstd = __ldg(a.rstd + r);
+    auto each = [&](auto work) {
+      for (int64_t col = static_cast<int64_t>(threadIdx.x) * V; col < a.k; col += kNormThreads * V) {
+        const int n = static_cast<int>(min(int64_t(V), a.k - col));
+        float g[V], h[V], w[V];
+        X::unpack(load_piece<false>(dy + r * a.lddy + col, dy, dy_end, n), g);
+        X::unpack(load_piece<false>(x + r * a.ldx + col, x, x_end, n), h);
+        if (a.w) load_vector<TYPE>(a.w, a.wtype, col, n, a.k, w);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          if (a.w) g[e] *= w[e];
+          g[e] = e < n ? g[e] : 0.f;
+          h[e] = e < n ? (h[e] - mean) * rstd : 0.f;
+        }
+        work(col, n, g, h);
+      }
+    };
+    float s[2] = {0.f, 0.f};
+    each([&](int64_t, int, float (&g)[V], float (&h)[V]) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        s[0] += g[e];
+        s[1] = fmaf(g[e], h[e], s[1]);
+      }
+    });
+    rows.sum(s);
+    const float level = a.mean ? s[0] * inv_k : 0.f, along = s[1] * inv_k;
+    each([&](int64_t col, int n, float (&g)[V], float (&h)[V]) {
+      float o[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) o[e] = 0.f;
+      if (res) X::unpack(load_piece<false, false>(res + r * a.ldr + col, res, r_end, n), o);
+#pragma unroll
+      for (int e = 0; e < V; ++e) g[e] = rstd * (g[e] - level - h[e] * along) + o[e];
+      store16_any(static_cast<T*>(a.dx) + r * a.lddx + col, X::pack(g), n, false);
+    });
+  }
+}
+// Their dw and db: a warp's lanes are 32·V columns, a block's warps walk over a chunk of
+// rows.
+template <int TYPE>
+__global__ void __launch_bounds__(256) norm_columns_kernel(NormGradArgs a, int64_t chunk, float* __restrict__ parts) {
+  using X = Elem<TYPE>;
+  using T = typename X::T;
+  constexpr int V = X::V;
+  __shared__ float sums[8][2][32 * V];
+  pdl_trigger();
+  pdl_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const T *dy = static_cast<const T*>(a.dy), *x = static_cast<const T*>(a.x);
+  const T *dy_end = dy + (a.m - 1) * a.lddy + a.k, *x_end = x + (a.m - 1) * a.ldx + a.k;
+  const int64_t col = (static_cast<int64_t>(blockIdx.x) * 32 + lane) * V, r1 = min(a.m, (blockIdx.y + 1) * chunk);
+  const int n = static_cast<int>(min(int64_t(V), a.k - col));
+  float dw[V], db[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) dw[e] = db[e] = 0.f;
+  if (n > 0) {
+#pragma unroll 2
+    for (int64_t r = blockIdx.y * chunk + warp; r < r1; r += 8) {
+      float g[V], h[V];
+      X::unpack(load_piece<false>(dy + r * a.lddy + col, dy, dy_end, n), g);
+      X::unpack(load_piece<false>(x + r * a.ldx + col, x, x_end, n), h);
+      const float mean = a.mean ? __ldg(a.mean + r) : 0.f, rstd = __ldg(a.rstd + r);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        dw[e] = fmaf(g[e], (h[e] - mean) * rstd, dw[e]);
+        db[e] += g[e];
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e) sums[warp][0][lane * V + e] = dw[e], sums[warp][1][lane * V + e] = db[e];
+  __syncthreads();
+  for (int c = threadIdx.x; c < 64 * V; c += 256) {
+    const int which = c / (32 * V), in = c % (32 * V);
+    const int64_t j = static_cast<int64_t>(blockIdx.x) * 32 * V + in;
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) s += sums[w][which][in];
+    if (j < a.k) parts[static_cast<int64_t>(blockIdx.y) * 2 * a.k + which * a.k + j] = s;
+  }
+}
+
+// dw and db from the blocks' rows of parts, in their order: a warp's lanes are columns,
+// its 8 warps each add up every eighth row.
+__global__ void __launch_bounds__(256) join_parts_kernel(int64_t k, int count, const float* __restrict__ parts,
+                                                         float* __restrict__ dw, float* __restrict__ db, int accumulate) {
+  __shared__ float sums[8][32];
+  pdl_trigger();
+  pdl_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t j = blockIdx.x * 32LL + lane;
+  float* out = blockIdx.y ? db : dw;
+  if (!out) return;
+  const float* p = parts + blockIdx.y * k + j;
+  float t = 0.f;
+  if (j < k) {
+#pragma unroll 8
+    for (int c = warp; c < count; c += 8) t += p[c * 2 * k];
+  }
+  sums[warp][lane] = t;
+  __syncthreads();
+  if (warp == 0 && j < k) {
+    t = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) t += sums[w][lane];
+    out[j] = accumulate ? out[j] + t : t;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Threads to a row and pieces to a thread: a row is at most 16384 elements (32 FP32
+// values a thread), longer ones are not held.
+// ---------------------------------------------------------------------------
+struct NormShape {
+  int tpr, vpt;  // 0: too long
+};
+NormShape shape_of(int64_t k, int type, int64_t rows) {
+  const int v = 16 / type_bytes(type), most = 32 / v;  // pieces a thread at most
+  const int64_t pieces = (k + v - 1) / v;
+  // Few rows: more threads to each of them.
+  const bool few = rows <= 2 * static_cast<int64_t>(num_sms());
+  for (int tpr : {32, 128, 512}) {
+    if (few && tpr < 512 && pieces > tpr) continue;
+    for (int vpt = 1; vpt <= most; vpt *= 2)
+      if (pieces <= static_cast<int64_t>(tpr) * vpt) return {tpr, vpt};
+  }
+  return {0, 0};
+}
+
+template <int TYPE, bool ALIGNED, template <int, int, int, bool> class K>
+auto by_shape(NormShape s) {
+  switch (s.tpr * 16 + s.vpt) {
+    case 32 * 16 + 1: return K<TYPE, 32, 1, ALIGNED>::f();
+    case 32 * 16 + 2: return K<TYPE, 32, 2, ALIGNED>::f();
+    case 32 * 16 + 4: return K<TYPE, 32, 4, ALIGNED>::f();
+    case 128 * 16 + 1: return K<TYPE, 128, 1, ALIGNED>::f();
+    case 128 * 16 + 2: return K<TYPE, 128, 2, ALIGNED>::f();
+    case 128 * 16 + 4: return K<TYPE, 128, 4, ALIGNED>::f();
+    case 512 * 16 + 1: return K<TYPE, 512, 1, ALIGNED>::f();
+    case 512 * 16 + 2: return K<TYPE, 512, 2, ALIGNED>::f();
+    case 512 * 16 + 4: return K<TYPE, 512, 4, ALIGNED>::f();
+    default: break;
+  }
+  if constexpr (TYPE == OZ2_TYPE_F32) {
+    if (s.vpt == 8) return s.tpr == 32 ? K<TYPE, 32, 8, ALIGNED>::f() : s.tpr == 128 ? K<TYPE, 128, 8, ALIGNED>::f() : K<TYPE, 512, 8, ALIGNED>::f();
+  }
+  return decltype(K<TYPE, 32, 1, ALIGNED>::f())(nullptr);
+}
+template <int TYPE, int TPR, int VPT, bool ALIGNED>
+struct Forward {
+  static auto f() { return &norm_kernel<TYPE, TPR, VPT, ALIGNED>; }
+};
+template <int TYPE, int TPR, int VPT, bool ALIGNED>
+struct Backward {
+  static auto f() { return &norm_grad_kernel<TYPE, TPR, VPT, ALIGNED>; }
+};
+
+template <int TYPE>
+cudaError_t forward(const NormArgs& a, cudaStream_t st) {
+  const int es = type_bytes(TYPE);
+  const NormShape s = shape_of(a.k, TYPE, a.m);
+  count_launch();
+  if (!s.tpr) {
+    const unsigned blocks = static_cast<unsigned>(std::min<int64_t>(a.m, 4 * num_sms()));
+    return launch_dependent(norm_long_kernel<TYPE>, dim3(blocks), dim3(kNormThreads), 0, st, a);
+  }
+  const bool aligned = rows_on16(a.x, a.ldx, es) && rows_on16(a.y, a.ldy, es);
+  auto kern = aligned ? by_shape<TYPE, true, Forward>(s) : by_shape<TYPE, false, Forward>(s);
+  const int block = s.tpr < 128 ? 128 : s.tpr, groups = block / s.tpr;
+  const int64_t blocks = std::min<int64_t>((a.m + groups - 1) / groups, 0x7FFFFFFF);
+  return launch_dependent(kern, dim3(static_cast<unsigned>(blocks)), dim3(block), 0, st, a);
+}
+
+constexpr int64_t kColumnRows = 64;  // rows of a long row's chunk, at least
+
+int64_t long_chunk(int64_t m) { return std::max<int64_t>(kColumnRows, (m + 511) / 512); }
+int64_t grad_blocks(const NormGradArgs& a, NormShape s) {
+  if (!s.tpr) return (a.m + long_chunk(a.m) - 1) / long_chunk(a.m);
+  const int groups = kNormThreads / s.tpr;
+  return std::min<int64_t>((a.m + groups - 1) / groups, num_sms());
+}
+
+template <int TYPE>
+cudaError_t backward(const NormGradArgs& a, float* parts, cudaStream_t st) {
+  const int es = type_bytes(TYPE);
+  const NormShape s = shape_of(a.k, TYPE, a.m);
+  const bool want = a.dw || a.db;
+  const int64_t blocks = grad_blocks(a, s);
+  cudaError_t err = cudaSuccess;
+  if (!s.tpr) {
+    if (a.dx) {
+      count_launch();
+      err = launch_dependent(norm_grad_long_kernel<TYPE>, dim3(static_cast<unsigned>(std::min<int64_t>(a.m, 4 * num_sms()))),
+                             dim3(kNormThreads), 0, st, a);
+    }
+    if (want && err == cudaSuccess) {
+      const int64_t across = (a.k + 32 * Elem<TYPE>::V - 1) / (32 * Elem<TYPE>::V);
+      count_launch();
+      err = launch_dependent(norm_columns_kernel<TYPE>, dim3(static_cast<unsigned>(across), static_cast<unsigned>(blocks)),
+                             dim3(256), 0, st, a, long_chunk(a.m), parts);
+    }
+  } else {
+    const bool aligned = rows_on16(a.dy, a.lddy, es) && rows_on16(a.x, a.ldx, es) && (!a.r || rows_on16(a.r, a.ldr, es)) &&
+                         (!a.dx || rows_on16(a.dx, a.lddx, es));
+    auto kern = aligned ? by_shape<TYPE, true, Backward>(s) : by_shape<TYPE, false, Backward>(s);
+    const size_t smem = s.tpr < kNormThreads ? 2 * sizeof(float) * s.tpr * s.vpt * Elem<TYPE>::V : 0;
+    err = allow_smem(reinterpret_cast<const void*>(kern), smem);
+    if (err != cudaSuccess) return err;
+    count_launch();
+    err = launch_dependent(kern, dim3(static_cast<unsigned>(blocks)), dim3(kNormThreads), smem, st, a, want ? parts : nullptr);
+  }
+  if (err != cudaSuccess || !want) return err;
+  count_launch();
+  return launch_dependent(join_parts_kernel, dim3(static_cast<unsigned>((a.k + 31) / 32), 2), dim3(256), 0, st, a.k,
+                          static_cast<int>(blocks), static_cast<const float*>(parts), a.dw, a.db, a.accumulate);
+}
+
+}  // namespace
+
+cudaError_t launch_layer_norm(const NormArgs& a, int type, cudaStream_t st) {
+  return type == OZ2_TYPE_F32    ? forward<OZ2_TYPE_F32>(a, st)
+         : type == OZ2_TYPE_BF16 ? forward<OZ2_TYPE_BF16>(a, st)
+                                 : forward<OZ2_TYPE_F16>(a, st);
+}
+
+size_t layer_norm_grad_scratch(const NormGradArgs& a, int type) {
+  if (!a.dw && !a.db) return 0;
+  return sizeof(float) * 2 * static_cast<size_t>(a.k) * grad_blocks(a, shape_of(a.k, type, a.m));
+}
+
+cudaError_t launch_layer_norm_grad(const NormGradArgs& a, int type, void* scratch, cudaStream_t st) {
+  float* parts = static_cast<float*>(scratch);
+  return type == OZ2_TYPE_F32    ? backward<OZ2_TYPE_F32>(a, parts, st)
+         : type == OZ2_TYPE_BF16 ? backward<OZ2_TYPE_BF16>(a, parts, st)
+                                 : backward<OZ2_TYPE_F16>(a, parts, st);
+}
+
+}  // namespace oz2

@@ -1,0 +1,329 @@
+"""The binding of the operators at a language model's ends (include/oz2_lm.h):
+embedding, layer norm, and the losses over a vocabulary that are taken from the last
+layer's input and the head's weights, each with its gradient.
+
+Arrays are as in `layers`: row-major (tokens, features) with stride(1) == 1 and any
+row stride, all on the current device.  Tokens name rows by int64 or int32.  A call
+runs on the current stream, or on `stream`, whose memory its new outputs then are.  The
+forward passes record no graph of gradients: tensors that require them are refused
+unless that is off (torch.no_grad()).
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from .layers import GRAD_ACCUMULATE, TYPE, _ENTRIES, _done, _entry, _ld, _new, _stream
+
+_I64, _P, _I, _U, _F = ctypes.c_int64, ctypes.c_void_p, ctypes.c_int, ctypes.c_uint, ctypes.c_float
+GRAD_ONE_DLOSS = 0x2
+MAX_TOP = 1024
+IDS = {torch.int64: 64, torch.int32: 32}
+
+SIGS = {
+    "oz2_embedding": (_I, [_I64, _I64, _I64, _I, _P, _I, _P, _I64, _F, _P, _I64, _P]),
+    "oz2_embedding_grad": (_I, [_I64, _I64, _I64, _I, _P, _I64, _P, _I, _F, _P, _I64, _I, _U, _P]),
+    "oz2_layer_norm": (_I, [_I64, _I64, _I, _P, _I64, _P, _P, _I, _F, _I, _P, _I64, _P, _P, _P]),
+    "oz2_layer_norm_grad": (_I, [_I64, _I64, _I, _P, _I64, _P, _I64, _P, _P, _P, _I, _P, _I64, _P, _I64, _P, _P, _U, _P]),
+    "oz2_linear_xent": (_I, [_I64, _I64, _I64, _I, _P, _I64, _P, _I64, _P, _I, _F, _F, _P, _P, _P, _P]),
+    "oz2_linear_xent_grad": (_I, [_I64, _I64, _I64, _I, _P, _P, _I64, _P, _I64, _P, _I, _P, _F, _F, _P, _I64, _P, _I64,
+                                  _I, _U, _P]),
+    "oz2_linear_distill": (_I, [_I64, _I64, _I64, _I64, _I, _P, _I64, _P, _I64, _P, _I64, _I, _P, _I64, _I, _F, _P, _P,
+                                _P, _P]),
+    "oz2_linear_distill_grad": (_I, [_I64, _I64, _I64, _I64, _I, _P, _P, _I64, _P, _I64, _P, _I64, _I, _P, _I64, _I, _F,
+                                     _P, _P, _I64, _P, _I64, _I, _U, _P]),
+}
+
+
+def _lost(what, *tensors):
+    """Refuse to lose a gradient."""
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            assert not torch.is_grad_enabled(), f"a tensor requires its gradient, which would be lost: call {what} " \
+                f"under torch.no_grad(), and {what}_grad for the gradients"
+
+
+def _here(t, what):
+    assert t.is_cuda and t.get_device() == torch._C._cuda_getDevice(), f"{what}: oz2 operates on CUDA tensors of the " \
+        "current device"
+
+
+def _matrix(t, rows, cols, dtype, what):
+    """(address, row stride) of a matrix of this shape and dtype."""
+    assert t.shape == (rows, cols) and t.dtype == dtype, \
+        f"{what}: expected shape ({rows}, {cols}) and {dtype}, got {tuple(t.shape)} and {t.dtype}"
+    _here(t, what)
+    return t.data_ptr(), _ld(t, rows, cols, what)
+
+
+def _floats(t, count, what):
+    assert t.shape == (count,) and t.dtype == torch.float32 and t.is_contiguous(), \
+        f"{what}: expected {count} contiguous float32 values, got {tuple(t.shape)} and {t.dtype}"
+    _here(t, what)
+    return t.data_ptr()
+
+
+def _weights(t, k, dtype, what):
+    """(address, type) of a vector of k values of the rows' dtype or float32."""
+    assert t.shape == (k,) and (t.dtype == dtype or t.dtype == torch.float32) and t.is_contiguous(), \
+        f"{what}: expected {k} contiguous values of {dtype} or float32, got {tuple(t.shape)} and {t.dtype}"
+    _here(t, what)
+    return t.data_ptr(), TYPE[t.dtype]
+
+
+def _ids(t, count, what):
+    assert t.shape == (count,) and t.dtype in IDS and t.is_contiguous(), \
+        f"{what}: expected {count} contiguous int64 or int32 values, got {tuple(t.shape)} and {t.dtype}"
+    _here(t, what)
+    return t.data_ptr(), IDS[t.dtype]
+
+
+def _call(name, *args):
+    _done((_ENTRIES.get(name) or _entry(name))(*args), name)
+
+
+def _on(stream):
+    return _stream() if stream is None else stream.cuda_stream
+
+
+def oz2_embedding(ids, table, scale=1.0, out=None, stream=None):
+    """scale·table[ids] for tokens ids (m,) and a table (n, k) of float32, bfloat16 or
+    float16: (m, k) of its dtype.  ids below 0 (padding) give zeros, ids of n or more NaN."""
+    _lost("oz2_embedding", table)
+    n, k = table.shape
+    m, = ids.shape
+    dt = table.dtype
+    assert dt in TYPE and dt != torch.float8_e4m3fn, "table: expected float32, bfloat16 or float16"
+    ip, bits = _ids(ids, m, "ids")
+    tp, ldt = _matrix(table, n, k, dt, "table")
+    if out is None:
+        out = _new(table, (m, k), dt, stream)
+        op, ldo = out.data_ptr(), k or 1
+    else:
+        op, ldo = _matrix(out, m, k, dt, "out")
+    _call("oz2_embedding", m, n, k, TYPE[dt], ip, bits, tp, ldt, scale, op, ldo, _on(stream))
+    return out
+
+
+def oz2_embedding_grad(dy, ids, n, scale=1.0, out=None, out_dtype=None, accumulate=False, stream=None):
+    """The gradient (n, k) of oz2_embedding's table from dy (m, k): the sum of scale·dy_t over
+    each row's tokens, in dy's dtype or float32 (out_dtype).  With accumulate it is added to
+    `out`, whose other rows stay; else rows without tokens are zeros.  ids outside [0, n) count
+    for nothing."""
+    m, k = dy.shape
+    dt = dy.dtype
+    assert dt in TYPE and dt != torch.float8_e4m3fn, "dy: expected float32, bfloat16 or float16"
+    assert out is not None or not accumulate, "accumulate: out has to be given"
+    dp, ldd = _matrix(dy, m, k, dt, "dy")
+    ip, bits = _ids(ids, m, "ids")
+    if out is None:
+        ot = out_dtype or dt
+        out = _new(dy, (n, k), ot, stream)
+        op, ldo = out.data_ptr(), k or 1
+    else:
+        ot = out.dtype
+        assert out_dtype is None or out_dtype == ot, "out_dtype: out has another"
+        op, ldo = _matrix(out, n, k, ot, "out")
+    _call("oz2_embedding_grad", m, n, k, TYPE[dt], dp, ldd, ip, bits, scale, op, ldo, TYPE.get(ot, -1),
+          GRAD_ACCUMULATE if accumulate else 0, _on(stream))
+    return out
+
+
+def oz2_layer_norm(x, weight=None, bias=None, eps=1e-5, center=True, save_stats=False, out=None, stream=None):
+    """(x - mean)·rstd·weight + bias over the features of each row of x (m, k), of float32,
+    bfloat16 or float16; without the mean where not center (rstd is then that of the mean of
+    squares).  weight and bias (k,) have x's dtype or float32, both the same.  With
+    save_stats, returns (y, mean, rstd) with the float32 (m,) that oz2_layer_norm_grad wants
+    (mean None where not center).  `out` may be x itself."""
+    _lost("oz2_layer_norm", x, weight, bias)
+    m, k = x.shape
+    dt = x.dtype
+    assert dt in TYPE and dt != torch.float8_e4m3fn, "x: expected float32, bfloat16 or float16"
+    xp, ldx = _matrix(x, m, k, dt, "x")
+    wp = bp = mp = sp = mean = rstd = None
+    wt = 0
+    if weight is not None:
+        wp, wt = _weights(weight, k, dt, "weight")
+    if bias is not None:
+        bp, bt = _weights(bias, k, dt, "bias")
+        assert weight is None or bt == wt, "weight and bias: expected one dtype"
+        wt = bt
+    if out is None:
+        out = _new(x, (m, k), dt, stream)
+        op, ldo = out.data_ptr(), k or 1
+    else:
+        op, ldo = _matrix(out, m, k, dt, "out")
+    if save_stats:
+        rstd = _new(x, (m,), torch.float32, stream)
+        sp = rstd.data_ptr()
+        if center:
+            mean = _new(x, (m,), torch.float32, stream)
+            mp = mean.data_ptr()
+    _call("oz2_layer_norm", m, k, TYPE[dt], xp, ldx, wp, bp, wt, eps, 1 if center else 0, op, ldo, mp, sp, _on(stream))
+    return (out, mean, rstd) if save_stats else out
+
+
+def oz2_layer_norm_grad(dy, x, mean, rstd, weight=None, residual=None, need=("dx", "dweight", "dbias"), dx=None,
+                        dweight=None, dbias=None, accumulate=False, stream=None):
+    """(dx, dweight, dbias) of oz2_layer_norm from dy, its x, and the mean (None: not centred)
+    and rstd that it kept.  residual (m, k), the gradient that comes by a skip connection, is
+    added to dx (which may be given as the same tensor).  `need` names the gradients wanted (the
+    others are None).  dx has x's dtype, dweight and dbias (k,) are float32; with accumulate those
+    two are added to, and must be given."""
+    m, k = x.shape
+    dt = x.dtype
+    assert dt in TYPE and dt != torch.float8_e4m3fn, "x: expected float32, bfloat16 or float16"
+    dp, ldd = _matrix(dy, m, k, dt, "dy")
+    xp, ldx = _matrix(x, m, k, dt, "x")
+    mp = _floats(mean, m, "mean") if mean is not None else None
+    sp = _floats(rstd, m, "rstd")
+    wp = rp = op = gp = bp = None
+    wt, ldr, ldo = 0, 1, k or 1
+    if weight is not None:
+        wp, wt = _weights(weight, k, dt, "weight")
+    if residual is not None:
+        rp, ldr = _matrix(residual, m, k, dt, "residual")
+    assert not accumulate or (("dweight" not in need or dweight is not None) and ("dbias" not in need or dbias is not None)), \
+        "accumulate: dweight and dbias have to be given"
+    if "dx" not in need:
+        dx = None
+    elif dx is None:
+        dx = _new(x, (m, k), dt, stream)
+        op = dx.data_ptr()
+    else:
+        op, ldo = _matrix(dx, m, k, dt, "dx")
+    if "dweight" not in need:
+        dweight = None
+    elif dweight is None:
+        dweight = _new(x, (k,), torch.float32, stream)
+        gp = dweight.data_ptr()
+    else:
+        gp = _floats(dweight, k, "dweight")
+    if "dbias" not in need:
+        dbias = None
+    elif dbias is None:
+        dbias = _new(x, (k,), torch.float32, stream)
+        bp = dbias.data_ptr()
+    else:
+        bp = _floats(dbias, k, "dbias")
+    _call("oz2_layer_norm_grad", m, k, TYPE[dt], dp, ldd, xp, ldx, mp, sp, wp, wt, rp, ldr, op, ldo, gp, bp,
+          GRAD_ACCUMULATE if accumulate else 0, _on(stream))
+    return dx, dweight, dbias
+
+
+def _head(x, w):
+    """Sizes and addresses of a head's input and weights."""
+    m, k = x.shape
+    n, k2 = w.shape
+    dt = x.dtype
+    assert k == k2 and w.dtype == dt, "x and w: expected (m, k) and (n, k) of one dtype"
+    assert dt == torch.bfloat16 or dt == torch.float16, "x and w: expected bfloat16 or float16"
+    _here(x, "x")
+    _here(w, "w")
+    return m, n, k, dt, x.data_ptr(), _ld(x, m, k, "x"), w.data_ptr(), _ld(w, n, k, "w")
+
+
+def _entries(ids, teacher, m):
+    """(entries of a token, the arguments of a teacher's rows and logits)."""
+    assert ids.dim() == 2 and ids.shape[0] == m and ids.dtype in IDS, \
+        f"ids: expected shape ({m}, top) of int64 or int32, got {tuple(ids.shape)} and {ids.dtype}"
+    top = ids.shape[1]
+    assert 1 <= top <= MAX_TOP, f"ids: expected 1 to {MAX_TOP} entries a token"
+    ip, ldi = _matrix(ids, m, top, ids.dtype, "ids")
+    assert teacher.dtype in TYPE and teacher.dtype != torch.float8_e4m3fn, "teacher: expected float32, bfloat16 or float16"
+    tp, ldt = _matrix(teacher, m, top, teacher.dtype, "teacher")
+    return top, (ip, ldi, IDS[ids.dtype], tp, ldt, TYPE[teacher.dtype])
+
+
+def oz2_linear_xent(x, w, targets, scale=1.0, z_loss=0.0, stream=None):
+    """Cross entropy over the rows of w (n, k) of tokens x (m, k), bfloat16 or float16, with
+    logits z = scale·x·wᵀ that are not kept: (loss, lse, picked), float32 (m,) each, with
+    loss = lse - picked + z_loss·lse², lse = log Σ exp z and picked the target's z.
+    targets (m,) below 0 do not count (loss and picked 0); of n or more: NaN."""
+    _lost("oz2_linear_xent", x, w)
+    m, n, k, dt, xp, ldx, wp, ldw = _head(x, w)
+    ip, bits = _ids(targets, m, "targets")
+    loss, lse, picked = (_new(x, (m,), torch.float32, stream) for _ in range(3))
+    _call("oz2_linear_xent", m, n, k, TYPE[dt], xp, ldx, wp, ldw, ip, bits, scale, z_loss, loss.data_ptr(),
+          lse.data_ptr(), picked.data_ptr(), _on(stream))
+    return loss, lse, picked
+
+
+def _outputs(x, w, m, n, k, dt, need, dx, dw, dw_dtype, accumulate, stream):
+    """(dx, dw, their arguments) of a head's gradient."""
+    assert not accumulate or "dw" not in need or dw is not None, "accumulate: dw has to be given"
+    xp = wp = None
+    ldx = ldw = k or 1
+    wt = TYPE[dt]
+    if "dx" not in need:
+        dx = None
+    elif dx is None:
+        dx = _new(x, (m, k), dt, stream)
+        xp = dx.data_ptr()
+    else:
+        xp, ldx = _matrix(dx, m, k, dt, "dx")
+    if "dw" not in need:
+        dw = None
+    elif dw is None:
+        dw = _new(x, (n, k), dw_dtype or dt, stream)
+        wp, wt = dw.data_ptr(), TYPE.get(dw.dtype, -1)
+    else:
+        wp, ldw = _matrix(dw, n, k, dw.dtype, "dw")
+        wt = TYPE.get(dw.dtype, -1)
+    return dx, dw, (xp, ldx, wp, ldw, wt)
+
+
+def _dloss(dloss, m):
+    """(address, flags) of the losses' gradient: float32, one a token or one for all."""
+    if dloss.dim() == 0 or (dloss.dim() == 1 and dloss.shape[0] == m and m > 1 and dloss.stride(0) == 0):
+        assert dloss.dtype == torch.float32, "dloss: expected float32"
+        _here(dloss, "dloss")
+        return dloss.data_ptr(), GRAD_ONE_DLOSS
+    return _floats(dloss, m, "dloss"), 0
+
+
+def oz2_linear_xent_grad(dloss, x, w, targets, lse, scale=1.0, z_loss=0.0, need=("dx", "dw"), dx=None, dw=None,
+                         dw_dtype=None, accumulate=False, stream=None):
+    """(dx, dw) of oz2_linear_xent from dloss, float32 (m,) or a scalar that goes for every
+    token, and the lse that it kept.  `need` names the gradients wanted (the others are None).
+    dx (m, k) has x's dtype, dw (n, k) that or float32 (dw_dtype); each may be given as the tensor
+    to write.  With accumulate, dw (float32) is added to, and must be given."""
+    m, n, k, dt, xp, ldx, wp, ldw = _head(x, w)
+    ip, bits = _ids(targets, m, "targets")
+    lp = _floats(lse, m, "lse")
+    gp, flags = _dloss(dloss, m)
+    dx, dw, outs = _outputs(x, w, m, n, k, dt, need, dx, dw, dw_dtype, accumulate, stream)
+    _call("oz2_linear_xent_grad", m, n, k, TYPE[dt], gp, xp, ldx, wp, ldw, ip, bits, lp, scale, z_loss, *outs,
+          flags | (GRAD_ACCUMULATE if accumulate else 0), _on(stream))
+    return dx, dw
+
+
+def oz2_linear_distill(x, w, ids, teacher, temperature=1.0, stream=None):
+    """The loss against a teacher's logits of `top` listed rows of each token, ids and teacher
+    (m, top), with logits z = x·wᵀ/temperature that are not kept: (loss, lse, picked) with
+    loss = Σ q·(log q - z_id) + lse, q the softmax of teacher/temperature over the token's listed
+    rows, lse = log Σ exp z, float32 (m,), and picked the listed rows' z, float32 (m, top).  ids
+    below 0 list nothing (picked 0); a token without rows does not count (loss 0); an id of n or
+    more gives NaN.  x and w as for oz2_linear_xent, teacher float32, bfloat16 or float16."""
+    _lost("oz2_linear_distill", x, w, teacher)
+    m, n, k, dt, xp, ldx, wp, ldw = _head(x, w)
+    top, listed = _entries(ids, teacher, m)
+    loss, lse = _new(x, (m,), torch.float32, stream), _new(x, (m,), torch.float32, stream)
+    picked = _new(x, (m, top), torch.float32, stream)
+    _call("oz2_linear_distill", m, n, k, top, TYPE[dt], xp, ldx, wp, ldw, *listed, temperature, loss.data_ptr(),
+          lse.data_ptr(), picked.data_ptr(), _on(stream))
+    return loss, lse, picked
+
+
+def oz2_linear_distill_grad(dloss, x, w, ids, teacher, lse, temperature=1.0, need=("dx", "dw"), dx=None, dw=None,
+                            dw_dtype=None, accumulate=False, stream=None):
+    """(dx, dw) of oz2_linear_distill, as oz2_linear_xent_grad's."""
+    m, n, k, dt, xp, ldx, wp, ldw = _head(x, w)
+    top, listed = _entries(ids, teacher, m)
+    lp = _floats(lse, m, "lse")
+    gp, flags = _dloss(dloss, m)
+    dx, dw, outs = _outputs(x, w, m, n, k, dt, need, dx, dw, dw_dtype, accumulate, stream)
+    _call("oz2_linear_distill_grad", m, n, k, top, TYPE[dt], gp, xp, ldx, wp, ldw, *listed, temperature, lp, *outs,
+          flags | (GRAD_ACCUMULATE if accumulate else 0), _on(stream))
+    return dx, dw
