@@ -120,7 +120,8 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_tokens_kernel(SortJob s,
   }
   uint32_t* mine = sort_smem + warp * kDigits;             // this warp's counts, then its next places
   uint32_t* total = sort_smem + kSortWarps * kDigits;      // the block's
-  uint32_t* scan = total + kDigits;
+  uint32_t* base = total + kDigits;                        // the first places of the block's pairs of a digit
+  __shared__ uint32_t sums[kSortWarps];
   const uint32_t rank = sorters > 1 ? cluster_ctarank() : 0, blocks = sorters;
   if (rank == 0 && threadIdx.x == 0) *s.long_runs = 0;
   const int64_t each = ((s.m + blocks * kSortWarps - 1) / (blocks * kSortWarps) + 31) / 32 * 32;
@@ -134,16 +135,29 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_tokens_kernel(SortJob s,
       const int64_t id = s.ids[i];
       return make_uint2(id < 0 || id >= s.n ? s.n : static_cast<uint32_t>(id), static_cast<uint32_t>(i));
     };
+    // A lane's pairs, eight at a time: read once where a warp's stretch is that short.
+    constexpr int kHeld = 8;
+    const bool once = i1 - i0 <= 32 * kHeld;
+    uint2 held[kHeld];
+    auto load = [&](int64_t i) {
+#pragma unroll
+      for (int q = 0; q < kHeld; ++q)
+        if (i + 32 * q + lane < i1) held[q] = pair(i + 32 * q + lane);
+    };
     for (int d = lane; d < digits; d += 32) mine[d] = 0;
     __syncwarp();
-#pragma unroll 4
-    for (int64_t i = i0 + lane; i < i1; i += 32) atomicAdd(mine + (pair(i).x >> shift & (digits - 1)), 1u);
+    for (int64_t i = i0; i < i1; i += 32 * kHeld) {
+      load(i);
+#pragma unroll
+      for (int q = 0; q < kHeld; ++q)
+        if (i + 32 * q + lane < i1) atomicAdd(mine + (held[q].x >> shift & (digits - 1)), 1u);
+    }
     __syncthreads();
     // Places: of the pairs of smaller digits, of the blocks before, of the warps before.
     const int d = threadIdx.x;
     uint32_t sum = 0;
     if (d < digits) {
-#pragma unroll 8
+#pragma unroll
       for (int w = 0; w < kSortWarps; ++w) {
         const uint32_t c = sort_smem[w * kDigits + d];
         sort_smem[w * kDigits + d] = sum;
@@ -156,7 +170,8 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_tokens_kernel(SortJob s,
       cluster_sync_all();
       if (d < digits) {
         all = 0;
-        for (uint32_t b = 0; b < blocks; ++b) {
+#pragma unroll
+        for (uint32_t b = 0; b < kSortCluster; ++b) {
           uint32_t v;
           asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(mapa_shared(smem_u32(total + d), b)));
           if (b < rank) before += v;
@@ -171,37 +186,36 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_tokens_kernel(SortJob s,
       const uint32_t v = __shfl_up_sync(0xffffffffu, inc, o);
       if (lane >= o) inc += v;
     }
-    if (lane == 31) scan[warp] = inc;
+    if (lane == 31) sums[warp] = inc;
     __syncthreads();
     if (warp == 0) {
-      uint32_t v = scan[lane], t = v;
+      uint32_t v = sums[lane], t = v;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const uint32_t u = __shfl_up_sync(0xffffffffu, t, o);
         if (lane >= o) t += u;
       }
-      scan[lane] = t - v;
+      sums[lane] = t - v;
     }
     __syncthreads();
-    if (d < digits) {
-      const uint32_t base = scan[warp] + inc - all + before;
-#pragma unroll 8
-      for (int w = 0; w < kSortWarps; ++w) sort_smem[w * kDigits + d] += base;
-    }
+    if (d < digits) base[d] = sums[warp] + inc - all + before;
     __syncthreads();
-    for (int64_t i = i0; i < i1; i += 32) {
-      const bool there = i + lane < i1;
-      const uint2 p = there ? pair(i + lane) : make_uint2(0, 0);
-      const uint32_t digit = there ? p.x >> shift & (digits - 1) : kDigits + lane;
-      const uint32_t same = __match_any_sync(0xffffffffu, digit);
-      const uint32_t at = there ? mine[digit] : 0;
-      __syncwarp();
-      if (there) {
-        const int ahead = __popc(same & ((1u << lane) - 1));
-        if (ahead == 0) mine[digit] = at + __popc(same);
-        __stcg(to + at + ahead, p);
+    for (int64_t i = i0; i < i1; i += 32 * kHeld) {
+      if (!once) load(i);
+#pragma unroll
+      for (int q = 0; q < kHeld; ++q) {
+        if (i + 32 * q >= i1) break;
+        const bool there = i + 32 * q + lane < i1;
+        const uint32_t digit = there ? held[q].x >> shift & (digits - 1) : kDigits + lane;
+        const uint32_t same = __match_any_sync(0xffffffffu, digit);
+        const uint32_t at = there ? mine[digit] : 0, ahead = __popc(same & ((1u << lane) - 1));
+        __syncwarp();
+        if (there) {
+          if (ahead == 0) mine[digit] = at + __popc(same);
+          __stcg(to + base[digit] + at + ahead, held[q]);
+        }
+        __syncwarp();
       }
-      __syncwarp();
     }
     uint2* t = from;
     from = to;
@@ -229,13 +243,14 @@ constexpr int kChunkPairs = 16, kLongRun = 32, kSumWarps = 8;
 // The rows around a chunk: the 32 pairs before it and the 64 from its first on.
 struct Window {
   uint32_t before, a, b;  // rows (n where there is no pair)
-  uint32_t ta, tb;        // tokens
-  __device__ __forceinline__ void load(const uint2* sorted, int64_t m, uint32_t n, int64_t p0, int lane) {
+  __device__ __forceinline__ void load(const uint2* sorted, int64_t m, uint32_t n, int64_t p0, int lane, uint2* pairs) {
     const int64_t p = p0 - 32 + lane;
     before = p >= 0 ? __ldg(&sorted[p].x) : 0xFFFFFFFFu;
     const uint2 none = make_uint2(n, 0), u = p0 + lane < m ? __ldg(sorted + p0 + lane) : none,
                 v = p0 + 32 + lane < m ? __ldg(sorted + p0 + 32 + lane) : none;
-    a = u.x, ta = u.y, b = v.x, tb = v.y;
+    a = u.x, b = v.x;
+    pairs[lane] = u, pairs[32 + lane] = v;
+    __syncwarp();
   }
   __device__ __forceinline__ uint32_t row(int i) const { return __shfl_sync(0xffffffffu, a, i); }  // i < 32
   // Pairs of row r from place i on (of which it holds).
@@ -247,44 +262,54 @@ struct Window {
     const uint32_t other = ~__ballot_sync(0xffffffffu, before == r);
     return __clz(static_cast<int>(other));
   }
-  __device__ __forceinline__ uint32_t token(int i) const {
-    const uint32_t x = __shfl_sync(0xffffffffu, ta, i & 31), y = __shfl_sync(0xffffffffu, tb, i & 31);
-    return i < 32 ? x : y;
-  }
 };
 
-template <int TYPE, int OUT>
-__device__ __forceinline__ void finish_row(void* dE, int64_t row, int64_t ldde, int64_t col, int n, float scale,
-                                           bool accumulate, bool vec, float (&s)[Elem<TYPE>::V]) {
+// A piece of a row of dE from its sums: stored, or added to what is there.  Each is added
+// to once, so an FP32 one can be left to the memory (a vector reduction; a result below
+// 2^-126 counts as 0), which spares the way there and back; a 16-bit one is read (`old`,
+// ahead) and rounded once.
+template <int TYPE, int OUT, bool ADD>
+__device__ __forceinline__ void finish_piece(void* dE, int64_t row, int64_t ldde, int64_t col, int n, float scale, bool vec,
+                                             uint4 old, const float* sums) {
+  using Y = Elem<OUT>;
   constexpr int V = Elem<TYPE>::V;
+  typename Y::T* p = static_cast<typename Y::T*>(dE) + row * ldde + col;
 #pragma unroll
-  for (int e = 0; e < V; ++e) s[e] *= scale;
-  if constexpr (OUT == TYPE) {
-    using X = Elem<TYPE>;
-    typename X::T* p = static_cast<typename X::T*>(dE) + row * ldde + col;
-    if (accumulate) {
-      float o[V];
-      X::unpack(vec && n >= V ? *reinterpret_cast<const uint4*>(p) : load16_singly<false>(p, n), o);
+  for (int h = 0; h < V; h += Y::V) {
+    float o[Y::V];
 #pragma unroll
-      for (int e = 0; e < V; ++e) s[e] += o[e];
-    }
-    store16_any(p, X::pack(s), n, vec && n >= V);
-  } else {  // F32 from 16 bits
-    float* p = static_cast<float*>(dE) + row * ldde + col;
-    if (vec && n >= V) {
+    for (int e = 0; e < Y::V; ++e) o[e] = sums[h + e] * scale;
+    if constexpr (ADD && OUT == OZ2_TYPE_F32) {
+      if (vec && n >= h + 4) {
+        asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p + h), "f"(o[0]), "f"(o[1]), "f"(o[2]),
+                     "f"(o[3])
+                     : "memory");
+      } else {
 #pragma unroll
-      for (int h = 0; h < V; h += 4) {
-        float4 o = accumulate ? *reinterpret_cast<const float4*>(p + h) : make_float4(0, 0, 0, 0);
-        o.x += s[h], o.y += s[h + 1], o.z += s[h + 2], o.w += s[h + 3];
-        *reinterpret_cast<float4*>(p + h) = o;
+        for (int e = 0; e < 4; ++e)
+          if (h + e < n) atomicAdd(reinterpret_cast<float*>(p) + h + e, o[e]);
       }
     } else {
+      if constexpr (ADD) {
+        float was[Y::V];
+        Y::unpack(old, was);
 #pragma unroll
-      for (int e = 0; e < V; ++e)
-        if (e < n) p[e] = accumulate ? p[e] + s[e] : s[e];
+        for (int e = 0; e < Y::V; ++e) o[e] = fmaf(sums[h + e], scale, was[e]);
+      }
+      store16_any(p + h, Y::pack(o), n - h, vec && n >= h + Y::V);
     }
   }
 }
+template <int OUT>
+__device__ __forceinline__ uint4 old_piece(const void* dE, int64_t row, int64_t ldde, int64_t col, int n, bool vec) {
+  using T = typename Elem<OUT>::T;
+  const T* p = static_cast<const T*>(dE) + row * ldde + col;
+  return vec && n >= Elem<OUT>::V ? *reinterpret_cast<const uint4*>(p) : load16_singly<false>(p, n);
+}
+
+// Pieces of a row to a lane: up to 16 FP32 sums.  (One a lane, the work on the pairs took
+// longer than the rows: 65536 tokens of 2048 f32 398 us.)
+constexpr int most_pieces(int type) { return type == OZ2_TYPE_F32 ? 4 : 2; }
 
 struct SumJob {
   int64_t m, k;
@@ -296,17 +321,18 @@ struct SumJob {
   float scale;
   int accumulate, vec;     // vec: dE's rows are on 16-byte boundaries
   const uint2* sorted;
-  float* parts;            // two rows a chunk, `slices` pieces of 32 lanes' values each
+  float* parts;            // two rows a chunk, of `slices` whole slices
   int2* runs;              // long runs: first chunk, and how many chunks
   int* long_runs;
-  int slices;
+  int slices, pieces;      // of a row, and of a slice to a lane
 };
 
-template <int TYPE, int OUT, bool ALIGNED>
+template <int TYPE, int OUT, int P, bool ALIGNED, bool ADD>
 __global__ void __launch_bounds__(32 * kSumWarps) sum_runs_kernel(SumJob j) {
   using X = Elem<TYPE>;
   using T = typename X::T;
   constexpr int V = X::V;
+  __shared__ uint2 pairs_s[kSumWarps][64];
   pdl_trigger();
   pdl_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -314,89 +340,136 @@ __global__ void __launch_bounds__(32 * kSumWarps) sum_runs_kernel(SumJob j) {
   const int slice = static_cast<int>(unit - chunk * j.slices);
   const int64_t p0 = chunk * kChunkPairs;
   if (p0 >= j.m) return;
+  const uint2* pairs = pairs_s[warp];
   Window w;
-  w.load(j.sorted, j.m, j.n, p0, lane);
-  const int64_t col = (static_cast<int64_t>(slice) * 32 + lane) * V;
-  const int n = static_cast<int>(max(int64_t(0), min(int64_t(V), j.k - col)));
+  w.load(j.sorted, j.m, j.n, p0, lane, pairs_s[warp]);
+  const int64_t col0 = (static_cast<int64_t>(slice) * P * 32 + lane) * V;
+  auto col = [&](int i) { return col0 + i * 32 * V; };
+  auto there = [&](int i) { return static_cast<int>(max(int64_t(0), min(int64_t(V), j.k - col(i)))); };
   const T* src = static_cast<const T*>(j.dY);
-  const T* end = src + (j.m - 1) * j.lddy + j.k;
-  float s[V];
-  auto add = [&](int from, int to) {
-#pragma unroll
-    for (int e = 0; e < V; ++e) s[e] = 0.f;
-    for (; from < to; from += 8) {
-      uint4 v[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int64_t t = w.token(min(from + i, to - 1));
-        v[i] = make_uint4(0, 0, 0, 0);
-        if (from + i < to && n > 0) v[i] = load_piece<ALIGNED>(src + t * j.lddy + col, src, end, n);
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float f[V];
-        X::unpack(v[i], f);
-        if (from + i < to) {
-#pragma unroll
-          for (int e = 0; e < V; ++e) s[e] += f[e];
-        }
-      }
-    }
-  };
-  auto keep = [&](int which) {
-    float* p = j.parts + ((2 * chunk + which) * j.slices + slice) * (32 * V) + lane * V;
-#pragma unroll
-    for (int h = 0; h < V; h += 4) *reinterpret_cast<float4*>(p + h) = make_float4(s[h], s[h + 1], s[h + 2], s[h + 3]);
-  };
-  int i = 0;
+  const T* stop = src + (j.m - 1) * j.lddy + j.k;
+  // What of the window is this warp's: from `begin` on (what lies before is a run's that
+  // started before) to `end`, a part of such a run that is long up to `head`, and a long
+  // run's first part from where the last one started.
   uint32_t r = w.row(0);
   if (r >= j.n) return;
+  int begin = 0, head = 0;
   const int behind = w.behind(r);
-  if (behind) {  // a run that started before: another warp's, or a part of a long one
+  if (behind) {
     const int here = w.count(r, 0);
     if (behind + here > kLongRun) {
-      add(0, min(here, kChunkPairs));
-      keep(0);
+      head = min(here, kChunkPairs);
+    } else {
+      begin = here;
     }
-    i = here;
   }
-  while (i < kChunkPairs) {
-    r = w.row(i);
-    if (r >= j.n) return;
-    const int here = w.count(r, i);
-    if (here > kLongRun) {
-      add(i, kChunkPairs);
-      keep(1);
-      if (slice == 0) {  // how many chunks it reaches: those whose first pair is its
-        int64_t c = chunk + 1;
-        for (;;) {
-          const int64_t p = (c + lane) * kChunkPairs;
-          const uint32_t in = __ballot_sync(0xffffffffu, p < j.m && __ldg(&j.sorted[p < j.m ? p : 0].x) == r);
-          c += __popc(in);
-          if (in != 0xFFFFFFFFu) break;
-        }
-        if (lane == 0) j.runs[atomicAdd(j.long_runs, 1)] = make_int2(static_cast<int>(chunk), static_cast<int>(c - chunk));
+  if (begin >= kChunkPairs) return;
+  const uint32_t valid = __ballot_sync(0xffffffffu, w.a < j.n);
+  r = w.row(kChunkPairs - 1);
+  int end = kChunkPairs, tail = 0;
+  if (r < j.n) {  // the last run that starts here, or goes through
+    const int last = __ffs(__ballot_sync(0xffffffffu, w.a == r)) - 1, here = w.count(r, last);
+    if (last > 0 || !behind) {
+      if (here > kLongRun) {
+        tail = 1;
+      } else {
+        end = last + here;
       }
-      return;
     }
-    add(i, i + here);
-    if (n > 0) finish_row<TYPE, OUT>(j.dE, r, j.ldde, col, n, j.scale, j.accumulate, j.vec, s);
-    i += here;
+  } else {
+    end = __popc(valid);
+  }
+  // Places whose pair is the last of its row.
+  const uint32_t after = __shfl_down_sync(0xffffffffu, w.a, 1), b0 = __shfl_sync(0xffffffffu, w.b, 0),
+                 after_b = __shfl_down_sync(0xffffffffu, w.b, 1);
+  const uint64_t ends = __ballot_sync(0xffffffffu, w.a != (lane < 31 ? after : b0)) |
+                        static_cast<uint64_t>(__ballot_sync(0xffffffffu, lane < 31 && w.b != after_b)) << 32;
+  float s[P][V];
+  auto clear = [&] {
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+#pragma unroll
+      for (int e = 0; e < V; ++e) s[i][e] = 0.f;
+  };
+  auto keep = [&](int which) {
+    float* p = j.parts + ((2 * chunk + which) * j.slices + slice) * (32 * P * V) + lane * V;
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+#pragma unroll
+      for (int h = 0; h < V; h += 4)
+        *reinterpret_cast<float4*>(p + i * 32 * V + h) = make_float4(s[i][h], s[i][h + 1], s[i][h + 2], s[i][h + 3]);
+  };
+  clear();
+  // Several pairs at a time, whatever rows they are of: all loads are under way before the
+  // first is added, and so are the old values of 16-bit rows that are added to.
+  constexpr bool kOld = ADD && OUT != OZ2_TYPE_F32;
+  constexpr int kAtOnce = 16 / P / (kOld ? 2 : 1);
+  for (int i = begin; i < end; i += kAtOnce) {
+    uint4 v[kAtOnce][P], old[kOld ? kAtOnce : 1][P];
+#pragma unroll
+    for (int q = 0; q < kAtOnce; ++q) {
+      const int at = min(i + q, end - 1);
+      const uint2 pair = pairs[at];
+      const T* row = src + static_cast<int64_t>(pair.y) * j.lddy;
+#pragma unroll
+      for (int c = 0; c < P; ++c) {
+        const int n = there(c);
+        if (n > 0 && i + q < end) v[q][c] = load_piece<ALIGNED>(row + col(c), src, stop, n);
+        if (kOld && n > 0 && i + q < end && (ends >> at & 1) && at >= head)
+          old[kOld ? q : 0][c] = old_piece<OUT>(j.dE, pair.x, j.ldde, col(c), n, j.vec);
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < kAtOnce; ++q) {
+      const int at = i + q;
+      if (at >= end) break;
+#pragma unroll
+      for (int c = 0; c < P; ++c) {
+        float f[V];
+        X::unpack(v[q][c], f);
+#pragma unroll
+        for (int e = 0; e < V; ++e) s[c][e] += f[e];
+      }
+      if (at + 1 == head) {
+        keep(0);
+        clear();
+      } else if (ends >> at & 1) {
+#pragma unroll
+        for (int c = 0; c < P; ++c)
+          if (there(c) > 0)
+            finish_piece<TYPE, OUT, ADD>(j.dE, pairs[at].x, j.ldde, col(c), there(c), j.scale, j.vec, old[kOld ? q : 0][c], s[c]);
+        clear();
+      }
+    }
+  }
+  if (!tail) return;
+  keep(1);
+  if (slice == 0) {  // how many chunks the run reaches: those whose first pair is its
+    int64_t c = chunk + 1;
+    for (;;) {
+      const int64_t p = (c + lane) * kChunkPairs;
+      const uint32_t in = __ballot_sync(0xffffffffu, p < j.m && __ldg(&j.sorted[p < j.m ? p : 0].x) == r);
+      c += __popc(in);
+      if (in != 0xFFFFFFFFu) break;
+    }
+    if (lane == 0) j.runs[atomicAdd(j.long_runs, 1)] = make_int2(static_cast<int>(chunk), static_cast<int>(c - chunk));
   }
 }
 
-// The parts of a long run, 512 bytes' worth of its columns to a block: each warp adds up
-// a stretch of them, and the warps' sums are added in order.
-template <int TYPE, int OUT>
+// The parts of a long run, 32·V of its columns to a block: each warp adds up a stretch of
+// them, and the warps' sums are added in order.
+template <int TYPE, int OUT, bool ADD>
 __global__ void __launch_bounds__(32 * kSumWarps) join_runs_kernel(SumJob j) {
   constexpr int V = Elem<TYPE>::V;
   __shared__ float sums[kSumWarps][32 * V];
   pdl_trigger();
   pdl_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t units = static_cast<int64_t>(*j.long_runs) * j.slices;
+  const int pieces = static_cast<int>((j.k + 32 * V - 1) / (32 * V));
+  const int64_t row_floats = static_cast<int64_t>(j.slices) * j.pieces * 32 * V;
+  const int64_t units = static_cast<int64_t>(*j.long_runs) * pieces;
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-    const int run = static_cast<int>(u / j.slices), slice = static_cast<int>(u - static_cast<int64_t>(run) * j.slices);
+    const int run = static_cast<int>(u / pieces), piece = static_cast<int>(u - static_cast<int64_t>(run) * pieces);
     const int64_t chunk = j.runs[run].x;
     const int chunks = j.runs[run].y, each = (chunks + kSumWarps - 1) / kSumWarps;
     const int c0 = min(chunks, warp * each), c1 = min(chunks, c0 + each);
@@ -405,7 +478,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) join_runs_kernel(SumJob j) {
     for (int e = 0; e < V; ++e) s[e] = 0.f;
 #pragma unroll 4
     for (int c = c0; c < c1; ++c) {
-      const float* p = j.parts + ((2 * (chunk + c) + (c == 0)) * j.slices + slice) * (32 * V) + lane * V;
+      const float* p = j.parts + (2 * (chunk + c) + (c == 0)) * row_floats + (static_cast<int64_t>(piece) * 32 + lane) * V;
 #pragma unroll
       for (int h = 0; h < V; h += 4) {
         const float4 v = *reinterpret_cast<const float4*>(p + h);
@@ -420,34 +493,58 @@ __global__ void __launch_bounds__(32 * kSumWarps) join_runs_kernel(SumJob j) {
       for (int o = 1; o < kSumWarps; ++o)
 #pragma unroll
         for (int e = 0; e < V; ++e) s[e] += sums[o][lane * V + e];
-      const int64_t col = (static_cast<int64_t>(slice) * 32 + lane) * V;
+      const int64_t col = (static_cast<int64_t>(piece) * 32 + lane) * V;
       const int n = static_cast<int>(max(int64_t(0), min(int64_t(V), j.k - col)));
       const uint32_t r = j.sorted[(chunk + 1) * kChunkPairs - 1].x;  // the chunk's last pair is the run's
-      if (n > 0) finish_row<TYPE, OUT>(j.dE, r, j.ldde, col, n, j.scale, j.accumulate, j.vec, s);
+      if (n > 0) {
+        uint4 old = make_uint4(0, 0, 0, 0);
+        if (ADD && OUT != OZ2_TYPE_F32) old = old_piece<OUT>(j.dE, r, j.ldde, col, n, j.vec);
+        finish_piece<TYPE, OUT, ADD>(j.dE, r, j.ldde, col, n, j.scale, j.vec, old, s);
+      }
     }
   }
 }
 
-int64_t slices_of(int64_t k, int type) { return (k * type_bytes(type) + 511) / 512; }
+// Pieces to a lane, and the slices of a row that come of it.
+int pieces_of(int64_t k, int type) {
+  const int64_t all = (k * type_bytes(type) + 511) / 512;
+  const int most = most_pieces(type);
+  return all >= most ? most : all >= 2 ? 2 : 1;
+}
+int64_t slices_of(int64_t k, int type) {
+  const int64_t bytes = 512 * pieces_of(k, type);
+  return (k * type_bytes(type) + bytes - 1) / bytes;
+}
 int64_t chunks_of(int64_t m) { return (m + kChunkPairs - 1) / kChunkPairs; }
 size_t up(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
+using SumKernel = void (*)(SumJob);
+template <int TYPE, int OUT, int P>
+SumKernel sum_kernel_of(bool aligned, bool add) {
+  return aligned ? (add ? sum_runs_kernel<TYPE, OUT, P, true, true> : sum_runs_kernel<TYPE, OUT, P, true, false>)
+                 : (add ? sum_runs_kernel<TYPE, OUT, P, false, true> : sum_runs_kernel<TYPE, OUT, P, false, false>);
+}
+template <int TYPE, int OUT>
+SumKernel sum_kernel(int pieces, bool aligned, bool add) {
+  return pieces == 1   ? sum_kernel_of<TYPE, OUT, 1>(aligned, add)
+         : pieces == 2 ? sum_kernel_of<TYPE, OUT, 2>(aligned, add)
+                       : sum_kernel_of<TYPE, OUT, most_pieces(TYPE)>(aligned, add);
+}
 template <int TYPE>
 cudaError_t launch_sums(const SumJob& j, int de_type, cudaStream_t st) {
-  const bool aligned = rows_on16(j.dY, j.lddy, type_bytes(TYPE));
+  const bool aligned = rows_on16(j.dY, j.lddy, type_bytes(TYPE)), add = j.accumulate != 0, same = de_type == TYPE;
   const int64_t blocks = (chunks_of(j.m) * j.slices + kSumWarps - 1) / kSumWarps;
   if (blocks > 0x7FFFFFFF) return cudaErrorInvalidValue;
   constexpr int F32 = OZ2_TYPE_F32;
-  const bool same = de_type == TYPE;
-  auto sum = same ? (aligned ? sum_runs_kernel<TYPE, TYPE, true> : sum_runs_kernel<TYPE, TYPE, false>)
-                  : (aligned ? sum_runs_kernel<TYPE, F32, true> : sum_runs_kernel<TYPE, F32, false>);
+  SumKernel sum = same ? sum_kernel<TYPE, TYPE>(j.pieces, aligned, add) : sum_kernel<TYPE, F32>(j.pieces, aligned, add);
   count_launch();
   cudaError_t err = launch_dependent(sum, dim3(static_cast<unsigned>(blocks)), dim3(32 * kSumWarps), 0, st, j);
   if (err != cudaSuccess || j.m <= kLongRun) return err;
-  const int64_t most = j.m / (kLongRun + 1) * j.slices;
+  const int64_t most = j.m / (kLongRun + 1) * j.slices * j.pieces;
+  SumKernel join = same ? (add ? join_runs_kernel<TYPE, TYPE, true> : join_runs_kernel<TYPE, TYPE, false>)
+                        : (add ? join_runs_kernel<TYPE, F32, true> : join_runs_kernel<TYPE, F32, false>);
   count_launch();
-  return launch_dependent(same ? join_runs_kernel<TYPE, TYPE> : join_runs_kernel<TYPE, F32>,
-                          dim3(static_cast<unsigned>(std::min<int64_t>(most, 4 * num_sms()))), dim3(32 * kSumWarps), 0, st, j);
+  return launch_dependent(join, dim3(static_cast<unsigned>(std::min<int64_t>(most, 4 * num_sms()))), dim3(32 * kSumWarps), 0, st, j);
 }
 
 }  // namespace
@@ -468,7 +565,7 @@ cudaError_t launch_embedding(int64_t m, int64_t n, int64_t k, int type, Ids ids,
 
 size_t embedding_grad_scratch(int64_t m, int64_t k, int type) {
   const size_t chunks = static_cast<size_t>(chunks_of(m));
-  const size_t values = 512 / type_bytes(type);  // of a slice
+  const size_t values = 512 / type_bytes(type) * pieces_of(k, type);  // of a slice
   return 2 * up(sizeof(uint2) * m) + up(sizeof(int2) * (m / (kLongRun + 1) + 1)) + 256 +
          up(m > kLongRun ? sizeof(float) * 2 * chunks * slices_of(k, type) * values : 0);
 }
@@ -522,7 +619,7 @@ cudaError_t launch_embedding_grad(int64_t m, int64_t n, int64_t k, int type, con
   err = cudaLaunchKernelEx(&cfg, sort_tokens_kernel, s, f, sorters);
   if (err != cudaSuccess) return err;
   SumJob j{m, k, static_cast<uint32_t>(n), dY, lddy, dE, ldde, scale, accumulate, rows_on16(dE, ldde, es),
-           passes & 1 ? a : b, parts, runs, long_runs, static_cast<int>(slices_of(k, type))};
+           passes & 1 ? a : b, parts, runs, long_runs, static_cast<int>(slices_of(k, type)), pieces_of(k, type)};
   return type == OZ2_TYPE_F32    ? launch_sums<OZ2_TYPE_F32>(j, de_type, st)
          : type == OZ2_TYPE_BF16 ? launch_sums<OZ2_TYPE_BF16>(j, de_type, st)
                                  : launch_sums<OZ2_TYPE_F16>(j, de_type, st);

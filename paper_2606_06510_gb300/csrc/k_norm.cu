@@ -206,14 +206,71 @@ __global__ void __launch_bounds__(kNormThreads) norm_long_kernel(NormArgs a) {
 // same in every row, so it adds up dw and db of them in registers; a block's groups add
 // theirs in shared memory, in order, into the block's row of `parts`, and
 // join_parts_kernel adds up the blocks'.
+//
+// Memory bounds it.  Rows on 16-byte boundaries go through shared memory, the next
+// STAGES of them on their way (cp.async) while one is worked on: each thread fetches
+// and reads its own pieces, so that no barrier is wanted, and reads them a second time
+// for dx instead of keeping them.  Other rows, and ones of which two do not fit, are
+// loaded to registers.
 // ---------------------------------------------------------------------------
-template <int TYPE, int TPR, int VPT, bool ALIGNED>
+__device__ __forceinline__ void fetch_async(uint32_t to, const void* from, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+constexpr int kStagedBytes = 200 * 1024;  // of a block's 227 KB
+constexpr int norm_stages(int vpt) {
+  const int n = kStagedBytes / (3 * vpt * 16 * kNormThreads);
+  return n < 2 ? 0 : n < 4 ? n : 4;
+}
+
+// Two FP32 values that one instruction works on.
+struct Two {
+  unsigned long long v;
+};
+__device__ __forceinline__ Two two(float a, float b) {
+  Two r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 both(Two t) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(t.v));
+  return r;
+}
+__device__ __forceinline__ Two operator*(Two a, Two b) {
+  Two r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Two operator+(Two a, Two b) {
+  Two r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Two fma(Two a, Two b, Two c) {
+  Two r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+template <int TYPE>
+__device__ __forceinline__ void unpack2(uint4 v, Two (&t)[Elem<TYPE>::V / 2]) {
+  float f[Elem<TYPE>::V];
+  Elem<TYPE>::unpack(v, f);
+#pragma unroll
+  for (int e = 0; e < Elem<TYPE>::V / 2; ++e) t[e] = two(f[2 * e], f[2 * e + 1]);
+}
+
+// Up to 16 values of a row to a thread stay in registers between the sums and dx; of
+// longer rows they are formed a second time.
+template <int TYPE, int TPR, int VPT, int STAGES>
 __global__ void __launch_bounds__(kNormThreads, 1) norm_grad_kernel(NormGradArgs a, float* __restrict__ parts) {
   using X = Elem<TYPE>;
   using T = typename X::T;
-  constexpr int V = X::V, kGroups = kNormThreads / TPR;
+  constexpr int V = X::V, H = V / 2, kGroups = kNormThreads / TPR;
+  constexpr bool STAGED = STAGES > 0, KEEP = VPT * V <= 16;
   __shared__ float exchange[kGroups][4 * TPR / 32];
-  extern __shared__ float columns[];  // of dw, then of db: TPR·VPT·V each, where there are groups to join
+  // The rows' pieces, and after them the columns of dw, then of db, where there are groups to join.
+  extern __shared__ __align__(16) uint8_t norm_smem[];
+  float* columns = reinterpret_cast<float*>(norm_smem);
   pdl_trigger();
   pdl_wait();
   const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
@@ -222,75 +279,148 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_grad_kernel(NormGradArgs
           *r_end = res + (a.m - 1) * a.ldr + a.k;
   const float inv_k = 1.f / static_cast<float>(a.k);
   RowSum<TPR, 2> rows{exchange[group], group, 0};
-  float dw[VPT][V], db[VPT][V];
+  // This thread's columns of a row: pieces from col(i) on, there(i) of their values.
+  auto col = [&](int i) { return static_cast<int64_t>(t + i * TPR) * V; };
+  auto there = [&](int i) { return static_cast<int>(max(int64_t(0), min(int64_t(V), a.k - col(i)))); };
+  const Two zero = two(0.f, 0.f), one = two(1.f, 1.f);
+  Two dw[VPT][H], db[VPT][H], w[KEEP ? VPT : 1][H];
+  auto weights = [&](int i, Two (&to)[H]) {
+    float f[V];
+    if (a.w && there(i)) load_vector<TYPE>(a.w, a.wtype, col(i), there(i), a.k, f);
 #pragma unroll
-  for (int i = 0; i < VPT; ++i)
+    for (int e = 0; e < H; ++e) to[e] = a.w && there(i) ? two(f[2 * e], f[2 * e + 1]) : one;
+  };
 #pragma unroll
-    for (int e = 0; e < V; ++e) dw[i][e] = db[i][e] = 0.f;
-  const int64_t stride = static_cast<int64_t>(gridDim.x) * kGroups;
-  for (int64_t r = static_cast<int64_t>(blockIdx.x) * kGroups + group; r < a.m; r += stride) {
-    uint4 rd[VPT], rx[VPT], rr[VPT];
+  for (int i = 0; i < VPT; ++i) {
+    if (KEEP) weights(i, w[KEEP ? i : 0]);
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      const int64_t col = static_cast<int64_t>(t + i * TPR) * V;
-      const int n = static_cast<int>(min(int64_t(V), a.k - col));
-      rd[i] = rx[i] = rr[i] = make_uint4(0, 0, 0, 0);
-      if (n > 0) {
-        rd[i] = load_piece<ALIGNED>(dy + r * a.lddy + col, dy, dy_end, n);
-        rx[i] = load_piece<ALIGNED>(x + r * a.ldx + col, x, x_end, n);
-        if (res) rr[i] = load_piece<ALIGNED, false>(res + r * a.ldr + col, res, r_end, n);
+    for (int e = 0; e < H; ++e) dw[i][e] = db[i][e] = zero;
+  }
+  const int64_t stride = static_cast<int64_t>(gridDim.x) * kGroups, first = static_cast<int64_t>(blockIdx.x) * kGroups + group;
+  uint4 rd[VPT], rx[VPT], rr[VPT];  // (not staged)
+  auto piece = [&](int stage, int which, int i) {
+    return norm_smem + (((stage * 3 + which) * VPT + i) * kNormThreads + threadIdx.x) * 16;
+  };
+  auto fetch = [&](int64_t r, int stage) {
+    if (r < a.m) {
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+        const int bytes = there(i) * sizeof(T);
+        const int64_t at = bytes ? col(i) : 0;
+        fetch_async(smem_u32(piece(stage, 0, i)), dy + r * a.lddy + at, bytes);
+        fetch_async(smem_u32(piece(stage, 1, i)), x + r * a.ldx + at, bytes);
+        if (res) fetch_async(smem_u32(piece(stage, 2, i)), res + r * a.ldr + at, bytes);
       }
     }
-    const float mean = a.mean ? __ldg(a.mean + r) : 0.f, rstd = __ldg(a.rstd + r);
-    float s[2] = {0.f, 0.f};
-    float g[VPT][V], h[VPT][V];  // g = dy·w and x̂
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  if constexpr (STAGED) {
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      const int64_t col = static_cast<int64_t>(t + i * TPR) * V;
-      const int n = static_cast<int>(min(int64_t(V), a.k - col));
-      X::unpack(rd[i], g[i]);
-      X::unpack(rx[i], h[i]);
+    for (int s = 0; s < STAGES; ++s) fetch(first + s * stride, s);
+  }
+  float mean = 0.f, rstd = 0.f;
+  auto statistics = [&](int64_t r) {
+    if (r < a.m) mean = a.mean ? __ldg(a.mean + r) : 0.f, rstd = __ldg(a.rstd + r);
+  };
+  statistics(first);
+  int stage = 0;
+  for (int64_t r = first; r < a.m; r += stride) {
+    if constexpr (STAGED) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+    } else {
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        h[i][e] = e < n ? (h[i][e] - mean) * rstd : 0.f;
-        dw[i][e] = fmaf(g[i][e], h[i][e], dw[i][e]);
-        db[i][e] += g[i][e];
-      }
-      if (a.w && n > 0) {
-        float w[V];
-        load_vector<TYPE>(a.w, a.wtype, col, n, a.k, w);
-#pragma unroll
-        for (int e = 0; e < V; ++e) g[i][e] *= w[e];
-      }
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        s[0] += g[i][e];
-        s[1] = fmaf(g[i][e], h[i][e], s[1]);
+      for (int i = 0; i < VPT; ++i) {
+        const int n = there(i);
+        rd[i] = rx[i] = rr[i] = make_uint4(0, 0, 0, 0);
+        if (n > 0) {
+          rd[i] = load_piece<false>(dy + r * a.lddy + col(i), dy, dy_end, n);
+          rx[i] = load_piece<false>(x + r * a.ldx + col(i), x, x_end, n);
+          if (res) rr[i] = load_piece<false, false>(res + r * a.ldr + col(i), res, r_end, n);
+        }
       }
     }
-    if (!a.dx) continue;
-    rows.sum(s);
-    const float level = a.mean ? s[0] * inv_k : 0.f, along = s[1] * inv_k;
+    const Two less = two(-mean, -mean), scale = two(rstd, rstd);
+    // dy, g = dy·w and x̂ of a piece.  (Past the row's end dy is zero, and whatever x̂ is there
+    // counts for nothing.)
+    auto values = [&](int i, Two (&d)[H], Two (&g)[H], Two (&h)[H]) {
+      unpack2<TYPE>(STAGED ? *reinterpret_cast<const uint4*>(piece(stage, 0, i)) : rd[i], d);
+      unpack2<TYPE>(STAGED ? *reinterpret_cast<const uint4*>(piece(stage, 1, i)) : rx[i], h);
+      Two own[H];
+      if (!KEEP) weights(i, own);
+#pragma unroll
+      for (int e = 0; e < H; ++e) {
+        h[e] = (h[e] + less) * scale;
+        g[e] = d[e] * (KEEP ? w[KEEP ? i : 0][e] : own[e]);
+      }
+    };
+    Two s0 = zero, s1 = zero, kg[KEEP ? VPT : 1][H], kh[KEEP ? VPT : 1][H];
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      const int64_t col = static_cast<int64_t>(t + i * TPR) * V;
-      const int n = static_cast<int>(min(int64_t(V), a.k - col));
-      if (n <= 0) continue;
+      Two d[H], gi[H], hi[H];
+      Two(&g)[H] = KEEP ? kg[KEEP ? i : 0] : gi;
+      Two(&h)[H] = KEEP ? kh[KEEP ? i : 0] : hi;
+      values(i, d, g, h);
 #pragma unroll
-      for (int e = 0; e < V; ++e) g[i][e] = rstd * (g[i][e] - level - h[i][e] * along);
-      if (res) {
-        float o[V];
-        X::unpack(rr[i], o);
-#pragma unroll
-        for (int e = 0; e < V; ++e) g[i][e] += o[e];
+      for (int e = 0; e < H; ++e) {
+        dw[i][e] = fma(d[e], h[e], dw[i][e]);
+        db[i][e] = db[i][e] + d[e];
+        s0 = s0 + g[e];
+        s1 = fma(g[e], h[e], s1);
       }
-      store16_any(static_cast<T*>(a.dx) + r * a.lddx + col, X::pack(g[i]), n, ALIGNED && n == V);
     }
+    if (a.dx) {
+      const float2 p0 = both(s0), p1 = both(s1);
+      float s[2] = {p0.x + p0.y, p1.x + p1.y};
+      rows.sum(s);
+      const float level = a.mean ? -rstd * (s[0] * inv_k) : 0.f, along = -rstd * (s[1] * inv_k);
+      const Two level2 = two(level, level), along2 = two(along, along);
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+        const int n = there(i);
+        if (n == 0) continue;
+        Two d[H], gi[H], hi[H];
+        Two(&g)[H] = KEEP ? kg[KEEP ? i : 0] : gi;
+        Two(&h)[H] = KEEP ? kh[KEEP ? i : 0] : hi;
+        if (!KEEP) values(i, d, g, h);
+#pragma unroll
+        for (int e = 0; e < H; ++e) d[e] = fma(h[e], along2, fma(g[e], scale, level2));
+        if (res) {
+          Two o[H];
+          unpack2<TYPE>(STAGED ? *reinterpret_cast<const uint4*>(piece(stage, 2, i)) : rr[i], o);
+#pragma unroll
+          for (int e = 0; e < H; ++e) d[e] = d[e] + o[e];
+        }
+        float y[V];
+#pragma unroll
+        for (int e = 0; e < H; ++e) {
+          const float2 f = both(d[e]);
+          y[2 * e] = f.x, y[2 * e + 1] = f.y;
+        }
+        store16_any(static_cast<T*>(a.dx) + r * a.lddx + col(i), X::pack(y), n, STAGED && n == V);
+      }
+    }
+    statistics(r + stride);
+    if constexpr (STAGED) {
+      fetch(r + STAGES * stride, stage);
+      stage = stage + 1 == STAGES ? 0 : stage + 1;
+    }
+  }
+  if constexpr (STAGED) {
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();  // the pieces' memory becomes the columns'
   }
   if (!parts) return;
   float* to = parts + static_cast<int64_t>(blockIdx.x) * 2 * a.k;
   constexpr int kCols = TPR * VPT * V;
-  auto keep = [&](const float (&v)[VPT][V], float* row, float* join) {
+  auto keep = [&](const Two (&two_of)[VPT][H], float* row, float* join) {
+    float v[VPT][V];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+#pragma unroll
+      for (int e = 0; e < H; ++e) {
+        const float2 f = both(two_of[i][e]);
+        v[i][2 * e] = f.x, v[i][2 * e + 1] = f.y;
+      }
     if (kGroups > 1) {
       for (int q = 0; q < kGroups; ++q) {
         __syncthreads();
@@ -446,64 +576,68 @@ __global__ void __launch_bounds__(256) join_parts_kernel(int64_t k, int count, c
 }
 
 // ---------------------------------------------------------------------------
-// Threads to a row and pieces to a thread: a row is at most 16384 elements (32 FP32
-// values a thread), longer ones are not held.
+// Threads to a row and pieces to a thread: as few threads as hold it with `each` values
+// to a thread, and up to 32 of them at the most.  Longer rows are not held.
 // ---------------------------------------------------------------------------
 struct NormShape {
   int tpr, vpt;  // 0: too long
 };
-NormShape shape_of(int64_t k, int type, int64_t rows) {
-  const int v = 16 / type_bytes(type), most = 32 / v;  // pieces a thread at most
+NormShape shape_of(int64_t k, int type, int each, int least) {
+  const int v = 16 / type_bytes(type);
   const int64_t pieces = (k + v - 1) / v;
-  // Few rows: more threads to each of them.
-  const bool few = rows <= 2 * static_cast<int64_t>(num_sms());
-  for (int tpr : {32, 128, 512}) {
-    if (few && tpr < 512 && pieces > tpr) continue;
-    for (int vpt = 1; vpt <= most; vpt *= 2)
+  for (int tpr : {32, 64, 128, 256, 512}) {
+    if (tpr < least && pieces > tpr) continue;
+    for (int vpt = 1; vpt * v <= (tpr < 512 ? each : 32); vpt *= 2)
       if (pieces <= static_cast<int64_t>(tpr) * vpt) return {tpr, vpt};
   }
   return {0, 0};
 }
-
-template <int TYPE, bool ALIGNED, template <int, int, int, bool> class K>
-auto by_shape(NormShape s) {
-  switch (s.tpr * 16 + s.vpt) {
-    case 32 * 16 + 1: return K<TYPE, 32, 1, ALIGNED>::f();
-    case 32 * 16 + 2: return K<TYPE, 32, 2, ALIGNED>::f();
-    case 32 * 16 + 4: return K<TYPE, 32, 4, ALIGNED>::f();
-    case 128 * 16 + 1: return K<TYPE, 128, 1, ALIGNED>::f();
-    case 128 * 16 + 2: return K<TYPE, 128, 2, ALIGNED>::f();
-    case 128 * 16 + 4: return K<TYPE, 128, 4, ALIGNED>::f();
-    case 512 * 16 + 1: return K<TYPE, 512, 1, ALIGNED>::f();
-    case 512 * 16 + 2: return K<TYPE, 512, 2, ALIGNED>::f();
-    case 512 * 16 + 4: return K<TYPE, 512, 4, ALIGNED>::f();
-    default: break;
-  }
-  if constexpr (TYPE == OZ2_TYPE_F32) {
-    if (s.vpt == 8) return s.tpr == 32 ? K<TYPE, 32, 8, ALIGNED>::f() : s.tpr == 128 ? K<TYPE, 128, 8, ALIGNED>::f() : K<TYPE, 512, 8, ALIGNED>::f();
-  }
-  return decltype(K<TYPE, 32, 1, ALIGNED>::f())(nullptr);
+// Forward: few rows get more threads each.
+NormShape forward_shape(int64_t m, int64_t k, int type) {
+  return shape_of(k, type, 32, m <= 2 * static_cast<int64_t>(num_sms()) ? 512 : 32);
 }
-template <int TYPE, int TPR, int VPT, bool ALIGNED>
+NormShape backward_shape(int64_t m, int64_t k, int type) { return shape_of(k, type, 16, 32); }
+
+template <template <int, int> class K, int TPR>
+auto by_pieces(int vpt) {
+  return vpt == 1 ? K<TPR, 1>::f() : vpt == 2 ? K<TPR, 2>::f() : vpt == 4 ? K<TPR, 4>::f() : K<TPR, 8>::f();
+}
+template <template <int, int> class K>
+auto by_shape(NormShape s) {  // the kernel K of these threads and pieces
+  return s.tpr == 32    ? by_pieces<K, 32>(s.vpt)
+         : s.tpr == 64  ? by_pieces<K, 64>(s.vpt)
+         : s.tpr == 128 ? by_pieces<K, 128>(s.vpt)
+         : s.tpr == 256 ? by_pieces<K, 256>(s.vpt)
+                        : by_pieces<K, 512>(s.vpt);
+}
+// (Of 8 pieces, those of 16-bit rows are never asked for.)
+template <int TYPE, bool ALIGNED>
 struct Forward {
-  static auto f() { return &norm_kernel<TYPE, TPR, VPT, ALIGNED>; }
+  template <int TPR, int VPT>
+  struct K {
+    static auto f() { return &norm_kernel<TYPE, TPR, VPT * Elem<TYPE>::V <= 32 ? VPT : 4, ALIGNED>; }
+  };
 };
-template <int TYPE, int TPR, int VPT, bool ALIGNED>
+template <int TYPE, bool ALIGNED>
 struct Backward {
-  static auto f() { return &norm_grad_kernel<TYPE, TPR, VPT, ALIGNED>; }
+  template <int TPR, int VPT>
+  struct K {
+    static constexpr int kMost = TPR < 512 ? 16 / Elem<TYPE>::V : 32 / Elem<TYPE>::V, kVpt = VPT < kMost ? VPT : kMost;
+    static auto f() { return &norm_grad_kernel<TYPE, TPR, kVpt, ALIGNED ? norm_stages(kVpt) : 0>; }
+  };
 };
 
 template <int TYPE>
 cudaError_t forward(const NormArgs& a, cudaStream_t st) {
   const int es = type_bytes(TYPE);
-  const NormShape s = shape_of(a.k, TYPE, a.m);
+  const NormShape s = forward_shape(a.m, a.k, TYPE);
   count_launch();
   if (!s.tpr) {
     const unsigned blocks = static_cast<unsigned>(std::min<int64_t>(a.m, 4 * num_sms()));
     return launch_dependent(norm_long_kernel<TYPE>, dim3(blocks), dim3(kNormThreads), 0, st, a);
   }
   const bool aligned = rows_on16(a.x, a.ldx, es) && rows_on16(a.y, a.ldy, es);
-  auto kern = aligned ? by_shape<TYPE, true, Forward>(s) : by_shape<TYPE, false, Forward>(s);
+  auto kern = aligned ? by_shape<Forward<TYPE, true>::template K>(s) : by_shape<Forward<TYPE, false>::template K>(s);
   const int block = s.tpr < 128 ? 128 : s.tpr, groups = block / s.tpr;
   const int64_t blocks = std::min<int64_t>((a.m + groups - 1) / groups, 0x7FFFFFFF);
   return launch_dependent(kern, dim3(static_cast<unsigned>(blocks)), dim3(block), 0, st, a);
@@ -521,7 +655,7 @@ int64_t grad_blocks(const NormGradArgs& a, NormShape s) {
 template <int TYPE>
 cudaError_t backward(const NormGradArgs& a, float* parts, cudaStream_t st) {
   const int es = type_bytes(TYPE);
-  const NormShape s = shape_of(a.k, TYPE, a.m);
+  const NormShape s = backward_shape(a.m, a.k, TYPE);
   const bool want = a.dw || a.db;
   const int64_t blocks = grad_blocks(a, s);
   cudaError_t err = cudaSuccess;
@@ -540,8 +674,9 @@ cudaError_t backward(const NormGradArgs& a, float* parts, cudaStream_t st) {
   } else {
     const bool aligned = rows_on16(a.dy, a.lddy, es) && rows_on16(a.x, a.ldx, es) && (!a.r || rows_on16(a.r, a.ldr, es)) &&
                          (!a.dx || rows_on16(a.dx, a.lddx, es));
-    auto kern = aligned ? by_shape<TYPE, true, Backward>(s) : by_shape<TYPE, false, Backward>(s);
-    const size_t smem = s.tpr < kNormThreads ? 2 * sizeof(float) * s.tpr * s.vpt * Elem<TYPE>::V : 0;
+    auto kern = aligned ? by_shape<Backward<TYPE, true>::template K>(s) : by_shape<Backward<TYPE, false>::template K>(s);
+    const size_t join = s.tpr < kNormThreads ? 2 * sizeof(float) * s.tpr * s.vpt * Elem<TYPE>::V : 0;
+    const size_t smem = std::max<size_t>(join, aligned ? 3 * 16 * kNormThreads * s.vpt * norm_stages(s.vpt) : 0);
     err = allow_smem(reinterpret_cast<const void*>(kern), smem);
     if (err != cudaSuccess) return err;
     count_launch();
@@ -563,7 +698,7 @@ cudaError_t launch_layer_norm(const NormArgs& a, int type, cudaStream_t st) {
 
 size_t layer_norm_grad_scratch(const NormGradArgs& a, int type) {
   if (!a.dw && !a.db) return 0;
-  return sizeof(float) * 2 * static_cast<size_t>(a.k) * grad_blocks(a, shape_of(a.k, type, a.m));
+  return sizeof(float) * 2 * static_cast<size_t>(a.k) * grad_blocks(a, backward_shape(a.m, a.k, type));
 }
 
 cudaError_t launch_layer_norm_grad(const NormGradArgs& a, int type, void* scratch, cudaStream_t st) {
