@@ -70,11 +70,10 @@ __global__ void __launch_bounds__(256)
 // rows' bits, up to 9 at a time, by one cluster: each warp has a stretch of the tokens,
 // counts its digits in shared memory, and after the counts have been summed over warps
 // and blocks (by distributed shared memory) gives each pair its place, which depends on
-// the order of the pairs alone.  The other blocks of the launch write the zeros of a
-// gradient that is not added to meanwhile.
+// the order of the pairs alone.
 // ---------------------------------------------------------------------------
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kDigitBits = 9, kDigits = 1 << kDigitBits;
-constexpr int kSortCluster = 8;
+constexpr int kSortCluster = 16, kFillThreads = 256;
 constexpr int kSortSmem = (kSortWarps + 2) * kDigits * 4;
 
 struct SortJob {
@@ -83,7 +82,7 @@ struct SortJob {
   uint32_t n;
   int passes, bits;    // of `bits` bits each
   uint2 *a, *b;        // the passes write a, b, a, ...
-  int* long_runs;      // a counter that is set to zero
+  int* long_runs;      // two counters that are set to zero
 };
 struct FillJob {       // `rows` rows of `bytes` bytes, `ld` bytes apart (one row: all of it)
   char* p;
@@ -103,27 +102,31 @@ __device__ __forceinline__ void zero_row(char* p, int64_t bytes, int unit, int64
     for (int b = 0; b < unit; b += 2) *reinterpret_cast<uint16_t*>(p + i + b) = 0;
 }
 
-__global__ void __launch_bounds__(kSortThreads, 1) sort_tokens_kernel(SortJob s, FillJob f, int sorters) {
-  extern __shared__ uint32_t sort_smem[];
+// The zeros are written beside the sort: this kernel starts once the sort has seen the end
+// of what came before the two, and ends after it, so that the kernel that follows has both
+// behind it.
+__global__ void __launch_bounds__(kFillThreads) fill_rows_kernel(FillJob f) {
   pdl_trigger();
-  pdl_wait();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (static_cast<int>(blockIdx.x) >= sorters) {
-    const int64_t blocks = gridDim.x - sorters, block = blockIdx.x - sorters;
-    if (f.rows == 1) {
-      zero_row(f.p, f.bytes, f.unit, block * kSortThreads + threadIdx.x, blocks * kSortThreads);
-    } else {
-      for (int64_t r = block * kSortWarps + warp; r < f.rows; r += blocks * kSortWarps)
-        zero_row(f.p + r * f.ld, f.bytes, f.unit, lane, 32);
-    }
-    return;
+  const int64_t threads = static_cast<int64_t>(gridDim.x) * kFillThreads, me = static_cast<int64_t>(blockIdx.x) * kFillThreads + threadIdx.x;
+  if (f.rows == 1) {
+    zero_row(f.p, f.bytes, f.unit, me, threads);
+  } else {
+    for (int64_t r = me >> 5; r < f.rows; r += threads >> 5) zero_row(f.p + r * f.ld, f.bytes, f.unit, threadIdx.x & 31, 32);
   }
+  pdl_wait();
+}
+
+__global__ void __launch_bounds__(kSortThreads, 1) sort_tokens_kernel(SortJob s, int sorters) {
+  extern __shared__ uint32_t sort_smem[];
+  pdl_wait();
+  pdl_trigger();  // (not before: see fill_rows_kernel)
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint32_t* mine = sort_smem + warp * kDigits;             // this warp's counts, then its next places
   uint32_t* total = sort_smem + kSortWarps * kDigits;      // the block's
   uint32_t* base = total + kDigits;                        // the first places of the block's pairs of a digit
   __shared__ uint32_t sums[kSortWarps];
   const uint32_t rank = sorters > 1 ? cluster_ctarank() : 0, blocks = sorters;
-  if (rank == 0 && threadIdx.x == 0) *s.long_runs = 0;
+  if (rank == 0 && threadIdx.x == 0) s.long_runs[0] = s.long_runs[1] = 0;
   const int64_t each = ((s.m + blocks * kSortWarps - 1) / (blocks * kSortWarps) + 31) / 32 * 32;
   const int64_t i0 = min(s.m, (static_cast<int64_t>(rank) * kSortWarps + warp) * each), i1 = min(s.m, i0 + each);
   const int digits = 1 << s.bits;
@@ -172,6 +175,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_tokens_kernel(SortJob s,
         all = 0;
 #pragma unroll
         for (uint32_t b = 0; b < kSortCluster; ++b) {
+          if (b >= blocks) break;
           uint32_t v;
           asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(mapa_shared(smem_u32(total + d), b)));
           if (b < rank) before += v;
@@ -222,7 +226,6 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_tokens_kernel(SortJob s,
     to = t;
     // (The pairs are read by other blocks, and the counts are set to zero.)
     if (blocks > 1) {
-      __threadfence();
       cluster_sync_all();
     } else {
       __syncthreads();
@@ -232,13 +235,14 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_tokens_kernel(SortJob s,
 
 // ---------------------------------------------------------------------------
 // The sums over runs of equal rows.  A warp takes the runs that start in a chunk of 16
-// sorted pairs, 512 bytes of the rows (a lane 16).  Runs of more than 32 pairs are cut
+// sorted pairs, a slice of the rows' columns.  Runs of more than 16 pairs are cut
 // at the chunks' ends: what of one lies in a chunk is summed into the chunk's FP32
 // rows `parts` (its first one for a run that started before, its second for one that
 // starts here), and join_runs_kernel adds those up in order.  So the work of a warp is
 // bounded, however often a row is named, and every sum has one order.
 // ---------------------------------------------------------------------------
-constexpr int kChunkPairs = 16, kLongRun = 32, kSumWarps = 8;
+constexpr int kChunkPairs = 16, kLongRun = 16, kSumWarps = 8;
+constexpr int kFewParts = 8;  // that a warp adds up
 
 // The rows around a chunk: the 32 pairs before it and the 64 from its first on.
 struct Window {
@@ -322,13 +326,14 @@ struct SumJob {
   int accumulate, vec;     // vec: dE's rows are on 16-byte boundaries
   const uint2* sorted;
   float* parts;            // two rows a chunk, of `slices` whole slices
-  int2* runs;              // long runs: first chunk, and how many chunks
-  int* long_runs;
+  int4* runs;              // long runs of many parts: row, first chunk and how many; those of few from the end on
+  int* long_runs;          // how many of either
+  int most_runs;
   int slices, pieces;      // of a row, and of a slice to a lane
 };
 
 template <int TYPE, int OUT, int P, bool ALIGNED, bool ADD>
-__global__ void __launch_bounds__(32 * kSumWarps) sum_runs_kernel(SumJob j) {
+__global__ void __launch_bounds__(32 * kSumWarps, P == 1 ? 4 : P == 2 ? 3 : 2) sum_runs_kernel(SumJob j) {
   using X = Elem<TYPE>;
   using T = typename X::T;
   constexpr int V = X::V;
@@ -403,7 +408,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) sum_runs_kernel(SumJob j) {
   // Several pairs at a time, whatever rows they are of: all loads are under way before the
   // first is added, and so are the old values of 16-bit rows that are added to.
   constexpr bool kOld = ADD && OUT != OZ2_TYPE_F32;
-  constexpr int kAtOnce = 16 / P / (kOld ? 2 : 1);
+  constexpr int kAtOnce = (P == 4 ? 16 : 8) / P / (kOld ? 2 : 1);
   for (int i = begin; i < end; i += kAtOnce) {
     uint4 v[kAtOnce][P], old[kOld ? kAtOnce : 1][P];
 #pragma unroll
@@ -452,31 +457,32 @@ __global__ void __launch_bounds__(32 * kSumWarps) sum_runs_kernel(SumJob j) {
       c += __popc(in);
       if (in != 0xFFFFFFFFu) break;
     }
-    if (lane == 0) j.runs[atomicAdd(j.long_runs, 1)] = make_int2(static_cast<int>(chunk), static_cast<int>(c - chunk));
+    if (lane == 0) {
+      const int few = c - chunk <= kFewParts, at = atomicAdd(j.long_runs + few, 1);
+      j.runs[few ? j.most_runs - 1 - at : at] = make_int4(static_cast<int>(r), static_cast<int>(chunk), static_cast<int>(c - chunk), 0);
+    }
   }
 }
 
-// The parts of a long run, 32·V of its columns to a block: each warp adds up a stretch of
-// them, and the warps' sums are added in order.
+// The parts of a long run, a piece of its columns at a time: by a warp, or where there are
+// many of them by a block, each warp of which adds up a stretch; the warps' sums are added
+// in order.
+constexpr int kJoinWarps = 16;
+
 template <int TYPE, int OUT, bool ADD>
-__global__ void __launch_bounds__(32 * kSumWarps) join_runs_kernel(SumJob j) {
+__global__ void __launch_bounds__(32 * kJoinWarps) join_runs_kernel(SumJob j) {
   constexpr int V = Elem<TYPE>::V;
-  __shared__ float sums[kSumWarps][32 * V];
+  __shared__ float sums[kJoinWarps][32 * V];
   pdl_trigger();
   pdl_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int pieces = static_cast<int>((j.k + 32 * V - 1) / (32 * V));
   const int64_t row_floats = static_cast<int64_t>(j.slices) * j.pieces * 32 * V;
-  const int64_t units = static_cast<int64_t>(*j.long_runs) * pieces;
-  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-    const int run = static_cast<int>(u / pieces), piece = static_cast<int>(u - static_cast<int64_t>(run) * pieces);
-    const int64_t chunk = j.runs[run].x;
-    const int chunks = j.runs[run].y, each = (chunks + kSumWarps - 1) / kSumWarps;
-    const int c0 = min(chunks, warp * each), c1 = min(chunks, c0 + each);
-    float s[V];
+  float s[V];
+  auto add = [&](int64_t chunk, int piece, int c0, int c1) {
 #pragma unroll
     for (int e = 0; e < V; ++e) s[e] = 0.f;
-#pragma unroll 4
+#pragma unroll 8
     for (int c = c0; c < c1; ++c) {
       const float* p = j.parts + (2 * (chunk + c) + (c == 0)) * row_floats + (static_cast<int64_t>(piece) * 32 + lane) * V;
 #pragma unroll
@@ -485,37 +491,52 @@ __global__ void __launch_bounds__(32 * kSumWarps) join_runs_kernel(SumJob j) {
         s[h] += v.x, s[h + 1] += v.y, s[h + 2] += v.z, s[h + 3] += v.w;
       }
     }
+  };
+  auto finish = [&](int row, int piece) {
+    const int64_t col = (static_cast<int64_t>(piece) * 32 + lane) * V;
+    const int n = static_cast<int>(max(int64_t(0), min(int64_t(V), j.k - col)));
+    if (n > 0) {
+      uint4 old = make_uint4(0, 0, 0, 0);
+      if (ADD && OUT != OZ2_TYPE_F32) old = old_piece<OUT>(j.dE, row, j.ldde, col, n, j.vec);
+      finish_piece<TYPE, OUT, ADD>(j.dE, row, j.ldde, col, n, j.scale, j.vec, old, s);
+    }
+  };
+  const int many = j.long_runs[0], few = j.long_runs[1];
+  for (int64_t u = static_cast<int64_t>(warp) * gridDim.x + blockIdx.x; u < static_cast<int64_t>(few) * pieces;
+       u += static_cast<int64_t>(gridDim.x) * kJoinWarps) {
+    const int at = static_cast<int>(u / pieces), piece = static_cast<int>(u - static_cast<int64_t>(at) * pieces);
+    const int4 run = j.runs[j.most_runs - 1 - at];
+    add(run.y, piece, 0, run.z);
+    finish(run.x, piece);
+  }
+  for (int64_t u = blockIdx.x; u < static_cast<int64_t>(many) * pieces; u += gridDim.x) {
+    const int at = static_cast<int>(u / pieces), piece = static_cast<int>(u - static_cast<int64_t>(at) * pieces);
+    const int4 run = j.runs[at];
+    const int each = (run.z + kJoinWarps - 1) / kJoinWarps, c0 = min(run.z, warp * each);
+    add(run.y, piece, c0, min(run.z, c0 + each));
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < V; ++e) sums[warp][lane * V + e] = s[e];
     __syncthreads();
     if (warp == 0) {
-      for (int o = 1; o < kSumWarps; ++o)
+      for (int o = 1; o < kJoinWarps; ++o)
 #pragma unroll
         for (int e = 0; e < V; ++e) s[e] += sums[o][lane * V + e];
-      const int64_t col = (static_cast<int64_t>(piece) * 32 + lane) * V;
-      const int n = static_cast<int>(max(int64_t(0), min(int64_t(V), j.k - col)));
-      const uint32_t r = j.sorted[(chunk + 1) * kChunkPairs - 1].x;  // the chunk's last pair is the run's
-      if (n > 0) {
-        uint4 old = make_uint4(0, 0, 0, 0);
-        if (ADD && OUT != OZ2_TYPE_F32) old = old_piece<OUT>(j.dE, r, j.ldde, col, n, j.vec);
-        finish_piece<TYPE, OUT, ADD>(j.dE, r, j.ldde, col, n, j.scale, j.vec, old, s);
-      }
+      finish(run.x, piece);
     }
   }
 }
 
 // Pieces to a lane, and the slices of a row that come of it.
-int pieces_of(int64_t k, int type) {
-  const int64_t all = (k * type_bytes(type) + 511) / 512;
-  const int most = most_pieces(type);
-  return all >= most ? most : all >= 2 ? 2 : 1;
-}
-int64_t slices_of(int64_t k, int type) {
-  const int64_t bytes = 512 * pieces_of(k, type);
-  return (k * type_bytes(type) + bytes - 1) / bytes;
-}
+// As many as leave 24 warps an SM (16384 tokens of 1024 bf16: 17 us with two, 10 with one).
 int64_t chunks_of(int64_t m) { return (m + kChunkPairs - 1) / kChunkPairs; }
+int64_t slices_of(int64_t k, int type, int pieces) { return (k * type_bytes(type) + 512 * pieces - 1) / (512 * pieces); }
+int pieces_of(int64_t m, int64_t k, int type) {
+  int p = most_pieces(type);
+  while (p > 1 && (512 * p / 2 >= k * type_bytes(type) || chunks_of(m) * slices_of(k, type, p) < 24 * static_cast<int64_t>(num_sms())))
+    p /= 2;
+  return p;
+}
 size_t up(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
 using SumKernel = void (*)(SumJob);
@@ -540,11 +561,11 @@ cudaError_t launch_sums(const SumJob& j, int de_type, cudaStream_t st) {
   count_launch();
   cudaError_t err = launch_dependent(sum, dim3(static_cast<unsigned>(blocks)), dim3(32 * kSumWarps), 0, st, j);
   if (err != cudaSuccess || j.m <= kLongRun) return err;
-  const int64_t most = j.m / (kLongRun + 1) * j.slices * j.pieces;
+  const int64_t most = (j.m / (kLongRun + 1) * j.slices * j.pieces + 1) / 2;
   SumKernel join = same ? (add ? join_runs_kernel<TYPE, TYPE, true> : join_runs_kernel<TYPE, TYPE, false>)
                         : (add ? join_runs_kernel<TYPE, F32, true> : join_runs_kernel<TYPE, F32, false>);
   count_launch();
-  return launch_dependent(join, dim3(static_cast<unsigned>(std::min<int64_t>(most, 4 * num_sms()))), dim3(32 * kSumWarps), 0, st, j);
+  return launch_dependent(join, dim3(static_cast<unsigned>(std::min<int64_t>(most, 2 * num_sms()))), dim3(32 * kJoinWarps), 0, st, j);
 }
 
 }  // namespace
@@ -565,9 +586,10 @@ cudaError_t launch_embedding(int64_t m, int64_t n, int64_t k, int type, Ids ids,
 
 size_t embedding_grad_scratch(int64_t m, int64_t k, int type) {
   const size_t chunks = static_cast<size_t>(chunks_of(m));
-  const size_t values = 512 / type_bytes(type) * pieces_of(k, type);  // of a slice
-  return 2 * up(sizeof(uint2) * m) + up(sizeof(int2) * (m / (kLongRun + 1) + 1)) + 256 +
-         up(m > kLongRun ? sizeof(float) * 2 * chunks * slices_of(k, type) * values : 0);
+  const int pieces = pieces_of(m, k, type);
+  const size_t values = 512 / type_bytes(type) * pieces;  // of a slice
+  return 2 * up(sizeof(uint2) * m) + up(sizeof(int4) * (m / (kLongRun + 1) + 1)) + 256 +
+         up(m > kLongRun ? sizeof(float) * 2 * chunks * slices_of(k, type, pieces) * values : 0);
 }
 
 cudaError_t launch_embedding_grad(int64_t m, int64_t n, int64_t k, int type, const void* dY, int64_t lddy, Ids ids,
@@ -581,7 +603,7 @@ cudaError_t launch_embedding_grad(int64_t m, int64_t n, int64_t k, int type, con
   };
   uint2* a = reinterpret_cast<uint2*>(take(sizeof(uint2) * m));
   uint2* b = reinterpret_cast<uint2*>(take(sizeof(uint2) * m));
-  int2* runs = reinterpret_cast<int2*>(take(sizeof(int2) * (m / (kLongRun + 1) + 1)));
+  int4* runs = reinterpret_cast<int4*>(take(sizeof(int4) * (m / (kLongRun + 1) + 1)));
   int* long_runs = reinterpret_cast<int*>(take(256));
   float* parts = reinterpret_cast<float*>(at);
   int bits = 1;
@@ -589,20 +611,15 @@ cudaError_t launch_embedding_grad(int64_t m, int64_t n, int64_t k, int type, con
   const int passes = (bits + kDigitBits - 1) / kDigitBits;
   SortJob s{ids, m, static_cast<uint32_t>(n), passes, (bits + passes - 1) / passes, a, b, long_runs};
   const int es = type_bytes(de_type);
-  FillJob f{static_cast<char*>(dE), 0, 0, 0, es};
-  if (!accumulate) {
-    const bool whole = ldde == k || n == 1;
-    f.rows = whole ? 1 : n;
-    f.bytes = (whole ? n : 1) * k * es;
-    f.ld = ldde * es;
-  }
+  // A block sorts up to 2048 tokens as fast as a cluster; 16 blocks want a cluster larger
+  // than every device has.
   const int sorters = m > 2048 ? kSortCluster : 1;
-  const int64_t fillers = accumulate ? 0 : std::min<int64_t>(n * k * es / (64 * kSortThreads) + 1, num_sms());
-  const int64_t blocks = sorters + (fillers + sorters - 1) / sorters * sorters;
-  cudaError_t err = allow_smem(reinterpret_cast<const void*>(sort_tokens_kernel), kSortSmem);
+  const void* sort = reinterpret_cast<const void*>(sort_tokens_kernel);
+  cudaError_t err = allow_smem(sort, kSortSmem);
+  if (err == cudaSuccess && sorters > 8) err = cudaFuncSetAttribute(sort, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (err != cudaSuccess) return err;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+  cfg.gridDim = dim3(static_cast<unsigned>(sorters));
   cfg.blockDim = dim3(kSortThreads);
   cfg.dynamicSmemBytes = kSortSmem;
   cfg.stream = st;
@@ -616,10 +633,20 @@ cudaError_t launch_embedding_grad(int64_t m, int64_t n, int64_t k, int type, con
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   count_launch();
-  err = cudaLaunchKernelEx(&cfg, sort_tokens_kernel, s, f, sorters);
+  err = cudaLaunchKernelEx(&cfg, sort_tokens_kernel, s, sorters);
   if (err != cudaSuccess) return err;
+  if (!accumulate) {
+    const bool whole = ldde == k || n == 1;
+    const FillJob f{static_cast<char*>(dE), whole ? 1 : n, (whole ? n : 1) * k * es, ldde * es, es};
+    const int64_t blocks = std::min<int64_t>(n * k * es / (64 * kFillThreads) + 1, 8 * static_cast<int64_t>(num_sms()));
+    count_launch();
+    err = launch_dependent(fill_rows_kernel, dim3(static_cast<unsigned>(blocks)), dim3(kFillThreads), 0, st, f);
+    if (err != cudaSuccess) return err;
+  }
+  const int pieces = pieces_of(m, k, type);
   SumJob j{m, k, static_cast<uint32_t>(n), dY, lddy, dE, ldde, scale, accumulate, rows_on16(dE, ldde, es),
-           passes & 1 ? a : b, parts, runs, long_runs, static_cast<int>(slices_of(k, type)), pieces_of(k, type)};
+           passes & 1 ? a : b, parts, runs, long_runs, static_cast<int>(m / (kLongRun + 1) + 1),
+           static_cast<int>(slices_of(k, type, pieces)), pieces};
   return type == OZ2_TYPE_F32    ? launch_sums<OZ2_TYPE_F32>(j, de_type, st)
          : type == OZ2_TYPE_BF16 ? launch_sums<OZ2_TYPE_BF16>(j, de_type, st)
                                  : launch_sums<OZ2_TYPE_F16>(j, de_type, st);

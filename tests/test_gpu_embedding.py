@@ -121,7 +121,7 @@ def test_gradient(oz, dt, kind, m, n, k, how):
         assert torch.equal(old[~hit[:n]], whole[~hit[:n]])  # rows without tokens: left as they were
 
 
-@pytest.mark.parametrize("m", [32, 33, 48, 49, 64, 65, 200])
+@pytest.mark.parametrize("m", [15, 16, 17, 31, 32, 33, 48, 49, 64, 65, 130, 200])
 def test_runs_at_the_chunks_ends(oz, m):
     """Runs of every length around those that are cut, starting anywhere in a chunk."""
     g = rng(m)
