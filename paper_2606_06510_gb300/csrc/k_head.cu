@@ -52,6 +52,32 @@ __device__ __forceinline__ bool head_tile(const HeadUnits& u, int i, HeadTile& t
   return true;
 }
 
+// A token's terms: of its target, or as they were prepared for listed rows.
+__device__ __forceinline__ HeadRow head_row(const HeadTerms& t, Ids ids, int64_t n, int64_t row) {
+  if (t.rows) {
+    const float4 f = __ldg(reinterpret_cast<const float4*>(t.rows) + row);
+    return HeadRow{f.x, f.y, f.z, __float_as_int(f.w)};
+  }
+  const int64_t id = ids[row];
+  if (id < 0) return HeadRow{0.f, 0.f, 0.f, 0};
+  const float l = __ldg(t.lse + row), g = __ldg(t.dloss + (t.dloss_each ? row : 0)) * t.scale;
+  return HeadRow{id < n ? g : __int_as_float(0x7FC00000), l * kLog2E, t.z_loss != 0.f ? 2.f * t.z_loss * l : 0.f, 1};
+}
+__device__ __forceinline__ float head_size(const HeadRow& r) {  // (what is no number does not count)
+  const float size = fabsf(r.a) * fmaxf(1.f, fabsf(1.f + r.e));
+  return size < INFINITY ? size : 0.f;
+}
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+__device__ __forceinline__ float warp_add(float v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
 // v[j] for a j that the compiler does not know.
 __device__ __forceinline__ float pick32(const float (&v)[32], int j) {
   float t[16];
@@ -217,7 +243,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     const float to2 = A.scale * kLog2E;   // logits in powers of two
     float up = 1.f;                       // dz's scale
     if (GRAD && A.largest) {
-      const int bits = __ldg(A.largest), e = (bits >> 23) - 127;
+      float most = 0.f;
+      for (int i = lane; i < A.maxima; i += 32) most = fmaxf(most, __ldg(A.largest + i));
+      const int bits = __float_as_int(warp_max(most)), e = (bits >> 23) - 127;
       const int s = bits > 0 ? max(-100, min(100, 14 - e)) : 0;
       up = __int_as_float((127 + s) << 23);
       if (blockIdx.x == 0 && threadIdx.x == 64) *A.unscale = __int_as_float((127 - s) << 23);
@@ -229,15 +257,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const int col0 = tile.col + kHeadGroup * h;             // in the piece
       const int cols = kHeadGroup * h < tile.width && col0 < A.cols ? min(static_cast<int64_t>(kHeadGroup), A.cols - col0) : 0;
       // This lane's next target in these columns: its row of w (in the piece), its value, and its place.
-      const int2* targets = A.targets + (row < A.m ? row : 0) * A.top;
+      const int2* targets = SOFT ? A.targets + (row < A.m ? row : 0) * A.top : nullptr;
       int next = kNoTarget, value = 0, at = 0;
       HeadRow terms = {0.f, 0.f, 0.f, 0};
       if (row < A.m && cols > 0) {
-        if (GRAD) {
-          const float4 f = __ldg(reinterpret_cast<const float4*>(A.rows) + row);
-          terms = HeadRow{f.x * up, f.y, f.z, __float_as_int(f.w)};
-        }
         const int first = static_cast<int>(A.c0) + col0;
+        if (GRAD) {
+          terms = head_row(A.terms, A.ids, A.n, row);
+          terms.a *= up;
+        }
         if (SOFT) {
           int end = A.top;
           while (at < end) {  // the first one from these columns on
@@ -248,10 +276,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
               end = mid;
             }
           }
-        }
-        if (at < A.top) {
-          const int2 t = __ldg(targets + at);
-          if (t.x >= first && t.x != kNoTarget) next = t.x - static_cast<int>(A.c0), value = t.y;
+          if (at < A.top) {
+            const int2 t = __ldg(targets + at);
+            if (t.x != kNoTarget) next = t.x - static_cast<int>(A.c0), value = t.y;
+          }
+        } else {
+          const int64_t id = A.ids[row];
+          if (id >= first && id < A.n) next = static_cast<int>(id - A.c0);
         }
       }
       auto advance = [&] {
@@ -301,7 +332,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (!GRAD) {
           while (__any_sync(0xffffffffu, next < end)) {
             if (next < end) {
-              A.picked[row * A.top + value] = pick32(z, next - (col0 + c)) * A.scale;
+              A.picked[SOFT ? row * A.top + value : row] = pick32(z, next - (col0 + c)) * A.scale;
               advance();
             }
           }
@@ -373,21 +404,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 }
 
 // ---------------------------------------------------------------------------
-// A token's targets, sorted by their rows (by place among equal ones), and with `rows`
-// its terms of the gradient: one warp to a token.
+// A token's listed rows, sorted (by place among equal ones), and with `rows` their weights
+// and its terms of the gradient: one warp to a token.
 // ---------------------------------------------------------------------------
 constexpr int kTargetWarps = 4;
 
-__device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-  return v;
-}
-__device__ __forceinline__ float warp_add(float v) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
 __device__ __forceinline__ float teacher_at(const HeadTargets& t, int64_t row, int i) {
   const int64_t at = row * t.ld_teacher + i;
   const float v = t.teacher_type == OZ2_TYPE_F32 ? __ldg(static_cast<const float*>(t.teacher) + at)
@@ -408,8 +429,7 @@ __device__ __forceinline__ void teacher_sums(const HeadTargets& t, int64_t row, 
 }
 
 __global__ void __launch_bounds__(32 * kTargetWarps)
-    head_targets_kernel(int64_t m, int64_t n, HeadTargets t, int padded, int2* sorted, HeadRow* rows, const float* lse,
-                        const float* dloss, int dloss_each, float scale, float z_loss, int* largest) {
+    head_targets_kernel(int64_t m, int64_t n, HeadTargets t, int padded, int2* sorted, HeadRow* rows, HeadTerms terms) {
   extern __shared__ unsigned long long keys_s[];
   pdl_trigger();
   pdl_wait();
@@ -428,7 +448,7 @@ __global__ void __launch_bounds__(32 * kTargetWarps)
   }
   live = __any_sync(0xffffffffu, live);
   bad = __any_sync(0xffffffffu, bad);
-  if (t.soft && rows) teacher_sums(t, row, lane, &top, &sum);
+  if (rows) teacher_sums(t, row, lane, &top, &sum);
   __syncwarp();
   for (int size = 2; size <= padded; size <<= 1)
     for (int step = size >> 1; step; step >>= 1) {
@@ -442,21 +462,12 @@ __global__ void __launch_bounds__(32 * kTargetWarps)
   for (int i = lane; i < t.top; i += 32) {
     const int id = static_cast<int>(keys[i] >> 32), place = static_cast<int>(keys[i] & 0xFFFFFFFFu);
     int value = place;
-    if (rows) value = __float_as_int(t.soft && id != kNoTarget ? expf(teacher_at(t, row, place) - top) / sum : 1.f);
+    if (rows && id != kNoTarget) value = __float_as_int(expf(teacher_at(t, row, place) - top) / sum);
     sorted[row * t.top + i] = make_int2(id, value);
   }
   if (rows && lane == 0) {
-    const float l = lse[row];
-    HeadRow r;
-    r.a = live ? (bad ? __int_as_float(0x7FC00000) : dloss[dloss_each ? row : 0] * scale) : 0.f;
-    r.lse2 = l * kLog2E;
-    r.e = z_loss != 0.f ? 2.f * z_loss * l : 0.f;
-    r.live = live;
-    rows[row] = r;
-    if (largest) {
-      const float size = fabsf(r.a) * fmaxf(1.f, fabsf(1.f + r.e));
-      if (live && size < INFINITY) atomicMax(largest, __float_as_int(size));
-    }
+    const float g = live ? terms.dloss[terms.dloss_each ? row : 0] * terms.scale : 0.f;
+    rows[row] = HeadRow{bad ? __int_as_float(0x7FC00000) : g, live ? terms.lse[row] * kLog2E : 0.f, 0.f, live};
   }
 }
 
@@ -538,21 +549,24 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
 // Rows of x, zeros for the tokens that do not count: their gradient is zero times what
 // they hold, which need not be a number.
 // ---------------------------------------------------------------------------
-__global__ void __launch_bounds__(256) live_rows_kernel(int64_t m, int64_t k, const uint16_t* __restrict__ x, int64_t ldx,
-                                                        const HeadRow* __restrict__ rows, uint16_t* __restrict__ dst,
-                                                        int64_t ld_dst) {
+__global__ void __launch_bounds__(256) live_rows_kernel(int64_t m, int64_t n, int64_t k, const uint16_t* __restrict__ x,
+                                                        int64_t ldx, Ids ids, HeadTerms terms, float* __restrict__ largest,
+                                                        uint16_t* __restrict__ dst, int64_t ld_dst) {
   pdl_trigger();
   pdl_wait();
   const int per = static_cast<int>((k + 7) / 8);
   const uint16_t* end = x + (m - 1) * ldx + k;
+  float most = 0.f;
   for (int64_t r = blockIdx.x; r < m; r += gridDim.x) {
-    const bool live = rows[r].live != 0;
+    const HeadRow row = head_row(terms, ids, n, r);
+    most = fmaxf(most, head_size(row));
     for (int c = threadIdx.x; c < per; c += 256) {
       const uint16_t* p = x + r * ldx + 8 * c;
       *reinterpret_cast<uint4*>(dst + r * ld_dst + 8 * c) =
-          live ? load16_any(p, x, end, static_cast<int>(min(int64_t(8), k - 8 * c))) : make_uint4(0, 0, 0, 0);
+          row.live ? load16_any(p, x, end, static_cast<int>(min(int64_t(8), k - 8 * c))) : make_uint4(0, 0, 0, 0);
     }
   }
+  if (largest && threadIdx.x == 0) largest[blockIdx.x] = most;
 }
 
 // FP32 sums to the rows' type.
@@ -619,21 +633,22 @@ int padded_top(int top) {
 
 }  // namespace
 
-cudaError_t launch_head_targets(int64_t m, int64_t n, const HeadTargets& t, int2* sorted, HeadRow* rows, const float* lse,
-                                const float* dloss, int dloss_each, float scale, float z_loss, int* largest,
-                                cudaStream_t st) {
+cudaError_t launch_head_targets(int64_t m, int64_t n, const HeadTargets& t, int2* sorted, HeadRow* rows,
+                                const HeadTerms& terms, cudaStream_t st) {
   const int padded = padded_top(t.top);
   count_launch();
   return launch_dependent(head_targets_kernel, dim3(static_cast<unsigned>((m + kTargetWarps - 1) / kTargetWarps)),
                           dim3(32 * kTargetWarps), sizeof(unsigned long long) * padded * kTargetWarps, st, m, n, t, padded,
-                          sorted, rows, lse, dloss, dloss_each, scale, z_loss, largest);
+                          sorted, rows, terms);
 }
 
-cudaError_t launch_live_rows(int64_t m, int64_t k, const void* x, int64_t ldx, const HeadRow* rows, void* dst,
-                             int64_t ld_dst, cudaStream_t st) {
+int live_rows_maxima(int64_t m) { return static_cast<int>(std::min<int64_t>(m, 8 * num_sms())); }
+
+cudaError_t launch_live_rows(int64_t m, int64_t n, int64_t k, const void* x, int64_t ldx, Ids ids, const HeadTerms& terms,
+                             float* largest, void* dst, int64_t ld_dst, cudaStream_t st) {
   count_launch();
-  return launch_dependent(live_rows_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(m, 8 * num_sms()))), dim3(256), 0, st, m,
-                          k, static_cast<const uint16_t*>(x), ldx, rows, static_cast<uint16_t*>(dst), ld_dst);
+  return launch_dependent(live_rows_kernel, dim3(static_cast<unsigned>(live_rows_maxima(m))), dim3(256), 0, st, m, n, k,
+                          static_cast<const uint16_t*>(x), ldx, ids, terms, largest, static_cast<uint16_t*>(dst), ld_dst);
 }
 
 cudaError_t launch_head_forward(const HeadArgs& a, int type, Oz2Device* dev, cudaStream_t st) {

@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_grad_kernel(NormGradArgs
   constexpr int V = X::V, H = V / 2, kGroups = kNormThreads / TPR;
   constexpr bool STAGED = STAGES > 0, KEEP = VPT * V <= 16;
   __shared__ float exchange[kGroups][4 * TPR / 32];
-  // The rows' pieces, and after them the columns of dw, then of db, where there are groups to join.
+  // The rows' pieces, and after them the groups' columns of dw and db.
   extern __shared__ __align__(16) uint8_t norm_smem[];
   float* columns = reinterpret_cast<float*>(norm_smem);
   pdl_trigger();
@@ -410,44 +410,28 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_grad_kernel(NormGradArgs
     __syncthreads();  // the pieces' memory becomes the columns'
   }
   if (!parts) return;
-  float* to = parts + static_cast<int64_t>(blockIdx.x) * 2 * a.k;
+  // The groups' columns in shared memory, dw's and then db's, and their sums in the groups' order.
   constexpr int kCols = TPR * VPT * V;
-  auto keep = [&](const Two (&two_of)[VPT][H], float* row, float* join) {
-    float v[VPT][V];
+  auto put = [&](const Two (&v)[VPT][H], float* row) {
 #pragma unroll
     for (int i = 0; i < VPT; ++i)
 #pragma unroll
-      for (int e = 0; e < H; ++e) {
-        const float2 f = both(two_of[i][e]);
-        v[i][2 * e] = f.x, v[i][2 * e + 1] = f.y;
+      for (int e = 0; e < H; e += 2) {
+        const float2 p = both(v[i][e]), q = both(v[i][e + 1]);
+        *reinterpret_cast<float4*>(row + (t + i * TPR) * V + 2 * e) = make_float4(p.x, p.y, q.x, q.y);
       }
-    if (kGroups > 1) {
-      for (int q = 0; q < kGroups; ++q) {
-        __syncthreads();
-        if (group == q) {
-#pragma unroll
-          for (int i = 0; i < VPT; ++i)
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-              const int c = (t + i * TPR) * V + e;
-              join[c] = q ? join[c] + v[i][e] : v[i][e];
-            }
-        }
-      }
-      __syncthreads();
-      for (int c = threadIdx.x; c < a.k; c += kNormThreads) row[c] = join[c];
-    } else {
-#pragma unroll
-      for (int i = 0; i < VPT; ++i)
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const int64_t c = static_cast<int64_t>(t + i * TPR) * V + e;
-          if (c < a.k) row[c] = v[i][e];
-        }
-    }
   };
-  if (a.dw) keep(dw, to, columns);
-  if (a.db) keep(db, to + a.k, columns + kCols);
+  put(dw, columns + group * kCols);
+  put(db, columns + (kGroups + group) * kCols);
+  __syncthreads();
+  float* to = parts + static_cast<int64_t>(blockIdx.x) * 2 * a.k;
+  for (int c = threadIdx.x; c < a.k; c += kNormThreads) {
+    float w_sum = columns[c], b_sum = columns[kGroups * kCols + c];
+#pragma unroll
+    for (int q = 1; q < kGroups; ++q) w_sum += columns[q * kCols + c], b_sum += columns[(kGroups + q) * kCols + c];
+    to[c] = w_sum;
+    to[a.k + c] = b_sum;
+  }
 }
 
 // Long rows: dx by a block to a row, which reads it twice.
@@ -675,7 +659,7 @@ cudaError_t backward(const NormGradArgs& a, float* parts, cudaStream_t st) {
     const bool aligned = rows_on16(a.dy, a.lddy, es) && rows_on16(a.x, a.ldx, es) && (!a.r || rows_on16(a.r, a.ldr, es)) &&
                          (!a.dx || rows_on16(a.dx, a.lddx, es));
     auto kern = aligned ? by_shape<Backward<TYPE, true>::template K>(s) : by_shape<Backward<TYPE, false>::template K>(s);
-    const size_t join = s.tpr < kNormThreads ? 2 * sizeof(float) * s.tpr * s.vpt * Elem<TYPE>::V : 0;
+    const size_t join = 2 * sizeof(float) * kNormThreads * s.vpt * Elem<TYPE>::V;
     const size_t smem = std::max<size_t>(join, aligned ? 3 * 16 * kNormThreads * s.vpt * norm_stages(s.vpt) : 0);
     err = allow_smem(reinterpret_cast<const void*>(kern), smem);
     if (err != cudaSuccess) return err;

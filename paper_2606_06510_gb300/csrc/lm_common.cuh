@@ -125,8 +125,8 @@ cudaError_t launch_layer_norm_grad(const NormGradArgs& a, int type, void* scratc
 
 // --- losses over a vocabulary (k_head.cu) ------------------------------------------------
 // The logits z = scale·x·wᵀ are formed tile by tile and used where they are.  What a
-// token wants of them besides their sum of exponentials: its targets, rows of w with a
-// value each, as sorted pairs (row, value) of `top` a token.  The value is the target's
+// token wants of them besides their sum of exponentials: its target, or its `top` listed
+// rows of w with a value each, as sorted pairs (row, value).  The value is the entry's
 // place in `picked` (forward) or its weight as FP32 bits (gradient).
 constexpr int kNoTarget = 0x7FFFFFFF;
 struct HeadTargets {
@@ -144,6 +144,14 @@ struct HeadRow {
   float a, lse2, e;
   int live;
 };
+// What they come of: the losses' gradient (one a token, or one for all) and lse, and for
+// listed rows, whose prepared terms are read.
+struct HeadTerms {
+  const HeadRow* rows;  // or null
+  const float *dloss, *lse;
+  int dloss_each;
+  float scale, z_loss;
+};
 struct HeadArgs {
   int64_t m, n, k;
   const void* x;       // rows on 16-byte boundaries, like w's
@@ -152,29 +160,31 @@ struct HeadArgs {
   int64_t ldw;
   int64_t c0, cols;    // the piece of the vocabulary
   float scale;
-  const int2* targets; // (m, top), sorted
+  Ids ids;             // targets, one a token
+  const int2* targets; // or sorted entries (m, top)
   int top, soft;
   // forward
   float2* stats;       // (groups of 64 columns, ld_stats): max and sum of exp2 of z·log2 e
   int64_t ld_stats;
   float* picked;       // (m, top)
   // gradient
-  const HeadRow* rows;
-  const int* largest;  // bits of the largest |a·(1 + e)|, or null: dz is not scaled
+  HeadTerms terms;
+  const float* largest;  // maxima of |a|·max(1, |1 + e|), `maxima` of them, or null: dz is not scaled
+  int maxima;
   float* unscale;      // dz's scale, inverted (written)
   uint16_t* dz;
   int64_t ld_dz;
 };
 constexpr int kHeadGroup = 64;
 constexpr int kMaxTop = 1024;
-// Targets sorted; with `rows`, weights and the rows' terms too (dloss: one a token, or one for
-// all), the largest of them into `largest` (zero before, or null).
-cudaError_t launch_head_targets(int64_t m, int64_t n, const HeadTargets& t, int2* sorted, HeadRow* rows, const float* lse,
-                                const float* dloss, int dloss_each, float scale, float z_loss, int* largest,
-                                cudaStream_t st);
-// x's rows of live tokens to rows of ld_dst elements on 16-byte boundaries, zeros for the others.
-cudaError_t launch_live_rows(int64_t m, int64_t k, const void* x, int64_t ldx, const HeadRow* rows, void* dst,
-                             int64_t ld_dst, cudaStream_t st);
+// A token's entries sorted; with `rows`, their weights and the rows' terms too.
+cudaError_t launch_head_targets(int64_t m, int64_t n, const HeadTargets& t, int2* sorted, HeadRow* rows,
+                                const HeadTerms& terms, cudaStream_t st);
+// x's rows of live tokens to rows of ld_dst elements on 16-byte boundaries, zeros for the others; and
+// with `largest` the maxima for HeadArgs, as many as live_rows_maxima(m).
+int live_rows_maxima(int64_t m);
+cudaError_t launch_live_rows(int64_t m, int64_t n, int64_t k, const void* x, int64_t ldx, Ids ids, const HeadTerms& terms,
+                             float* largest, void* dst, int64_t ld_dst, cudaStream_t st);
 cudaError_t launch_head_forward(const HeadArgs& a, int type, Oz2Device* dev, cudaStream_t st);
 cudaError_t launch_head_grad(const HeadArgs& a, int type, Oz2Device* dev, cudaStream_t st);
 // lse from the groups' stats; then losses, and picked where no logit is.

@@ -54,16 +54,17 @@ int head_forward(const HeadCall& c, float* loss, float* lse, float* picked, cuda
   Workspace ws(st);
   Operand X(c.X, c.ldx, c.k ? c.m : 0, c.k, 2, ws), W(c.W, c.ldw, c.k ? c.n : 0, c.k, 2, ws);
   const int64_t ld_stats = (c.m + 31) / 32 * 32, groups = (c.n + kHeadGroup - 1) / kHeadGroup;
-  const size_t stats = ws.ask(sizeof(float2) * ld_stats * groups), sorted = ws.ask(sizeof(int2) * c.m * c.t.top);
+  const size_t stats = ws.ask(sizeof(float2) * ld_stats * groups);
+  const size_t sorted = c.t.soft ? ws.ask(sizeof(int2) * c.m * c.t.top) : 0;
   if (!ws.take()) return OZ2_ERR_ALLOC;
   cudaError_t err = place(X, W, ws, st);
-  if (err == cudaSuccess)
-    err = launch_head_targets(c.m, c.n, c.t, ws.at<int2>(sorted), nullptr, nullptr, nullptr, 0, 0.f, 0.f, nullptr, st);
+  if (err == cudaSuccess && c.t.soft) err = launch_head_targets(c.m, c.n, c.t, ws.at<int2>(sorted), nullptr, HeadTerms{}, st);
   HeadArgs a{};
   a.m = c.m, a.n = c.n, a.k = c.k;
   a.x = X.p, a.ldx = X.ld, a.w = W.p, a.ldw = W.ld;
   a.cols = c.n;
   a.scale = c.scale;
+  a.ids = c.t.ids;
   a.targets = ws.at<int2>(sorted);
   a.top = c.t.top, a.soft = c.t.soft;
   a.stats = ws.at<float2>(stats), a.ld_stats = ld_stats;
@@ -111,8 +112,10 @@ int head_grad(const HeadCall& c, const HeadGrads& g, int id_bits, cudaStream_t s
   } kinds[2];
   const int64_t ld_dz = (piece + 63) / 64 * 64, ld_sum = (c.k + 31) / 32 * 32;
   Workspace ws(st);
-  const size_t rows = ws.ask(sizeof(HeadRow) * c.m), sorted = ws.ask(sizeof(int2) * c.m * c.t.top), words = ws.ask(2 * sizeof(float));
-  Operand X(c.X, c.ldx, c.m, c.k, 2, ws, want_dw), W(c.W, c.ldw, c.n, c.k, 2, ws);
+  const size_t rows = c.t.soft ? ws.ask(sizeof(HeadRow) * c.m) : 0, sorted = c.t.soft ? ws.ask(sizeof(int2) * c.m * c.t.top) : 0;
+  const size_t maxima = scaled ? ws.ask(sizeof(float) * (live_rows_maxima(c.m) + 1)) : 0;
+  // (x's copy is where the largest of the terms is found, and dead tokens' x made zeros for dw.)
+  Operand X(c.X, c.ldx, c.m, c.k, 2, ws, want_dw || scaled), W(c.W, c.ldw, c.n, c.k, 2, ws);
   const size_t dz = ws.ask(2 * static_cast<size_t>(c.m) * ld_dz);
   const size_t sums = want_dx && pieces > 1 ? ws.ask(sizeof(float) * static_cast<size_t>(c.m) * ld_sum) : 0;
   for (int kind = 0; kind < 2; ++kind) {
@@ -140,15 +143,17 @@ int head_grad(const HeadCall& c, const HeadGrads& g, int id_bits, cudaStream_t s
     for (int i = 0; i < q.launches; ++i) q.scratch[i] = ws.ask(q.plan[i].scratch);
   }
   if (!ws.take()) return OZ2_ERR_ALLOC;
-  int* largest = scaled ? ws.at<int>(words) : nullptr;
-  float* unscale = scaled ? ws.at<float>(words) + 1 : nullptr;
-  cudaError_t err = scaled ? cudaMemsetAsync(largest, 0, sizeof(int), st) : cudaSuccess;
-  if (err == cudaSuccess)
-    err = launch_head_targets(c.m, c.n, c.t, ws.at<int2>(sorted), ws.at<HeadRow>(rows), g.lse, g.dloss,
-                              (g.flags & OZ2_GRAD_ONE_DLOSS) == 0, c.scale, c.z_loss, largest, st);
+  float* largest = scaled ? ws.at<float>(maxima) + 1 : nullptr;
+  float* unscale = scaled ? ws.at<float>(maxima) : nullptr;
+  HeadTerms terms{nullptr, g.dloss, g.lse, (g.flags & OZ2_GRAD_ONE_DLOSS) == 0, c.scale, c.z_loss};
+  cudaError_t err = cudaSuccess;
+  if (c.t.soft) {
+    err = launch_head_targets(c.m, c.n, c.t, ws.at<int2>(sorted), ws.at<HeadRow>(rows), terms, st);
+    terms.rows = ws.at<HeadRow>(rows);
+  }
   if (err == cudaSuccess && X.copy) {
     const int64_t ld = padded_ld(c.k, 2);
-    err = launch_live_rows(c.m, c.k, c.X, c.ldx, ws.at<HeadRow>(rows), ws.at<void>(X.off), ld, st);
+    err = launch_live_rows(c.m, c.n, c.k, c.X, c.ldx, c.t.ids, terms, largest, ws.at<void>(X.off), ld, st);
     X.p = ws.at<void>(X.off);
     X.ld = ld;
     X.copy = false;
@@ -163,10 +168,11 @@ int head_grad(const HeadCall& c, const HeadGrads& g, int id_bits, cudaStream_t s
     a.x = X.p, a.ldx = X.ld, a.w = w, a.ldw = W.ld;
     a.c0 = c0, a.cols = cols;
     a.scale = c.scale;
+    a.ids = c.t.ids;
     a.targets = ws.at<int2>(sorted);
     a.top = c.t.top, a.soft = c.t.soft;
-    a.rows = ws.at<HeadRow>(rows);
-    a.largest = largest, a.unscale = unscale;
+    a.terms = terms;
+    a.largest = largest, a.maxima = live_rows_maxima(c.m), a.unscale = unscale;
     a.dz = ws.at<uint16_t>(dz), a.ld_dz = ld_dz;
     err = launch_head_grad(a, c.type, dev, st);
     int at = 0;
