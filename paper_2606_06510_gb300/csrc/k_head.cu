@@ -78,9 +78,30 @@ __device__ __forceinline__ float warp_add(float v) {
   return v;
 }
 
+// The first of `count` sorted entries whose row is `first` or more: eight parts at a time,
+// whose ends are loaded together (by halves, 64 entries are six loads one after another in
+// every tile's epilogue: 1111 tokens, 33 entries each, 62 us of which the tiles' products
+// are 40).
+__device__ __forceinline__ int first_from(const int2* entries, int count, int first) {
+  int at = 0;
+  while (count > 0) {  // it is one of [at, at + count]
+    const int step = (count + 7) >> 3;
+    int below = 0;
+#pragma unroll
+    for (int i = 1; i < 8; ++i) {
+      const int p = i * step - 1;
+      if (p < count && __ldg(&entries[at + p].x) < first) ++below;
+    }
+    const int passed = below * step, end = passed + step - 1;
+    at += passed;
+    count = below < 7 && end < count ? step - 1 : count - passed;
+  }
+  return at;
+}
+
 // v[j] for a j that the compiler does not know.
-__device__ __forceinline__ float pick32(const float (&v)[32], int j) {
-  float t[16];
+__device__ __forceinline__ float pick32(const uint32_t (&v)[32], int j) {
+  uint32_t t[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) t[i] = j & 1 ? v[2 * i + 1] : v[2 * i];
 #pragma unroll
@@ -88,7 +109,7 @@ __device__ __forceinline__ float pick32(const float (&v)[32], int j) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (i < n) t[i] = j & b ? t[2 * i + 1] : t[2 * i];
-  return t[0];
+  return __uint_as_float(t[0]);
 }
 __device__ __forceinline__ void add32(float (&v)[32], int j, float d) {
 #pragma unroll
@@ -101,14 +122,56 @@ __device__ __forceinline__ void set32(float (&v)[32], int j, float d) {
     if (i == j) v[i] = d;
 }
 
+// A lane's maximum of v·to2 over its 64 sums (the first `cols` where not WHOLE), and the sum
+// of exp2 of the differences: the largest sum first, in its own units (NEGATIVE to2: the
+// smallest), then one multiply-add for two differences.
+template <bool NEGATIVE>
+__device__ __forceinline__ float extreme(float a, float b, float c) {
+  float r;
+  if (NEGATIVE) {
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  } else {
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  }
+  return r;
+}
+template <bool WHOLE, bool NEGATIVE>
+__device__ __forceinline__ void head_sums(const uint32_t (&v0)[32], const uint32_t (&v1)[32], int cols, float to2, float& most,
+                                          float& sum) {
+  auto t = [&](int j) {  // past the vocabulary's end: the first one again
+    const float v = __uint_as_float(j < 32 ? v0[j & 31] : v1[j & 31]);
+    return WHOLE || j < cols ? v : __uint_as_float(v0[0]);
+  };
+  float top[4] = {t(0), t(1), t(2), t(3)};
+#pragma unroll
+  for (int j = 4; j < 60; j += 8)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top[e] = extreme<NEGATIVE>(top[e], t(j + e), t(j + 4 + e));
+  top[0] = extreme<NEGATIVE>(top[0], top[1], t(60));
+  top[1] = extreme<NEGATIVE>(top[2], t(61), t(62));
+  top[2] = extreme<NEGATIVE>(top[3], t(63), t(63));
+  most = fmaxf(extreme<NEGATIVE>(top[0], top[1], top[2]) * to2, kLowest);
+  const Two to = two(to2, to2), less = two(-most, -most);
+  Two s[2] = {two(0.f, 0.f), two(0.f, 0.f)};
+#pragma unroll
+  for (int j = 0; j < 64; j += 2) {
+    const float2 x = both(fma(two(t(j), t(j + 1)), to, less));
+    float a = exp2_fast(x.x), b = exp2_fast(x.y);
+    if (!WHOLE) a = j < cols ? a : 0.f, b = j + 1 < cols ? b : 0.f;
+    s[j >> 1 & 1] = s[j >> 1 & 1] + two(a, b);
+  }
+  const float2 r = both(s[0] + s[1]);
+  sum = r.x + r.y;
+}
+
 // ---------------------------------------------------------------------------
 // Tiles of 256 tokens × 256 rows of w on CTA pairs as in linear_pair_kernel: 128 rows
 // of each operand a CTA, two accumulators in tensor memory, so that a tile's epilogue
 // runs beside the next one's products.  An epilogue warp has 32 tokens, one a lane, and
 // 64 columns.
 //
-// Forward, a lane brings its logits to powers of two, takes their maximum and sums
-// exp2 of the differences, 32 columns and then the next 32 joined to them.
+// Forward, a lane takes the maximum of its logits in powers of two and sums exp2 of the
+// differences; its group's two numbers are joined to the others' by head_join_kernel.
 // ---------------------------------------------------------------------------
 template <int TYPE, bool GRAD, bool SOFT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
@@ -251,47 +314,48 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       if (blockIdx.x == 0 && threadIdx.x == 64) *A.unscale = __int_as_float((127 - s) << 23);
     }
     uint32_t acc = 0, accph = 0;
-    for (int i = pair; head_tile(U, i, tile); i += npairs) {
-      // A half tile is two warps' columns: the others have none.
-      const int64_t row = static_cast<int64_t>(tile.tm) * kTile + rank * kRows + 32 * q + lane;
-      const int col0 = tile.col + kHeadGroup * h;             // in the piece
-      const int cols = kHeadGroup * h < tile.width && col0 < A.cols ? min(static_cast<int64_t>(kHeadGroup), A.cols - col0) : 0;
-      // This lane's next target in these columns: its row of w (in the piece), its value, and its place.
-      const int2* targets = SOFT ? A.targets + (row < A.m ? row : 0) * A.top : nullptr;
-      int next = kNoTarget, value = 0, at = 0;
-      HeadRow terms = {0.f, 0.f, 0.f, 0};
-      if (row < A.m && cols > 0) {
-        const int first = static_cast<int>(A.c0) + col0;
+    // What a lane has to know of its token for a tile, and where in the tile its warp is: read
+    // while the tile before is worked on.
+    struct Part {
+      int row;
+      int col0, cols;        // in the piece; of the warp (a half tile is two warps' columns)
+      int next, value, at;   // the token's first target here: its row of w (in the piece), value and place,
+      int2 after;            // and the entry that follows
+      HeadRow terms;
+    };
+    auto find = [&](int i, Part& p) {
+      if (!head_tile(U, i, tile)) return false;
+      p.row = tile.tm * kTile + rank * kRows + 32 * q + lane;
+      p.col0 = tile.col + kHeadGroup * h;
+      p.cols = kHeadGroup * h < tile.width && p.col0 < A.cols ? min(static_cast<int64_t>(kHeadGroup), A.cols - p.col0) : 0;
+      p.next = kNoTarget, p.value = 0, p.at = 0;
+      p.terms = HeadRow{0.f, 0.f, 0.f, 0};
+      if (p.row < A.m && p.cols > 0) {
+        const int first = static_cast<int>(A.c0) + p.col0;
         if (GRAD) {
-          terms = head_row(A.terms, A.ids, A.n, row);
-          terms.a *= up;
+          p.terms = head_row(A.terms, A.ids, A.n, p.row);
+          p.terms.a *= up;
         }
         if (SOFT) {
-          int end = A.top;
-          while (at < end) {  // the first one from these columns on
-            const int mid = (at + end) >> 1;
-            if (__ldg(&targets[mid].x) < first) {
-              at = mid + 1;
-            } else {
-              end = mid;
-            }
-          }
-          if (at < A.top) {
-            const int2 t = __ldg(targets + at);
-            if (t.x != kNoTarget) next = t.x - static_cast<int>(A.c0), value = t.y;
+          const int2* targets = A.targets + static_cast<int64_t>(p.row) * A.top;
+          p.at = first_from(targets, A.top, first);
+          p.after = make_int2(kNoTarget, 0);
+          if (p.at < A.top) {
+            const int2 t = __ldg(targets + p.at);
+            if (p.at + 1 < A.top) p.after = __ldg(targets + p.at + 1);
+            if (t.x != kNoTarget) p.next = t.x - static_cast<int>(A.c0), p.value = t.y;
           }
         } else {
-          const int64_t id = A.ids[row];
-          if (id >= first && id < A.n) next = static_cast<int>(id - A.c0);
+          const int64_t id = A.ids[p.row];
+          if (id >= first && id < A.n) p.next = static_cast<int>(id - A.c0);
         }
       }
-      auto advance = [&] {
-        next = kNoTarget;
-        if (SOFT && ++at < A.top) {
-          const int2 t = __ldg(targets + at);
-          if (t.x != kNoTarget) next = t.x - static_cast<int>(A.c0), value = t.y;
-        }
-      };
+      return true;
+    };
+    Part now, then;
+    bool more = find(pair, now);
+    for (int i = pair; more; now = then) {
+      i += npairs;
       if (steps) {
         if (!mbar_wait_bounded(acc_full + 8 * acc, accph, kWaitLimit)) ok = false;
         if (!__all_sync(0xffffffffu, ok)) {
@@ -300,7 +364,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
         tc_fence_after();
       }
+      const int row = now.row;
+      const int col0 = now.col0, cols = now.cols;
       const uint32_t from = tmem + (static_cast<uint32_t>(32 * q) << 16) + acc * kTile + kHeadGroup * h;
+      auto load = [&](int c, uint32_t (&v)[32]) {
+        if (steps) {
+          tmem_ld32(from + c, v);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = 0u;
+        }
+      };
       auto release = [&] {  // the sums are in registers: the next but one tile's products may begin
         if (steps) {
           tc_fence_before();
@@ -310,67 +384,74 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           if (acc == 0) accph ^= 1;
         }
       };
-      if (cols == 0) release();
-      float most = kLowest, sum = 0.f;
-      const float main = terms.a * (1.f + terms.e);
-      const int64_t row0 = row - lane;
-#pragma unroll 1
-      for (int c = 0; c < cols; c += kChunk) {
-        float z[32];
-        if (steps) {
-          uint32_t v[32];
-          tmem_ld32(from + c, v);
-          tmem_ld_wait();
-          if (c + kChunk >= cols) release();
-#pragma unroll
-          for (int j = 0; j < 32; ++j) z[j] = __uint_as_float(v[j]);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 32; ++j) z[j] = 0.f;
+      if (cols == 0) {
+        release();
+        more = find(i, then);
+        continue;
+      }
+      const int2* targets = SOFT ? A.targets + static_cast<int64_t>(row < A.m ? row : 0) * A.top : nullptr;
+      auto advance = [&] {
+        now.next = kNoTarget;
+        if (SOFT) {  // (the one after it is on its way while this one is looked for in the columns)
+          if (now.after.x != kNoTarget) now.next = now.after.x - static_cast<int>(A.c0), now.value = now.after.y;
+          now.after = make_int2(kNoTarget, 0);
+          if (++now.at + 1 < A.top) now.after = __ldg(targets + now.at + 1);
         }
-        const int left = cols - c, end = col0 + c + kChunk;
-        if (!GRAD) {
-          while (__any_sync(0xffffffffu, next < end)) {
-            if (next < end) {
-              A.picked[SOFT ? row * A.top + value : row] = pick32(z, next - (col0 + c)) * A.scale;
+      };
+      if (!GRAD) {
+        auto pick = [&](const uint32_t (&v)[32], int from) {
+          while (__any_sync(0xffffffffu, now.next < from + 32)) {
+            if (now.next < from + 32) {
+              A.picked[SOFT ? static_cast<int64_t>(row) * A.top + now.value : row] = pick32(v, now.next - from) * A.scale;
               advance();
             }
           }
           __syncwarp();
-#pragma unroll
-          for (int j = 0; j < 32; ++j) z[j] *= to2;
-          if (left < kChunk) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (j >= left) z[j] = -INFINITY;
-          }
-          float top = most;
-#pragma unroll
-          for (int j = 0; j < 32; ++j) top = fmaxf(top, z[j]);
-          sum *= exp2_fast(most - top);
-          most = top;
-          float s[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int j = 0; j < 32; ++j) s[j & 3] += exp2_fast(z[j] - top);
-          sum += (s[0] + s[1]) + (s[2] + s[3]);
+        };
+        uint32_t v0[32], v1[32];
+        load(0, v0);
+        load(32, v1);
+        tmem_ld_wait();
+        release();
+        more = find(i, then);
+        pick(v0, col0);
+        pick(v1, col0 + 32);
+        float most, sum;
+        if (to2 >= 0.f) {
+          cols == kHeadGroup ? head_sums<true, false>(v0, v1, cols, to2, most, sum)
+                             : head_sums<false, false>(v0, v1, cols, to2, most, sum);
         } else {
+          head_sums<false, true>(v0, v1, cols, to2, most, sum);
+        }
+        if (row < A.m) A.stats[static_cast<int64_t>(col0 / kHeadGroup) * A.ld_stats + row] = make_float2(most, sum);
+      } else {
+        const int row0 = row - lane;
+        auto gradients = [&](const uint32_t (&v)[32], int c) {
+          const HeadRow& t = now.terms;
+          const int from = col0 + c, end = from + 32;
           float hard = 0.f;
-          if (!SOFT && next < end) hard = pick32(z, next - (col0 + c));
+          if (!SOFT && now.next < end) hard = pick32(v, now.next - from);
+          const float main = t.a * (1.f + t.e);
+          const Two to = two(to2, to2), less = two(-t.lse2, -t.lse2), by = two(main, main);
+          float z[32];
 #pragma unroll
-          for (int j = 0; j < 32; ++j) z[j] = main * exp2_fast(fmaf(z[j], to2, -terms.lse2));
-          while (__any_sync(0xffffffffu, next < end)) {
-            if (next < end) {
+          for (int j = 0; j < 32; j += 2) {
+            const float2 x = both(fma(two(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), to, less));
+            const float2 d = both(two(exp2_fast(x.x), exp2_fast(x.y)) * by);
+            z[j] = d.x, z[j + 1] = d.y;
+          }
+          while (__any_sync(0xffffffffu, now.next < end)) {
+            if (now.next < end) {
               if (SOFT) {
-                add32(z, next - (col0 + c), -terms.a * __int_as_float(value));
+                add32(z, now.next - from, -t.a * __int_as_float(now.value));
               } else {  // (1 + e)·p - 1 with p near 1: by p - 1
-                set32(z, next - (col0 + c),
-                      terms.a * fmaf(1.f + terms.e, expm1f(fmaf(hard, to2, -terms.lse2) * kLn2), terms.e));
+                set32(z, now.next - from, t.a * fmaf(1.f + t.e, expm1f(fmaf(hard, to2, -t.lse2) * kLn2), t.e));
               }
               advance();
             }
           }
           __syncwarp();
-          if (!terms.live) {
+          if (!t.live) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) z[j] = 0.f;
           }
@@ -382,15 +463,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           __syncwarp();
           // (dz's rows are on 16-byte boundaries, and there are multiples of 64 of its columns.)
           if (row0 + 32 <= A.m) {
-            store_fast(A.dz + (row0 + (lane >> 2)) * A.ld_dz + col0 + c + 8 * (lane & 3), A.ld_dz, lane, buf);
+            store_fast(A.dz + static_cast<int64_t>(row0 + (lane >> 2)) * A.ld_dz + from + 8 * (lane & 3), A.ld_dz, lane, buf);
           } else {
-            store_slow(A.dz, A.ld_dz, A.m, A.cols, row0, col0 + c, lane, buf);
+            store_slow(A.dz, A.ld_dz, A.m, A.cols, row0, from, lane, buf);
           }
           __syncwarp();
-        }
+        };
+        uint32_t v[32];
+        load(0, v);
+        tmem_ld_wait();
+        more = find(i, then);
+        gradients(v, 0);
+        if (cols > 32) load(32, v);
+        tmem_ld_wait();
+        release();
+        if (cols > 32) gradients(v, 32);
       }
-      if (!GRAD && cols > 0 && row < A.m)
-        A.stats[static_cast<int64_t>(col0 / kHeadGroup) * A.ld_stats + row] = make_float2(most, sum);
     }
     if (!ok) {
       dev->status = kStatusTimeout;

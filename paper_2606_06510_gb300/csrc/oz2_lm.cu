@@ -48,11 +48,27 @@ bool head_pointers(const HeadCall& c, int id_bits) {
          (!c.t.soft || (c.t.teacher && on(c.t.teacher, type_bytes(c.t.teacher_type))));
 }
 
+// Operands on 16-byte boundaries that are not 32-byte ones slow TMA (see oz2_linear): 4096
+// tokens × 32000×1000 take 196 us, so 142 at 1024.  The smaller one is copied where that pays,
+// and w where its products (`uses` of them) gain enough by what is then left, a ninth of their time.
+struct HeadCopies {
+  bool x, w;
+};
+HeadCopies head_copies(const HeadCall& c, int uses, bool x_copied) {
+  const bool slow_x = on16_only(c.X, c.ldx, 2) && !x_copied, slow_w = on16_only(c.W, c.ldw, 2);
+  const double product = static_cast<double>(c.m) * c.n * c.k;
+  HeadCopies r{false, false};
+  if (slow_x && slow_w && copy_pays(2.0 * std::min(c.m, c.n) * c.k, product, 2)) (c.m <= c.n ? r.x : r.w) = true;
+  if (slow_w && !r.w && (r.x || x_copied) && copy_pays(2.0 * c.n * c.k, 0.55 * uses * product, 2)) r.w = true;
+  return r;
+}
+
 int head_forward(const HeadCall& c, float* loss, float* lse, float* picked, cudaStream_t st) {
   Oz2Device* dev = device_status();
   if (!dev) return OZ2_ERR_CUDA;
   Workspace ws(st);
-  Operand X(c.X, c.ldx, c.k ? c.m : 0, c.k, 2, ws), W(c.W, c.ldw, c.k ? c.n : 0, c.k, 2, ws);
+  const HeadCopies copies = head_copies(c, 1, false);
+  Operand X(c.X, c.ldx, c.k ? c.m : 0, c.k, 2, ws, copies.x), W(c.W, c.ldw, c.k ? c.n : 0, c.k, 2, ws, copies.w);
   const int64_t ld_stats = (c.m + 31) / 32 * 32, groups = (c.n + kHeadGroup - 1) / kHeadGroup;
   const size_t stats = ws.ask(sizeof(float2) * ld_stats * groups);
   const size_t sorted = c.t.soft ? ws.ask(sizeof(int2) * c.m * c.t.top) : 0;
@@ -115,7 +131,8 @@ int head_grad(const HeadCall& c, const HeadGrads& g, int id_bits, cudaStream_t s
   const size_t rows = c.t.soft ? ws.ask(sizeof(HeadRow) * c.m) : 0, sorted = c.t.soft ? ws.ask(sizeof(int2) * c.m * c.t.top) : 0;
   const size_t maxima = scaled ? ws.ask(sizeof(float) * (live_rows_maxima(c.m) + 1)) : 0;
   // (x's copy is where the largest of the terms is found, and dead tokens' x made zeros for dw.)
-  Operand X(c.X, c.ldx, c.m, c.k, 2, ws, want_dw || scaled), W(c.W, c.ldw, c.n, c.k, 2, ws);
+  const HeadCopies copies = head_copies(c, want_dx ? 2 : 1, want_dw || scaled);
+  Operand X(c.X, c.ldx, c.m, c.k, 2, ws, want_dw || scaled || copies.x), W(c.W, c.ldw, c.n, c.k, 2, ws, copies.w);
   const size_t dz = ws.ask(2 * static_cast<size_t>(c.m) * ld_dz);
   const size_t sums = want_dx && pieces > 1 ? ws.ask(sizeof(float) * static_cast<size_t>(c.m) * ld_sum) : 0;
   for (int kind = 0; kind < 2; ++kind) {
