@@ -78,27 +78,6 @@ __device__ __forceinline__ float warp_add(float v) {
   return v;
 }
 
-// The first of `count` sorted entries whose row is `first` or more: eight parts at a time,
-// whose ends are loaded together (by halves, 64 entries are six loads one after another in
-// every tile's epilogue: 1111 tokens, 33 entries each, 62 us of which the tiles' products
-// are 40).
-__device__ __forceinline__ int first_from(const int2* entries, int count, int first) {
-  int at = 0;
-  while (count > 0) {  // it is one of [at, at + count]
-    const int step = (count + 7) >> 3;
-    int below = 0;
-#pragma unroll
-    for (int i = 1; i < 8; ++i) {
-      const int p = i * step - 1;
-      if (p < count && __ldg(&entries[at + p].x) < first) ++below;
-    }
-    const int passed = below * step, end = passed + step - 1;
-    at += passed;
-    count = below < 7 && end < count ? step - 1 : count - passed;
-  }
-  return at;
-}
-
 // v[j] for a j that the compiler does not know.
 __device__ __forceinline__ float pick32(const uint32_t (&v)[32], int j) {
   uint32_t t[16];
@@ -110,11 +89,6 @@ __device__ __forceinline__ float pick32(const uint32_t (&v)[32], int j) {
     for (int i = 0; i < 8; ++i)
       if (i < n) t[i] = j & b ? t[2 * i + 1] : t[2 * i];
   return __uint_as_float(t[0]);
-}
-__device__ __forceinline__ void add32(float (&v)[32], int j, float d) {
-#pragma unroll
-  for (int i = 0; i < 32; ++i)
-    if (i == j) v[i] += d;
 }
 __device__ __forceinline__ void set32(float (&v)[32], int j, float d) {
 #pragma unroll
@@ -319,16 +293,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     struct Part {
       int row;
       int col0, cols;        // in the piece; of the warp (a half tile is two warps' columns)
-      int next, value, at;   // the token's first target here: its row of w (in the piece), value and place,
-      int2 after;            // and the entry that follows
+      int next;              // the token's target here: its row of w (in the piece)
+      int at, end;           // or the warp's entries here
       HeadRow terms;
+    };
+    auto entry_at = [&](int at, int end) {
+      return at < end ? __ldg(A.entries + at) : make_int4(kNoTarget, 0, 0, 0);
     };
     auto find = [&](int i, Part& p) {
       if (!head_tile(U, i, tile)) return false;
       p.row = tile.tm * kTile + rank * kRows + 32 * q + lane;
       p.col0 = tile.col + kHeadGroup * h;
       p.cols = kHeadGroup * h < tile.width && p.col0 < A.cols ? min(static_cast<int64_t>(kHeadGroup), A.cols - p.col0) : 0;
-      p.next = kNoTarget, p.value = 0, p.at = 0;
+      p.next = kNoTarget;
+      if (SOFT) p.at = p.end = 0;
       p.terms = HeadRow{0.f, 0.f, 0.f, 0};
       if (p.row < A.m && p.cols > 0) {
         const int first = static_cast<int>(A.c0) + p.col0;
@@ -336,19 +314,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           p.terms = head_row(A.terms, A.ids, A.n, p.row);
           p.terms.a *= up;
         }
-        if (SOFT) {
-          const int2* targets = A.targets + static_cast<int64_t>(p.row) * A.top;
-          p.at = first_from(targets, A.top, first);
-          p.after = make_int2(kNoTarget, 0);
-          if (p.at < A.top) {
-            const int2 t = __ldg(targets + p.at);
-            if (p.at + 1 < A.top) p.after = __ldg(targets + p.at + 1);
-            if (t.x != kNoTarget) p.next = t.x - static_cast<int>(A.c0), p.value = t.y;
-          }
-        } else {
+        if (!SOFT) {
           const int64_t id = A.ids[p.row];
           if (id >= first && id < A.n) p.next = static_cast<int>(id - A.c0);
         }
+      }
+      if (SOFT && p.cols > 0 && p.row - lane < A.m) {
+        const int* offset = A.offsets + ((p.row >> 5) * A.groups1 + (A.c0 + p.col0) / kHeadGroup);
+        p.at = __ldg(offset), p.end = __ldg(offset + 1);
       }
       return true;
     };
@@ -356,6 +329,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     bool more = find(pair, now);
     for (int i = pair; more; now = then) {
       i += npairs;
+      int4 entry;
+      if (SOFT) entry = entry_at(now.at + lane, now.end);
       if (steps) {
         if (!mbar_wait_bounded(acc_full + 8 * acc, accph, kWaitLimit)) ok = false;
         if (!__all_sync(0xffffffffu, ok)) {
@@ -389,24 +364,45 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         more = find(i, then);
         continue;
       }
-      const int2* targets = SOFT ? A.targets + static_cast<int64_t>(row < A.m ? row : 0) * A.top : nullptr;
-      auto advance = [&] {
-        now.next = kNoTarget;
-        if (SOFT) {  // (the one after it is on its way while this one is looked for in the columns)
-          if (now.after.x != kNoTarget) now.next = now.after.x - static_cast<int>(A.c0), now.value = now.after.y;
-          now.after = make_int2(kNoTarget, 0);
-          if (++now.at + 1 < A.top) now.after = __ldg(targets + now.at + 1);
-        }
+      // Listed rows: the warp walks its entries in the order of their columns, each of which is
+      // one lane's.
+      int taken = 0, column = kNoTarget;  // of the 32 at hand; of the next one, in the piece
+      auto look = [&] {
+        column = __shfl_sync(0xffffffffu, entry.x, taken);
+        if (column != kNoTarget) column -= static_cast<int>(A.c0);
       };
+      auto advance = [&] {
+        if (++taken == 32) {
+          taken = 0;
+          now.at += 32;
+          entry = entry_at(now.at + lane, now.end);
+        }
+        look();
+      };
+      if (SOFT) {
+        look();
+      }
       if (!GRAD) {
         auto pick = [&](const uint32_t (&v)[32], int from) {
-          while (__any_sync(0xffffffffu, now.next < from + 32)) {
-            if (now.next < from + 32) {
-              A.picked[SOFT ? static_cast<int64_t>(row) * A.top + now.value : row] = pick32(v, now.next - from) * A.scale;
-              advance();
+          if (SOFT) {
+#pragma unroll
+            for (int g = 0; g < 32; g += 8) {
+              while (column < from + g + 8) {
+                const int at = column - (from + g), who = __shfl_sync(0xffffffffu, entry.y, taken);
+                uint32_t e = v[g];
+#pragma unroll
+                for (int j = 1; j < 8; ++j) e = j == at ? v[g + j] : e;
+                if (lane == (who & 31)) A.picked[static_cast<int64_t>(row) * A.top + (who >> 5)] = __uint_as_float(e) * A.scale;
+                advance();
+              }
             }
+          } else if (__any_sync(0xffffffffu, now.next < from + 32)) {
+            if (now.next < from + 32) {
+              A.picked[row] = pick32(v, now.next - from) * A.scale;
+              now.next = kNoTarget;
+            }
+            __syncwarp();
           }
-          __syncwarp();
         };
         uint32_t v0[32], v1[32];
         load(0, v0);
@@ -435,19 +431,29 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           const Two to = two(to2, to2), less = two(-t.lse2, -t.lse2), by = two(main, main);
           float z[32];
 #pragma unroll
-          for (int j = 0; j < 32; j += 2) {
-            const float2 x = both(fma(two(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), to, less));
-            const float2 d = both(two(exp2_fast(x.x), exp2_fast(x.y)) * by);
-            z[j] = d.x, z[j + 1] = d.y;
-          }
-          while (__any_sync(0xffffffffu, now.next < end)) {
-            if (now.next < end) {
-              if (SOFT) {
-                add32(z, now.next - from, -t.a * __int_as_float(now.value));
-              } else {  // (1 + e)·p - 1 with p near 1: by p - 1
-                set32(z, now.next - from, t.a * fmaf(1.f + t.e, expm1f(fmaf(hard, to2, -t.lse2) * kLn2), t.e));
+          for (int g = 0; g < 32; g += 8) {
+#pragma unroll
+            for (int j = g; j < g + 8; j += 2) {
+              const float2 x = both(fma(two(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), to, less));
+              const float2 d = both(two(exp2_fast(x.x), exp2_fast(x.y)) * by);
+              z[j] = d.x, z[j + 1] = d.y;
+            }
+            if (SOFT) {
+              while (column < from + g + 8) {
+                const int at = column - (from + g), who = __shfl_sync(0xffffffffu, entry.y, taken);
+                const float weight = __int_as_float(__shfl_sync(0xffffffffu, entry.z, taken));
+                const float less = lane == (who & 31) ? -t.a * weight : 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                  if (j == at) z[g + j] += less;
+                advance();
               }
-              advance();
+            }
+          }
+          if (!SOFT && __any_sync(0xffffffffu, now.next < end)) {
+            if (now.next < end) {  // (1 + e)·p - 1 with p near 1: by p - 1
+              set32(z, now.next - from, t.a * fmaf(1.f + t.e, expm1f(fmaf(hard, to2, -t.lse2) * kLn2), t.e));
+              now.next = kNoTarget;
             }
           }
           __syncwarp();
@@ -492,10 +498,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 }
 
 // ---------------------------------------------------------------------------
-// A token's listed rows, sorted (by place among equal ones), and with `rows` their weights
-// and its terms of the gradient: one warp to a token.
+// The listed rows of 32 tokens, sorted by row of w (then token, then place), and where the
+// entries of each group of 64 rows of w begin: an epilogue warp then has its own together.
+// (Each token's entries on their own, found by search in every tile, 32 lanes reading 32
+// lists, took more than the products: 350 us for 4096 tokens × 50257×1024 with 64 entries, 250
+// without any.)  With `rows` the entries' weights and the tokens' terms of the gradient.
 // ---------------------------------------------------------------------------
-constexpr int kTargetWarps = 4;
+constexpr int kListThreads = 1024;
 
 __device__ __forceinline__ float teacher_at(const HeadTargets& t, int64_t row, int i) {
   const int64_t at = row * t.ld_teacher + i;
@@ -516,63 +525,134 @@ __device__ __forceinline__ void teacher_sums(const HeadTargets& t, int64_t row, 
   *sum = warp_add(s);
 }
 
-__global__ void __launch_bounds__(32 * kTargetWarps)
-    head_targets_kernel(int64_t m, int64_t n, HeadTargets t, int padded, int2* sorted, HeadRow* rows, HeadTerms terms) {
-  extern __shared__ unsigned long long keys_s[];
+// Steps of 32 and less of a bitonic merge of `size`, 64 keys to a warp in registers (a lane
+// has two of them next to each other); with `first`, of all sizes up to 64.
+template <typename Key>
+__device__ __forceinline__ void sort_64(Key* keys, int at, int size, bool first, int lane) {
+  Key a = keys[at + 2 * lane], b = keys[at + 2 * lane + 1];
+  for (int n = first ? 2 : size; n <= size; n <<= 1) {
+    const bool up = ((at + 2 * lane) & n) == 0;
+    for (int step = min(n >> 1, 32); step > 1; step >>= 1) {
+      const int other = step >> 1;  // lanes away
+      const bool low = (lane & other) == 0;
+      const Key c = __shfl_xor_sync(0xffffffffu, a, other), d = __shfl_xor_sync(0xffffffffu, b, other);
+      a = (a > c) == (low == up) ? c : a;
+      b = (b > d) == (low == up) ? d : b;
+    }
+    if ((a > b) == up) {
+      const Key c = a;
+      a = b, b = c;
+    }
+  }
+  keys[at + 2 * lane] = a, keys[at + 2 * lane + 1] = b;
+}
+
+// A key is the row of w and, in its low `bits` bits, the entry's number: 32 bits of them where
+// that is enough (its shuffles and comparisons are half).
+template <typename Key>
+__global__ void __launch_bounds__(kListThreads)
+    head_targets_kernel(int64_t m, int64_t n, HeadTargets t, int padded, int bits, int64_t groups1, int4* entries, int* offsets,
+                        HeadRow* rows, HeadTerms terms) {
+  extern __shared__ unsigned long long list_smem[];  // keys, then the teacher's logits
+  Key* keys = reinterpret_cast<Key*>(list_smem);
+  constexpr Key kNone = ~Key(0), kBad = kNone - 1;   // not there; no row of w
+  __shared__ float top_s[32], sum_s[32];
   pdl_trigger();
   pdl_wait();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * kTargetWarps + warp;
-  if (row >= m) return;
-  bool live = false, bad = false;
-  float top = 0.f, sum = 1.f;
-  unsigned long long* keys = keys_s + warp * padded;
-  for (int i = lane; i < padded; i += 32) {
-    int64_t id = i < t.top ? t.ids[row * t.ld + i] : -1;
-    live = live || id >= 0;
-    bad = bad || id >= n;
-    if (id < 0 || id >= n) id = kNoTarget;
-    keys[i] = static_cast<unsigned long long>(id) << 32 | static_cast<uint32_t>(i);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, top = t.top;
+  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * 32, mine = row0 + warp;
+  float* logits = reinterpret_cast<float*>(keys + padded);
+  float g = 0.f, l = 0.f;
+  if (rows && mine < m && lane == 0) g = terms.dloss[terms.dloss_each ? mine : 0], l = terms.lse[mine];
+  const int count = static_cast<int>(min(int64_t(32), m - row0)) * top;
+  for (int i = threadIdx.x; i < padded; i += kListThreads) {
+    const int r = i / top, place = i - r * top;
+    int64_t id = -1;
+    if (i < count) {
+      id = t.ids[(row0 + r) * t.ld + place];
+      if (rows) logits[i] = teacher_at(t, row0 + r, place);
+    }
+    keys[i] = id < 0 ? kNone : id >= n ? kBad : static_cast<Key>(id) << bits | static_cast<Key>(i);
   }
-  live = __any_sync(0xffffffffu, live);
-  bad = __any_sync(0xffffffffu, bad);
-  if (rows) teacher_sums(t, row, lane, &top, &sum);
-  __syncwarp();
-  for (int size = 2; size <= padded; size <<= 1)
-    for (int step = size >> 1; step; step >>= 1) {
-      for (int p = lane; p < padded / 2; p += 32) {
+  __syncthreads();
+  if (rows && mine < m) {
+    bool live = false, bad = false;
+    float most = kLowest, sum = 0.f;
+    for (int i = warp * top + lane; i < (warp + 1) * top; i += 32) {
+      if (keys[i] == kNone) continue;
+      live = true;
+      bad = bad || keys[i] == kBad;
+      most = fmaxf(most, logits[i]);
+    }
+    live = __any_sync(0xffffffffu, live);
+    bad = __any_sync(0xffffffffu, bad);
+    most = warp_max(most);
+    for (int i = warp * top + lane; i < (warp + 1) * top; i += 32)
+      if (keys[i] != kNone) sum += expf(logits[i] - most);
+    sum = warp_add(sum);
+    if (lane == 0) {
+      top_s[warp] = most, sum_s[warp] = sum;
+      rows[mine] = HeadRow{bad ? __int_as_float(0x7FC00000) : live ? g * terms.scale : 0.f, live ? l * kLog2E : 0.f, 0.f, live};
+    }
+  }
+  __syncthreads();
+  for (int at = warp * 64; at < padded; at += 2 * kListThreads) sort_64(keys, at, 64, true, lane);
+  __syncthreads();
+  for (int size = 128; size <= padded; size <<= 1) {
+    for (int step = size >> 1; step >= 64; step >>= 1) {
+      for (int p = threadIdx.x; p < padded / 2; p += kListThreads) {
         const int i = 2 * p - (p & (step - 1)), j = i + step;
-        const unsigned long long a = keys[i], b = keys[j];
+        const Key a = keys[i], b = keys[j];
         if ((a > b) == ((i & size) == 0)) keys[i] = b, keys[j] = a;
       }
-      __syncwarp();
+      __syncthreads();
     }
-  for (int i = lane; i < t.top; i += 32) {
-    const int id = static_cast<int>(keys[i] >> 32), place = static_cast<int>(keys[i] & 0xFFFFFFFFu);
-    int value = place;
-    if (rows && id != kNoTarget) value = __float_as_int(expf(teacher_at(t, row, place) - top) / sum);
-    sorted[row * t.top + i] = make_int2(id, value);
+    for (int at = warp * 64; at < padded; at += 2 * kListThreads) sort_64(keys, at, size, false, lane);
+    __syncthreads();
   }
-  if (rows && lane == 0) {
-    const float g = live ? terms.dloss[terms.dloss_each ? row : 0] * terms.scale : 0.f;
-    rows[row] = HeadRow{bad ? __int_as_float(0x7FC00000) : g, live ? terms.lse[row] * kLog2E : 0.f, 0.f, live};
+  const int64_t base = row0 * top;
+  for (int i = threadIdx.x; i < count; i += kListThreads) {
+    const Key key = keys[i];
+    int4 e = make_int4(kNoTarget, 0, 0, 0);
+    if (key < kBad) {
+      const int index = static_cast<int>(key & ((Key(1) << bits) - 1)), r = index / top;
+      e.x = static_cast<int>(key >> bits);
+      e.y = (index - r * top) << 5 | r;
+      if (rows) e.z = __float_as_int(expf(logits[index] - top_s[r]) / sum_s[r]);
+    }
+    entries[base + i] = e;
+  }
+  for (int64_t q = threadIdx.x; q < groups1; q += kListThreads) {
+    const Key first = q + 1 < groups1 ? static_cast<Key>(q * kHeadGroup) << bits : kBad;
+    int at = 0, left = count;  // the first one of these columns
+    while (left > 0) {
+      const int half = left >> 1;
+      if (keys[at + half] < first) {
+        at += half + 1;
+        left -= half + 1;
+      } else {
+        left = half;
+      }
+    }
+    offsets[blockIdx.x * groups1 + q] = static_cast<int>(base) + at;
   }
 }
 
 // ---------------------------------------------------------------------------
 // lse and losses.  A block has 32 tokens, one a lane; its warps take the groups of
-// columns in turn, and their maxima and sums are joined in shared memory.
+// columns in turn, eight loads at once, and their maxima and sums are joined in shared
+// memory.  (One by one, the 2048 groups of a large vocabulary took 13 us.)
 // ---------------------------------------------------------------------------
-constexpr int kJoinWarps = 32;
+constexpr int kJoinWarps = 32, kJoinAhead = 8;
 
 __global__ void __launch_bounds__(32 * kJoinWarps)
     head_join_kernel(int64_t m, int64_t n, HeadTargets t, const float2* __restrict__ stats, int64_t ld_stats, int groups,
-                     float z_loss, float* __restrict__ loss, float* __restrict__ lse, float* picked) {
+                     int join_warps, float z_loss, float* __restrict__ loss, float* __restrict__ lse, float* picked) {
   __shared__ float2 parts[kJoinWarps][32];
   __shared__ float lse_s[32];
   pdl_trigger();
   pdl_wait();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
   const int64_t row0 = static_cast<int64_t>(blockIdx.x) * 32, row = row0 + lane;
   float most = kLowest, sum = 0.f;
   auto join = [&](float2 p) {
@@ -580,14 +660,25 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
     sum = sum * exp2_fast(most - top) + p.y * exp2_fast(p.x - top);
     most = top;
   };
-  if (row < m) {
-#pragma unroll 4
-    for (int g = warp; g < groups; g += kJoinWarps) join(stats[g * ld_stats + row]);
+  if (row < m && warp < join_warps) {
+    for (int g = warp; g < groups; g += kJoinAhead * join_warps) {
+      float2 p[kJoinAhead];
+#pragma unroll
+      for (int i = 0; i < kJoinAhead; ++i)
+        p[i] = g + i * join_warps < groups ? stats[(g + i * join_warps) * ld_stats + row] : make_float2(kLowest, 0.f);
+      float2 all = p[0];
+#pragma unroll
+      for (int i = 1; i < kJoinAhead; ++i) all.x = fmaxf(all.x, p[i].x);
+      all.y = 0.f;
+#pragma unroll
+      for (int i = 0; i < kJoinAhead; ++i) all.y = fmaf(p[i].y, exp2_fast(p[i].x - all.x), all.y);
+      join(all);
+    }
   }
   parts[warp][lane] = make_float2(most, sum);
   __syncthreads();
   if (warp == 0) {
-    for (int w = 1; w < kJoinWarps; ++w) join(parts[w][lane]);
+    for (int w = 1; w < join_warps; ++w) join(parts[w][lane]);
     const float l = most == INFINITY ? INFINITY : kLn2 * most + logf(sum);
     lse_s[lane] = l;
     if (row < m) {
@@ -606,31 +697,31 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
   }
   if (!t.soft) return;
   __syncthreads();
-  const int64_t mine = row0 + warp;
-  if (mine >= m) return;
-  float top, all;
-  teacher_sums(t, mine, lane, &top, &all);
-  const float log_all = logf(all);
-  float s = 0.f;
-  bool live = false;
-  for (int i = lane; i < t.top; i += 32) {
-    const int64_t id = t.ids[mine * t.ld + i];
-    float* p = picked + mine * t.top + i;
-    float z = 0.f;
-    if (id >= 0 && id < n) {
-      z = *p;
-    } else {
-      *p = z = id >= n ? __int_as_float(0x7FC00000) : 0.f;
+  for (int64_t mine = row0 + warp; mine < min(m, row0 + 32); mine += warps) {
+    float top, all;
+    teacher_sums(t, mine, lane, &top, &all);
+    const float log_all = logf(all);
+    float s = 0.f;
+    bool live = false;
+    for (int i = lane; i < t.top; i += 32) {
+      const int64_t id = t.ids[mine * t.ld + i];
+      float* p = picked + mine * t.top + i;
+      float z = 0.f;
+      if (id >= 0 && id < n) {
+        z = *p;
+      } else {
+        *p = z = id >= n ? __int_as_float(0x7FC00000) : 0.f;
+      }
+      if (id >= 0) {
+        live = true;
+        const float log_q = teacher_at(t, mine, i) - top - log_all, weight = expf(log_q);
+        if (weight != 0.f) s = fmaf(weight, log_q - z, s);  // (a row that the teacher rules out weighs nothing)
+      }
     }
-    if (id >= 0) {
-      live = true;
-      const float log_q = teacher_at(t, mine, i) - top - log_all, weight = expf(log_q);
-      if (weight != 0.f) s = fmaf(weight, log_q - z, s);  // (a row that the teacher rules out weighs nothing)
-    }
+    s = warp_add(s);
+    live = __any_sync(0xffffffffu, live);
+    if (lane == 0) loss[mine] = live ? s + lse_s[mine - row0] : 0.f;
   }
-  s = warp_add(s);
-  live = __any_sync(0xffffffffu, live);
-  if (lane == 0) loss[mine] = live ? s + lse_s[warp] : 0.f;
 }
 
 // ---------------------------------------------------------------------------
@@ -640,21 +731,36 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
 __global__ void __launch_bounds__(256) live_rows_kernel(int64_t m, int64_t n, int64_t k, const uint16_t* __restrict__ x,
                                                         int64_t ldx, Ids ids, HeadTerms terms, float* __restrict__ largest,
                                                         uint16_t* __restrict__ dst, int64_t ld_dst) {
+  __shared__ float most_s[8];
   pdl_trigger();
   pdl_wait();
-  const int per = static_cast<int>((k + 7) / 8);
+  // 16-byte pieces, one grid's stride apart.
+  const uint32_t per = static_cast<uint32_t>((k + 7) / 8);
+  const uint32_t first = blockIdx.x * blockDim.x + threadIdx.x, stride = gridDim.x * blockDim.x;
+  const uint32_t stride_rows = stride / per, stride_pieces = stride - stride_rows * per;
   const uint16_t* end = x + (m - 1) * ldx + k;
   float most = 0.f;
-  for (int64_t r = blockIdx.x; r < m; r += gridDim.x) {
-    const HeadRow row = head_row(terms, ids, n, r);
-    most = fmaxf(most, head_size(row));
-    for (int c = threadIdx.x; c < per; c += 256) {
-      const uint16_t* p = x + r * ldx + 8 * c;
-      *reinterpret_cast<uint4*>(dst + r * ld_dst + 8 * c) =
-          row.live ? load16_any(p, x, end, static_cast<int>(min(int64_t(8), k - 8 * c))) : make_uint4(0, 0, 0, 0);
-    }
+  int64_t r = first / per;
+  uint32_t c = first - static_cast<uint32_t>(r) * per;
+  while (r < m) {
+    const bool live = terms.rows ? __ldg(&terms.rows[r].live) != 0 : ids[r] >= 0;
+    if (largest && c == 0) most = fmaxf(most, head_size(head_row(terms, ids, n, r)));
+    const uint16_t* p = x + r * ldx + 8 * c;
+    *reinterpret_cast<uint4*>(dst + r * ld_dst + 8 * c) =
+        live ? load16_any(p, x, end, static_cast<int>(min(int64_t(8), k - 8 * c))) : make_uint4(0, 0, 0, 0);
+    r += stride_rows;
+    c += stride_pieces;
+    if (c >= per) c -= per, ++r;
   }
-  if (largest && threadIdx.x == 0) largest[blockIdx.x] = most;
+  if (!largest) return;
+  most = warp_max(most);
+  if ((threadIdx.x & 31) == 0) most_s[threadIdx.x >> 5] = most;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+#pragma unroll
+    for (int w = 1; w < 8; ++w) most = fmaxf(most, most_s[w]);
+    largest[blockIdx.x] = most;
+  }
 }
 
 // FP32 sums to the rows' type.
@@ -721,21 +827,34 @@ int padded_top(int top) {
 
 }  // namespace
 
-cudaError_t launch_head_targets(int64_t m, int64_t n, const HeadTargets& t, int2* sorted, HeadRow* rows,
-                                const HeadTerms& terms, cudaStream_t st) {
-  const int padded = padded_top(t.top);
-  count_launch();
-  return launch_dependent(head_targets_kernel, dim3(static_cast<unsigned>((m + kTargetWarps - 1) / kTargetWarps)),
-                          dim3(32 * kTargetWarps), sizeof(unsigned long long) * padded * kTargetWarps, st, m, n, t, padded,
-                          sorted, rows, terms);
+HeadLists head_lists(int64_t m, int64_t n, int top) {
+  return HeadLists{m * top, (n + kHeadGroup - 1) / kHeadGroup + 1, (m + 31) / 32};
 }
 
-int live_rows_maxima(int64_t m) { return static_cast<int>(std::min<int64_t>(m, 8 * num_sms())); }
+cudaError_t launch_head_targets(int64_t m, int64_t n, const HeadTargets& t, int4* entries, int* offsets, HeadRow* rows,
+                                const HeadTerms& terms, cudaStream_t st) {
+  const HeadLists l = head_lists(m, n, t.top);
+  const int padded = std::max(64, padded_top(32 * t.top));
+  int bits = 0;
+  while (padded >> bits > 1) ++bits;
+  const bool narrow = n < (int64_t(1) << (32 - bits)) - 1;
+  const size_t smem = (narrow ? 4 : 8) * padded + (rows ? sizeof(float) * 32 * t.top : 0);
+  auto kern = narrow ? head_targets_kernel<uint32_t> : head_targets_kernel<unsigned long long>;
+  const cudaError_t err = allow_smem(reinterpret_cast<const void*>(kern), smem);
+  if (err != cudaSuccess) return err;
+  count_launch();
+  return launch_dependent(kern, dim3(static_cast<unsigned>(l.blocks)), dim3(kListThreads), smem, st, m, n, t, padded, bits, l.groups1,
+                          entries, offsets, rows, terms);
+}
+
+int live_rows_maxima(int64_t m, int64_t k) {
+  return static_cast<int>(std::min<int64_t>((m * ((k + 7) / 8) + 255) / 256, 8 * static_cast<int64_t>(num_sms())));
+}
 
 cudaError_t launch_live_rows(int64_t m, int64_t n, int64_t k, const void* x, int64_t ldx, Ids ids, const HeadTerms& terms,
                              float* largest, void* dst, int64_t ld_dst, cudaStream_t st) {
   count_launch();
-  return launch_dependent(live_rows_kernel, dim3(static_cast<unsigned>(live_rows_maxima(m))), dim3(256), 0, st, m, n, k,
+  return launch_dependent(live_rows_kernel, dim3(static_cast<unsigned>(live_rows_maxima(m, k))), dim3(256), 0, st, m, n, k,
                           static_cast<const uint16_t*>(x), ldx, ids, terms, largest, static_cast<uint16_t*>(dst), ld_dst);
 }
 
@@ -753,9 +872,13 @@ cudaError_t launch_head_grad(const HeadArgs& a, int type, Oz2Device* dev, cudaSt
 
 cudaError_t launch_head_join(int64_t m, int64_t n, const HeadTargets& t, const float2* stats, int64_t ld_stats,
                              float z_loss, float* loss, float* lse, float* picked, cudaStream_t st) {
+  // As many warps as have eight groups each; listed rows, which are a warp's each, want all.
+  const int groups = static_cast<int>((n + kHeadGroup - 1) / kHeadGroup);
+  const int join_warps = std::min(kJoinWarps, (groups + kJoinAhead - 1) / kJoinAhead);
+  const int warps = t.soft ? kJoinWarps : join_warps;
   count_launch();
-  return launch_dependent(head_join_kernel, dim3(static_cast<unsigned>((m + 31) / 32)), dim3(32 * kJoinWarps), 0, st, m, n, t,
-                          stats, ld_stats, static_cast<int>((n + kHeadGroup - 1) / kHeadGroup), z_loss, loss, lse, picked);
+  return launch_dependent(head_join_kernel, dim3(static_cast<unsigned>((m + 31) / 32)), dim3(32 * warps), 0, st, m, n, t,
+                          stats, ld_stats, groups, join_warps, z_loss, loss, lse, picked);
 }
 
 cudaError_t launch_round_rows(int64_t m, int64_t k, int type, const float* src, int64_t ld_src, const float* unscale,

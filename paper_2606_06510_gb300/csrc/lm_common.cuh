@@ -155,8 +155,8 @@ cudaError_t launch_layer_norm_grad(const NormGradArgs& a, int type, void* scratc
 // --- losses over a vocabulary (k_head.cu) ------------------------------------------------
 // The logits z = scale·x·wᵀ are formed tile by tile and used where they are.  What a
 // token wants of them besides their sum of exponentials: its target, or its `top` listed
-// rows of w with a value each, as sorted pairs (row, value).  The value is the entry's
-// place in `picked` (forward) or its weight as FP32 bits (gradient).
+// rows of w with a weight each.  Those are sorted for every 32 tokens: entries (row of w,
+// place << 5 | token of the 32, weight's bits, -).
 constexpr int kNoTarget = 0x7FFFFFFF;
 struct HeadTargets {
   Ids ids;
@@ -190,7 +190,9 @@ struct HeadArgs {
   int64_t c0, cols;    // the piece of the vocabulary
   float scale;
   Ids ids;             // targets, one a token
-  const int2* targets; // or sorted entries (m, top)
+  const int4* entries; // or entries of every 32 tokens,
+  const int* offsets;  // and where those of a group of 64 rows of w begin: groups1 for every 32 tokens
+  int64_t groups1;
   int top, soft;
   // forward
   float2* stats;       // (groups of 64 columns, ld_stats): max and sum of exp2 of z·log2 e
@@ -205,13 +207,18 @@ struct HeadArgs {
   int64_t ld_dz;
 };
 constexpr int kHeadGroup = 64;
-constexpr int kMaxTop = 1024;
-// A token's entries sorted; with `rows`, their weights and the rows' terms too.
-cudaError_t launch_head_targets(int64_t m, int64_t n, const HeadTargets& t, int2* sorted, HeadRow* rows,
+constexpr int kMaxTop = 512;  // (32 tokens' entries are sorted in shared memory)
+// The entries of m tokens (so many, offsets `groups1` for each of the `blocks` of 32); with
+// `rows`, their weights and the rows' terms too.
+struct HeadLists {
+  int64_t entries, groups1, blocks;
+};
+HeadLists head_lists(int64_t m, int64_t n, int top);
+cudaError_t launch_head_targets(int64_t m, int64_t n, const HeadTargets& t, int4* entries, int* offsets, HeadRow* rows,
                                 const HeadTerms& terms, cudaStream_t st);
 // x's rows of live tokens to rows of ld_dst elements on 16-byte boundaries, zeros for the others; and
-// with `largest` the maxima for HeadArgs, as many as live_rows_maxima(m).
-int live_rows_maxima(int64_t m);
+// with `largest` the maxima for HeadArgs, as many as live_rows_maxima(m, k).
+int live_rows_maxima(int64_t m, int64_t k);
 cudaError_t launch_live_rows(int64_t m, int64_t n, int64_t k, const void* x, int64_t ldx, Ids ids, const HeadTerms& terms,
                              float* largest, void* dst, int64_t ld_dst, cudaStream_t st);
 cudaError_t launch_head_forward(const HeadArgs& a, int type, Oz2Device* dev, cudaStream_t st);

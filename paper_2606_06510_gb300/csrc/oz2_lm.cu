@@ -40,7 +40,7 @@ int check_head(const HeadCall& c, int id_bits) {
   if (c.t.soft && (c.t.top < 1 || c.t.top > kMaxTop || c.t.ld < c.t.top || c.t.ld_teacher < c.t.top ||
                    !valid_type(c.t.teacher_type) || !(c.t.temperature > 0)))
     return OZ2_ERR_INVALID_ARG;
-  if (too_large(c.m, c.n, c.k)) return OZ2_ERR_UNSUPPORTED;
+  if (too_large(c.m, c.n, c.k) || (c.t.soft && c.m * c.t.top > 0x7FFFFFFF)) return OZ2_ERR_UNSUPPORTED;
   return OZ2_OK;
 }
 bool head_pointers(const HeadCall& c, int id_bits) {
@@ -71,17 +71,20 @@ int head_forward(const HeadCall& c, float* loss, float* lse, float* picked, cuda
   Operand X(c.X, c.ldx, c.k ? c.m : 0, c.k, 2, ws, copies.x), W(c.W, c.ldw, c.k ? c.n : 0, c.k, 2, ws, copies.w);
   const int64_t ld_stats = (c.m + 31) / 32 * 32, groups = (c.n + kHeadGroup - 1) / kHeadGroup;
   const size_t stats = ws.ask(sizeof(float2) * ld_stats * groups);
-  const size_t sorted = c.t.soft ? ws.ask(sizeof(int2) * c.m * c.t.top) : 0;
+  const HeadLists lists = head_lists(c.m, c.n, c.t.top);
+  const size_t entries = c.t.soft ? ws.ask(sizeof(int4) * lists.entries) : 0;
+  const size_t offsets = c.t.soft ? ws.ask(sizeof(int) * lists.groups1 * lists.blocks) : 0;
   if (!ws.take()) return OZ2_ERR_ALLOC;
   cudaError_t err = place(X, W, ws, st);
-  if (err == cudaSuccess && c.t.soft) err = launch_head_targets(c.m, c.n, c.t, ws.at<int2>(sorted), nullptr, HeadTerms{}, st);
+  if (err == cudaSuccess && c.t.soft)
+    err = launch_head_targets(c.m, c.n, c.t, ws.at<int4>(entries), ws.at<int>(offsets), nullptr, HeadTerms{}, st);
   HeadArgs a{};
   a.m = c.m, a.n = c.n, a.k = c.k;
   a.x = X.p, a.ldx = X.ld, a.w = W.p, a.ldw = W.ld;
   a.cols = c.n;
   a.scale = c.scale;
   a.ids = c.t.ids;
-  a.targets = ws.at<int2>(sorted);
+  a.entries = ws.at<int4>(entries), a.offsets = ws.at<int>(offsets), a.groups1 = lists.groups1;
   a.top = c.t.top, a.soft = c.t.soft;
   a.stats = ws.at<float2>(stats), a.ld_stats = ld_stats;
   a.picked = picked;
@@ -128,8 +131,10 @@ int head_grad(const HeadCall& c, const HeadGrads& g, int id_bits, cudaStream_t s
   } kinds[2];
   const int64_t ld_dz = (piece + 63) / 64 * 64, ld_sum = (c.k + 31) / 32 * 32;
   Workspace ws(st);
-  const size_t rows = c.t.soft ? ws.ask(sizeof(HeadRow) * c.m) : 0, sorted = c.t.soft ? ws.ask(sizeof(int2) * c.m * c.t.top) : 0;
-  const size_t maxima = scaled ? ws.ask(sizeof(float) * (live_rows_maxima(c.m) + 1)) : 0;
+  const HeadLists lists = head_lists(c.m, c.n, c.t.top);
+  const size_t rows = c.t.soft ? ws.ask(sizeof(HeadRow) * c.m) : 0, entries = c.t.soft ? ws.ask(sizeof(int4) * lists.entries) : 0;
+  const size_t offsets = c.t.soft ? ws.ask(sizeof(int) * lists.groups1 * lists.blocks) : 0;
+  const size_t maxima = scaled ? ws.ask(sizeof(float) * (live_rows_maxima(c.m, c.k) + 1)) : 0;
   // (x's copy is where the largest of the terms is found, and dead tokens' x made zeros for dw.)
   const HeadCopies copies = head_copies(c, want_dx ? 2 : 1, want_dw || scaled);
   Operand X(c.X, c.ldx, c.m, c.k, 2, ws, want_dw || scaled || copies.x), W(c.W, c.ldw, c.n, c.k, 2, ws, copies.w);
@@ -165,7 +170,7 @@ int head_grad(const HeadCall& c, const HeadGrads& g, int id_bits, cudaStream_t s
   HeadTerms terms{nullptr, g.dloss, g.lse, (g.flags & OZ2_GRAD_ONE_DLOSS) == 0, c.scale, c.z_loss};
   cudaError_t err = cudaSuccess;
   if (c.t.soft) {
-    err = launch_head_targets(c.m, c.n, c.t, ws.at<int2>(sorted), ws.at<HeadRow>(rows), terms, st);
+    err = launch_head_targets(c.m, c.n, c.t, ws.at<int4>(entries), ws.at<int>(offsets), ws.at<HeadRow>(rows), terms, st);
     terms.rows = ws.at<HeadRow>(rows);
   }
   if (err == cudaSuccess && X.copy) {
@@ -186,10 +191,10 @@ int head_grad(const HeadCall& c, const HeadGrads& g, int id_bits, cudaStream_t s
     a.c0 = c0, a.cols = cols;
     a.scale = c.scale;
     a.ids = c.t.ids;
-    a.targets = ws.at<int2>(sorted);
+    a.entries = ws.at<int4>(entries), a.offsets = ws.at<int>(offsets), a.groups1 = lists.groups1;
     a.top = c.t.top, a.soft = c.t.soft;
     a.terms = terms;
-    a.largest = largest, a.maxima = live_rows_maxima(c.m), a.unscale = unscale;
+    a.largest = largest, a.maxima = live_rows_maxima(c.m, c.k), a.unscale = unscale;
     a.dz = ws.at<uint16_t>(dz), a.ld_dz = ld_dz;
     err = launch_head_grad(a, c.type, dev, st);
     int at = 0;
