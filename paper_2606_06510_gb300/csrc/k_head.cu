@@ -364,36 +364,57 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         more = find(i, then);
         continue;
       }
-      // Listed rows: the warp walks its entries in the order of their columns, each of which is
-      // one lane's.
-      int taken = 0, column = kNoTarget;  // of the 32 at hand; of the next one, in the piece
-      auto look = [&] {
-        column = __shfl_sync(0xffffffffu, entry.x, taken);
-        if (column != kNoTarget) column -= static_cast<int>(A.c0);
-      };
-      auto advance = [&] {
-        if (++taken == 32) {
-          taken = 0;
-          now.at += 32;
-          entry = entry_at(now.at + lane, now.end);
+      // Listed rows: each lane walks its own of the warp's entries, which are sorted by token and
+      // column: by shuffles where there are at most 32 of them, else where they lie.
+      int index = 0, column = kNoTarget, value = 0;  // of the lane's next one: its column in the piece, and what it has
+      const int many = SOFT ? now.end - now.at : 0;
+      auto take = [&] {
+        int4 e = make_int4(kNoTarget, 0, 0, 0);
+        if (many <= 32) {
+          e.x = __shfl_sync(0xffffffffu, entry.x, index & 31);
+          e.y = __shfl_sync(0xffffffffu, entry.y, index & 31);
+          if (GRAD) e.z = __shfl_sync(0xffffffffu, entry.z, index & 31);
+        } else if (index < many) {
+          e = __ldg(A.entries + now.at + index);
         }
-        look();
+        column = index < many && (e.y & 31) == lane ? e.x - static_cast<int>(A.c0) : kNoTarget;
+        value = GRAD ? e.z : e.y >> 5;
       };
-      if (SOFT) {
-        look();
+      if (SOFT && many > 0) {  // the first entry whose token is not before this lane's
+        if (many <= 32) {
+          const int token = lane < many ? entry.y & 31 : 32;
+#pragma unroll
+          for (int s = 16; s; s >>= 1)
+            if (__shfl_sync(0xffffffffu, token, index + s - 1) < lane) index += s;
+          if (__shfl_sync(0xffffffffu, token, index) < lane) ++index;
+        } else {
+          for (int left = many; left > 0;) {
+            const int half = left >> 1;
+            if ((__ldg(&A.entries[now.at + index + half].y) & 31) < lane) {
+              index += half + 1;
+              left -= half + 1;
+            } else {
+              left = half;
+            }
+          }
+          __syncwarp();
+        }
+        take();
       }
       if (!GRAD) {
         auto pick = [&](const uint32_t (&v)[32], int from) {
           if (SOFT) {
 #pragma unroll
             for (int g = 0; g < 32; g += 8) {
-              while (column < from + g + 8) {
-                const int at = column - (from + g), who = __shfl_sync(0xffffffffu, entry.y, taken);
+              while (__any_sync(0xffffffffu, column < from + g + 8)) {
+                const bool here = column < from + g + 8;
+                const int at = column - (from + g);
                 uint32_t e = v[g];
 #pragma unroll
                 for (int j = 1; j < 8; ++j) e = j == at ? v[g + j] : e;
-                if (lane == (who & 31)) A.picked[static_cast<int64_t>(row) * A.top + (who >> 5)] = __uint_as_float(e) * A.scale;
-                advance();
+                if (here) A.picked[static_cast<int64_t>(row) * A.top + value] = __uint_as_float(e) * A.scale;
+                index += here;
+                take();
               }
             }
           } else if (__any_sync(0xffffffffu, now.next < from + 32)) {
@@ -439,14 +460,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
               z[j] = d.x, z[j + 1] = d.y;
             }
             if (SOFT) {
-              while (column < from + g + 8) {
-                const int at = column - (from + g), who = __shfl_sync(0xffffffffu, entry.y, taken);
-                const float weight = __int_as_float(__shfl_sync(0xffffffffu, entry.z, taken));
-                const float less = lane == (who & 31) ? -t.a * weight : 0.f;
+              while (__any_sync(0xffffffffu, column < from + g + 8)) {
+                const bool here = column < from + g + 8;
+                const int at = column - (from + g);
+                const float weight = -t.a * __int_as_float(value);
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                  if (j == at) z[g + j] += less;
-                advance();
+                  if (j == at) z[g + j] += weight;  // (past these columns: no j)
+                index += here;
+                take();
               }
             }
           }
@@ -498,8 +520,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 }
 
 // ---------------------------------------------------------------------------
-// The listed rows of 32 tokens, sorted by row of w (then token, then place), and where the
-// entries of each group of 64 rows of w begin: an epilogue warp then has its own together.
+// The listed rows of 32 tokens, sorted by group of 64 rows of w, token, row of w and place, and
+// where the entries of each group begin: an epilogue warp then has its own together.
 // (Each token's entries on their own, found by search in every tile, 32 lanes reading 32
 // lists, took more than the products: 350 us for 4096 tokens × 50257×1024 with 64 entries, 250
 // without any.)  With `rows` the entries' weights and the tokens' terms of the gradient.
@@ -547,8 +569,8 @@ __device__ __forceinline__ void sort_64(Key* keys, int at, int size, bool first,
   keys[at + 2 * lane] = a, keys[at + 2 * lane + 1] = b;
 }
 
-// A key is the row of w and, in its low `bits` bits, the entry's number: 32 bits of them where
-// that is enough (its shuffles and comparisons are half).
+// A key is the group, the token of the 32 (5 bits), the row of w in the group (6) and the place
+// (`bits`): 32 bits of them where that is enough (its shuffles and comparisons are half).
 template <typename Key>
 __global__ void __launch_bounds__(kListThreads)
     head_targets_kernel(int64_t m, int64_t n, HeadTargets t, int padded, int bits, int64_t groups1, int4* entries, int* offsets,
@@ -572,7 +594,7 @@ __global__ void __launch_bounds__(kListThreads)
       id = t.ids[(row0 + r) * t.ld + place];
       if (rows) logits[i] = teacher_at(t, row0 + r, place);
     }
-    keys[i] = id < 0 ? kNone : id >= n ? kBad : static_cast<Key>(id) << bits | static_cast<Key>(i);
+    keys[i] = id < 0 ? kNone : id >= n ? kBad : ((static_cast<Key>(id >> 6) << 11 | static_cast<Key>(r << 6 | (id & 63))) << bits) | static_cast<Key>(place);
   }
   __syncthreads();
   if (rows && mine < m) {
@@ -615,15 +637,15 @@ __global__ void __launch_bounds__(kListThreads)
     const Key key = keys[i];
     int4 e = make_int4(kNoTarget, 0, 0, 0);
     if (key < kBad) {
-      const int index = static_cast<int>(key & ((Key(1) << bits) - 1)), r = index / top;
-      e.x = static_cast<int>(key >> bits);
-      e.y = (index - r * top) << 5 | r;
-      if (rows) e.z = __float_as_int(expf(logits[index] - top_s[r]) / sum_s[r]);
+      const int place = static_cast<int>(key & ((Key(1) << bits) - 1)), r = static_cast<int>(key >> (bits + 6) & 31);
+      e.x = static_cast<int>(key >> (bits + 11)) << 6 | static_cast<int>(key >> bits & 63);
+      e.y = place << 5 | r;
+      if (rows) e.z = __float_as_int(expf(logits[r * top + place] - top_s[r]) / sum_s[r]);
     }
     entries[base + i] = e;
   }
   for (int64_t q = threadIdx.x; q < groups1; q += kListThreads) {
-    const Key first = q + 1 < groups1 ? static_cast<Key>(q * kHeadGroup) << bits : kBad;
+    const Key first = q + 1 < groups1 ? static_cast<Key>(q) << (11 + bits) : kBad;
     int at = 0, left = count;  // the first one of these columns
     while (left > 0) {
       const int half = left >> 1;
@@ -836,8 +858,8 @@ cudaError_t launch_head_targets(int64_t m, int64_t n, const HeadTargets& t, int4
   const HeadLists l = head_lists(m, n, t.top);
   const int padded = std::max(64, padded_top(32 * t.top));
   int bits = 0;
-  while (padded >> bits > 1) ++bits;
-  const bool narrow = n < (int64_t(1) << (32 - bits)) - 1;
+  while (t.top - 1 >> bits) ++bits;
+  const bool narrow = l.groups1 << (11 + bits) < 0xFFFFFFFELL;
   const size_t smem = (narrow ? 4 : 8) * padded + (rows ? sizeof(float) * 32 * t.top : 0);
   auto kern = narrow ? head_targets_kernel<uint32_t> : head_targets_kernel<unsigned long long>;
   const cudaError_t err = allow_smem(reinterpret_cast<const void*>(kern), smem);

@@ -44,8 +44,9 @@ struct LinLaunch {
   int half_units;                     // on pairs: halves of tiles, after those, all of the last product
   // On pairs: the parts of the tiles of products with split > 1, one to a pair from
   // the first on; the pairs without one take whole tiles in `ahead` rounds of their
-  // own meanwhile.
-  int parts, ahead;
+  // own meanwhile.  Or so the whole tiles of the first product, where they are fewer
+  // than the pairs and long (`alone`).
+  int parts, ahead, alone;
   float* sums;                        // the parts' sums: kPartFloats each
   int* arrived;                       // parts done, for each of their tiles, CTA and epilogue warp
   LinUnits u[kMaxProducts];
@@ -192,6 +193,16 @@ struct PairWork {
     p.width = kLinTile;
     if (round < 0) {
       round = L.ahead;
+      if (L.alone) {
+        const LinUnits& x = L.u[0];
+        p.i = 0;
+        unit_tile(x, pair, &p.tm, &p.tn);
+        p.col = p.tn * kLinTile;
+        p.t0 = 0;
+        p.t1 = x.steps;
+        p.parts = 1;
+        return true;
+      }
       const int first = L.u[0].split > 1 ? L.u[0].units * L.u[0].split : 0;
       p.i = pair >= first ? 1 : 0;
       const LinUnits& x = L.u[p.i];
@@ -212,7 +223,7 @@ struct PairWork {
     int u = round < L.ahead ? round * others + pair - L.parts : L.ahead * others + (round - L.ahead) * npairs + pair;
     ++round;
     if (u >= L.units + L.half_units) return false;
-    const int first = L.u[0].split > 1 ? 0 : L.u[0].units - L.u[0].halves, half = u - L.units;
+    const int first = L.alone || L.u[0].split > 1 ? 0 : L.u[0].units - L.u[0].halves, half = u - L.units;
     p.i = half >= 0 ? L.count - 1 : u >= first ? 1 : 0;
     const LinUnits& x = L.u[p.i];
     unit_tile(x, half >= 0 ? x.units - x.halves + half / 2 : p.i ? u - first : u, &p.tm, &p.tn);
@@ -1027,6 +1038,25 @@ void plan_pairs(const int64_t (&tiles)[kMaxProducts], const int64_t (&steps)[kMa
       best->halves = static_cast<int>(last);
     }
   }
+  // The first product's tiles, fewer than the pairs, take long: one to a pair, whose turns at
+  // the second's then come after theirs.  (In turn, 64 tiles of 786 steps and 788 of 64 left 12
+  // pairs idle for half of the time: the gradient of 4096×50257×1024 461 us, so 430.)
+  if (count == 2 && tiles[0] > 0 && tiles[0] < pairs && tiles[1] > 0) {
+    const int64_t others = pairs - tiles[0];
+    const int64_t ahead = std::min<int64_t>(static_cast<int64_t>(t0 / t1), tiles[1] / others);
+    const int64_t rest = tiles[1] - ahead * others, over = rest % pairs;
+    const bool half = over > 0 && 2 * over <= pairs;
+    const double cost = kPairLaunch + std::max({std::max(t0, ahead * t1) + rest / pairs * t1 +
+                                                    (half ? half_tile_cycles(steps[1]) : over ? t1 : 0.0),
+                                                bytes / (kMemoryRate * 2 * pairs)});
+    if (ahead > 0 && cost < best->cost) {
+      best->cost = cost;
+      best->alone = true;
+      best->parts = static_cast<int>(tiles[0]);
+      best->ahead = static_cast<int>(ahead);
+      best->halves = half ? static_cast<int>(over) : 0;
+    }
+  }
   // The parts of the products of few tiles, while they fit, each next one to the
   // tile that takes longest.
   int split[kMaxProducts] = {1, 1};
@@ -1064,6 +1094,7 @@ void plan_pairs(const int64_t (&tiles)[kMaxProducts], const int64_t (&steps)[kMa
   if (parts == 0 || cost >= best->cost) return;
   best->cost = cost;
   best->halves = 0;
+  best->alone = false;
   for (int i = 0; i < count; ++i) best->pair_split[i] = split[i];
   best->parts = static_cast<int>(parts);
   // Rounds of whole tiles that the other pairs have time for beside a part.
@@ -1188,7 +1219,9 @@ cudaError_t launch_linear(const LinProduct* products, int count, int type, const
     x.p_mn = p.p_mn;
     x.q_mn = p.q_mn;
     x.ep = p.ep;
-    if (x.split > 1) {
+    if (plan.alone && i == 0) {
+      L.alone = x.units;
+    } else if (x.split > 1) {
       split_tiles += x.units;
     } else {
       L.units += x.units - x.halves;
@@ -1201,7 +1234,7 @@ cudaError_t launch_linear(const LinProduct* products, int count, int type, const
       return cudaErrorInvalidValue;
   }
   L.count = count;
-  if (L.units + split_tiles == 0) return cudaSuccess;
+  if (L.units + L.half_units + L.alone + split_tiles == 0) return cudaSuccess;
   if (plan.nt) {
     SplitKernel kern = type == OZ2_TYPE_BF16  ? split_kernel<OZ2_TYPE_BF16>(plan.nt)
                        : type == OZ2_TYPE_F16 ? split_kernel<OZ2_TYPE_F16>(plan.nt)
@@ -1225,6 +1258,8 @@ cudaError_t launch_linear(const LinProduct* products, int count, int type, const
     pairs = num_sms() / 2;
     L.parts = plan.parts;
     L.ahead = plan.ahead;
+  }
+  if (plan.parts && !plan.alone) {
     L.sums = static_cast<float*>(scratch);
     L.arrived = reinterpret_cast<int*>(L.sums + static_cast<int64_t>(plan.parts) * kPartFloats);
     err = cudaMemsetAsync(L.arrived, 0, sizeof(int) * split_tiles * 2 * kLinEpiWarps, st);

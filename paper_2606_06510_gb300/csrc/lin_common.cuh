@@ -188,13 +188,15 @@ struct LinProduct {
 constexpr int kMaxProducts = 2;
 
 // How a launch runs: on CTA pairs (nt = 0), the depth of product i's tiles cut into
-// pair_split[i] parts (`parts` of them in all, `ahead`: see LinLaunch) and the last
-// product's last `halves` tiles taken as two halves each, or in tiles
+// pair_split[i] parts (`parts` of them in all, `ahead`: see LinLaunch), or the first
+// product's whole tiles one to a pair (`alone`), and the last product's last `halves`
+// tiles taken as two halves each, or in tiles
 // of nt rows with the depth split over `split` CTAs and `stages` of operands in
 // flight.  `scratch` bytes of workspace; `cost`, an estimate in cycles.
 struct LinPlan {
   int nt = 0, split = 1, stages = 0;
   int pair_split[kMaxProducts] = {1, 1}, parts = 0, ahead = 0, halves = 0;
+  bool alone = false;
   size_t scratch = 0;
   double cost = 0;
 };
