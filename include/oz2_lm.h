@@ -102,7 +102,7 @@ int oz2_linear_xent_grad(int64_t m, int64_t n, int64_t k, int type, const float*
  *   d_ids     `top` rows of each token (top×m, ldi ≥ top), in any order; below 0: none there
  *   d_teacher the teacher's logits of them (top×m, ldt ≥ top) of teacher_type F32, BF16 or F16
  *   d_loss, d_lse   m floats;  d_picked   top×m floats (ld top): the listed rows' z, 0 where none is
- * A token without rows does not count: its loss is 0.  id ≥ n: NaN.  1 ≤ top ≤ 512;
+ * A token without rows does not count: its loss is 0.  id ≥ n: NaN.  1 ≤ top ≤ 1024;
  * temperature > 0. */
 int oz2_linear_distill(int64_t m, int64_t n, int64_t k, int64_t top, int type, const void* d_X, int64_t ldx,
                        const void* d_W, int64_t ldw, const void* d_ids, int64_t ldi, int id_bits,

@@ -281,6 +281,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     float up = 1.f;                       // dz's scale
     if (GRAD && A.largest) {
       float most = 0.f;
+#pragma unroll 16
       for (int i = lane; i < A.maxima; i += 32) most = fmaxf(most, __ldg(A.largest + i));
       const int bits = __float_as_int(warp_max(most)), e = (bits >> 23) - 127;
       const int s = bits > 0 ? max(-100, min(100, 14 - e)) : 0;
@@ -294,11 +295,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       int row;
       int col0, cols;        // in the piece; of the warp (a half tile is two warps' columns)
       int next;              // the token's target here: its row of w (in the piece)
-      int at, end;           // or the warp's entries here
+      int at, end;           // or its entries here
       HeadRow terms;
     };
-    auto entry_at = [&](int at, int end) {
-      return at < end ? __ldg(A.entries + at) : make_int4(kNoTarget, 0, 0, 0);
+    auto entry_at = [&](const Part& p, int at) {
+      return at < p.end ? __ldg(A.entries + static_cast<int64_t>(p.row) * A.top + at) : make_int2(kNoTarget, 0);
     };
     auto find = [&](int i, Part& p) {
       if (!head_tile(U, i, tile)) return false;
@@ -319,9 +320,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           if (id >= first && id < A.n) p.next = static_cast<int>(id - A.c0);
         }
       }
-      if (SOFT && p.cols > 0 && p.row - lane < A.m) {
-        const int* offset = A.offsets + ((p.row >> 5) * A.groups1 + (A.c0 + p.col0) / kHeadGroup);
-        p.at = __ldg(offset), p.end = __ldg(offset + 1);
+      if (SOFT && p.cols > 0 && p.row < A.m) {
+        const uint16_t* offset = A.offsets + (A.c0 + p.col0) / kHeadGroup * A.ld_offsets + p.row;
+        p.at = __ldg(offset), p.end = __ldg(offset + A.ld_offsets);
       }
       return true;
     };
@@ -329,8 +330,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     bool more = find(pair, now);
     for (int i = pair; more; now = then) {
       i += npairs;
-      int4 entry;
-      if (SOFT) entry = entry_at(now.at + lane, now.end);
+      int2 entry, after;  // the lane's next two entries, whose loads are on their way while it waits
+      if (SOFT) entry = entry_at(now, now.at), after = entry_at(now, now.at + 1);
       if (steps) {
         if (!mbar_wait_bounded(acc_full + 8 * acc, accph, kWaitLimit)) ok = false;
         if (!__all_sync(0xffffffffu, ok)) {
@@ -364,59 +365,33 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         more = find(i, then);
         continue;
       }
-      // Listed rows: each lane walks its own of the warp's entries, which are sorted by token and
-      // column: by shuffles where there are at most 32 of them, else where they lie.
-      int index = 0, column = kNoTarget, value = 0;  // of the lane's next one: its column in the piece, and what it has
-      const int many = SOFT ? now.end - now.at : 0;
-      auto take = [&] {
-        int4 e = make_int4(kNoTarget, 0, 0, 0);
-        if (many <= 32) {
-          e.x = __shfl_sync(0xffffffffu, entry.x, index & 31);
-          e.y = __shfl_sync(0xffffffffu, entry.y, index & 31);
-          if (GRAD) e.z = __shfl_sync(0xffffffffu, entry.z, index & 31);
-        } else if (index < many) {
-          e = __ldg(A.entries + now.at + index);
-        }
-        column = index < many && (e.y & 31) == lane ? e.x - static_cast<int>(A.c0) : kNoTarget;
-        value = GRAD ? e.z : e.y >> 5;
+      // The column in the piece of the lane's next entry.
+      int column = kNoTarget;
+      auto look = [&] { column = entry.x != kNoTarget ? entry.x - static_cast<int>(A.c0) : kNoTarget; };
+      auto advance = [&] {
+        entry = after;
+        ++now.at;
+        after = entry_at(now, now.at + 1);
+        look();
       };
-      if (SOFT && many > 0) {  // the first entry whose token is not before this lane's
-        if (many <= 32) {
-          const int token = lane < many ? entry.y & 31 : 32;
-#pragma unroll
-          for (int s = 16; s; s >>= 1)
-            if (__shfl_sync(0xffffffffu, token, index + s - 1) < lane) index += s;
-          if (__shfl_sync(0xffffffffu, token, index) < lane) ++index;
-        } else {
-          for (int left = many; left > 0;) {
-            const int half = left >> 1;
-            if ((__ldg(&A.entries[now.at + index + half].y) & 31) < lane) {
-              index += half + 1;
-              left -= half + 1;
-            } else {
-              left = half;
-            }
-          }
-          __syncwarp();
-        }
-        take();
-      }
+      if (SOFT) look();
       if (!GRAD) {
         auto pick = [&](const uint32_t (&v)[32], int from) {
           if (SOFT) {
 #pragma unroll
             for (int g = 0; g < 32; g += 8) {
               while (__any_sync(0xffffffffu, column < from + g + 8)) {
-                const bool here = column < from + g + 8;
-                const int at = column - (from + g);
-                uint32_t e = v[g];
+                if (column < from + g + 8) {
+                  const int at = column - (from + g);
+                  uint32_t e = v[g];
 #pragma unroll
-                for (int j = 1; j < 8; ++j) e = j == at ? v[g + j] : e;
-                if (here) A.picked[static_cast<int64_t>(row) * A.top + value] = __uint_as_float(e) * A.scale;
-                index += here;
-                take();
+                  for (int j = 1; j < 8; ++j) e = j == at ? v[g + j] : e;
+                  A.picked[static_cast<int64_t>(row) * A.top + entry.y] = __uint_as_float(e) * A.scale;
+                  advance();
+                }
               }
             }
+            __syncwarp();
           } else if (__any_sync(0xffffffffu, now.next < from + 32)) {
             if (now.next < from + 32) {
               A.picked[row] = pick32(v, now.next - from) * A.scale;
@@ -461,14 +436,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             }
             if (SOFT) {
               while (__any_sync(0xffffffffu, column < from + g + 8)) {
-                const bool here = column < from + g + 8;
-                const int at = column - (from + g);
-                const float weight = -t.a * __int_as_float(value);
+                if (column < from + g + 8) {
+                  const int at = column - (from + g);
+                  const float weight = -t.a * __int_as_float(entry.y);
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                  if (j == at) z[g + j] += weight;  // (past these columns: no j)
-                index += here;
-                take();
+                  for (int j = 0; j < 8; ++j)
+                    if (j == at) z[g + j] += weight;
+                  advance();
+                }
               }
             }
           }
@@ -520,13 +495,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 }
 
 // ---------------------------------------------------------------------------
-// The listed rows of 32 tokens, sorted by group of 64 rows of w, token, row of w and place, and
-// where the entries of each group begin: an epilogue warp then has its own together.
-// (Each token's entries on their own, found by search in every tile, 32 lanes reading 32
-// lists, took more than the products: 350 us for 4096 tokens × 50257×1024 with 64 entries, 250
-// without any.)  With `rows` the entries' weights and the tokens' terms of the gradient.
+// A token's listed rows, sorted by row of w and place, and where those of each group of 64
+// rows of w begin: an epilogue's lane then reads its own two places, beside its neighbours'.
+// (Found by search in every tile, 32 lanes reading 32 lists, the entries took more than the
+// products: 350 us for 4096 tokens × 50257×1024 with 64 entries, 250 without any.  Sorted for
+// 32 tokens together and handed out by shuffles, short lists were as fast, long ones not.)
+// With `rows` the entries' weights and the token's terms of the gradient.  One warp to a token.
 // ---------------------------------------------------------------------------
-constexpr int kListThreads = 1024;
+constexpr int kListWarps = 16;  // (whose offsets of a group are a sector)
 
 __device__ __forceinline__ float teacher_at(const HeadTargets& t, int64_t row, int i) {
   const int64_t at = row * t.ld_teacher + i;
@@ -569,84 +545,80 @@ __device__ __forceinline__ void sort_64(Key* keys, int at, int size, bool first,
   keys[at + 2 * lane] = a, keys[at + 2 * lane + 1] = b;
 }
 
-// A key is the group, the token of the 32 (5 bits), the row of w in the group (6) and the place
-// (`bits`): 32 bits of them where that is enough (its shuffles and comparisons are half).
+// A key is the row of w and, in its low `bits` bits, the place: 32 bits of them where that is
+// enough (its shuffles and comparisons are half).
 template <typename Key>
-__global__ void __launch_bounds__(kListThreads)
-    head_targets_kernel(int64_t m, int64_t n, HeadTargets t, int padded, int bits, int64_t groups1, int4* entries, int* offsets,
-                        HeadRow* rows, HeadTerms terms) {
-  extern __shared__ unsigned long long list_smem[];  // keys, then the teacher's logits
-  Key* keys = reinterpret_cast<Key*>(list_smem);
+__global__ void __launch_bounds__(32 * kListWarps)
+    head_targets_kernel(int64_t m, int64_t n, HeadTargets t, int padded, int bits, int64_t groups1, int64_t ld_offsets,
+                        int2* entries, uint16_t* offsets, HeadRow* rows, HeadTerms terms) {
+  extern __shared__ unsigned long long list_smem[];  // the warps' keys, then the teacher's logits
   constexpr Key kNone = ~Key(0), kBad = kNone - 1;   // not there; no row of w
-  __shared__ float top_s[32], sum_s[32];
   pdl_trigger();
   pdl_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, top = t.top;
-  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * 32, mine = row0 + warp;
-  float* logits = reinterpret_cast<float*>(keys + padded);
+  __shared__ uint16_t offsets_s[2][32][kListWarps];
+  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * kListWarps, row = row0 + warp;
+  const bool there = row < m;
+  Key* keys = reinterpret_cast<Key*>(list_smem) + warp * padded;
+  float* logits = reinterpret_cast<float*>(reinterpret_cast<Key*>(list_smem) + kListWarps * padded) + warp * top;
   float g = 0.f, l = 0.f;
-  if (rows && mine < m && lane == 0) g = terms.dloss[terms.dloss_each ? mine : 0], l = terms.lse[mine];
-  const int count = static_cast<int>(min(int64_t(32), m - row0)) * top;
-  for (int i = threadIdx.x; i < padded; i += kListThreads) {
-    const int r = i / top, place = i - r * top;
+  if (rows && there) g = terms.dloss[terms.dloss_each ? row : 0], l = terms.lse[row];
+  bool live = false, bad = false;
+  float most = kLowest, sum = 0.f;
+  for (int i = lane; i < padded; i += 32) {
     int64_t id = -1;
-    if (i < count) {
-      id = t.ids[(row0 + r) * t.ld + place];
-      if (rows) logits[i] = teacher_at(t, row0 + r, place);
+    if (i < top && there) {
+      id = t.ids[row * t.ld + i];
+      if (rows) {
+        const float u = teacher_at(t, row, i);
+        logits[i] = u;
+        if (id >= 0) most = fmaxf(most, u);
+      }
     }
-    keys[i] = id < 0 ? kNone : id >= n ? kBad : ((static_cast<Key>(id >> 6) << 11 | static_cast<Key>(r << 6 | (id & 63))) << bits) | static_cast<Key>(place);
+    live = live || id >= 0;
+    bad = bad || id >= n;
+    keys[i] = id < 0 ? kNone : id >= n ? kBad : static_cast<Key>(id) << bits | static_cast<Key>(i);
   }
-  __syncthreads();
-  if (rows && mine < m) {
-    bool live = false, bad = false;
-    float most = kLowest, sum = 0.f;
-    for (int i = warp * top + lane; i < (warp + 1) * top; i += 32) {
-      if (keys[i] == kNone) continue;
-      live = true;
-      bad = bad || keys[i] == kBad;
-      most = fmaxf(most, logits[i]);
-    }
+  if (rows) {
     live = __any_sync(0xffffffffu, live);
     bad = __any_sync(0xffffffffu, bad);
     most = warp_max(most);
-    for (int i = warp * top + lane; i < (warp + 1) * top; i += 32)
+    for (int i = lane; i < top; i += 32)
       if (keys[i] != kNone) sum += expf(logits[i] - most);
     sum = warp_add(sum);
-    if (lane == 0) {
-      top_s[warp] = most, sum_s[warp] = sum;
-      rows[mine] = HeadRow{bad ? __int_as_float(0x7FC00000) : live ? g * terms.scale : 0.f, live ? l * kLog2E : 0.f, 0.f, live};
-    }
+    if (lane == 0 && there) rows[row] = HeadRow{bad ? __int_as_float(0x7FC00000) : live ? g * terms.scale : 0.f, live ? l * kLog2E : 0.f, 0.f, live};
   }
-  __syncthreads();
-  for (int at = warp * 64; at < padded; at += 2 * kListThreads) sort_64(keys, at, 64, true, lane);
-  __syncthreads();
+  __syncwarp();
+  for (int at = 0; at < padded; at += 64) sort_64(keys, at, 64, true, lane);
+  __syncwarp();
   for (int size = 128; size <= padded; size <<= 1) {
     for (int step = size >> 1; step >= 64; step >>= 1) {
-      for (int p = threadIdx.x; p < padded / 2; p += kListThreads) {
+      for (int p = lane; p < padded / 2; p += 32) {
         const int i = 2 * p - (p & (step - 1)), j = i + step;
         const Key a = keys[i], b = keys[j];
         if ((a > b) == ((i & size) == 0)) keys[i] = b, keys[j] = a;
       }
-      __syncthreads();
+      __syncwarp();
     }
-    for (int at = warp * 64; at < padded; at += 2 * kListThreads) sort_64(keys, at, size, false, lane);
-    __syncthreads();
+    for (int at = 0; at < padded; at += 64) sort_64(keys, at, size, false, lane);
+    __syncwarp();
   }
-  const int64_t base = row0 * top;
-  for (int i = threadIdx.x; i < count; i += kListThreads) {
+  for (int i = lane; i < top && there; i += 32) {
     const Key key = keys[i];
-    int4 e = make_int4(kNoTarget, 0, 0, 0);
+    int2 e = make_int2(kNoTarget, 0);
     if (key < kBad) {
-      const int place = static_cast<int>(key & ((Key(1) << bits) - 1)), r = static_cast<int>(key >> (bits + 6) & 31);
-      e.x = static_cast<int>(key >> (bits + 11)) << 6 | static_cast<int>(key >> bits & 63);
-      e.y = place << 5 | r;
-      if (rows) e.z = __float_as_int(expf(logits[r * top + place] - top_s[r]) / sum_s[r]);
+      const int place = static_cast<int>(key & ((Key(1) << bits) - 1));
+      e.x = static_cast<int>(key >> bits);
+      e.y = rows ? __float_as_int(expf(logits[place] - most) / sum) : place;
     }
-    entries[base + i] = e;
+    entries[row * top + i] = e;
   }
-  for (int64_t q = threadIdx.x; q < groups1; q += kListThreads) {
-    const Key first = q + 1 < groups1 ? static_cast<Key>(q) << (11 + bits) : kBad;
-    int at = 0, left = count;  // the first one of these columns
+  // The offsets, 32 groups at a time, by way of shared memory: a group's are beside each other.
+  int turn = 0;
+  for (int64_t q0 = 0; q0 < groups1; q0 += 32, turn ^= 1) {
+    const int64_t q = q0 + lane;
+    const Key first = q + 1 < groups1 ? static_cast<Key>(q * kHeadGroup) << bits : kBad;
+    int at = 0, left = top;  // the first one of these columns
     while (left > 0) {
       const int half = left >> 1;
       if (keys[at + half] < first) {
@@ -656,7 +628,10 @@ __global__ void __launch_bounds__(kListThreads)
         left = half;
       }
     }
-    offsets[blockIdx.x * groups1 + q] = static_cast<int>(base) + at;
+    offsets_s[turn][lane][warp] = static_cast<uint16_t>(at);
+    __syncthreads();  // (the other set is written again behind the next one)
+    const int64_t to = q0 + threadIdx.x / kListWarps;
+    if (to < groups1) offsets[to * ld_offsets + row0 + threadIdx.x % kListWarps] = offsets_s[turn][threadIdx.x / kListWarps][threadIdx.x % kListWarps];
   }
 }
 
@@ -850,23 +825,23 @@ int padded_top(int top) {
 }  // namespace
 
 HeadLists head_lists(int64_t m, int64_t n, int top) {
-  return HeadLists{m * top, (n + kHeadGroup - 1) / kHeadGroup + 1, (m + 31) / 32};
+  return HeadLists{m * top, (n + kHeadGroup - 1) / kHeadGroup + 1, (m + 31) / 32 * 32};
 }
 
-cudaError_t launch_head_targets(int64_t m, int64_t n, const HeadTargets& t, int4* entries, int* offsets, HeadRow* rows,
+cudaError_t launch_head_targets(int64_t m, int64_t n, const HeadTargets& t, int2* entries, uint16_t* offsets, HeadRow* rows,
                                 const HeadTerms& terms, cudaStream_t st) {
   const HeadLists l = head_lists(m, n, t.top);
-  const int padded = std::max(64, padded_top(32 * t.top));
+  const int padded = std::max(64, padded_top(t.top));
   int bits = 0;
-  while (t.top - 1 >> bits) ++bits;
-  const bool narrow = l.groups1 << (11 + bits) < 0xFFFFFFFELL;
-  const size_t smem = (narrow ? 4 : 8) * padded + (rows ? sizeof(float) * 32 * t.top : 0);
+  while ((t.top - 1) >> bits) ++bits;
+  const bool narrow = n < (int64_t(1) << (32 - bits)) - 1;
+  const size_t smem = kListWarps * ((narrow ? 4 : 8) * padded + (rows ? sizeof(float) * t.top : 0));
   auto kern = narrow ? head_targets_kernel<uint32_t> : head_targets_kernel<unsigned long long>;
   const cudaError_t err = allow_smem(reinterpret_cast<const void*>(kern), smem);
   if (err != cudaSuccess) return err;
   count_launch();
-  return launch_dependent(kern, dim3(static_cast<unsigned>(l.blocks)), dim3(kListThreads), smem, st, m, n, t, padded, bits, l.groups1,
-                          entries, offsets, rows, terms);
+  return launch_dependent(kern, dim3(static_cast<unsigned>((m + kListWarps - 1) / kListWarps)), dim3(32 * kListWarps), smem, st, m, n, t,
+                          padded, bits, l.groups1, l.ld_offsets, entries, offsets, rows, terms);
 }
 
 int live_rows_maxima(int64_t m, int64_t k) {

@@ -155,8 +155,7 @@ cudaError_t launch_layer_norm_grad(const NormGradArgs& a, int type, void* scratc
 // --- losses over a vocabulary (k_head.cu) ------------------------------------------------
 // The logits z = scale·x·wᵀ are formed tile by tile and used where they are.  What a
 // token wants of them besides their sum of exponentials: its target, or its `top` listed
-// rows of w with a weight each.  Those are sorted for every 32 tokens: entries (row of w,
-// place << 5 | token of the 32, weight's bits, -).
+// rows of w, sorted, with their places in `picked` (forward) or their weights (gradient).
 constexpr int kNoTarget = 0x7FFFFFFF;
 struct HeadTargets {
   Ids ids;
@@ -190,9 +189,9 @@ struct HeadArgs {
   int64_t c0, cols;    // the piece of the vocabulary
   float scale;
   Ids ids;             // targets, one a token
-  const int4* entries; // or entries of every 32 tokens,
-  const int* offsets;  // and where those of a group of 64 rows of w begin: groups1 for every 32 tokens
-  int64_t groups1;
+  const int2* entries; // or (m, top) sorted entries: row of w, place or weight's bits;
+  const uint16_t* offsets;  // where those of a group of 64 rows of w begin: (groups + 1, ld_offsets)
+  int64_t ld_offsets;
   int top, soft;
   // forward
   float2* stats;       // (groups of 64 columns, ld_stats): max and sum of exp2 of z·log2 e
@@ -207,14 +206,13 @@ struct HeadArgs {
   int64_t ld_dz;
 };
 constexpr int kHeadGroup = 64;
-constexpr int kMaxTop = 512;  // (32 tokens' entries are sorted in shared memory)
-// The entries of m tokens (so many, offsets `groups1` for each of the `blocks` of 32); with
-// `rows`, their weights and the rows' terms too.
+constexpr int kMaxTop = 1024;
+// Entries and offsets (groups1 rows of ld_offsets); with `rows`, weights and the rows' terms.
 struct HeadLists {
-  int64_t entries, groups1, blocks;
+  int64_t entries, groups1, ld_offsets;
 };
 HeadLists head_lists(int64_t m, int64_t n, int top);
-cudaError_t launch_head_targets(int64_t m, int64_t n, const HeadTargets& t, int4* entries, int* offsets, HeadRow* rows,
+cudaError_t launch_head_targets(int64_t m, int64_t n, const HeadTargets& t, int2* entries, uint16_t* offsets, HeadRow* rows,
                                 const HeadTerms& terms, cudaStream_t st);
 // x's rows of live tokens to rows of ld_dst elements on 16-byte boundaries, zeros for the others; and
 // with `largest` the maxima for HeadArgs, as many as live_rows_maxima(m, k).

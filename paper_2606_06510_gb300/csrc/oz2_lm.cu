@@ -40,7 +40,7 @@ int check_head(const HeadCall& c, int id_bits) {
   if (c.t.soft && (c.t.top < 1 || c.t.top > kMaxTop || c.t.ld < c.t.top || c.t.ld_teacher < c.t.top ||
                    !valid_type(c.t.teacher_type) || !(c.t.temperature > 0)))
     return OZ2_ERR_INVALID_ARG;
-  if (too_large(c.m, c.n, c.k) || (c.t.soft && c.m * c.t.top > 0x7FFFFFFF)) return OZ2_ERR_UNSUPPORTED;
+  if (too_large(c.m, c.n, c.k)) return OZ2_ERR_UNSUPPORTED;
   return OZ2_OK;
 }
 bool head_pointers(const HeadCall& c, int id_bits) {
@@ -72,19 +72,19 @@ int head_forward(const HeadCall& c, float* loss, float* lse, float* picked, cuda
   const int64_t ld_stats = (c.m + 31) / 32 * 32, groups = (c.n + kHeadGroup - 1) / kHeadGroup;
   const size_t stats = ws.ask(sizeof(float2) * ld_stats * groups);
   const HeadLists lists = head_lists(c.m, c.n, c.t.top);
-  const size_t entries = c.t.soft ? ws.ask(sizeof(int4) * lists.entries) : 0;
-  const size_t offsets = c.t.soft ? ws.ask(sizeof(int) * lists.groups1 * lists.blocks) : 0;
+  const size_t entries = c.t.soft ? ws.ask(sizeof(int2) * lists.entries) : 0;
+  const size_t offsets = c.t.soft ? ws.ask(sizeof(uint16_t) * lists.groups1 * lists.ld_offsets) : 0;
   if (!ws.take()) return OZ2_ERR_ALLOC;
   cudaError_t err = place(X, W, ws, st);
   if (err == cudaSuccess && c.t.soft)
-    err = launch_head_targets(c.m, c.n, c.t, ws.at<int4>(entries), ws.at<int>(offsets), nullptr, HeadTerms{}, st);
+    err = launch_head_targets(c.m, c.n, c.t, ws.at<int2>(entries), ws.at<uint16_t>(offsets), nullptr, HeadTerms{}, st);
   HeadArgs a{};
   a.m = c.m, a.n = c.n, a.k = c.k;
   a.x = X.p, a.ldx = X.ld, a.w = W.p, a.ldw = W.ld;
   a.cols = c.n;
   a.scale = c.scale;
   a.ids = c.t.ids;
-  a.entries = ws.at<int4>(entries), a.offsets = ws.at<int>(offsets), a.groups1 = lists.groups1;
+  a.entries = ws.at<int2>(entries), a.offsets = ws.at<uint16_t>(offsets), a.ld_offsets = lists.ld_offsets;
   a.top = c.t.top, a.soft = c.t.soft;
   a.stats = ws.at<float2>(stats), a.ld_stats = ld_stats;
   a.picked = picked;
@@ -132,8 +132,8 @@ int head_grad(const HeadCall& c, const HeadGrads& g, int id_bits, cudaStream_t s
   const int64_t ld_dz = (piece + 63) / 64 * 64, ld_sum = (c.k + 31) / 32 * 32;
   Workspace ws(st);
   const HeadLists lists = head_lists(c.m, c.n, c.t.top);
-  const size_t rows = c.t.soft ? ws.ask(sizeof(HeadRow) * c.m) : 0, entries = c.t.soft ? ws.ask(sizeof(int4) * lists.entries) : 0;
-  const size_t offsets = c.t.soft ? ws.ask(sizeof(int) * lists.groups1 * lists.blocks) : 0;
+  const size_t rows = c.t.soft ? ws.ask(sizeof(HeadRow) * c.m) : 0, entries = c.t.soft ? ws.ask(sizeof(int2) * lists.entries) : 0;
+  const size_t offsets = c.t.soft ? ws.ask(sizeof(uint16_t) * lists.groups1 * lists.ld_offsets) : 0;
   const size_t maxima = scaled ? ws.ask(sizeof(float) * (live_rows_maxima(c.m, c.k) + 1)) : 0;
   // (x's copy is where the largest of the terms is found, and dead tokens' x made zeros for dw.)
   const HeadCopies copies = head_copies(c, want_dx ? 2 : 1, want_dw || scaled);
@@ -170,7 +170,7 @@ int head_grad(const HeadCall& c, const HeadGrads& g, int id_bits, cudaStream_t s
   HeadTerms terms{nullptr, g.dloss, g.lse, (g.flags & OZ2_GRAD_ONE_DLOSS) == 0, c.scale, c.z_loss};
   cudaError_t err = cudaSuccess;
   if (c.t.soft) {
-    err = launch_head_targets(c.m, c.n, c.t, ws.at<int4>(entries), ws.at<int>(offsets), ws.at<HeadRow>(rows), terms, st);
+    err = launch_head_targets(c.m, c.n, c.t, ws.at<int2>(entries), ws.at<uint16_t>(offsets), ws.at<HeadRow>(rows), terms, st);
     terms.rows = ws.at<HeadRow>(rows);
   }
   if (err == cudaSuccess && X.copy) {
@@ -191,7 +191,7 @@ int head_grad(const HeadCall& c, const HeadGrads& g, int id_bits, cudaStream_t s
     a.c0 = c0, a.cols = cols;
     a.scale = c.scale;
     a.ids = c.t.ids;
-    a.entries = ws.at<int4>(entries), a.offsets = ws.at<int>(offsets), a.groups1 = lists.groups1;
+    a.entries = ws.at<int2>(entries), a.offsets = ws.at<uint16_t>(offsets), a.ld_offsets = lists.ld_offsets;
     a.top = c.t.top, a.soft = c.t.soft;
     a.terms = terms;
     a.largest = largest, a.maxima = live_rows_maxima(c.m, c.k), a.unscale = unscale;

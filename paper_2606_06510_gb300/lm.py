@@ -18,7 +18,7 @@ from .layers import GRAD_ACCUMULATE, TYPE, _ENTRIES, _done, _entry, _ld, _new
 
 _I64, _P, _I, _U, _F = ctypes.c_int64, ctypes.c_void_p, ctypes.c_int, ctypes.c_uint, ctypes.c_float
 GRAD_ONE_DLOSS = 0x2
-MAX_TOP = 512
+MAX_TOP = 1024
 IDS = {torch.int64: 64, torch.int32: 32}
 
 SIGS = {

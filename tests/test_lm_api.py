@@ -151,7 +151,7 @@ def distill(oz, m=4, n=8, k=8, top=4, type=BF16, X=16, ldx=8, W=16, ldw=8, ids=1
                                        picked, N)
 
 
-DISTILL = [dict(m=-1), dict(n=0), dict(k=-1), dict(top=0), dict(top=-1), dict(top=513, ldi=2000, ldt=2000), dict(type=F32),
+DISTILL = [dict(m=-1), dict(n=0), dict(k=-1), dict(top=0), dict(top=-1), dict(top=1025, ldi=2000, ldt=2000), dict(type=F32),
            dict(ldi=3), dict(ldt=3), dict(bits=16), dict(tt=E4M3), dict(temp=0.0), dict(temp=-1.0), dict(temp=NAN),
            dict(temp=1e-45), dict(ids=N), dict(T=N), dict(T=18), dict(ids=20), dict(X=N), dict(W=N), dict(lse=N)]
 
