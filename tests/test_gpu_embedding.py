@@ -96,7 +96,8 @@ def test_forward_offsets_pass_32_bits(oz):
 @pytest.mark.parametrize("dt", TYPES)
 @pytest.mark.parametrize("kind", ["zipf", "even", "one"])
 @pytest.mark.parametrize("m,n,k,how", [
-    (1, 1, 1, "whole"), (5, 7, 8, "whole"), (31, 40, 33, "odd"), (100, 3, 264, "strided"), (300, 511, 64, "whole"),
+    (1, 1, 1, "whole"), (5, 7, 8, "whole"), (31, 40, 33, "odd"), (100, 3, 264, "strided"), (255, 9000, 16, "odd"),
+    (256, 300, 4100, "whole"), (257, 300, 4100, "whole"), (200, 131071, 24, "strided"), (300, 511, 64, "whole"),
     (1000, 512, 777, "whole"), (2049, 70000, 40, "whole"), (5000, 131071, 16, "whole"), (20000, 600, 24, "odd")])
 def test_gradient(oz, dt, kind, m, n, k, how):
     g = rng(m + n + k)
@@ -145,16 +146,17 @@ def test_gradient_nothing_to_do(oz):
     assert oz.oz2_embedding_grad(dy, none, 0).shape == (0, 8)
 
 
-def test_nan_stays_with_its_row(oz):
-    dy = torch.ones(40, 16, device="cuda")
+@pytest.mark.parametrize("m", [40, 400])
+def test_nan_stays_with_its_row(oz, m):
+    dy = torch.ones(m, 16, device="cuda")
     dy[3] = float("nan")
     dy[7] = float("inf")
-    ids = torch.arange(40, device="cuda") % 20
+    ids = torch.arange(m, device="cuda") % (m // 2)
     ids[9] = -1
     dy[9] = float("nan")
-    got = oz.oz2_embedding_grad(dy, ids, 30)
+    got = oz.oz2_embedding_grad(dy, ids, m)
     assert got[3].isnan().all() and got[7].isinf().all()
-    keep = torch.ones(30, dtype=torch.bool, device="cuda")
+    keep = torch.ones(m, dtype=torch.bool, device="cuda")
     keep[[3, 7]] = False
     assert got[keep].isfinite().all() and (got[9] == 1).all()
 
