@@ -32,7 +32,7 @@ __global__ void __launch_bounds__(256)
   const uint32_t stride_rows = stride / per, stride_pieces = stride - stride_rows * per;
   int64_t r = first / per;
   uint32_t c = first - static_cast<uint32_t>(r) * per;
-  while (r < m) {
+  while (ALIGNED ? r < m : __any_sync(0xffffffffu, r < m) != 0) {
     int64_t row[kAhead], id[kAhead];
     int col[kAhead];
     uint4 v[kAhead];
@@ -53,13 +53,13 @@ __global__ void __launch_bounds__(256)
     }
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      if (row[j] >= m) continue;
+      if (ALIGNED && row[j] >= m) continue;
       float f[X::V];
       X::unpack(v[j], f);
 #pragma unroll
       for (int e = 0; e < X::V; ++e) f[e] = id[j] >= n ? __int_as_float(0x7FC00000) : f[e] * scale;
-      const int there = static_cast<int>(min(int64_t(X::V), k - col[j]));
-      store16_any(dst + row[j] * ldy + col[j], X::pack(f), there, ALIGNED && there == X::V);
+      const int there = row[j] < m ? static_cast<int>(min(int64_t(X::V), k - col[j])) : 0;
+      store_piece<ALIGNED>(dst + (there ? row[j] * ldy + col[j] : 0), X::pack(f), there);
     }
   }
 }
@@ -268,7 +268,7 @@ struct Window {
   }
 };
 
-// A piece of a row of dE from its sums: stored, or added to what is there.  Each is added
+// By a warp, a piece of a row of dE from its sums: stored, or added to what is there.  Each is added
 // to once, so an FP32 one can be left to the memory (a vector reduction; a result below
 // 2^-126 counts as 0), which spares the way there and back; a 16-bit one is read (`old`,
 // ahead) and rounded once.
@@ -300,17 +300,14 @@ __device__ __forceinline__ void finish_piece(void* dE, int64_t row, int64_t ldde
 #pragma unroll
         for (int e = 0; e < Y::V; ++e) o[e] = fmaf(sums[h + e], scale, was[e]);
       }
-      store16_any(p + h, Y::pack(o), n - h, vec && n >= h + Y::V);
+      if (vec) {
+        store16_any(p + h, Y::pack(o), n - h, n >= h + Y::V);
+      } else {
+        store16_warp(p + h, Y::pack(o), min(max(n - h, 0), Y::V));
+      }
     }
   }
 }
-template <int OUT>
-__device__ __forceinline__ uint4 old_piece(const void* dE, int64_t row, int64_t ldde, int64_t col, int n, bool vec) {
-  using T = typename Elem<OUT>::T;
-  const T* p = static_cast<const T*>(dE) + row * ldde + col;
-  return vec && n >= Elem<OUT>::V ? *reinterpret_cast<const uint4*>(p) : load16_singly<false>(p, n);
-}
-
 // Pieces of a row to a lane: up to 16 FP32 sums.  (One a lane, the work on the pairs took
 // longer than the rows: 65536 tokens of 2048 f32 398 us.)
 constexpr int most_pieces(int type) { return type == OZ2_TYPE_F32 ? 4 : 2; }
@@ -331,6 +328,16 @@ struct SumJob {
   int most_runs;
   int slices, pieces;      // of a row, and of a slice to a lane
 };
+
+// What a piece of dE holds.  (Words around it may hold others' pieces, which are not looked at.)
+template <int OUT>
+__device__ __forceinline__ uint4 old_piece(const SumJob& j, int64_t row, int64_t col, int n) {
+  using T = typename Elem<OUT>::T;
+  const T* base = static_cast<const T*>(j.dE);
+  const T* p = base + row * j.ldde + col;
+  if (j.vec) return load_piece<true, false>(p, base, base, n);
+  return load_piece<false, false>(p, base, base + (static_cast<int64_t>(j.n) - 1) * j.ldde + j.k, n);
+}
 
 template <int TYPE, int OUT, int P, bool ALIGNED, bool ADD>
 __global__ void __launch_bounds__(32 * kSumWarps, P == 1 ? 4 : P == 2 ? 3 : 2) sum_runs_kernel(SumJob j) {
@@ -421,7 +428,7 @@ __global__ void __launch_bounds__(32 * kSumWarps, P == 1 ? 4 : P == 2 ? 3 : 2) s
         const int n = there(c);
         if (n > 0 && i + q < end) v[q][c] = load_piece<ALIGNED>(row + col(c), src, stop, n);
         if (kOld && n > 0 && i + q < end && (ends >> at & 1) && at >= head)
-          old[kOld ? q : 0][c] = old_piece<OUT>(j.dE, pair.x, j.ldde, col(c), n, j.vec);
+          old[kOld ? q : 0][c] = old_piece<OUT>(j, pair.x, col(c), n);
       }
     }
 #pragma unroll
@@ -441,8 +448,7 @@ __global__ void __launch_bounds__(32 * kSumWarps, P == 1 ? 4 : P == 2 ? 3 : 2) s
       } else if (ends >> at & 1) {
 #pragma unroll
         for (int c = 0; c < P; ++c)
-          if (there(c) > 0)
-            finish_piece<TYPE, OUT, ADD>(j.dE, pairs[at].x, j.ldde, col(c), there(c), j.scale, j.vec, old[kOld ? q : 0][c], s[c]);
+          finish_piece<TYPE, OUT, ADD>(j.dE, pairs[at].x, j.ldde, col(c), there(c), j.scale, j.vec, old[kOld ? q : 0][c], s[c]);
         clear();
       }
     }
@@ -495,11 +501,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_runs_kernel(SumJob j) {
   auto finish = [&](int row, int piece) {
     const int64_t col = (static_cast<int64_t>(piece) * 32 + lane) * V;
     const int n = static_cast<int>(max(int64_t(0), min(int64_t(V), j.k - col)));
-    if (n > 0) {
-      uint4 old = make_uint4(0, 0, 0, 0);
-      if (ADD && OUT != OZ2_TYPE_F32) old = old_piece<OUT>(j.dE, row, j.ldde, col, n, j.vec);
-      finish_piece<TYPE, OUT, ADD>(j.dE, row, j.ldde, col, n, j.scale, j.vec, old, s);
-    }
+    uint4 old = make_uint4(0, 0, 0, 0);
+    if (ADD && OUT != OZ2_TYPE_F32 && n > 0) old = old_piece<OUT>(j, row, col, n);
+    finish_piece<TYPE, OUT, ADD>(j.dE, row, j.ldde, col, n, j.scale, j.vec, old, s);
   };
   const int many = j.long_runs[0], few = j.long_runs[1];
   for (int64_t u = static_cast<int64_t>(warp) * gridDim.x + blockIdx.x; u < static_cast<int64_t>(few) * pieces;
@@ -593,11 +597,10 @@ __global__ void __launch_bounds__(32 * kSumWarps) few_tokens_kernel(SumJob j, Id
   if (list_s[0] != token) return;
   const int64_t col = (static_cast<int64_t>(slice) * 32 + lane) * V;
   const int n = static_cast<int>(max(int64_t(0), min(int64_t(V), j.k - col)));
-  if (n == 0) return;
   const T* src = static_cast<const T*>(j.dY);
   const T* stop = src + (j.m - 1) * j.lddy + j.k;
   uint4 old = make_uint4(0, 0, 0, 0);
-  if (ADD && OUT != OZ2_TYPE_F32) old = old_piece<OUT>(j.dE, row, j.ldde, col, n, j.vec);
+  if (ADD && OUT != OZ2_TYPE_F32 && n > 0) old = old_piece<OUT>(j, row, col, n);
   float s[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) s[e] = 0.f;
@@ -605,7 +608,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) few_tokens_kernel(SumJob j, Id
     uint4 v[8];
 #pragma unroll
     for (int q = 0; q < 8; ++q)
-      if (i + q < count) v[q] = load_piece<ALIGNED>(src + list_s[i + q] * j.lddy + col, src, stop, n);
+      if (i + q < count && n > 0) v[q] = load_piece<ALIGNED>(src + list_s[i + q] * j.lddy + col, src, stop, n);
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
       if (i + q >= count) break;

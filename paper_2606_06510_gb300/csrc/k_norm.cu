@@ -65,18 +65,33 @@ __device__ __forceinline__ void load_vector(const void* p, int wtype, int64_t co
     }
   } else {
     const typename X::T* s = static_cast<const typename X::T*>(p);
-    X::unpack(load_piece<false>(s + col, s, s + k, n), f);
+    if (reinterpret_cast<uintptr_t>(s) & 15) {
+      X::unpack(load_piece<false>(s + col, s, s + k, n), f);
+    } else {
+      X::unpack(load_piece<true>(s + col, s, s + k, n), f);
+    }
   }
 }
 
+template <int TYPE>
+__device__ __forceinline__ void unpack2(uint4 v, Two (&t)[Elem<TYPE>::V / 2]) {
+  float f[Elem<TYPE>::V];
+  Elem<TYPE>::unpack(v, f);
+#pragma unroll
+  for (int e = 0; e < Elem<TYPE>::V / 2; ++e) t[e] = two(f[2 * e], f[2 * e + 1]);
+}
+
 // ---------------------------------------------------------------------------
-// Forward.  TPR threads to a row, VPT 16-byte pieces of it to a thread.
+// Forward.  TPR threads to a row, VPT 16-byte pieces of it to a thread: up to 16 values, two
+// to an instruction (with 32 of them the row's work was longer than its way from memory).
 // ---------------------------------------------------------------------------
+constexpr int norm_block(int tpr, int least) { return tpr < least ? least : tpr; }
+
 template <int TYPE, int TPR, int VPT, bool ALIGNED>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) norm_kernel(NormArgs a) {
+__global__ void __launch_bounds__(norm_block(TPR, 256)) norm_kernel(NormArgs a) {
   using X = Elem<TYPE>;
   using T = typename X::T;
-  constexpr int V = X::V, kBlock = TPR < 128 ? 128 : TPR, kGroups = kBlock / TPR;
+  constexpr int V = X::V, H = V / 2, kGroups = norm_block(TPR, 256) / TPR;
   __shared__ float exchange[kGroups][2 * TPR / 32];
   pdl_trigger();
   pdl_wait();
@@ -85,64 +100,75 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) norm_kernel(NormArgs a)
   const T* end = src + (a.m - 1) * a.ldx + a.k;
   const float inv_k = 1.f / static_cast<float>(a.k);
   RowSum<TPR, 1> rows{exchange[group], group, 0};
+  auto col = [&](int i) { return static_cast<int64_t>(t + i * TPR) * V; };
+  auto there = [&](int i) { return static_cast<int>(max(int64_t(0), min(int64_t(V), a.k - col(i)))); };
   for (int64_t r = static_cast<int64_t>(blockIdx.x) * kGroups + group; r < a.m; r += static_cast<int64_t>(gridDim.x) * kGroups) {
     uint4 raw[VPT];
-    float x[VPT][V];
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      const int64_t col = static_cast<int64_t>(t + i * TPR) * V;
       raw[i] = make_uint4(0, 0, 0, 0);
-      if (col < a.k)
-        raw[i] = load_piece<ALIGNED>(src + r * a.ldx + col, src, end, static_cast<int>(min(int64_t(V), a.k - col)));
+      if (there(i)) raw[i] = load_piece<ALIGNED>(src + r * a.ldx + col(i), src, end, there(i));
     }
-    float s[1] = {0.f};
+    Two x[VPT][H], s = two(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      X::unpack(raw[i], x[i]);  // (zeros past the row's end)
+      unpack2<TYPE>(raw[i], x[i]);  // (zeros past the row's end)
 #pragma unroll
-      for (int e = 0; e < V; ++e) s[0] += x[i][e];
+      for (int e = 0; e < H; ++e) s = s + x[i][e];
     }
-    float mean = 0.f;
+    float mean = 0.f, sum[1];
     if (a.center) {
-      rows.sum(s);
-      mean = s[0] * inv_k;
+      const float2 p = both(s);
+      sum[0] = p.x + p.y;
+      rows.sum(sum);
+      mean = sum[0] * inv_k;
     }
-    s[0] = 0.f;
+    const Two less = two(-mean, -mean);
+    s = two(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      const int64_t col = static_cast<int64_t>(t + i * TPR) * V;
+      const int n = there(i);
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        x[i][e] -= mean;
-        if (col + e < a.k) s[0] = fmaf(x[i][e], x[i][e], s[0]);
+      for (int e = 0; e < H; ++e) {
+        x[i][e] = x[i][e] + less;
+        if (n < V) {  // the row's end: what is past it deviates by nothing
+          const float2 p = both(x[i][e]);
+          x[i][e] = two(2 * e < n ? p.x : 0.f, 2 * e + 1 < n ? p.y : 0.f);
+        }
+        s = fma(x[i][e], x[i][e], s);
       }
     }
-    rows.sum(s);
-    const float rstd = 1.f / sqrtf(fmaf(s[0], inv_k, a.eps));
+    const float2 p = both(s);
+    sum[0] = p.x + p.y;
+    rows.sum(sum);
+    const float rstd = 1.f / sqrtf(fmaf(sum[0], inv_k, a.eps));
     if (t == 0) {
       if (a.mean) a.mean[r] = mean;
       if (a.rstd) a.rstd[r] = rstd;
     }
+    const Two scale = two(rstd, rstd);
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      const int64_t col = static_cast<int64_t>(t + i * TPR) * V;
-      if (col >= a.k) continue;
-      const int n = static_cast<int>(min(int64_t(V), a.k - col));
+      const int n = there(i);
+      float f[V];
 #pragma unroll
-      for (int e = 0; e < V; ++e) x[i][e] *= rstd;
-      if (a.w) {
-        float w[V];
-        load_vector<TYPE>(a.w, a.wtype, col, n, a.k, w);
+      for (int e = 0; e < H; ++e) x[i][e] = x[i][e] * scale;
+      if (a.w && n) {
+        load_vector<TYPE>(a.w, a.wtype, col(i), n, a.k, f);
 #pragma unroll
-        for (int e = 0; e < V; ++e) x[i][e] *= w[e];
+        for (int e = 0; e < H; ++e) x[i][e] = x[i][e] * two(f[2 * e], f[2 * e + 1]);
       }
-      if (a.b) {
-        float b[V];
-        load_vector<TYPE>(a.b, a.wtype, col, n, a.k, b);
+      if (a.b && n) {
+        load_vector<TYPE>(a.b, a.wtype, col(i), n, a.k, f);
 #pragma unroll
-        for (int e = 0; e < V; ++e) x[i][e] += b[e];
+        for (int e = 0; e < H; ++e) x[i][e] = x[i][e] + two(f[2 * e], f[2 * e + 1]);
       }
-      store16_any(static_cast<T*>(a.y) + r * a.ldy + col, X::pack(x[i]), n, ALIGNED && n == V);
+#pragma unroll
+      for (int e = 0; e < H; ++e) {
+        const float2 q = both(x[i][e]);
+        f[2 * e] = q.x, f[2 * e + 1] = q.y;
+      }
+      store_piece<ALIGNED>(static_cast<T*>(a.y) + r * a.ldy + (n ? col(i) : 0), X::pack(f), n);
     }
   }
 }
@@ -217,27 +243,19 @@ __device__ __forceinline__ void fetch_async(uint32_t to, const void* from, int b
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
 }
 constexpr int kStagedBytes = 200 * 1024;  // of a block's 227 KB
-constexpr int norm_stages(int vpt) {
-  const int n = kStagedBytes / (3 * vpt * 16 * kNormThreads);
-  return n < 2 ? 0 : n < 4 ? n : 4;
+constexpr int norm_stages(int tpr, int vpt) {
+  const int n = kStagedBytes / (3 * vpt * 16 * norm_block(tpr, kNormThreads));
+  return n < 4 ? n : 4;
 }
 
-template <int TYPE>
-__device__ __forceinline__ void unpack2(uint4 v, Two (&t)[Elem<TYPE>::V / 2]) {
-  float f[Elem<TYPE>::V];
-  Elem<TYPE>::unpack(v, f);
-#pragma unroll
-  for (int e = 0; e < Elem<TYPE>::V / 2; ++e) t[e] = two(f[2 * e], f[2 * e + 1]);
-}
-
-// Up to 16 values of a row to a thread stay in registers between the sums and dx; of
-// longer rows they are formed a second time.
+// A thread's 16 values of a row stay in registers between the sums and dx; the 1024 threads of
+// rows over 8192 have registers for the columns' sums alone and form them a second time.
 template <int TYPE, int TPR, int VPT, int STAGES>
-__global__ void __launch_bounds__(kNormThreads, 1) norm_grad_kernel(NormGradArgs a, float* __restrict__ parts) {
+__global__ void __launch_bounds__(norm_block(TPR, kNormThreads), 1) norm_grad_kernel(NormGradArgs a, float* __restrict__ parts) {
   using X = Elem<TYPE>;
   using T = typename X::T;
-  constexpr int V = X::V, H = V / 2, kGroups = kNormThreads / TPR;
-  constexpr bool STAGED = STAGES > 0, KEEP = VPT * V <= 16;
+  constexpr int V = X::V, H = V / 2, kBlock = norm_block(TPR, kNormThreads), kGroups = kBlock / TPR;
+  constexpr bool STAGED = STAGES > 0, KEEP = TPR < 1024;
   __shared__ float exchange[kGroups][4 * TPR / 32];
   // The rows' pieces, and after them the groups' columns of dw and db.
   extern __shared__ __align__(16) uint8_t norm_smem[];
@@ -270,7 +288,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_grad_kernel(NormGradArgs
   const int64_t stride = static_cast<int64_t>(gridDim.x) * kGroups, first = static_cast<int64_t>(blockIdx.x) * kGroups + group;
   uint4 rd[VPT], rx[VPT], rr[VPT];  // (not staged)
   auto piece = [&](int stage, int which, int i) {
-    return norm_smem + (((stage * 3 + which) * VPT + i) * kNormThreads + threadIdx.x) * 16;
+    return norm_smem + (((stage * 3 + which) * VPT + i) * kBlock + threadIdx.x) * 16;
   };
   auto fetch = [&](int64_t r, int stage) {
     if (r < a.m) {
@@ -348,7 +366,6 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_grad_kernel(NormGradArgs
 #pragma unroll
       for (int i = 0; i < VPT; ++i) {
         const int n = there(i);
-        if (n == 0) continue;
         Two d[H], gi[H], hi[H];
         Two(&g)[H] = KEEP ? kg[KEEP ? i : 0] : gi;
         Two(&h)[H] = KEEP ? kh[KEEP ? i : 0] : hi;
@@ -367,7 +384,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_grad_kernel(NormGradArgs
           const float2 f = both(d[e]);
           y[2 * e] = f.x, y[2 * e + 1] = f.y;
         }
-        store16_any(static_cast<T*>(a.dx) + r * a.lddx + col(i), X::pack(y), n, STAGED && n == V);
+        store_piece<STAGED>(static_cast<T*>(a.dx) + r * a.lddx + (n ? col(i) : 0), X::pack(y), n);
       }
     }
     statistics(r + stride);
@@ -396,7 +413,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_grad_kernel(NormGradArgs
   put(db, columns + (kGroups + group) * kCols);
   __syncthreads();
   float* to = parts + static_cast<int64_t>(blockIdx.x) * 2 * a.k;
-  for (int c = threadIdx.x; c < a.k; c += kNormThreads) {
+  for (int c = threadIdx.x; c < a.k; c += kBlock) {
     float w_sum = columns[c], b_sum = columns[kGroups * kCols + c];
 #pragma unroll
     for (int q = 1; q < kGroups; ++q) w_sum += columns[q * kCols + c], b_sum += columns[(kGroups + q) * kCols + c];
@@ -531,31 +548,32 @@ __global__ void __launch_bounds__(256) join_parts_kernel(int64_t k, int count, c
 }
 
 // ---------------------------------------------------------------------------
-// Threads to a row and pieces to a thread: as few threads as hold it with `each` values
-// to a thread, and up to 32 of them at the most.  Longer rows are not held.
+// Threads to a row and pieces to a thread: as few threads as hold it with 16 values to a
+// thread (`least` of them at least, if it has that many pieces).  Rows of more than 16384 are
+// not held.
 // ---------------------------------------------------------------------------
 struct NormShape {
   int tpr, vpt;  // 0: too long
 };
-NormShape shape_of(int64_t k, int type, int each, int least) {
+NormShape shape_of(int64_t k, int type, int least) {
   const int v = 16 / type_bytes(type);
   const int64_t pieces = (k + v - 1) / v;
-  for (int tpr : {32, 64, 128, 256, 512}) {
+  for (int tpr : {32, 64, 128, 256, 512, 1024}) {
     if (tpr < least && pieces > tpr) continue;
-    for (int vpt = 1; vpt * v <= (tpr < 512 ? each : 32); vpt *= 2)
+    for (int vpt = 1; vpt * v <= 16; vpt *= 2)
       if (pieces <= static_cast<int64_t>(tpr) * vpt) return {tpr, vpt};
   }
   return {0, 0};
 }
 // Forward: few rows get more threads each.
 NormShape forward_shape(int64_t m, int64_t k, int type) {
-  return shape_of(k, type, 32, m <= 2 * static_cast<int64_t>(num_sms()) ? 512 : 32);
+  return shape_of(k, type, m <= 2 * static_cast<int64_t>(num_sms()) ? 512 : 32);
 }
-NormShape backward_shape(int64_t m, int64_t k, int type) { return shape_of(k, type, 16, 32); }
+NormShape backward_shape(int64_t k, int type) { return shape_of(k, type, 32); }
 
 template <template <int, int> class K, int TPR>
 auto by_pieces(int vpt) {
-  return vpt == 1 ? K<TPR, 1>::f() : vpt == 2 ? K<TPR, 2>::f() : vpt == 4 ? K<TPR, 4>::f() : K<TPR, 8>::f();
+  return vpt == 1 ? K<TPR, 1>::f() : vpt == 2 ? K<TPR, 2>::f() : K<TPR, 4>::f();
 }
 template <template <int, int> class K>
 auto by_shape(NormShape s) {  // the kernel K of these threads and pieces
@@ -563,22 +581,23 @@ auto by_shape(NormShape s) {  // the kernel K of these threads and pieces
          : s.tpr == 64  ? by_pieces<K, 64>(s.vpt)
          : s.tpr == 128 ? by_pieces<K, 128>(s.vpt)
          : s.tpr == 256 ? by_pieces<K, 256>(s.vpt)
-                        : by_pieces<K, 512>(s.vpt);
+         : s.tpr == 512 ? by_pieces<K, 512>(s.vpt)
+                        : by_pieces<K, 1024>(s.vpt);
 }
-// (Of 8 pieces, those of 16-bit rows are never asked for.)
+// (Of 4 pieces, those of 16-bit rows are never asked for.)
 template <int TYPE, bool ALIGNED>
 struct Forward {
   template <int TPR, int VPT>
   struct K {
-    static auto f() { return &norm_kernel<TYPE, TPR, VPT * Elem<TYPE>::V <= 32 ? VPT : 4, ALIGNED>; }
+    static auto f() { return &norm_kernel<TYPE, TPR, VPT * Elem<TYPE>::V <= 16 ? VPT : 2, ALIGNED>; }
   };
 };
 template <int TYPE, bool ALIGNED>
 struct Backward {
   template <int TPR, int VPT>
   struct K {
-    static constexpr int kMost = TPR < 512 ? 16 / Elem<TYPE>::V : 32 / Elem<TYPE>::V, kVpt = VPT < kMost ? VPT : kMost;
-    static auto f() { return &norm_grad_kernel<TYPE, TPR, kVpt, ALIGNED ? norm_stages(kVpt) : 0>; }
+    static constexpr int kVpt = VPT * Elem<TYPE>::V <= 16 ? VPT : 2;
+    static auto f() { return &norm_grad_kernel<TYPE, TPR, kVpt, ALIGNED ? norm_stages(TPR, kVpt) : 0>; }
   };
 };
 
@@ -593,7 +612,7 @@ cudaError_t forward(const NormArgs& a, cudaStream_t st) {
   }
   const bool aligned = rows_on16(a.x, a.ldx, es) && rows_on16(a.y, a.ldy, es);
   auto kern = aligned ? by_shape<Forward<TYPE, true>::template K>(s) : by_shape<Forward<TYPE, false>::template K>(s);
-  const int block = s.tpr < 128 ? 128 : s.tpr, groups = block / s.tpr;
+  const int block = norm_block(s.tpr, 256), groups = block / s.tpr;
   const int64_t blocks = std::min<int64_t>((a.m + groups - 1) / groups, 0x7FFFFFFF);
   return launch_dependent(kern, dim3(static_cast<unsigned>(blocks)), dim3(block), 0, st, a);
 }
@@ -603,14 +622,14 @@ constexpr int64_t kColumnRows = 64;  // rows of a long row's chunk, at least
 int64_t long_chunk(int64_t m) { return std::max<int64_t>(kColumnRows, (m + 511) / 512); }
 int64_t grad_blocks(const NormGradArgs& a, NormShape s) {
   if (!s.tpr) return (a.m + long_chunk(a.m) - 1) / long_chunk(a.m);
-  const int groups = kNormThreads / s.tpr;
+  const int groups = norm_block(s.tpr, kNormThreads) / s.tpr;
   return std::min<int64_t>((a.m + groups - 1) / groups, num_sms());
 }
 
 template <int TYPE>
 cudaError_t backward(const NormGradArgs& a, float* parts, cudaStream_t st) {
   const int es = type_bytes(TYPE);
-  const NormShape s = backward_shape(a.m, a.k, TYPE);
+  const NormShape s = backward_shape(a.k, TYPE);
   const bool want = a.dw || a.db;
   const int64_t blocks = grad_blocks(a, s);
   cudaError_t err = cudaSuccess;
@@ -630,12 +649,13 @@ cudaError_t backward(const NormGradArgs& a, float* parts, cudaStream_t st) {
     const bool aligned = rows_on16(a.dy, a.lddy, es) && rows_on16(a.x, a.ldx, es) && (!a.r || rows_on16(a.r, a.ldr, es)) &&
                          (!a.dx || rows_on16(a.dx, a.lddx, es));
     auto kern = aligned ? by_shape<Backward<TYPE, true>::template K>(s) : by_shape<Backward<TYPE, false>::template K>(s);
-    const size_t join = 2 * sizeof(float) * kNormThreads * s.vpt * Elem<TYPE>::V;
-    const size_t smem = std::max<size_t>(join, aligned ? 3 * 16 * kNormThreads * s.vpt * norm_stages(s.vpt) : 0);
+    const int block = norm_block(s.tpr, kNormThreads);
+    const size_t join = 2 * sizeof(float) * block * s.vpt * Elem<TYPE>::V;
+    const size_t smem = std::max<size_t>(join, aligned ? 3 * 16 * block * s.vpt * norm_stages(s.tpr, s.vpt) : 0);
     err = allow_smem(reinterpret_cast<const void*>(kern), smem);
     if (err != cudaSuccess) return err;
     count_launch();
-    err = launch_dependent(kern, dim3(static_cast<unsigned>(blocks)), dim3(kNormThreads), smem, st, a, want ? parts : nullptr);
+    err = launch_dependent(kern, dim3(static_cast<unsigned>(blocks)), dim3(block), smem, st, a, want ? parts : nullptr);
   }
   if (err != cudaSuccess || !want) return err;
   count_launch();
@@ -653,7 +673,7 @@ cudaError_t launch_layer_norm(const NormArgs& a, int type, cudaStream_t st) {
 
 size_t layer_norm_grad_scratch(const NormGradArgs& a, int type) {
   if (!a.dw && !a.db) return 0;
-  return sizeof(float) * 2 * static_cast<size_t>(a.k) * grad_blocks(a, backward_shape(a.m, a.k, type));
+  return sizeof(float) * 2 * static_cast<size_t>(a.k) * grad_blocks(a, backward_shape(a.k, type));
 }
 
 cudaError_t launch_layer_norm_grad(const NormGradArgs& a, int type, void* scratch, cudaStream_t st) {

@@ -88,6 +88,44 @@ __device__ __forceinline__ void store16_any(T* p, uint4 v, int n, bool whole) {
       }
     }
 }
+// The same by a whole warp whose lanes have pieces that mostly follow each other, anywhere
+// (n = 0: a lane has none): a lane stores the 16-byte word that ends in its piece and begins in
+// that of the lane before, and single elements only at the ends.
+template <typename T>
+__device__ __forceinline__ void store16_warp(T* p, uint4 v, int n) {
+  constexpr int V = 16 / sizeof(T);
+  const int lane = threadIdx.x & 31;
+  const uint32_t at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p));
+  const int s = at & 15, head = (16 - s) / static_cast<int>(sizeof(T));  // elements up to the next boundary
+  const uint4 b = make_uint4(__shfl_up_sync(0xffffffffu, v.x, 1), __shfl_up_sync(0xffffffffu, v.y, 1),
+                             __shfl_up_sync(0xffffffffu, v.z, 1), __shfl_up_sync(0xffffffffu, v.w, 1));
+  const uint32_t before = __shfl_up_sync(0xffffffffu, n == V ? at + 16 : 1u, 1);  // (an odd address is no piece's)
+  const bool word = n >= head && (s == 0 || (lane > 0 && before == at));
+  const uint32_t words = __ballot_sync(0xffffffffu, word && s != 0);
+  if (word)
+    *reinterpret_cast<uint4*>(reinterpret_cast<char*>(p) - s) =
+        s ? shift_words16(reinterpret_cast<const void*>(static_cast<uintptr_t>(16 - s)), Words{b, v}) : v;
+  const bool tail = lane < 31 && (words >> (lane + 1) & 1);  // the next lane stores what is behind the boundary
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    if (e >= n || (e < head ? word : tail)) continue;
+    if (sizeof(T) == 4) {
+      reinterpret_cast<uint32_t*>(p)[e] = w[e & 3];
+    } else {
+      reinterpret_cast<uint16_t*>(p)[e] = static_cast<uint16_t>(w[e >> 1 & 3] >> (16 * (e & 1)));
+    }
+  }
+}
+// By the warp: rows on 16-byte boundaries, of which only a row's last piece is short, or any.
+template <bool ALIGNED, typename T>
+__device__ __forceinline__ void store_piece(T* p, uint4 v, int n) {
+  if (!ALIGNED) {
+    store16_warp(p, v, n);
+  } else if (n > 0) {
+    store16_any(p, v, n, n >= static_cast<int>(16 / sizeof(T)));
+  }
+}
 // A piece of which the first n elements are there; rows on 16-byte boundaries (ALIGNED)
 // or anywhere.  Where n is short, the rest are zeros.
 template <bool ALIGNED, bool FIXED = true, typename T>
