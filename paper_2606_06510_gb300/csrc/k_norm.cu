@@ -82,40 +82,152 @@ __device__ __forceinline__ void unpack2(uint4 v, Two (&t)[Elem<TYPE>::V / 2]) {
 }
 
 // ---------------------------------------------------------------------------
-// Forward.  TPR threads to a row, VPT 16-byte pieces of it to a thread: up to 16 values, two
-// to an instruction (with 32 of them the row's work was longer than its way from memory).
+// Rows on their way through shared memory (cp.async): each thread fetches its own 16-byte
+// pieces of a row that is worked on later and reads them then, so no barrier is wanted.  Rows
+// off the 16-byte grid come as the aligned words around them: a thread fetches the one in
+// which its piece begins, and the one after it is the next lane's; the last lane of a warp,
+// and of the row, fetches that too.
 // ---------------------------------------------------------------------------
-constexpr int norm_block(int tpr, int least) { return tpr < least ? least : tpr; }
+__device__ __forceinline__ void fetch_async(uint32_t to, const void* from, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void fetch_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void fetch_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
+}
 
-template <int TYPE, int TPR, int VPT, bool ALIGNED>
-__global__ void __launch_bounds__(norm_block(TPR, 256)) norm_kernel(NormArgs a) {
+// A thread's pieces of one row, VPT of them, TPR pieces apart, t its number among the row's
+// threads; `at` is the memory of a tensor's rows in one stage.
+template <int TYPE, int TPR, int VPT, int BLOCK, bool ALIGNED>
+struct Pieces {
   using X = Elem<TYPE>;
   using T = typename X::T;
-  constexpr int V = X::V, H = V / 2, kGroups = norm_block(TPR, 256) / TPR;
+  static constexpr int V = X::V, kWords = BLOCK + (ALIGNED ? 0 : BLOCK / 32), kBytes = VPT * kWords * 16;
+  const T *base, *end;
+  int64_t k;
+  int t;
+  __device__ __forceinline__ int64_t col(int i) const { return static_cast<int64_t>(t + i * TPR) * V; }
+  __device__ __forceinline__ int there(int i) const {
+    return static_cast<int>(max(int64_t(0), min(int64_t(V), k - col(i))));
+  }
+  static __device__ __forceinline__ uint8_t* slot(uint8_t* at, int i) { return at + (i * kWords + threadIdx.x) * 16; }
+  static __device__ __forceinline__ uint8_t* after(uint8_t* at, int i) {
+    return (threadIdx.x & 31) == 31 ? at + (i * kWords + BLOCK + (threadIdx.x >> 5)) * 16 : slot(at, i) + 16;
+  }
+  __device__ __forceinline__ void fetch(uint8_t* at, const T* row) const {
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const int n = there(i);
+      if (ALIGNED) {  // (zeros past the row's end)
+        fetch_async(smem_u32(slot(at, i)), row + (n ? col(i) : 0), n * sizeof(T));
+      } else if (n) {
+        const T* p = row + col(i);
+        const int s = static_cast<int>(reinterpret_cast<uintptr_t>(p) & 15);
+        const char* word = reinterpret_cast<const char*>(p) - s;
+        const int64_t left = reinterpret_cast<const char*>(end) - word;
+        if (word >= reinterpret_cast<const char*>(base)) {
+          fetch_async(smem_u32(slot(at, i)), word, static_cast<int>(min(int64_t(16), left)));
+        } else {  // the tensor's first word is not all its own
+          for (int e = 0; e < n && s + e * static_cast<int>(sizeof(T)) < 16; ++e) reinterpret_cast<T*>(slot(at, i) + s)[e] = p[e];
+        }
+        if (s + n * static_cast<int>(sizeof(T)) > 16 && ((threadIdx.x & 31) == 31 || col(i) + V >= k))
+          fetch_async(smem_u32(after(at, i)), word + 16, static_cast<int>(min(int64_t(16), left - 16)));
+      }
+    }
+  }
+  // (Other lanes' words: between the wait for them and this, and between this and the next fetch, a
+  // warp barrier.)
+  __device__ __forceinline__ uint4 read(uint8_t* at, const T* row, int i) const {
+    if (ALIGNED) return *reinterpret_cast<const uint4*>(slot(at, i));
+    const int n = there(i);
+    if (n == 0) return make_uint4(0, 0, 0, 0);
+    const uintptr_t s = reinterpret_cast<uintptr_t>(row + col(i)) & 15;
+    Words w;
+    w.a = *reinterpret_cast<const uint4*>(slot(at, i));
+    w.b = s ? *reinterpret_cast<const uint4*>(after(at, i)) : w.a;
+    uint4 v = shift_words16(reinterpret_cast<const void*>(s), w);
+    if (n < V) {
+      uint32_t* q = &v.x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int kept = n * static_cast<int>(sizeof(T)) - 4 * e;  // bytes of this word
+        (&v.x)[e] = kept >= 4 ? q[e] : kept <= 0 ? 0u : q[e] & 0xFFFFu;
+      }
+    }
+    return v;
+  }
+  static __device__ __forceinline__ void meet() {
+    if (!ALIGNED) __syncwarp();
+  }
+};
+constexpr int norm_block(int tpr, int least) { return tpr < least ? least : tpr; }
+constexpr int norm_stages(int bytes, int room) { return room / bytes < 1 ? 1 : room / bytes > 6 ? 6 : room / bytes; }
+
+// ---------------------------------------------------------------------------
+// Forward.  TPR threads to a row, VPT 16-byte pieces of it to a thread: up to 16 values, two
+// to an instruction.  Groups of threads walk over rows, the next ones on their way meanwhile.
+// (A block to each few rows, loaded when it came to them, took 254 us for 65536×1024 f32.)
+// ---------------------------------------------------------------------------
+constexpr int kForwardThreads = 256;
+constexpr int forward_room(int block) { return block == 256 ? 64 * 1024 : 200 * 1024; }  // three blocks an SM, or one
+template <int TYPE, int TPR, int VPT, bool ALIGNED>
+constexpr int forward_stages() {
+  constexpr int block = norm_block(TPR, kForwardThreads);
+  return norm_stages(Pieces<TYPE, TPR, VPT, block, ALIGNED>::kBytes, forward_room(block));
+}
+
+template <int TYPE, int TPR, int VPT, bool ALIGNED>
+__global__ void __launch_bounds__(norm_block(TPR, kForwardThreads), norm_block(TPR, kForwardThreads) == 256 ? 3 : 1)
+    norm_kernel(NormArgs a) {
+  using X = Elem<TYPE>;
+  using T = typename X::T;
+  constexpr int V = X::V, H = V / 2, kBlock = norm_block(TPR, kForwardThreads), kGroups = kBlock / TPR;
+  using Rows = Pieces<TYPE, TPR, VPT, kBlock, ALIGNED>;
+  constexpr int STAGES = forward_stages<TYPE, TPR, VPT, ALIGNED>();
+  constexpr bool KEEP = TPR < 1024;  // weights in registers
   __shared__ float exchange[kGroups][2 * TPR / 32];
+  extern __shared__ __align__(16) uint8_t norm_smem[];
   pdl_trigger();
   pdl_wait();
   const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
   const T* src = static_cast<const T*>(a.x);
-  const T* end = src + (a.m - 1) * a.ldx + a.k;
+  const Rows in{src, src + (a.m - 1) * a.ldx + a.k, a.k, t};
   const float inv_k = 1.f / static_cast<float>(a.k);
   RowSum<TPR, 1> rows{exchange[group], group, 0};
-  auto col = [&](int i) { return static_cast<int64_t>(t + i * TPR) * V; };
-  auto there = [&](int i) { return static_cast<int>(max(int64_t(0), min(int64_t(V), a.k - col(i)))); };
-  for (int64_t r = static_cast<int64_t>(blockIdx.x) * kGroups + group; r < a.m; r += static_cast<int64_t>(gridDim.x) * kGroups) {
-    uint4 raw[VPT];
+  const int64_t stride = static_cast<int64_t>(gridDim.x) * kGroups, first = static_cast<int64_t>(blockIdx.x) * kGroups + group;
+  auto fetch = [&](int64_t r, int stage) {
+    if (r < a.m) in.fetch(norm_smem + stage * Rows::kBytes, src + r * a.ldx);
+    fetch_commit();
+  };
+#pragma unroll
+  for (int s = 0; s < STAGES; ++s) fetch(first + s * stride, s);
+  const Two one = two(1.f, 1.f), zero = two(0.f, 0.f);
+  auto vector = [&](const void* p, int i, Two none, Two (&to)[H]) {
+    float f[V];
+    if (p && in.there(i)) load_vector<TYPE>(p, a.wtype, in.col(i), in.there(i), a.k, f);
+#pragma unroll
+    for (int e = 0; e < H; ++e) to[e] = p && in.there(i) ? two(f[2 * e], f[2 * e + 1]) : none;
+  };
+  Two w[KEEP ? VPT : 1][H], b[KEEP ? VPT : 1][H];
+  if (KEEP) {
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) vector(a.w, i, one, w[KEEP ? i : 0]), vector(a.b, i, zero, b[KEEP ? i : 0]);
+  }
+  int stage = 0;
+  for (int64_t r = first; r < a.m; r += stride) {
+    fetch_wait<STAGES - 1>();
+    Rows::meet();
+    Two x[VPT][H], s = zero;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      raw[i] = make_uint4(0, 0, 0, 0);
-      if (there(i)) raw[i] = load_piece<ALIGNED>(src + r * a.ldx + col(i), src, end, there(i));
-    }
-    Two x[VPT][H], s = two(0.f, 0.f);
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      unpack2<TYPE>(raw[i], x[i]);  // (zeros past the row's end)
+      unpack2<TYPE>(in.read(norm_smem + stage * Rows::kBytes, src + r * a.ldx, i), x[i]);  // (zeros past the row's end)
 #pragma unroll
       for (int e = 0; e < H; ++e) s = s + x[i][e];
     }
+    Rows::meet();
+    fetch(r + STAGES * stride, stage);
+    stage = stage + 1 == STAGES ? 0 : stage + 1;
     float mean = 0.f, sum[1];
     if (a.center) {
       const float2 p = both(s);
@@ -124,10 +236,10 @@ __global__ void __launch_bounds__(norm_block(TPR, 256)) norm_kernel(NormArgs a) 
       mean = sum[0] * inv_k;
     }
     const Two less = two(-mean, -mean);
-    s = two(0.f, 0.f);
+    s = zero;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      const int n = there(i);
+      const int n = in.there(i);
 #pragma unroll
       for (int e = 0; e < H; ++e) {
         x[i][e] = x[i][e] + less;
@@ -149,28 +261,19 @@ __global__ void __launch_bounds__(norm_block(TPR, 256)) norm_kernel(NormArgs a) 
     const Two scale = two(rstd, rstd);
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      const int n = there(i);
+      const int n = in.there(i);
       float f[V];
-#pragma unroll
-      for (int e = 0; e < H; ++e) x[i][e] = x[i][e] * scale;
-      if (a.w && n) {
-        load_vector<TYPE>(a.w, a.wtype, col(i), n, a.k, f);
-#pragma unroll
-        for (int e = 0; e < H; ++e) x[i][e] = x[i][e] * two(f[2 * e], f[2 * e + 1]);
-      }
-      if (a.b && n) {
-        load_vector<TYPE>(a.b, a.wtype, col(i), n, a.k, f);
-#pragma unroll
-        for (int e = 0; e < H; ++e) x[i][e] = x[i][e] + two(f[2 * e], f[2 * e + 1]);
-      }
+      Two wi[H], bi[H];
+      if (!KEEP) vector(a.w, i, one, wi), vector(a.b, i, zero, bi);
 #pragma unroll
       for (int e = 0; e < H; ++e) {
-        const float2 q = both(x[i][e]);
+        const float2 q = both(fma(x[i][e] * scale, KEEP ? w[KEEP ? i : 0][e] : wi[e], KEEP ? b[KEEP ? i : 0][e] : bi[e]));
         f[2 * e] = q.x, f[2 * e + 1] = q.y;
       }
-      store_piece<ALIGNED>(static_cast<T*>(a.y) + r * a.ldy + (n ? col(i) : 0), X::pack(f), n);
+      store_piece<ALIGNED>(static_cast<T*>(a.y) + r * a.ldy + (n ? in.col(i) : 0), X::pack(f), n);
     }
   }
+  fetch_wait<0>();
 }
 
 // Rows too long for registers: a block to a row, which it reads again for each of the
@@ -233,29 +336,23 @@ __global__ void __launch_bounds__(kNormThreads) norm_long_kernel(NormArgs a) {
 // theirs in shared memory, in order, into the block's row of `parts`, and
 // join_parts_kernel adds up the blocks'.
 //
-// Memory bounds it.  Rows on 16-byte boundaries go through shared memory, the next
-// STAGES of them on their way (cp.async) while one is worked on: each thread fetches
-// and reads its own pieces, so that no barrier is wanted, and reads them a second time
-// for dx instead of keeping them.  Other rows, and ones of which two do not fit, are
-// loaded to registers.
+// Memory bounds it.  A thread's 16 values of a row stay in registers between the sums and dx;
+// the 1024 threads of rows over 8192 have registers for the columns' sums alone and form them
+// a second time.
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ void fetch_async(uint32_t to, const void* from, int bytes) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
-}
-constexpr int kStagedBytes = 200 * 1024;  // of a block's 227 KB
-constexpr int norm_stages(int tpr, int vpt) {
-  const int n = kStagedBytes / (3 * vpt * 16 * norm_block(tpr, kNormThreads));
-  return n < 4 ? n : 4;
+template <int TYPE, int TPR, int VPT, bool ALIGNED>
+constexpr int backward_stages() {
+  return norm_stages(3 * Pieces<TYPE, TPR, VPT, norm_block(TPR, kNormThreads), ALIGNED>::kBytes, 208 * 1024);
 }
 
-// A thread's 16 values of a row stay in registers between the sums and dx; the 1024 threads of
-// rows over 8192 have registers for the columns' sums alone and form them a second time.
-template <int TYPE, int TPR, int VPT, int STAGES>
+template <int TYPE, int TPR, int VPT, bool ALIGNED>
 __global__ void __launch_bounds__(norm_block(TPR, kNormThreads), 1) norm_grad_kernel(NormGradArgs a, float* __restrict__ parts) {
   using X = Elem<TYPE>;
   using T = typename X::T;
   constexpr int V = X::V, H = V / 2, kBlock = norm_block(TPR, kNormThreads), kGroups = kBlock / TPR;
-  constexpr bool STAGED = STAGES > 0, KEEP = TPR < 1024;
+  using Rows = Pieces<TYPE, TPR, VPT, kBlock, ALIGNED>;
+  constexpr int STAGES = backward_stages<TYPE, TPR, VPT, ALIGNED>();
+  constexpr bool KEEP = TPR < 1024;
   __shared__ float exchange[kGroups][4 * TPR / 32];
   // The rows' pieces, and after them the groups' columns of dw and db.
   extern __shared__ __align__(16) uint8_t norm_smem[];
@@ -264,13 +361,12 @@ __global__ void __launch_bounds__(norm_block(TPR, kNormThreads), 1) norm_grad_ke
   pdl_wait();
   const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
   const T *dy = static_cast<const T*>(a.dy), *x = static_cast<const T*>(a.x), *res = static_cast<const T*>(a.r);
-  const T *dy_end = dy + (a.m - 1) * a.lddy + a.k, *x_end = x + (a.m - 1) * a.ldx + a.k,
-          *r_end = res + (a.m - 1) * a.ldr + a.k;
+  const Rows in_dy{dy, dy + (a.m - 1) * a.lddy + a.k, a.k, t}, in_x{x, x + (a.m - 1) * a.ldx + a.k, a.k, t},
+      in_r{res, res + (a.m - 1) * a.ldr + a.k, a.k, t};
   const float inv_k = 1.f / static_cast<float>(a.k);
   RowSum<TPR, 2> rows{exchange[group], group, 0};
-  // This thread's columns of a row: pieces from col(i) on, there(i) of their values.
-  auto col = [&](int i) { return static_cast<int64_t>(t + i * TPR) * V; };
-  auto there = [&](int i) { return static_cast<int>(max(int64_t(0), min(int64_t(V), a.k - col(i)))); };
+  auto col = [&](int i) { return in_x.col(i); };
+  auto there = [&](int i) { return in_x.there(i); };
   const Two zero = two(0.f, 0.f), one = two(1.f, 1.f);
   Two dw[VPT][H], db[VPT][H], w[KEEP ? VPT : 1][H];
   auto weights = [&](int i, Two (&to)[H]) {
@@ -286,27 +382,17 @@ __global__ void __launch_bounds__(norm_block(TPR, kNormThreads), 1) norm_grad_ke
     for (int e = 0; e < H; ++e) dw[i][e] = db[i][e] = zero;
   }
   const int64_t stride = static_cast<int64_t>(gridDim.x) * kGroups, first = static_cast<int64_t>(blockIdx.x) * kGroups + group;
-  uint4 rd[VPT], rx[VPT], rr[VPT];  // (not staged)
-  auto piece = [&](int stage, int which, int i) {
-    return norm_smem + (((stage * 3 + which) * VPT + i) * kBlock + threadIdx.x) * 16;
-  };
+  auto memory = [&](int stage, int which) { return norm_smem + (stage * 3 + which) * Rows::kBytes; };
   auto fetch = [&](int64_t r, int stage) {
     if (r < a.m) {
-#pragma unroll
-      for (int i = 0; i < VPT; ++i) {
-        const int bytes = there(i) * sizeof(T);
-        const int64_t at = bytes ? col(i) : 0;
-        fetch_async(smem_u32(piece(stage, 0, i)), dy + r * a.lddy + at, bytes);
-        fetch_async(smem_u32(piece(stage, 1, i)), x + r * a.ldx + at, bytes);
-        if (res) fetch_async(smem_u32(piece(stage, 2, i)), res + r * a.ldr + at, bytes);
-      }
+      in_dy.fetch(memory(stage, 0), dy + r * a.lddy);
+      in_x.fetch(memory(stage, 1), x + r * a.ldx);
+      if (res) in_r.fetch(memory(stage, 2), res + r * a.ldr);
     }
-    asm volatile("cp.async.commit_group;" ::: "memory");
+    fetch_commit();
   };
-  if constexpr (STAGED) {
 #pragma unroll
-    for (int s = 0; s < STAGES; ++s) fetch(first + s * stride, s);
-  }
+  for (int s = 0; s < STAGES; ++s) fetch(first + s * stride, s);
   float mean = 0.f, rstd = 0.f;
   auto statistics = [&](int64_t r) {
     if (r < a.m) mean = a.mean ? __ldg(a.mean + r) : 0.f, rstd = __ldg(a.rstd + r);
@@ -314,26 +400,14 @@ __global__ void __launch_bounds__(norm_block(TPR, kNormThreads), 1) norm_grad_ke
   statistics(first);
   int stage = 0;
   for (int64_t r = first; r < a.m; r += stride) {
-    if constexpr (STAGED) {
-      asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
-    } else {
-#pragma unroll
-      for (int i = 0; i < VPT; ++i) {
-        const int n = there(i);
-        rd[i] = rx[i] = rr[i] = make_uint4(0, 0, 0, 0);
-        if (n > 0) {
-          rd[i] = load_piece<false>(dy + r * a.lddy + col(i), dy, dy_end, n);
-          rx[i] = load_piece<false>(x + r * a.ldx + col(i), x, x_end, n);
-          if (res) rr[i] = load_piece<false, false>(res + r * a.ldr + col(i), res, r_end, n);
-        }
-      }
-    }
+    fetch_wait<STAGES - 1>();
+    Rows::meet();
     const Two less = two(-mean, -mean), scale = two(rstd, rstd);
     // dy, g = dy·w and x̂ of a piece.  (Past the row's end dy is zero, and whatever x̂ is there
     // counts for nothing.)
     auto values = [&](int i, Two (&d)[H], Two (&g)[H], Two (&h)[H]) {
-      unpack2<TYPE>(STAGED ? *reinterpret_cast<const uint4*>(piece(stage, 0, i)) : rd[i], d);
-      unpack2<TYPE>(STAGED ? *reinterpret_cast<const uint4*>(piece(stage, 1, i)) : rx[i], h);
+      unpack2<TYPE>(in_dy.read(memory(stage, 0), dy + r * a.lddy, i), d);
+      unpack2<TYPE>(in_x.read(memory(stage, 1), x + r * a.ldx, i), h);
       Two own[H];
       if (!KEEP) weights(i, own);
 #pragma unroll
@@ -374,7 +448,7 @@ __global__ void __launch_bounds__(norm_block(TPR, kNormThreads), 1) norm_grad_ke
         for (int e = 0; e < H; ++e) d[e] = fma(h[e], along2, fma(g[e], scale, level2));
         if (res) {
           Two o[H];
-          unpack2<TYPE>(STAGED ? *reinterpret_cast<const uint4*>(piece(stage, 2, i)) : rr[i], o);
+          unpack2<TYPE>(in_r.read(memory(stage, 2), res + r * a.ldr, i), o);
 #pragma unroll
           for (int e = 0; e < H; ++e) d[e] = d[e] + o[e];
         }
@@ -384,19 +458,16 @@ __global__ void __launch_bounds__(norm_block(TPR, kNormThreads), 1) norm_grad_ke
           const float2 f = both(d[e]);
           y[2 * e] = f.x, y[2 * e + 1] = f.y;
         }
-        store_piece<STAGED>(static_cast<T*>(a.dx) + r * a.lddx + (n ? col(i) : 0), X::pack(y), n);
+        store_piece<ALIGNED>(static_cast<T*>(a.dx) + r * a.lddx + (n ? col(i) : 0), X::pack(y), n);
       }
     }
     statistics(r + stride);
-    if constexpr (STAGED) {
-      fetch(r + STAGES * stride, stage);
-      stage = stage + 1 == STAGES ? 0 : stage + 1;
-    }
+    Rows::meet();
+    fetch(r + STAGES * stride, stage);
+    stage = stage + 1 == STAGES ? 0 : stage + 1;
   }
-  if constexpr (STAGED) {
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
-    __syncthreads();  // the pieces' memory becomes the columns'
-  }
+  fetch_wait<0>();
+  __syncthreads();  // the pieces' memory becomes the columns'
   if (!parts) return;
   // The groups' columns in shared memory, dw's and then db's, and their sums in the groups' order.
   constexpr int kCols = TPR * VPT * V;
@@ -585,19 +656,35 @@ auto by_shape(NormShape s) {  // the kernel K of these threads and pieces
                         : by_pieces<K, 1024>(s.vpt);
 }
 // (Of 4 pieces, those of 16-bit rows are never asked for.)
+template <typename Args>
+struct Kernel {
+  Args kernel;
+  int block;
+  size_t smem;
+};
+using ForwardKernel = Kernel<void (*)(NormArgs)>;
+using BackwardKernel = Kernel<void (*)(NormGradArgs, float*)>;
 template <int TYPE, bool ALIGNED>
 struct Forward {
   template <int TPR, int VPT>
   struct K {
-    static auto f() { return &norm_kernel<TYPE, TPR, VPT * Elem<TYPE>::V <= 16 ? VPT : 2, ALIGNED>; }
+    static ForwardKernel f() {
+      constexpr int kVpt = VPT * Elem<TYPE>::V <= 16 ? VPT : 2, kBlock = norm_block(TPR, kForwardThreads);
+      return {norm_kernel<TYPE, TPR, kVpt, ALIGNED>, kBlock,
+              Pieces<TYPE, TPR, kVpt, kBlock, ALIGNED>::kBytes * forward_stages<TYPE, TPR, kVpt, ALIGNED>()};
+    }
   };
 };
 template <int TYPE, bool ALIGNED>
 struct Backward {
   template <int TPR, int VPT>
   struct K {
-    static constexpr int kVpt = VPT * Elem<TYPE>::V <= 16 ? VPT : 2;
-    static auto f() { return &norm_grad_kernel<TYPE, TPR, kVpt, ALIGNED ? norm_stages(TPR, kVpt) : 0>; }
+    static BackwardKernel f() {
+      constexpr int kVpt = VPT * Elem<TYPE>::V <= 16 ? VPT : 2, kBlock = norm_block(TPR, kNormThreads);
+      constexpr size_t columns = 2 * sizeof(float) * kBlock * kVpt * Elem<TYPE>::V;
+      constexpr size_t pieces = 3 * Pieces<TYPE, TPR, kVpt, kBlock, ALIGNED>::kBytes * backward_stages<TYPE, TPR, kVpt, ALIGNED>();
+      return {norm_grad_kernel<TYPE, TPR, kVpt, ALIGNED>, kBlock, pieces > columns ? pieces : columns};
+    }
   };
 };
 
@@ -611,10 +698,12 @@ cudaError_t forward(const NormArgs& a, cudaStream_t st) {
     return launch_dependent(norm_long_kernel<TYPE>, dim3(blocks), dim3(kNormThreads), 0, st, a);
   }
   const bool aligned = rows_on16(a.x, a.ldx, es) && rows_on16(a.y, a.ldy, es);
-  auto kern = aligned ? by_shape<Forward<TYPE, true>::template K>(s) : by_shape<Forward<TYPE, false>::template K>(s);
-  const int block = norm_block(s.tpr, 256), groups = block / s.tpr;
-  const int64_t blocks = std::min<int64_t>((a.m + groups - 1) / groups, 0x7FFFFFFF);
-  return launch_dependent(kern, dim3(static_cast<unsigned>(blocks)), dim3(block), 0, st, a);
+  const ForwardKernel f = aligned ? by_shape<Forward<TYPE, true>::template K>(s) : by_shape<Forward<TYPE, false>::template K>(s);
+  const cudaError_t err = allow_smem(reinterpret_cast<const void*>(f.kernel), f.smem);
+  if (err != cudaSuccess) return err;
+  const int groups = f.block / s.tpr;
+  const int64_t blocks = std::min<int64_t>((a.m + groups - 1) / groups, (f.block == 256 ? 3 : 1) * static_cast<int64_t>(num_sms()));
+  return launch_dependent(f.kernel, dim3(static_cast<unsigned>(blocks)), dim3(f.block), f.smem, st, a);
 }
 
 constexpr int64_t kColumnRows = 64;  // rows of a long row's chunk, at least
@@ -648,14 +737,11 @@ cudaError_t backward(const NormGradArgs& a, float* parts, cudaStream_t st) {
   } else {
     const bool aligned = rows_on16(a.dy, a.lddy, es) && rows_on16(a.x, a.ldx, es) && (!a.r || rows_on16(a.r, a.ldr, es)) &&
                          (!a.dx || rows_on16(a.dx, a.lddx, es));
-    auto kern = aligned ? by_shape<Backward<TYPE, true>::template K>(s) : by_shape<Backward<TYPE, false>::template K>(s);
-    const int block = norm_block(s.tpr, kNormThreads);
-    const size_t join = 2 * sizeof(float) * block * s.vpt * Elem<TYPE>::V;
-    const size_t smem = std::max<size_t>(join, aligned ? 3 * 16 * block * s.vpt * norm_stages(s.tpr, s.vpt) : 0);
-    err = allow_smem(reinterpret_cast<const void*>(kern), smem);
+    const BackwardKernel f = aligned ? by_shape<Backward<TYPE, true>::template K>(s) : by_shape<Backward<TYPE, false>::template K>(s);
+    err = allow_smem(reinterpret_cast<const void*>(f.kernel), f.smem);
     if (err != cudaSuccess) return err;
     count_launch();
-    err = launch_dependent(kern, dim3(static_cast<unsigned>(blocks)), dim3(block), smem, st, a, want ? parts : nullptr);
+    err = launch_dependent(f.kernel, dim3(static_cast<unsigned>(blocks)), dim3(f.block), f.smem, st, a, want ? parts : nullptr);
   }
   if (err != cudaSuccess || !want) return err;
   count_launch();
