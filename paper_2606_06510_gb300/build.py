@@ -20,7 +20,7 @@ SOURCES = ["oz2_api.cu", "k_scan.cu", "k_deconstruct.cu", "k_gemm.cu", "k_crt.cu
            "k_fused.cu", "k_short.cu", "k_skinny.cu",
            "oz2_noalloc.cu",
            "oz2_layers.cu", "k_linear.cu", "k_linear_rows.cu", "k_linear_aux.cu", "k_adamw.cu",
-           "oz2_lm.cu", "k_embed.cu", "k_norm.cu", "k_head.cu"]
+           "oz2_lm.cu", "k_embed.cu", "k_norm.cu", "k_norm_grad.cu", "k_head.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-O2",
          "--expt-relaxed-constexpr", "-DNDEBUG"]

@@ -35,7 +35,8 @@ def view(t, how):
 # Every number of threads and pieces a row has, with rows that end inside a piece.
 SHAPES = [(1, 1), (1, 16), (3, 7), (7, 64), (5, 250), (9, 512), (40, 777), (65, 1024), (33, 1031), (130, 2048), (4, 4000),
           (64, 4096), (3, 8192), (2, 12345), (2, 16384), (3, 16392), (2, 20001), (400, 100), (700, 1000), (400, 2056),
-          (330, 4104), (320, 9000), (310, 16384), (309, 17000), (5000, 40)]
+          (330, 4104), (320, 9000), (310, 16384), (309, 17000), (5000, 40),
+          (1001, 64), (1001, 63), (1003, 128), (2005, 24), (777, 33), (1500, 5), (333, 9001), (200, 16383)]
 
 
 def inputs(m, k, dt, how, affine, center, seed):
