@@ -613,20 +613,18 @@ __global__ void __launch_bounds__(32 * kListWarps)
     }
     entries[row * top + i] = e;
   }
-  // The offsets, 32 groups at a time, by way of shared memory: a group's are beside each other.
-  int turn = 0;
+  // The offsets, 32 groups at a time: the warp walks over its entries there once.  By way of
+  // shared memory: a group's are beside each other.
+  int turn = 0, next = 0;
   for (int64_t q0 = 0; q0 < groups1; q0 += 32, turn ^= 1) {
-    const int64_t q = q0 + lane;
-    const Key first = q + 1 < groups1 ? static_cast<Key>(q * kHeadGroup) << bits : kBad;
-    int at = 0, left = top;  // the first one of these columns
-    while (left > 0) {
-      const int half = left >> 1;
-      if (keys[at + half] < first) {
-        at += half + 1;
-        left -= half + 1;
-      } else {
-        left = half;
-      }
+    int at = next;
+    while (next < top) {
+      const Key key = keys[next];
+      if (key >= kBad) break;  // (as the offset of what is past the last group: of the ones that are rows of w)
+      const int64_t group = static_cast<int64_t>(key >> bits) / kHeadGroup - q0;
+      if (group >= 32) break;
+      at += group < lane;
+      ++next;
     }
     offsets_s[turn][lane][warp] = static_cast<uint16_t>(at);
     __syncthreads();  // (the other set is written again behind the next one)
