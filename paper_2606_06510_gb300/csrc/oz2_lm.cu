@@ -272,6 +272,7 @@ int oz2_layer_norm(int64_t m, int64_t k, int type, const void* d_X, int64_t ldx,
   if (ldx < std::max<int64_t>(1, k) || ldy < std::max<int64_t>(1, k)) return OZ2_ERR_INVALID_ARG;
   if (too_large(m, k, 0)) return OZ2_ERR_UNSUPPORTED;
   if (m == 0 || k == 0) return OZ2_OK;
+  if (d_Y == d_X && ldy != ldx && m > 1) return OZ2_ERR_INVALID_ARG;
   const int es = type_bytes(type), wb = type_bytes(wtype);
   if (!d_X || !d_Y || !on(d_X, es) || !on(d_Y, es) || (d_w && !on(d_w, wb)) || (d_b && !on(d_b, wb)) || !on(d_mean, 4) ||
       !on(d_rstd, 4))
@@ -291,6 +292,7 @@ int oz2_layer_norm_grad(int64_t m, int64_t k, int type, const void* d_dY, int64_
   if (too_large(m, k, 0)) return OZ2_ERR_UNSUPPORTED;
   const int es = type_bytes(type);
   if (!on(d_dw, 4) || !on(d_db, 4) || !on(d_dX, es)) return OZ2_ERR_INVALID_ARG;
+  if (d_R && d_R == d_dX && ldr != lddx && m > 1) return OZ2_ERR_INVALID_ARG;
   if ((!d_dX && !d_dw && !d_db) || k == 0) return OZ2_OK;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool accumulate = (flags & OZ2_GRAD_ACCUMULATE) != 0;

@@ -77,7 +77,7 @@ def norm(oz, m=4, k=8, type=BF16, X=16, ldx=8, w=16, b=16, wt=BF16, eps=1e-5, ce
 @pytest.mark.parametrize("bad", [
     dict(m=-1), dict(k=-1), dict(type=E4M3), dict(wt=F16), dict(wt=E4M3), dict(eps=-1.0), dict(eps=NAN), dict(ldx=7),
     dict(ldy=7), dict(X=N), dict(Y=N), dict(X=17), dict(Y=17), dict(w=17), dict(b=17), dict(wt=F32, w=18), dict(mean=18),
-    dict(rstd=18)])
+    dict(rstd=18), dict(ldy=9)])
 def test_norm_refuses(oz, bad):
     assert norm(oz, **bad) == -1
 
@@ -95,7 +95,7 @@ def norm_grad(oz, m=4, k=8, type=BF16, dY=16, lddy=8, X=16, ldx=8, mean=16, rstd
 @pytest.mark.parametrize("bad", [
     dict(m=-1), dict(k=-1), dict(type=E4M3), dict(wt=F16), dict(flags=2), dict(lddy=7), dict(ldx=7), dict(ldr=7),
     dict(lddx=7), dict(dY=N), dict(X=N), dict(rstd=N), dict(dY=17), dict(X=17), dict(R=17), dict(dX=17), dict(dw=18),
-    dict(db=18), dict(mean=18), dict(rstd=18), dict(w=17)])
+    dict(db=18), dict(mean=18), dict(rstd=18), dict(w=17), dict(lddx=9)])
 def test_norm_grad_refuses(oz, bad):
     assert norm_grad(oz, **bad) == -1
 
