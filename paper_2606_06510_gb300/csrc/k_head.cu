@@ -549,9 +549,10 @@ __device__ __forceinline__ void sort_64(Key* keys, int at, int size, bool first,
 // enough (its shuffles and comparisons are half).
 template <typename Key>
 __global__ void __launch_bounds__(32 * kListWarps)
-    head_targets_kernel(int64_t m, int64_t n, HeadTargets t, int padded, int bits, int64_t groups1, int64_t ld_offsets,
-                        int2* entries, uint16_t* offsets, HeadRow* rows, HeadTerms terms) {
-  extern __shared__ unsigned long long list_smem[];  // the warps' keys, then the teacher's logits
+    head_targets_kernel(int64_t m, int64_t n, HeadTargets t, int padded, int bits, int table, int64_t groups1,
+                        int64_t ld_offsets, int2* entries, uint16_t* offsets, HeadRow* rows, HeadTerms terms) {
+  // The warps' keys, then the teacher's logits, and `table` bytes on (0: it does not fit) the offsets.
+  extern __shared__ __align__(16) unsigned long long list_smem[];
   constexpr Key kNone = ~Key(0), kBad = kNone - 1;   // not there; no row of w
   pdl_trigger();
   pdl_wait();
@@ -612,6 +613,23 @@ __global__ void __launch_bounds__(32 * kListWarps)
       e.y = rows ? __float_as_int(expf(logits[place] - most) / sum) : place;
     }
     entries[row * top + i] = e;
+  }
+  // The offsets, all of them in shared memory where they fit: between two entries' groups they are
+  // the number of entries before.
+  if (table) {
+    uint16_t* mine = reinterpret_cast<uint16_t*>(reinterpret_cast<uint8_t*>(list_smem) + table) + warp;
+    for (int i = lane; i <= top; i += 32) {
+      if (i > 0 && keys[i - 1] >= kBad) continue;
+      const int before = i > 0 ? static_cast<int>(static_cast<int64_t>(keys[i - 1] >> bits) / kHeadGroup) : -1;
+      const int last = i < top && keys[i] < kBad ? static_cast<int>(static_cast<int64_t>(keys[i] >> bits) / kHeadGroup)
+                                                 : static_cast<int>(groups1) - 1;
+      for (int q = before + 1; q <= last; ++q) mine[q * kListWarps] = static_cast<uint16_t>(i);
+    }
+    __syncthreads();
+    const uint4* from = reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(list_smem) + table);
+    for (int i = threadIdx.x; i < 2 * groups1; i += 32 * kListWarps)  // (a group's 16 tokens: 32 bytes)
+      *reinterpret_cast<uint4*>(offsets + (i >> 1) * ld_offsets + row0 + 8 * (i & 1)) = from[i];
+    return;
   }
   // The offsets, 32 groups at a time: the warp walks over its entries there once.  By way of
   // shared memory: a group's are beside each other.
@@ -833,13 +851,16 @@ cudaError_t launch_head_targets(int64_t m, int64_t n, const HeadTargets& t, int2
   int bits = 0;
   while ((t.top - 1) >> bits) ++bits;
   const bool narrow = n < (int64_t(1) << (32 - bits)) - 1;
-  const size_t smem = kListWarps * ((narrow ? 4 : 8) * padded + (rows ? sizeof(float) * t.top : 0));
+  const size_t lists = (kListWarps * ((narrow ? 4 : 8) * padded + (rows ? sizeof(float) * t.top : 0)) + 15) / 16 * 16;
+  const size_t table = sizeof(uint16_t) * kListWarps * l.groups1;
+  const bool fits = lists + table <= 200 * 1024;
+  const size_t smem = lists + (fits ? table : 0);
   auto kern = narrow ? head_targets_kernel<uint32_t> : head_targets_kernel<unsigned long long>;
   const cudaError_t err = allow_smem(reinterpret_cast<const void*>(kern), smem);
   if (err != cudaSuccess) return err;
   count_launch();
   return launch_dependent(kern, dim3(static_cast<unsigned>((m + kListWarps - 1) / kListWarps)), dim3(32 * kListWarps), smem, st, m, n, t,
-                          padded, bits, l.groups1, l.ld_offsets, entries, offsets, rows, terms);
+                          padded, bits, fits ? static_cast<int>(lists) : 0, l.groups1, l.ld_offsets, entries, offsets, rows, terms);
 }
 
 int live_rows_maxima(int64_t m, int64_t k) {

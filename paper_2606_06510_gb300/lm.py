@@ -14,7 +14,7 @@ import ctypes
 
 import torch
 
-from .layers import GRAD_ACCUMULATE, TYPE, _ENTRIES, _done, _entry, _ld, _new
+from .layers import _EMPTY, GRAD_ACCUMULATE, TYPE, _ENTRIES, _done, _entry, _ld, _new
 
 _I64, _P, _I, _U, _F = ctypes.c_int64, ctypes.c_void_p, ctypes.c_int, ctypes.c_uint, ctypes.c_float
 GRAD_ONE_DLOSS = 0x2
@@ -40,6 +40,17 @@ SIGS = {
 # operator asks for all of a tensor's properties at once, and only where one is not as
 # expected goes to the function that says which, or finds that it does not matter.
 _device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
+_F32, _FLOATS = torch.float32, (torch.float32, torch.bfloat16, torch.float16)
+
+
+def _empty(shape, strides, dtype):
+    return torch.empty_strided(shape, strides, dtype=dtype, device="cuda")
+
+
+# A new output on the current device, of the current stream's memory.
+_fresh = _EMPTY or _empty
 
 
 def _lost(what):
@@ -82,9 +93,6 @@ def _vector(t, count, dtype, other, dev, what):
     return t.data_ptr()
 
 
-_FLOATS = (torch.float32, torch.bfloat16, torch.float16)
-
-
 def oz2_embedding(ids, table, scale=1.0, out=None, stream=None):
     """scale·table[ids] for tokens ids (m,) and a table (n, k) of float32, bfloat16 or
     float16: (m, k) of its dtype.  ids below 0 (padding) give zeros, ids of n or more NaN."""
@@ -97,9 +105,12 @@ def oz2_embedding(ids, table, scale=1.0, out=None, stream=None):
     assert ids.dtype in IDS, "ids: expected int64 or int32"
     dev = _home(table, "table")
     ip = _vector(ids, m, torch.int64, torch.int32, dev, "ids")
-    tp, ldt = _matrix(table, n, k, dt, dev, "table")
+    ldt, one = table.stride()
+    if one != 1 or ldt < k or ldt < 1:
+        ldt = _odd(table, n, k, dt, dev, "table")
+    tp = table.data_ptr()
     if out is None:
-        out = _new(table, (m, k), dt, stream)
+        out = _fresh((m, k), (k or 1, 1), dt) if stream is None else _new(table, (m, k), dt, stream)
         op, ldo = out.data_ptr(), k or 1
     else:
         op, ldo = _matrix(out, m, k, dt, dev, "out")
@@ -152,7 +163,10 @@ def oz2_layer_norm(x, weight=None, bias=None, eps=1e-5, center=True, save_stats=
     dt = x.dtype
     assert dt in _FLOATS, "x: expected float32, bfloat16 or float16"
     dev = _home(x, "x")
-    xp, ldx = _matrix(x, m, k, dt, dev, "x")
+    ldx, one = x.stride()
+    if one != 1 or ldx < k or ldx < 1:
+        ldx = _odd(x, m, k, dt, dev, "x")
+    xp = x.data_ptr()
     wp = bp = mp = sp = mean = rstd = None
     wt = 0
     if weight is not None:
@@ -162,15 +176,15 @@ def oz2_layer_norm(x, weight=None, bias=None, eps=1e-5, center=True, save_stats=
         assert weight is None or bias.dtype is weight.dtype, "weight and bias: expected one dtype"
         wt = TYPE[bias.dtype]
     if out is None:
-        out = _new(x, (m, k), dt, stream)
+        out = _fresh((m, k), (k or 1, 1), dt) if stream is None else _new(x, (m, k), dt, stream)
         op, ldo = out.data_ptr(), k or 1
     else:
         op, ldo = _matrix(out, m, k, dt, dev, "out")
     if save_stats:
-        rstd = _new(x, (m,), torch.float32, stream)
+        rstd = _fresh((m,), (1,), _F32) if stream is None else _new(x, (m,), _F32, stream)
         sp = rstd.data_ptr()
         if center:
-            mean = _new(x, (m,), torch.float32, stream)
+            mean = _fresh((m,), (1,), _F32) if stream is None else _new(x, (m,), _F32, stream)
             mp = mean.data_ptr()
     code = (_ENTRIES.get("oz2_layer_norm") or _entry("oz2_layer_norm"))(
         m, k, TYPE[dt], xp, ldx, wp, bp, wt, eps, 1 if center else 0, op, ldo, mp, sp,
@@ -189,7 +203,7 @@ def oz2_layer_norm_grad(dy, x, mean, rstd, weight=None, residual=None, need=("dx
     two are added to, and must be given."""
     m, k = x.shape
     dt = x.dtype
-    f32 = torch.float32
+    f32 = _F32
     assert dt in _FLOATS, "x: expected float32, bfloat16 or float16"
     assert dy.dtype is dt, "dy: expected x's dtype"
     dev = _home(x, "x")
@@ -208,21 +222,21 @@ def oz2_layer_norm_grad(dy, x, mean, rstd, weight=None, residual=None, need=("dx
     if "dx" not in need:
         dx = None
     elif dx is None:
-        dx = _new(x, (m, k), dt, stream)
+        dx = _fresh((m, k), (k or 1, 1), dt) if stream is None else _new(x, (m, k), dt, stream)
         op = dx.data_ptr()
     else:
         op, ldo = _matrix(dx, m, k, dt, dev, "dx")
     if "dweight" not in need:
         dweight = None
     elif dweight is None:
-        dweight = _new(x, (k,), f32, stream)
+        dweight = _fresh((k,), (1,), f32) if stream is None else _new(x, (k,), f32, stream)
         gp = dweight.data_ptr()
     else:
         gp = _vector(dweight, k, f32, f32, dev, "dweight")
     if "dbias" not in need:
         dbias = None
     elif dbias is None:
-        dbias = _new(x, (k,), f32, stream)
+        dbias = _fresh((k,), (1,), f32) if stream is None else _new(x, (k,), f32, stream)
         bp = dbias.data_ptr()
     else:
         bp = _vector(dbias, k, f32, f32, dev, "dbias")
@@ -242,9 +256,13 @@ def _head(x, w):
     assert k == k2 and w.dtype is dt, "x and w: expected (m, k) and (n, k) of one dtype"
     assert dt is torch.bfloat16 or dt is torch.float16, "x and w: expected bfloat16 or float16"
     dev = _home(x, "x")
-    xp, ldx = _matrix(x, m, k, dt, dev, "x")
-    wp, ldw = _matrix(w, n, k, dt, dev, "w")
-    return m, n, k, dt, dev, xp, ldx, wp, ldw
+    ldx, one = x.stride()
+    if one != 1 or ldx < k or ldx < 1:
+        ldx = _odd(x, m, k, dt, dev, "x")
+    ldw, one = w.stride()
+    if one != 1 or ldw < k or ldw < 1 or w.get_device() != dev:
+        ldw = _odd(w, n, k, dt, dev, "w")
+    return m, n, k, dt, dev, x.data_ptr(), ldx, w.data_ptr(), ldw
 
 
 def _entries(ids, teacher, m, dev):
@@ -269,9 +287,10 @@ def oz2_linear_xent(x, w, targets, scale=1.0, z_loss=0.0, stream=None):
     m, n, k, dt, dev, xp, ldx, wp, ldw = _head(x, w)
     assert targets.dtype in IDS, "targets: expected int64 or int32"
     ip = _vector(targets, m, torch.int64, torch.int32, dev, "targets")
-    loss = _new(x, (m,), torch.float32, stream)
-    lse = _new(x, (m,), torch.float32, stream)
-    picked = _new(x, (m,), torch.float32, stream)
+    if stream is None:
+        loss, lse, picked = _fresh((m,), (1,), _F32), _fresh((m,), (1,), _F32), _fresh((m,), (1,), _F32)
+    else:
+        loss, lse, picked = (_new(x, (m,), _F32, stream) for _ in range(3))
     code = (_ENTRIES.get("oz2_linear_xent") or _entry("oz2_linear_xent"))(
         m, n, k, TYPE[dt], xp, ldx, wp, ldw, ip, IDS[targets.dtype], scale, z_loss, loss.data_ptr(), lse.data_ptr(),
         picked.data_ptr(), _raw_stream(dev) if stream is None else stream.cuda_stream)
@@ -289,14 +308,14 @@ def _outputs(x, m, n, k, dt, dev, need, dx, dw, dw_dtype, accumulate, stream):
     if "dx" not in need:
         dx = None
     elif dx is None:
-        dx = _new(x, (m, k), dt, stream)
+        dx = _fresh((m, k), (k or 1, 1), dt) if stream is None else _new(x, (m, k), dt, stream)
         xp = dx.data_ptr()
     else:
         xp, ldx = _matrix(dx, m, k, dt, dev, "dx")
     if "dw" not in need:
         dw = None
     elif dw is None:
-        dw = _new(x, (n, k), dw_dtype or dt, stream)
+        dw = _fresh((n, k), (k or 1, 1), dw_dtype or dt) if stream is None else _new(x, (n, k), dw_dtype or dt, stream)
         wp, wt = dw.data_ptr(), TYPE.get(dw.dtype, -1)
     else:
         wp, ldw = _matrix(dw, n, k, dw.dtype, dev, "dw")

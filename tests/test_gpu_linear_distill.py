@@ -40,7 +40,8 @@ CASES = [
     (1, 1, 64, 1, {}), (2, 64, 64, 1, {}), (3, 100, 72, 2, dict(teacher=BF16)), (40, 300, 128, 33, dict(how="odd")),
     (130, 700, 96, 64, dict(teacher=F16, ids=torch.int32)), (257, 513, 65, 5, dict(how="odd", ids=torch.int32)),
     (300, 2000, 256, 128, dict(how="strided")), (20, 50, 64, 50, dict(ragged=False)), (30, 200, 64, 100, dict(repeated=True)),
-    (9, 5000, 64, 1024, {}), (70, 300, 128, 300, dict(ragged=False)), (600, 9000, 40, 17, dict(ragged=False)), (5, 64, 64, 300, dict(repeated=True))]
+    (9, 5000, 64, 1024, {}), (70, 300, 128, 300, dict(ragged=False)),
+    (20, 400000, 8, 40, {}), (600, 9000, 40, 17, dict(ragged=False)), (5, 64, 64, 300, dict(repeated=True))]
 
 
 @pytest.mark.parametrize("dt", [BF16, F16])
