@@ -36,7 +36,7 @@ int oz2_embedding(int64_t m, int64_t n, int64_t k, int type, const void* d_ids, 
  *   flags     OZ2_GRAD_ACCUMULATE: the sums are added to dE, whose other rows are left
  *             as they are; else rows without tokens become zeros
  * A row's tokens are summed in ascending order, in stretches that depend on the sorted
- * tokens alone. */
+ * tokens alone.  (F32 sums are added to dE in memory, where a result below 2^-126 counts as 0.) */
 int oz2_embedding_grad(int64_t m, int64_t n, int64_t k, int type, const void* d_dY, int64_t lddy,
                        const void* d_ids, int id_bits, float scale, void* d_dE, int64_t ldde, int de_type,
                        unsigned flags, void* stream);

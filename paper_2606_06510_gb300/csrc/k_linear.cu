@@ -1040,7 +1040,7 @@ void plan_pairs(const int64_t (&tiles)[kMaxProducts], const int64_t (&steps)[kMa
   }
   // The first product's tiles, fewer than the pairs, take long: one to a pair, whose turns at
   // the second's then come after theirs.  (In turn, 64 tiles of 786 steps and 788 of 64 left 12
-  // pairs idle for half of the time: the gradient of 4096×50257×1024 461 us, so 430.)
+  // pairs idle for half of the time: the gradient of 4096×50257×1024 461 µs, so 435.)
   if (count == 2 && tiles[0] > 0 && tiles[0] < pairs && tiles[1] > 0) {
     const int64_t others = pairs - tiles[0];
     const int64_t ahead = std::min<int64_t>(static_cast<int64_t>(t0 / t1), tiles[1] / others);

@@ -9,7 +9,11 @@ using ForwardKernel = Kernel<void (*)(NormArgs)>;
 // ---------------------------------------------------------------------------
 // Forward.  TPR threads to a row, VPT 16-byte pieces of it to a thread: up to 16 values, two
 // to an instruction.  Groups of threads walk over rows, the next ones on their way meanwhile.
-// (A block to each few rows, loaded when it came to them, took 254 us for 65536×1024 f32.)
+//
+// Memory bounds it: 65536×1024 f32 100 µs (5.4 TB/s; a block to each few rows, loaded when it came
+// to them, 254), 16384×4096 bf16 58 (4.7).  Rows over 4096 are one group of 512 or 1024 threads an
+// SM and wait for its two sums (8192² 66, 4096×16384 94); rows off the grid for the shifts of
+// their words (16384×777 f16 39, 15 at the copy rate).
 // ---------------------------------------------------------------------------
 constexpr int kForwardThreads = 256;
 constexpr int forward_blocks(int block) { return block == 256 ? 3 : 1; }  // an SM
@@ -28,7 +32,7 @@ __global__ void __launch_bounds__(norm_block(TPR, kForwardThreads), forward_bloc
   constexpr int V = X::V, H = V / 2, kBlock = norm_block(TPR, kForwardThreads), kGroups = kBlock / TPR;
   using Rows = Pieces<TYPE, TPR, VPT, kBlock, ALIGNED>;
   constexpr int STAGES = forward_stages<TYPE, TPR, VPT, ALIGNED>();
-  constexpr bool KEEP = TPR < 1024;  // weights in registers (read again for each row by two blocks of 512: 8192² 66 to 84 us)
+  constexpr bool KEEP = TPR < 1024;  // weights in registers (read again for each row by two blocks of 512: 8192² 66 to 84 µs)
   __shared__ float exchange[kGroups][TPR < 32 ? 1 : 2 * TPR / 32];
   extern __shared__ __align__(16) uint8_t norm_smem[];
   pdl_trigger();

@@ -12,9 +12,11 @@ using BackwardKernel = Kernel<void (*)(NormGradArgs, float*)>;
 // theirs in shared memory, in order, into the block's row of `parts`, and
 // join_parts_kernel adds up the blocks'.
 //
-// Memory bounds it.  A thread's 16 values of a row stay in registers between the sums and dx;
-// the 1024 threads of rows over 8192 have registers for the columns' sums alone and form them
-// a second time.
+// Memory bounds it: 16384×4096 bf16 with a skip connection, 537 MB, take 101 µs, 5.3 TB/s (each
+// row loaded when it came and the sums one value an instruction: 151), 65536×1024 f32 162 (6.6).
+// A thread's 16 values of a row stay in registers between the sums and dx; the 1024 threads of
+// rows over 8192 have registers for the columns' sums alone and form them a second time
+// (4096×16384 bf16 184 µs, f32 244).
 // ---------------------------------------------------------------------------
 template <int TYPE, int TPR, int VPT, bool ALIGNED>
 constexpr int backward_stages() {

@@ -14,7 +14,8 @@ bool valid_type(int t) { return t == OZ2_TYPE_F32 || is_16bit(t); }
 bool valid_ids(int bits) { return bits == 64 || bits == 32; }
 bool too_large(int64_t a, int64_t b, int64_t c) { return a >= kMaxSize || b >= kMaxSize || c >= kMaxSize; }
 
-// The bytes of dz, in 16 bits, that a piece of the vocabulary may have.
+// The bytes of dz, in 16 bits, that a piece of the vocabulary may have.  (Against no pieces,
+// 8192×131072×2048 takes 1.4% longer, with 128 MB 2.7%; 4096×50257×1024 in two pieces of 256 MB 2.6%.)
 constexpr int64_t kPieceBytes = 512LL << 20;
 
 int64_t piece_columns(int64_t m, int64_t n) {
@@ -49,7 +50,7 @@ bool head_pointers(const HeadCall& c, int id_bits) {
 }
 
 // Operands on 16-byte boundaries that are not 32-byte ones slow TMA (see oz2_linear): 4096
-// tokens × 32000×1000 take 196 us, so 142 at 1024.  The smaller one is copied where that pays,
+// tokens × 32000×1000 take 196 µs, so 142 at 1024.  The smaller one is copied where that pays,
 // and w where its products (`uses` of them) gain enough by what is then left, a ninth of their time.
 struct HeadCopies {
   bool x, w;
