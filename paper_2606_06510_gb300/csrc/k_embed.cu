@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(256)
       float f[X::V];
       X::unpack(v[j], f);
 #pragma unroll
-      for (int e = 0; e < X::V; ++e) f[e] = id[j] >= n ? __int_as_float(0x7FC00000) : f[e] * scale;
+      for (int e = 0; e < X::V; ++e) f[e] = id[j] >= n ? __int_as_float(0x7FC00000) : id[j] < 0 ? 0.f : f[e] * scale;
       const int there = row[j] < m ? static_cast<int>(min(int64_t(X::V), k - col[j])) : 0;
       store_piece<ALIGNED>(dst + (there ? row[j] * ldy + col[j] : 0), X::pack(f), there);
     }

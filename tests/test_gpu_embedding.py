@@ -63,6 +63,9 @@ def test_forward_padding_and_beyond(oz):
     ids = torch.tensor([2, -1, 4, -100, 2, 1 << 40, -(1 << 40)], device="cuda")
     y = oz.oz2_embedding(ids, table)
     assert (y[0] == 3).all() and (y[4] == 3).all() and not y[[1, 3, 6]].any() and y[[2, 5]].isnan().all()
+    for scale in (float("inf"), float("nan")):
+        y = oz.oz2_embedding(ids, table, scale=scale)
+        assert not y[[1, 3, 6]].any() and not y[[0, 2, 4, 5]].isfinite().any()
     assert oz.oz2_embedding(ids[:0], table).shape == (0, 40)
     assert oz.oz2_embedding(torch.tensor([0, -1], device="cuda"), table[:0])[0].isnan().all()
 
