@@ -735,7 +735,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
       if (id >= 0) {
         live = true;
         const float log_q = teacher_at(t, mine, i) - top - log_all, weight = expf(log_q);
-        if (weight != 0.f) s = fmaf(weight, log_q - z, s);  // (a row that the teacher rules out weighs nothing)
+        if (weight != 0.f || id >= n) s = fmaf(weight, log_q - z, s);  // (a row that the teacher rules out weighs nothing)
       }
     }
     s = warp_add(s);

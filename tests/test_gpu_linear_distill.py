@@ -119,6 +119,7 @@ def test_an_entry_beyond_is_nan(oz):
     good = oz.oz2_linear_distill(x, w, ids, teacher)
     i2 = ids.clone()
     i2[5, 3], i2[6, 0] = 300, 1 << 50
+    i2[7, 1], teacher[7, 1] = 301, -float("inf")  # nor does it matter what the teacher thinks of it
     loss, lse, picked = oz.oz2_linear_distill(x, w, i2, teacher)
     bad = (i2 >= 300).any(1)
     assert loss[bad].isnan().all() and torch.equal(loss[~bad], good[0][~bad])
