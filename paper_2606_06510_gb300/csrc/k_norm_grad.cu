@@ -82,8 +82,8 @@ __global__ void __launch_bounds__(norm_block(TPR, kNormThreads), 1) norm_grad_ke
     fetch_wait<STAGES - 1>();
     Rows::meet();
     const Two less = two(-mean, -mean), scale = two(rstd, rstd);
-    // dy, g = dy·w and x̂ of a piece.  (Past the row's end dy is zero, and whatever x̂ is there
-    // counts for nothing.)
+    // dy, g = dy·w and x̂ of a piece.  (Past the row's end both are zeros: of -mean·rstd, which
+    // may be infinite, not even 0 times it counts for nothing.)
     auto values = [&](int i, Two (&d)[H], Two (&g)[H], Two (&h)[H]) {
       const uint4 none = make_uint4(0, 0, 0, 0);
       unpack2<TYPE>(live ? in_dy.read(memory(stage, 0), dy + r * a.lddy, i) : none, d);
@@ -94,6 +94,14 @@ __global__ void __launch_bounds__(norm_block(TPR, kNormThreads), 1) norm_grad_ke
       for (int e = 0; e < H; ++e) {
         h[e] = (h[e] + less) * scale;
         g[e] = d[e] * (KEEP ? w[KEEP ? i : 0][e] : own[e]);
+      }
+      const int n = live ? there(i) : 0;
+      if (n < V) {
+#pragma unroll
+        for (int e = 0; e < H; ++e) {
+          const float2 p = both(h[e]);
+          h[e] = two(2 * e < n ? p.x : 0.f, 2 * e + 1 < n ? p.y : 0.f);
+        }
       }
     };
     Two s0 = zero, s1 = zero, kg[KEEP ? VPT : 1][H], kh[KEEP ? VPT : 1][H];

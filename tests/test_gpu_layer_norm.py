@@ -133,6 +133,23 @@ def test_hard_rows(oz):
     assert y[5:7].isnan().any(1).all() and torch.equal(y[[0, 1, 2, 3, 4, 7]], gy[[0, 1, 2, 3, 4, 7]])
 
 
+@pytest.mark.parametrize("m", [3, 8, 700])
+@pytest.mark.parametrize("k", [1, 2, 16, 128])
+def test_constant_rows_of_large_values(oz, m, k):
+    """mean·rstd passes FP32's range, but no row deviates from its mean (exact: k is a power of two,
+    and equal values are added): dx = rstd·(dy - mean dy), dw = 0."""
+    x = torch.full((m, k), 2.0 ** 120, device="cuda")
+    y, mean, rstd = oz.oz2_layer_norm(x, save_stats=True)
+    assert not y.any() and torch.equal(mean, x[:, 0])
+    dy = torch.randn(m, k, generator=rng(k), device="cuda")
+    dx, dw, db = oz.oz2_layer_norm_grad(dy, x, mean, rstd)
+    dev, r = dy.double() - dy.double().mean(1, keepdim=True), rstd.double()[:, None]
+    # The mean of k, its product and difference: k + 3 roundings of what is no larger than Σ|dy|/k + |dy|.
+    close(dx, r * dev, r * (k + 3) * ref.u * (dy.double().abs() + dy.double().abs().mean(1, keepdim=True)), "dx")
+    assert not dw.any()
+    close(db, dy.double().sum(0), m * ref.u * dy.double().abs().sum(0), "db")
+
+
 def test_empty(oz):
     x = torch.zeros(0, 8, device="cuda")
     y, mean, rstd = oz.oz2_layer_norm(x, save_stats=True)
