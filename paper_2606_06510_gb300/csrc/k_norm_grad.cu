@@ -64,7 +64,7 @@ __global__ void __launch_bounds__(norm_block(TPR, kNormThreads), 1) norm_grad_ke
   auto fetch = [&](int64_t r, int stage) {
     if (r < a.m) {
       in_dy.fetch(memory(stage, 0), dy + r * a.lddy);
-      in_x.fetch(memory(stage, 1), x + r * a.ldx);
+      in_x.template fetch<true>(memory(stage, 1), x + r * a.ldx);
       if (res) in_r.fetch(memory(stage, 2), res + r * a.ldr);
     }
     fetch_commit();
@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(norm_block(TPR, kNormThreads), 1) norm_grad_ke
   for (int s = 0; s < STAGES; ++s) fetch(first + s * stride, s);
   float mean = 0.f, rstd = 0.f;
   auto statistics = [&](int64_t r) {
-    if (r < a.m) mean = a.mean ? __ldg(a.mean + r) : 0.f, rstd = __ldg(a.rstd + r);
+    mean = r < a.m && a.mean ? __ldg(a.mean + r) : 0.f, rstd = r < a.m ? __ldg(a.rstd + r) : 0.f;
   };
   statistics(first);
   int stage = 0;
@@ -82,8 +82,10 @@ __global__ void __launch_bounds__(norm_block(TPR, kNormThreads), 1) norm_grad_ke
     fetch_wait<STAGES - 1>();
     Rows::meet();
     const Two less = two(-mean, -mean), scale = two(rstd, rstd);
-    // dy, g = dy·w and x̂ of a piece.  (Past the row's end both are zeros: of -mean·rstd, which
-    // may be infinite, not even 0 times it counts for nothing.)
+    // dy, g = dy·w and x̂ of a piece.  Past the row's end dy is zero, and x̂ counts for nothing as
+    // long as it is a number: of a whole piece it is the row's first one's; of elements -mean·rstd,
+    // which may be infinite (rows of one large value), and is then left out.
+    const bool wild = !ALIGNED && !(fabsf(mean * rstd) < INFINITY);
     auto values = [&](int i, Two (&d)[H], Two (&g)[H], Two (&h)[H]) {
       const uint4 none = make_uint4(0, 0, 0, 0);
       unpack2<TYPE>(live ? in_dy.read(memory(stage, 0), dy + r * a.lddy, i) : none, d);
@@ -95,8 +97,8 @@ __global__ void __launch_bounds__(norm_block(TPR, kNormThreads), 1) norm_grad_ke
         h[e] = (h[e] + less) * scale;
         g[e] = d[e] * (KEEP ? w[KEEP ? i : 0][e] : own[e]);
       }
-      const int n = live ? there(i) : 0;
-      if (n < V) {
+      if (wild) {
+        const int n = there(i);
 #pragma unroll
         for (int e = 0; e < H; ++e) {
           const float2 p = both(h[e]);
@@ -348,7 +350,7 @@ cudaError_t backward(const NormGradArgs& a, float* parts, cudaStream_t st) {
                              dim3(256), 0, st, a, long_chunk(a.m), parts);
     }
   } else {
-    const bool aligned = rows_on16(a.dy, a.lddy, es) && rows_on16(a.x, a.ldx, es) && (!a.r || rows_on16(a.r, a.ldr, es)) &&
+    const bool aligned = a.k % Elem<TYPE>::V == 0 && rows_on16(a.dy, a.lddy, es) && rows_on16(a.x, a.ldx, es) && (!a.r || rows_on16(a.r, a.ldr, es)) &&
                          (!a.dx || rows_on16(a.dx, a.lddx, es));
     const BackwardKernel f = aligned ? by_shape<Backward<TYPE, true>::template K>(s) : by_shape<Backward<TYPE, false>::template K>(s);
     err = allow_smem(reinterpret_cast<const void*>(f.kernel), f.smem);

@@ -120,12 +120,14 @@ struct Pieces {
   static __device__ __forceinline__ uint8_t* after(uint8_t* at, int i) {
     return last() ? at + (i * kWords + BLOCK + threadIdx.x / kLanes) * 16 : slot(at, i) + 16;
   }
+  // (REAL: what is past the row's end, by whole pieces, becomes its first piece again, not zeros.)
+  template <bool REAL = false>
   __device__ __forceinline__ void fetch(uint8_t* at, const T* row) const {
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       const int n = there(i);
       if (ALIGNED) {  // (zeros past the row's end)
-        fetch_async(smem_u32(slot(at, i)), row + (n ? col(i) : 0), n * sizeof(T));
+        fetch_async(smem_u32(slot(at, i)), row + (n ? col(i) : 0), REAL && n == 0 ? 16 : n * static_cast<int>(sizeof(T)));
       } else if (n) {
         const T* p = row + col(i);
         const int s = static_cast<int>(reinterpret_cast<uintptr_t>(p) & 15);
