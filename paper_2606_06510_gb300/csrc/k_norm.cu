@@ -11,30 +11,39 @@ using ForwardKernel = Kernel<void (*)(NormArgs)>;
 // to an instruction.  Groups of threads walk over rows, the next ones on their way meanwhile.
 //
 // Memory bounds it: 65536×1024 f32 100 µs (5.4 TB/s; a block to each few rows, loaded when it came
-// to them, 254), 16384×4096 bf16 58 (4.7).  Rows over 4096 are one group of 512 or 1024 threads an
-// SM and wait for its two sums (8192² 66, 4096×16384 94); rows off the grid for the shifts of
-// their words (16384×777 f16 39, 15 at the copy rate).
+// to them, 254), 16384×4096 bf16 58 (4.7).  Rows over 4096 wait for their two sums: one or two
+// groups an SM, with their weights in shared memory (8192² bf16 62 µs, 4096×16384 62; read again for
+// each row from L2, 84 and 96); rows off the grid for the shifts of their words (16384×777 f16 39,
+// 15 at the copy rate).
 // ---------------------------------------------------------------------------
 constexpr int kForwardThreads = 256;
-constexpr int forward_blocks(int block) { return block == 256 ? 3 : 1; }  // an SM
-constexpr int forward_room(int block) { return 200 * 1024 / forward_blocks(block); }
+// Where the weights are: in a thread's registers; of wide rows, whose threads have not enough for
+// them, as FP32 in shared memory, but where those and the rows together do not fit.
+enum Weights { kInRegisters, kInShared, kInMemory };
 template <int TYPE, int TPR, int VPT, bool ALIGNED>
-constexpr int forward_stages() {
-  constexpr int block = norm_block(TPR, kForwardThreads);
-  return norm_stages(Pieces<TYPE, TPR, VPT, block, ALIGNED>::kBytes, forward_room(block));
-}
+struct ForwardShape {
+  static constexpr int cols = TPR * VPT * Elem<TYPE>::V;
+  static constexpr Weights weights = cols <= 4096 ? kInRegisters : cols <= 8192 || TYPE != OZ2_TYPE_F32 ? kInShared : kInMemory;
+  static constexpr int block = weights == kInRegisters ? norm_block(TPR, kForwardThreads) : 1024;
+  static constexpr int blocks = block == 256 ? 3 : 1;  // an SM
+  using Rows = Pieces<TYPE, TPR, VPT, block, ALIGNED>;
+  static constexpr int weight_bytes = weights == kInShared ? 2 * 4 * cols : 0;
+  static constexpr int stages = norm_stages(Rows::kBytes, 200 * 1024 / blocks - weight_bytes);
+  static constexpr int smem = weight_bytes + Rows::kBytes * stages;
+};
 
 template <int TYPE, int TPR, int VPT, bool ALIGNED>
-__global__ void __launch_bounds__(norm_block(TPR, kForwardThreads), forward_blocks(norm_block(TPR, kForwardThreads)))
+__global__ void __launch_bounds__(ForwardShape<TYPE, TPR, VPT, ALIGNED>::block, ForwardShape<TYPE, TPR, VPT, ALIGNED>::blocks)
     norm_kernel(NormArgs a) {
   using X = Elem<TYPE>;
   using T = typename X::T;
-  constexpr int V = X::V, H = V / 2, kBlock = norm_block(TPR, kForwardThreads), kGroups = kBlock / TPR;
-  using Rows = Pieces<TYPE, TPR, VPT, kBlock, ALIGNED>;
-  constexpr int STAGES = forward_stages<TYPE, TPR, VPT, ALIGNED>();
-  constexpr bool KEEP = TPR < 1024;  // weights in registers (read again for each row by two blocks of 512: 8192² 66 to 84 µs)
+  using Shape = ForwardShape<TYPE, TPR, VPT, ALIGNED>;
+  using Rows = typename Shape::Rows;
+  constexpr int V = X::V, H = V / 2, kGroups = Shape::block / TPR, STAGES = Shape::stages;
+  constexpr bool KEEP = Shape::weights == kInRegisters, SHARED = Shape::weights == kInShared;
   __shared__ float exchange[kGroups][TPR < 32 ? 1 : 2 * TPR / 32];
-  extern __shared__ __align__(16) uint8_t norm_smem[];
+  extern __shared__ __align__(16) uint8_t norm_all[];
+  uint8_t* norm_smem = norm_all + Shape::weight_bytes;
   pdl_trigger();
   pdl_wait();
   const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
@@ -61,6 +70,33 @@ __global__ void __launch_bounds__(norm_block(TPR, kForwardThreads), forward_bloc
 #pragma unroll
     for (int i = 0; i < VPT; ++i) vector(a.w, i, one, w[KEEP ? i : 0]), vector(a.b, i, zero, b[KEEP ? i : 0]);
   }
+  // In shared memory, four values of each piece side by side: w's, then b's.
+  constexpr int kPlane = TPR * VPT;
+  auto plane = [&](int which, int i, int e) { return reinterpret_cast<float4*>(norm_all) + (which * (V / 4) + e / 2) * kPlane + i * TPR + t; };
+  if (SHARED) {
+#pragma unroll
+    for (int which = 0; which < 2; ++which)
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+        Two v[H];
+        if (group == 0) {
+          vector(which ? a.b : a.w, i, which ? zero : one, v);
+#pragma unroll
+          for (int e = 0; e < H; e += 2) {
+            const float2 p = both(v[e]), q = both(v[e + 1]);
+            *plane(which, i, e) = make_float4(p.x, p.y, q.x, q.y);
+          }
+        }
+      }
+    __syncthreads();
+  }
+  auto shared_vector = [&](int which, int i, Two (&to)[H]) {
+#pragma unroll
+    for (int e = 0; e < H; e += 2) {
+      const float4 v = *plane(which, i, e);
+      to[e] = two(v.x, v.y), to[e + 1] = two(v.z, v.w);
+    }
+  };
   int stage = 0;
   for (int64_t r = first; r - groups_before<TPR>() < a.m; r += stride) {
     const bool live = TPR >= 32 || r < a.m;
@@ -112,7 +148,11 @@ __global__ void __launch_bounds__(norm_block(TPR, kForwardThreads), forward_bloc
       const int n = in.there(i);
       float f[V];
       Two wi[H], bi[H];
-      if (!KEEP) vector(a.w, i, one, wi), vector(a.b, i, zero, bi);
+      if (SHARED) {
+        shared_vector(0, i, wi), shared_vector(1, i, bi);
+      } else if (!KEEP) {
+        vector(a.w, i, one, wi), vector(a.b, i, zero, bi);
+      }
 #pragma unroll
       for (int e = 0; e < H; ++e) {
         const float2 q = both(fma(x[i][e] * scale, KEEP ? w[KEEP ? i : 0][e] : wi[e], KEEP ? b[KEEP ? i : 0][e] : bi[e]));
@@ -183,9 +223,9 @@ struct Forward {
   template <int TPR, int VPT>
   struct K {
     static ForwardKernel f() {
-      constexpr int kVpt = VPT * Elem<TYPE>::V <= 16 ? VPT : 2, kBlock = norm_block(TPR, kForwardThreads);
-      return {norm_kernel<TYPE, TPR, kVpt, ALIGNED>, kBlock,
-              Pieces<TYPE, TPR, kVpt, kBlock, ALIGNED>::kBytes * forward_stages<TYPE, TPR, kVpt, ALIGNED>()};
+      constexpr int kVpt = VPT * Elem<TYPE>::V <= 16 ? VPT : 2;
+      using Shape = ForwardShape<TYPE, TPR, kVpt, ALIGNED>;
+      return {norm_kernel<TYPE, TPR, kVpt, ALIGNED>, Shape::block, Shape::smem};
     }
   };
 };
@@ -203,7 +243,7 @@ cudaError_t forward(const NormArgs& a, cudaStream_t st) {
   const cudaError_t err = allow_smem(reinterpret_cast<const void*>(f.kernel), f.smem);
   if (err != cudaSuccess) return err;
   const int groups = f.block / s.tpr;
-  const int64_t blocks = std::min<int64_t>((a.m + groups - 1) / groups, forward_blocks(f.block) * static_cast<int64_t>(num_sms()));
+  const int64_t blocks = std::min<int64_t>((a.m + groups - 1) / groups, (f.block == kForwardThreads ? 3 : 1) * static_cast<int64_t>(num_sms()));
   return launch_dependent(f.kernel, dim3(static_cast<unsigned>(blocks)), dim3(f.block), f.smem, st, a);
 }
 
