@@ -14,7 +14,7 @@ namespace {
 // Forward: a thread takes 16-byte pieces of the result, one grid's stride apart; its
 // row and place in it are found by one division and carried on.  The id is read, then
 // the piece: kAhead of these chains are under way at once.  Memory bounds it (65536×2048
-// bf16 73 µs: the result's 268 MB, and rows that mostly come from L2), for few tokens the
+// bf16 72 µs: the result's 268 MB, and rows that mostly come from L2), for few tokens the
 // launch (64×4096 4 µs in a graph).
 // ---------------------------------------------------------------------------
 constexpr int kAhead = 4, kBlocks = 8;  // pieces of a thread at once, blocks an SM
@@ -37,7 +37,10 @@ __global__ void __launch_bounds__(256)
   while (ALIGNED ? r < m : __any_sync(0xffffffffu, r < m) != 0) {
     int64_t row[kAhead], id[kAhead];
     int col[kAhead];
+    // Rows off the 16-byte grid: the words around a piece, which are shifted when all are under way.
     uint4 v[kAhead];
+    Words around[ALIGNED ? 1 : kAhead];
+    bool inside[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       row[j] = r;
@@ -50,16 +53,27 @@ __global__ void __launch_bounds__(256)
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       v[j] = make_uint4(0, 0, 0, 0);
-      if (id[j] >= 0 && id[j] < n)
-        v[j] = load_piece<ALIGNED>(src + id[j] * lde + col[j], src, end, static_cast<int>(min(int64_t(X::V), k - col[j])));
+      const bool real = id[j] >= 0 && id[j] < n;
+      const T* p = src + (real ? id[j] * lde + col[j] : 0);
+      if (ALIGNED) {
+        if (real) v[j] = load_piece<true>(p, src, end, static_cast<int>(min(int64_t(X::V), k - col[j])));
+      } else {
+        inside[j] = real && words_inside(p, src, end);
+        if (inside[j]) around[ALIGNED ? 0 : j] = load_words16(p);
+      }
     }
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       if (ALIGNED && row[j] >= m) continue;
+      if (!ALIGNED && id[j] >= 0 && id[j] < n) {
+        const T* p = src + id[j] * lde + col[j];
+        v[j] = inside[j] ? shift_words16(p, around[ALIGNED ? 0 : j]) : load16_singly(p, static_cast<int>(min(int64_t(X::V), k - col[j])));
+      }
       float f[X::V];
       X::unpack(v[j], f);
+      const float by = id[j] < 0 ? 0.f : id[j] < n ? scale : __int_as_float(0x7FC00000);  // (of zeros, where there is no row)
 #pragma unroll
-      for (int e = 0; e < X::V; ++e) f[e] = id[j] >= n ? __int_as_float(0x7FC00000) : id[j] < 0 ? 0.f : f[e] * scale;
+      for (int e = 0; e < X::V; ++e) f[e] *= by;
       const int there = row[j] < m ? static_cast<int>(min(int64_t(X::V), k - col[j])) : 0;
       store_piece<ALIGNED>(dst + (there ? row[j] * ldy + col[j] : 0), X::pack(f), there);
     }
@@ -386,8 +400,19 @@ __device__ __forceinline__ uint4 old_piece(const SumJob& j, int64_t row, int64_t
   return load_piece<false, false>(p, base, base + (static_cast<int64_t>(j.n) - 1) * j.ldde + j.k, n);
 }
 
+// The next lane's word, of the last lane lane `from`'s `after`.
+__device__ __forceinline__ uint4 next_lane(uint4 v, uint4 after, int from, int lane) {
+  uint4 r;
+  auto one = [&](uint32_t a, uint32_t b) {
+    const uint32_t x = __shfl_down_sync(0xffffffffu, a, 1), y = __shfl_sync(0xffffffffu, b, from);
+    return lane == 31 ? y : x;
+  };
+  r.x = one(v.x, after.x), r.y = one(v.y, after.y), r.z = one(v.z, after.z), r.w = one(v.w, after.w);
+  return r;
+}
+
 template <int TYPE, int OUT, int P, bool ALIGNED, bool ADD>
-__global__ void __launch_bounds__(32 * kSumWarps, P == 1 ? 4 : P == 2 ? 3 : 2) sum_runs_kernel(SumJob j) {
+__global__ void __launch_bounds__(32 * kSumWarps, (P == 1 ? 4 : P == 2 ? 3 : 2) - (ALIGNED || P == 4 ? 0 : 1)) sum_runs_kernel(SumJob j) {
   using X = Elem<TYPE>;
   using T = typename X::T;
   constexpr int V = X::V;
@@ -463,27 +488,58 @@ __global__ void __launch_bounds__(32 * kSumWarps, P == 1 ? 4 : P == 2 ? 3 : 2) s
   // first is added, and so are the old values of 16-bit rows that are added to.
   constexpr bool kOld = ADD && OUT != OZ2_TYPE_F32;
   constexpr int kAtOnce = (P == 4 ? 16 : 8) / P / (kOld ? 2 : 1);
+  // Rows off the 16-byte grid: a lane loads the word in which its piece begins, the next lane's is the
+  // one after it, and what comes after the last lane's are one load more, a lane's for each piece.
+  // (Two words a piece, each waited for: 65536×1001 bf16 into 1000 rows 144 µs in all, so 89, and 66 at
+  // 1000.  More blocks an SM spill.)
+  const char* const first = reinterpret_cast<const char*>(src);
+  const int64_t slice0 = static_cast<int64_t>(slice) * P * 32 * V, slice1 = min(j.k, slice0 + P * 32 * V);
+  auto words_there = [&](const T* row) {  // the words around the slice are the tensor's own
+    const uintptr_t from = reinterpret_cast<uintptr_t>(row + slice0) & ~static_cast<uintptr_t>(15),
+                    to = (reinterpret_cast<uintptr_t>(row + slice1) + 15) & ~static_cast<uintptr_t>(15);
+    return from >= reinterpret_cast<uintptr_t>(first) && to <= reinterpret_cast<uintptr_t>(stop);
+  };
   for (int i = begin; i < end; i += kAtOnce) {
-    uint4 v[kAtOnce][P], old[kOld ? kAtOnce : 1][P];
+    uint4 v[kAtOnce][P], old[kOld ? kAtOnce : 1][P], after = make_uint4(0, 0, 0, 0);
+    const char* after_at = nullptr;
 #pragma unroll
     for (int q = 0; q < kAtOnce; ++q) {
       const int at = min(i + q, end - 1);
       const uint2 pair = pairs[at];
       const T* row = src + static_cast<int64_t>(pair.y) * j.lddy;
+      const bool words = !ALIGNED && words_there(row);
 #pragma unroll
       for (int c = 0; c < P; ++c) {
         const int n = there(c);
-        if (n > 0 && i + q < end) v[q][c] = load_piece<ALIGNED>(row + col(c), src, stop, n);
+        if (ALIGNED) {
+          if (n > 0 && i + q < end) v[q][c] = load_piece<true>(row + col(c), src, stop, n);
+        } else if (words && i + q < end) {
+          const char* stops = reinterpret_cast<const char*>(row + slice1);
+          const char* word = reinterpret_cast<const char*>(row + col(c)) - (reinterpret_cast<uintptr_t>(row) & 15);
+          if (word < stops) v[q][c] = load_global<true>(reinterpret_cast<const uint4*>(word));
+          const char* next = word + 16 * (32 - lane);  // (behind lane 31's)
+          if (lane == q * P + c && next < stops) after_at = next;
+        }
         if (kOld && n > 0 && i + q < end && (ends >> at & 1) && at >= head)
           old[kOld ? q : 0][c] = old_piece<OUT>(j, pair.x, col(c), n);
       }
     }
+    if (!ALIGNED && after_at) after = load_global<true>(reinterpret_cast<const uint4*>(after_at));
 #pragma unroll
     for (int q = 0; q < kAtOnce; ++q) {
       const int at = i + q;
       if (at >= end) break;
 #pragma unroll
       for (int c = 0; c < P; ++c) {
+        if (!ALIGNED) {
+          const T* row = src + static_cast<int64_t>(pairs[at].y) * j.lddy;
+          if (words_there(row)) {
+            const Words w{v[q][c], next_lane(v[q][c], after, q * P + c, lane)};
+            v[q][c] = shift_words16(reinterpret_cast<const void*>(reinterpret_cast<uintptr_t>(row) & 15), w);
+          } else if (there(c) > 0) {
+            v[q][c] = load16_singly(row + col(c), there(c));
+          }
+        }
         float f[V];
         X::unpack(v[q][c], f);
 #pragma unroll
