@@ -14,7 +14,7 @@ using ForwardKernel = Kernel<void (*)(NormArgs)>;
 // to them, 254), 16384×4096 bf16 58 (4.7).  Rows over 4096 wait for their two sums: one or two
 // groups an SM, with their weights in shared memory (8192² bf16 62 µs, 4096×16384 62; read again for
 // each row from L2, 84 and 96); rows off the grid for the shifts of their words (16384×777 f16 39,
-// 15 at the copy rate).
+// 8 at the copy rate).
 // ---------------------------------------------------------------------------
 constexpr int kForwardThreads = 256;
 // Where the weights are: in a thread's registers; of wide rows, whose threads have not enough for
