@@ -61,7 +61,7 @@ __device__ __forceinline__ HeadRow head_row(const HeadTerms& t, Ids ids, int64_t
   const int64_t id = ids[row];
   if (id < 0) return HeadRow{0.f, 0.f, 0.f, 0};
   const float l = __ldg(t.lse + row), g = __ldg(t.dloss + (t.dloss_each ? row : 0)) * t.scale;
-  return HeadRow{id < n ? g : __int_as_float(0x7FC00000), l * kLog2E, t.z_loss != 0.f ? 2.f * t.z_loss * l : 0.f, 1};
+  return HeadRow{id < n ? g : __int_as_float(0x7FC00000), l, t.z_loss != 0.f ? 2.f * t.z_loss * l : 0.f, 1};
 }
 __device__ __forceinline__ float head_size(const HeadRow& r) {  // (what is no number does not count)
   const float size = fabsf(r.a) * fmaxf(1.f, fabsf(1.f + r.e));
@@ -431,7 +431,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           float hard = 0.f;
           if (!SOFT && now.next < end) hard = pick32(v, now.next - from);
           const float main = t.a * (1.f + t.e);
-          const Two to = two(to2, to2), less = two(-t.lse2, -t.lse2), by = two(main, main);
+          const float lse2 = t.lse * kLog2E;
+          const Two to = two(to2, to2), less = two(-lse2, -lse2), by = two(main, main);
           float z[32];
 #pragma unroll
           for (int g = 0; g < 32; g += 8) {
@@ -455,8 +456,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             }
           }
           if (!SOFT && __any_sync(0xffffffffu, now.next < end)) {
-            if (now.next < end) {  // (1 + e)·p - 1 with p near 1: by p - 1
-              set32(z, now.next - from, t.a * fmaf(1.f + t.e, expm1f(fmaf(hard, to2, -t.lse2) * kLn2), t.e));
+            if (now.next < end) {  // (1 + e)·p - 1 with p near 1: by p - 1, of z - lse rounded once
+              set32(z, now.next - from, t.a * fmaf(1.f + t.e, expm1f(fmaf(hard, A.scale, -t.lse)), t.e));
               now.next = kNoTarget;
             }
           }
@@ -594,7 +595,7 @@ __global__ void __launch_bounds__(32 * kListWarps)
     for (int i = lane; i < top; i += 32)
       if (keys[i] != kNone) sum += expf(logits[i] - most);
     sum = warp_add(sum);
-    if (lane == 0 && there) rows[row] = HeadRow{bad ? __int_as_float(0x7FC00000) : live ? g * terms.scale : 0.f, live ? l * kLog2E : 0.f, 0.f, live};
+    if (lane == 0 && there) rows[row] = HeadRow{bad ? __int_as_float(0x7FC00000) : live ? g * terms.scale : 0.f, live ? l : 0.f, 0.f, live};
   }
   __syncwarp();
   for (int at = 0; at < padded; at += 64) sort_64(keys, at, 64, true, lane);

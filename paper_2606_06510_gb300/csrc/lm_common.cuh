@@ -205,9 +205,9 @@ struct HeadTargets {
   int teacher_type;
   float temperature;
 };
-// A token's terms of the gradient dz_j = a·((1 + e)·exp2(z2_j - lse2) - its targets' weights).
+// A token's terms of the gradient dz_j = a·((1 + e)·exp(z_j - lse) - its targets' weights).
 struct HeadRow {
-  float a, lse2, e;
+  float a, lse, e;
   int live;
 };
 // What they come of: the losses' gradient (one a token, or one for all) and lse, and for

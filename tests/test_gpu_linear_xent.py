@@ -306,3 +306,28 @@ def test_streams_and_graphs(oz):
         graph.replay()
         assert all(torch.equal(u, v) for u, v in zip(f2, fwd)) and all(torch.equal(u, v) for u, v in zip(g2, want))
     assert oz.oz2_check_device_status() == 0
+
+
+@pytest.mark.parametrize("dt", [BF16, F16])
+@pytest.mark.parametrize("scale", [1.0, 0.3, -0.7])
+@pytest.mark.parametrize("z_loss", [0.0, 1e-3])
+def test_a_certain_targets_gradient_keeps_its_accuracy(oz, dt, scale, z_loss):
+    """dz of targets whose p is within 1e-6 to 1e-3 of 1, or 1, for z and lse as they are given: z - lse
+    is rounded once, so dz is off by its rounding to 16 bits, the result's, and a few steps of FP32
+    relative to itself (with z_loss, to its terms); where z = lse it is 0 but for z_loss's term."""
+    z = torch.tensor([4.0, 8, 12, 16, 20, 22, 27, 30], device="cuda")
+    w = torch.zeros(64, 64, device="cuda").to(dt)  # (the other rows are 0 in the one feature looked at)
+    w[0, 0] = 1 if scale > 0 else -1
+    x = torch.zeros(8, 64, device="cuda").to(dt)
+    x[:, 0] = (z / abs(scale)).round()  # whole numbers: the products are exact
+    t = torch.zeros(8, dtype=torch.int64, device="cuda")
+    s, c = torch.tensor([scale, z_loss], dtype=torch.float32).double().cuda()
+    z = s * x.double() @ w[0].double()
+    for off in (0.0, 1e-6, 5e-6, 2e-5, 1e-3):
+        lse = (z + off).float()
+        e = 2 * c * lse.double()
+        dx, _ = oz.oz2_linear_xent_grad(torch.ones(8, device="cuda"), x, w, t, lse, scale=scale, z_loss=z_loss)
+        want = s * ((1 + e) * torch.expm1(z - lse.double()) + e) * w[0, 0].double()
+        # (f16: dz and results below its normal range.)
+        err = 2 * ref.U[dt] * want.abs() + 16 * ref.u * (s.abs() * e + want.abs()) + (2.0 ** -25 + 2.0 ** -38 if dt == F16 else 0)
+        assert ((dx[:, 0].double() - want).abs() <= err).all()
