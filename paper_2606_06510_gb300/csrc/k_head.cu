@@ -96,6 +96,14 @@ __device__ __forceinline__ void set32(float (&v)[32], int j, float d) {
     if (i == j) v[i] = d;
 }
 
+// The larger one; NaN where either is NaN: a maximum of infinity then says that there is none, and
+// lse is infinity (the sum beside it is no number in both cases).
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
 // A lane's maximum of v·to2 over its 64 sums (the first `cols` where not WHOLE), and the sum
 // of exp2 of the differences: the largest sum first, in its own units (NEGATIVE to2: the
 // smallest), then one multiply-add for two differences.
@@ -103,9 +111,9 @@ template <bool NEGATIVE>
 __device__ __forceinline__ float extreme(float a, float b, float c) {
   float r;
   if (NEGATIVE) {
-    asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   } else {
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   }
   return r;
 }
@@ -124,7 +132,7 @@ __device__ __forceinline__ void head_sums(const uint32_t (&v0)[32], const uint32
   top[0] = extreme<NEGATIVE>(top[0], top[1], t(60));
   top[1] = extreme<NEGATIVE>(top[2], t(61), t(62));
   top[2] = extreme<NEGATIVE>(top[3], t(63), t(63));
-  most = fmaxf(extreme<NEGATIVE>(top[0], top[1], top[2]) * to2, kLowest);
+  most = max_nan(extreme<NEGATIVE>(top[0], top[1], top[2]) * to2, kLowest);
   const Two to = two(to2, to2), less = two(-most, -most);
   Two s[2] = {two(0.f, 0.f), two(0.f, 0.f)};
 #pragma unroll
@@ -677,7 +685,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
   const int64_t row0 = static_cast<int64_t>(blockIdx.x) * 32, row = row0 + lane;
   float most = kLowest, sum = 0.f;
   auto join = [&](float2 p) {
-    const float top = fmaxf(most, p.x);
+    const float top = max_nan(most, p.x);
     sum = sum * exp2_fast(most - top) + p.y * exp2_fast(p.x - top);
     most = top;
   };
@@ -689,7 +697,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
         p[i] = g + i * join_warps < groups ? stats[(g + i * join_warps) * ld_stats + row] : make_float2(kLowest, 0.f);
       float2 all = p[0];
 #pragma unroll
-      for (int i = 1; i < kJoinAhead; ++i) all.x = fmaxf(all.x, p[i].x);
+      for (int i = 1; i < kJoinAhead; ++i) all.x = max_nan(all.x, p[i].x);
       all.y = 0.f;
 #pragma unroll
       for (int i = 0; i < kJoinAhead; ++i) all.y = fmaf(p[i].y, exp2_fast(p[i].x - all.x), all.y);

@@ -331,3 +331,20 @@ def test_a_certain_targets_gradient_keeps_its_accuracy(oz, dt, scale, z_loss):
         # (f16: dz and results below its normal range.)
         err = 2 * ref.U[dt] * want.abs() + 16 * ref.u * (s.abs() * e + want.abs()) + (2.0 ** -25 + 2.0 ** -38 if dt == F16 else 0)
         assert ((dx[:, 0].double() - want).abs() <= err).all()
+
+
+def test_nan_beside_infinity(oz):
+    """A token with a logit of plus infinity and one that is NaN: lse is NaN, wherever they are; with
+    the infinity alone it is that."""
+    w = torch.zeros(700, 64, device="cuda").to(BF16)
+    x = torch.zeros(5, 64, device="cuda").to(BF16)
+    x[:, 0] = 1
+    t = torch.zeros(5, dtype=torch.int64, device="cuda")
+    for a, b in ((3, 5), (5, 3), (0, 63), (3, 600), (600, 3), (130, 699), (699, 698)):
+        for scale in (1.0, -1.0):
+            w[:, 0] = 0
+            w[a, 0], w[b, 0] = scale * float("inf"), float("nan")
+            loss, lse, _ = oz.oz2_linear_xent(x, w, t, scale=scale)
+            assert lse.isnan().all() and loss.isnan().all()
+            w[b, 0] = 1
+            assert (oz.oz2_linear_xent(x, w, t, scale=scale)[1] == float("inf")).all()
