@@ -63,8 +63,10 @@ __device__ __forceinline__ HeadRow head_row(const HeadTerms& t, Ids ids, int64_t
   const float l = __ldg(t.lse + row), g = __ldg(t.dloss + (t.dloss_each ? row : 0)) * t.scale;
   return HeadRow{id < n ? g : __int_as_float(0x7FC00000), l, t.z_loss != 0.f ? 2.f * t.z_loss * l : 0.f, 1};
 }
-__device__ __forceinline__ float head_size(const HeadRow& r) {  // (what is no number does not count)
-  const float size = fabsf(r.a) * fmaxf(1.f, fabsf(1.f + r.e));
+// The largest |dz| that a token's terms can give: a·(1 + e)·p, or a target's a·((1 + e)·p - 1), for
+// p up to 1.  (What is no number does not count.)
+__device__ __forceinline__ float head_size(const HeadRow& r) {
+  const float size = fabsf(r.a) * fmaxf(fmaxf(1.f, fabsf(r.e)), fabsf(1.f + r.e));
   return size < INFINITY ? size : 0.f;
 }
 __device__ __forceinline__ float warp_max(float v) {

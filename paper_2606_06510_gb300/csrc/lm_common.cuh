@@ -237,7 +237,7 @@ struct HeadArgs {
   float* picked;       // (m, top)
   // gradient
   HeadTerms terms;
-  const float* largest;  // maxima of |a|·max(1, |1 + e|), `maxima` of them, or null: dz is not scaled
+  const float* largest;  // maxima of |a|·max(1, |e|, |1 + e|), `maxima` of them, or null: dz is not scaled
   int maxima;
   float* unscale;      // dz's scale, inverted (written)
   uint16_t* dz;

@@ -348,3 +348,18 @@ def test_nan_beside_infinity(oz):
             assert lse.isnan().all() and loss.isnan().all()
             w[b, 0] = 1
             assert (oz.oz2_linear_xent(x, w, t, scale=scale)[1] == float("inf")).all()
+
+
+@pytest.mark.parametrize("dloss", [1.9999, 1.0, 3.9999 * 2.0 ** -9])
+def test_f16_scale_has_room_for_negative_z_loss(oz, dloss):
+    """1 + 2·z_loss·lse at -1: a certain target's dz is -2·dloss, twice any other's, and stays in
+    f16's range under the scale that the largest dloss gets (one row of w: p is 1)."""
+    x = torch.full((3, 1), 10.0, device="cuda").half()
+    w = torch.ones(1, 1, device="cuda").half()
+    t = torch.zeros(3, dtype=torch.int64, device="cuda")
+    d, lse = torch.full((3,), dloss, device="cuda"), torch.full((3,), 10.0, device="cuda")
+    dx, dw = oz.oz2_linear_xent_grad(d, x, w, t, lse, z_loss=-0.1, dw_dtype=torch.float32)
+    dz = d.double() * 2 * -0.1 * 10
+    assert ((dx[:, 0].double() - dz).abs() <= 2 * ref.U[F16] * dz.abs()).all()
+    want = (dz * 10).sum()
+    assert abs(dw[0, 0].double() - want) <= (ref.U[F16] + 8 * ref.u) * abs(want)
