@@ -524,19 +524,21 @@ constexpr int kListWarps = 16;  // (whose offsets of a group are a sector)
 
 __device__ __forceinline__ float teacher_at(const HeadTargets& t, int64_t row, int i) {
   const int64_t at = row * t.ld_teacher + i;
-  const float v = t.teacher_type == OZ2_TYPE_F32 ? __ldg(static_cast<const float*>(t.teacher) + at)
-                                                 : load16(static_cast<const uint16_t*>(t.teacher) + at,
-                                                          t.teacher_type == OZ2_TYPE_BF16);
-  return v / t.temperature;
+  return t.teacher_type == OZ2_TYPE_F32 ? __ldg(static_cast<const float*>(t.teacher) + at)
+                                        : load16(static_cast<const uint16_t*>(t.teacher) + at,
+                                                 t.teacher_type == OZ2_TYPE_BF16);
 }
-// The listed logits' maximum and the logarithm of their exponentials' sum over it.
+// A logit's distance from the largest one, which is then divided: the type's lowest value over a
+// temperature below 1 would be minus infinity, and a list of nothing else no softmax.
+__device__ __forceinline__ float below(float v, float most, const HeadTargets& t) { return (v - most) / t.temperature; }
+// The listed logits' maximum, and the sum of the exponentials of their distances from it.
 __device__ __forceinline__ void teacher_sums(const HeadTargets& t, int64_t row, int lane, float* top, float* sum) {
   float m = kLowest, s = 0.f;
   for (int i = lane; i < t.top; i += 32)
     if (t.ids[row * t.ld + i] >= 0) m = fmaxf(m, teacher_at(t, row, i));
   m = warp_max(m);
   for (int i = lane; i < t.top; i += 32)
-    if (t.ids[row * t.ld + i] >= 0) s += expf(teacher_at(t, row, i) - m);
+    if (t.ids[row * t.ld + i] >= 0) s += expf(below(teacher_at(t, row, i), m, t));
   *top = m;
   *sum = warp_add(s);
 }
@@ -603,7 +605,7 @@ __global__ void __launch_bounds__(32 * kListWarps)
     bad = __any_sync(0xffffffffu, bad);
     most = warp_max(most);
     for (int i = lane; i < top; i += 32)
-      if (keys[i] != kNone) sum += expf(logits[i] - most);
+      if (keys[i] != kNone) sum += expf(logits[i] = below(logits[i], most, t));
     sum = warp_add(sum);
     if (lane == 0 && there) rows[row] = HeadRow{bad ? __int_as_float(0x7FC00000) : live ? g * terms.scale : 0.f, live ? l : 0.f, 0.f, live};
   }
@@ -628,7 +630,7 @@ __global__ void __launch_bounds__(32 * kListWarps)
     if (key < kBad) {
       const int place = static_cast<int>(key & ((Key(1) << bits) - 1));
       e.x = static_cast<int>(key >> bits);
-      e.y = rows ? __float_as_int(expf(logits[place] - most) / sum) : place;
+      e.y = rows ? __float_as_int(expf(logits[place]) / sum) : place;
     }
     entries[row * top + i] = e;
   }
@@ -745,7 +747,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
       }
       if (id >= 0) {
         live = true;
-        const float log_q = teacher_at(t, mine, i) - top - log_all, weight = expf(log_q);
+        const float log_q = below(teacher_at(t, mine, i), top, t) - log_all, weight = expf(log_q);
         if (weight != 0.f || id >= n) s = fmaf(weight, log_q - z, s);  // (a row that the teacher rules out weighs nothing)
       }
     }

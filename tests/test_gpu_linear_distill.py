@@ -157,3 +157,25 @@ def test_against_differences(oz):
         num, want = loss(*args[0]) - loss(*args[1]), (grad.double() * moved).sum()
         room = 2.0 ** -7 * (grad.double().abs() * moved.abs()).sum() + m * (2.0 ** -7 * 8 * 8) ** 3 / 6 * 1e-2
         assert abs(num - want) < room
+
+
+@pytest.mark.parametrize("teacher_type", [torch.float32, BF16, F16])
+@pytest.mark.parametrize("temperature", [0.5, 1e-3, 3.0])
+def test_lowest_logits_at_any_temperature(oz, teacher_type, temperature):
+    """A list of the teacher's lowest values is even, though they pass FP32's range once divided;
+    beside others they weigh nothing."""
+    g, x, w, ids, _ = inputs(60, 300, 64, 16, BF16, ragged=False)
+    d = torch.ones(60, device="cuda")
+    even = torch.full((60, 16), torch.finfo(teacher_type).min, device="cuda", dtype=teacher_type)
+    got = oz.oz2_linear_distill(x, w, ids, even, temperature=temperature)
+    want = oz.oz2_linear_distill(x, w, ids, torch.zeros_like(even), temperature=temperature)
+    assert got[0].isfinite().all() and all(torch.equal(a, b) for a, b in zip(got, want))
+    a = oz.oz2_linear_distill_grad(d, x, w, ids, even, got[1], temperature=temperature)
+    b = oz.oz2_linear_distill_grad(d, x, w, ids, torch.zeros_like(even), got[1], temperature=temperature)
+    assert all(v.isfinite().all() and torch.equal(v, u) for v, u in zip(a, b))
+    one = even.clone()
+    one[:, 3] = 1
+    sure = torch.full_like(even, -float("inf"))
+    sure[:, 3] = 1
+    got = oz.oz2_linear_distill(x, w, ids, one, temperature=temperature)
+    assert torch.equal(got[0], oz.oz2_linear_distill(x, w, ids, sure, temperature=temperature)[0])
