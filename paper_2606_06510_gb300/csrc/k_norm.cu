@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(ForwardShape<TYPE, TPR, VPT, ALIGNED>::block, 
 }
 
 // Rows too long for registers: a block to a row, which it reads again for each of the
-// two sums and the result (from L2, mostly).
+// two sums and the result (from L2, mostly).  Not as memory that nothing writes: y may be x.
 template <int TYPE>
 __global__ void __launch_bounds__(kNormThreads) norm_long_kernel(NormArgs a) {
   using X = Elem<TYPE>;
@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_long_kernel(NormArgs a) {
       for (int64_t col = static_cast<int64_t>(threadIdx.x) * V; col < a.k; col += kNormThreads * V) {
         const int n = static_cast<int>(min(int64_t(V), a.k - col));
         float x[V];
-        X::unpack(load_piece<false>(src + r * a.ldx + col, src, end, n), x);
+        X::unpack(load_piece<false, false>(src + r * a.ldx + col, src, end, n), x);
         work(col, n, x);
       }
     };

@@ -202,3 +202,20 @@ def test_streams_and_graphs(oz):
     for _ in range(2):
         graph.replay()
         assert torch.equal(y2, y) and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("k", [5, 33, 777, 4097, 8201, 20001])
+def test_in_place_off_the_grid(oz, dt, k):
+    """y over x where the words around a piece hold others' values, of the same row or of the next:
+    rows of their own stride that begin anywhere, and rows without a gap."""
+    g, x, w, b = inputs(203, k, dt, "odd", 1, True, 5)
+    y, mean, rstd = oz.oz2_layer_norm(x, w, b, save_stats=True)
+    for own in (view(x, "odd"), x.contiguous()):
+        got, m2, r2 = oz.oz2_layer_norm(own, w, b, out=own, save_stats=True)
+        assert got is own and torch.equal(own, y) and torch.equal(m2, mean) and torch.equal(r2, rstd)
+    dy, r = (view(torch.randn(203, k, generator=g, device="cuda").to(dt), "odd") for _ in range(2))
+    want = oz.oz2_layer_norm_grad(dy, x, mean, rstd, w, residual=r)
+    for own in (view(r, "odd"), r.contiguous()):
+        got = oz.oz2_layer_norm_grad(dy, x, mean, rstd, w, residual=own, dx=own)
+        assert got[0] is own and all(torch.equal(a, b) for a, b in zip(got, want))
