@@ -48,7 +48,8 @@ int oz2_embedding_grad(int64_t m, int64_t n, int64_t k, int type, const void* d_
  *             its ldx)
  *   d_w, d_b  k values of wtype (`type` or F32), or null: 1 and 0
  *   d_mean, d_rstd  m floats that receive μ and r, or null
- * In FP32, the variance from the deviations.  m = 0 or k = 0: nothing.  eps ≥ 0. */
+ * In FP32, the variance from the deviations.  m = 0: nothing.  k = 0: r and, where centred, μ
+ * are NaN, as the mean of nothing is.  eps ≥ 0. */
 int oz2_layer_norm(int64_t m, int64_t k, int type, const void* d_X, int64_t ldx, const void* d_w, const void* d_b,
                    int wtype, float eps, int center, void* d_Y, int64_t ldy, float* d_mean, float* d_rstd,
                    void* stream);

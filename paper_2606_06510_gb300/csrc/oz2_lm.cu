@@ -272,7 +272,14 @@ int oz2_layer_norm(int64_t m, int64_t k, int type, const void* d_X, int64_t ldx,
   if ((d_w || d_b) && wtype != type && wtype != OZ2_TYPE_F32) return OZ2_ERR_INVALID_ARG;
   if (ldx < std::max<int64_t>(1, k) || ldy < std::max<int64_t>(1, k)) return OZ2_ERR_INVALID_ARG;
   if (too_large(m, k, 0)) return OZ2_ERR_UNSUPPORTED;
-  if (m == 0 || k == 0) return OZ2_OK;
+  if (m == 0) return OZ2_OK;
+  if (k == 0) {
+    if (!on(d_mean, 4) || !on(d_rstd, 4)) return OZ2_ERR_INVALID_ARG;
+    cudaError_t err = cudaSuccess;  // (all bits set: NaN; not centred, μ is 0)
+    if (d_mean) err = cudaMemsetAsync(d_mean, center ? 0xFF : 0, sizeof(float) * m, static_cast<cudaStream_t>(stream));
+    if (d_rstd && err == cudaSuccess) err = cudaMemsetAsync(d_rstd, 0xFF, sizeof(float) * m, static_cast<cudaStream_t>(stream));
+    return status_of(err);
+  }
   if (d_Y == d_X && ldy != ldx && m > 1) return OZ2_ERR_INVALID_ARG;
   const int es = type_bytes(type), wb = type_bytes(wtype);
   if (!d_X || !d_Y || !on(d_X, es) || !on(d_Y, es) || (d_w && !on(d_w, wb)) || (d_b && !on(d_b, wb)) || !on(d_mean, 4) ||

@@ -219,3 +219,16 @@ def test_in_place_off_the_grid(oz, dt, k):
     for own in (view(r, "odd"), r.contiguous()):
         got = oz.oz2_layer_norm_grad(dy, x, mean, rstd, w, residual=own, dx=own)
         assert got[0] is own and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("center", [True, False])
+def test_statistics_of_no_features(oz, center):
+    """They are NaN, not what the memory held before."""
+    x = torch.zeros(3, 0, device="cuda")
+    for _ in range(4):
+        del_me = torch.full((3,), 7.0, device="cuda"), torch.full((3,), 7.0, device="cuda")
+        del del_me
+        y, mean, rstd = oz.oz2_layer_norm(x, center=center, save_stats=True)
+        assert y.shape == (3, 0) and rstd.isnan().all() and (mean.isnan().all() if center else mean is None)
+    dx, dw, db = oz.oz2_layer_norm_grad(x, x, mean, rstd)
+    assert dx.shape == (3, 0) and dw.shape == db.shape == (0,)
