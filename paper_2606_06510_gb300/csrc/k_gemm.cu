@@ -1137,6 +1137,7 @@ struct KernelFact {
   int dev;
   size_t smem;       // dynamic shared memory allowed so far
   int64_t pairs;     // resident two-CTA clusters (0: not asked yet)
+  int cluster;       // blocks of the largest cluster that it may have (0: not asked yet)
 };
 std::mutex g_fact_mu;
 std::vector<KernelFact> g_facts;
@@ -1150,7 +1151,7 @@ int current_device() {
 KernelFact& fact_of(const void* kernel, int dev) {  // with g_fact_mu held
   for (KernelFact& f : g_facts)
     if (f.kernel == kernel && f.dev == dev) return f;
-  g_facts.push_back(KernelFact{kernel, dev, 0, 0});
+  g_facts.push_back(KernelFact{kernel, dev, 0, 0, 0});
   return g_facts.back();
 }
 }  // namespace
@@ -1203,6 +1204,35 @@ int64_t resident_pairs(const void* kernel, int threads, size_t smem) {
     f.pairs = std::min<int64_t>(most, clusters);
   }
   return f.pairs;
+}
+
+int cluster_blocks(const void* kernel, int threads, size_t smem, int most) {
+  const int dev = current_device();
+  std::lock_guard<std::mutex> lk(g_fact_mu);
+  KernelFact& f = fact_of(kernel, dev);
+  if (!f.cluster) {
+    int size = most;
+    for (; size > 1; size /= 2) {  // (clusters of more than 8 blocks are not every device's)
+      cudaError_t err = size > 8 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) : cudaSuccess;
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3(static_cast<unsigned>(size));
+      cfg.blockDim = dim3(static_cast<unsigned>(threads));
+      cfg.dynamicSmemBytes = smem;
+      cudaLaunchAttribute attr;
+      attr.id = cudaLaunchAttributeClusterDimension;
+      attr.val.clusterDim.x = static_cast<unsigned>(size);
+      attr.val.clusterDim.y = 1;
+      attr.val.clusterDim.z = 1;
+      cfg.attrs = &attr;
+      cfg.numAttrs = 1;
+      int clusters = 0;
+      if (err == cudaSuccess) err = cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg);
+      if (err == cudaSuccess && clusters > 0) break;
+      cudaGetLastError();
+    }
+    f.cluster = size;
+  }
+  return f.cluster;
 }
 
 // mode: 0 residues (tensor cores), 1 magnitude (tensor cores),

@@ -121,5 +121,8 @@ cudaError_t allow_smem(const void* kernel, size_t smem);
 // Two-CTA clusters of `kernel` that can be resident at once on the current
 // device (at most half its SMs).
 int64_t resident_pairs(const void* kernel, int threads, size_t smem);
+// The largest cluster of `kernel` of `most` blocks, or a half, a quarter, ... of that, which the
+// current device (or the part of one that the process has) takes; 1 always does.
+int cluster_blocks(const void* kernel, int threads, size_t smem, int most);
 
 }  // namespace oz2

@@ -220,3 +220,18 @@ def test_current_stream_is_used(oz):
         d = oz.oz2_embedding_grad(y, ids, 8)
     s.synchronize()
     assert (y == 2).all() and (d == 2).all()
+
+
+@pytest.mark.parametrize("m", [2048, 2049, 3001, 4096, 8191, 8192, 8193, 16385, 65535, 65537, 140001])
+@pytest.mark.parametrize("n", [3, 700, 70001])
+def test_sorts_of_all_sizes(oz, m, n):
+    """By one block, a cluster of 8 and one of 16; a block's pairs in shared memory (up to 4096) or
+    written where they belong; a warp's stretch held (up to 256) or read twice."""
+    g = rng(m + n)
+    ids = tokens(g, m, n, "zipf" if m % 2 else "even")
+    ids[torch.rand(m, generator=g, device="cuda") < 0.05] = -1
+    dy = torch.randn(m, 24, generator=g, device="cuda")
+    s, e = ref.embedding_grad(dy, ids, n, 1.0, torch.float32)
+    got = oz.oz2_embedding_grad(dy, ids, n)
+    close(got, s, e, "dE")
+    assert torch.equal(got, oz.oz2_embedding_grad(dy, ids, n))
