@@ -6,7 +6,9 @@ Arrays are as in `layers`: row-major (tokens, features) with stride(1) == 1 and 
 row stride, all on the current device.  Tokens name rows by int64 or int32.  A call
 runs on the current stream, or on `stream`, whose memory its new outputs then are.  The
 forward passes record no graph of gradients: tensors that require them are refused
-unless that is off (torch.no_grad()).
+unless that is off (torch.no_grad()).  Nor do the gradients' functions, whose results are
+plain numbers: their x, weights and so on may require gradients, but a dy, dloss or
+residual that does, as on the way to second derivatives, is refused in the same way.
 """
 from __future__ import annotations
 
@@ -56,6 +58,11 @@ _fresh = _EMPTY or _empty
 def _lost(what):
     assert not torch.is_grad_enabled(), f"a tensor requires its gradient, which would be lost: call {what} " \
         f"under torch.no_grad(), and {what}_grad for the gradients"
+
+
+def _lost_twice(what):
+    assert not torch.is_grad_enabled(), f"a gradient requires its gradient, which would be lost: {what} records no " \
+        "graph for second derivatives; call it under torch.no_grad()"
 
 
 def _home(t, what):
@@ -127,6 +134,8 @@ def oz2_embedding_grad(dy, ids, n, scale=1.0, out=None, out_dtype=None, accumula
     each row's tokens, in dy's dtype or float32 (out_dtype).  With accumulate it is added to
     `out`, whose other rows stay; else rows without tokens are zeros.  ids outside [0, n) count
     for nothing."""
+    if dy.requires_grad:
+        _lost_twice("oz2_embedding_grad")
     m, k = dy.shape
     dt = dy.dtype
     assert dt in _FLOATS, "dy: expected float32, bfloat16 or float16"
@@ -201,6 +210,8 @@ def oz2_layer_norm_grad(dy, x, mean, rstd, weight=None, residual=None, need=("dx
     added to dx (which may be given as the same tensor).  `need` names the gradients wanted (the
     others are None).  dx has x's dtype, dweight and dbias (k,) are float32; with accumulate those
     two are added to, and must be given."""
+    if dy.requires_grad or (residual is not None and residual.requires_grad):
+        _lost_twice("oz2_layer_norm_grad")
     m, k = x.shape
     dt = x.dtype
     f32 = _F32
@@ -338,6 +349,8 @@ def oz2_linear_xent_grad(dloss, x, w, targets, lse, scale=1.0, z_loss=0.0, need=
     token, and the lse that it kept.  `need` names the gradients wanted (the others are None).
     dx (m, k) has x's dtype, dw (n, k) that or float32 (dw_dtype); each may be given as the tensor
     to write.  With accumulate, dw (float32) is added to, and must be given."""
+    if dloss.requires_grad:
+        _lost_twice("oz2_linear_xent_grad")
     m, n, k, dt, dev, xp, ldx, wp, ldw = _head(x, w)
     assert targets.dtype in IDS, "targets: expected int64 or int32"
     ip = _vector(targets, m, torch.int64, torch.int32, dev, "targets")
@@ -377,6 +390,8 @@ def oz2_linear_distill(x, w, ids, teacher, temperature=1.0, stream=None):
 def oz2_linear_distill_grad(dloss, x, w, ids, teacher, lse, temperature=1.0, need=("dx", "dw"), dx=None, dw=None,
                             dw_dtype=None, accumulate=False, stream=None):
     """(dx, dw) of oz2_linear_distill, as oz2_linear_xent_grad's."""
+    if dloss.requires_grad:
+        _lost_twice("oz2_linear_distill_grad")
     m, n, k, dt, dev, xp, ldx, wp, ldw = _head(x, w)
     top, listed = _entries(ids, teacher, m, dev)
     lp = _vector(lse, m, torch.float32, torch.float32, dev, "lse")

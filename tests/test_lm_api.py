@@ -226,3 +226,25 @@ def test_a_lost_gradient_is_refused(oz, what):
         call()
     with torch.no_grad(), pytest.raises(AssertionError, match="CUDA"):
         call()
+
+
+@pytest.mark.parametrize("what", ["embedding", "norm", "residual", "xent", "distill"])
+def test_a_second_derivative_is_refused(oz, what):
+    """A gradient that requires its own, before anything else of the call is looked at; x and weights
+    that do are taken, up to the check of their device."""
+    x, w = torch.zeros(4, 8, dtype=torch.bfloat16), torch.zeros(6, 8, dtype=torch.bfloat16)
+    ids, f = torch.zeros(4, dtype=torch.int64), torch.zeros(4)
+    d = torch.zeros(4) if what in ("xent", "distill") else torch.zeros(4, 8, dtype=torch.bfloat16)
+    x.requires_grad_()
+    w.requires_grad_()
+    call = dict(embedding=lambda: oz.oz2_embedding_grad(d, ids, 6), norm=lambda: oz.oz2_layer_norm_grad(d, x, f, f),
+                residual=lambda: oz.oz2_layer_norm_grad(x.detach(), x, f, f, residual=d),
+                xent=lambda: oz.oz2_linear_xent_grad(d, x, w, ids, f),
+                distill=lambda: oz.oz2_linear_distill_grad(d, x, w, ids[:, None], f[:, None], f))[what]
+    with pytest.raises(AssertionError, match="CUDA"):
+        call()
+    d.requires_grad_()
+    with pytest.raises(AssertionError, match="requires its gradient"):
+        call()
+    with torch.no_grad(), pytest.raises(AssertionError, match="CUDA"):
+        call()
