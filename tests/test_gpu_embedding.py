@@ -235,3 +235,48 @@ def test_sorts_of_all_sizes(oz, m, n):
     got = oz.oz2_embedding_grad(dy, ids, n)
     close(got, s, e, "dE")
     assert torch.equal(got, oz.oz2_embedding_grad(dy, ids, n))
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("k,how", [(200, "whole"), (203, "odd"), (264, "whole"), (520, "strided"), (520, "odd"), (777, "odd"),
+                                   (2100, "whole"), (2101, "odd")])
+@pytest.mark.parametrize("kind", ["zipf", "even", "one"])
+def test_several_pieces_a_lane(oz, dt, kind, k, how):
+    """So many tokens that a lane has two or four pieces of a row (from 256 columns of 16 bits on, 128
+    and 256 of 32), of one slice or several; short and long runs, stored and added to."""
+    m, n = 60000, 20000
+    assert (m + 15) // 16 >= 24 * 152
+    g = rng(k)
+    dy = view(torch.randn(m, k, generator=g, device="cuda").to(dt), how)
+    ids = tokens(g, m, n, kind)
+    if kind == "zipf":
+        ids[torch.rand(m, generator=g, device="cuda") < 0.1] = -1
+        ids[m // 2] = n
+    for out in {dt, torch.float32}:
+        s, e = ref.embedding_grad(dy, ids, n, 0.5, out)
+        got = oz.oz2_embedding_grad(dy, ids, n, scale=0.5, out_dtype=out)
+        close(got, s, e, "dE")
+        assert torch.equal(got, oz.oz2_embedding_grad(dy, ids, n, scale=0.5, out_dtype=out))
+        old = view(torch.randn(n, k, generator=g, device="cuda").to(out), how)
+        s, e = ref.embedding_grad(dy, ids, n, 0.5, out, old)
+        oz.oz2_embedding_grad(dy, ids, n, scale=0.5, out=old, accumulate=True)
+        close(old, s, e, "added to")
+
+
+@pytest.mark.parametrize("m", [1, 2, 14, 15, 16, 17, 18, 31, 32, 33, 47, 48, 49, 64, 65, 130, 200])
+@pytest.mark.parametrize("dt,k", [(torch.float32, 72), (torch.bfloat16, 33)])
+def test_runs_around_the_cut_at_any_place(oz, m, dt, k):
+    """Runs as long as those that are cut, and one less and more, starting at every place of a chunk
+    of 16 sorted pairs; what follows brings the tokens over those that are not sorted (256)."""
+    g = rng(m)
+    for lead in list(range(18)) + [30, 31, 32, 33, 40]:
+        ids = torch.cat([torch.zeros(lead, dtype=torch.int64), torch.ones(m, dtype=torch.int64),
+                         torch.full((5,), 2), torch.full((m + 1,), 5), torch.arange(6, 306)]).cuda()
+        assert len(ids) > 256
+        ids = ids[torch.randperm(len(ids), generator=g, device="cuda")]
+        dy = torch.randn(len(ids), k, generator=g, device="cuda").to(dt)
+        s, e = ref.embedding_grad(dy, ids, 306, 1.0, dt)
+        close(oz.oz2_embedding_grad(dy, ids, 306), s, e, f"lead {lead}")
+        old = torch.randn(306, k, generator=g, device="cuda").to(dt)
+        s, e = ref.embedding_grad(dy, ids, 306, 1.0, dt, old)
+        close(oz.oz2_embedding_grad(dy, ids, 306, out=old, accumulate=True), s, e, f"lead {lead}, added to")

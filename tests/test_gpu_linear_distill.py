@@ -179,3 +179,69 @@ def test_lowest_logits_at_any_temperature(oz, teacher_type, temperature):
     sure[:, 3] = 1
     got = oz.oz2_linear_distill(x, w, ids, one, temperature=temperature)
     assert torch.equal(got[0], oz.oz2_linear_distill(x, w, ids, sure, temperature=temperature)[0])
+
+
+@pytest.mark.parametrize("dt", [BF16, F16])
+def test_pieces_of_the_vocabulary(oz, dt):
+    """dz formed in pieces of the vocabulary (three of 23552 rows here), with listed rows on both sides
+    of their borders; dw stored, and added to in float32."""
+    m, n, k, top, T = 9000, 70001, 24, 9, 1.5
+    g, x, w, ids, teacher = inputs(m, n, k, top, dt, repeated=True)
+    ids[:, :top] = torch.randint(0, n, (m, top), generator=g, device="cuda")
+    borders = torch.tensor([0, 23551, 23552, 47103, 47104, 70000], device="cuda")
+    ids[:, 2:5] = borders[torch.randint(0, 6, (m, 3), generator=g, device="cuda")]
+    ids[torch.rand(ids.shape, generator=g, device="cuda") < 0.2] = -1
+    ids[::11] = -1
+    live = (ids >= 0).any(1)
+    loss, lse, picked = oz.oz2_linear_distill(x, w, ids, teacher, temperature=T)
+    d = torch.rand(m, generator=g, device="cuda") / m
+    dx, dw = oz.oz2_linear_distill_grad(d, x, w, ids, teacher, lse, temperature=T, dw_dtype=torch.float32)
+    rows = torch.tensor([0, 1, 5, 4500, 8990, 8999], device="cuda")
+    want, bound = ref.distill(x[rows], w, ids[rows], teacher[rows], T)
+    for a, v, e in zip((loss, lse, picked), want, bound):
+        close(a[rows], v, e)
+    big = float(max(1, d.max() / d[rows].max()))  # (f16's scale is that of all tokens)
+    want, bound = ref.distill_grad(d[rows], x[rows], w, ids[rows], teacher[rows], lse[rows], T)
+    close(dx[rows], want[0], bound[0] * big)
+    # dw of rows of w around the borders: dz's rounding, the logits' error (a depth of 24: 18 steps of
+    # 2^-22), the weights' and the sums' of 9000.
+    cols = torch.cat([torch.arange(a, b) for a, b in ((0, 40), (23500, 23600), (47050, 47160), (69950, 70001))]).cuda()
+    p = torch.exp(x.double() @ w[cols].double().t() / T - lse.double()[:, None])
+    q = ref.teacher(ids, teacher, T, n)[0]
+    hot = torch.zeros(m, n, device="cuda").double().scatter_add_(1, ids.clamp_min(0), q)[:, cols]
+    c = (d.double() / T * live)[:, None]
+    dz, parts = c * (p - hot), c * (p + hot)
+    near = ref.U[dt] + 1e-4 + (m / 16 + 16) * 2.0 ** -22
+    size = dz.abs().t() @ x.double().abs() * near + 2e-4 * (parts.t() @ x.double().abs()) + \
+        2.0 ** -38 * float(d.max()) * x.double().abs().sum(0)
+    close(dw[cols], dz.t() @ x.double(), size)
+    old = torch.randn(n, k, generator=g, device="cuda")
+    sums = old + dw  # (the same sums, then one addition)
+    _, to = oz.oz2_linear_distill_grad(d, x, w, ids, teacher, lse, temperature=T, dw=old, accumulate=True)
+    assert to is old and torch.equal(old, sums)
+    only = oz.oz2_linear_distill_grad(d, x, w, ids, teacher, lse, temperature=T, need=("dx",))
+    close(only[0][rows], want[0], bound[0] * big)
+
+
+def test_long_lists_of_a_large_vocabulary(oz):
+    """Lists whose keys, a row and a place among 1024, take more than 32 bits."""
+    m, n, k, top = 2, 4200000, 8, 1024
+    g = rng(9)
+    w = (torch.randn(n, k, generator=g, device="cuda") / 2).to(BF16)
+    x = torch.randn(m, k, generator=g, device="cuda").to(BF16)
+    ids = torch.randint(0, n, (m, top), generator=g, device="cuda")
+    ids[:, :300] = n - 1 - torch.arange(300, device="cuda")
+    ids[:, 300:310] = torch.arange(10, device="cuda")
+    ids = ids[:, torch.randperm(top, generator=g, device="cuda")].contiguous()
+    ids[1, ::3] = -1
+    teacher = 3 * torch.randn(m, top, generator=g, device="cuda")
+    want, bound = ref.distill(x, w, ids, teacher, 1.0)
+    got = oz.oz2_linear_distill(x, w, ids, teacher)
+    for a, v, e, what in zip(got, want, bound, ("loss", "lse", "picked")):
+        close(a, v, e, what)
+    d = torch.ones(m, device="cuda")
+    lse = want[1].float()
+    want, bound = ref.distill_grad(d, x, w, ids, teacher, lse, 1.0, torch.float32)
+    for a, v, e, what in zip(oz.oz2_linear_distill_grad(d, x, w, ids, teacher, lse, dw_dtype=torch.float32), want, bound,
+                             ("dx", "dw")):
+        close(a, v, e, what)

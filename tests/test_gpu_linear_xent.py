@@ -363,3 +363,21 @@ def test_f16_scale_has_room_for_negative_z_loss(oz, dloss):
     assert ((dx[:, 0].double() - dz).abs() <= 2 * ref.U[F16] * dz.abs()).all()
     want = (dz * 10).sum()
     assert abs(dw[0, 0].double() - want) <= (ref.U[F16] + 8 * ref.u) * abs(want)
+
+
+@pytest.mark.parametrize("how", ["whole", "odd"])
+def test_added_to_over_pieces(oz, how):
+    """dw in float32 added to where dz is formed in pieces of the vocabulary: what is stored, and one
+    addition; what lies beside it stays."""
+    m, n, k = 9000, 70001, 40
+    g, x, w, t = inputs(m, n, k, BF16)
+    lse = oz.oz2_linear_xent(x, w, t)[1]
+    d = torch.rand(m, generator=g, device="cuda") / m
+    dx, dw = oz.oz2_linear_xent_grad(d, x, w, t, lse, dw_dtype=torch.float32)
+    old = view(torch.randn(n, k, generator=g, device="cuda"), how)
+    whole, sums = old._base, old + dw
+    dx2, to = oz.oz2_linear_xent_grad(d, x, w, t, lse, dw=old, accumulate=True)
+    assert to is old and torch.equal(old, sums) and torch.equal(dx, dx2)
+    if how == "odd":
+        old[:] = float("nan")
+        assert whole.isnan().all()
