@@ -72,8 +72,9 @@ int oz2_layer_norm_grad(int64_t m, int64_t k, int type, const void* d_dY, int64_
  *   z = scale·Wᵀ·x      lse = log Σ_j exp z_j      loss = lse - z_target + z_loss·lse²
  *   d_loss, d_lse, d_picked   m floats each: the loss, lse, and the target's logit
  * target < 0: the token does not count, loss and picked are 0, whatever its x is; target ≥ n:
- * loss and picked are NaN.  The logits live on chip, 256 × 256 at a time; the workspace is
- * 8 bytes for 64 of them.  m = 0: nothing.  n < 1: OZ2_ERR_INVALID_ARG.
+ * loss and picked are NaN.  The logits live on chip, 256 × 256 at a time, as powers of two
+ * (scale·log2 e is finite, and a logit beyond 2^127.47, 2.3e38, counts as infinite in lse); the
+ * workspace is 8 bytes for 64 of them.  m = 0: nothing.  n < 1: OZ2_ERR_INVALID_ARG.
  * Operands are copied to rows that TMA can read as by oz2_linear. */
 int oz2_linear_xent(int64_t m, int64_t n, int64_t k, int type, const void* d_X, int64_t ldx, const void* d_W,
                     int64_t ldw, const void* d_targets, int id_bits, float scale, float z_loss, float* d_loss,

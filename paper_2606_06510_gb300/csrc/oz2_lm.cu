@@ -36,7 +36,7 @@ struct HeadCall {
 
 int check_head(const HeadCall& c, int id_bits) {
   if (c.m < 0 || c.n < 0 || c.k < 0 || !is_16bit(c.type) || !valid_ids(id_bits) || c.n < 1) return OZ2_ERR_INVALID_ARG;
-  if (!std::isfinite(c.scale) || !std::isfinite(c.z_loss)) return OZ2_ERR_INVALID_ARG;
+  if (!std::isfinite(c.scale * kLog2E) || !std::isfinite(c.z_loss)) return OZ2_ERR_INVALID_ARG;  // (logits are powers of two)
   if (c.ldx < std::max<int64_t>(1, c.k) || c.ldw < std::max<int64_t>(1, c.k)) return OZ2_ERR_INVALID_ARG;
   if (c.t.soft && (c.t.top < 1 || c.t.top > kMaxTop || c.t.ld < c.t.top || c.t.ld_teacher < c.t.top ||
                    !valid_type(c.t.teacher_type) || !(c.t.temperature > 0)))

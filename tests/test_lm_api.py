@@ -248,3 +248,10 @@ def test_a_second_derivative_is_refused(oz, what):
         call()
     with torch.no_grad(), pytest.raises(AssertionError, match="CUDA"):
         call()
+
+
+def test_scales_that_pass_fp32_in_powers_of_two_are_refused(oz):
+    """scale·log2 e is what multiplies the products: 3e38 is a number, that is not."""
+    assert xent(oz, scale=3e38) == xent(oz, scale=-3e38) == xent_grad(oz, scale=3e38) == -1
+    assert distill(oz, temp=1 / 3e38) == distill_grad(oz, temp=1 / 3e38) == -1
+    assert xent(oz, m=0, scale=2e38) == 0
