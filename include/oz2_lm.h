@@ -36,7 +36,8 @@ int oz2_embedding(int64_t m, int64_t n, int64_t k, int type, const void* d_ids, 
  *   flags     OZ2_GRAD_ACCUMULATE: the sums are added to dE, whose other rows are left
  *             as they are; else rows without tokens become zeros
  * A row's tokens are summed in ascending order, in stretches that depend on the sorted
- * tokens alone.  (F32 sums are added to dE in memory, where a result below 2^-126 counts as 0.) */
+ * tokens alone.  (16-bit rows are added to in FP32 and rounded once; sums for F32 ones are rounded and
+ * then added in memory, where a result below 2^-126 counts as 0.) */
 int oz2_embedding_grad(int64_t m, int64_t n, int64_t k, int type, const void* d_dY, int64_t lddy,
                        const void* d_ids, int id_bits, float scale, void* d_dE, int64_t ldde, int de_type,
                        unsigned flags, void* stream);
@@ -87,10 +88,11 @@ int oz2_linear_xent(int64_t m, int64_t n, int64_t k, int type, const void* d_X, 
  *   d_dX      k×m of `type` (lddx ≥ k), or null: not wanted
  *   d_dW      k×n of dw_type (`type` or F32; lddw ≥ k), or null: not wanted
  *   flags     OZ2_GRAD_ACCUMULATE: dW (F32 only) is added to
- * The logits are formed again, and dz is rounded to `type` (F16: under a power of two that
- * brings the largest dloss into its range, taken out of the sums) in pieces of the vocabulary of
- * at most some 512 MB.  Tokens that do not count have zeros in dX and no part in dW, whatever
- * their x, lse and dloss are; a target ≥ n makes its dX and all of dW NaN. */
+ * The logits are formed again, and dz is rounded to `type`, for dW in F32 too (F16: under a power
+ * of two that brings the largest dloss into its range, taken out of the sums), in pieces of the
+ * vocabulary of at most some 512 MB.  Tokens that do not count have zeros in dX (with W finite: they
+ * are 0·W) and no part in dW, whatever their x, lse and dloss are; a target ≥ n makes its dX and all
+ * of dW NaN. */
 #define OZ2_GRAD_ONE_DLOSS 0x2u
 int oz2_linear_xent_grad(int64_t m, int64_t n, int64_t k, int type, const float* d_dloss, const void* d_X, int64_t ldx,
                          const void* d_W, int64_t ldw, const void* d_targets, int id_bits, const float* d_lse,

@@ -158,6 +158,12 @@ __device__ __forceinline__ void head_sums(const uint32_t (&v0)[32], const uint32
 // differences; its group's two numbers are joined to the others' by head_join_kernel.  Gradient,
 // it turns them into dz, which goes to memory by way of its warp's two KB.
 //
+// Fewer bits: exp2 is the approximate one (2^-22 of the value, a few steps of FP32), and dz is
+// rounded to the operands' 16 bits, the type in which the tensor cores take both sides of a
+// product.  dX and dW then carry that rounding beside their own: 1.4 times the error of one, up to
+// 1.65 where few terms make a sum.  Two 16-bit terms for each dz would take it away and run dX's and
+// dW's products, over half of the gradient's time, twice.
+//
 // What bounds it: the tensor pipes (4096×50257×1024 bf16: 96% of their cycles, 209 µs alone, 238
 // back to back under the power cap; the gradient's 84%, 239 µs, its epilogue being nearly as
 // long as 16 steps of products).  A depth of 128 is all epilogue: 2 µs a tile forward, 4 with dz,

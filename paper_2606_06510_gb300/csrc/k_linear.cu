@@ -106,7 +106,8 @@ __device__ __forceinline__ void fetch_end_slow(const Fetched& f, int lane, uint8
   for (int i = 0; i < 16; ++i)
     *reinterpret_cast<uint32_t*>(value_at(buf, 2 * i + (lane >> 4), 2 * (lane & 15))) = f.v[i];
 }
-// 16 columns of FP32, stored or added to.
+// 16 columns of FP32, stored or added to.  (Added to, a row's load waits for the row before's store:
+// a gradient with a dW of 50257×1024 over 1024 tokens takes 651 µs, 278 where dW is stored.)
 __device__ __noinline__ void store32(const LinUnits& x, void* dst, int64_t ld, int64_t row0, int64_t col0, int lane,
                                         const uint8_t* buf, bool add) {
   float* d = static_cast<float*>(dst);

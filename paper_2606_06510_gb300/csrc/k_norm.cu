@@ -13,8 +13,9 @@ using ForwardKernel = Kernel<void (*)(NormArgs)>;
 // Memory bounds it: 65536×1024 f32 100 µs (5.4 TB/s; a block to each few rows, loaded when it came
 // to them, 254), 16384×4096 bf16 58 (4.7).  Rows over 4096 wait for their two sums: one or two
 // groups an SM, with their weights in shared memory (8192² bf16 62 µs, 4096×16384 62; read again for
-// each row from L2, 84 and 96); rows off the grid for the shifts of their words (16384×777 f16 39,
-// 8 at the copy rate).
+// each row from L2, 84 and 96); rows off the grid are instructions, 2.3 times those of rows on it
+// (shifts, masks and stores by single elements, five times as many): 16384×777 f16 39, at 776 20, 8 at
+// the copy rate.
 // ---------------------------------------------------------------------------
 constexpr int kForwardThreads = 256;
 // Where the weights are: in a thread's registers; of wide rows, whose threads have not enough for

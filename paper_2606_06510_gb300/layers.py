@@ -161,7 +161,8 @@ def oz2_linear_grad(dy, x, w, pre=None, act="none", need=("dx", "dw", "db"), dx=
     `need` names the gradients wanted (the others are None).  dx (m, k) has x's
     dtype, dw (n, k) that or float32, db (n,) float32; each may be given as the
     tensor to write.  With accumulate, dw (float32) and db are added to, and
-    must be given.  The residual's gradient is dy itself.
+    must be given.  The residual's gradient is dy itself.  The results have no graph of
+    gradients of their own, whatever the arguments require.
     """
     m, n = dy.shape
     k = x.shape[1]
